@@ -65,6 +65,11 @@ extern "C" {
 #define SF_CNN8         1          /* wide row = P positions x 8 channels (channels last) */
 #define SF_F32          0
 #define SF_BF16         1
+#define SF_F16          2          /* rows of the packed-row and expert calls below; no model is built in it */
+#define SF_GATE_SOFTMAX        0   /* weight of a picked expert = its softmax over all scores of the row */
+#define SF_GATE_SOFTMAX_PICKED 1   /* ... over the picked scores only */
+#define SF_GATE_SHARE          2   /* ... its share of the picked scores' sum (scores = class probabilities of the fast model) */
+#define SF_MAX_EXPERTS  1024
 
 /* |margin| threshold equivalent to |sigmoid(margin) - 0.5| < 0.2: fp32(ln(0.7/0.3)) */
 #define SF_TAU_MARGIN_DEFAULT 0x1.b1d106p-1f
@@ -303,6 +308,90 @@ void sf_slow_destroy(sf_slow* slow);
  * the error word. */
 int  sf_slow_infer(sf_ctx* ctx, const sf_slow* slow, const void* rows, const uint32_t* n_rows_dev,
                    uint32_t capacity, float* logits_out, uint8_t* label_out, void* stream);
+
+/* ---- rows in 4 bits --------------------------------------------------------- */
+/* Microscaled 4-bit floating point.  32 consecutive values x_i of a row share a scale 2^e, e = max(floor(log2(max|x_i|)) - 2,
+ * -127); value i is kept as x_i * 2^-e rounded to the nearest of 0, .5, 1, 1.5, 2, 3, 4, 6 with its sign (ties to the even
+ * code, beyond 6 to 6).  A block that holds an infinity or a NaN stands for 32 NaNs.  Rows of K values are packed as
+ *   data    uint8[rows][ceil(K/32)*16]  two values a byte, the first in the low half (a row is filled up to whole blocks with zeros)
+ *   scales  one byte e + 127 per block (255 = NaN), in tiles of 128 rows x 4 blocks: tile (r/128)*ceil(K/128) + b/4 has 512
+ *           bytes, its byte (r%32)*16 + (r%128)/32*4 + b%4 belongs to block b of row r
+ * The scales of the blocks that fill a row up to ceil(K/128)*4 are 127 (sf_mx4_quantise writes them; a caller's own must not be
+ * 255); those of rows that fill the last tile are never used.  Both arrays start on 16-byte boundaries.  K <= 2^24.
+ *
+ * sf_mx4_sizes (host): bytes of the two arrays (either out pointer may be NULL). */
+int  sf_mx4_sizes(uint32_t rows, uint32_t K, size_t* data_bytes_out, size_t* scale_bytes_out);
+/* Packs rows of x (dtype SF_F32 | SF_BF16 | SF_F16, row pitch ld >= K elements, n_src rows).  Row r of the output is row r of x or,
+ * with row_ids (nullable, int32[capacity]), row row_ids[r]; an id outside 0..n_src-1 gives a row of zeros, so the flow_of_row
+ * list of sf_expert_sort packs the rows in the experts' order in one pass.  Rows r < min(*n_rows_dev, capacity) are written
+ * (n_rows_dev nullable: capacity rows; a larger count records SF_ERR_CAPACITY), the others left as they were. */
+int  sf_mx4_quantise(sf_ctx* ctx, const void* x, int dtype, uint32_t n_src, uint32_t K, size_t ld, const int32_t* row_ids,
+                     const uint32_t* n_rows_dev, uint32_t capacity, uint8_t* data_out, uint8_t* scales_out, void* stream);
+/* The values that packed rows stand for, rounded to dtype (exact in fp32 and bf16), into out[rows][ld]. */
+int  sf_mx4_unpack(sf_ctx* ctx, const uint8_t* data, const uint8_t* scales, const uint32_t* n_rows_dev, uint32_t capacity, uint32_t K,
+                   int dtype, void* out, size_t ld, void* stream);
+/* out[r][n] = act(sum_k A[r][k] W[n][k] + bias[n]): packed rows (capacity x K, the first *n_rows_dev of them) times packed weights
+ * (N rows of K), products summed in fp32, bias fp32[N] (nullable), act = ReLU if relu != 0, rounded once to out_dtype
+ * (SF_F32 | SF_BF16 | SF_F16), row pitch ld >= N elements.  Rows at or beyond the count are left as they were. */
+int  sf_mx4_matmul(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_scales, const uint32_t* n_rows_dev, uint32_t capacity,
+                   const uint8_t* w, const uint8_t* w_scales, uint32_t N, uint32_t K, const float* bias, int relu,
+                   int out_dtype, void* out, size_t ld, void* stream);
+/* The same with one weight matrix per expert: rows offsets[e] .. offsets[e+1]-1 (DEVICE uint32[E+1], as sf_expert_sort writes them
+ * with an `align` that is a multiple of 128) are multiplied with weights e.  w: E matrices of N packed rows one behind the
+ * other, w_scales: their E scale arrays one behind the other, bias fp32[E][N].  An expert whose first row is not a multiple of
+ * 128 is skipped and SF_ERR_ARG recorded in the error word; rows at or beyond offsets[E] or capacity are left as they were. */
+int  sf_mx4_matmul_experts(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_scales, const uint32_t* offsets, uint32_t E,
+                           uint32_t capacity, const uint8_t* w, const uint8_t* w_scales, uint32_t N, uint32_t K,
+                           const float* bias, int relu, int out_dtype, void* out, size_t ld, void* stream);
+
+/* ---- several slow models: experts -------------------------------------------- */
+/* sf_route assigns a flow to THE slow model; these calls assign it to k of E experts: gate -> sort -> gather (or sf_mx4_quantise
+ * with flow_of_row) -> the experts' layers on their rows (sf_mx4_matmul_experts) -> combine, and the gradients of each for
+ * training.  n = flows the arrays hold; n_dev (nullable, device) = flows present (a larger count is clamped and records
+ * SF_ERR_CAPACITY); what belongs to flows at or beyond it is left as it was.  E <= SF_MAX_EXPERTS, k <= E (where E is
+ * given), n*k < 2^31.  None of them uses the context's workspace, so they may be captured in graphs and run on several streams of
+ * one context at once.  All sums are fp32 in a fixed order; results do not vary from run to run.
+ *
+ * Gate: the k largest of each row's E scores (scores[n][ld]), largest first, ties to the lowest index, into ids_out int32[n][k]
+ * and their weights (SF_GATE_*) into weights_out fp32[n][k].  A score of -infinity or NaN (a masked expert) is never picked and
+ * adds nothing; where fewer than k are left the rest of the row is id -1, weight 0.  SF_GATE_SHARE gives weights 0 where the
+ * picked scores' sum is not positive. */
+int  sf_expert_gate(sf_ctx* ctx, const void* scores, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t E, size_t ld,
+                    uint32_t k, int mode, int32_t* ids_out, float* weights_out, void* stream);
+/* d_scores_out[n][ldd] (same dtype) from the weights' gradient d_weights fp32[n][k]; ids are those that the gate gave. */
+int  sf_expert_gate_backward(sf_ctx* ctx, const void* scores, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t E, size_t ld,
+                             uint32_t k, int mode, const int32_t* ids, const float* d_weights, void* d_scores_out, size_t ldd,
+                             void* stream);
+/* Sorts the pairs (flow f, choice j) by expert ids[f*k+j], stable.  Expert e's rows start at offsets_out[e] (uint32[E+1]), a multiple
+ * of `align` (a power of two <= 65536), and number counts_out[e] (uint32[E]); flow_of_row_out int32[capacity] is the flow of each
+ * row, -1 for rows that only fill a segment up to its aligned end (rows at or beyond offsets_out[E] are left as they were);
+ * row_of_pair_out int32[n][k] is the row of each pair, -1 where the id is outside 0..E-1 or the row would lie at or beyond
+ * `capacity` (offsets and counts are then cut at capacity and SF_ERR_CAPACITY is recorded).  n*k + E*(align-1) rows always
+ * suffice.  workspace: sf_expert_sort_workspace bytes of device memory that no other call uses meanwhile (not needed, may be
+ * NULL, up to 4096 pairs). */
+int  sf_expert_sort_workspace(uint32_t n, uint32_t k, uint32_t E, size_t* bytes_out);
+int  sf_expert_sort(sf_ctx* ctx, const int32_t* ids, const uint32_t* n_dev, uint32_t n, uint32_t k, uint32_t E, uint32_t align,
+                    uint32_t capacity, uint32_t* offsets_out, uint32_t* counts_out, int32_t* flow_of_row_out,
+                    int32_t* row_of_pair_out, void* workspace, size_t workspace_bytes, void* stream);
+/* rows_out[row_of_pair[f][j]] = x[f] for every pair that has a row; rows that only fill a segment become zeros. */
+int  sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t D, size_t ldx, uint32_t k,
+                      const int32_t* row_of_pair, uint32_t E, const uint32_t* offsets, const uint32_t* counts, uint32_t capacity,
+                      void* rows_out, size_t ldr, void* stream);
+/* Its gradient: dx_out[f] = sum over the flow's pairs of d_rows[row_of_pair[f][j]] (a flow without a row gets zeros). */
+int  sf_expert_gather_backward(sf_ctx* ctx, const void* d_rows, int dtype, uint32_t capacity, uint32_t D, size_t ldr,
+                               const int32_t* row_of_pair, const uint32_t* n_dev, uint32_t n, uint32_t k, void* dx_out, size_t ldx,
+                               void* stream);
+/* y_out[f] = sum over j of weights[f][j] * rows[row_of_pair[f][j]] (weights fp32[n][k], NULL = all 1; a pair without a row adds
+ * nothing, whatever its weight). */
+int  sf_expert_combine(sf_ctx* ctx, const void* rows, int dtype, uint32_t capacity, uint32_t D, size_t ldr, const int32_t* row_of_pair,
+                       const float* weights, const uint32_t* n_dev, uint32_t n, uint32_t k, void* y_out, size_t ldy, void* stream);
+/* Its gradients: d_rows_out[row_of_pair[f][j]] = weights[f][j] * dy[f] (rows that only fill a segment become zeros; offsets and
+ * counts are needed for those) and d_weights_out fp32[n][k] = <dy[f], rows[row_of_pair[f][j]]> (0 for a pair without a row).
+ * Either output may be NULL. */
+int  sf_expert_combine_backward(sf_ctx* ctx, const void* dy, int dtype, size_t ldy, const void* rows, uint32_t capacity, uint32_t D,
+                                size_t ldr, const int32_t* row_of_pair, const float* weights, const uint32_t* n_dev, uint32_t n,
+                                uint32_t k, uint32_t E, const uint32_t* offsets, const uint32_t* counts, void* d_rows_out,
+                                size_t ldd, float* d_weights_out, void* stream);
 
 /* ---- S1..S5: the whole cascade on one batch -------------------------------- */
 /* Features of fast_ctx (first N packets) -> fast model -> assignment -> wide rows

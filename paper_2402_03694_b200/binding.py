@@ -21,7 +21,9 @@ SF_NOALLOC_MAX_FLOWS = 4194304
 SF_RF, SF_GBDT, SF_GBDT_MC = 0, 1, 2
 SF_LC_GT, SF_ABSMARGIN_LT, SF_ENTROPY_GT, SF_SOFTMAX_LC_GT = 0, 1, 2, 3
 SF_MLP16, SF_CNN8 = 0, 1
-SF_F32, SF_BF16 = 0, 1
+SF_F32, SF_BF16, SF_F16 = 0, 1, 2
+SF_GATE_SOFTMAX, SF_GATE_SOFTMAX_PICKED, SF_GATE_SHARE = 0, 1, 2
+SF_MAX_EXPERTS = 1024
 SF_TAU_MARGIN_DEFAULT = float.fromhex("0x1.b1d106p-1")
 
 
@@ -85,6 +87,9 @@ EXPORTS = [
     "sf_route_noalloc",
     "sf_universal_thresholds", "sf_universal_thresholds_dev", "sf_per_class_thresholds", "sf_mlp_create", "sf_cnn_create", "sf_slow_destroy", "sf_slow_infer",
     "sf_serve_batch", "sf_serve_batch3", "sf_serve_batch_host", "sf_serve_batch_intermediates",
+    "sf_mx4_sizes", "sf_mx4_quantise", "sf_mx4_unpack", "sf_mx4_matmul", "sf_mx4_matmul_experts",
+    "sf_expert_gate", "sf_expert_gate_backward", "sf_expert_sort_workspace", "sf_expert_sort", "sf_expert_gather",
+    "sf_expert_gather_backward", "sf_expert_combine", "sf_expert_combine_backward",
     "sf_table_create", "sf_table_destroy", "sf_table_ingest", "sf_table_ingest_host", "sf_table_lookup", "sf_table_set_time", "sf_table_sweep", "sf_table_set_pipelined", "sf_table_flush",
 ]
 
@@ -129,6 +134,20 @@ def _lib():
         L.sf_serve_batch3.argtypes = [V, V, V, V, C.POINTER(sf_packets), U32, U32, C.POINTER(sf_packets),
                                       C.POINTER(sf_route_cfg), C.POINTER(sf_route_cfg), V, V, V, V]
         L.sf_serve_batch_intermediates.argtypes = [V] + [C.POINTER(V)] * 7
+        Z = C.c_size_t
+        L.sf_mx4_sizes.argtypes = [U32, U32, C.POINTER(Z), C.POINTER(Z)]
+        L.sf_mx4_quantise.argtypes = [V, V, I, U32, U32, Z, V, V, U32, V, V, V]
+        L.sf_mx4_unpack.argtypes = [V, V, V, V, U32, U32, I, V, Z, V]
+        L.sf_mx4_matmul.argtypes = [V, V, V, V, U32, V, V, U32, U32, V, I, I, V, Z, V]
+        L.sf_mx4_matmul_experts.argtypes = [V, V, V, V, U32, U32, V, V, U32, U32, V, I, I, V, Z, V]
+        L.sf_expert_gate.argtypes = [V, V, I, V, U32, U32, Z, U32, I, V, V, V]
+        L.sf_expert_gate_backward.argtypes = [V, V, I, V, U32, U32, Z, U32, I, V, V, V, Z, V]
+        L.sf_expert_sort_workspace.argtypes = [U32, U32, U32, C.POINTER(Z)]
+        L.sf_expert_sort.argtypes = [V, V, V, U32, U32, U32, U32, U32, V, V, V, V, V, Z, V]
+        L.sf_expert_gather.argtypes = [V, V, I, V, U32, U32, Z, U32, V, U32, V, V, U32, V, Z, V]
+        L.sf_expert_gather_backward.argtypes = [V, V, I, U32, U32, Z, V, V, U32, U32, V, Z, V]
+        L.sf_expert_combine.argtypes = [V, V, I, U32, U32, Z, V, V, V, U32, U32, V, Z, V]
+        L.sf_expert_combine_backward.argtypes = [V, V, I, Z, V, U32, U32, Z, V, V, V, U32, U32, U32, V, V, V, Z, V, V]
         L.sf_table_create.argtypes = [V, U32, U32, U32, U32, C.POINTER(V)]
         L.sf_table_ingest.argtypes = [V, V, C.POINTER(sf_pkt_batch), V, U32, V, C.POINTER(sf_route_cfg), V, V]
         L.sf_table_ingest_host.argtypes = L.sf_table_ingest.argtypes
@@ -345,6 +364,185 @@ def sf_serve_batch_intermediates(ctx):
     _check(_lib().sf_serve_batch_intermediates(ctx, *[C.byref(p) for p in ptrs]), "sf_serve_batch_intermediates")
     names = ("feat", "fast_out", "esc_ids", "rows", "logits", "label_fast", "label_slow")
     return {k: p.value for k, p in zip(names, ptrs)}
+
+
+# ---- rows in 4 bits, experts: device tensors in, sizes and pitches taken from them ----------------------------------------
+# Unlike the calls above these take their sizes from the tensors, so they look at them first: a wrong type, shape, stride or a
+# tensor in host memory raises SfError(SF_ERR_ARG) before anything is launched.
+
+def _arg(ok, where):
+    if not ok:
+        raise SfError(SF_ERR_ARG, where)
+
+
+_TYPES = {}
+
+
+def _rows(t, where):
+    """(address, dtype code, rows, columns, row pitch) of a 2-D device tensor whose rows are contiguous."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16})
+    code = _TYPES.get(t.dtype)
+    _arg(code is not None and t.is_cuda and t.dim() == 2, where)
+    n, d = t.shape
+    s0, s1 = t.stride()
+    _arg((d <= 1 or s1 == 1) and (n <= 1 or s0 >= d), where)
+    return t.data_ptr(), code, n, d, (s0 if n > 1 else d)
+
+
+def _flat(t, count, size, where):
+    """Address of a contiguous device tensor of at least `count` elements of `size` bytes; None stays None."""
+    if t is None:
+        return None
+    _arg(t.is_cuda and t.is_contiguous() and t.numel() >= count and t.element_size() == size, where)
+    return t.data_ptr()
+
+
+def _whole(t, shape, where):
+    """Address of a contiguous 4-byte device tensor of this shape."""
+    _arg(t.is_cuda and t.is_contiguous() and t.element_size() == 4 and tuple(t.shape) == shape, where)
+    return t.data_ptr()
+
+
+def _mx4_bytes(rows, K):
+    return -(-K // 32) * 16, -(-rows // 128) * (-(-K // 128)) * 512
+
+
+def sf_mx4_sizes(rows, K):
+    """(data bytes, scale bytes) of `rows` packed rows of K values."""
+    d, s = C.c_size_t(), C.c_size_t()
+    _check(_lib().sf_mx4_sizes(rows, K, C.byref(d), C.byref(s)), "sf_mx4_sizes")
+    return d.value, s.value
+
+
+def sf_mx4_quantise(ctx, x, data_out, scales_out, row_ids=None, n_rows_dev=None, stream=None):
+    """Packs x[rows][K]; with row_ids (int32 device tensor) output row r is x[row_ids[r]]."""
+    w = "sf_mx4_quantise"
+    p, dt, n, K, ld = _rows(x, w)
+    m = n if row_ids is None else row_ids.numel()
+    pitch, sb = _mx4_bytes(m, K)
+    _check(_lib().sf_mx4_quantise(ctx, p, dt, n, K, ld, _flat(row_ids, m, 4, w), _flat(n_rows_dev, 1, 4, w), m,
+                                  _flat(data_out, m * pitch, 1, w), _flat(scales_out, sb, 1, w), _stream(stream)), w)
+
+
+def sf_mx4_unpack(ctx, data, scales, out, n_rows_dev=None, stream=None):
+    w = "sf_mx4_unpack"
+    p, dt, n, K, ld = _rows(out, w)
+    pitch, sb = _mx4_bytes(n, K)
+    _check(_lib().sf_mx4_unpack(ctx, _flat(data, n * pitch, 1, w), _flat(scales, sb, 1, w), _flat(n_rows_dev, 1, 4, w), n, K, dt, p, ld,
+                                _stream(stream)), w)
+
+
+def sf_mx4_matmul(ctx, a, a_scales, w, w_scales, K, out, bias=None, relu=False, n_rows_dev=None, stream=None):
+    """out[rows][N] = act(A W^T + bias); A and W packed rows of K values, out bf16, fp16 or fp32."""
+    s = "sf_mx4_matmul"
+    p, dt, n, N, ld = _rows(out, s)
+    pitch, ab = _mx4_bytes(n, K)
+    _check(_lib().sf_mx4_matmul(ctx, _flat(a, n * pitch, 1, s), _flat(a_scales, ab, 1, s), _flat(n_rows_dev, 1, 4, s), n,
+                                _flat(w, N * pitch, 1, s), _flat(w_scales, _mx4_bytes(N, K)[1], 1, s), N, K, _flat(bias, N, 4, s),
+                                int(relu), dt, p, ld, _stream(stream)), s)
+
+
+def sf_mx4_matmul_experts(ctx, a, a_scales, w, w_scales, K, offsets, out, bias=None, relu=False, stream=None):
+    """The same over rows sorted by expert: offsets [E + 1] (device), w, w_scales and bias of the E experts one behind the other."""
+    s = "sf_mx4_matmul_experts"
+    p, dt, n, N, ld = _rows(out, s)
+    E = offsets.numel() - 1
+    _arg(E >= 1, s)
+    pitch, ab = _mx4_bytes(n, K)
+    _check(_lib().sf_mx4_matmul_experts(ctx, _flat(a, n * pitch, 1, s), _flat(a_scales, ab, 1, s), _flat(offsets, E + 1, 4, s), E, n,
+                                        _flat(w, E * N * pitch, 1, s), _flat(w_scales, E * _mx4_bytes(N, K)[1], 1, s), N, K,
+                                        _flat(bias, E * N, 4, s), int(relu), dt, p, ld, _stream(stream)), s)
+
+
+def sf_expert_gate(ctx, scores, mode, ids_out, weights_out, n_dev=None, stream=None):
+    """ids_out int32 [n][k], weights_out float32 [n][k] from scores [n][E]."""
+    w = "sf_expert_gate"
+    p, dt, n, E, ld = _rows(scores, w)
+    _arg(ids_out.dim() == 2, w)
+    k = ids_out.shape[1]
+    _check(_lib().sf_expert_gate(ctx, p, dt, _flat(n_dev, 1, 4, w), n, E, ld, k, mode, _whole(ids_out, (n, k), w),
+                                 _whole(weights_out, (n, k), w), _stream(stream)), w)
+
+
+def sf_expert_gate_backward(ctx, scores, mode, ids, d_weights, d_scores_out, n_dev=None, stream=None):
+    w = "sf_expert_gate_backward"
+    p, dt, n, E, ld = _rows(scores, w)
+    q, dq, m, F, ldd = _rows(d_scores_out, w)
+    _arg(dq == dt and m == n and F == E and ids.dim() == 2, w)
+    k = ids.shape[1]
+    _check(_lib().sf_expert_gate_backward(ctx, p, dt, _flat(n_dev, 1, 4, w), n, E, ld, k, mode, _whole(ids, (n, k), w),
+                                          _whole(d_weights, (n, k), w), q, ldd, _stream(stream)), w)
+
+
+def sf_expert_sort_workspace(n, k, E):
+    """Bytes of device scratch that sorting n * k pairs over E experts needs at most."""
+    b = C.c_size_t()
+    _check(_lib().sf_expert_sort_workspace(n, k, E, C.byref(b)), "sf_expert_sort_workspace")
+    return b.value
+
+
+def sf_expert_sort(ctx, ids, E, align, offsets_out, counts_out, flow_of_row_out, row_of_pair_out, workspace=None, n_dev=None, stream=None):
+    """ids int32 [n][k]; capacity = flow_of_row_out's length."""
+    w = "sf_expert_sort"
+    _arg(ids.dim() == 2, w)
+    n, k = ids.shape
+    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _arg(workspace is None or (workspace.is_cuda and workspace.is_contiguous()), w)
+    cap = flow_of_row_out.numel()
+    _check(_lib().sf_expert_sort(ctx, _whole(ids, (n, k), w), _flat(n_dev, 1, 4, w), n, k, E, align, cap, _flat(offsets_out, E + 1, 4, w),
+                                 _flat(counts_out, E, 4, w), _flat(flow_of_row_out, cap, 4, w), _whole(row_of_pair_out, (n, k), w),
+                                 _dp(workspace), wb, _stream(stream)), w)
+
+
+def sf_expert_gather(ctx, x, row_of_pair, offsets, counts, rows_out, n_dev=None, stream=None):
+    """rows_out [capacity][D] from x [n][D] by row_of_pair int32 [n][k]."""
+    w = "sf_expert_gather"
+    p, dt, n, D, ld = _rows(x, w)
+    q, dq, cap, F, ldr = _rows(rows_out, w)
+    E = counts.numel()
+    _arg(dq == dt and F == D and row_of_pair.dim() == 2, w)
+    k = row_of_pair.shape[1]
+    _check(_lib().sf_expert_gather(ctx, p, dt, _flat(n_dev, 1, 4, w), n, D, ld, k, _whole(row_of_pair, (n, k), w), E,
+                                   _flat(offsets, E + 1, 4, w), _flat(counts, E, 4, w), cap, q, ldr, _stream(stream)), w)
+
+
+def _pairs_of(rows, row_of_pair, y, w):
+    p, dt, cap, D, ldr = _rows(rows, w)
+    q, dq, n, F, ldy = _rows(y, w)
+    _arg(dq == dt and F == D and row_of_pair.dim() == 2, w)
+    k = row_of_pair.shape[1]
+    return p, dt, cap, D, ldr, _whole(row_of_pair, (n, k), w), q, n, k, ldy
+
+
+def sf_expert_gather_backward(ctx, d_rows, row_of_pair, dx_out, n_dev=None, stream=None):
+    w = "sf_expert_gather_backward"
+    p, dt, cap, D, ldr, at, q, n, k, ldx = _pairs_of(d_rows, row_of_pair, dx_out, w)
+    _check(_lib().sf_expert_gather_backward(ctx, p, dt, cap, D, ldr, at, _flat(n_dev, 1, 4, w), n, k, q, ldx, _stream(stream)), w)
+
+
+def sf_expert_combine(ctx, rows, row_of_pair, weights, y_out, n_dev=None, stream=None):
+    """weights float32 [n][k] or None (all 1)."""
+    w = "sf_expert_combine"
+    p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, y_out, w)
+    g = None if weights is None else _whole(weights, (n, k), w)
+    _check(_lib().sf_expert_combine(ctx, p, dt, cap, D, ldr, at, g, _flat(n_dev, 1, 4, w), n, k, q, ldy, _stream(stream)), w)
+
+
+def sf_expert_combine_backward(ctx, dy, rows, row_of_pair, weights, offsets, counts, d_rows_out, d_weights_out, n_dev=None, stream=None):
+    """Either output may be None."""
+    w = "sf_expert_combine_backward"
+    p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, dy, w)
+    g = None if weights is None else _whole(weights, (n, k), w)
+    E = counts.numel()
+    r, ldd = None, 0
+    if d_rows_out is not None:
+        r, dr, c2, D2, ldd = _rows(d_rows_out, w)
+        _arg((dr, c2, D2) == (dt, cap, D), w)
+    dw = None if d_weights_out is None else _whole(d_weights_out, (n, k), w)
+    _check(_lib().sf_expert_combine_backward(ctx, q, dt, ldy, p, cap, D, ldr, at, g, _flat(n_dev, 1, 4, w), n, k, E,
+                                             _flat(offsets, E + 1, 4, w), _flat(counts, E, 4, w), r, ldd, dw, _stream(stream)), w)
 
 
 def sf_table_create(ctx, log2_slots, fast_pkts, slow_pkts, slow_slabs):

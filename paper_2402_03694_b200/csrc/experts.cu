@@ -1,0 +1,590 @@
+// A slow model made of experts: the gate (which experts a flow goes to and with what weights), the (flow, expert) pairs
+// sorted by expert, the rows brought into that order and the experts' rows added back, each with its gradient.
+//
+// Everything is deterministic: the sort is stable (pairs of one expert keep the order of their flows), sums run in a fixed order.
+#include "rows_common.cuh"
+#include <algorithm>
+
+namespace {
+using namespace sfrow;
+
+constexpr uint32_t kThreads = 256;
+constexpr uint32_t kWarps = kThreads / 32;
+
+// ---- gate ------------------------------------------------------------------------------------------------------
+// LPR lanes share a row, V scores each (consecutive, LPR * V >= E).  Bound: HBM where a row fills its lanes; the scores are read
+// once and stay in registers over the k rounds of "largest that is left, lowest index first".
+constexpr float kNegInf = -__builtin_huge_valf();
+
+template <typename T, int LPR, int V, bool ALIGNED>
+__device__ __forceinline__ void load_scores(const T* __restrict__ p, uint32_t E, uint32_t first, float (&s)[V]) {
+    if (ALIGNED && first + V <= E) {
+        load_f32<T, V, ALIGNED && (V * sizeof(T)) % 16 == 0>(p + first, s);
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; v++) s[v] = first + v < E ? to_f32(p[first + v]) : kNegInf;
+    }
+#pragma unroll
+    for (int v = 0; v < V; v++) s[v] = s[v] > kNegInf ? s[v] : kNegInf;          // a NaN is never picked and adds nothing
+}
+// exp(s - m) with the largest score (an infinite one too) at 1 and masked ones at 0
+__device__ __forceinline__ float near_top(float s, float m) { return s == kNegInf ? 0.0f : (s == m ? 1.0f : expf(s - m)); }
+
+template <int LPR> __device__ __forceinline__ float sum_lanes(float v) {
+#pragma unroll
+    for (int o = LPR / 2; o >= 1; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+template <int LPR> __device__ __forceinline__ float max_lanes(float v) {
+#pragma unroll
+    for (int o = LPR / 2; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    return v;
+}
+
+template <typename T, int LPR, int V, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads)
+gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t E, size_t ld, uint32_t k, int mode,
+            int32_t* __restrict__ ids, float* __restrict__ weights, sf_dev_state* st)
+{
+    sf_chain_enter();
+    const uint32_t rows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
+    const uint32_t lane = threadIdx.x & (LPR - 1);
+    constexpr uint32_t kPer = kThreads / LPR;          // rows of a block at a time
+    // (the loop runs the same number of times in every lane of a warp: the shuffles need them all)
+    for (uint64_t base = (uint64_t)blockIdx.x * kPer; base < rows; base += (uint64_t)gridDim.x * kPer) {
+        const uint64_t row = base + threadIdx.x / LPR;
+        const bool live = row < rows;
+        float s[V];
+        load_scores<T, LPR, V, ALIGNED>(scores + (live ? row : base) * ld, E, lane * V, s);
+        float left[V];
+#pragma unroll
+        for (int v = 0; v < V; v++) left[v] = s[v];
+        float best_s[V]; int best_id[V];               // the picks of rounds j with j % LPR == lane
+        float m = 0.0f, total = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; v++) { best_s[v] = kNegInf; best_id[v] = -1; }
+        for (uint32_t j = 0; j < k; j++) {
+            float b = kNegInf; int id = 0x7FFFFFFF;
+#pragma unroll
+            for (int v = 0; v < V; v++) if (left[v] > b) { b = left[v]; id = (int)(lane * V) + v; }
+#pragma unroll
+            for (int o = LPR / 2; o >= 1; o >>= 1) {
+                const float ob = __shfl_xor_sync(0xFFFFFFFFu, b, o);
+                const int oid = __shfl_xor_sync(0xFFFFFFFFu, id, o);
+                if (ob > b || (ob == b && oid < id)) { b = ob; id = oid; }
+            }
+            if (b == kNegInf) id = -1;
+            if (j == 0) m = b;
+#pragma unroll
+            for (int v = 0; v < V; v++) {
+                if (id == (int)(lane * V) + v) left[v] = kNegInf;
+                if (j == (uint32_t)v * LPR + lane) { best_s[v] = b; best_id[v] = id; }
+            }
+            if (id >= 0) total += mode == SF_GATE_SHARE ? b : near_top(b, m);
+        }
+        if (mode == SF_GATE_SOFTMAX) {
+            float t = 0.0f;
+#pragma unroll
+            for (int v = 0; v < V; v++) t += near_top(s[v], m);
+            total = sum_lanes<LPR>(t);
+        }
+        if (live) {
+#pragma unroll
+            for (int v = 0; v < V; v++) {
+                const uint32_t j = v * LPR + lane;
+                if (j < k) {
+                    const float top = mode == SF_GATE_SHARE ? best_s[v] : near_top(best_s[v], m);
+                    ids[row * k + j] = best_id[v];
+                    weights[row * k + j] = best_id[v] >= 0 && total > 0.0f ? top / total : 0.0f;
+                }
+            }
+        }
+    }
+}
+
+// With p the weights' softmax (over all experts, or over the picked ones) and g the weights' gradient at the picked experts:
+// d_s = p (g - sum g p); for shares d_s = (g - sum g w) / sum s at the picked experts.
+template <typename T, int LPR, int V, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads)
+gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t E, size_t ld, uint32_t k,
+                     int mode, const int32_t* __restrict__ ids, const float* __restrict__ d_weights, T* __restrict__ d_scores, size_t ldd,
+                     sf_dev_state* st)
+{
+    sf_chain_enter();
+    const uint32_t rows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
+    const uint32_t lane = threadIdx.x & (LPR - 1);
+    constexpr uint32_t kPer = kThreads / LPR;
+    for (uint64_t base = (uint64_t)blockIdx.x * kPer; base < rows; base += (uint64_t)gridDim.x * kPer) {
+        const uint64_t row = base + threadIdx.x / LPR;
+        const bool live = row < rows;
+        const uint64_t at = live ? row : base;
+        float s[V], g[V];
+        load_scores<T, LPR, V, ALIGNED>(scores + at * ld, E, lane * V, s);
+        bool picked[V];
+#pragma unroll
+        for (int v = 0; v < V; v++) { g[v] = 0.0f; picked[v] = false; }
+        for (uint32_t j = 0; j < k; j++) {
+            const int id = ids[at * k + j];
+            const float gj = d_weights[at * k + j];
+#pragma unroll
+            for (int v = 0; v < V; v++) if (id == (int)(lane * V) + v && s[v] > kNegInf) { g[v] += gj; picked[v] = true; }
+        }
+        float m = kNegInf;
+#pragma unroll
+        for (int v = 0; v < V; v++) m = fmaxf(m, s[v]);
+        m = max_lanes<LPR>(m);
+        float p[V], t = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            p[v] = mode == SF_GATE_SHARE ? (picked[v] ? s[v] : 0.0f) : (mode == SF_GATE_SOFTMAX || picked[v] ? near_top(s[v], m) : 0.0f);
+            t += p[v];
+        }
+        t = sum_lanes<LPR>(t);
+        float dot = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; v++) { p[v] = t > 0.0f ? p[v] / t : 0.0f; if (picked[v]) dot += g[v] * p[v]; }
+        dot = sum_lanes<LPR>(dot);
+        if (!live) continue;
+        float d[V];
+#pragma unroll
+        for (int v = 0; v < V; v++) d[v] = mode == SF_GATE_SHARE ? (picked[v] && t > 0.0f ? (g[v] - dot) / t : 0.0f) : (p[v] != 0.0f ? p[v] * (g[v] - dot) : 0.0f);
+        T* q = d_scores + row * ldd;
+        const uint32_t first = lane * V;
+        if (ALIGNED && first + V <= E) store_f32<T, V, ALIGNED && (V * sizeof(T)) % 16 == 0>(q + first, d);
+        else {
+#pragma unroll
+            for (int v = 0; v < V; v++) if (first + v < E) q[first + v] = from_f32<T>(d[v]);
+        }
+    }
+}
+
+// calls f with the lanes and values per row that fit E: four scores a lane up to 128 experts
+template <typename F> int by_experts(uint32_t E, F f) {
+    using std::integral_constant;
+    if (E <= 4) return f(integral_constant<int, 1>(), integral_constant<int, 4>());
+    if (E <= 8) return f(integral_constant<int, 2>(), integral_constant<int, 4>());
+    if (E <= 16) return f(integral_constant<int, 4>(), integral_constant<int, 4>());
+    if (E <= 32) return f(integral_constant<int, 8>(), integral_constant<int, 4>());
+    if (E <= 64) return f(integral_constant<int, 16>(), integral_constant<int, 4>());
+    if (E <= 128) return f(integral_constant<int, 32>(), integral_constant<int, 4>());
+    if (E <= 256) return f(integral_constant<int, 32>(), integral_constant<int, 8>());
+    return f(integral_constant<int, 32>(), integral_constant<int, 32>());
+}
+
+// ---- sort --------------------------------------------------------------------------------------------------------
+// The pairs are cut into as many tiles as blocks run at once; a tile's warps take consecutive pieces of it.  Launch 1 counts each
+// tile's pairs per expert; in launch 2 every block adds up the tiles before its own (tiles x E words, read from L2), turns the
+// totals into aligned segment offsets and places its pairs: rank within the warp by match_any, running positions per warp
+// and expert in shared memory.  A batch of one tile needs launch 2 alone.
+struct sort_args {
+    const int32_t* ids; const uint32_t* n_dev; uint32_t n, k, E, align, capacity, tiles;
+    uint32_t* hist;                                       // [tiles][E]
+    uint32_t* offsets; uint32_t* counts; int32_t* flow_of_row; int32_t* row_of_pair;
+};
+constexpr uint32_t kOneTile = 4096;                       // pairs that one block sorts alone
+
+__device__ __forceinline__ void sort_piece(const sort_args& a, uint64_t pairs, uint32_t tile, uint32_t warp, uint64_t& lo, uint64_t& hi) {
+    const uint64_t per_tile = ((pairs + a.tiles - 1) / a.tiles + kWarps * 32 - 1) / (kWarps * 32) * (kWarps * 32);
+    const uint64_t per_warp = per_tile / kWarps;
+    lo = min(pairs, per_tile * tile + per_warp * warp);
+    hi = min(pairs, lo + per_warp);
+}
+
+// counts of this block's pairs per warp and expert -> shared memory [kWarps][E]
+__device__ __forceinline__ void sort_count(const sort_args& a, uint64_t pairs, uint32_t* mine) {
+    for (uint32_t i = threadIdx.x; i < kWarps * a.E; i += kThreads) mine[i] = 0;
+    __syncthreads();
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint64_t lo, hi;
+    sort_piece(a, pairs, blockIdx.x, warp, lo, hi);
+    for (uint64_t i = lo + lane; i < hi; i += 32) {
+        const uint32_t e = (uint32_t)a.ids[i];
+        if (e < a.E) atomicAdd(&mine[warp * a.E + e], 1u);
+    }
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(kThreads)
+sort_count_kernel(const sort_args a, sf_dev_state* st)
+{
+    extern __shared__ uint32_t sm[];
+    sf_chain_enter();
+    const uint64_t pairs = (uint64_t)(a.n_dev ? sf_clamp_rows(*a.n_dev, a.n, st) : a.n) * a.k;
+    sort_count(a, pairs, sm);
+    for (uint32_t e = threadIdx.x; e < a.E; e += kThreads) {
+        uint32_t t = 0;
+        for (uint32_t w = 0; w < kWarps; w++) t += sm[w * a.E + e];
+        a.hist[(size_t)blockIdx.x * a.E + e] = t;
+    }
+}
+
+__global__ void __launch_bounds__(kThreads)
+sort_place_kernel(const sort_args a, sf_dev_state* st)
+{
+    extern __shared__ uint32_t sm[];
+    uint32_t* mine = sm;                                  // [kWarps][E]: counts, then the next position of each warp and expert
+    uint32_t* total = sm + kWarps * a.E;                  // [E]: pairs of the whole batch
+    uint32_t* before = total + a.E;                       // [E]: pairs in the tiles before this one
+    uint32_t* first = before + a.E;                       // [E + 1]: segment offsets
+    sf_chain_enter();
+    const uint64_t pairs = (uint64_t)(a.n_dev ? sf_clamp_rows(*a.n_dev, a.n, st) : a.n) * a.k;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    sort_count(a, pairs, mine);
+    for (uint32_t e = threadIdx.x; e < a.E; e += kThreads) {
+        uint32_t t = 0, b = 0;
+        if (a.tiles == 1) {
+            for (uint32_t w = 0; w < kWarps; w++) t += mine[w * a.E + e];
+        } else {
+            for (uint32_t i = 0; i < a.tiles; i++) {
+                const uint32_t h = __ldcg(a.hist + (size_t)i * a.E + e);
+                if (i < blockIdx.x) b += h;
+                t += h;
+            }
+        }
+        total[e] = t; before[e] = b;
+    }
+    __syncthreads();
+    if (warp == 0) {                                      // exclusive sum of the aligned segment sizes
+        uint32_t run = 0;
+        for (uint32_t e0 = 0; e0 < a.E; e0 += 32) {
+            const uint32_t e = e0 + lane;
+            const uint32_t size = e < a.E ? (total[e] + a.align - 1) / a.align * a.align : 0;
+            uint32_t s = size;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(0xFFFFFFFFu, s, o); if (lane >= (uint32_t)o) s += u; }
+            if (e < a.E) first[e] = run + s - size;
+            run += __shfl_sync(0xFFFFFFFFu, s, 31);
+        }
+        if (lane == 0) first[a.E] = run;
+    }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < a.E; e += kThreads) {
+        uint32_t run = first[e] + before[e];
+        for (uint32_t w = 0; w < kWarps; w++) { const uint32_t c = mine[w * a.E + e]; mine[w * a.E + e] = run; run += c; }
+    }
+    if (blockIdx.x == 0) {
+        for (uint32_t e = threadIdx.x; e <= a.E; e += kThreads) {
+            a.offsets[e] = min(first[e], a.capacity);
+            if (e < a.E) a.counts[e] = min(total[e], a.capacity - min(first[e], a.capacity));
+        }
+        if (threadIdx.x == 0) {
+            bool over = false;
+            for (uint32_t e = 0; e < a.E; e++) over |= first[e] + total[e] > a.capacity;
+            if (over) sf_dev_set_error(st, SF_ERR_CAPACITY);
+        }
+    }
+    // rows that only fill a segment up to its aligned end
+    for (uint32_t e = blockIdx.x; e < a.E; e += gridDim.x)
+        for (uint32_t r = first[e] + total[e] + threadIdx.x; r < min(first[e + 1], a.capacity); r += kThreads) a.flow_of_row[r] = -1;
+    __syncthreads();
+    uint64_t lo, hi;
+    sort_piece(a, pairs, blockIdx.x, warp, lo, hi);
+    uint32_t* next = mine + warp * a.E;
+    for (uint64_t i0 = lo; i0 < hi; i0 += 32) {
+        const uint64_t i = i0 + lane;
+        const uint32_t e = i < hi ? (uint32_t)a.ids[i] : 0xFFFFFFFFu;
+        const bool real = e < a.E;
+        const uint32_t same = __match_any_sync(0xFFFFFFFFu, real ? e : 0xFFFFFFFFu);
+        uint32_t row = 0xFFFFFFFFu;
+        if (real) row = next[e] + __popc(same & ((1u << lane) - 1u));
+        __syncwarp();
+        if (real && (same >> lane) == 1u) next[e] = row + 1;          // the last lane of its expert
+        __syncwarp();
+        const bool kept = real && row < a.capacity;
+        if (i < hi) a.row_of_pair[i] = kept ? (int32_t)row : -1;
+        if (kept) a.flow_of_row[row] = (int32_t)(i / a.k);
+    }
+}
+
+uint32_t sort_tiles(const sf_ctx* ctx, uint32_t n, uint32_t k) {
+    const uint64_t pairs = (uint64_t)n * k;
+    if (pairs <= kOneTile) return 1;
+    return (uint32_t)std::min<uint64_t>((uint64_t)ctx->num_sms, (pairs + 1023) / 1024);
+}
+
+// ---- rows into the experts' order and back -------------------------------------------------------------------------------
+// Units of U bytes (16 where base, pitch and width allow, else one element).  A group of lanes (a power of two up to 32) shares a
+// flow: its row is read once and written k times.  Bound: HBM.
+template <typename Q>
+__global__ void __launch_bounds__(kThreads)
+gather_kernel(const Q* __restrict__ x, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t units, size_t ldx, uint32_t k,
+              const int32_t* __restrict__ row_of_pair, uint32_t E, const uint32_t* __restrict__ offsets, const uint32_t* __restrict__ counts,
+              uint32_t capacity, Q* __restrict__ rows, size_t ldr, uint32_t lanes, uint32_t flow_blocks, sf_dev_state* st)
+{
+    sf_chain_enter();
+    if (blockIdx.x >= flow_blocks) {                      // the rows that only fill a segment: zeros
+        for (uint32_t e = blockIdx.x - flow_blocks; e < E; e += gridDim.x - flow_blocks) {
+            const uint32_t lo = min(offsets[e] + counts[e], capacity), hi = min(offsets[e + 1], capacity);
+            if (lo >= hi) continue;
+            const uint64_t all = (uint64_t)(hi - lo) * units;
+            for (uint64_t i = threadIdx.x; i < all; i += kThreads) {
+                const uint32_t r = (uint32_t)(i / units), c = (uint32_t)(i - (uint64_t)r * units);
+                rows[(size_t)(lo + r) * ldr + c] = Q{};
+            }
+        }
+        return;
+    }
+    const uint32_t flows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
+    const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1);
+    for (uint64_t f = (uint64_t)blockIdx.x * per + threadIdx.x / lanes; f < flows; f += (uint64_t)flow_blocks * per) {
+        const Q* src = x + f * ldx;
+        for (uint32_t c = lane; c < units; c += 4 * lanes) {
+            Q q[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) if (c + u * lanes < units) q[u] = src[c + u * lanes];
+            for (uint32_t j = 0; j < k; j++) {
+                const uint32_t r = (uint32_t)__ldg(row_of_pair + f * k + j);
+                if (r >= capacity) continue;
+                Q* dst = rows + (size_t)r * ldr;
+#pragma unroll
+                for (int u = 0; u < 4; u++) if (c + u * lanes < units) dst[c + u * lanes] = q[u];
+            }
+        }
+    }
+}
+
+// y[f] = sum_j w[f][j] rows[row_of_pair[f][j]], j ascending, in fp32, rounded once; V elements a lane and step
+template <typename T, int V, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads)
+combine_kernel(const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t ldr, const int32_t* __restrict__ row_of_pair,
+               const float* __restrict__ weights, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t k, T* __restrict__ y, size_t ldy,
+               uint32_t lanes, sf_dev_state* st)
+{
+    sf_chain_enter();
+    const uint32_t flows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
+    const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1);
+    for (uint64_t f = (uint64_t)blockIdx.x * per + threadIdx.x / lanes; f < flows; f += (uint64_t)gridDim.x * per) {
+        for (uint32_t c = lane * V; c < D; c += lanes * V) {
+            float acc[V];
+#pragma unroll
+            for (int v = 0; v < V; v++) acc[v] = 0.0f;
+            for (uint32_t j = 0; j < k; j++) {
+                const uint32_t r = (uint32_t)__ldg(row_of_pair + f * k + j);
+                if (r >= capacity) continue;
+                const float w = weights ? __ldg(weights + f * k + j) : 1.0f;
+                float x[V];
+                load_f32<T, V, ALIGNED>(rows + (size_t)r * ldr + c, x);
+#pragma unroll
+                for (int v = 0; v < V; v++) acc[v] = fmaf(w, x[v], acc[v]);
+            }
+            store_f32<T, V, ALIGNED>(y + f * ldy + c, acc);
+        }
+    }
+}
+
+// d_rows[row_of_pair[f][j]] = w[f][j] dy[f], d_w[f][j] = <dy[f], rows[row_of_pair[f][j]]>
+template <typename T, int V, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads)
+combine_backward_kernel(const T* __restrict__ dy, size_t ldy, const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t ldr,
+                        const int32_t* __restrict__ row_of_pair, const float* __restrict__ weights, const uint32_t* __restrict__ n_dev,
+                        uint32_t n, uint32_t k, uint32_t E, const uint32_t* __restrict__ offsets, const uint32_t* __restrict__ counts,
+                        T* __restrict__ d_rows, size_t ldd, float* __restrict__ d_weights, uint32_t lanes, uint32_t flow_blocks, sf_dev_state* st)
+{
+    sf_chain_enter();
+    if (blockIdx.x >= flow_blocks) {
+        for (uint32_t e = blockIdx.x - flow_blocks; e < E; e += gridDim.x - flow_blocks) {
+            const uint32_t lo = min(offsets[e] + counts[e], capacity), hi = min(offsets[e + 1], capacity);
+            if (lo >= hi) continue;
+            const uint32_t units = D / V;
+            const uint64_t all = (uint64_t)(hi - lo) * units;
+            const float zero[V] = {};
+            for (uint64_t i = threadIdx.x; i < all; i += kThreads) {
+                const uint32_t r = (uint32_t)(i / units), c = (uint32_t)(i - (uint64_t)r * units);
+                store_f32<T, V, ALIGNED>(d_rows + (size_t)(lo + r) * ldd + (size_t)c * V, zero);
+            }
+        }
+        return;
+    }
+    const uint32_t flows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
+    const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1);
+    for (uint64_t base = (uint64_t)blockIdx.x * per; base < flows; base += (uint64_t)flow_blocks * per) {
+        const uint64_t f = base + threadIdx.x / lanes;
+        const bool live = f < flows;                      // (the sums over lanes below need whole warps)
+        for (uint32_t j = 0; j < k; j++) {
+            const uint32_t r = live ? (uint32_t)__ldg(row_of_pair + f * k + j) : 0xFFFFFFFFu;
+            const bool real = r < capacity;
+            float dot = 0.0f;
+            if (real) {
+                const float w = weights ? __ldg(weights + f * k + j) : 1.0f;
+                for (uint32_t c = lane * V; c < D; c += lanes * V) {
+                    float g[V];
+                    load_f32<T, V, ALIGNED>(dy + f * ldy + c, g);
+                    if (d_weights) {
+                        float x[V];
+                        load_f32<T, V, ALIGNED>(rows + (size_t)r * ldr + c, x);
+#pragma unroll
+                        for (int v = 0; v < V; v++) dot = fmaf(g[v], x[v], dot);
+                    }
+                    if (d_rows) {
+#pragma unroll
+                        for (int v = 0; v < V; v++) g[v] *= w;
+                        store_f32<T, V, ALIGNED>(d_rows + (size_t)r * ldd + c, g);
+                    }
+                }
+            }
+            if (d_weights) {
+                for (uint32_t o = lanes / 2; o >= 1; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
+                if (live && lane == 0) d_weights[f * k + j] = dot;
+            }
+        }
+    }
+}
+
+// lanes that share a flow whose row has `units` units: a power of two up to 32
+uint32_t lanes_for(uint32_t units) { uint32_t l = 1; while (l < 32 && l < units) l *= 2; return l; }
+uint32_t flow_grid(const sf_ctx* ctx, uint32_t n, uint32_t lanes) {
+    const uint32_t per = kThreads / lanes;
+    return std::min<uint32_t>((n + per - 1) / per, (uint32_t)ctx->num_sms * 8);
+}
+bool sizes_ok(uint32_t n, uint32_t k) { return k >= 1 && k <= SF_MAX_EXPERTS && (uint64_t)n * k <= 0x7FFFFFFFull; }
+bool fits16(const void* p, size_t ld, int dtype) { return aligned(p, 16) && (ld * type_bytes(dtype)) % 16 == 0; }
+
+}  // namespace
+
+extern "C" int sf_expert_gate(sf_ctx* ctx, const void* scores, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t E, size_t ld,
+                              uint32_t k, int mode, int32_t* ids_out, float* weights_out, void* stream)
+{
+    if (!ctx || !type_ok(dtype) || E == 0 || E > SF_MAX_EXPERTS || k > E || ld < E || !sizes_ok(n, k)) return SF_ERR_ARG;
+    if (mode != SF_GATE_SOFTMAX && mode != SF_GATE_SOFTMAX_PICKED && mode != SF_GATE_SHARE) return SF_ERR_ARG;
+    if (n == 0) return SF_OK;
+    if (!scores || !ids_out || !weights_out) return SF_ERR_ARG;
+    if (!aligned(scores, type_bytes(dtype)) || !aligned(ids_out, 4) || !aligned(weights_out, 4) || !aligned(n_dev, 4)) return SF_ERR_ARG;
+    SF_ON_DEVICE(ctx);
+    const bool al = fits16(scores, ld, dtype);
+    return by_type(dtype, [&](auto zero) {
+        typedef decltype(zero) T;
+        return by_experts(E, [&](auto lpr, auto v) {
+            constexpr int L = decltype(lpr)::value, V = decltype(v)::value;
+            auto kern = al ? gate_kernel<T, L, V, true> : gate_kernel<T, L, V, false>;
+            SF_CUDA(sf_launch_chained(kern, flow_grid(ctx, n, L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, mode, ids_out, weights_out, ctx->d_state));
+            return SF_OK;
+        });
+    });
+}
+
+extern "C" int sf_expert_gate_backward(sf_ctx* ctx, const void* scores, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t E, size_t ld,
+                                       uint32_t k, int mode, const int32_t* ids, const float* d_weights, void* d_scores_out, size_t ldd, void* stream)
+{
+    if (!ctx || !type_ok(dtype) || E == 0 || E > SF_MAX_EXPERTS || k > E || ld < E || ldd < E || !sizes_ok(n, k)) return SF_ERR_ARG;
+    if (mode != SF_GATE_SOFTMAX && mode != SF_GATE_SOFTMAX_PICKED && mode != SF_GATE_SHARE) return SF_ERR_ARG;
+    if (n == 0) return SF_OK;
+    if (!scores || !ids || !d_weights || !d_scores_out) return SF_ERR_ARG;
+    if (!aligned(scores, type_bytes(dtype)) || !aligned(d_scores_out, type_bytes(dtype)) || !aligned(ids, 4) || !aligned(d_weights, 4) || !aligned(n_dev, 4)) return SF_ERR_ARG;
+    SF_ON_DEVICE(ctx);
+    const bool al = fits16(scores, ld, dtype) && fits16(d_scores_out, ldd, dtype);
+    return by_type(dtype, [&](auto zero) {
+        typedef decltype(zero) T;
+        return by_experts(E, [&](auto lpr, auto v) {
+            constexpr int L = decltype(lpr)::value, V = decltype(v)::value;
+            auto kern = al ? gate_backward_kernel<T, L, V, true> : gate_backward_kernel<T, L, V, false>;
+            SF_CUDA(sf_launch_chained(kern, flow_grid(ctx, n, L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, mode, ids, d_weights,
+                                      (T*)d_scores_out, ldd, ctx->d_state));
+            return SF_OK;
+        });
+    });
+}
+
+extern "C" int sf_expert_sort_workspace(uint32_t n, uint32_t k, uint32_t E, size_t* bytes_out)
+{
+    if (!bytes_out || E == 0 || E > SF_MAX_EXPERTS || !sizes_ok(n, k)) return SF_ERR_ARG;
+    // one word per tile and expert; a tile has at least 1024 pairs
+    *bytes_out = ((uint64_t)n * k + 1023) / 1024 * E * 4;
+    return SF_OK;
+}
+
+extern "C" int sf_expert_sort(sf_ctx* ctx, const int32_t* ids, const uint32_t* n_dev, uint32_t n, uint32_t k, uint32_t E, uint32_t align,
+                              uint32_t capacity, uint32_t* offsets_out, uint32_t* counts_out, int32_t* flow_of_row_out,
+                              int32_t* row_of_pair_out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx || E == 0 || E > SF_MAX_EXPERTS || !sizes_ok(n, k) || capacity > 0x7FFFFFFFu) return SF_ERR_ARG;
+    if (align == 0 || align > 65536 || (align & (align - 1)) || (uint64_t)n * k + (uint64_t)E * (align - 1) > 0x7FFFFFFFull) return SF_ERR_ARG;
+    if (!offsets_out || !counts_out || (n && (!ids || !row_of_pair_out)) || (capacity && !flow_of_row_out)) return SF_ERR_ARG;
+    if (!aligned(ids, 4) || !aligned(n_dev, 4) || !aligned(offsets_out, 4) || !aligned(counts_out, 4) || !aligned(flow_of_row_out, 4) ||
+        !aligned(row_of_pair_out, 4) || !aligned(workspace, 4)) return SF_ERR_ARG;
+    SF_ON_DEVICE(ctx);
+    const uint32_t tiles = sort_tiles(ctx, n, k);
+    if (tiles > 1 && (!workspace || workspace_bytes < (size_t)tiles * E * 4)) return SF_ERR_ARG;
+    const sort_args a = {ids, n_dev, n, k, E, align, capacity, tiles, (uint32_t*)workspace, offsets_out, counts_out, flow_of_row_out, row_of_pair_out};
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (tiles > 1) SF_CUDA(sf_launch_chained(sort_count_kernel, tiles, kThreads, kWarps * E * 4, st, a, ctx->d_state));
+    SF_CUDA(sf_launch_chained(sort_place_kernel, tiles, kThreads, (kWarps * E + 3 * E + 1) * 4, st, a, ctx->d_state));
+    return SF_OK;
+}
+
+extern "C" int sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t D, size_t ldx, uint32_t k,
+                                const int32_t* row_of_pair, uint32_t E, const uint32_t* offsets, const uint32_t* counts, uint32_t capacity,
+                                void* rows_out, size_t ldr, void* stream)
+{
+    if (!ctx || !type_ok(dtype) || D == 0 || ldx < D || ldr < D || E == 0 || E > SF_MAX_EXPERTS || !sizes_ok(n, k) || capacity > 0x7FFFFFFFu) return SF_ERR_ARG;
+    if (capacity == 0) return SF_OK;
+    if ((n && (!x || !row_of_pair)) || !offsets || !counts || !rows_out) return SF_ERR_ARG;
+    if (!aligned(x, type_bytes(dtype)) || !aligned(rows_out, type_bytes(dtype)) || !aligned(row_of_pair, 4) || !aligned(offsets, 4) || !aligned(counts, 4) || !aligned(n_dev, 4)) return SF_ERR_ARG;
+    SF_ON_DEVICE(ctx);
+    const uint32_t size = type_bytes(dtype);
+    const bool al = fits16(x, ldx, dtype) && fits16(rows_out, ldr, dtype) && ((size_t)D * size) % 16 == 0;
+    auto go = [&](auto q) {
+        typedef decltype(q) Q;
+        const uint32_t per = sizeof(Q) / size, units = D / per, lanes = lanes_for(units), fb = flow_grid(ctx, n, lanes);
+        SF_CUDA(sf_launch_chained(gather_kernel<Q>, fb + E, kThreads, 0, (cudaStream_t)stream, (const Q*)x, n_dev, n, units, ldx / per, k, row_of_pair, E,
+                                  offsets, counts, capacity, (Q*)rows_out, ldr / per, lanes, fb, ctx->d_state));
+        return SF_OK;
+    };
+    if (al) return go(uint4());
+    return size == 4 ? go(uint32_t()) : go(uint16_t());
+}
+
+static int combine(sf_ctx* ctx, const void* rows, int dtype, uint32_t capacity, uint32_t D, size_t ldr, const int32_t* row_of_pair,
+                   const float* weights, const uint32_t* n_dev, uint32_t n, uint32_t k, void* y, size_t ldy, void* stream)
+{
+    if (!ctx || !type_ok(dtype) || D == 0 || ldr < D || ldy < D || !sizes_ok(n, k) || capacity > 0x7FFFFFFFu) return SF_ERR_ARG;
+    if (n == 0) return SF_OK;
+    if ((capacity && !rows) || !row_of_pair || !y) return SF_ERR_ARG;
+    if (!aligned(rows, type_bytes(dtype)) || !aligned(y, type_bytes(dtype)) || !aligned(row_of_pair, 4) || !aligned(weights, 4) || !aligned(n_dev, 4)) return SF_ERR_ARG;
+    SF_ON_DEVICE(ctx);
+    const bool al = fits16(rows, ldr, dtype) && fits16(y, ldy, dtype) && ((size_t)D * type_bytes(dtype)) % 16 == 0;
+    return by_type(dtype, [&](auto zero) {
+        typedef decltype(zero) T;
+        constexpr int V = 16 / sizeof(T);
+        const uint32_t lanes = lanes_for(al ? D / V : D), grid = flow_grid(ctx, n, lanes);
+        auto kern = al ? combine_kernel<T, V, true> : combine_kernel<T, 1, false>;
+        SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, (T*)y, ldy, lanes, ctx->d_state));
+        return SF_OK;
+    });
+}
+
+extern "C" int sf_expert_combine(sf_ctx* ctx, const void* rows, int dtype, uint32_t capacity, uint32_t D, size_t ldr, const int32_t* row_of_pair,
+                                 const float* weights, const uint32_t* n_dev, uint32_t n, uint32_t k, void* y_out, size_t ldy, void* stream)
+{
+    return combine(ctx, rows, dtype, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, y_out, ldy, stream);
+}
+
+extern "C" int sf_expert_gather_backward(sf_ctx* ctx, const void* d_rows, int dtype, uint32_t capacity, uint32_t D, size_t ldr,
+                                         const int32_t* row_of_pair, const uint32_t* n_dev, uint32_t n, uint32_t k, void* dx_out, size_t ldx, void* stream)
+{
+    return combine(ctx, d_rows, dtype, capacity, D, ldr, row_of_pair, nullptr, n_dev, n, k, dx_out, ldx, stream);
+}
+
+extern "C" int sf_expert_combine_backward(sf_ctx* ctx, const void* dy, int dtype, size_t ldy, const void* rows, uint32_t capacity, uint32_t D,
+                                          size_t ldr, const int32_t* row_of_pair, const float* weights, const uint32_t* n_dev, uint32_t n,
+                                          uint32_t k, uint32_t E, const uint32_t* offsets, const uint32_t* counts, void* d_rows_out,
+                                          size_t ldd, float* d_weights_out, void* stream)
+{
+    if (!ctx || !type_ok(dtype) || D == 0 || ldr < D || ldy < D || (d_rows_out && ldd < D) || E == 0 || E > SF_MAX_EXPERTS || !sizes_ok(n, k) || capacity > 0x7FFFFFFFu) return SF_ERR_ARG;
+    if (!d_rows_out && !d_weights_out) return SF_ERR_ARG;
+    if (n && (!dy || !row_of_pair || (d_weights_out && capacity && !rows))) return SF_ERR_ARG;
+    if (d_rows_out && (!offsets || !counts)) return SF_ERR_ARG;
+    if (!aligned(dy, type_bytes(dtype)) || !aligned(rows, type_bytes(dtype)) || !aligned(d_rows_out, type_bytes(dtype)) || !aligned(row_of_pair, 4) || !aligned(weights, 4) ||
+        !aligned(offsets, 4) || !aligned(counts, 4) || !aligned(d_weights_out, 4) || !aligned(n_dev, 4)) return SF_ERR_ARG;
+    SF_ON_DEVICE(ctx);
+    const bool al = fits16(dy, ldy, dtype) && (!d_weights_out || fits16(rows, ldr, dtype)) && (!d_rows_out || fits16(d_rows_out, ldd, dtype)) && ((size_t)D * type_bytes(dtype)) % 16 == 0;
+    return by_type(dtype, [&](auto zero) {
+        typedef decltype(zero) T;
+        constexpr int V = 16 / sizeof(T);
+        const uint32_t lanes = lanes_for(al ? D / V : D), fb = flow_grid(ctx, n, lanes), grid = fb + (d_rows_out ? E : 0);
+        if (grid == 0) return SF_OK;
+        auto kern = al ? combine_backward_kernel<T, V, true> : combine_backward_kernel<T, 1, false>;
+        SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)dy, ldy, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, E,
+                                  offsets, counts, (T*)d_rows_out, ldd, d_weights_out, lanes, fb, ctx->d_state));
+        return SF_OK;
+    });
+}
