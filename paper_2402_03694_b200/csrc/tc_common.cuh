@@ -226,7 +226,10 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---- host: tensor-map encoding through the driver entry point ---------------
-// 2-D bf16 row-major matrix [rows][cols]; box = box_rows x box_cols; 128-byte swizzle
+// 2-D row-major matrix [rows][cols] with a row pitch in bytes (a multiple of 16); box = box_rows x box_cols
+int encode_tmap_2d(CUtensorMap* out, CUtensorMapDataType type, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch_bytes,
+                   uint32_t box_rows, uint32_t box_cols, CUtensorMapSwizzle swizzle);
+// the same for dense bf16 rows with a 128-byte swizzle
 int encode_tmap_bf16_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols,
                         uint32_t box_rows, uint32_t box_cols);
 

@@ -347,6 +347,49 @@ def test_refusals(env):
         sf.sf_mx4_quantise(ctx, x[:1], big, big[8:])
 
 
+def check_rows(got, a, w, bias, relu, kind):
+    """check_product on the GPU's doubles, for outputs that are long on the CPU."""
+    K = a.shape[1]
+    exact = a @ w.T + bias
+    slack = (K + 2) * 2.0 ** -23 * (a.abs() @ w.abs().T + bias.abs())
+    exact = exact.clamp(min=0) if relu else exact
+    off = (got.double() - exact).abs() - slack - HALF_STEP[kind] * (exact.abs() + slack)
+    assert float(off.max()) <= 0, float(off.max())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,K,N,E", [(20011, 1024, 1024, 1), (5000, 2048, 1000, 1), (40000, 224, 257, 1), (19000, 4096, 512, 1), (30000, 512, 512, 7), (3000, 640, 160, 1)])
+def test_product_of_many_rows(env, n, K, N, E, kind):
+    """Sizes that fill the machine (CTA pairs): packed by the library, whose packing the tests above hold to the definition."""
+    sf, ctx = env
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    rng = np.random.default_rng(n)
+    counts = rng.multinomial(n - 128 * E, np.ones(E) / E) if E > 1 else [n]
+    offsets = np.concatenate([[0], np.cumsum([-(-c // 128) * 128 for c in counts])]).astype(np.int32) if E > 1 else np.array([0, n], np.int32)
+    x, w = torch.randn(n, K, device="cuda", generator=g), torch.randn(E * N, K, device="cuda", generator=g) / K ** 0.5
+    def packed(v):
+        d, s = sf.sf_mx4_sizes(*v.shape)
+        d, s = torch.zeros(d, dtype=torch.uint8, device="cuda"), torch.full((s,), 255, dtype=torch.uint8, device="cuda")
+        sf.sf_mx4_quantise(ctx, v, d, s)
+        r = torch.zeros_like(v)
+        sf.sf_mx4_unpack(ctx, d, s, r)
+        return d, s, r.double()
+    a, sa, ra = packed(x)
+    ws = [packed(w[e * N:(e + 1) * N]) for e in range(E)]
+    bias = torch.randn(E, N, device="cuda", generator=g)
+    out = torch.full((n, N), 7.0, dtype=TYPES[kind], device="cuda")
+    if E == 1:
+        sf.sf_mx4_matmul(ctx, a, sa, ws[0][0], ws[0][1], K, out, bias=bias, relu=True)
+    else:
+        sf.sf_mx4_matmul_experts(ctx, a, sa, torch.cat([v[0] for v in ws]), torch.cat([v[1] for v in ws]), K, dev(offsets), out, bias=bias, relu=True)
+    sf.sf_ctx_poll(ctx)
+    for e in range(E):
+        lo, hi = int(offsets[e]), int(offsets[e + 1])
+        check_rows(out[lo:hi], ra[lo:hi], ws[e][2], bias[e].double(), True, kind)
+    assert (out[int(offsets[-1]):] == 7).all()
+
+
 def test_captured_replayed_and_on_another_stream(env):
     sf, ctx = env
     rng = np.random.default_rng(14)
