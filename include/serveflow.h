@@ -66,6 +66,7 @@ extern "C" {
 #define SF_F32          0
 #define SF_BF16         1
 #define SF_F16          2          /* rows of the packed-row and expert calls below; no model is built in it */
+#define SF_MX4          3          /* packed rows (microscaled 4-bit floating point, see sf_mx4_quantise) */
 #define SF_GATE_SOFTMAX        0   /* weight of a picked expert = its softmax over all scores of the row */
 #define SF_GATE_SOFTMAX_PICKED 1   /* ... over the picked scores only */
 #define SF_GATE_SHARE          2   /* ... its share of the picked scores' sum (scores = class probabilities of the fast model) */
@@ -332,17 +333,19 @@ int  sf_mx4_unpack(sf_ctx* ctx, const uint8_t* data, const uint8_t* scales, cons
                    int dtype, void* out, size_t ld, void* stream);
 /* out[r][n] = act(sum_k A[r][k] W[n][k] + bias[n]): packed rows (capacity x K, the first *n_rows_dev of them) times packed weights
  * (N rows of K), products summed in fp32, bias fp32[N] (nullable), act = ReLU if relu != 0, rounded once to out_dtype
- * (SF_F32 | SF_BF16 | SF_F16), row pitch ld >= N elements.  Rows at or beyond the count are left as they were. */
+ * (SF_F32 | SF_BF16 | SF_F16), row pitch ld >= N elements, out_scales NULL.  With out_dtype SF_MX4 the rows are packed again, from
+ * the fp32 sums, for a next layer: out = the data array of rows of N values, out_scales = their scale array, ld ignored.  Rows at
+ * or beyond the count are left as they were. */
 int  sf_mx4_matmul(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_scales, const uint32_t* n_rows_dev, uint32_t capacity,
                    const uint8_t* w, const uint8_t* w_scales, uint32_t N, uint32_t K, const float* bias, int relu,
-                   int out_dtype, void* out, size_t ld, void* stream);
+                   int out_dtype, void* out, size_t ld, uint8_t* out_scales, void* stream);
 /* The same with one weight matrix per expert: rows offsets[e] .. offsets[e+1]-1 (DEVICE uint32[E+1], as sf_expert_sort writes them
  * with an `align` that is a multiple of 128) are multiplied with weights e.  w: E matrices of N packed rows one behind the
  * other, w_scales: their E scale arrays one behind the other, bias fp32[E][N].  An expert whose first row is not a multiple of
  * 128 is skipped and SF_ERR_ARG recorded in the error word; rows at or beyond offsets[E] or capacity are left as they were. */
 int  sf_mx4_matmul_experts(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_scales, const uint32_t* offsets, uint32_t E,
                            uint32_t capacity, const uint8_t* w, const uint8_t* w_scales, uint32_t N, uint32_t K,
-                           const float* bias, int relu, int out_dtype, void* out, size_t ld, void* stream);
+                           const float* bias, int relu, int out_dtype, void* out, size_t ld, uint8_t* out_scales, void* stream);
 
 /* ---- several slow models: experts -------------------------------------------- */
 /* sf_route assigns a flow to THE slow model; these calls assign it to k of E experts: gate -> sort -> gather (or sf_mx4_quantise

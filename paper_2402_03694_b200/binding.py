@@ -21,7 +21,7 @@ SF_NOALLOC_MAX_FLOWS = 4194304
 SF_RF, SF_GBDT, SF_GBDT_MC = 0, 1, 2
 SF_LC_GT, SF_ABSMARGIN_LT, SF_ENTROPY_GT, SF_SOFTMAX_LC_GT = 0, 1, 2, 3
 SF_MLP16, SF_CNN8 = 0, 1
-SF_F32, SF_BF16, SF_F16 = 0, 1, 2
+SF_F32, SF_BF16, SF_F16, SF_MX4 = 0, 1, 2, 3
 SF_GATE_SOFTMAX, SF_GATE_SOFTMAX_PICKED, SF_GATE_SHARE = 0, 1, 2
 SF_MAX_EXPERTS = 1024
 SF_TAU_MARGIN_DEFAULT = float.fromhex("0x1.b1d106p-1")
@@ -138,8 +138,8 @@ def _lib():
         L.sf_mx4_sizes.argtypes = [U32, U32, C.POINTER(Z), C.POINTER(Z)]
         L.sf_mx4_quantise.argtypes = [V, V, I, U32, U32, Z, V, V, U32, V, V, V]
         L.sf_mx4_unpack.argtypes = [V, V, V, V, U32, U32, I, V, Z, V]
-        L.sf_mx4_matmul.argtypes = [V, V, V, V, U32, V, V, U32, U32, V, I, I, V, Z, V]
-        L.sf_mx4_matmul_experts.argtypes = [V, V, V, V, U32, U32, V, V, U32, U32, V, I, I, V, Z, V]
+        L.sf_mx4_matmul.argtypes = [V, V, V, V, U32, V, V, U32, U32, V, I, I, V, Z, V, V]
+        L.sf_mx4_matmul_experts.argtypes = [V, V, V, V, U32, U32, V, V, U32, U32, V, I, I, V, Z, V, V]
         L.sf_expert_gate.argtypes = [V, V, I, V, U32, U32, Z, U32, I, V, V, V]
         L.sf_expert_gate_backward.argtypes = [V, V, I, V, U32, U32, Z, U32, I, V, V, V, Z, V]
         L.sf_expert_sort_workspace.argtypes = [U32, U32, U32, C.POINTER(Z)]
@@ -434,26 +434,38 @@ def sf_mx4_unpack(ctx, data, scales, out, n_rows_dev=None, stream=None):
                                 _stream(stream)), w)
 
 
-def sf_mx4_matmul(ctx, a, a_scales, w, w_scales, K, out, bias=None, relu=False, n_rows_dev=None, stream=None):
-    """out[rows][N] = act(A W^T + bias); A and W packed rows of K values, out bf16, fp16 or fp32."""
+def _product_out(out, out_scales, N, w):
+    """(address, type, rows, N, pitch, scales' address) of a product's output: a 2-D float tensor, or packed rows of N values."""
+    if out_scales is None:
+        p, dt, n, cols, ld = _rows(out, w)
+        _arg(N is None or N == cols, w)
+        return p, dt, n, cols, ld, None
+    _arg(N is not None and N >= 1 and out.dim() == 2 and out.shape[1] == -(-N // 32) * 16, w)
+    n = out.shape[0]
+    return _flat(out, 0, 1, w), SF_MX4, n, N, 0, _flat(out_scales, _mx4_bytes(n, N)[1], 1, w)
+
+
+def sf_mx4_matmul(ctx, a, a_scales, w, w_scales, K, out, bias=None, relu=False, n_rows_dev=None, out_scales=None, N=None, stream=None):
+    """out[rows][N] = act(A W^T + bias); A and W packed rows of K values, out bf16, fp16 or fp32 - or, with out_scales and N, packed rows
+    again (out uint8 [rows][ceil(N/32)*16])."""
     s = "sf_mx4_matmul"
-    p, dt, n, N, ld = _rows(out, s)
+    p, dt, n, N, ld, os_ = _product_out(out, out_scales, N, s)
     pitch, ab = _mx4_bytes(n, K)
     _check(_lib().sf_mx4_matmul(ctx, _flat(a, n * pitch, 1, s), _flat(a_scales, ab, 1, s), _flat(n_rows_dev, 1, 4, s), n,
                                 _flat(w, N * pitch, 1, s), _flat(w_scales, _mx4_bytes(N, K)[1], 1, s), N, K, _flat(bias, N, 4, s),
-                                int(relu), dt, p, ld, _stream(stream)), s)
+                                int(relu), dt, p, ld, os_, _stream(stream)), s)
 
 
-def sf_mx4_matmul_experts(ctx, a, a_scales, w, w_scales, K, offsets, out, bias=None, relu=False, stream=None):
+def sf_mx4_matmul_experts(ctx, a, a_scales, w, w_scales, K, offsets, out, bias=None, relu=False, out_scales=None, N=None, stream=None):
     """The same over rows sorted by expert: offsets [E + 1] (device), w, w_scales and bias of the E experts one behind the other."""
     s = "sf_mx4_matmul_experts"
-    p, dt, n, N, ld = _rows(out, s)
+    p, dt, n, N, ld, os_ = _product_out(out, out_scales, N, s)
     E = offsets.numel() - 1
     _arg(E >= 1, s)
     pitch, ab = _mx4_bytes(n, K)
     _check(_lib().sf_mx4_matmul_experts(ctx, _flat(a, n * pitch, 1, s), _flat(a_scales, ab, 1, s), _flat(offsets, E + 1, 4, s), E, n,
                                         _flat(w, E * N * pitch, 1, s), _flat(w_scales, E * _mx4_bytes(N, K)[1], 1, s), N, K,
-                                        _flat(bias, E * N, 4, s), int(relu), dt, p, ld, _stream(stream)), s)
+                                        _flat(bias, E * N, 4, s), int(relu), dt, p, ld, os_, _stream(stream)), s)
 
 
 def sf_expert_gate(ctx, scores, mode, ids_out, weights_out, n_dev=None, stream=None):

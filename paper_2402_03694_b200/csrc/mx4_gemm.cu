@@ -4,11 +4,18 @@
 // tcgen05.mma kind::mxf4 multiplies 4-bit values with one power-of-two scale per 32 of them and sums in fp32: both
 // operands go to shared memory as they are packed (TMA, 256 values = one 128-byte swizzled row per matrix row and stage), their
 // scale bytes as 512-byte tiles that tcgen05.cp spreads over the TMEM lanes in front of the MMAs (64 values of K each).
-// Persistent kernel, one CTA per SM.  Warp roles:
-//   warp 0      producer: the A, W and scale tiles of a ring of stages, all by TMA (boxes beyond an array read zeros)
-//   warp 1      allocates TMEM; one lane copies scales and issues MMAs
-//   warps 2..9  epilogue: tcgen05.ld (lane quarter = warp % 4, column half = (warp - 2) / 4), bias, ReLU, rounding, 128-byte row
-//               pieces through shared memory
+// Persistent kernel, one CTA per SM, each with a run of consecutive tiles (a row panel's column tiles one after the other).  While
+// K <= 1280 a panel's slices of A stay in shared memory (a ring of five) for all its column tiles and only W is streamed: 2 % at
+// 120,000 x 1024 x 1024 (a longer ring, with fewer stages of W or without the 128-byte staging below, gains nothing: 240,001 x
+// 2048 x 1024 in 0.215 ms with eight slots and 64-byte stores, 0.217 ms this way).  Warp roles:
+//   warp 0      producer: slices of A and W with their scales, all by TMA (boxes beyond an array read zeros)
+//   warp 1      allocates TMEM; copies scales and issues MMAs.  The whole warp walks the loop and one elected lane issues: descriptors
+//               and addresses then stay in uniform registers.  With a loop of one lane every copy and MMA first moves its operands
+//               there (about 57 cycles each), and the six copies and four MMAs of a stage took 870 cycles to issue instead of
+//               the 512 that the MMAs run
+//   warps 2..9  epilogue: tcgen05.ld (lane quarter = warp % 4, column half = (warp - 2) / 4), bias, ReLU, rounding, then 32 rows x 128
+//               bytes through shared memory and out by TMA (plain 64-byte row pieces: 76 instead of 67 us at 120,000 x 1024 x
+//               1024), or by plain stores where rows are not on 16-byte boundaries or a tile ends inside
 // Every wait is bounded as in gemm_tc.cu: on a timeout the block records SF_ERR_DEVICE_TIMEOUT, lets its copies land, frees TMEM
 // and returns.
 //
@@ -19,6 +26,7 @@
 #include "tc_common.cuh"
 #include "mx4.cuh"
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 using namespace sfrow;
@@ -30,25 +38,29 @@ constexpr uint32_t kThreads = 64 + kEpiWarps * 32;
 constexpr uint32_t kBK = 256;                        // values of K per stage: 128 bytes a row
 constexpr uint32_t kSfCol = 448;                     // first TMEM column of the scales (two buffers)
 
+struct Bars {
+    uint64_t a_full[5], a_empty[5], w_full[5], w_empty[5], acc_full[2], acc_free[2];
+    uint32_t tmem_base, abort_flag;
+};
 template <uint32_t BN, bool PAIR> struct Cfg {
     static constexpr uint32_t kRows = PAIR ? 256 : 128;                   // rows of a tile
     static constexpr uint32_t kNT = (BN + 127) / 128;                     // scale row tiles of W per stage
-    static constexpr uint32_t kA = 128 * 128, kB = (PAIR ? BN / 2 : BN) * 128, kSA = 1024, kSB = kNT * 1024;
-    static constexpr uint32_t kStage = kA + kB + kSA + kSB;
-    static constexpr uint32_t kStages = BN == 64 ? 6 : 5;
-    static constexpr uint32_t kStaging = kEpiWarps * (4096 + 512);        // per epilogue warp: 32 rows x 128 bytes, 128 biases
+    static constexpr uint32_t kA = 128 * 128, kSlot = kA + 1024;          // a slice of A: 128 rows x 256 values and their scales
+    static constexpr uint32_t kB = (PAIR ? BN / 2 : BN) * 128, kStage = kB + kNT * 1024;      // a slice of W
+    static constexpr uint32_t kSlots = 5, kStages = 5;
+    static constexpr uint32_t kStaging = kEpiWarps * 4096 + BN * 4;       // per epilogue warp: 32 rows x 128 bytes; a tile's biases
     static constexpr uint32_t kOverlap = BN == 256 ? 64 : 0;              // columns that the two accumulators share
     static constexpr uint32_t kSecond = BN - kOverlap;                    // first column of the second accumulator
     static constexpr uint32_t kSfCols = 8 + 8 * kNT;
     static_assert(kSecond + BN <= kSfCol && kSfCol + 2 * kSfCols <= 512, "TMEM");
-    static_assert(kStage % 1024 == 0, "swizzled tiles start on 1024-byte boundaries");
-    static uint32_t smem(uint32_t E) { return 1024 + kStages * kStage + kStaging + 512 + (2 * E + 2) * 4; }
+    static_assert(kSlot % 1024 == 0 && kStage % 1024 == 0, "swizzled tiles start on 1024-byte boundaries");
+    static constexpr uint32_t smem(uint32_t E) { return 1024 + kSlots * kSlot + kStages * kStage + kStaging + sizeof(Bars) + (2 * E + 2) * 4; }
 };
 
-struct Bars {
-    uint64_t full[8], empty[8], acc_full[2], acc_free[2];
-    uint32_t tmem_base, abort_flag;
-};
+static_assert(Cfg<256, true>::smem(SF_MAX_EXPERTS) <= 232448 && Cfg<128, false>::smem(SF_MAX_EXPERTS) <= 232448 &&
+              Cfg<64, false>::smem(SF_MAX_EXPERTS) <= 232448, "shared memory of a block");
+
+struct Mx4 {};                                       // output type: packed again
 
 // 4-bit operands, fp32 accumulators, power-of-two scales per 32 values; sf = 0 or 2: which pair of a scale word's bytes
 __host__ __device__ constexpr uint32_t make_idesc(uint32_t M, uint32_t N, uint32_t sf) {
@@ -72,25 +84,74 @@ template <bool PAIR> __device__ __forceinline__ void copy_scales(uint32_t tmem, 
     else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 
+// one lane of a converged warp
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p != 0;
+}
+
+// Arrival on a barrier of the leader CTA that releases TMEM only: the tcgen05 fence orders that.  A releasing arrival at cluster scope
+// would first wait for the thread's stores of the tile before.
+__device__ __forceinline__ void mbar_arrive_relaxed(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// 128 threads meet at named barrier `id`: true in all of them if it is in each
+__device__ __forceinline__ bool half_agrees(uint32_t id, bool mine) {
+    uint32_t r;
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %2, 0;\nbar.red.and.pred q, %1, 128, p;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"(id), "r"((uint32_t)mine) : "memory");
+    return r != 0;
+}
+
 __device__ __forceinline__ float relu_keep_nan(float v) {
     float r;
     asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(v));
     return r;
 }
-template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
-template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
+// two outputs in one word, the first in the low half; the conversion itself clamps at zero and keeps a NaN
+template <typename T, bool RELU> __device__ __forceinline__ uint32_t pack2(float a, float b) {
     uint32_t h;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        if constexpr (RELU) asm("cvt.rn.relu.bf16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
+        else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
+    } else {
+        if constexpr (RELU) asm("cvt.rn.relu.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
+        else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
+    }
     return h;
 }
-template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
-    uint32_t h;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
-    return h;
+// (a0, a1) + (b0, b1): two fp32 additions in one instruction
+__device__ __forceinline__ void add_pair(float& x0, float& x1, uint32_t a0, uint32_t a1, float b0, float b1) {
+    uint64_t a, b;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(a) : "r"(a0), "r"(a1));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(b) : "f"(b0), "f"(b1));
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(a) : "l"(b));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(a));
+}
+// accumulators + biases, ReLU, rounding: v[0..COLS) -> the row's words (fp32 values for T = float and for rows packed again)
+template <typename T, uint32_t COLS, bool RELU> __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const float* bias_s) {
+#pragma unroll
+    for (uint32_t g = 0; g < COLS; g += 4) {
+        const float4 b = *reinterpret_cast<const float4*>(bias_s + g);
+        float x[4];
+        add_pair(x[0], x[1], v[g], v[g + 1], b.x, b.y);
+        add_pair(x[2], x[3], v[g + 2], v[g + 3], b.z, b.w);
+        if constexpr (sizeof(T) == 2) {
+            v[g / 2] = pack2<T, RELU>(x[0], x[1]);
+            v[g / 2 + 1] = pack2<T, RELU>(x[2], x[3]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; q++) v[g + q] = __float_as_uint(RELU ? relu_keep_nan(x[q]) : x[q]);
+        }
+    }
 }
 
-// What a CTA (pair) works through: tiles of kRows x BN outputs, every n_units-th one, expert by expert, a row panel's column tiles
-// one after the other.
+// A value that is the same in all lanes, told to the compiler as such: loop bounds and addresses that come out of shared memory
+// would otherwise keep the issuing warps' operands out of the uniform registers.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
+
+// What a CTA (pair) works through: tiles of kRows x BN outputs, expert by expert, panel by panel; unit u of U takes tiles
+// [n u / U, n (u + 1) / U).
 struct Segments {
     const uint32_t* begin;           // [E] first row
     const uint32_t* tile;            // [E + 1] first tile
@@ -98,36 +159,42 @@ struct Segments {
     uint32_t e = 0;                  // cursor: tiles come in rising order
     __device__ __forceinline__ void find(uint32_t t, uint32_t rows_per_tile, uint32_t& row, uint32_t& tn) {
         while (e + 1 < E && t >= tile[e + 1]) e++;
-        const uint32_t local = t - tile[e], tm = local / tiles_n;
+        e = uniform(e);
+        const uint32_t local = uniform(t - tile[e]), tm = local / tiles_n;
         tn = local - tm * tiles_n;
-        row = begin[e] + tm * rows_per_tile;
+        row = uniform(begin[e]) + tm * rows_per_tile;
     }
 };
 
 template <uint32_t BN, bool PAIR, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
 mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmSA,
-                   const __grid_constant__ CUtensorMap tmSW, const sf_mx4_product p, sf_dev_state* st)
+                   const __grid_constant__ CUtensorMap tmSW, const __grid_constant__ CUtensorMap tmO,
+                   const uint32_t tma_out, const sf_mx4_product p, sf_dev_state* st)
 {
     using C = Cfg<BN, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     sf_chain_enter();
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const tiles = smem_raw + (base - smem_u32(smem_raw));
-    uint8_t* const staging = tiles + C::kStages * C::kStage;
+    uint8_t* const w_ring = tiles + C::kSlots * C::kSlot;
+    uint8_t* const staging = w_ring + C::kStages * C::kStage;
     Bars* const bars = reinterpret_cast<Bars*>(staging + C::kStaging);
-    uint32_t* const seg_begin = reinterpret_cast<uint32_t*>(staging + C::kStaging + 512);
+    uint32_t* const seg_begin = reinterpret_cast<uint32_t*>(bars + 1);
     uint32_t* const seg_tile = seg_begin + p.E;
     volatile uint32_t* const abort_flag = &bars->abort_flag;
 
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tiles_n = (p.N + BN - 1) / BN;
+    const uint32_t warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    constexpr bool kPacked = std::is_same<T, Mx4>::value;
+    const uint32_t tiles_n = ((kPacked ? k_tiles(p.N) * 128 : p.N) + BN - 1) / BN;      // packed rows: up to the last scale tile's end
     const uint32_t k_blocks = (p.K + kBK - 1) / kBK;
+    const bool keep = k_blocks <= C::kSlots;          // a panel of A fits in the ring
     const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
     const uint32_t unit = PAIR ? blockIdx.x >> 1 : blockIdx.x, n_units = PAIR ? gridDim.x >> 1 : gridDim.x;
 
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < C::kStages; s++) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
+        for (uint32_t s = 0; s < C::kStages; s++) { mbar_init(&bars->w_full[s], 1); mbar_init(&bars->w_empty[s], 1); }
+        for (uint32_t s = 0; s < C::kSlots; s++) { mbar_init(&bars->a_full[s], 1); mbar_init(&bars->a_empty[s], 1); }
         for (uint32_t b = 0; b < 2; b++) { mbar_init(&bars->acc_full[b], 1); mbar_init(&bars->acc_free[b], (PAIR ? 2 : 1) * kEpiWarps); }
         bars->abort_flag = 0;
         fence_barrier_init();
@@ -159,104 +226,147 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     __syncthreads();
     if constexpr (PAIR) cluster_sync_all();
     tc_fence_after();
-    const uint32_t tmem = bars->tmem_base;
-    const uint32_t n_tiles = seg_tile[p.E];
+    const uint32_t tmem = uniform(bars->tmem_base);
+    const uint32_t n_tiles = uniform(seg_tile[p.E]);
+    const uint32_t t_begin = (uint32_t)((uint64_t)n_tiles * unit / n_units), t_end = (uint32_t)((uint64_t)n_tiles * (unit + 1) / n_units);
     Segments seg = {seg_begin, seg_tile, p.E, tiles_n};
 
     if (warp == 0) {
-        if (lane == 0) {
-            tma_prefetch_desc(&tmA); tma_prefetch_desc(&tmW); tma_prefetch_desc(&tmSA); tma_prefetch_desc(&tmSW);
-            const uint32_t nt = (p.N + 127) / 128;   // scale row tiles of one expert's weights
-            uint32_t stage = 0, phase = 0;
-            bool ok = true;
-            for (uint32_t t = unit; t < n_tiles && ok; t += n_units) {
-                uint32_t row, tn;
-                seg.find(t, C::kRows, row, tn);
-                const int32_t ra = (int32_t)(row + rank * 128), rw = (int32_t)(seg.e * p.N + tn * BN + rank * (BN / 2));
-                const int32_t sw = (int32_t)(seg.e * nt + tn * BN / 128);
-                for (uint32_t kb = 0; kb < k_blocks; kb++) {
-                    if (!mbar_wait(&bars->empty[stage], phase ^ 1u, abort_flag)) { ok = false; break; }
-                    uint8_t* const s = tiles + stage * C::kStage;
-                    if constexpr (PAIR) {
-                        const uint32_t bar = map_to_cta(smem_u32(&bars->full[stage]), 0);
-                        if (rank == 0) mbar_expect_tx(&bars->full[stage], 2 * C::kStage);
-                        tma_load_2d_pair(s, &tmA, (int32_t)(kb * 128), ra, bar);
-                        tma_load_2d_pair(s + C::kA, &tmW, (int32_t)(kb * 128), rw, bar);
-                        tma_load_2d_pair(s + C::kA + C::kB, &tmSA, (int32_t)(kb * 256), ra / 128, bar);
-                        tma_load_2d_pair(s + C::kA + C::kB + C::kSA, &tmSW, (int32_t)(kb * 256), sw, bar);
-                    } else {
-                        mbar_expect_tx(&bars->full[stage], C::kStage);
-                        tma_load_2d(s, &tmA, (int32_t)(kb * 128), ra, &bars->full[stage]);
-                        tma_load_2d(s + C::kA, &tmW, (int32_t)(kb * 128), rw, &bars->full[stage]);
-                        tma_load_2d(s + C::kA + C::kB, &tmSA, (int32_t)(kb * 256), ra / 128, &bars->full[stage]);
-                        tma_load_2d(s + C::kA + C::kB + C::kSA, &tmSW, (int32_t)(kb * 256), sw, &bars->full[stage]);
+        if (elect_one()) { tma_prefetch_desc(&tmA); tma_prefetch_desc(&tmW); tma_prefetch_desc(&tmSA); tma_prefetch_desc(&tmSW); }
+        const uint32_t nt = (p.N + 127) / 128;       // scale row tiles of one expert's weights
+        uint32_t stage = 0, phase = 0, slot = 0, sphase = 0;
+        bool ok = true;
+        for (uint32_t t = t_begin; t < t_end && ok; t++) {
+            uint32_t row, tn;
+            seg.find(t, C::kRows, row, tn);
+            const bool fresh = !keep || tn == 0 || t == t_begin;           // A's slices have to be loaded
+            const int32_t ra = (int32_t)(row + rank * 128), rw = (int32_t)(seg.e * p.N + tn * BN + rank * (BN / 2));
+            const int32_t sw = (int32_t)(seg.e * nt + tn * BN / 128);
+            for (uint32_t kb = 0; kb < k_blocks; kb++) {
+                if (fresh) {
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->a_empty[slot], sphase ^ 1u, abort_flag));
+                    if (!ok) break;
+                    if (elect_one()) {
+                        uint8_t* const s = tiles + slot * C::kSlot;
+                        if constexpr (PAIR) {
+                            const uint32_t bar = map_to_cta(smem_u32(&bars->a_full[slot]), 0);
+                            if (rank == 0) mbar_expect_tx(&bars->a_full[slot], 2 * C::kSlot);
+                            tma_load_2d_pair(s, &tmA, (int32_t)(kb * 128), ra, bar);
+                            tma_load_2d_pair(s + C::kA, &tmSA, (int32_t)(kb * 256), ra / 128, bar);
+                        } else {
+                            mbar_expect_tx(&bars->a_full[slot], C::kSlot);
+                            tma_load_2d(s, &tmA, (int32_t)(kb * 128), ra, &bars->a_full[slot]);
+                            tma_load_2d(s + C::kA, &tmSA, (int32_t)(kb * 256), ra / 128, &bars->a_full[slot]);
+                        }
                     }
-                    if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+                    __syncwarp();
+                    if (++slot == C::kSlots) { slot = 0; sphase ^= 1u; }
                 }
-            }
-            // every stage's last use released: no copy is in flight, no arrival on its way to this CTA's barriers
-            for (uint32_t s = 0; s < C::kStages && ok; s++) {
-                if (!mbar_wait(&bars->empty[stage], phase ^ 1u, abort_flag)) ok = false;
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->w_empty[stage], phase ^ 1u, abort_flag));
+                if (!ok) break;
+                if (elect_one()) {
+                    uint8_t* const s = w_ring + stage * C::kStage;
+                    if constexpr (PAIR) {
+                        const uint32_t bar = map_to_cta(smem_u32(&bars->w_full[stage]), 0);
+                        if (rank == 0) mbar_expect_tx(&bars->w_full[stage], 2 * C::kStage);
+                        tma_load_2d_pair(s, &tmW, (int32_t)(kb * 128), rw, bar);
+                        tma_load_2d_pair(s + C::kB, &tmSW, (int32_t)(kb * 256), sw, bar);
+                    } else {
+                        mbar_expect_tx(&bars->w_full[stage], C::kStage);
+                        tma_load_2d(s, &tmW, (int32_t)(kb * 128), rw, &bars->w_full[stage]);
+                        tma_load_2d(s + C::kB, &tmSW, (int32_t)(kb * 256), sw, &bars->w_full[stage]);
+                    }
+                }
+                __syncwarp();
                 if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
             }
         }
+        // every stage's and slot's last use released: no copy is in flight, no arrival on its way to this CTA's barriers
+        for (uint32_t s = 0; s < C::kStages && ok; s++) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->w_empty[stage], phase ^ 1u, abort_flag));
+            if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+        }
+        for (uint32_t s = 0; s < C::kSlots && ok; s++) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->a_empty[slot], sphase ^ 1u, abort_flag));
+            if (++slot == C::kSlots) { slot = 0; sphase ^= 1u; }
+        }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             uint32_t stage = 0, phase = 0, i = 0, sbuf = 0;
+            uint32_t panel = 0, pphase = 0;           // first slot of the current panel and its phase
             bool ok = true;
-            for (uint32_t t = unit; t < n_tiles && ok; t += n_units, i++) {
+            for (uint32_t t = t_begin; t < t_end && ok; t++, i++) {
                 uint32_t row, tn;
                 seg.find(t, C::kRows, row, tn);
+                const bool fresh = !keep || tn == 0 || t == t_begin;
+                const bool last = !keep || tn + 1 == tiles_n || t + 1 == t_end;       // the panel's last tile here
                 // overlapping accumulators: the shared columns of the tile before have been read; else: the tile before that
+                // (waited for with the first slices and their scales already on their way)
                 constexpr uint32_t kBack = C::kOverlap ? 1 : 2;
-                if (i >= kBack && !mbar_wait(&bars->acc_free[(i - kBack) & 1u], ((i - kBack) >> 1) & 1u, abort_flag)) { ok = false; break; }
-                tc_fence_after();
                 const uint32_t d = tmem + (i & 1u) * C::kSecond;
                 const uint32_t half = BN == 64 ? (tn & 1u) * 2u : 0u;      // 64 columns: half of a scale tile
+                uint32_t slot = panel, sphase = pphase;
                 for (uint32_t kb = 0; kb < k_blocks; kb++) {
-                    if (!mbar_wait(&bars->full[stage], phase, abort_flag)) { ok = false; break; }
+                    if (fresh) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->a_full[slot], sphase, abort_flag));
+                    if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->w_full[stage], phase, abort_flag));
+                    if (!ok) break;
                     tc_fence_after();
-                    const uint32_t a = base + stage * C::kStage, b = a + C::kA, sa = b + C::kB, sb = sa + C::kSA;
+                    const uint32_t a = base + slot * C::kSlot, sa = a + C::kA;
+                    const uint32_t b = base + C::kSlots * C::kSlot + stage * C::kStage, sb = b + C::kB;
                     const uint32_t sf = tmem + kSfCol + sbuf * C::kSfCols;
+                    const uint32_t left = p.K - kb * kBK;                  // values of K from here on
+                    const bool issue = elect_one();
+                    if (issue) {
 #pragma unroll
-                    for (uint32_t j = 0; j < 2; j++) {
-                        copy_scales<PAIR>(sf + j * 4, sa + j * 512);
+                        for (uint32_t j = 0; j < 2; j++) {
+                            copy_scales<PAIR>(sf + j * 4, sa + j * 512);
 #pragma unroll
-                        for (uint32_t r = 0; r < C::kNT; r++) copy_scales<PAIR>(sf + 8 + (j * C::kNT + r) * 4, sb + r * 1024 + j * 512);
+                            for (uint32_t r = 0; r < C::kNT; r++) copy_scales<PAIR>(sf + 8 + (j * C::kNT + r) * 4, sb + r * 1024 + j * 512);
+                        }
                     }
-                    const uint32_t steps = min(4u, (p.K - kb * kBK + 63) / 64);
-                    for (uint32_t k = 0; k < steps; k++) {
-                        const uint64_t ad = make_smem_desc(a + k * 32, 16, 1024, 2), bd = make_smem_desc(b + k * 32, 16, 1024, 2);
-                        mma4<PAIR>(d, ad, bd, make_idesc(C::kRows, BN, 0) + (k & 1u) * ((2u << 4) + (2u << 29)), sf + (k / 2) * 4,
-                                   sf + 8 + (k / 2) * 4 * C::kNT + half, (kb | k) != 0 ? 1u : 0u);
+                    if (kb == 0 && i >= kBack) {
+                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_free[(i - kBack) & 1u], ((i - kBack) >> 1) & 1u, abort_flag));
+                        if (!ok) break;
+                        tc_fence_after();
                     }
-                    if constexpr (PAIR) umma_commit_pair(&bars->empty[stage]); else umma_commit(&bars->empty[stage]);
+                    if (issue) {
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; k++) {
+                            if (k == 0 || k * 64 < left)
+                                mma4<PAIR>(d, make_smem_desc(a + k * 32, 16, 1024, 2), make_smem_desc(b + k * 32, 16, 1024, 2), make_idesc(C::kRows, BN, (k & 1u) * 2u),
+                                           sf + (k / 2) * 4, sf + 8 + (k / 2) * 4 * C::kNT + half, (kb | k) != 0 ? 1u : 0u);
+                        }
+                        if constexpr (PAIR) umma_commit_pair(&bars->w_empty[stage]); else umma_commit(&bars->w_empty[stage]);
+                        if (last) { if constexpr (PAIR) umma_commit_pair(&bars->a_empty[slot]); else umma_commit(&bars->a_empty[slot]); }
+                        if (kb + 1 == k_blocks) { if constexpr (PAIR) umma_commit_pair(&bars->acc_full[i & 1u]); else umma_commit(&bars->acc_full[i & 1u]); }
+                    }
+                    __syncwarp();
                     sbuf ^= 1u;
                     if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+                    if (++slot == C::kSlots) { slot = 0; sphase ^= 1u; }
                 }
-                if (!ok) break;
-                if constexpr (PAIR) umma_commit_pair(&bars->acc_full[i & 1u]); else umma_commit(&bars->acc_full[i & 1u]);
+                if (last) { panel = slot; pphase = sphase; }
             }
         }
     } else {
         constexpr uint32_t kHalf = BN / 2;                                   // columns of this warp
-        constexpr uint32_t kCols = sizeof(T) == 4 ? 32 : (kHalf < 64 ? kHalf : 64);      // columns taken at once: 128 bytes of a row (64 for a narrow tile)
-        constexpr uint32_t kPieces = kCols * sizeof(T) / 16;                 // 16-byte pieces of a staged row
+        constexpr uint32_t kCols = kHalf < 64 ? kHalf : 64;                  // columns read at once
         const uint32_t quarter = warp & 3u, half = (warp - 2u) >> 2;
-        uint8_t* const stg = staging + (warp - 2u) * 4608u;
-        float* const bias_s = reinterpret_cast<float*>(stg + 4096);
-        const bool vec = (p.ld * sizeof(T)) % 16 == 0 && ((uintptr_t)p.out & 15) == 0;
+        uint8_t* const stg = staging + (warp - 2u) * 4096u;
+        const bool vec = !kPacked && (p.ld * sizeof(T)) % 16 == 0 && ((uintptr_t)p.out & 15) == 0;
+        float* const bias_s = reinterpret_cast<float*>(staging + kEpiWarps * 4096) + half * kHalf;       // shared by the half's four warps
         uint32_t i = 0;
         bool ok = true;
-        for (uint32_t t = unit; t < n_tiles && ok; t += n_units, i++) {
+        for (uint32_t t = t_begin; t < t_end && ok; t++, i++) {
             uint32_t row, tn;
             seg.find(t, C::kRows, row, tn);
             const uint32_t end = p.offsets ? min(p.offsets[seg.e + 1], p.capacity) : (p.n_rows_dev ? min(*p.n_rows_dev, p.capacity) : p.capacity);
             const uint32_t row0 = row + rank * 128 + quarter * 32, col0 = tn * BN + half * kHalf;
-            const float* const bias = p.bias ? p.bias + (size_t)seg.e * p.N : nullptr;
-            for (uint32_t c = lane; c < kHalf; c += 32) bias_s[c] = bias && col0 + c < p.N ? __ldg(bias + col0 + c) : 0.0f;
-            __syncwarp();
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full[i & 1u], (i >> 1) & 1u, abort_flag));
+            // (columns quarter * 32 ... of the half, fetched while the tile is multiplied)
+            const uint32_t bias_c = quarter * (kHalf / 4) + lane;
+            const float bias_v = p.bias && lane < kHalf / 4 && col0 + bias_c < p.N ? __ldg(p.bias + (size_t)seg.e * p.N + col0 + bias_c) : 0.0f;
+            // (the half's four warps go on, or leave, together: they meet again below.  All have written the tile before by now)
+            ok = half_agrees(1u + half, mbar_wait(&bars->acc_full[i & 1u], (i >> 1) & 1u, abort_flag));
             if (!ok) break;
             tc_fence_after();
             const uint32_t taddr = tmem + ((quarter * 32u) << 16) + (i & 1u) * C::kSecond + half * kHalf;
@@ -264,7 +374,7 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    if constexpr (PAIR) mbar_arrive_cluster(map_to_cta(smem_u32(&bars->acc_free[i & 1u]), 0));
+                    if constexpr (PAIR) mbar_arrive_relaxed(map_to_cta(smem_u32(&bars->acc_free[i & 1u]), 0));
                     else mbar_arrive(&bars->acc_free[i & 1u]);
                 }
             };
@@ -279,48 +389,86 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 #pragma unroll
                 for (uint32_t g = 0; g < kCols; g += 32) tmem_ld32(taddr + c + g, *reinterpret_cast<uint32_t(*)[32]>(v + g));
                 tmem_ld_wait();
-                if (shares && (n + 1) * kCols == C::kOverlap) release();
-#pragma unroll
-                for (uint32_t g = 0; g < kCols; g += 4) {
-                    const float4 b = *reinterpret_cast<const float4*>(bias_s + c + g);
-                    float x[4] = {__uint_as_float(v[g]) + b.x, __uint_as_float(v[g + 1]) + b.y, __uint_as_float(v[g + 2]) + b.z, __uint_as_float(v[g + 3]) + b.w};
-                    if (p.relu) {
-#pragma unroll
-                        for (int q = 0; q < 4; q++) x[q] = relu_keep_nan(x[q]);
-                    }
-                    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                        for (int q = 0; q < 4; q++) v[g + q] = __float_as_uint(x[q]);
-                    } else {
-                        v[g / 2] = pack2<T>(x[0], x[1]);
-                        v[g / 2 + 1] = pack2<T>(x[2], x[3]);
-                    }
+                if ((shares && n == 0) || (!C::kOverlap && n + 1 == kHalf / kCols)) release();
+                if (n == 0) {
+                    if (lane < kHalf / 4) bias_s[bias_c] = bias_v;
+                    asm volatile("bar.sync %0, 128;" ::"r"(1u + half) : "memory");
                 }
+                if (col0 + c >= (kPacked ? k_tiles(p.N) * 128 : p.N)) continue;
+                if (p.relu) finish<T, kCols, true>(v, bias_s + c);
+                else finish<T, kCols, false>(v, bias_s + c);
+                if constexpr (kPacked) {
+                    // a lane's 32 consecutive columns are one scale block
+                    const uint32_t pitch = row_bytes(p.N), kt = k_tiles(p.N);
 #pragma unroll
-                for (uint32_t q = 0; q < kPieces; q++)
-                    *reinterpret_cast<uint4*>(stg + lane * 128u + ((q ^ (lane & 7u)) << 4)) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-                __syncwarp();
-                constexpr uint32_t kRowsAt = 32 / kPieces;                   // rows per store instruction
-                const uint32_t q = lane % kPieces;
+                    for (uint32_t g = 0; g < kCols; g += 32) {
+                        const uint32_t col = col0 + c + g;
+                        uint32_t top = 0;
 #pragma unroll
-                for (uint32_t r0 = 0; r0 < 32; r0 += kRowsAt) {
-                    const uint32_t r = r0 + lane / kPieces;
-                    const uint4 val = *reinterpret_cast<const uint4*>(stg + r * 128u + ((q ^ (r & 7u)) << 4));
-                    const uint32_t col = col0 + c + q * (16 / sizeof(T));
-                    if (row0 + r < end && col < p.N) {
-                        T* const o = reinterpret_cast<T*>(p.out) + (size_t)(row0 + r) * p.ld + col;
-                        if (vec && col + 16 / sizeof(T) <= p.N) *reinterpret_cast<uint4*>(o) = val;
-                        else {
-                            const T* const e = reinterpret_cast<const T*>(&val);
+                        for (uint32_t q = 0; q < 32; q++) {
+                            if (col + q >= p.N) v[g + q] = 0;              // columns that fill the last block
+                            top = max(top, v[g + q] & 0x7FFFFFFFu);
+                        }
+                        const uint32_t byte = scale_byte(top);
+                        uint32_t w[4];
 #pragma unroll
-                            for (uint32_t x = 0; x < 16 / sizeof(T); x++) if (col + x < p.N) o[x] = e[x];
+                        for (uint32_t q = 0; q < 4; q++) {
+                            float x[8];
+#pragma unroll
+                            for (uint32_t r = 0; r < 8; r++) x[r] = __uint_as_float(v[g + q * 8 + r]);
+                            w[q] = encode8(x, byte);
+                        }
+                        if (row0 + lane < end) {
+                            if (col < p.N) *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(p.out) + (size_t)(row0 + lane) * pitch + col / 2) = make_uint4(w[0], w[1], w[2], w[3]);
+                            if (col / 32 < kt * 4) p.out_scales[scale_at(row0 + lane, col / 32, kt)] = col < p.N ? (uint8_t)byte : (uint8_t)127;
                         }
                     }
+                } else {
+                    constexpr uint32_t kWords = kCols * sizeof(T) / 4;       // a row's words,
+                    constexpr uint32_t kAt = kWords < 32 ? kWords : 32;      // ... 32 of them (128 bytes) staged at a time, 16-byte pieces
+                    constexpr uint32_t kPieces = kAt / 4;                    // XOR-swizzled by row as a 128-byte swizzled TMA box has them
+                    constexpr uint32_t kPer = 16 / sizeof(T);                // values of a piece
+                    const bool inside = row0 + 32 <= end;
+#pragma unroll
+                    for (uint32_t g = 0; g < kWords; g += kAt) {
+                        const uint32_t col = col0 + c + g / 4 * kPer;
+                        if (tma_out) {                                       // the last box has been read
+                            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                            __syncwarp();
+                        }
+#pragma unroll
+                        for (uint32_t j = 0; j < kPieces; j++)
+                            *reinterpret_cast<uint4*>(stg + lane * 128u + ((j ^ (lane & 7u)) << 4)) = make_uint4(v[g + 4 * j], v[g + 4 * j + 1], v[g + 4 * j + 2], v[g + 4 * j + 3]);
+                        if (tma_out && inside) {                             // (columns beyond N are left out by the map)
+                            fence_proxy_async();
+                            __syncwarp();
+                            if (lane == 0 && col < p.N) {
+                                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                                             ::"l"(reinterpret_cast<uint64_t>(&tmO)), "r"(col), "r"(row0), "r"(smem_u32(stg)) : "memory");
+                                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                            }
+                            continue;
+                        }
+                        __syncwarp();
+                        constexpr uint32_t kRowsAt = 32 / kPieces;           // rows per store instruction
+                        const uint32_t q = lane % kPieces, r = lane / kPieces, at = col + q * kPer;
+                        T* const o = reinterpret_cast<T*>(p.out) + (size_t)(row0 + r) * p.ld + at;
+#pragma unroll
+                        for (uint32_t k = 0; k < 32; k += kRowsAt) {
+                            if (row0 + k + r >= end || at >= p.N) continue;
+                            const uint4 val = *reinterpret_cast<const uint4*>(stg + (k + r) * 128u + ((q ^ ((k + r) & 7u)) << 4));
+                            T* const d = o + (size_t)k * p.ld;
+                            if (vec && at + kPer <= p.N) { *reinterpret_cast<uint4*>(d) = val; continue; }
+                            const T* const e = reinterpret_cast<const T*>(&val);
+#pragma unroll
+                            for (uint32_t x = 0; x < kPer; x++) if (at + x < p.N) d[x] = e[x];
+                        }
+                        __syncwarp();
+                    }
                 }
-                __syncwarp();
             }
-            if (!C::kOverlap) release();
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
 
     __syncthreads();
@@ -343,18 +491,26 @@ int launch(sf_ctx* ctx, const sf_mx4_product& p, cudaStream_t st)
 {
     using C = Cfg<BN, PAIR>;
     const uint32_t pitch = row_bytes(p.K), kt = k_tiles(p.K);
-    CUtensorMap tmA, tmW, tmSA, tmSW;
+    // the most tiles there can be: every expert's last tile may be a part of one
+    const uint64_t most = ((uint64_t)p.capacity / C::kRows + p.E) * (((std::is_same<T, Mx4>::value ? k_tiles(p.N) * 128 : p.N) + BN - 1) / BN);
+    if (most > 0x7FFFFFFFull) return SF_ERR_UNSUPPORTED;
+    CUtensorMap tmA, tmW, tmSA, tmSW, tmO;
     int rc = encode_tmap_2d(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.a, p.capacity, pitch, pitch, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == SF_OK) rc = encode_tmap_2d(&tmW, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.w, (uint64_t)p.E * p.N, pitch, pitch, PAIR ? BN / 2 : BN, 128, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == SF_OK) rc = encode_tmap_2d(&tmSA, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.a_scales, (p.capacity + 127) / 128, kt * 128, kt * 512, 1, 256, CU_TENSOR_MAP_SWIZZLE_NONE);
     if (rc == SF_OK) rc = encode_tmap_2d(&tmSW, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.w_scales, (uint64_t)p.E * ((p.N + 127) / 128), kt * 128, kt * 512, C::kNT, 256, CU_TENSOR_MAP_SWIZZLE_NONE);
+    bool tma_out = false;
+    if constexpr (!std::is_same<T, Mx4>::value) {
+        tma_out = aligned(p.out, 16) && (p.ld * sizeof(T)) % 16 == 0 && (p.N * sizeof(T)) % 16 == 0 && !(BN == 64 && sizeof(T) == 2);      // (64 16-bit columns: a warp has 64 bytes of a row)
+        if (rc == SF_OK && tma_out) rc = encode_tmap_2d(&tmO, sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, p.out,
+                                                        p.capacity, p.N, p.ld * sizeof(T), 32, 128 / sizeof(T), CU_TENSOR_MAP_SWIZZLE_128B);
+    }
+    if (!tma_out) tmO = tmA;                           // not read
     if (rc != SF_OK) return rc;
     auto kern = mx4_product_kernel<BN, PAIR, T>;
     static bool set_dev[64] = {};                      // the opt-in is per device
     bool& set = set_dev[ctx->device & 63];
     if (!set) { SF_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::smem(SF_MAX_EXPERTS))); set = true; }
-    // the most tiles there can be: every expert's last tile may be a part of one
-    const uint64_t most = ((uint64_t)p.capacity / C::kRows + p.E) * ((p.N + BN - 1) / BN);
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((PAIR ? 2u : 1u) * (uint32_t)std::min<uint64_t>((uint64_t)ctx->num_sms / (PAIR ? 2 : 1), most));
     lc.blockDim = dim3(kThreads); lc.dynamicSmemBytes = C::smem(p.E); lc.stream = st;
@@ -364,7 +520,7 @@ int launch(sf_ctx* ctx, const sf_mx4_product& p, cudaStream_t st)
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = 2; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     lc.attrs = at; lc.numAttrs = PAIR ? 2 : 1;
-    SF_CUDA(cudaLaunchKernelEx(&lc, kern, tmA, tmW, tmSA, tmSW, p, ctx->d_state));
+    SF_CUDA(cudaLaunchKernelEx(&lc, kern, tmA, tmW, tmSA, tmSW, tmO, (uint32_t)tma_out, p, ctx->d_state));
     return SF_OK;
 }
 
@@ -392,12 +548,14 @@ template <typename T> bool pairs_supported(const sf_ctx* ctx) {
 
 int check(const sf_ctx* ctx, const sf_mx4_product& p)
 {
-    if (!ctx || !type_ok(p.out_dtype) || p.N == 0 || p.K == 0 || p.K > SF_MX4_MAX_K || p.N > SF_MX4_MAX_K || p.ld < p.N) return SF_ERR_ARG;
+    const bool packed = p.out_dtype == SF_MX4;
+    if (!ctx || (!packed && !type_ok(p.out_dtype)) || p.N == 0 || p.K == 0 || p.K > SF_MX4_MAX_K || p.N > SF_MX4_MAX_K || (!packed && p.ld < p.N)) return SF_ERR_ARG;
     if (p.capacity > 0x7FFFFF00u || (uint64_t)p.E * p.N > 0x7FFFFFFFull) return SF_ERR_ARG;      // tile coordinates are 32-bit signed
     if (p.capacity == 0) return SF_OK;
     if (!p.a || !p.a_scales || !p.w || !p.w_scales || !p.out) return SF_ERR_ARG;
     if (!aligned(p.a, 16) || !aligned(p.a_scales, 16) || !aligned(p.w, 16) || !aligned(p.w_scales, 16)) return SF_ERR_ARG;
-    if (!aligned(p.out, type_bytes(p.out_dtype)) || !aligned(p.bias, 4) || !aligned(p.n_rows_dev, 4) || !aligned(p.offsets, 4)) return SF_ERR_ARG;
+    if (packed != (p.out_scales != nullptr) || !aligned(p.out_scales, 16)) return SF_ERR_ARG;
+    if (!aligned(p.out, packed ? 16 : type_bytes(p.out_dtype)) || !aligned(p.bias, 4) || !aligned(p.n_rows_dev, 4) || !aligned(p.offsets, 4)) return SF_ERR_ARG;
     return SF_OK;
 }
 
@@ -409,18 +567,19 @@ int sf_launch_mx4_product(sf_ctx* ctx, const sf_mx4_product& p, cudaStream_t st)
     const uint64_t rows = std::max<uint64_t>(1, p.capacity / p.E);
     const bool pairs = p.N > 128 && rows >= 256 && (rows + 255) / 256 * p.E * ((p.N + 255) / 256) >= (uint64_t)ctx->num_sms / 2;
     const bool narrow = (rows + 127) / 128 * p.E * ((p.N + 127) / 128) < (uint64_t)ctx->num_sms;
-    return by_type(p.out_dtype, [&](auto zero) {
+    auto go = [&](auto zero) {
         typedef decltype(zero) T;
         if (pairs && pairs_supported<T>(ctx)) return launch<256, true, T>(ctx, p, st);
         return narrow ? launch<64, false, T>(ctx, p, st) : launch<128, false, T>(ctx, p, st);
-    });
+    };
+    return p.out_scales ? go(Mx4()) : by_type(p.out_dtype, go);
 }
 
 extern "C" int sf_mx4_matmul(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_scales, const uint32_t* n_rows_dev, uint32_t capacity,
                              const uint8_t* w, const uint8_t* w_scales, uint32_t N, uint32_t K, const float* bias, int relu,
-                             int out_dtype, void* out, size_t ld, void* stream)
+                             int out_dtype, void* out, size_t ld, uint8_t* out_scales, void* stream)
 {
-    const sf_mx4_product p = {a, a_scales, n_rows_dev, nullptr, 1, capacity, w, w_scales, N, K, bias, relu, out_dtype, out, ld, nullptr};
+    const sf_mx4_product p = {a, a_scales, n_rows_dev, nullptr, 1, capacity, w, w_scales, N, K, bias, relu, out_dtype, out, ld, out_scales};
     const int rc = check(ctx, p);
     if (rc != SF_OK || capacity == 0) return rc;
     SF_ON_DEVICE(ctx);
@@ -429,10 +588,10 @@ extern "C" int sf_mx4_matmul(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_sca
 
 extern "C" int sf_mx4_matmul_experts(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_scales, const uint32_t* offsets, uint32_t E,
                                      uint32_t capacity, const uint8_t* w, const uint8_t* w_scales, uint32_t N, uint32_t K,
-                                     const float* bias, int relu, int out_dtype, void* out, size_t ld, void* stream)
+                                     const float* bias, int relu, int out_dtype, void* out, size_t ld, uint8_t* out_scales, void* stream)
 {
     if (E == 0 || E > SF_MAX_EXPERTS || (capacity && !offsets)) return SF_ERR_ARG;
-    const sf_mx4_product p = {a, a_scales, nullptr, offsets, E, capacity, w, w_scales, N, K, bias, relu, out_dtype, out, ld, nullptr};
+    const sf_mx4_product p = {a, a_scales, nullptr, offsets, E, capacity, w, w_scales, N, K, bias, relu, out_dtype, out, ld, out_scales};
     const int rc = check(ctx, p);
     if (rc != SF_OK || capacity == 0) return rc;
     SF_ON_DEVICE(ctx);

@@ -274,7 +274,8 @@ def test_product_nan_blocks_stay_in_their_rows_and_columns(env):
 
 
 @pytest.mark.parametrize("kind", ["fp32", "bf16"])
-@pytest.mark.parametrize("counts,K,N", [([1], 64, 8), ([200, 0, 1, 129, 0, 383], 416, 200), ([0, 0, 0], 128, 64), ([5] * 40, 96, 33), ([1000, 30, 257], 1024, 512)])
+@pytest.mark.parametrize("counts,K,N", [([1], 64, 8), ([200, 0, 1, 129, 0, 383], 416, 200), ([0, 0, 0], 128, 64), ([5] * 40, 96, 33), ([1000, 30, 257], 1024, 512),
+                                        ([3] * 300, 64, 70), ([4000, 700, 9000, 300], 2304, 300)])
 def test_product_by_expert(env, counts, K, N, kind):
     sf, ctx = env
     rng = np.random.default_rng(len(counts) + K)
@@ -388,6 +389,77 @@ def test_product_of_many_rows(env, n, K, N, E, kind):
         lo, hi = int(offsets[e]), int(offsets[e + 1])
         check_rows(out[lo:hi], ra[lo:hi], ws[e][2], bias[e].double(), True, kind)
     assert (out[int(offsets[-1]):] == 7).all()
+
+
+def check_packed_product(sf, ctx, data, scales, rows, N, a, w, bias):
+    """Packed outputs against the definition applied to the exact product.  A sum that is off by `slack` may fall on the other side of
+    a border between two codes (or, for the largest of a block, of a power of two): a value has to be what some sum within
+    slack of the exact one is rounded to, with the scale that the kernel chose, and that scale what some largest magnitude gives."""
+    K = a.shape[1]
+    exact = np.maximum(a @ w.T + bias, 0)
+    slack = (K + 2) * 2.0 ** -23 * (np.abs(a) @ np.abs(w).T + np.abs(bias))
+    Np, kt = -(-N // 32) * 32, -(-N // 128)
+    byte = scales.cpu().numpy()[pr.scale_index(len(exact), N)]
+    assert (byte[:, Np // 32:] == 127).all()
+    lo, hi = np.zeros((len(exact), Np)), np.zeros((len(exact), Np))
+    lo[:, :N], hi[:, :N] = np.maximum(exact - slack, 0), exact + slack
+    e = byte[:, :Np // 32].astype(int) - 127
+    e_of = lambda m: pr.quantise(m.reshape(-1, 1))[1].reshape(m.shape).astype(int) - 127  # noqa: E731
+    assert (e >= e_of(lo.reshape(len(exact), -1, 32).max(-1))).all() and (e <= e_of(hi.reshape(len(exact), -1, 32).max(-1))).all()
+    d = data.cpu().numpy()
+    code = np.stack([d & 15, d >> 4], -1).reshape(len(exact), Np)
+    assert (code < 8).all()
+    unit = np.repeat(2.0 ** e, 32, axis=1)
+    assert (code >= pr.nearest_code(np.minimum(lo / unit, 6))).all() and (code <= pr.nearest_code(np.minimum(hi / unit, 6))).all()
+
+
+@pytest.mark.parametrize("n,K,N", [(1, 32, 1), (10, 1024, 1024), (300, 416, 200), (129, 96, 130), (70, 2304, 64), (257, 256, 33), (2000, 640, 1024), (6000, 512, 1000)])
+def test_product_packed_again(env, n, K, N):
+    sf, ctx = env
+    rng = np.random.default_rng(n + K + N)
+    a, w, ra, rw = operands(rng, n, N, K)
+    pa, pw = [dev(v) for v in pr.pack(a)], [dev(v) for v in pr.pack(w)]
+    bias = rng.normal(size=N).astype(np.float32)
+    data = torch.full((n, -(-N // 32) * 16), 0xAA, dtype=torch.uint8, device="cuda")
+    scales = torch.full((sf.sf_mx4_sizes(n, N)[1],), 0x55, dtype=torch.uint8, device="cuda")
+    count = max(1, n - 3)
+    sf.sf_mx4_matmul(ctx, pa[0], pa[1], pw[0], pw[1], K, data, bias=dev(bias), relu=True, n_rows_dev=dev(np.array([count], np.int32)), out_scales=scales, N=N)
+    check_packed_product(sf, ctx, data[:count], scales, count, N, ra[:count], rw, bias)
+    got = scales.cpu().numpy()
+    rest = np.ones(got.size, bool)
+    rest[pr.scale_index(count, N).reshape(-1)] = False
+    assert (got[rest] == 0x55).all() and (data[count:] == 0xAA).all()
+    sf.sf_ctx_poll(ctx)
+
+
+def test_product_packed_again_by_expert_and_nan(env):
+    sf, ctx = env
+    rng = np.random.default_rng(31)
+    E, N, K = 3, 96, 160
+    offsets = np.array([0, 128, 128, 512], np.int32)
+    a, w, _, rw = operands(rng, 512, E * N, K)
+    a[200, 3] = np.nan
+    ra = pr.rounded(a)
+    pa = [dev(v) for v in pr.pack(a)]
+    packed = [pr.pack(w[e * N:(e + 1) * N]) for e in range(E)]
+    bias = rng.normal(size=(E, N)).astype(np.float32)
+    data = torch.full((512, N // 2), 0xAA, dtype=torch.uint8, device="cuda")
+    scales = torch.full((sf.sf_mx4_sizes(512, N)[1],), 0x55, dtype=torch.uint8, device="cuda")
+    sf.sf_mx4_matmul_experts(ctx, pa[0], pa[1], dev(np.stack([p[0] for p in packed])), dev(np.stack([p[1] for p in packed])), K, dev(offsets), data,
+                             bias=dev(bias), relu=True, out_scales=scales, N=N)
+    s = scales.cpu().numpy()[pr.scale_index(512, N)]
+    assert (s[200, :3] == 255).all() and (np.delete(s, 200, 0) != 255).all()
+    for e, lo, hi in ((0, 0, 128), (2, 128, 256), (2, 256, 384), (2, 384, 512)):
+        keep = [r for r in range(lo, hi) if r != 200]
+        at = scales[lo * 4:hi * 4]                       # a 128-row block of one k tile is 512 bytes
+        sub = at.clone()
+        if lo <= 200 < hi:
+            continue
+        check_packed_product(sf, ctx, data[lo:hi], sub, hi - lo, N, ra[lo:hi], rw[e * N:(e + 1) * N], bias[e])
+        assert len(keep) == hi - lo
+    with pytest.raises(sf.SfError):
+        sf.sf_mx4_matmul(ctx, pa[0], pa[1], dev(packed[0][0]), dev(packed[0][1]), K, data[:, :32].contiguous(), out_scales=scales, N=N)
+    sf.sf_ctx_poll(ctx)
 
 
 def test_captured_replayed_and_on_another_stream(env):

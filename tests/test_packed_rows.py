@@ -73,8 +73,8 @@ def test_no_context_is_refused(sf):
     L = sf._lib()
     assert L.sf_mx4_quantise(None, 16, 0, 1, 32, 32, None, None, 1, 16, 16, None) == sf.SF_ERR_ARG
     assert L.sf_mx4_unpack(None, 16, 16, None, 1, 32, 0, 16, 32, None) == sf.SF_ERR_ARG
-    assert L.sf_mx4_matmul(None, 16, 16, None, 1, 16, 16, 1, 32, None, 0, 0, 16, 1, None) == sf.SF_ERR_ARG
-    assert L.sf_mx4_matmul_experts(None, 16, 16, 16, 1, 1, 16, 16, 1, 32, None, 0, 0, 16, 1, None) == sf.SF_ERR_ARG
+    assert L.sf_mx4_matmul(None, 16, 16, None, 1, 16, 16, 1, 32, None, 0, 0, 16, 1, None, None) == sf.SF_ERR_ARG
+    assert L.sf_mx4_matmul_experts(None, 16, 16, 16, 1, 1, 16, 16, 1, 32, None, 0, 0, 16, 1, None, None) == sf.SF_ERR_ARG
     assert L.sf_expert_gate(None, 16, 0, None, 1, 4, 4, 1, 0, 16, 16, None) == sf.SF_ERR_ARG
     assert L.sf_expert_gate_backward(None, 16, 0, None, 1, 4, 4, 1, 0, 16, 16, 16, 4, None) == sf.SF_ERR_ARG
     assert L.sf_expert_sort(None, 16, None, 1, 1, 1, 1, 1, 16, 16, 16, 16, None, 0, None) == sf.SF_ERR_ARG
