@@ -176,10 +176,20 @@ def _dp(t):
     return t.data_ptr()
 
 
+_current = None
+
+
 def _stream(stream):
+    """Address of a stream; None = torch's current one (asked for through torch's raw accessors where it has them: a torch.cuda.Stream
+    object per call costs more than a small launch)."""
+    global _current
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _current is None:
+            import torch
+            raw, dev = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+            torch.cuda.current_stream()               # initialises CUDA
+            _current = (lambda: raw(dev())) if raw and dev else (lambda: torch.cuda.current_stream().cuda_stream)
+        return _current()
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -383,25 +393,31 @@ def _rows(t, where):
     if not _TYPES:
         import torch
         _TYPES.update({torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16})
-    code = _TYPES.get(t.dtype)
-    _arg(code is not None and t.is_cuda and t.dim() == 2, where)
-    n, d = t.shape
-    s0, s1 = t.stride()
-    _arg((d <= 1 or s1 == 1) and (n <= 1 or s0 >= d), where)
-    return t.data_ptr(), code, n, d, (s0 if n > 1 else d)
+    code, shape = _TYPES.get(t.dtype), t.shape
+    if code is None or len(shape) != 2 or not t.is_cuda:
+        raise SfError(SF_ERR_ARG, where)
+    n, d = shape
+    ld, s1 = t.stride()
+    if n <= 1:
+        ld = d
+    if ld < d or (d > 1 and s1 != 1):
+        raise SfError(SF_ERR_ARG, where)
+    return t.data_ptr(), code, n, d, ld
 
 
 def _flat(t, count, size, where):
     """Address of a contiguous device tensor of at least `count` elements of `size` bytes; None stays None."""
     if t is None:
         return None
-    _arg(t.is_cuda and t.is_contiguous() and t.numel() >= count and t.element_size() == size, where)
+    if not t.is_cuda or t.itemsize != size or t.nbytes < count * size or not t.is_contiguous():
+        raise SfError(SF_ERR_ARG, where)
     return t.data_ptr()
 
 
 def _whole(t, shape, where):
     """Address of a contiguous 4-byte device tensor of this shape."""
-    _arg(t.is_cuda and t.is_contiguous() and t.element_size() == 4 and tuple(t.shape) == shape, where)
+    if not t.is_cuda or t.itemsize != 4 or t.shape != shape or not t.is_contiguous():
+        raise SfError(SF_ERR_ARG, where)
     return t.data_ptr()
 
 

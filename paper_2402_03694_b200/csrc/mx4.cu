@@ -15,79 +15,138 @@ using namespace sfrow;
 using namespace sfmx;
 
 constexpr uint32_t kQThreads = 256;
-constexpr uint32_t kQCols = 256;                   // columns a warp takes at once: 8 per lane, 4 lanes to a scale block
+constexpr uint32_t kPCols = 512;                   // columns a warp packs or unpacks at once: 16 per lane, 2 lanes to a scale block
 
-// x[rows][ld] -> data[rows][pitch], scales (tiles).  Bound: HBM (reads 2 or 4 bytes a value, writes 17/32).  A warp takes 256
-// consecutive values of one row (one 16-byte load per lane for 16-bit types, 8 four-bit codes = one 4-byte store per lane);
-// the block's maximum is taken over 4 lanes.  Items are (row, 256 columns), kUnroll of them in flight per warp.
-template <typename T, bool ALIGNED>
+// bits of the largest magnitude of 16 values, as fp32: magnitudes order as their bits do, so 16-bit values are compared in pairs
+// as they are
+__device__ __forceinline__ uint32_t top_bits(const uint4 (&q)[4], float) {
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        t = max(max(t, q[i].x & 0x7FFFFFFFu), q[i].y & 0x7FFFFFFFu);
+        t = max(max(t, q[i].z & 0x7FFFFFFFu), q[i].w & 0x7FFFFFFFu);
+    }
+    return t;
+}
+__device__ __forceinline__ uint32_t top_16(const uint4 (&q)[2]) {
+    uint32_t t = __vimax3_u16x2(q[0].x & 0x7FFF7FFFu, q[0].y & 0x7FFF7FFFu, q[0].z & 0x7FFF7FFFu);
+    t = __vimax3_u16x2(t, q[0].w & 0x7FFF7FFFu, q[1].x & 0x7FFF7FFFu);
+    t = __vimax3_u16x2(t, q[1].y & 0x7FFF7FFFu, q[1].z & 0x7FFF7FFFu);
+    t = __vimax3_u16x2(t, q[1].w & 0x7FFF7FFFu, 0u);
+    return max(t & 0xFFFFu, t >> 16);
+}
+__device__ __forceinline__ uint32_t top_bits(const uint4 (&q)[2], __nv_bfloat16) { return top_16(q) << 16; }
+__device__ __forceinline__ uint32_t top_bits(const uint4 (&q)[2], __half) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)top_16(q)))); }
+
+// x[rows][ld] -> data[rows][pitch], scales (tiles).  Bound: HBM (reads 2 or 4 bytes a value, writes 17/32).  A warp takes 512
+// consecutive values of one row (16 per lane: two or four 16-byte loads, one 8-byte store), a block's maximum is taken over two
+// lanes, and U such pieces are on their way before the first is packed.  Smaller pieces one at a time (8 values a lane) ran
+// at 2.9 TB/s at 240,001 x 2048 bf16.
+template <typename T, bool ALIGNED, int U>
 __global__ void __launch_bounds__(kQThreads)
 mx4_quantise_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, size_t ld, const int32_t* __restrict__ row_ids,
                     const uint32_t* __restrict__ n_rows_dev, uint32_t capacity, uint8_t* __restrict__ data,
                     uint8_t* __restrict__ scales, sf_dev_state* st)
 {
+    constexpr int Q = sizeof(T);                       // 16-byte words of 16 values
     sf_chain_enter();
     const uint32_t rows = n_rows_dev ? sf_clamp_rows(*n_rows_dev, capacity, st) : capacity;
     const uint32_t pitch = row_bytes(K), blocks = pitch / 16, kt = k_tiles(K);
-    const uint32_t chunks = (kt * 128 + kQCols - 1) / kQCols;
+    const uint32_t chunks = (kt * 128 + kPCols - 1) / kPCols;
     const uint32_t lane = threadIdx.x & 31;
     const uint64_t items = (uint64_t)rows * chunks;
-    const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32);
-    for (uint64_t i = (uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5); i < items; i += step) {
-        const uint32_t row = (uint32_t)(i / chunks), c = (uint32_t)(i - (uint64_t)row * chunks);
-        const uint32_t k = c * kQCols + lane * 8;
-        int64_t src = row;
-        if (row_ids) { const int32_t id = row_ids[row]; src = (id >= 0 && (uint32_t)id < n_src) ? id : -1; }
-        float v[8];
+    const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32) * U;
+    for (uint64_t i0 = ((uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5)) * U; i0 < items; i0 += step) {
+        union Words { uint4 q[Q]; T e[16]; } w[U];
+        uint32_t row[U], k[U];
+        uint32_t r = (uint32_t)(i0 / chunks), c = (uint32_t)(i0 - (uint64_t)r * chunks);
 #pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = 0.0f;
-        if (src >= 0 && k < K) {
-            const T* p = x + (size_t)src * ld + k;
-            if (ALIGNED && k + 8 <= K) load_f32<T, 8, ALIGNED>(p, v);
-            else {
+        for (int u = 0; u < U; u++) {
+            row[u] = r;
+            k[u] = c * kPCols + lane * 16;
+            if (++c == chunks) { c = 0; r++; }
+            int64_t src = i0 + u < items ? (int64_t)row[u] : -1;
+            if (row_ids && src >= 0) { const int32_t id = row_ids[row[u]]; src = (id >= 0 && (uint32_t)id < n_src) ? id : -1; }
 #pragma unroll
-                for (int j = 0; j < 8; j++) if (k + j < K) v[j] = to_f32(p[j]);
+            for (int q = 0; q < Q; q++) w[u].q[q] = make_uint4(0, 0, 0, 0);
+            if (src >= 0 && k[u] < K) {
+                const T* p = x + (size_t)src * ld + k[u];
+                if (ALIGNED && k[u] + 16 <= K) {
+#pragma unroll
+                    for (int q = 0; q < Q; q++) w[u].q[q] = __ldg(reinterpret_cast<const uint4*>(p) + q);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; j++) if (k[u] + j < K) w[u].e[j] = p[j];
+                }
             }
         }
-        uint32_t top = 0;                          // bits of the block's largest magnitude: they order as the values do
 #pragma unroll
-        for (int j = 0; j < 8; j++) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        const uint32_t byte = scale_byte(top);
-        const uint32_t codes = encode8(v, byte);
-        if (k < pitch * 2) *reinterpret_cast<uint32_t*>(data + (size_t)row * pitch + k / 2) = codes;
-        if ((lane & 3) == 0) {
-            const uint32_t b = k / 32;
-            if (b < kt * 4) scales[scale_at(row, b, kt)] = b < blocks ? (uint8_t)byte : (uint8_t)127;
+        for (int u = 0; u < U; u++) {
+            if (i0 + u >= items) break;                // (the same in all lanes)
+            uint32_t top = top_bits(w[u].q, T());
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            const uint32_t byte = scale_byte(top);
+            float v[8];
+            uint2 codes;
+#pragma unroll
+            for (int j = 0; j < 8; j++) v[j] = to_f32(w[u].e[j]);
+            codes.x = encode8(v, byte);
+#pragma unroll
+            for (int j = 0; j < 8; j++) v[j] = to_f32(w[u].e[8 + j]);
+            codes.y = encode8(v, byte);
+            if (k[u] < pitch * 2) *reinterpret_cast<uint2*>(data + (size_t)row[u] * pitch + k[u] / 2) = codes;
+            if ((lane & 1) == 0) {
+                const uint32_t b = k[u] / 32;
+                if (b < kt * 4) scales[scale_at(row[u], b, kt)] = b < blocks ? (uint8_t)byte : (uint8_t)127;
+            }
         }
     }
 }
 
-// data, scales -> out[rows][ld].  The same split as above, the other way round.  Bound: HBM.
-template <typename T, bool ALIGNED>
+// data, scales -> out[rows][ld].  The same split the other way round: 16 values a lane, whole 32-byte sectors where rows are on
+// 32-byte boundaries (SECTORS).  Bound: HBM writes (this card writes 3.9 TB/s where it copies 6.5).
+template <typename T, bool SECTORS>
 __global__ void __launch_bounds__(kQThreads)
 mx4_unpack_kernel(const uint8_t* __restrict__ data, const uint8_t* __restrict__ scales, const uint32_t* __restrict__ n_rows_dev,
                   uint32_t capacity, uint32_t K, T* __restrict__ out, size_t ld, sf_dev_state* st)
 {
+    constexpr int U = 2;
     sf_chain_enter();
     const uint32_t rows = n_rows_dev ? sf_clamp_rows(*n_rows_dev, capacity, st) : capacity;
     const uint32_t pitch = row_bytes(K), kt = k_tiles(K);
-    const uint32_t chunks = (K + kQCols - 1) / kQCols;
+    const uint32_t chunks = (K + kPCols - 1) / kPCols;
     const uint32_t lane = threadIdx.x & 31;
     const uint64_t items = (uint64_t)rows * chunks;
-    const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32);
-    for (uint64_t i = (uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5); i < items; i += step) {
-        const uint32_t row = (uint32_t)(i / chunks), c = (uint32_t)(i - (uint64_t)row * chunks);
-        const uint32_t k = c * kQCols + lane * 8;
-        if (k >= K) continue;
-        float v[8];
-        decode8(*reinterpret_cast<const uint32_t*>(data + (size_t)row * pitch + k / 2), scale_f32(scales[scale_at(row, k / 32, kt)]), v);
-        T* p = out + (size_t)row * ld + k;
-        if (ALIGNED && k + 8 <= K) store_f32<T, 8, ALIGNED>(p, v);
-        else {
+    const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32) * U;
+    for (uint64_t i0 = ((uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5)) * U; i0 < items; i0 += step) {
+        uint32_t r = (uint32_t)(i0 / chunks), c = (uint32_t)(i0 - (uint64_t)r * chunks);
+        uint2 codes[U];
+        uint32_t byte[U], row[U], k[U];
 #pragma unroll
-            for (int j = 0; j < 8; j++) if (k + j < K) p[j] = from_f32<T>(v[j]);
+        for (int u = 0; u < U; u++) {
+            row[u] = r;
+            k[u] = c * kPCols + lane * 16;
+            if (++c == chunks) { c = 0; r++; }
+            if (i0 + u < items && k[u] < K) {
+                codes[u] = __ldg(reinterpret_cast<const uint2*>(data + (size_t)row[u] * pitch + k[u] / 2));
+                byte[u] = __ldg(scales + scale_at(row[u], k[u] / 32, kt));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (i0 + u >= items || k[u] >= K) continue;
+            const float scale = scale_f32(byte[u]);
+            float a[8], b[8], v[16];
+            decode8(codes[u].x, scale, a);
+            decode8(codes[u].y, scale, b);
+#pragma unroll
+            for (int j = 0; j < 8; j++) { v[j] = a[j]; v[8 + j] = b[j]; }
+            T* p = out + (size_t)row[u] * ld + k[u];
+            if (SECTORS && k[u] + 16 <= K) store_sectors<T, 16>(p, v);
+            else {
+#pragma unroll
+                for (int j = 0; j < 16; j++) if (k[u] + j < K) p[j] = from_f32<T>(v[j]);
+            }
         }
     }
 }
@@ -123,12 +182,14 @@ extern "C" int sf_mx4_quantise(sf_ctx* ctx, const void* x, int dtype, uint32_t n
 int sf_launch_mx4_quantise(sf_ctx* ctx, const void* x, int dtype, uint32_t n_src, uint32_t K, size_t ld, const int32_t* row_ids,
                            const uint32_t* n_rows_dev, uint32_t capacity, uint8_t* data, uint8_t* scales, cudaStream_t st)
 {
-    const uint32_t grid = row_grid(ctx, (uint64_t)capacity * ((k_tiles(K) * 128 + kQCols - 1) / kQCols), 8);
+    const uint64_t items = (uint64_t)capacity * ((k_tiles(K) * 128 + kPCols - 1) / kPCols);
     const bool al = aligned(x, 16) && (ld * type_bytes(dtype)) % 16 == 0;
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        auto k = al ? mx4_quantise_kernel<T, true> : mx4_quantise_kernel<T, false>;
-        SF_CUDA(sf_launch_chained(k, grid, kQThreads, 0, st, (const T*)x, n_src, K, ld, row_ids, n_rows_dev, capacity, data, scales, ctx->d_state));
+        constexpr int U = 8 / sizeof(T);               // 8 16-byte words a lane on their way, where there are pieces enough for all warps
+        const bool many = items >= (uint64_t)ctx->num_sms * 64 * U;
+        auto k = al ? (many ? mx4_quantise_kernel<T, true, U> : mx4_quantise_kernel<T, true, 1>) : mx4_quantise_kernel<T, false, 1>;
+        SF_CUDA(sf_launch_chained(k, row_grid(ctx, al && many ? (items + U - 1) / U : items, 32), kQThreads, 0, st, (const T*)x, n_src, K, ld, row_ids, n_rows_dev, capacity, data, scales, ctx->d_state));
         return SF_OK;
     });
 }
@@ -141,8 +202,8 @@ extern "C" int sf_mx4_unpack(sf_ctx* ctx, const uint8_t* data, const uint8_t* sc
     if (!data || !scales || !out) return SF_ERR_ARG;
     if (!aligned(out, type_bytes(dtype)) || !aligned(data, 16) || !aligned(scales, 16) || !aligned(n_rows_dev, 4)) return SF_ERR_ARG;
     SF_ON_DEVICE(ctx);
-    const uint32_t grid = row_grid(ctx, (uint64_t)capacity * ((K + kQCols - 1) / kQCols), 8);
-    const bool al = aligned(out, 16) && (ld * type_bytes(dtype)) % 16 == 0;
+    const uint32_t grid = row_grid(ctx, ((uint64_t)capacity * ((K + kPCols - 1) / kPCols) + 1) / 2, 8);
+    const bool al = aligned(out, 32) && (ld * type_bytes(dtype)) % 32 == 0;
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
         auto k = al ? mx4_unpack_kernel<T, true> : mx4_unpack_kernel<T, false>;

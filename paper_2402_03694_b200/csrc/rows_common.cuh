@@ -14,9 +14,7 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
-// N consecutive elements of T: one 16-byte access (two for 8 floats) where ALIGNED, else one access per element
-template <typename T, int N> struct alignas(16) Pack { T v[N]; };
-
+// N consecutive elements of T: 16-byte accesses where ALIGNED, else one access per element
 template <typename T, int N, bool ALIGNED>
 __device__ __forceinline__ void load_f32(const T* __restrict__ p, float (&x)[N]) {
     if constexpr (ALIGNED) {
@@ -43,6 +41,33 @@ __device__ __forceinline__ void store_f32(T* __restrict__ p, const float (&x)[N]
 #pragma unroll
         for (int i = 0; i < N; i++) p[i] = from_f32<T>(x[i]);
     }
+}
+
+// N elements as whole 32-byte accesses (p on a 32-byte boundary): a lane that has 32 bytes or more of a row to itself then moves whole
+// sectors, where 16-byte stores would send every sector twice
+template <typename T, int N>
+__device__ __forceinline__ void load_sectors(const T* __restrict__ p, float (&x)[N]) {
+    static_assert((N * sizeof(T)) % 32 == 0, "whole sectors");
+    union { uint32_t w[N * sizeof(T) / 4]; T e[N]; } u;
+#pragma unroll
+    for (int i = 0; i < (int)(N * sizeof(T) / 32); i++)
+        asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(u.w[8 * i]), "=r"(u.w[8 * i + 1]), "=r"(u.w[8 * i + 2]), "=r"(u.w[8 * i + 3]), "=r"(u.w[8 * i + 4]), "=r"(u.w[8 * i + 5]),
+                       "=r"(u.w[8 * i + 6]), "=r"(u.w[8 * i + 7]) : "l"(reinterpret_cast<const char*>(p) + 32 * i));
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = to_f32(u.e[i]);
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_sectors(T* __restrict__ p, const float (&x)[N]) {
+    static_assert((N * sizeof(T)) % 32 == 0, "whole sectors");
+    union { uint32_t w[N * sizeof(T) / 4]; T e[N]; } u;
+#pragma unroll
+    for (int i = 0; i < N; i++) u.e[i] = from_f32<T>(x[i]);
+#pragma unroll
+    for (int i = 0; i < (int)(N * sizeof(T) / 32); i++)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(reinterpret_cast<char*>(p) + 32 * i), "r"(u.w[8 * i]), "r"(u.w[8 * i + 1]), "r"(u.w[8 * i + 2]), "r"(u.w[8 * i + 3]), "r"(u.w[8 * i + 4]),
+                       "r"(u.w[8 * i + 5]), "r"(u.w[8 * i + 6]), "r"(u.w[8 * i + 7]) : "memory");
 }
 
 // ---- host ---------------------------------------------------------------------
