@@ -28,10 +28,12 @@ __device__ __forceinline__ void load_scores(const T* __restrict__ p, uint32_t E,
         for (int v = 0; v < V; v++) s[v] = first + v < E ? to_f32(p[first + v]) : kNegInf;
     }
 #pragma unroll
-    for (int v = 0; v < V; v++) s[v] = s[v] > kNegInf ? s[v] : kNegInf;          // a NaN is never picked and adds nothing
+    for (int v = 0; v < V; v++) s[v] = fmaxf(s[v], kNegInf);                      // a NaN is never picked and adds nothing
 }
-// exp(s - m) with the largest score (an infinite one too) at 1 and masked ones at 0
-__device__ __forceinline__ float near_top(float s, float m) { return s == kNegInf ? 0.0f : (s == m ? 1.0f : expf(s - m)); }
+// exp(s - m) with the largest score m at 1 and masked ones at 0; an infinite m (nothing left, or an infinite score) has no difference
+__device__ __forceinline__ float near_top(float s, float m, bool finite) {
+    return finite ? expf(s - m) : (s == m && s != kNegInf ? 1.0f : 0.0f);
+}
 
 template <int LPR> __device__ __forceinline__ float sum_lanes(float v) {
 #pragma unroll
@@ -45,9 +47,9 @@ template <int LPR> __device__ __forceinline__ float max_lanes(float v) {
 }
 
 // A lane keeps the picks of rounds j with j % LPR == lane; S of them (k <= S * LPR).
-template <typename T, int LPR, int V, int S, bool ALIGNED>
+template <typename T, int LPR, int V, int S, int mode, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads)
-gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t E, size_t ld, uint32_t k, int mode,
+gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t E, size_t ld, uint32_t k,
             int32_t* __restrict__ ids, float* __restrict__ weights, sf_dev_state* st)
 {
     sf_chain_enter();
@@ -65,6 +67,7 @@ gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, ui
         for (int v = 0; v < V; v++) left[v] = s[v];
         float best_s[S]; int best_id[S];
         float m = 0.0f, total = 0.0f;
+        bool finite = true;
 #pragma unroll
         for (int v = 0; v < S; v++) { best_s[v] = kNegInf; best_id[v] = -1; }
         for (uint32_t j = 0; j < k; j++) {
@@ -78,17 +81,17 @@ gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, ui
                 if (ob > b || (ob == b && oid < id)) { b = ob; id = oid; }
             }
             if (b == kNegInf) id = -1;
-            if (j == 0) m = b;
+            if (j == 0) { m = b; finite = fabsf(m) < -kNegInf; }
 #pragma unroll
             for (int v = 0; v < V; v++) if (id == (int)(lane * V) + v) left[v] = kNegInf;
 #pragma unroll
             for (int v = 0; v < S; v++) if (j == (uint32_t)v * LPR + lane) { best_s[v] = b; best_id[v] = id; }
-            if (id >= 0) total += mode == SF_GATE_SHARE ? b : near_top(b, m);
+            if (mode != SF_GATE_SOFTMAX && id >= 0) total += mode == SF_GATE_SHARE ? b : near_top(b, m, finite);
         }
         if (mode == SF_GATE_SOFTMAX) {
             float t = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; v++) t += near_top(s[v], m);
+            for (int v = 0; v < V; v++) t += near_top(s[v], m, finite);
             total = sum_lanes<LPR>(t);
         }
         if (live) {
@@ -96,7 +99,7 @@ gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, ui
             for (int v = 0; v < S; v++) {
                 const uint32_t j = v * LPR + lane;
                 if (j < k) {
-                    const float top = mode == SF_GATE_SHARE ? best_s[v] : near_top(best_s[v], m);
+                    const float top = mode == SF_GATE_SHARE ? best_s[v] : near_top(best_s[v], m, finite);
                     ids[row * k + j] = best_id[v];
                     weights[row * k + j] = best_id[v] >= 0 && total > 0.0f ? top / total : 0.0f;
                 }
@@ -106,11 +109,14 @@ gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, ui
 }
 
 // With p the weights' softmax (over all experts, or over the picked ones) and g the weights' gradient at the picked experts:
-// d_s = p (g - sum g p); for shares d_s = (g - sum g w) / sum s at the picked experts.
-template <typename T, int LPR, int V, bool ALIGNED>
+// d_s = p (g - sum g p); for shares d_s = (g - sum g w) / sum s at the picked experts.  Away from the picked experts that is
+// -p sum g p, or nothing, so a lane writes its part of the row without looking at the picks, and then the picked ones that are its own,
+// whose scores it reads again by their ids: comparing every id with every expert in registers took twice as long (61 us at
+// 1,000,000 x 16, k = 2).  Picks are fetched four at a time.
+template <typename T, int LPR, int V, int mode, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads)
 gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t E, size_t ld, uint32_t k,
-                     int mode, const int32_t* __restrict__ ids, const float* __restrict__ d_weights, T* __restrict__ d_scores, size_t ldd,
+                     const int32_t* __restrict__ ids, const float* __restrict__ d_weights, T* d_scores, size_t ldd,
                      sf_dev_state* st)
 {
     sf_chain_enter();
@@ -121,53 +127,71 @@ gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ 
         const uint64_t row = base + threadIdx.x / LPR;
         const bool live = row < rows;
         const uint64_t at = live ? row : base;
-        float s[V], g[V];
-        load_scores<T, LPR, V, ALIGNED>(scores + at * ld, E, lane * V, s);
-        uint32_t picked = 0;                           // bit v: expert lane * V + v
+        const T* const x = scores + at * ld;
+        uint32_t id[4];
+        float g[4], sp[4];                             // of a pick that does not count: -inf and 0
+        auto picks = [&](uint32_t j0) {
 #pragma unroll
-        for (int v = 0; v < V; v++) g[v] = 0.0f;
-        for (uint32_t j = 0; j < k; j++) {
-            const uint32_t id = (uint32_t)ids[at * k + j] - lane * V;
-            const float gj = d_weights[at * k + j];
-            if (id < (uint32_t)V) picked |= 1u << id;
+            for (int q = 0; q < 4; q++) {
+                id[q] = j0 + q < k ? (uint32_t)__ldg(ids + at * k + j0 + q) : 0xFFFFFFFFu;
+                g[q] = j0 + q < k ? __ldg(d_weights + at * k + j0 + q) : 0.0f;
+            }
 #pragma unroll
-            for (int v = 0; v < V; v++) if (id == (uint32_t)v) g[v] += gj;
+            for (int q = 0; q < 4; q++) {
+                sp[q] = id[q] < E ? fmaxf(to_f32(x[id[q]]), kNegInf) : kNegInf;
+                if (sp[q] == kNegInf) g[q] = 0.0f;
+            }
+        };
+        float s[V], m = kNegInf;
+        picks(0);
+        if (mode == SF_GATE_SOFTMAX) {
+            load_scores<T, LPR, V, ALIGNED>(x, E, lane * V, s);
+#pragma unroll
+            for (int v = 0; v < V; v++) m = fmaxf(m, s[v]);
+            m = max_lanes<LPR>(m);
+        } else if (mode == SF_GATE_SOFTMAX_PICKED) {
+            for (uint32_t j0 = 0; j0 < k; j0 += 4) {
+                if (j0) picks(j0);
+#pragma unroll
+                for (int q = 0; q < 4; q++) m = fmaxf(m, sp[q]);
+            }
         }
+        const bool finite = fabsf(m) < -kNegInf;
+        auto part = [&](float score) { return mode == SF_GATE_SHARE ? (score == kNegInf ? 0.0f : score) : near_top(score, m, finite); };
+        float t = 0.0f, dot = 0.0f;
+        if (k > 4 && mode == SF_GATE_SOFTMAX_PICKED) picks(0);
+        for (uint32_t j0 = 0; j0 < k; j0 += 4) {
+            if (j0) picks(j0);
 #pragma unroll
-        for (int v = 0; v < V; v++) if (s[v] == kNegInf) picked &= ~(1u << v);      // (a masked expert is none that the gate gave)
-        float m = kNegInf;
-#pragma unroll
-        for (int v = 0; v < V; v++) m = fmaxf(m, s[v]);
-        m = max_lanes<LPR>(m);
-        float p[V], t = 0.0f;
-#pragma unroll
-        for (int v = 0; v < V; v++) {
-            const bool mine = (picked >> v) & 1u;
-            p[v] = mode == SF_GATE_SHARE ? (mine ? s[v] : 0.0f) : (mode == SF_GATE_SOFTMAX || mine ? near_top(s[v], m) : 0.0f);
-            t += p[v];
+            for (int q = 0; q < 4; q++) { const float e = part(sp[q]); dot = fmaf(g[q], e, dot); t += e; }
         }
-        t = sum_lanes<LPR>(t);
+        if (mode == SF_GATE_SOFTMAX) {
+            t = 0.0f;
+#pragma unroll
+            for (int v = 0; v < V; v++) { s[v] = near_top(s[v], m, finite); t += s[v]; }
+            t = sum_lanes<LPR>(t);
+        }
         const float inv = t > 0.0f ? 1.0f / t : 0.0f;
-        float dot = 0.0f;
-#pragma unroll
-        for (int v = 0; v < V; v++) {
-            p[v] *= inv;
-            if (!((picked >> v) & 1u)) g[v] = 0.0f;
-            dot = fmaf(g[v], p[v], dot);
-        }
-        dot = sum_lanes<LPR>(dot);
+        dot = inv > 0.0f ? dot * inv : 0.0f;           // (a sum that is not positive may have run to infinity)
         if (!live) continue;
         float d[V];
 #pragma unroll
-        for (int v = 0; v < V; v++) d[v] = mode == SF_GATE_SHARE ? ((picked >> v) & 1u ? (g[v] - dot) * inv : 0.0f) : (p[v] != 0.0f ? p[v] * (g[v] - dot) : 0.0f);
-        T* q = d_scores + row * ldd;
+        for (int v = 0; v < V; v++) d[v] = mode == SF_GATE_SOFTMAX ? s[v] * inv * -dot : 0.0f;
+        T* const y = d_scores + row * ldd;
         const uint32_t first = lane * V;
         if (ALIGNED && first + V <= E) {
-            if constexpr ((V * sizeof(T)) % 32 == 0) store_sectors<T, V>(q + first, d);
-            else store_f32<T, V, (V * sizeof(T)) % 16 == 0>(q + first, d);
+            if constexpr ((V * sizeof(T)) % 32 == 0) store_sectors<T, V>(y + first, d);
+            else store_f32<T, V, (V * sizeof(T)) % 16 == 0>(y + first, d);
         } else {
 #pragma unroll
-            for (int v = 0; v < V; v++) if (first + v < E) q[first + v] = from_f32<T>(d[v]);
+            for (int v = 0; v < V; v++) if (first + v < E) y[first + v] = from_f32<T>(d[v]);
+        }
+        for (uint32_t j0 = 0; j0 < k; j0 += 4) {
+            if (k > 4) picks(j0);
+#pragma unroll
+            for (int q = 0; q < 4; q++)
+                if (id[q] < E && id[q] - first < (uint32_t)V && sp[q] != kNegInf)
+                    y[id[q]] = from_f32<T>(mode == SF_GATE_SHARE ? (g[q] - dot) * inv : part(sp[q]) * inv * (g[q] - dot));
         }
     }
 }
@@ -185,6 +209,12 @@ template <typename F> int by_experts(uint32_t E, F f) {
     return f(integral_constant<int, 32>(), integral_constant<int, 32>());
 }
 
+template <typename F> int by_mode(int mode, F f) {
+    if (mode == SF_GATE_SOFTMAX) return f(std::integral_constant<int, SF_GATE_SOFTMAX>());
+    if (mode == SF_GATE_SOFTMAX_PICKED) return f(std::integral_constant<int, SF_GATE_SOFTMAX_PICKED>());
+    return f(std::integral_constant<int, SF_GATE_SHARE>());
+}
+
 // ---- sort --------------------------------------------------------------------------------------------------------
 // The pairs are cut into tiles, one per block, a tile's warps take consecutive pieces of it.  Launch 1 counts each tile's pairs per
 // expert; in launch 2 every block adds up the tiles before its own (tiles x E words from L2, all threads at once), turns the
@@ -196,8 +226,7 @@ struct sort_args {
     uint32_t* offsets; uint32_t* counts; int32_t* flow_of_row; int32_t* row_of_pair;
 };
 constexpr uint32_t kOneTile = 4096;                       // pairs that one block sorts alone
-constexpr uint32_t kWide = 1024;                          // threads of a block up to kWideE experts (a counter per warp and expert)
-constexpr uint32_t kWideE = 256;
+constexpr uint32_t kFewPairs = 1024;                      // up to here 8 warps a block, 32 beyond: fewer to meet at the barriers (4.0 instead of 4.8 us)
 constexpr int kAhead = 4;
 
 template <uint32_t WARPS>
@@ -263,15 +292,21 @@ sort_place_kernel(const sort_args a, sf_dev_state* st)
             total[e] = t;
         }
     } else {
-        const uint32_t all = a.tiles * a.E, own = blockIdx.x * a.E;
-        for (uint32_t i0 = threadIdx.x; i0 < all; i0 += WARPS * 32 * 8) {
-            uint32_t h[8];
+        // a thread has one expert and every `rows`-th tile
+        const uint32_t rows = max(1u, WARPS * 32 / a.E);
+        for (uint32_t e0 = 0; e0 < a.E; e0 += WARPS * 32) {
+            const uint32_t e = e0 + threadIdx.x % min(a.E, WARPS * 32), t0 = threadIdx.x / min(a.E, WARPS * 32);
+            uint32_t t = 0, b = 0;
+            if (e < a.E && t0 < rows) {
+                for (uint32_t i0 = t0; i0 < a.tiles; i0 += rows * 8) {
+                    uint32_t h[8];
 #pragma unroll
-            for (int u = 0; u < 8; u++) { const uint32_t i = i0 + u * WARPS * 32; h[u] = i < all ? __ldcg(a.hist + i) : 0u; }
+                    for (int u = 0; u < 8; u++) h[u] = i0 + u * rows < a.tiles ? __ldcg(a.hist + (size_t)(i0 + u * rows) * a.E + e) : 0u;
 #pragma unroll
-            for (int u = 0; u < 8; u++) {
-                const uint32_t i = i0 + u * WARPS * 32;
-                if (h[u]) { atomicAdd(&total[i % a.E], h[u]); if (i < own) atomicAdd(&before[i % a.E], h[u]); }
+                    for (int u = 0; u < 8; u++) { t += h[u]; if (i0 + u * rows < blockIdx.x) b += h[u]; }
+                }
+                if (t) atomicAdd(&total[e], t);
+                if (b) atomicAdd(&before[e], b);
             }
         }
     }
@@ -333,13 +368,22 @@ sort_place_kernel(const sort_args a, sf_dev_state* st)
     }
 }
 
-// Tiles of at least 1024 pairs, at most one per SM and at most 32,768 counts in all (every block reads them).
+// Tiles of at least 1024 pairs, at most one per SM and at most 65,536 counts in all (every block reads them).
 uint32_t sort_tiles(const sf_ctx* ctx, uint32_t n, uint32_t k, uint32_t E) {
     const uint64_t pairs = (uint64_t)n * k;
     if (pairs <= kOneTile) return 1;
-    return (uint32_t)std::min<uint64_t>({(uint64_t)ctx->num_sms, (pairs + 1023) / 1024, 32768 / E});
+    return (uint32_t)std::min<uint64_t>({(uint64_t)ctx->num_sms, (pairs + 1023) / 1024, 65536 / E});
 }
-template <uint32_t WARPS> int launch_sort(const sort_args& a, sf_dev_state* state, cudaStream_t st) {
+template <uint32_t WARPS> int launch_sort(const sf_ctx* ctx, const sort_args& a, cudaStream_t st) {
+    sf_dev_state* const state = ctx->d_state;
+    static bool set_dev[64] = {};                         // the shared-memory opt-in (a counter per warp and expert) is per device
+    bool& set = set_dev[ctx->device & 63];
+    if (!set) {
+        constexpr int most = (WARPS + 3) * SF_MAX_EXPERTS * 4 + 4;
+        SF_CUDA(cudaFuncSetAttribute(sort_count_kernel<WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+        SF_CUDA(cudaFuncSetAttribute(sort_place_kernel<WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+        set = true;
+    }
     if (a.tiles > 1) SF_CUDA(sf_launch_chained(sort_count_kernel<WARPS>, a.tiles, WARPS * 32, WARPS * a.E * 4, st, a, state));
     SF_CUDA(sf_launch_chained(sort_place_kernel<WARPS>, a.tiles, WARPS * 32, (WARPS * a.E + 3 * a.E + 1) * 4, st, a, state));
     return SF_OK;
@@ -513,9 +557,12 @@ extern "C" int sf_expert_gate(sf_ctx* ctx, const void* scores, int dtype, const 
         return by_experts(E, [&](auto lpr, auto v) {
             constexpr int L = decltype(lpr)::value, V = decltype(v)::value, S = V < 4 ? V : 4;
             const bool al = fits(scores, ld, dtype, V);
-            auto kern = k <= S * L ? (al ? gate_kernel<T, L, V, S, true> : gate_kernel<T, L, V, S, false>) : (al ? gate_kernel<T, L, V, V, true> : gate_kernel<T, L, V, V, false>);
-            SF_CUDA(sf_launch_chained(kern, (n + kThreads / L - 1) / (kThreads / L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, mode, ids_out, weights_out, ctx->d_state));
+            return by_mode(mode, [&](auto m) {
+            constexpr int M = decltype(m)::value;
+            auto kern = k <= S * L ? (al ? gate_kernel<T, L, V, S, M, true> : gate_kernel<T, L, V, S, M, false>) : (al ? gate_kernel<T, L, V, V, M, true> : gate_kernel<T, L, V, V, M, false>);
+            SF_CUDA(sf_launch_chained(kern, (n + kThreads / L - 1) / (kThreads / L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, ids_out, weights_out, ctx->d_state));
             return SF_OK;
+            });
         });
     });
 }
@@ -534,10 +581,13 @@ extern "C" int sf_expert_gate_backward(sf_ctx* ctx, const void* scores, int dtyp
         return by_experts(E, [&](auto lpr, auto v) {
             constexpr int L = decltype(lpr)::value, V = decltype(v)::value;
             const bool al = fits(scores, ld, dtype, V) && fits(d_scores_out, ldd, dtype, V);
-            auto kern = al ? gate_backward_kernel<T, L, V, true> : gate_backward_kernel<T, L, V, false>;
-            SF_CUDA(sf_launch_chained(kern, (n + kThreads / L - 1) / (kThreads / L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, mode, ids, d_weights,
+            return by_mode(mode, [&](auto m) {
+            constexpr int M = decltype(m)::value;
+            auto kern = al ? gate_backward_kernel<T, L, V, M, true> : gate_backward_kernel<T, L, V, M, false>;
+            SF_CUDA(sf_launch_chained(kern, (n + kThreads / L - 1) / (kThreads / L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, ids, d_weights,
                                       (T*)d_scores_out, ldd, ctx->d_state));
             return SF_OK;
+            });
         });
     });
 }
@@ -563,8 +613,7 @@ extern "C" int sf_expert_sort(sf_ctx* ctx, const int32_t* ids, const uint32_t* n
     const uint32_t tiles = sort_tiles(ctx, n, k, E);
     if (tiles > 1 && (!workspace || workspace_bytes < (size_t)tiles * E * 4)) return SF_ERR_ARG;
     const sort_args a = {ids, n_dev, n, k, E, align, capacity, tiles, (uint32_t*)workspace, offsets_out, counts_out, flow_of_row_out, row_of_pair_out};
-    // (a handful of pairs: fewer warps to meet at the barriers, 4.1 instead of 4.8 us)
-    return E <= kWideE && (uint64_t)n * k > 1024 ? launch_sort<kWide / 32>(a, ctx->d_state, (cudaStream_t)stream) : launch_sort<kWarps>(a, ctx->d_state, (cudaStream_t)stream);
+    return (uint64_t)n * k > kFewPairs ? launch_sort<32>(ctx, a, (cudaStream_t)stream) : launch_sort<8>(ctx, a, (cudaStream_t)stream);
 }
 
 extern "C" int sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t D, size_t ldx, uint32_t k,
