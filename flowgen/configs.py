@@ -22,7 +22,7 @@ class Config:
     P: int                      # packets seen by the slow model
     H: int                      # header bytes per packet in the wide planes
     slow: str                   # "mlp" | "cnn"
-    slow_dtype: str             # "f32" | "bf16"
+    slow_dtype: str             # "f32" | "bf16" | "mx4" (an MLP's hidden layers in 4 bits)
     dims: Tuple[int, ...]       # MLP layer widths, or () for the CNN
     q_percent: int              # Alg. 1 quantile (percent) used for tau; 0 = fixed rule
     n_val: int = 65536          # validation flows for threshold calibration

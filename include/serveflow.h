@@ -289,7 +289,10 @@ int  sf_per_class_thresholds(sf_ctx* ctx, const float* scores, const uint8_t* la
  * fp32[dims[k+1]].  SF_BF16: weights and hidden activations are bf16 (RNE),
  * products accumulate in fp32 on the tensor cores, biases and logits fp32; needs
  * hidden widths that are multiples of 64 and dims[0] a multiple of 64.  SF_F32:
- * plain fp32.  The last layer may have any width up to 16 classes. */
+ * plain fp32.  SF_MX4: takes bf16 rows (sf_route_cfg.row_dtype SF_BF16, same widths as SF_BF16); rows, hidden weights and
+ * hidden activations are packed in 4 bits as sf_mx4_quantise packs them (activations from the fp32 sums after bias and
+ * ReLU), products accumulate in fp32; the last hidden layer's activations and the last layer's weights are bf16, logits
+ * fp32.  The last layer may have any width up to 16 classes. */
 int  sf_mlp_create(sf_ctx* ctx, int dtype, uint32_t n_layers, const uint32_t* dims_host,
                    const float* const* W_host, const float* const* b_host, sf_slow** out);
 /* 1-D CNN over L positions x Cin channels (channels last): conv(k) Cin->C1 + ReLU,
@@ -301,8 +304,8 @@ int  sf_cnn_create(sf_ctx* ctx, int dtype, uint32_t L, uint32_t Cin, uint32_t C1
                    const float* b2_host, const float* w3_host, const float* b3_host, sf_slow** out);
 void sf_slow_destroy(sf_slow* slow);
 /* The slow model of the cascade (Sec. 3.1) on the first *n_rows_dev rows (a DEVICE
- * count, read by the kernels: no host round trip) of rows[capacity][D] (bf16 or
- * fp32 as the model's dtype).  logits_out fp32[capacity][n_cls]; label_out
+ * count, read by the kernels: no host round trip) of rows[capacity][D] (fp32 for an
+ * SF_F32 model, else bf16).  logits_out fp32[capacity][n_cls]; label_out
  * uint8[capacity] (nullable) = argmax, lowest index on ties.  Rows at or beyond
  * the count are not written.  A count above `capacity` is treated as `capacity`
  * (nothing is read or written beyond the buffers) and SF_ERR_CAPACITY is recorded in

@@ -220,7 +220,7 @@ int check_serve_args(sf_ctx* ctx, const sf_forest* fo, const sf_slow* s, const s
     if (cfg->wide_layout != SF_MLP16 && cfg->wide_layout != SF_CNN8) return SF_ERR_ARG;
     if ((cfg->wide_layout == SF_CNN8) != (s->arch == SF_SLOW_CNN)) return SF_ERR_ARG;
     if (cfg->P * W != slow_width(s)) return SF_ERR_ARG;
-    if (cfg->row_dtype != s->dtype) return SF_ERR_ARG;
+    if (cfg->row_dtype != s->row_dtype) return SF_ERR_ARG;
     const uint32_t P_real = cfg->P_real ? cfg->P_real : cfg->P;
     if (P_real > cfg->P || P_real > wide->pitch_pkts) return SF_ERR_ARG;
     if (wide->hdr_bytes < (cfg->wide_layout == SF_MLP16 ? 13u : 5u)) return SF_ERR_ARG;

@@ -70,10 +70,12 @@ enum { SF_SLOW_MLP = 0, SF_SLOW_CNN = 1 };
 struct sf_slow {
     sf_ctx* ctx;
     int arch;                 // SF_SLOW_MLP | SF_SLOW_CNN
-    int dtype;                // SF_F32 | SF_BF16
+    int dtype;                // SF_F32 | SF_BF16 | SF_MX4
+    int row_dtype;            // of the wide rows it takes: SF_F32 | SF_BF16
     uint32_t n_layers;
     uint32_t dims[9];
-    void*  d_W[8];            // bf16 or fp32 [out][in]
+    void*  d_W[8];            // bf16 or fp32 [out][in]; SF_MX4: hidden layers packed
+    void*  d_S[8];            // SF_MX4: their scales
     float* d_b[8];
     // CNN
     uint32_t L, Cin, C1, C2, k, n_cls;
@@ -178,6 +180,13 @@ int sf_launch_forest_leaf_index_packets(const sf_forest* fo, const sf_packets* p
 // bf16 tensor-core layers (gemm_tc.cu)
 int sf_mlp_bf16_forward(sf_ctx* ctx, const sf_slow* s, const void* rows, const uint32_t* n_rows_dev, uint32_t capacity,
                         float* logits, uint8_t* label, void* scratch, cudaStream_t st);
+// the narrow last layer on its own: W16 = bf16 [16][K], rows past C zero
+int sf_mlp_head_bf16(sf_ctx* ctx, const void* A, const void* W16, const float* bias, const uint32_t* n_rows_dev, uint32_t capacity,
+                     uint32_t K, uint32_t C, float* logits, uint8_t* label, cudaStream_t st);
+// hidden layers in 4 bits (mx4_gemm.cu)
+size_t sf_mlp_mx4_scratch_bytes(const sf_slow* s, uint32_t capacity);
+int sf_mlp_mx4_forward(sf_ctx* ctx, const sf_slow* s, const void* rows, const uint32_t* n_rows_dev, uint32_t capacity,
+                       float* logits, uint8_t* label, void* scratch, cudaStream_t st);
 int sf_cnn_bf16_forward(sf_ctx* ctx, const sf_slow* s, const void* rows, const uint32_t* n_rows_dev, uint32_t capacity,
                         float* logits, uint8_t* label, void* scratch, cudaStream_t st);
 int sf_cnn_prepare(sf_slow* s, const float* w1, const float* b1, const float* w2, const float* b2,

@@ -711,6 +711,13 @@ int launch_head_tc(sf_ctx* ctx, const void* A, const void* W16, const float* bia
 
 }  // namespace
 
+int sf_mlp_head_bf16(sf_ctx* ctx, const void* A, const void* W16, const float* bias, const uint32_t* n_rows_dev, uint32_t capacity,
+                     uint32_t K, uint32_t C, float* logits, uint8_t* label, cudaStream_t st)
+{
+    const uint32_t small_max = capacity <= 65536 && K <= kSmallMaxK && K % 8 == 0 ? kSmallRows : 0u;
+    return launch_head_tc(ctx, A, W16, bias, n_rows_dev, capacity, K, C, logits, label, st, small_max);
+}
+
 int sf_mlp_bf16_forward(sf_ctx* ctx, const sf_slow* s, const void* rows, const uint32_t* n_rows_dev, uint32_t capacity,
                         float* logits, uint8_t* label, void* scratch, cudaStream_t st)
 {

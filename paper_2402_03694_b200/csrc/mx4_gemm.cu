@@ -575,6 +575,52 @@ int sf_launch_mx4_product(sf_ctx* ctx, const sf_mx4_product& p, cudaStream_t st)
     return p.out_scales ? go(Mx4()) : by_type(p.out_dtype, go);
 }
 
+// ---- the slow model's hidden layers in 4 bits ------------------------------------------------------------------
+// The wide rows (bf16) are packed once; every hidden layer but the last packs its own output in its epilogue (from the fp32 sums: no
+// activations in 16 bits in between), the last one writes bf16 for the head, which stays in bf16: its few columns cost
+// nothing and its logits decide labels.
+namespace {
+struct MlpScratch { size_t data, scales, half, bytes; };      // two packed buffers, then the bf16 rows of the last hidden layer
+MlpScratch mlp_scratch(const sf_slow* s, uint32_t capacity) {
+    uint32_t widest = 0;
+    for (uint32_t l = 0; l + 1 < s->n_layers; l++) widest = std::max(widest, s->dims[l]);
+    MlpScratch m;
+    m.data = sf_align256((size_t)capacity * row_bytes(widest));
+    m.scales = sf_align256(scale_bytes(capacity, widest));
+    m.half = 2 * (m.data + m.scales);
+    m.bytes = m.half + sf_align256((size_t)capacity * s->dims[s->n_layers - 1] * 2) + 256;
+    return m;
+}
+}  // namespace
+
+size_t sf_mlp_mx4_scratch_bytes(const sf_slow* s, uint32_t capacity) { return mlp_scratch(s, capacity).bytes; }
+
+int sf_mlp_mx4_forward(sf_ctx* ctx, const sf_slow* s, const void* rows, const uint32_t* n_rows_dev, uint32_t capacity,
+                       float* logits, uint8_t* label, void* scratch, cudaStream_t st)
+{
+    const MlpScratch m = mlp_scratch(s, capacity);
+    uint8_t* const w = reinterpret_cast<uint8_t*>(scratch);
+    uint8_t* const data[2] = {w, w + m.data + m.scales};
+    uint8_t* const scales[2] = {data[0] + m.data, data[1] + m.data};
+    const uint32_t L = s->n_layers - 1;                  // the head
+    sf_time_begin(ctx, SF_T_GEMM, st);
+    int rc = sf_launch_mx4_quantise(ctx, rows, SF_BF16, capacity, s->dims[0], s->dims[0], nullptr, n_rows_dev, capacity, data[0], scales[0], st);
+    for (uint32_t l = 0; l < L && rc == SF_OK; l++) {
+        const bool last = l + 1 == L;
+        const uint32_t i = l & 1u;
+        sf_mx4_product p = {data[i], scales[i], n_rows_dev, nullptr, 1, capacity, (const uint8_t*)s->d_W[l], (const uint8_t*)s->d_S[l], s->dims[l + 1], s->dims[l],
+                            s->d_b[l], 1, SF_BF16, w + m.half, s->dims[l + 1], nullptr};
+        if (!last) { p.out_dtype = SF_MX4; p.out = data[i ^ 1u]; p.out_scales = scales[i ^ 1u]; }
+        rc = sf_launch_mx4_product(ctx, p, st);
+    }
+    sf_time_end(ctx, SF_T_GEMM, st);
+    if (rc != SF_OK) return rc;
+    sf_time_begin(ctx, SF_T_HEAD, st);
+    rc = sf_mlp_head_bf16(ctx, w + m.half, s->d_W[L], s->d_b[L], n_rows_dev, capacity, s->dims[L], s->dims[L + 1], logits, label, st);
+    sf_time_end(ctx, SF_T_HEAD, st);
+    return rc;
+}
+
 extern "C" int sf_mx4_matmul(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_scales, const uint32_t* n_rows_dev, uint32_t capacity,
                              const uint8_t* w, const uint8_t* w_scales, uint32_t N, uint32_t K, const float* bias, int relu,
                              int out_dtype, void* out, size_t ld, uint8_t* out_scales, void* stream)

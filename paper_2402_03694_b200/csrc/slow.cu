@@ -1,6 +1,7 @@
 // S4: slow-model handles, the fp32 MLP path (plain FFMA tiles) and dispatch to
 // the bf16 tensor-core paths.
 #include "common.cuh"
+#include "mx4.cuh"
 #include <new>
 #include <stdlib.h>
 #include <string.h>
@@ -114,6 +115,7 @@ void f32_to_bf16_host(const float* src, uint16_t* dst, size_t n) {
 
 size_t sf_slow_scratch_bytes(const sf_slow* s, uint32_t capacity) {
     if (s->arch == SF_SLOW_CNN) return sf_align256((size_t)capacity * s->C2 * sizeof(float)) + 256;
+    if (s->dtype == SF_MX4) return sf_mlp_mx4_scratch_bytes(s, capacity);
     uint32_t maxh = 0;
     for (uint32_t l = 1; l < s->n_layers; l++) if (s->dims[l] > maxh) maxh = s->dims[l];
     size_t esz = s->dtype == SF_BF16 ? 2 : 4;
@@ -129,6 +131,8 @@ int sf_launch_slow(sf_ctx* ctx, const sf_slow* s, const void* rows, const uint32
         rc = sf_cnn_bf16_forward(ctx, s, rows, n_rows_dev, capacity, logits, label, scratch, st);
     } else if (s->dtype == SF_BF16) {
         rc = sf_mlp_bf16_forward(ctx, s, rows, n_rows_dev, capacity, logits, label, scratch, st);
+    } else if (s->dtype == SF_MX4) {
+        rc = sf_mlp_mx4_forward(ctx, s, rows, n_rows_dev, capacity, logits, label, scratch, st);
     } else {
         uint32_t maxh = 0;
         for (uint32_t l = 1; l < s->n_layers; l++) if (s->dims[l] > maxh) maxh = s->dims[l];
@@ -176,12 +180,12 @@ extern "C" int sf_mlp_create(sf_ctx* ctx, int dtype, uint32_t n_layers, const ui
                              const float* const* W, const float* const* b, sf_slow** out)
 {
     if (!ctx || !dims || !W || !b || !out) return SF_ERR_ARG;
-    if (dtype != SF_F32 && dtype != SF_BF16) return SF_ERR_ARG;
+    if (dtype != SF_F32 && dtype != SF_BF16 && dtype != SF_MX4) return SF_ERR_ARG;
     if (n_layers < 1 || n_layers > 8) return SF_ERR_ARG;
     for (uint32_t l = 0; l <= n_layers; l++) if (dims[l] == 0 || dims[l] > 65536) return SF_ERR_ARG;
     for (uint32_t l = 0; l < n_layers; l++) if (!W[l] || !b[l]) return SF_ERR_ARG;
     if (dims[n_layers] > 16) return SF_ERR_UNSUPPORTED;
-    if (dtype == SF_BF16) {
+    if (dtype != SF_F32) {
         if (n_layers < 2) return SF_ERR_UNSUPPORTED;
         for (uint32_t l = 0; l < n_layers; l++) if (dims[l] % 64 != 0) return SF_ERR_UNSUPPORTED;
     }
@@ -189,7 +193,7 @@ extern "C" int sf_mlp_create(sf_ctx* ctx, int dtype, uint32_t n_layers, const ui
     sf_slow* s = new (std::nothrow) sf_slow();
     if (!s) return SF_ERR_ALLOC;
     memset(s, 0, sizeof(*s));
-    s->ctx = ctx; s->arch = SF_SLOW_MLP; s->dtype = dtype; s->n_layers = n_layers;
+    s->ctx = ctx; s->arch = SF_SLOW_MLP; s->dtype = dtype; s->row_dtype = dtype == SF_F32 ? SF_F32 : SF_BF16; s->n_layers = n_layers;
     for (uint32_t l = 0; l <= n_layers; l++) s->dims[l] = dims[l];
     cudaError_t e = cudaSuccess;
     for (uint32_t l = 0; l < n_layers && e == cudaSuccess; l++) {
@@ -197,7 +201,20 @@ extern "C" int sf_mlp_create(sf_ctx* ctx, int dtype, uint32_t n_layers, const ui
         e = cudaMalloc(&s->d_b[l], sizeof(float) * dims[l + 1]);
         if (e == cudaSuccess) e = cudaMemcpy(s->d_b[l], b[l], sizeof(float) * dims[l + 1], cudaMemcpyHostToDevice);
         if (e != cudaSuccess) break;
-        if (dtype == SF_BF16) {
+        if (dtype == SF_MX4 && l + 1 < n_layers) {
+            // a hidden layer: up in fp32, packed on the device
+            float* up = nullptr;
+            e = cudaMalloc(&up, cnt * 4);
+            if (e == cudaSuccess) e = cudaMemcpy(up, W[l], cnt * 4, cudaMemcpyHostToDevice);
+            if (e == cudaSuccess) e = cudaMalloc(&s->d_W[l], (size_t)dims[l + 1] * sfmx::row_bytes(dims[l]));
+            if (e == cudaSuccess) e = cudaMalloc(&s->d_S[l], sfmx::scale_bytes(dims[l + 1], dims[l]));
+            if (e == cudaSuccess) {
+                const int rc = sf_launch_mx4_quantise(ctx, up, SF_F32, dims[l + 1], dims[l], dims[l], nullptr, nullptr, dims[l + 1], (uint8_t*)s->d_W[l], (uint8_t*)s->d_S[l], nullptr);
+                if (rc != SF_OK) { cudaFree(up); sf_slow_destroy(s); return rc; }
+                e = cudaDeviceSynchronize();
+            }
+            if (up) cudaFree(up);
+        } else if (dtype != SF_F32) {
             // the last layer runs as a 128 x 16 tensor-core tile: pad its rows to 16 with zeros
             const size_t rows_pad = (l + 1 == n_layers) ? 16 : dims[l + 1];
             const size_t cnt_pad = rows_pad * dims[l];
@@ -228,7 +245,7 @@ extern "C" int sf_cnn_create(sf_ctx* ctx, int dtype, uint32_t L, uint32_t Cin, u
     sf_slow* s = new (std::nothrow) sf_slow();
     if (!s) return SF_ERR_ALLOC;
     memset(s, 0, sizeof(*s));
-    s->ctx = ctx; s->arch = SF_SLOW_CNN; s->dtype = dtype;
+    s->ctx = ctx; s->arch = SF_SLOW_CNN; s->dtype = dtype; s->row_dtype = dtype;
     s->L = L; s->Cin = Cin; s->C1 = C1; s->C2 = C2; s->k = k; s->n_cls = n_cls;
     int rc = sf_cnn_prepare(s, w1, b1, w2, b2, w3, b3);
     if (rc != SF_OK) { sf_slow_destroy(s); return rc; }
@@ -238,7 +255,7 @@ extern "C" int sf_cnn_create(sf_ctx* ctx, int dtype, uint32_t L, uint32_t Cin, u
 
 extern "C" void sf_slow_destroy(sf_slow* s) {
     if (!s) return;
-    for (int l = 0; l < 8; l++) { if (s->d_W[l]) cudaFree(s->d_W[l]); if (s->d_b[l]) cudaFree(s->d_b[l]); }
+    for (int l = 0; l < 8; l++) { if (s->d_W[l]) cudaFree(s->d_W[l]); if (s->d_S[l]) cudaFree(s->d_S[l]); if (s->d_b[l]) cudaFree(s->d_b[l]); }
     if (s->d_w1) cudaFree(s->d_w1); if (s->d_w2) cudaFree(s->d_w2); if (s->d_w3) cudaFree(s->d_w3);
     if (s->d_b1) cudaFree(s->d_b1); if (s->d_b2) cudaFree(s->d_b2); if (s->d_b3) cudaFree(s->d_b3);
     delete s;

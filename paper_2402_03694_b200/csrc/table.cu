@@ -655,7 +655,7 @@ int ingest_chunk(sf_ctx* ctx, sf_table* t, const sf_pkt_batch* batch, const sf_f
     if (!batch->src || !batch->dst || !batch->sport || !batch->dport || !batch->proto || !batch->dir || !batch->size ||
         !batch->iat_us || !batch->hdr) return SF_ERR_ARG;
     if (F != fo->F || fo->kind != SF_RF || cfg->rule != SF_LC_GT) return SF_ERR_UNSUPPORTED;
-    if (slow->arch != SF_SLOW_MLP || cfg->wide_layout != SF_MLP16 || cfg->row_dtype != slow->dtype) return SF_ERR_UNSUPPORTED;
+    if (slow->arch != SF_SLOW_MLP || cfg->wide_layout != SF_MLP16 || cfg->row_dtype != slow->row_dtype) return SF_ERR_UNSUPPORTED;
     if (cfg->P * 16 != slow->dims[0] || cfg->P < t->d.slow_pkts) return SF_ERR_ARG;
     SF_CUDA(cudaSetDevice(ctx->device));
     cudaStream_t ss = (cudaStream_t)stream;                   // look-up and sort: the caller's stream
@@ -672,7 +672,7 @@ int ingest_chunk(sf_ctx* ctx, sf_table* t, const sf_pkt_batch* batch, const sf_f
     TableDev d = t->d;
     d.first = S.first;
     // workspace: features, probabilities, decisions, wide rows and slow-model scratch for at most n flows
-    const size_t esz = slow->dtype == SF_BF16 ? 2 : 4;
+    const size_t esz = slow->row_dtype == SF_BF16 ? 2 : 4;
     const uint32_t Cs = slow->dims[slow->n_layers];
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off += sf_align256(bytes); return o; };

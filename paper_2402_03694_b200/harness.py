@@ -38,7 +38,7 @@ def make_forest(ctx, fo):
 
 
 def make_slow(ctx, cfg, model):
-    dt = sf.SF_BF16 if cfg.slow_dtype == "bf16" else sf.SF_F32
+    dt = {"bf16": sf.SF_BF16, "f32": sf.SF_F32, "mx4": sf.SF_MX4}[cfg.slow_dtype]
     if cfg.slow == "mlp":
         return sf.sf_mlp_create(ctx, dt, model["dims"], model["W"], model["b"])
     return sf.sf_cnn_create(ctx, dt, model)
@@ -54,7 +54,7 @@ def bf16_bits_to_f32(t):
 def route_cfg_for(cfg, tau_dev, capacity, P_real=0):
     rule = sf.SF_LC_GT if cfg.kind == "rf" else sf.SF_ABSMARGIN_LT
     layout = sf.SF_MLP16 if cfg.slow == "mlp" else sf.SF_CNN8
-    dt = sf.SF_BF16 if cfg.slow_dtype == "bf16" else sf.SF_F32
+    dt = sf.SF_F32 if cfg.slow_dtype == "f32" else sf.SF_BF16
     return sf.make_route_cfg(rule, tau_dev, layout, dt, cfg.P, capacity, P_real)
 
 
