@@ -339,8 +339,8 @@ sort_place_kernel(const sort_args a, sf_dev_state* st)
         }
     }
     // rows that only fill a segment up to its aligned end
-    for (uint32_t e = blockIdx.x; e < a.E; e += gridDim.x)
-        for (uint32_t r = first[e] + total[e] + threadIdx.x; r < min(first[e + 1], a.capacity); r += WARPS * 32) a.flow_of_row[r] = -1;
+    for (uint32_t e = blockIdx.x * WARPS + warp; e < a.E; e += gridDim.x * WARPS)
+        for (uint32_t r = first[e] + total[e] + lane; r < min(first[e + 1], a.capacity); r += 32) a.flow_of_row[r] = -1;
     __syncthreads();
     uint64_t lo, hi;
     sort_piece<WARPS>(a, pairs, blockIdx.x, warp, lo, hi);
@@ -390,9 +390,11 @@ template <uint32_t WARPS> int launch_sort(const sf_ctx* ctx, const sort_args& a,
 }
 
 // ---- rows into the experts' order and back -------------------------------------------------------------------------------
-// Units of U bytes (16 where base, pitch and width allow, else one element).  A group of lanes (a power of two up to 32) shares a
-// flow: its row is read once and written k times.  Bound: HBM.
-template <typename Q>
+// A group of lanes (a power of two, up to the whole block where flows are few) shares a flow.  Elements move in words of 16 bytes where
+// bases, pitches and widths allow, else of 4 bytes, else one by one.  Bound: HBM.
+
+// Every row is read once and written k times; U words a lane on their way.
+template <typename Q, int U>
 __global__ void __launch_bounds__(kThreads)
 gather_kernel(const Q* __restrict__ x, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t units, size_t ldx, uint32_t k,
               const int32_t* __restrict__ row_of_pair, uint32_t E, const uint32_t* __restrict__ offsets, const uint32_t* __restrict__ counts,
@@ -413,24 +415,25 @@ gather_kernel(const Q* __restrict__ x, const uint32_t* __restrict__ n_dev, uint3
     const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1);
     for (uint64_t f = (uint64_t)blockIdx.x * per + threadIdx.x / lanes; f < flows; f += (uint64_t)flow_blocks * per) {
         const Q* src = x + f * ldx;
-        for (uint32_t c = lane; c < units; c += 4 * lanes) {
-            Q q[4];
+        for (uint32_t c = lane; c < units; c += U * lanes) {
+            Q q[U];
 #pragma unroll
-            for (int u = 0; u < 4; u++) if (c + u * lanes < units) q[u] = src[c + u * lanes];
+            for (int u = 0; u < U; u++) if (c + u * lanes < units) q[u] = __ldg(src + c + u * lanes);
             for (uint32_t j = 0; j < k; j++) {
                 const uint32_t r = (uint32_t)__ldg(row_of_pair + f * k + j);
-                if (r >= capacity) continue;
-                Q* dst = rows + (size_t)r * ldr;
+                if (r < capacity) {
+                    Q* dst = rows + (size_t)r * ldr;
 #pragma unroll
-                for (int u = 0; u < 4; u++) if (c + u * lanes < units) dst[c + u * lanes] = q[u];
+                    for (int u = 0; u < U; u++) if (c + u * lanes < units) dst[c + u * lanes] = q[u];
+                }
             }
         }
     }
 }
 
-// y[f] = sum_j w[f][j] rows[row_of_pair[f][j]], j ascending, in fp32, rounded once.  A lane has U vectors of V elements of a row on their
-// way, two rows at a time.  Bound: HBM.
-template <typename T, int V, int U, bool ALIGNED>
+// y[f] = sum_j w[f][j] rows[row_of_pair[f][j]], j ascending, in fp32, rounded once.  A lane has U words of V elements of a row on their
+// way, four rows at a time.
+template <typename T, int V, int U>
 __global__ void __launch_bounds__(kThreads)
 combine_kernel(const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t ldr, const int32_t* __restrict__ row_of_pair,
                const float* __restrict__ weights, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t k, T* __restrict__ y, size_t ldy,
@@ -446,14 +449,14 @@ combine_kernel(const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t
             for (int u = 0; u < U; u++)
 #pragma unroll
                 for (int v = 0; v < V; v++) acc[u][v] = 0.0f;
-#pragma unroll 2
+#pragma unroll (V * U > 16 ? 2 : 4)
             for (uint32_t j = 0; j < k; j++) {
                 const uint32_t r = (uint32_t)__ldg(row_of_pair + f * k + j);
                 if (r < capacity) {
                     const float w = weights ? __ldg(weights + f * k + j) : 1.0f;
                     float x[U][V];
 #pragma unroll
-                    for (int u = 0; u < U; u++) if (u == 0 || c + u * lanes * V < D) load_f32<T, V, ALIGNED>(rows + (size_t)r * ldr + c + u * lanes * V, x[u]);
+                    for (int u = 0; u < U; u++) if (u == 0 || c + u * lanes * V < D) load_word<T, V>(rows + (size_t)r * ldr + c + u * lanes * V, x[u]);
 #pragma unroll
                     for (int u = 0; u < U; u++)
                         if (u == 0 || c + u * lanes * V < D) {
@@ -463,71 +466,136 @@ combine_kernel(const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t
                 }
             }
 #pragma unroll
-            for (int u = 0; u < U; u++) if (u == 0 || c + u * lanes * V < D) store_f32<T, V, ALIGNED>(y + f * ldy + c + u * lanes * V, acc[u]);
+            for (int u = 0; u < U; u++) if (u == 0 || c + u * lanes * V < D) store_word<T, V>(y + f * ldy + c + u * lanes * V, acc[u]);
         }
     }
 }
 
-// d_rows[row_of_pair[f][j]] = w[f][j] dy[f], d_w[f][j] = <dy[f], rows[row_of_pair[f][j]]>
-template <typename T, int V, bool ALIGNED>
+// d_rows[row_of_pair[f][j]] = w[f][j] dy[f], d_w[f][j] = <dy[f], rows[row_of_pair[f][j]]>; J pairs of a flow at a time, U words of V elements.
+// A flow's dot products are summed over its lanes in a fixed tree (over the block's warps through shared memory).
+template <typename T, int V, int U, int J>
 __global__ void __launch_bounds__(kThreads)
 combine_backward_kernel(const T* __restrict__ dy, size_t ldy, const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t ldr,
                         const int32_t* __restrict__ row_of_pair, const float* __restrict__ weights, const uint32_t* __restrict__ n_dev,
                         uint32_t n, uint32_t k, uint32_t E, const uint32_t* __restrict__ offsets, const uint32_t* __restrict__ counts,
                         T* __restrict__ d_rows, size_t ldd, float* __restrict__ d_weights, uint32_t lanes, uint32_t flow_blocks, uint32_t fill_blocks, sf_dev_state* st)
 {
+    __shared__ float part[kWarps][J];
     sf_chain_enter();
     if (blockIdx.x >= flow_blocks) {
-        const uint32_t e = (blockIdx.x - flow_blocks) / fill_blocks, part = (blockIdx.x - flow_blocks) % fill_blocks;
+        const uint32_t e = (blockIdx.x - flow_blocks) / fill_blocks, part_ = (blockIdx.x - flow_blocks) % fill_blocks;
         const uint32_t lo = min(offsets[e] + counts[e], capacity), hi = min(offsets[e + 1], capacity), units = D / V;
         const uint64_t all = lo < hi ? (uint64_t)(hi - lo) * units : 0;
         const float zero[V] = {};
-        for (uint64_t i = part * kThreads + threadIdx.x; i < all; i += fill_blocks * kThreads) {
+        for (uint64_t i = part_ * kThreads + threadIdx.x; i < all; i += fill_blocks * kThreads) {
             const uint32_t r = (uint32_t)(i / units), c = (uint32_t)(i - (uint64_t)r * units);
-            store_f32<T, V, ALIGNED>(d_rows + (size_t)(lo + r) * ldd + (size_t)c * V, zero);
+            store_word<T, V>(d_rows + (size_t)(lo + r) * ldd + (size_t)c * V, zero);
         }
         return;
     }
     const uint32_t flows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
-    const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1);
+    const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1), warp = threadIdx.x >> 5;
     for (uint64_t base = (uint64_t)blockIdx.x * per; base < flows; base += (uint64_t)flow_blocks * per) {
         const uint64_t f = base + threadIdx.x / lanes;
-        const bool live = f < flows;                      // (the sums over lanes below need whole warps)
-        for (uint32_t j = 0; j < k; j++) {
-            const uint32_t r = live ? (uint32_t)__ldg(row_of_pair + f * k + j) : 0xFFFFFFFFu;
-            const bool real = r < capacity;
-            float dot = 0.0f;
-            if (real) {
-                const float w = weights ? __ldg(weights + f * k + j) : 1.0f;
-                for (uint32_t c = lane * V; c < D; c += lanes * V) {
-                    float g[V];
-                    load_f32<T, V, ALIGNED>(dy + f * ldy + c, g);
-                    if (d_weights) {
-                        float x[V];
-                        load_f32<T, V, ALIGNED>(rows + (size_t)r * ldr + c, x);
+        const bool live = f < flows;                      // (the sums over lanes below need whole warps and blocks)
+        for (uint32_t j0 = 0; j0 < k; j0 += J) {
+            uint32_t r[J], any = 0xFFFFFFFFu;             // a pair without a row reads that of another (no branch among the loads)
+            bool real[J];
+            float w[J], dot[J];
 #pragma unroll
-                        for (int v = 0; v < V; v++) dot = fmaf(g[v], x[v], dot);
-                    }
-                    if (d_rows) {
+            for (int j = 0; j < J; j++) {
+                const bool have = live && j0 + j < k;
+                r[j] = have ? (uint32_t)__ldg(row_of_pair + f * k + j0 + j) : 0xFFFFFFFFu;
+                w[j] = have && weights ? __ldg(weights + f * k + j0 + j) : 1.0f;
+                real[j] = r[j] < capacity;
+                if (real[j]) any = r[j];
+                dot[j] = 0.0f;
+            }
 #pragma unroll
-                        for (int v = 0; v < V; v++) g[v] *= w;
-                        store_f32<T, V, ALIGNED>(d_rows + (size_t)r * ldd + c, g);
-                    }
+            for (int j = 0; j < J; j++) if (!real[j]) r[j] = any;
+            if (any != 0xFFFFFFFFu) for (uint32_t c0 = lane * V; c0 < D; c0 += lanes * V * U) {
+                float g[U][V];
+#pragma unroll
+                for (int u = 0; u < U; u++) if (u == 0 || c0 + u * lanes * V < D) load_word<T, V>(dy + f * ldy + c0 + u * lanes * V, g[u]);
+                if (d_weights) {
+                    float x[J][U][V];
+#pragma unroll
+                    for (int j = 0; j < J; j++)
+#pragma unroll
+                        for (int u = 0; u < U; u++)
+                            if (u == 0 || c0 + u * lanes * V < D) load_word<T, V>(rows + (size_t)r[j] * ldr + c0 + u * lanes * V, x[j][u]);
+#pragma unroll
+                    for (int j = 0; j < J; j++)
+#pragma unroll
+                        for (int u = 0; u < U; u++)
+                            if (u == 0 || c0 + u * lanes * V < D) {
+#pragma unroll
+                                for (int v = 0; v < V; v++) dot[j] = fmaf(g[u][v], x[j][u][v], dot[j]);
+                            }
+                }
+                if (d_rows) {
+#pragma unroll
+                    for (int j = 0; j < J; j++)
+#pragma unroll
+                        for (int u = 0; u < U; u++)
+                            if (real[j] && (u == 0 || c0 + u * lanes * V < D)) {
+                                float d[V];
+#pragma unroll
+                                for (int v = 0; v < V; v++) d[v] = w[j] * g[u][v];
+                                store_word<T, V>(d_rows + (size_t)r[j] * ldd + c0 + u * lanes * V, d);
+                            }
                 }
             }
-            if (d_weights) {
-                for (uint32_t o = lanes / 2; o >= 1; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
-                if (live && lane == 0) d_weights[f * k + j] = dot;
+            if (!d_weights) continue;
+#pragma unroll
+            for (int j = 0; j < J; j++) if (!real[j]) dot[j] = 0.0f;
+            const uint32_t in_warp = min(lanes, 32u);
+#pragma unroll
+            for (int j = 0; j < J; j++)
+                for (uint32_t o = in_warp / 2; o >= 1; o >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], o);
+            if (lanes > 32) {
+                if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+                    for (int j = 0; j < J; j++) part[warp][j] = dot[j];
+                }
+                __syncthreads();
+                if (lane == 0) {
+#pragma unroll
+                    for (int j = 0; j < J; j++) { dot[j] = 0.0f; for (uint32_t q = 0; q < lanes / 32; q++) dot[j] += part[warp + q][j]; }
+                }
+                __syncthreads();
+            }
+            if (live && lane == 0) {
+#pragma unroll
+                for (int j = 0; j < J; j++) if (j0 + j < k) d_weights[f * k + j0 + j] = dot[j];
             }
         }
     }
 }
 
-// lanes that share a flow whose row has `units` units: a power of two up to 32
-uint32_t lanes_for(uint32_t units) { uint32_t l = 1; while (l < 32 && l < units) l *= 2; return l; }
+// Lanes that share a flow whose row has `units` words: up to a warp, and more while the flows alone would not fill the machine (5 flows of
+// 2489 values over 8 experts: 167 us with a warp a flow).
+uint32_t lanes_for(const sf_ctx* ctx, uint32_t units, uint32_t n) {
+    uint32_t l = 1;
+    while (l < 32 && l < units) l *= 2;
+    while (l >= 32 && l < kThreads && l < units && (uint64_t)n * l < (uint64_t)ctx->num_sms * 1024) l *= 2;
+    return l;
+}
 uint32_t flow_grid(const sf_ctx* ctx, uint32_t n, uint32_t lanes) {
     const uint32_t per = kThreads / lanes;
     return std::min<uint32_t>((n + per - 1) / per, (uint32_t)ctx->num_sms * 8);
+}
+// the largest word (16, 4 or sizeof(element) bytes) in which rows at p with pitch ld can be moved
+uint32_t word_of(const void* p, size_t ld, uint32_t size) {
+    const size_t at = (uintptr_t)p | (ld * size);
+    return at % 16 == 0 ? 16 : (at % 4 == 0 ? 4 : size);
+}
+// calls f with the elements per word and words per lane
+template <typename T, typename F> int by_word(uint32_t bytes, F f) {
+    using std::integral_constant;
+    if (bytes == 16) return f(integral_constant<int, 16 / sizeof(T)>());
+    if constexpr (sizeof(T) == 2) { if (bytes == 4) return f(integral_constant<int, 2>()); }
+    return f(integral_constant<int, 1>());
 }
 // blocks that zero an expert's filling rows (up to align - 1 of them; the host knows neither their number nor `align`)
 uint32_t fill_blocks(const sf_ctx* ctx, uint32_t E, uint32_t units) {
@@ -539,7 +607,6 @@ bool fits(const void* p, size_t ld, int dtype, uint32_t count) {
     const size_t piece = std::min<size_t>(32, count * type_bytes(dtype));
     return aligned(p, piece) && (ld * type_bytes(dtype)) % piece == 0;
 }
-bool fits16(const void* p, size_t ld, int dtype) { return aligned(p, 16) && (ld * type_bytes(dtype)) % 16 == 0; }
 
 }  // namespace
 
@@ -626,16 +693,16 @@ extern "C" int sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uin
     if (!aligned(x, type_bytes(dtype)) || !aligned(rows_out, type_bytes(dtype)) || !aligned(row_of_pair, 4) || !aligned(offsets, 4) || !aligned(counts, 4) || !aligned(n_dev, 4)) return SF_ERR_ARG;
     SF_ON_DEVICE(ctx);
     const uint32_t size = type_bytes(dtype);
-    const bool al = fits16(x, ldx, dtype) && fits16(rows_out, ldr, dtype) && ((size_t)D * size) % 16 == 0;
+    const uint32_t word = std::min({word_of(x, ldx, size), word_of(rows_out, ldr, size), word_of(nullptr, D, size)});
     auto go = [&](auto q) {
         typedef decltype(q) Q;
-        const uint32_t per = sizeof(Q) / size, units = D / per, lanes = lanes_for(units), fb = flow_grid(ctx, n, lanes), zb = fill_blocks(ctx, E, units);
-        SF_CUDA(sf_launch_chained(gather_kernel<Q>, fb + E * zb, kThreads, 0, (cudaStream_t)stream, (const Q*)x, n_dev, n, units, ldx / per, k, row_of_pair, E,
+        constexpr int U = sizeof(Q) == 16 ? 4 : 8;
+        const uint32_t per = sizeof(Q) / size, units = D / per, lanes = lanes_for(ctx, units, n), fb = flow_grid(ctx, n, lanes), zb = fill_blocks(ctx, E, units);
+        SF_CUDA(sf_launch_chained(gather_kernel<Q, U>, fb + E * zb, kThreads, 0, (cudaStream_t)stream, (const Q*)x, n_dev, n, units, ldx / per, k, row_of_pair, E,
                                   offsets, counts, capacity, (Q*)rows_out, ldr / per, lanes, fb, zb, ctx->d_state));
         return SF_OK;
     };
-    if (al) return go(uint4());
-    return size == 4 ? go(uint32_t()) : go(uint16_t());
+    return word == 16 ? go(uint4()) : (word == 4 ? go(uint32_t()) : go(uint16_t()));
 }
 
 static int combine(sf_ctx* ctx, const void* rows, int dtype, uint32_t capacity, uint32_t D, size_t ldr, const int32_t* row_of_pair,
@@ -646,14 +713,17 @@ static int combine(sf_ctx* ctx, const void* rows, int dtype, uint32_t capacity, 
     if ((capacity && !rows) || !row_of_pair || !y) return SF_ERR_ARG;
     if (!aligned(rows, type_bytes(dtype)) || !aligned(y, type_bytes(dtype)) || !aligned(row_of_pair, 4) || !aligned(weights, 4) || !aligned(n_dev, 4)) return SF_ERR_ARG;
     SF_ON_DEVICE(ctx);
-    const bool al = fits16(rows, ldr, dtype) && fits16(y, ldy, dtype) && ((size_t)D * type_bytes(dtype)) % 16 == 0;
+    const uint32_t size = type_bytes(dtype);
+    const uint32_t word = std::min({word_of(rows, ldr, size), word_of(y, ldy, size), word_of(nullptr, D, size)});
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        constexpr int V = 16 / sizeof(T);
-        const uint32_t units = al ? D / V : D, lanes = lanes_for(units), grid = flow_grid(ctx, n, lanes);
-        auto kern = !al ? combine_kernel<T, 1, 4, false> : (units > 64 ? combine_kernel<T, V, 4, true> : (units > 32 ? combine_kernel<T, V, 2, true> : combine_kernel<T, V, 1, true>));
-        SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, (T*)y, ldy, lanes, ctx->d_state));
-        return SF_OK;
+        return by_word<T>(word, [&](auto v) {
+            constexpr int V = decltype(v)::value, U = V * sizeof(T) == 16 ? 4 : 8;
+            const uint32_t units = D / V, lanes = lanes_for(ctx, units, n), grid = flow_grid(ctx, n, lanes);
+            auto kern = units > 2 * lanes ? combine_kernel<T, V, U> : (units > lanes ? combine_kernel<T, V, 2> : combine_kernel<T, V, 1>);
+            SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, (T*)y, ldy, lanes, ctx->d_state));
+            return SF_OK;
+        });
     });
 }
 
@@ -681,15 +751,24 @@ extern "C" int sf_expert_combine_backward(sf_ctx* ctx, const void* dy, int dtype
     if (!aligned(dy, type_bytes(dtype)) || !aligned(rows, type_bytes(dtype)) || !aligned(d_rows_out, type_bytes(dtype)) || !aligned(row_of_pair, 4) || !aligned(weights, 4) ||
         !aligned(offsets, 4) || !aligned(counts, 4) || !aligned(d_weights_out, 4) || !aligned(n_dev, 4)) return SF_ERR_ARG;
     SF_ON_DEVICE(ctx);
-    const bool al = fits16(dy, ldy, dtype) && (!d_weights_out || fits16(rows, ldr, dtype)) && (!d_rows_out || fits16(d_rows_out, ldd, dtype)) && ((size_t)D * type_bytes(dtype)) % 16 == 0;
+    const uint32_t size = type_bytes(dtype);
+    uint32_t word = std::min(word_of(dy, ldy, size), word_of(nullptr, D, size));
+    if (d_weights_out) word = std::min(word, word_of(rows, ldr, size));
+    if (d_rows_out) word = std::min(word, word_of(d_rows_out, ldd, size));
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        constexpr int V = 16 / sizeof(T);
-        const uint32_t units = al ? D / V : D, lanes = lanes_for(units), fb = flow_grid(ctx, n, lanes), zb = fill_blocks(ctx, E, units), grid = fb + (d_rows_out ? E * zb : 0);
-        if (grid == 0) return SF_OK;
-        auto kern = al ? combine_backward_kernel<T, V, true> : combine_backward_kernel<T, 1, false>;
-        SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)dy, ldy, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, E,
-                                  offsets, counts, (T*)d_rows_out, ldd, d_weights_out, lanes, fb, zb, ctx->d_state));
-        return SF_OK;
+        return by_word<T>(word, [&](auto v) {
+            constexpr int V = decltype(v)::value, U = V * sizeof(T) == 16 ? 1 : 4;
+            const uint32_t units = D / V, lanes = lanes_for(ctx, units, n), fb = flow_grid(ctx, n, lanes), zb = fill_blocks(ctx, E, units), grid = fb + (d_rows_out ? E * zb : 0);
+            if (grid == 0) return (int)SF_OK;
+            // where flows fill the machine one pair at a time with two words on their way (120,003 x 1024 bf16, k = 2: 202 us; one word 276, two
+            // pairs 226 to 239), else up to four pairs in flight
+            constexpr int U2 = U == 1 ? 2 : U;
+            auto kern = (uint64_t)n * lanes >= (uint64_t)ctx->num_sms * 2048 ? combine_backward_kernel<T, V, U2, 1> : (k == 1 ? combine_backward_kernel<T, V, U, 1> :
+                        (k == 2 ? combine_backward_kernel<T, V, U, 2> : combine_backward_kernel<T, V, U, 4>));
+            SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)dy, ldy, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, E,
+                                      offsets, counts, (T*)d_rows_out, ldd, d_weights_out, lanes, fb, zb, ctx->d_state));
+            return (int)SF_OK;
+        });
     });
 }

@@ -17,6 +17,12 @@ using namespace sfmx;
 constexpr uint32_t kQThreads = 256;
 constexpr uint32_t kPCols = 512;                   // columns a warp packs or unpacks at once: 16 per lane, 2 lanes to a scale block
 
+// item i of rows of `chunks` pieces -> row and piece (a 64-bit division only where 32 bits do not hold i)
+__device__ __forceinline__ void row_and_piece(uint64_t i, uint32_t chunks, uint32_t& row, uint32_t& c) {
+    if (i >> 32) { row = (uint32_t)(i / chunks); c = (uint32_t)(i - (uint64_t)row * chunks); }
+    else { row = (uint32_t)i / chunks; c = (uint32_t)i - row * chunks; }
+}
+
 // bits of the largest magnitude of 16 values, as fp32: magnitudes order as their bits do, so 16-bit values are compared in pairs
 // as they are
 __device__ __forceinline__ uint32_t top_bits(const uint4 (&q)[4], float) {
@@ -42,7 +48,7 @@ __device__ __forceinline__ uint32_t top_bits(const uint4 (&q)[2], __half) { retu
 // consecutive values of one row (16 per lane: two or four 16-byte loads, one 8-byte store), a block's maximum is taken over two
 // lanes, and U such pieces are on their way before the first is packed.  Smaller pieces one at a time (8 values a lane) ran
 // at 2.9 TB/s at 240,001 x 2048 bf16.
-template <typename T, bool ALIGNED, int U>
+template <typename T, int U>
 __global__ void __launch_bounds__(kQThreads)
 mx4_quantise_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, size_t ld, const int32_t* __restrict__ row_ids,
                     const uint32_t* __restrict__ n_rows_dev, uint32_t capacity, uint8_t* __restrict__ data,
@@ -59,7 +65,8 @@ mx4_quantise_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, size_t 
     for (uint64_t i0 = ((uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5)) * U; i0 < items; i0 += step) {
         union Words { uint4 q[Q]; T e[16]; } w[U];
         uint32_t row[U], k[U];
-        uint32_t r = (uint32_t)(i0 / chunks), c = (uint32_t)(i0 - (uint64_t)r * chunks);
+        uint32_t r, c;
+        row_and_piece(i0, chunks, r, c);
 #pragma unroll
         for (int u = 0; u < U; u++) {
             row[u] = r;
@@ -71,7 +78,7 @@ mx4_quantise_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, size_t 
             for (int q = 0; q < Q; q++) w[u].q[q] = make_uint4(0, 0, 0, 0);
             if (src >= 0 && k[u] < K) {
                 const T* p = x + (size_t)src * ld + k[u];
-                if (ALIGNED && k[u] + 16 <= K) {
+                if (k[u] + 16 <= K) {
 #pragma unroll
                     for (int q = 0; q < Q; q++) w[u].q[q] = __ldg(reinterpret_cast<const uint4*>(p) + q);
                 } else {
@@ -103,9 +110,61 @@ mx4_quantise_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, size_t 
     }
 }
 
+// The same for rows on any boundary: a warp takes 256 consecutive values with coalesced loads of single elements, 8 on their way in every lane
+// and piece, and turns them round in shared memory so that a lane has 8 consecutive ones (lanes that load their own 16 values
+// element by element ran at 0.6 TB/s at 141,031 x 1065 bf16).
+constexpr uint32_t kACols = 256;
+template <typename T>
+__global__ void __launch_bounds__(kQThreads)
+mx4_quantise_any_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, size_t ld, const int32_t* __restrict__ row_ids,
+                        const uint32_t* __restrict__ n_rows_dev, uint32_t capacity, uint8_t* __restrict__ data,
+                        uint8_t* __restrict__ scales, sf_dev_state* st)
+{
+    __shared__ float4 turn[kQThreads / 32][kACols / 4];
+    sf_chain_enter();
+    const uint32_t rows = n_rows_dev ? sf_clamp_rows(*n_rows_dev, capacity, st) : capacity;
+    const uint32_t pitch = row_bytes(K), blocks = pitch / 16, kt = k_tiles(K);
+    const uint32_t chunks = (kt * 128 + kACols - 1) / kACols;
+    const uint32_t lane = threadIdx.x & 31;
+    float* const mine = reinterpret_cast<float*>(turn[threadIdx.x >> 5]);
+    const uint64_t items = (uint64_t)rows * chunks;
+    const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32);
+    for (uint64_t i = (uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5); i < items; i += step) {
+        uint32_t row, k0;
+        row_and_piece(i, chunks, row, k0);
+        k0 *= kACols;
+        int64_t src = row;
+        if (row_ids) { const int32_t id = row_ids[row]; src = (id >= 0 && (uint32_t)id < n_src) ? id : -1; }
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const uint32_t k = k0 + j * 32 + lane;
+            v[j] = src >= 0 && k < K ? to_f32(x[(size_t)src * ld + k]) : 0.0f;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; j++) mine[j * 32 + lane] = v[j];
+        __syncwarp();
+        const float4 a = reinterpret_cast<const float4*>(mine)[2 * lane], b = reinterpret_cast<const float4*>(mine)[2 * lane + 1];
+        const float y[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; j++) top = max(top, __float_as_uint(y[j]) & 0x7FFFFFFFu);
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const uint32_t byte = scale_byte(top), k = k0 + lane * 8;
+        const uint32_t codes = encode8(y, byte);
+        if (k < pitch * 2) *reinterpret_cast<uint32_t*>(data + (size_t)row * pitch + k / 2) = codes;
+        if ((lane & 3) == 0) {
+            const uint32_t q = k / 32;
+            if (q < kt * 4) scales[scale_at(row, q, kt)] = q < blocks ? (uint8_t)byte : (uint8_t)127;
+        }
+    }
+}
+
 // data, scales -> out[rows][ld].  The same split the other way round: 16 values a lane, whole 32-byte sectors where rows are on
-// 32-byte boundaries (SECTORS).  Bound: HBM writes (this card writes 3.9 TB/s where it copies 6.5).
-template <typename T, bool SECTORS>
+// 32-byte boundaries.  Bound: HBM writes (this card writes 3.9 TB/s where it copies 6.5).
+template <typename T>
 __global__ void __launch_bounds__(kQThreads)
 mx4_unpack_kernel(const uint8_t* __restrict__ data, const uint8_t* __restrict__ scales, const uint32_t* __restrict__ n_rows_dev,
                   uint32_t capacity, uint32_t K, T* __restrict__ out, size_t ld, sf_dev_state* st)
@@ -119,7 +178,8 @@ mx4_unpack_kernel(const uint8_t* __restrict__ data, const uint8_t* __restrict__ 
     const uint64_t items = (uint64_t)rows * chunks;
     const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32) * U;
     for (uint64_t i0 = ((uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5)) * U; i0 < items; i0 += step) {
-        uint32_t r = (uint32_t)(i0 / chunks), c = (uint32_t)(i0 - (uint64_t)r * chunks);
+        uint32_t r, c;
+        row_and_piece(i0, chunks, r, c);
         uint2 codes[U];
         uint32_t byte[U], row[U], k[U];
 #pragma unroll
@@ -142,11 +202,45 @@ mx4_unpack_kernel(const uint8_t* __restrict__ data, const uint8_t* __restrict__ 
 #pragma unroll
             for (int j = 0; j < 8; j++) { v[j] = a[j]; v[8 + j] = b[j]; }
             T* p = out + (size_t)row[u] * ld + k[u];
-            if (SECTORS && k[u] + 16 <= K) store_sectors<T, 16>(p, v);
+            if (k[u] + 16 <= K) store_sectors<T, 16>(p, v);
             else {
 #pragma unroll
                 for (int j = 0; j < 16; j++) if (k[u] + j < K) p[j] = from_f32<T>(v[j]);
             }
+        }
+    }
+}
+
+// The same for rows on any boundary: turned round in shared memory, stored element by element, coalesced.
+template <typename T>
+__global__ void __launch_bounds__(kQThreads)
+mx4_unpack_any_kernel(const uint8_t* __restrict__ data, const uint8_t* __restrict__ scales, const uint32_t* __restrict__ n_rows_dev,
+                      uint32_t capacity, uint32_t K, T* __restrict__ out, size_t ld, sf_dev_state* st)
+{
+    __shared__ float4 turn[kQThreads / 32][kACols / 4];
+    sf_chain_enter();
+    const uint32_t rows = n_rows_dev ? sf_clamp_rows(*n_rows_dev, capacity, st) : capacity;
+    const uint32_t pitch = row_bytes(K), kt = k_tiles(K);
+    const uint32_t chunks = (K + kACols - 1) / kACols;
+    const uint32_t lane = threadIdx.x & 31;
+    float* const mine = reinterpret_cast<float*>(turn[threadIdx.x >> 5]);
+    const uint64_t items = (uint64_t)rows * chunks;
+    const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32);
+    for (uint64_t i = (uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5); i < items; i += step) {
+        uint32_t row, k0;
+        row_and_piece(i, chunks, row, k0);
+        k0 *= kACols;
+        const uint32_t k = k0 + lane * 8;
+        float v[8] = {};
+        if (k < K) decode8(__ldg(reinterpret_cast<const uint32_t*>(data + (size_t)row * pitch + k / 2)), scale_f32(__ldg(scales + scale_at(row, k / 32, kt))), v);
+        __syncwarp();
+        reinterpret_cast<float4*>(mine)[2 * lane] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(mine)[2 * lane + 1] = make_float4(v[4], v[5], v[6], v[7]);
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const uint32_t c = k0 + j * 32 + lane;
+            if (c < K) out[(size_t)row * ld + c] = from_f32<T>(mine[j * 32 + lane]);
         }
     }
 }
@@ -182,14 +276,15 @@ extern "C" int sf_mx4_quantise(sf_ctx* ctx, const void* x, int dtype, uint32_t n
 int sf_launch_mx4_quantise(sf_ctx* ctx, const void* x, int dtype, uint32_t n_src, uint32_t K, size_t ld, const int32_t* row_ids,
                            const uint32_t* n_rows_dev, uint32_t capacity, uint8_t* data, uint8_t* scales, cudaStream_t st)
 {
-    const uint64_t items = (uint64_t)capacity * ((k_tiles(K) * 128 + kPCols - 1) / kPCols);
     const bool al = aligned(x, 16) && (ld * type_bytes(dtype)) % 16 == 0;
+    const uint32_t cols = al ? kPCols : kACols;
+    const uint64_t items = (uint64_t)capacity * ((k_tiles(K) * 128 + cols - 1) / cols);
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
         constexpr int U = 8 / sizeof(T);               // 8 16-byte words a lane on their way, where there are pieces enough for all warps
-        const bool many = items >= (uint64_t)ctx->num_sms * 64 * U;
-        auto k = al ? (many ? mx4_quantise_kernel<T, true, U> : mx4_quantise_kernel<T, true, 1>) : mx4_quantise_kernel<T, false, 1>;
-        SF_CUDA(sf_launch_chained(k, row_grid(ctx, al && many ? (items + U - 1) / U : items, 32), kQThreads, 0, st, (const T*)x, n_src, K, ld, row_ids, n_rows_dev, capacity, data, scales, ctx->d_state));
+        const bool many = al && items >= (uint64_t)ctx->num_sms * 64 * U;
+        auto k = al ? (many ? mx4_quantise_kernel<T, U> : mx4_quantise_kernel<T, 1>) : mx4_quantise_any_kernel<T>;
+        SF_CUDA(sf_launch_chained(k, row_grid(ctx, many ? (items + U - 1) / U : items, 32), kQThreads, 0, st, (const T*)x, n_src, K, ld, row_ids, n_rows_dev, capacity, data, scales, ctx->d_state));
         return SF_OK;
     });
 }
@@ -202,11 +297,11 @@ extern "C" int sf_mx4_unpack(sf_ctx* ctx, const uint8_t* data, const uint8_t* sc
     if (!data || !scales || !out) return SF_ERR_ARG;
     if (!aligned(out, type_bytes(dtype)) || !aligned(data, 16) || !aligned(scales, 16) || !aligned(n_rows_dev, 4)) return SF_ERR_ARG;
     SF_ON_DEVICE(ctx);
-    const uint32_t grid = row_grid(ctx, ((uint64_t)capacity * ((K + kPCols - 1) / kPCols) + 1) / 2, 8);
     const bool al = aligned(out, 32) && (ld * type_bytes(dtype)) % 32 == 0;
+    const uint32_t grid = al ? row_grid(ctx, ((uint64_t)capacity * ((K + kPCols - 1) / kPCols) + 1) / 2, 8) : row_grid(ctx, (uint64_t)capacity * ((K + kACols - 1) / kACols), 32);
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        auto k = al ? mx4_unpack_kernel<T, true> : mx4_unpack_kernel<T, false>;
+        auto k = al ? mx4_unpack_kernel<T> : mx4_unpack_any_kernel<T>;
         SF_CUDA(sf_launch_chained(k, grid, kQThreads, 0, (cudaStream_t)stream, data, scales, n_rows_dev, capacity, K, (T*)out, ld, ctx->d_state));
         return SF_OK;
     });

@@ -25,24 +25,42 @@ __device__ __forceinline__ float scale_f32(uint32_t byte) {
     return __uint_as_float(byte == 255u ? 0x7FC00000u : (byte ? byte << 23 : 0x00400000u));
 }
 
-// eight values -> eight codes (value j in bits 4j..4j+3).  1 / scale = 2^(127 - byte) is a normal number for every byte <= 252,
-// the largest that occurs.
+// eight values -> eight codes (value j in bits 4j..4j+3); RELU: negative ones become 0.  1 / scale = 2^(127 - byte) is a normal number for
+// every byte <= 252, the largest that occurs.  A block that stands for NaN has codes 0.
+template <bool RELU = false>
 __device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t byte) {
-    const float inv = byte == 255u ? 0.0f : __uint_as_float((254u - byte) << 23);
+    const float inv = __uint_as_float((254u - min(byte, 253u)) << 23);
     float q[8];
 #pragma unroll
-    for (int j = 0; j < 8; j++) q[j] = byte == 255u ? 0.0f : v[j] * inv;
+    for (int j = 0; j < 8; j += 2) {
+        uint64_t a, b;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(a) : "f"(v[j]), "f"(v[j + 1]));
+        asm("mov.b64 %0, {%1, %1};" : "=l"(b) : "f"(inv));
+        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(a) : "l"(b));
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(q[j]), "=f"(q[j + 1]) : "l"(a));
+    }
     uint32_t r;
-    asm("{\n"
-        ".reg .b8 b0, b1, b2, b3;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
-        "mov.b32 %0, {b0, b1, b2, b3};\n"
-        "}\n"
-        : "=r"(r) : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
-    return r;
+    if constexpr (RELU)
+        asm("{\n"
+            ".reg .b8 b0, b1, b2, b3;\n"
+            "cvt.rn.satfinite.relu.e2m1x2.f32 b0, %2, %1;\n"
+            "cvt.rn.satfinite.relu.e2m1x2.f32 b1, %4, %3;\n"
+            "cvt.rn.satfinite.relu.e2m1x2.f32 b2, %6, %5;\n"
+            "cvt.rn.satfinite.relu.e2m1x2.f32 b3, %8, %7;\n"
+            "mov.b32 %0, {b0, b1, b2, b3};\n"
+            "}\n"
+            : "=r"(r) : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
+    else
+        asm("{\n"
+            ".reg .b8 b0, b1, b2, b3;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+            "mov.b32 %0, {b0, b1, b2, b3};\n"
+            "}\n"
+            : "=r"(r) : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
+    return byte == 255u ? 0u : r;
 }
 __device__ __forceinline__ void decode8(uint32_t codes, float scale, float (&v)[8]) {
     uint32_t h[4];

@@ -146,6 +146,29 @@ template <typename T, uint32_t COLS, bool RELU> __device__ __forceinline__ void 
     }
 }
 
+// 32-column blocks of a row's fp32 values -> words of codes and scale bytes.  With ReLU a negative value orders below 0 as a signed
+// integer and the conversion clamps it; a NaN that an addition made is positive and orders above infinity.
+template <uint32_t COLS, bool RELU> __device__ __forceinline__ void pack_blocks(const uint32_t (&v)[COLS], uint32_t (&w)[COLS / 8], uint32_t& bytes) {
+#pragma unroll
+    for (uint32_t g = 0; g < COLS; g += 32) {
+        int top = 0;
+#pragma unroll
+        for (uint32_t q = 0; q < 32; q += 2) {
+            if (RELU) top = __vimax3_s32(top, (int)v[g + q], (int)v[g + q + 1]);
+            else top = __vimax3_s32(top, (int)(v[g + q] & 0x7FFFFFFFu), (int)(v[g + q + 1] & 0x7FFFFFFFu));
+        }
+        const uint32_t byte = scale_byte((uint32_t)top);
+        bytes |= byte << (g / 4);
+#pragma unroll
+        for (uint32_t q = 0; q < 4; q++) {
+            float x[8];
+#pragma unroll
+            for (uint32_t r = 0; r < 8; r++) x[r] = __uint_as_float(v[g + q * 8 + r]);
+            w[g / 8 + q] = encode8<RELU>(x, byte);
+        }
+    }
+}
+
 // A value that is the same in all lanes, told to the compiler as such: loop bounds and addresses that come out of shared memory
 // would otherwise keep the issuing warps' operands out of the uniform registers.
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
@@ -395,32 +418,34 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     asm volatile("bar.sync %0, 128;" ::"r"(1u + half) : "memory");
                 }
                 if (col0 + c >= (kPacked ? k_tiles(p.N) * 128 : p.N)) continue;
-                if (p.relu) finish<T, kCols, true>(v, bias_s + c);
+                if (!kPacked && p.relu) finish<T, kCols, true>(v, bias_s + c);
                 else finish<T, kCols, false>(v, bias_s + c);
                 if constexpr (kPacked) {
                     // a lane's 32 consecutive columns are one scale block
-                    const uint32_t pitch = row_bytes(p.N), kt = k_tiles(p.N);
+                    const uint32_t col = col0 + c, pitch = row_bytes(p.N), kt = k_tiles(p.N);
+                    if (col + kCols > p.N) {                                 // columns that fill the last block, and blocks behind it
 #pragma unroll
-                    for (uint32_t g = 0; g < kCols; g += 32) {
-                        const uint32_t col = col0 + c + g;
-                        uint32_t top = 0;
+                        for (uint32_t q = 0; q < kCols; q++) if (col + q >= p.N) v[q] = 0;
+                    }
+                    uint32_t w[kCols / 8], bytes = 0;
+                    if (p.relu) pack_blocks<kCols, true>(v, w, bytes); else pack_blocks<kCols, false>(v, w, bytes);
 #pragma unroll
-                        for (uint32_t q = 0; q < 32; q++) {
-                            if (col + q >= p.N) v[g + q] = 0;              // columns that fill the last block
-                            top = max(top, v[g + q] & 0x7FFFFFFFu);
-                        }
-                        const uint32_t byte = scale_byte(top);
-                        uint32_t w[4];
-#pragma unroll
-                        for (uint32_t q = 0; q < 4; q++) {
-                            float x[8];
-#pragma unroll
-                            for (uint32_t r = 0; r < 8; r++) x[r] = __uint_as_float(v[g + q * 8 + r]);
-                            w[q] = encode8(x, byte);
-                        }
-                        if (row0 + lane < end) {
-                            if (col < p.N) *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(p.out) + (size_t)(row0 + lane) * pitch + col / 2) = make_uint4(w[0], w[1], w[2], w[3]);
-                            if (col / 32 < kt * 4) p.out_scales[scale_at(row0 + lane, col / 32, kt)] = col < p.N ? (uint8_t)byte : (uint8_t)127;
+                    for (uint32_t g = 0; g < kCols; g += 32) if (col + g >= p.N) bytes = (bytes & ~(0xFFu << (g / 4))) | 127u << (g / 4);
+                    if (row0 + lane < end) {
+                        uint8_t* const o = reinterpret_cast<uint8_t*>(p.out) + (size_t)(row0 + lane) * pitch + col / 2;
+                        uint8_t* const so = p.out_scales + scale_at(row0 + lane, col / 32, kt);
+                        if constexpr (kCols == 64) {
+                            if (col + 32 < p.N && (((uintptr_t)p.out | pitch) & 31u) == 0)         // whole 32-byte sectors
+                                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                                             ::"l"(o), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+                            else {
+                                if (col < p.N) *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+                                if (col + 32 < p.N) *reinterpret_cast<uint4*>(o + 16) = make_uint4(w[4], w[5], w[6], w[7]);
+                            }
+                            *reinterpret_cast<uint16_t*>(so) = (uint16_t)bytes;              // (col < k_tiles * 128: both blocks have a place)
+                        } else {
+                            if (col < p.N) *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+                            *so = (uint8_t)bytes;
                         }
                     }
                 } else {

@@ -43,6 +43,26 @@ __device__ __forceinline__ void store_f32(T* __restrict__ p, const float (&x)[N]
     }
 }
 
+// N elements as one access of N * sizeof(T) = 2, 4 or 16 bytes (p on a boundary of as many)
+template <int BYTES> struct Word;
+template <> struct Word<2> { typedef uint16_t type; };
+template <> struct Word<4> { typedef uint32_t type; };
+template <> struct Word<16> { typedef uint4 type; };
+template <typename T, int N> __device__ __forceinline__ void load_word(const T* __restrict__ p, float (&x)[N]) {
+    typedef typename Word<N * sizeof(T)>::type W;
+    union { W w; T e[N]; } u;
+    u.w = __ldg(reinterpret_cast<const W*>(p));
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = to_f32(u.e[i]);
+}
+template <typename T, int N> __device__ __forceinline__ void store_word(T* __restrict__ p, const float (&x)[N]) {
+    typedef typename Word<N * sizeof(T)>::type W;
+    union { W w; T e[N]; } u;
+#pragma unroll
+    for (int i = 0; i < N; i++) u.e[i] = from_f32<T>(x[i]);
+    *reinterpret_cast<W*>(p) = u.w;
+}
+
 // N elements as whole 32-byte accesses (p on a 32-byte boundary): a lane that has 32 bytes or more of a row to itself then moves whole
 // sectors, where 16-byte stores would send every sector twice
 template <typename T, int N>
