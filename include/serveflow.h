@@ -71,6 +71,7 @@ extern "C" {
 #define SF_GATE_SOFTMAX_PICKED 1   /* ... over the picked scores only */
 #define SF_GATE_SHARE          2   /* ... its share of the picked scores' sum (scores = class probabilities of the fast model) */
 #define SF_MAX_EXPERTS  1024
+#define SF_EXPERT_MAX_D 16777216u  /* widest row that the expert calls move */
 
 /* |margin| threshold equivalent to |sigmoid(margin) - 0.5| < 0.2: fp32(ln(0.7/0.3)) */
 #define SF_TAU_MARGIN_DEFAULT 0x1.b1d106p-1f
@@ -355,7 +356,7 @@ int  sf_mx4_matmul_experts(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_scale
  * with flow_of_row) -> the experts' layers on their rows (sf_mx4_matmul_experts) -> combine, and the gradients of each for
  * training.  n = flows the arrays hold; n_dev (nullable, device) = flows present (a larger count is clamped and records
  * SF_ERR_CAPACITY); what belongs to flows at or beyond it is left as it was.  E <= SF_MAX_EXPERTS, k <= E (where E is
- * given), n*k < 2^31.  None of them uses the context's workspace, so they may be captured in graphs and run on several streams of
+ * given), n*k < 2^31, D <= SF_EXPERT_MAX_D.  None of them uses the context's workspace, so they may be captured in graphs and run on several streams of
  * one context at once.  All sums are fp32 in a fixed order; results do not vary from run to run.
  *
  * Gate: the k largest of each row's E scores (scores[n][ld]), largest first, ties to the lowest index, into ids_out int32[n][k]
@@ -364,7 +365,7 @@ int  sf_mx4_matmul_experts(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_scale
  * picked scores' sum is not positive. */
 int  sf_expert_gate(sf_ctx* ctx, const void* scores, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t E, size_t ld,
                     uint32_t k, int mode, int32_t* ids_out, float* weights_out, void* stream);
-/* d_scores_out[n][ldd] (same dtype) from the weights' gradient d_weights fp32[n][k]; ids are those that the gate gave. */
+/* d_scores_out[n][ldd] (same dtype, apart from scores) from the weights' gradient d_weights fp32[n][k]; ids are those that the gate gave. */
 int  sf_expert_gate_backward(sf_ctx* ctx, const void* scores, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t E, size_t ld,
                              uint32_t k, int mode, const int32_t* ids, const float* d_weights, void* d_scores_out, size_t ldd,
                              void* stream);

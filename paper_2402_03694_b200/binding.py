@@ -176,20 +176,10 @@ def _dp(t):
     return t.data_ptr()
 
 
-_current = None
-
-
 def _stream(stream):
-    """Address of a stream; None = torch's current one (asked for through torch's raw accessors where it has them: a torch.cuda.Stream
-    object per call costs more than a small launch)."""
-    global _current
     if stream is None:
-        if _current is None:
-            import torch
-            raw, dev = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
-            torch.cuda.current_stream()               # initialises CUDA
-            _current = (lambda: raw(dev())) if raw and dev else (lambda: torch.cuda.current_stream().cuda_stream)
-        return _current()
+        import torch
+        return torch.cuda.current_stream().cuda_stream
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -220,13 +210,18 @@ def make_route_cfg(rule, tau, wide_layout, row_dtype, P, capacity, P_real=0):
     return c
 
 
+_ctx_device = {}                  # context -> device, for the calls that look at their tensors
+
+
 def sf_ctx_create(device=0, workspace_bytes=0):
     h = C.c_void_p()
     _check(_lib().sf_ctx_create(C.byref(h), device, workspace_bytes), "sf_ctx_create")
+    _ctx_device[h.value] = device
     return h
 
 
 def sf_ctx_destroy(ctx):
+    _ctx_device.pop(getattr(ctx, "value", ctx), None)
     _lib().sf_ctx_destroy(ctx)
 
 
@@ -377,8 +372,24 @@ def sf_serve_batch_intermediates(ctx):
 
 
 # ---- rows in 4 bits, experts: device tensors in, sizes and pitches taken from them ----------------------------------------
-# Unlike the calls above these take their sizes from the tensors, so they look at them first: a wrong type, shape, stride or a
-# tensor in host memory raises SfError(SF_ERR_ARG) before anything is launched.
+# Unlike the calls above these take their sizes from the tensors, so they look at them first: a wrong type, shape or stride, a tensor in
+# host memory or on another device than the context raises SfError(SF_ERR_ARG) before anything is launched.
+_raw_stream = None
+
+
+def _stream_on(ctx, t, stream, where):
+    """Address of a stream for a call of `ctx` on tensor t; None = torch's current one on the tensor's device (by torch's raw accessor where
+    it has one: a torch.cuda.Stream object per call costs more than a small launch)."""
+    global _raw_stream
+    device = t.get_device()
+    if device != _ctx_device.get(getattr(ctx, "value", ctx), device):
+        raise SfError(SF_ERR_ARG, where)
+    if stream is None:
+        if _raw_stream is None:
+            import torch
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+        return _raw_stream(device)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 def _arg(ok, where):
     if not ok:
@@ -439,7 +450,7 @@ def sf_mx4_quantise(ctx, x, data_out, scales_out, row_ids=None, n_rows_dev=None,
     m = n if row_ids is None else row_ids.numel()
     pitch, sb = _mx4_bytes(m, K)
     _check(_lib().sf_mx4_quantise(ctx, p, dt, n, K, ld, _flat(row_ids, m, 4, w), _flat(n_rows_dev, 1, 4, w), m,
-                                  _flat(data_out, m * pitch, 1, w), _flat(scales_out, sb, 1, w), _stream(stream)), w)
+                                  _flat(data_out, m * pitch, 1, w), _flat(scales_out, sb, 1, w), _stream_on(ctx, x, stream, w)), w)
 
 
 def sf_mx4_unpack(ctx, data, scales, out, n_rows_dev=None, stream=None):
@@ -447,7 +458,7 @@ def sf_mx4_unpack(ctx, data, scales, out, n_rows_dev=None, stream=None):
     p, dt, n, K, ld = _rows(out, w)
     pitch, sb = _mx4_bytes(n, K)
     _check(_lib().sf_mx4_unpack(ctx, _flat(data, n * pitch, 1, w), _flat(scales, sb, 1, w), _flat(n_rows_dev, 1, 4, w), n, K, dt, p, ld,
-                                _stream(stream)), w)
+                                _stream_on(ctx, out, stream, w)), w)
 
 
 def _product_out(out, out_scales, N, w):
@@ -469,7 +480,7 @@ def sf_mx4_matmul(ctx, a, a_scales, w, w_scales, K, out, bias=None, relu=False, 
     pitch, ab = _mx4_bytes(n, K)
     _check(_lib().sf_mx4_matmul(ctx, _flat(a, n * pitch, 1, s), _flat(a_scales, ab, 1, s), _flat(n_rows_dev, 1, 4, s), n,
                                 _flat(w, N * pitch, 1, s), _flat(w_scales, _mx4_bytes(N, K)[1], 1, s), N, K, _flat(bias, N, 4, s),
-                                int(relu), dt, p, ld, os_, _stream(stream)), s)
+                                int(relu), dt, p, ld, os_, _stream_on(ctx, out, stream, s)), s)
 
 
 def sf_mx4_matmul_experts(ctx, a, a_scales, w, w_scales, K, offsets, out, bias=None, relu=False, out_scales=None, N=None, stream=None):
@@ -481,7 +492,7 @@ def sf_mx4_matmul_experts(ctx, a, a_scales, w, w_scales, K, offsets, out, bias=N
     pitch, ab = _mx4_bytes(n, K)
     _check(_lib().sf_mx4_matmul_experts(ctx, _flat(a, n * pitch, 1, s), _flat(a_scales, ab, 1, s), _flat(offsets, E + 1, 4, s), E, n,
                                         _flat(w, E * N * pitch, 1, s), _flat(w_scales, E * _mx4_bytes(N, K)[1], 1, s), N, K,
-                                        _flat(bias, E * N, 4, s), int(relu), dt, p, ld, os_, _stream(stream)), s)
+                                        _flat(bias, E * N, 4, s), int(relu), dt, p, ld, os_, _stream_on(ctx, out, stream, s)), s)
 
 
 def sf_expert_gate(ctx, scores, mode, ids_out, weights_out, n_dev=None, stream=None):
@@ -491,7 +502,7 @@ def sf_expert_gate(ctx, scores, mode, ids_out, weights_out, n_dev=None, stream=N
     _arg(ids_out.dim() == 2, w)
     k = ids_out.shape[1]
     _check(_lib().sf_expert_gate(ctx, p, dt, _flat(n_dev, 1, 4, w), n, E, ld, k, mode, _whole(ids_out, (n, k), w),
-                                 _whole(weights_out, (n, k), w), _stream(stream)), w)
+                                 _whole(weights_out, (n, k), w), _stream_on(ctx, scores, stream, w)), w)
 
 
 def sf_expert_gate_backward(ctx, scores, mode, ids, d_weights, d_scores_out, n_dev=None, stream=None):
@@ -501,7 +512,7 @@ def sf_expert_gate_backward(ctx, scores, mode, ids, d_weights, d_scores_out, n_d
     _arg(dq == dt and m == n and F == E and ids.dim() == 2, w)
     k = ids.shape[1]
     _check(_lib().sf_expert_gate_backward(ctx, p, dt, _flat(n_dev, 1, 4, w), n, E, ld, k, mode, _whole(ids, (n, k), w),
-                                          _whole(d_weights, (n, k), w), q, ldd, _stream(stream)), w)
+                                          _whole(d_weights, (n, k), w), q, ldd, _stream_on(ctx, scores, stream, w)), w)
 
 
 def sf_expert_sort_workspace(n, k, E):
@@ -521,7 +532,7 @@ def sf_expert_sort(ctx, ids, E, align, offsets_out, counts_out, flow_of_row_out,
     cap = flow_of_row_out.numel()
     _check(_lib().sf_expert_sort(ctx, _whole(ids, (n, k), w), _flat(n_dev, 1, 4, w), n, k, E, align, cap, _flat(offsets_out, E + 1, 4, w),
                                  _flat(counts_out, E, 4, w), _flat(flow_of_row_out, cap, 4, w), _whole(row_of_pair_out, (n, k), w),
-                                 _dp(workspace), wb, _stream(stream)), w)
+                                 _dp(workspace), wb, _stream_on(ctx, ids, stream, w)), w)
 
 
 def sf_expert_gather(ctx, x, row_of_pair, offsets, counts, rows_out, n_dev=None, stream=None):
@@ -533,7 +544,7 @@ def sf_expert_gather(ctx, x, row_of_pair, offsets, counts, rows_out, n_dev=None,
     _arg(dq == dt and F == D and row_of_pair.dim() == 2, w)
     k = row_of_pair.shape[1]
     _check(_lib().sf_expert_gather(ctx, p, dt, _flat(n_dev, 1, 4, w), n, D, ld, k, _whole(row_of_pair, (n, k), w), E,
-                                   _flat(offsets, E + 1, 4, w), _flat(counts, E, 4, w), cap, q, ldr, _stream(stream)), w)
+                                   _flat(offsets, E + 1, 4, w), _flat(counts, E, 4, w), cap, q, ldr, _stream_on(ctx, x, stream, w)), w)
 
 
 def _pairs_of(rows, row_of_pair, y, w):
@@ -547,7 +558,7 @@ def _pairs_of(rows, row_of_pair, y, w):
 def sf_expert_gather_backward(ctx, d_rows, row_of_pair, dx_out, n_dev=None, stream=None):
     w = "sf_expert_gather_backward"
     p, dt, cap, D, ldr, at, q, n, k, ldx = _pairs_of(d_rows, row_of_pair, dx_out, w)
-    _check(_lib().sf_expert_gather_backward(ctx, p, dt, cap, D, ldr, at, _flat(n_dev, 1, 4, w), n, k, q, ldx, _stream(stream)), w)
+    _check(_lib().sf_expert_gather_backward(ctx, p, dt, cap, D, ldr, at, _flat(n_dev, 1, 4, w), n, k, q, ldx, _stream_on(ctx, dx_out, stream, w)), w)
 
 
 def sf_expert_combine(ctx, rows, row_of_pair, weights, y_out, n_dev=None, stream=None):
@@ -555,7 +566,7 @@ def sf_expert_combine(ctx, rows, row_of_pair, weights, y_out, n_dev=None, stream
     w = "sf_expert_combine"
     p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, y_out, w)
     g = None if weights is None else _whole(weights, (n, k), w)
-    _check(_lib().sf_expert_combine(ctx, p, dt, cap, D, ldr, at, g, _flat(n_dev, 1, 4, w), n, k, q, ldy, _stream(stream)), w)
+    _check(_lib().sf_expert_combine(ctx, p, dt, cap, D, ldr, at, g, _flat(n_dev, 1, 4, w), n, k, q, ldy, _stream_on(ctx, y_out, stream, w)), w)
 
 
 def sf_expert_combine_backward(ctx, dy, rows, row_of_pair, weights, offsets, counts, d_rows_out, d_weights_out, n_dev=None, stream=None):
@@ -570,7 +581,7 @@ def sf_expert_combine_backward(ctx, dy, rows, row_of_pair, weights, offsets, cou
         _arg((dr, c2, D2) == (dt, cap, D), w)
     dw = None if d_weights_out is None else _whole(d_weights_out, (n, k), w)
     _check(_lib().sf_expert_combine_backward(ctx, q, dt, ldy, p, cap, D, ldr, at, g, _flat(n_dev, 1, 4, w), n, k, E,
-                                             _flat(offsets, E + 1, 4, w), _flat(counts, E, 4, w), r, ldd, dw, _stream(stream)), w)
+                                             _flat(offsets, E + 1, 4, w), _flat(counts, E, 4, w), r, ldd, dw, _stream_on(ctx, dy, stream, w)), w)
 
 
 def sf_table_create(ctx, log2_slots, fast_pkts, slow_pkts, slow_slabs):

@@ -687,7 +687,7 @@ extern "C" int sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uin
                                 const int32_t* row_of_pair, uint32_t E, const uint32_t* offsets, const uint32_t* counts, uint32_t capacity,
                                 void* rows_out, size_t ldr, void* stream)
 {
-    if (!ctx || !type_ok(dtype) || D == 0 || ldx < D || ldr < D || E == 0 || E > SF_MAX_EXPERTS || !sizes_ok(n, k) || capacity > 0x7FFFFFFFu) return SF_ERR_ARG;
+    if (!ctx || !type_ok(dtype) || D == 0 || D > SF_EXPERT_MAX_D || ldx < D || ldr < D || E == 0 || E > SF_MAX_EXPERTS || !sizes_ok(n, k) || capacity > 0x7FFFFFFFu) return SF_ERR_ARG;
     if (capacity == 0) return SF_OK;
     if ((n && (!x || !row_of_pair)) || !offsets || !counts || !rows_out) return SF_ERR_ARG;
     if (!aligned(x, type_bytes(dtype)) || !aligned(rows_out, type_bytes(dtype)) || !aligned(row_of_pair, 4) || !aligned(offsets, 4) || !aligned(counts, 4) || !aligned(n_dev, 4)) return SF_ERR_ARG;
@@ -708,7 +708,7 @@ extern "C" int sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uin
 static int combine(sf_ctx* ctx, const void* rows, int dtype, uint32_t capacity, uint32_t D, size_t ldr, const int32_t* row_of_pair,
                    const float* weights, const uint32_t* n_dev, uint32_t n, uint32_t k, void* y, size_t ldy, void* stream)
 {
-    if (!ctx || !type_ok(dtype) || D == 0 || ldr < D || ldy < D || !sizes_ok(n, k) || capacity > 0x7FFFFFFFu) return SF_ERR_ARG;
+    if (!ctx || !type_ok(dtype) || D == 0 || D > SF_EXPERT_MAX_D || ldr < D || ldy < D || !sizes_ok(n, k) || capacity > 0x7FFFFFFFu) return SF_ERR_ARG;
     if (n == 0) return SF_OK;
     if ((capacity && !rows) || !row_of_pair || !y) return SF_ERR_ARG;
     if (!aligned(rows, type_bytes(dtype)) || !aligned(y, type_bytes(dtype)) || !aligned(row_of_pair, 4) || !aligned(weights, 4) || !aligned(n_dev, 4)) return SF_ERR_ARG;
@@ -744,7 +744,7 @@ extern "C" int sf_expert_combine_backward(sf_ctx* ctx, const void* dy, int dtype
                                           uint32_t k, uint32_t E, const uint32_t* offsets, const uint32_t* counts, void* d_rows_out,
                                           size_t ldd, float* d_weights_out, void* stream)
 {
-    if (!ctx || !type_ok(dtype) || D == 0 || ldr < D || ldy < D || (d_rows_out && ldd < D) || E == 0 || E > SF_MAX_EXPERTS || !sizes_ok(n, k) || capacity > 0x7FFFFFFFu) return SF_ERR_ARG;
+    if (!ctx || !type_ok(dtype) || D == 0 || D > SF_EXPERT_MAX_D || ldr < D || ldy < D || (d_rows_out && ldd < D) || E == 0 || E > SF_MAX_EXPERTS || !sizes_ok(n, k) || capacity > 0x7FFFFFFFu) return SF_ERR_ARG;
     if (!d_rows_out && !d_weights_out) return SF_ERR_ARG;
     if (n && (!dy || !row_of_pair || (d_weights_out && capacity && !rows))) return SF_ERR_ARG;
     if (d_rows_out && (!offsets || !counts)) return SF_ERR_ARG;

@@ -391,6 +391,11 @@ def test_refusals(env):
     ids, f = z(5000, 2), z(5000, 2, t=torch.float32)
     x, x16 = z(5000, 4, t=torch.float32), z(5000, 4, t=torch.bfloat16)
     small = z(3)
+    with pytest.raises(sf.SfError):
+        sf.sf_expert_gate(None, x, 0, ids, f)                                                        # no context
+    wide = torch.zeros(1, dtype=torch.uint8, device="cuda").expand(1)
+    assert sf._lib().sf_expert_combine(ctx, wide.data_ptr(), 0, 1, (1 << 24) + 1, (1 << 24) + 1, ids.data_ptr(), None, None, 1, 1, wide.data_ptr(),
+                                       (1 << 24) + 1, None) == sf.SF_ERR_ARG                          # wider than SF_EXPERT_MAX_D
     for call in (lambda: sf.sf_expert_gate(ctx, z(5000, 1, t=torch.float32), 0, ids, f),            # k > E
                  lambda: sf.sf_expert_gate(ctx, x, 3, ids, f),
                  lambda: sf.sf_expert_gate(ctx, z(5000, 1025, t=torch.float32), 0, ids, f),
