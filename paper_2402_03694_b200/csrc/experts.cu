@@ -13,11 +13,13 @@ constexpr uint32_t kThreads = 256;
 constexpr uint32_t kWarps = kThreads / 32;
 
 // ---- gate ------------------------------------------------------------------------------------------------------
-// LPR lanes share a row, V scores each (consecutive, LPR * V >= E).  Bound: HBM; the scores are read once and stay in registers over
+// LPR lanes share a row, V scores each (LPR * V >= E): lane l has experts l V .. l V + V - 1 where rows may be read in whole vectors
+// (ALIGNED), else l, l + LPR, ... so that a row's lanes read side by side.  Bound: HBM; the scores are read once and stay in registers over
 // the k rounds of "largest that is left, lowest index first".  Up to 16 experts a thread has a whole row: with four lanes a
 // row the shuffles of the rounds made 1,000,000 x 16, k = 2 take 59 us.
 constexpr float kNegInf = -__builtin_huge_valf();
 
+template <int LPR, int V, bool ALIGNED> __device__ __forceinline__ uint32_t expert_of(uint32_t lane, int v) { return ALIGNED ? lane * V + v : v * LPR + lane; }
 template <typename T, int LPR, int V, bool ALIGNED>
 __device__ __forceinline__ void load_scores(const T* __restrict__ p, uint32_t E, uint32_t first, float (&s)[V]) {
     if (ALIGNED && first + V <= E) {
@@ -25,7 +27,7 @@ __device__ __forceinline__ void load_scores(const T* __restrict__ p, uint32_t E,
         else load_f32<T, V, (V * sizeof(T)) % 16 == 0>(p + first, s);
     } else {
 #pragma unroll
-        for (int v = 0; v < V; v++) s[v] = first + v < E ? to_f32(p[first + v]) : kNegInf;
+        for (int v = 0; v < V; v++) { const uint32_t e = expert_of<LPR, V, ALIGNED>(first / V, v); s[v] = e < E ? to_f32(p[e]) : kNegInf; }
     }
 #pragma unroll
     for (int v = 0; v < V; v++) s[v] = fmaxf(s[v], kNegInf);                      // a NaN is never picked and adds nothing
@@ -73,7 +75,7 @@ gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, ui
         for (uint32_t j = 0; j < k; j++) {
             float b = kNegInf; int id = 0x7FFFFFFF;
 #pragma unroll
-            for (int v = 0; v < V; v++) if (left[v] > b) { b = left[v]; id = (int)(lane * V) + v; }
+            for (int v = 0; v < V; v++) if (left[v] > b) { b = left[v]; id = (int)expert_of<LPR, V, ALIGNED>(lane, v); }
 #pragma unroll
             for (int o = LPR / 2; o >= 1; o >>= 1) {
                 const float ob = __shfl_xor_sync(0xFFFFFFFFu, b, o);
@@ -83,7 +85,7 @@ gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, ui
             if (b == kNegInf) id = -1;
             if (j == 0) { m = b; finite = fabsf(m) < -kNegInf; }
 #pragma unroll
-            for (int v = 0; v < V; v++) if (id == (int)(lane * V) + v) left[v] = kNegInf;
+            for (int v = 0; v < V; v++) if (id == (int)expert_of<LPR, V, ALIGNED>(lane, v)) left[v] = kNegInf;
 #pragma unroll
             for (int v = 0; v < S; v++) if (j == (uint32_t)v * LPR + lane) { best_s[v] = b; best_id[v] = id; }
             if (mode != SF_GATE_SOFTMAX && id >= 0) total += mode == SF_GATE_SHARE ? b : near_top(b, m, finite);
@@ -184,13 +186,13 @@ gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ 
             else store_f32<T, V, (V * sizeof(T)) % 16 == 0>(y + first, d);
         } else {
 #pragma unroll
-            for (int v = 0; v < V; v++) if (first + v < E) y[first + v] = from_f32<T>(d[v]);
+            for (int v = 0; v < V; v++) { const uint32_t e = expert_of<LPR, V, ALIGNED>(lane, v); if (e < E) y[e] = from_f32<T>(d[v]); }
         }
         for (uint32_t j0 = 0; j0 < k; j0 += 4) {
             if (k > 4) picks(j0);
 #pragma unroll
             for (int q = 0; q < 4; q++)
-                if (id[q] < E && id[q] - first < (uint32_t)V && sp[q] != kNegInf)
+                if (id[q] < E && (ALIGNED ? id[q] / V : id[q] % LPR) == lane && sp[q] != kNegInf)
                     y[id[q]] = from_f32<T>(mode == SF_GATE_SHARE ? (g[q] - dot) * inv : part(sp[q]) * inv * (g[q] - dot));
         }
     }
@@ -393,8 +395,9 @@ template <uint32_t WARPS> int launch_sort(const sf_ctx* ctx, const sort_args& a,
 // A group of lanes (a power of two, up to the whole block where flows are few) shares a flow.  Elements move in words of 16 bytes where
 // bases, pitches and widths allow, else of 4 bytes, else one by one.  Bound: HBM.
 
-// Every row is read once and written k times; U words a lane on their way.
-template <typename Q, int U>
+// Every row is read once and written k times; U words a lane on their way, of one flow, or (NARROW: a row has at most one word a lane) of
+// U flows (325,401 rows of 17 fp16 values, k = 2: 60 us with one).
+template <typename Q, int U, bool NARROW>
 __global__ void __launch_bounds__(kThreads)
 gather_kernel(const Q* __restrict__ x, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t units, size_t ldx, uint32_t k,
               const int32_t* __restrict__ row_of_pair, uint32_t E, const uint32_t* __restrict__ offsets, const uint32_t* __restrict__ counts,
@@ -413,6 +416,23 @@ gather_kernel(const Q* __restrict__ x, const uint32_t* __restrict__ n_dev, uint3
     }
     const uint32_t flows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
     const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1);
+    if constexpr (NARROW) {
+        const uint64_t hop = (uint64_t)flow_blocks * per;
+        if (lane >= units) return;
+        for (uint64_t f0 = (uint64_t)blockIdx.x * per + threadIdx.x / lanes; f0 < flows; f0 += hop * U) {
+            Q q[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) if (f0 + u * hop < flows) q[u] = __ldg(x + (f0 + u * hop) * ldx + lane);
+            for (uint32_t j = 0; j < k; j++) {
+                uint32_t r[U];
+#pragma unroll
+                for (int u = 0; u < U; u++) r[u] = f0 + u * hop < flows ? (uint32_t)__ldg(row_of_pair + (f0 + u * hop) * k + j) : 0xFFFFFFFFu;
+#pragma unroll
+                for (int u = 0; u < U; u++) if (r[u] < capacity) rows[(size_t)r[u] * ldr + lane] = q[u];
+            }
+        }
+        return;
+    }
     for (uint64_t f = (uint64_t)blockIdx.x * per + threadIdx.x / lanes; f < flows; f += (uint64_t)flow_blocks * per) {
         const Q* src = x + f * ldx;
         for (uint32_t c = lane; c < units; c += U * lanes) {
@@ -468,6 +488,45 @@ combine_kernel(const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t
 #pragma unroll
             for (int u = 0; u < U; u++) if (u == 0 || c + u * lanes * V < D) store_word<T, V>(y + f * ldy + c + u * lanes * V, acc[u]);
         }
+    }
+}
+
+// The same for rows of at most one word a lane: four flows at a time.
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads)
+combine_narrow_kernel(const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t ldr, const int32_t* __restrict__ row_of_pair,
+                      const float* __restrict__ weights, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t k, T* __restrict__ y, size_t ldy,
+                      uint32_t lanes, sf_dev_state* st)
+{
+    constexpr int F = 4;
+    sf_chain_enter();
+    const uint32_t flows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
+    const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1), c = lane * V;
+    const uint64_t hop = (uint64_t)gridDim.x * per;
+    if (c >= D) return;
+    for (uint64_t f0 = (uint64_t)blockIdx.x * per + threadIdx.x / lanes; f0 < flows; f0 += hop * F) {
+        float acc[F][V] = {};
+#pragma unroll 2
+        for (uint32_t j = 0; j < k; j++) {
+            uint32_t r[F];
+            float w[F], x[F][V];
+#pragma unroll
+            for (int u = 0; u < F; u++) {
+                const bool have = f0 + u * hop < flows;
+                r[u] = have ? (uint32_t)__ldg(row_of_pair + (f0 + u * hop) * k + j) : 0xFFFFFFFFu;
+                w[u] = have && weights ? __ldg(weights + (f0 + u * hop) * k + j) : 1.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < F; u++) if (r[u] < capacity) load_word<T, V>(rows + (size_t)r[u] * ldr + c, x[u]);
+#pragma unroll
+            for (int u = 0; u < F; u++)
+                if (r[u] < capacity) {
+#pragma unroll
+                    for (int v = 0; v < V; v++) acc[u][v] = fmaf(w[u], x[u][v], acc[u][v]);
+                }
+        }
+#pragma unroll
+        for (int u = 0; u < F; u++) if (f0 + u * hop < flows) store_word<T, V>(y + (f0 + u * hop) * ldy + c, acc[u]);
     }
 }
 
@@ -698,7 +757,8 @@ extern "C" int sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uin
         typedef decltype(q) Q;
         constexpr int U = sizeof(Q) == 16 ? 4 : 8;
         const uint32_t per = sizeof(Q) / size, units = D / per, lanes = lanes_for(ctx, units, n), fb = flow_grid(ctx, n, lanes), zb = fill_blocks(ctx, E, units);
-        SF_CUDA(sf_launch_chained(gather_kernel<Q, U>, fb + E * zb, kThreads, 0, (cudaStream_t)stream, (const Q*)x, n_dev, n, units, ldx / per, k, row_of_pair, E,
+        auto kern = units <= lanes ? gather_kernel<Q, 4, true> : gather_kernel<Q, U, false>;
+        SF_CUDA(sf_launch_chained(kern, fb + E * zb, kThreads, 0, (cudaStream_t)stream, (const Q*)x, n_dev, n, units, ldx / per, k, row_of_pair, E,
                                   offsets, counts, capacity, (Q*)rows_out, ldr / per, lanes, fb, zb, ctx->d_state));
         return SF_OK;
     };
@@ -720,7 +780,7 @@ static int combine(sf_ctx* ctx, const void* rows, int dtype, uint32_t capacity, 
         return by_word<T>(word, [&](auto v) {
             constexpr int V = decltype(v)::value, U = V * sizeof(T) == 16 ? 4 : 8;
             const uint32_t units = D / V, lanes = lanes_for(ctx, units, n), grid = flow_grid(ctx, n, lanes);
-            auto kern = units > 2 * lanes ? combine_kernel<T, V, U> : (units > lanes ? combine_kernel<T, V, 2> : combine_kernel<T, V, 1>);
+            auto kern = units > 2 * lanes ? combine_kernel<T, V, U> : (units > lanes ? combine_kernel<T, V, 2> : combine_narrow_kernel<T, V>);
             SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, (T*)y, ldy, lanes, ctx->d_state));
             return SF_OK;
         });

@@ -110,55 +110,62 @@ mx4_quantise_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, size_t 
     }
 }
 
-// The same for rows on any boundary: a warp takes 256 consecutive values with coalesced loads of single elements, 8 on their way in every lane
-// and piece, and turns them round in shared memory so that a lane has 8 consecutive ones (lanes that load their own 16 values
-// element by element ran at 0.6 TB/s at 141,031 x 1065 bf16).
-constexpr uint32_t kACols = 256;
+// The same for rows on any boundary and for narrow ones: pieces of 128 columns (a row's share of a scale tile), four of them per warp, loaded
+// element by element, coalesced, 16 loads a lane on their way, and turned round in shared memory so that a lane has 16 consecutive
+// values of a piece (lanes that load their own 16 values element by element ran at 0.6 TB/s at 141,031 x 1065 bf16).
 template <typename T>
 __global__ void __launch_bounds__(kQThreads)
 mx4_quantise_any_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, size_t ld, const int32_t* __restrict__ row_ids,
                         const uint32_t* __restrict__ n_rows_dev, uint32_t capacity, uint8_t* __restrict__ data,
                         uint8_t* __restrict__ scales, sf_dev_state* st)
 {
-    __shared__ float4 turn[kQThreads / 32][kACols / 4];
+    __shared__ float4 turn[kQThreads / 32][4 * 32];
     sf_chain_enter();
     const uint32_t rows = n_rows_dev ? sf_clamp_rows(*n_rows_dev, capacity, st) : capacity;
     const uint32_t pitch = row_bytes(K), blocks = pitch / 16, kt = k_tiles(K);
-    const uint32_t chunks = (kt * 128 + kACols - 1) / kACols;
     const uint32_t lane = threadIdx.x & 31;
     float* const mine = reinterpret_cast<float*>(turn[threadIdx.x >> 5]);
-    const uint64_t items = (uint64_t)rows * chunks;
-    const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32);
-    for (uint64_t i = (uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5); i < items; i += step) {
-        uint32_t row, k0;
-        row_and_piece(i, chunks, row, k0);
-        k0 *= kACols;
-        int64_t src = row;
-        if (row_ids) { const int32_t id = row_ids[row]; src = (id >= 0 && (uint32_t)id < n_src) ? id : -1; }
-        float v[8];
+    const uint64_t items = (uint64_t)rows * kt;
+    const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32) * 4;
+    for (uint64_t i0 = ((uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5)) * 4; i0 < items; i0 += step) {
+        uint32_t r, c;
+        row_and_piece(i0, kt, r, c);
+        const uint32_t r0 = r, c0 = c;
+        float v[4][4];
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const uint32_t k = k0 + j * 32 + lane;
-            v[j] = src >= 0 && k < K ? to_f32(x[(size_t)src * ld + k]) : 0.0f;
+        for (int u = 0; u < 4; u++) {
+            int64_t src = i0 + u < items ? (int64_t)r : -1;
+            if (row_ids && src >= 0) { const int32_t id = row_ids[r]; src = (id >= 0 && (uint32_t)id < n_src) ? id : -1; }
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const uint32_t k = c * 128 + j * 32 + lane;
+                v[u][j] = src >= 0 && k < K ? to_f32(x[(size_t)src * ld + k]) : 0.0f;
+            }
+            if (++c == kt) { c = 0; r++; }
         }
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 8; j++) mine[j * 32 + lane] = v[j];
+        for (int u = 0; u < 4; u++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) mine[u * 128 + j * 32 + lane] = v[u][j];
         __syncwarp();
-        const float4 a = reinterpret_cast<const float4*>(mine)[2 * lane], b = reinterpret_cast<const float4*>(mine)[2 * lane + 1];
-        const float y[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        float y[2][8];
         uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < 8; j++) top = max(top, __float_as_uint(y[j]) & 0x7FFFFFFFu);
-        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        const uint32_t byte = scale_byte(top), k = k0 + lane * 8;
-        const uint32_t codes = encode8(y, byte);
-        if (k < pitch * 2) *reinterpret_cast<uint32_t*>(data + (size_t)row * pitch + k / 2) = codes;
-        if ((lane & 3) == 0) {
-            const uint32_t q = k / 32;
-            if (q < kt * 4) scales[scale_at(row, q, kt)] = q < blocks ? (uint8_t)byte : (uint8_t)127;
+        for (int h = 0; h < 2; h++) {
+            const float4 a = reinterpret_cast<const float4*>(mine)[4 * lane + 2 * h], b = reinterpret_cast<const float4*>(mine)[4 * lane + 2 * h + 1];
+            y[h][0] = a.x; y[h][1] = a.y; y[h][2] = a.z; y[h][3] = a.w;
+            y[h][4] = b.x; y[h][5] = b.y; y[h][6] = b.z; y[h][7] = b.w;
+#pragma unroll
+            for (int j = 0; j < 8; j++) top = max(top, __float_as_uint(y[h][j]) & 0x7FFFFFFFu);
         }
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        const uint32_t byte = scale_byte(top), u = lane / 8;
+        const uint2 codes = make_uint2(encode8(y[0], byte), encode8(y[1], byte));
+        if (i0 + u >= items) continue;
+        const uint32_t piece = c0 + u, row = r0 + piece / kt, k = (piece % kt) * 128 + (lane & 7) * 16;
+        if (k < pitch * 2) *reinterpret_cast<uint2*>(data + (size_t)row * pitch + k / 2) = codes;
+        if ((lane & 1) == 0) scales[scale_at(row, k / 32, kt)] = k / 32 < blocks ? (uint8_t)byte : (uint8_t)127;
     }
 }
 
@@ -211,36 +218,46 @@ mx4_unpack_kernel(const uint8_t* __restrict__ data, const uint8_t* __restrict__ 
     }
 }
 
-// The same for rows on any boundary: turned round in shared memory, stored element by element, coalesced.
+// The same for rows on any boundary and for narrow ones: turned round in shared memory, stored element by element, coalesced.
 template <typename T>
 __global__ void __launch_bounds__(kQThreads)
 mx4_unpack_any_kernel(const uint8_t* __restrict__ data, const uint8_t* __restrict__ scales, const uint32_t* __restrict__ n_rows_dev,
                       uint32_t capacity, uint32_t K, T* __restrict__ out, size_t ld, sf_dev_state* st)
 {
-    __shared__ float4 turn[kQThreads / 32][kACols / 4];
+    __shared__ float4 turn[kQThreads / 32][4 * 32];
     sf_chain_enter();
     const uint32_t rows = n_rows_dev ? sf_clamp_rows(*n_rows_dev, capacity, st) : capacity;
     const uint32_t pitch = row_bytes(K), kt = k_tiles(K);
-    const uint32_t chunks = (K + kACols - 1) / kACols;
     const uint32_t lane = threadIdx.x & 31;
     float* const mine = reinterpret_cast<float*>(turn[threadIdx.x >> 5]);
-    const uint64_t items = (uint64_t)rows * chunks;
-    const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32);
-    for (uint64_t i = (uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5); i < items; i += step) {
-        uint32_t row, k0;
-        row_and_piece(i, chunks, row, k0);
-        k0 *= kACols;
-        const uint32_t k = k0 + lane * 8;
-        float v[8] = {};
-        if (k < K) decode8(__ldg(reinterpret_cast<const uint32_t*>(data + (size_t)row * pitch + k / 2)), scale_f32(__ldg(scales + scale_at(row, k / 32, kt))), v);
+    const uint64_t items = (uint64_t)rows * kt;
+    const uint64_t step = (uint64_t)gridDim.x * (kQThreads / 32) * 4;
+    for (uint64_t i0 = ((uint64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5)) * 4; i0 < items; i0 += step) {
+        uint32_t r, c;
+        row_and_piece(i0, kt, r, c);
+        const uint32_t q = lane / 8, piece = c + q, row = r + piece / kt, k = (piece % kt) * 128 + (lane & 7) * 16;
+        float a[8] = {}, b[8] = {};
+        if (i0 + q < items && k < K) {
+            const uint2 codes = __ldg(reinterpret_cast<const uint2*>(data + (size_t)row * pitch + k / 2));
+            const float scale = scale_f32(__ldg(scales + scale_at(row, k / 32, kt)));
+            decode8(codes.x, scale, a);
+            decode8(codes.y, scale, b);
+        }
         __syncwarp();
-        reinterpret_cast<float4*>(mine)[2 * lane] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(mine)[2 * lane + 1] = make_float4(v[4], v[5], v[6], v[7]);
+        float4* const m4 = reinterpret_cast<float4*>(mine) + 4 * lane;
+        m4[0] = make_float4(a[0], a[1], a[2], a[3]);
+        m4[1] = make_float4(a[4], a[5], a[6], a[7]);
+        m4[2] = make_float4(b[0], b[1], b[2], b[3]);
+        m4[3] = make_float4(b[4], b[5], b[6], b[7]);
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const uint32_t c = k0 + j * 32 + lane;
-            if (c < K) out[(size_t)row * ld + c] = from_f32<T>(mine[j * 32 + lane]);
+        for (int u = 0; u < 4; u++) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const uint32_t col = c * 128 + j * 32 + lane;
+                if (i0 + u < items && col < K) out[(size_t)r * ld + col] = from_f32<T>(mine[u * 128 + j * 32 + lane]);
+            }
+            if (++c == kt) { c = 0; r++; }
         }
     }
 }
@@ -276,9 +293,9 @@ extern "C" int sf_mx4_quantise(sf_ctx* ctx, const void* x, int dtype, uint32_t n
 int sf_launch_mx4_quantise(sf_ctx* ctx, const void* x, int dtype, uint32_t n_src, uint32_t K, size_t ld, const int32_t* row_ids,
                            const uint32_t* n_rows_dev, uint32_t capacity, uint8_t* data, uint8_t* scales, cudaStream_t st)
 {
-    const bool al = aligned(x, 16) && (ld * type_bytes(dtype)) % 16 == 0;
-    const uint32_t cols = al ? kPCols : kACols;
-    const uint64_t items = (uint64_t)capacity * ((k_tiles(K) * 128 + cols - 1) / cols);
+    // (rows up to 128 columns wide leave three quarters of the other kernel's lanes idle)
+    const bool al = aligned(x, 16) && (ld * type_bytes(dtype)) % 16 == 0 && K > 128;
+    const uint64_t items = al ? (uint64_t)capacity * ((k_tiles(K) * 128 + kPCols - 1) / kPCols) : ((uint64_t)capacity * k_tiles(K) + 3) / 4;
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
         constexpr int U = 8 / sizeof(T);               // 8 16-byte words a lane on their way, where there are pieces enough for all warps
@@ -297,8 +314,8 @@ extern "C" int sf_mx4_unpack(sf_ctx* ctx, const uint8_t* data, const uint8_t* sc
     if (!data || !scales || !out) return SF_ERR_ARG;
     if (!aligned(out, type_bytes(dtype)) || !aligned(data, 16) || !aligned(scales, 16) || !aligned(n_rows_dev, 4)) return SF_ERR_ARG;
     SF_ON_DEVICE(ctx);
-    const bool al = aligned(out, 32) && (ld * type_bytes(dtype)) % 32 == 0;
-    const uint32_t grid = al ? row_grid(ctx, ((uint64_t)capacity * ((K + kPCols - 1) / kPCols) + 1) / 2, 8) : row_grid(ctx, (uint64_t)capacity * ((K + kACols - 1) / kACols), 32);
+    const bool al = aligned(out, 32) && (ld * type_bytes(dtype)) % 32 == 0 && K > 128;
+    const uint32_t grid = al ? row_grid(ctx, ((uint64_t)capacity * ((K + kPCols - 1) / kPCols) + 1) / 2, 8) : row_grid(ctx, ((uint64_t)capacity * k_tiles(K) + 3) / 4, 32);
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
         auto k = al ? mx4_unpack_kernel<T> : mx4_unpack_any_kernel<T>;

@@ -475,6 +475,22 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                             continue;
                         }
                         __syncwarp();
+                        if (!vec) {                                          // rows on any boundary: consecutive columns, element by element
+                            constexpr uint32_t kLane = kAt * 4 / sizeof(T) / 32;             // columns of a row per lane
+                            T* const o = reinterpret_cast<T*>(p.out) + (size_t)row0 * p.ld + col;
+                            const uint32_t rows_in = end > row0 ? min(32u, end - row0) : 0u;
+#pragma unroll 8
+                            for (uint32_t r = 0; r < rows_in; r++) {
+#pragma unroll
+                                for (uint32_t h = 0; h < kLane; h++) {
+                                    const uint32_t x = h * 32 + lane;        // its 16-byte piece is swizzled by row
+                                    const T val = *reinterpret_cast<const T*>(stg + r * 128u + (((x / kPer) ^ (r & 7u)) << 4) + (x % kPer) * sizeof(T));
+                                    if (col + x < p.N) o[(size_t)r * p.ld + x] = val;
+                                }
+                            }
+                            __syncwarp();
+                            continue;
+                        }
                         constexpr uint32_t kRowsAt = 32 / kPieces;           // rows per store instruction
                         const uint32_t q = lane % kPieces, r = lane / kPieces, at = col + q * kPer;
                         T* const o = reinterpret_cast<T*>(p.out) + (size_t)(row0 + r) * p.ld + at;
