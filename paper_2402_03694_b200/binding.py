@@ -416,18 +416,18 @@ def _rows(t, where):
     return t.data_ptr(), code, n, d, ld
 
 
-def _flat(t, count, size, where):
-    """Address of a contiguous device tensor of at least `count` elements of `size` bytes; None stays None."""
+def _flat(t, count, size, where, real=False):
+    """Address of a contiguous device tensor of at least `count` whole (real: floating) numbers of `size` bytes; None stays None."""
     if t is None:
         return None
-    if not t.is_cuda or t.itemsize != size or t.nbytes < count * size or not t.is_contiguous():
+    if not t.is_cuda or t.itemsize != size or t.nbytes < count * size or t.is_floating_point() != real or not t.is_contiguous():
         raise SfError(SF_ERR_ARG, where)
     return t.data_ptr()
 
 
-def _whole(t, shape, where):
-    """Address of a contiguous 4-byte device tensor of this shape."""
-    if not t.is_cuda or t.itemsize != 4 or t.shape != shape or not t.is_contiguous():
+def _whole(t, shape, where, real=False):
+    """Address of a contiguous device tensor of this shape of 4-byte whole (real: floating) numbers."""
+    if not t.is_cuda or t.itemsize != 4 or t.shape != shape or t.is_floating_point() != real or not t.is_contiguous():
         raise SfError(SF_ERR_ARG, where)
     return t.data_ptr()
 
@@ -479,7 +479,7 @@ def sf_mx4_matmul(ctx, a, a_scales, w, w_scales, K, out, bias=None, relu=False, 
     p, dt, n, N, ld, os_ = _product_out(out, out_scales, N, s)
     pitch, ab = _mx4_bytes(n, K)
     _check(_lib().sf_mx4_matmul(ctx, _flat(a, n * pitch, 1, s), _flat(a_scales, ab, 1, s), _flat(n_rows_dev, 1, 4, s), n,
-                                _flat(w, N * pitch, 1, s), _flat(w_scales, _mx4_bytes(N, K)[1], 1, s), N, K, _flat(bias, N, 4, s),
+                                _flat(w, N * pitch, 1, s), _flat(w_scales, _mx4_bytes(N, K)[1], 1, s), N, K, _flat(bias, N, 4, s, True),
                                 int(relu), dt, p, ld, os_, _stream_on(ctx, out, stream, s)), s)
 
 
@@ -492,7 +492,7 @@ def sf_mx4_matmul_experts(ctx, a, a_scales, w, w_scales, K, offsets, out, bias=N
     pitch, ab = _mx4_bytes(n, K)
     _check(_lib().sf_mx4_matmul_experts(ctx, _flat(a, n * pitch, 1, s), _flat(a_scales, ab, 1, s), _flat(offsets, E + 1, 4, s), E, n,
                                         _flat(w, E * N * pitch, 1, s), _flat(w_scales, E * _mx4_bytes(N, K)[1], 1, s), N, K,
-                                        _flat(bias, E * N, 4, s), int(relu), dt, p, ld, os_, _stream_on(ctx, out, stream, s)), s)
+                                        _flat(bias, E * N, 4, s, True), int(relu), dt, p, ld, os_, _stream_on(ctx, out, stream, s)), s)
 
 
 def sf_expert_gate(ctx, scores, mode, ids_out, weights_out, n_dev=None, stream=None):
@@ -502,7 +502,7 @@ def sf_expert_gate(ctx, scores, mode, ids_out, weights_out, n_dev=None, stream=N
     _arg(ids_out.dim() == 2, w)
     k = ids_out.shape[1]
     _check(_lib().sf_expert_gate(ctx, p, dt, _flat(n_dev, 1, 4, w), n, E, ld, k, mode, _whole(ids_out, (n, k), w),
-                                 _whole(weights_out, (n, k), w), _stream_on(ctx, scores, stream, w)), w)
+                                 _whole(weights_out, (n, k), w, True), _stream_on(ctx, scores, stream, w)), w)
 
 
 def sf_expert_gate_backward(ctx, scores, mode, ids, d_weights, d_scores_out, n_dev=None, stream=None):
@@ -512,7 +512,7 @@ def sf_expert_gate_backward(ctx, scores, mode, ids, d_weights, d_scores_out, n_d
     _arg(dq == dt and m == n and F == E and ids.dim() == 2, w)
     k = ids.shape[1]
     _check(_lib().sf_expert_gate_backward(ctx, p, dt, _flat(n_dev, 1, 4, w), n, E, ld, k, mode, _whole(ids, (n, k), w),
-                                          _whole(d_weights, (n, k), w), q, ldd, _stream_on(ctx, scores, stream, w)), w)
+                                          _whole(d_weights, (n, k), w, True), q, ldd, _stream_on(ctx, scores, stream, w)), w)
 
 
 def sf_expert_sort_workspace(n, k, E):
@@ -565,7 +565,7 @@ def sf_expert_combine(ctx, rows, row_of_pair, weights, y_out, n_dev=None, stream
     """weights float32 [n][k] or None (all 1)."""
     w = "sf_expert_combine"
     p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, y_out, w)
-    g = None if weights is None else _whole(weights, (n, k), w)
+    g = None if weights is None else _whole(weights, (n, k), w, True)
     _check(_lib().sf_expert_combine(ctx, p, dt, cap, D, ldr, at, g, _flat(n_dev, 1, 4, w), n, k, q, ldy, _stream_on(ctx, y_out, stream, w)), w)
 
 
@@ -573,13 +573,13 @@ def sf_expert_combine_backward(ctx, dy, rows, row_of_pair, weights, offsets, cou
     """Either output may be None."""
     w = "sf_expert_combine_backward"
     p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, dy, w)
-    g = None if weights is None else _whole(weights, (n, k), w)
+    g = None if weights is None else _whole(weights, (n, k), w, True)
     E = counts.numel()
     r, ldd = None, 0
     if d_rows_out is not None:
         r, dr, c2, D2, ldd = _rows(d_rows_out, w)
         _arg((dr, c2, D2) == (dt, cap, D), w)
-    dw = None if d_weights_out is None else _whole(d_weights_out, (n, k), w)
+    dw = None if d_weights_out is None else _whole(d_weights_out, (n, k), w, True)
     _check(_lib().sf_expert_combine_backward(ctx, q, dt, ldy, p, cap, D, ldr, at, g, _flat(n_dev, 1, 4, w), n, k, E,
                                              _flat(offsets, E + 1, 4, w), _flat(counts, E, 4, w), r, ldd, dw, _stream_on(ctx, dy, stream, w)), w)
 

@@ -395,9 +395,9 @@ template <uint32_t WARPS> int launch_sort(const sf_ctx* ctx, const sort_args& a,
 // A group of lanes (a power of two, up to the whole block where flows are few) shares a flow.  Elements move in words of 16 bytes where
 // bases, pitches and widths allow, else of 4 bytes, else one by one.  Bound: HBM.
 
-// Every row is read once and written k times; U words a lane on their way, of one flow, or (NARROW: a row has at most one word a lane) of
-// U flows (325,401 rows of 17 fp16 values, k = 2: 60 us with one).
-template <typename Q, int U, bool NARROW>
+// Every row is read once and written k times; U words a lane of F flows on their way (F > 1: a row has at most U words a lane; 325,401 rows of 17
+// fp16 values, k = 2: dispatch and gradient 164 us with one flow, 79 with four).
+template <typename Q, int U, int F>
 __global__ void __launch_bounds__(kThreads)
 gather_kernel(const Q* __restrict__ x, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t units, size_t ldx, uint32_t k,
               const int32_t* __restrict__ row_of_pair, uint32_t E, const uint32_t* __restrict__ offsets, const uint32_t* __restrict__ counts,
@@ -416,19 +416,24 @@ gather_kernel(const Q* __restrict__ x, const uint32_t* __restrict__ n_dev, uint3
     }
     const uint32_t flows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
     const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1);
-    if constexpr (NARROW) {
+    if constexpr (F > 1) {
         const uint64_t hop = (uint64_t)flow_blocks * per;
-        if (lane >= units) return;
-        for (uint64_t f0 = (uint64_t)blockIdx.x * per + threadIdx.x / lanes; f0 < flows; f0 += hop * U) {
-            Q q[U];
+        for (uint64_t f0 = (uint64_t)blockIdx.x * per + threadIdx.x / lanes; f0 < flows; f0 += hop * F) {
+            Q q[F][U];
 #pragma unroll
-            for (int u = 0; u < U; u++) if (f0 + u * hop < flows) q[u] = __ldg(x + (f0 + u * hop) * ldx + lane);
+            for (int i = 0; i < F; i++)
+#pragma unroll
+                for (int u = 0; u < U; u++) if (f0 + i * hop < flows && lane + u * lanes < units) q[i][u] = __ldg(x + (f0 + i * hop) * ldx + lane + u * lanes);
             for (uint32_t j = 0; j < k; j++) {
-                uint32_t r[U];
+                uint32_t r[F];
 #pragma unroll
-                for (int u = 0; u < U; u++) r[u] = f0 + u * hop < flows ? (uint32_t)__ldg(row_of_pair + (f0 + u * hop) * k + j) : 0xFFFFFFFFu;
+                for (int i = 0; i < F; i++) r[i] = f0 + i * hop < flows ? (uint32_t)__ldg(row_of_pair + (f0 + i * hop) * k + j) : 0xFFFFFFFFu;
 #pragma unroll
-                for (int u = 0; u < U; u++) if (r[u] < capacity) rows[(size_t)r[u] * ldr + lane] = q[u];
+                for (int i = 0; i < F; i++)
+                    if (r[i] < capacity) {
+#pragma unroll
+                        for (int u = 0; u < U; u++) if (lane + u * lanes < units) rows[(size_t)r[i] * ldr + lane + u * lanes] = q[i][u];
+                    }
             }
         }
         return;
@@ -491,8 +496,8 @@ combine_kernel(const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t
     }
 }
 
-// The same for rows of at most one word a lane: four flows at a time.
-template <typename T, int V>
+// The same for rows of at most U words a lane: four flows at a time.
+template <typename T, int V, int U>
 __global__ void __launch_bounds__(kThreads)
 combine_narrow_kernel(const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t ldr, const int32_t* __restrict__ row_of_pair,
                       const float* __restrict__ weights, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t k, T* __restrict__ y, size_t ldy,
@@ -501,32 +506,37 @@ combine_narrow_kernel(const T* __restrict__ rows, uint32_t capacity, uint32_t D,
     constexpr int F = 4;
     sf_chain_enter();
     const uint32_t flows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
-    const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1), c = lane * V;
+    const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1);
     const uint64_t hop = (uint64_t)gridDim.x * per;
-    if (c >= D) return;
     for (uint64_t f0 = (uint64_t)blockIdx.x * per + threadIdx.x / lanes; f0 < flows; f0 += hop * F) {
-        float acc[F][V] = {};
-#pragma unroll 2
+        float acc[F][U][V] = {};
+#pragma unroll (U == 1 ? 2 : 1)
         for (uint32_t j = 0; j < k; j++) {
             uint32_t r[F];
-            float w[F], x[F][V];
+            float w[F], x[F][U][V];
 #pragma unroll
-            for (int u = 0; u < F; u++) {
-                const bool have = f0 + u * hop < flows;
-                r[u] = have ? (uint32_t)__ldg(row_of_pair + (f0 + u * hop) * k + j) : 0xFFFFFFFFu;
-                w[u] = have && weights ? __ldg(weights + (f0 + u * hop) * k + j) : 1.0f;
+            for (int i = 0; i < F; i++) {
+                const bool have = f0 + i * hop < flows;
+                r[i] = have ? (uint32_t)__ldg(row_of_pair + (f0 + i * hop) * k + j) : 0xFFFFFFFFu;
+                w[i] = have && weights ? __ldg(weights + (f0 + i * hop) * k + j) : 1.0f;
             }
 #pragma unroll
-            for (int u = 0; u < F; u++) if (r[u] < capacity) load_word<T, V>(rows + (size_t)r[u] * ldr + c, x[u]);
+            for (int i = 0; i < F; i++)
 #pragma unroll
-            for (int u = 0; u < F; u++)
-                if (r[u] < capacity) {
+                for (int u = 0; u < U; u++) if (r[i] < capacity && (lane + u * lanes) * V < D) load_word<T, V>(rows + (size_t)r[i] * ldr + (lane + u * lanes) * V, x[i][u]);
 #pragma unroll
-                    for (int v = 0; v < V; v++) acc[u][v] = fmaf(w[u], x[u][v], acc[u][v]);
-                }
+            for (int i = 0; i < F; i++)
+#pragma unroll
+                for (int u = 0; u < U; u++)
+                    if (r[i] < capacity && (lane + u * lanes) * V < D) {
+#pragma unroll
+                        for (int v = 0; v < V; v++) acc[i][u][v] = fmaf(w[i], x[i][u][v], acc[i][u][v]);
+                    }
         }
 #pragma unroll
-        for (int u = 0; u < F; u++) if (f0 + u * hop < flows) store_word<T, V>(y + (f0 + u * hop) * ldy + c, acc[u]);
+        for (int i = 0; i < F; i++)
+#pragma unroll
+            for (int u = 0; u < U; u++) if (f0 + i * hop < flows && (lane + u * lanes) * V < D) store_word<T, V>(y + (f0 + i * hop) * ldy + (lane + u * lanes) * V, acc[i][u]);
     }
 }
 
@@ -757,7 +767,7 @@ extern "C" int sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uin
         typedef decltype(q) Q;
         constexpr int U = sizeof(Q) == 16 ? 4 : 8;
         const uint32_t per = sizeof(Q) / size, units = D / per, lanes = lanes_for(ctx, units, n), fb = flow_grid(ctx, n, lanes), zb = fill_blocks(ctx, E, units);
-        auto kern = units <= lanes ? gather_kernel<Q, 4, true> : gather_kernel<Q, U, false>;
+        auto kern = units <= lanes ? gather_kernel<Q, 1, 4> : (units <= 2 * lanes ? gather_kernel<Q, 2, 4> : (units <= 4 * lanes && sizeof(Q) < 16 ? gather_kernel<Q, 4, 2> : gather_kernel<Q, U, 1>));
         SF_CUDA(sf_launch_chained(kern, fb + E * zb, kThreads, 0, (cudaStream_t)stream, (const Q*)x, n_dev, n, units, ldx / per, k, row_of_pair, E,
                                   offsets, counts, capacity, (Q*)rows_out, ldr / per, lanes, fb, zb, ctx->d_state));
         return SF_OK;
@@ -780,7 +790,7 @@ static int combine(sf_ctx* ctx, const void* rows, int dtype, uint32_t capacity, 
         return by_word<T>(word, [&](auto v) {
             constexpr int V = decltype(v)::value, U = V * sizeof(T) == 16 ? 4 : 8;
             const uint32_t units = D / V, lanes = lanes_for(ctx, units, n), grid = flow_grid(ctx, n, lanes);
-            auto kern = units > 2 * lanes ? combine_kernel<T, V, U> : (units > lanes ? combine_kernel<T, V, 2> : combine_narrow_kernel<T, V>);
+            auto kern = units > 2 * lanes ? combine_kernel<T, V, U> : (units > lanes ? combine_narrow_kernel<T, V, 2> : combine_narrow_kernel<T, V, 1>);
             SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, (T*)y, ldy, lanes, ctx->d_state));
             return SF_OK;
         });

@@ -110,10 +110,14 @@ mx4_quantise_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, size_t 
     }
 }
 
+// Place of element e in the buffer that turns 512 elements round: written and read without bank conflicts, by lanes that have consecutive
+// elements (or pairs) and by lanes that have 16 consecutive ones as four 16-byte pieces.
+__device__ __forceinline__ uint32_t turned(uint32_t e) { return (e & ~15u) | ((((e >> 2) ^ (e >> 5)) & 3u) << 2) | (e & 3u); }
+
 // The same for rows on any boundary and for narrow ones: pieces of 128 columns (a row's share of a scale tile), four of them per warp, loaded
-// element by element, coalesced, 16 loads a lane on their way, and turned round in shared memory so that a lane has 16 consecutive
+// W elements at a time (two 16-bit ones where rows are on 4-byte boundaries), coalesced, up to 16 loads a lane on their way, and turned round in shared memory so that a lane has 16 consecutive
 // values of a piece (lanes that load their own 16 values element by element ran at 0.6 TB/s at 141,031 x 1065 bf16).
-template <typename T>
+template <typename T, int W>
 __global__ void __launch_bounds__(kQThreads)
 mx4_quantise_any_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, size_t ld, const int32_t* __restrict__ row_ids,
                         const uint32_t* __restrict__ n_rows_dev, uint32_t capacity, uint8_t* __restrict__ data,
@@ -131,15 +135,21 @@ mx4_quantise_any_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, siz
         uint32_t r, c;
         row_and_piece(i0, kt, r, c);
         const uint32_t r0 = r, c0 = c;
-        float v[4][4];
+        float v[4][4 / W][W];
 #pragma unroll
         for (int u = 0; u < 4; u++) {
             int64_t src = i0 + u < items ? (int64_t)r : -1;
             if (row_ids && src >= 0) { const int32_t id = row_ids[r]; src = (id >= 0 && (uint32_t)id < n_src) ? id : -1; }
+            const T* const p = x + (size_t)max(src, (int64_t)0) * ld + c * 128;
+            const uint32_t left = src >= 0 ? K - c * 128 : 0u;               // values of the row from this piece on
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const uint32_t k = c * 128 + j * 32 + lane;
-                v[u][j] = src >= 0 && k < K ? to_f32(x[(size_t)src * ld + k]) : 0.0f;
+            for (int j = 0; j < 4 / W; j++) {
+                const uint32_t k = (j * 32 + lane) * W;
+                if (k < left) load_word<T, W>(p + k, v[u][j]);               // (W = 2: K is even)
+                else {
+#pragma unroll
+                    for (int w = 0; w < W; w++) v[u][j][w] = 0.0f;
+                }
             }
             if (++c == kt) { c = 0; r++; }
         }
@@ -147,13 +157,16 @@ mx4_quantise_any_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, siz
 #pragma unroll
         for (int u = 0; u < 4; u++)
 #pragma unroll
-            for (int j = 0; j < 4; j++) mine[u * 128 + j * 32 + lane] = v[u][j];
+            for (int j = 0; j < 4 / W; j++) {
+                float* const q = mine + turned(u * 128 + (j * 32 + lane) * W);
+                if constexpr (W == 2) *reinterpret_cast<float2*>(q) = make_float2(v[u][j][0], v[u][j][1]); else *q = v[u][j][0];
+            }
         __syncwarp();
         float y[2][8];
         uint32_t top = 0;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const float4 a = reinterpret_cast<const float4*>(mine)[4 * lane + 2 * h], b = reinterpret_cast<const float4*>(mine)[4 * lane + 2 * h + 1];
+            const float4 a = *reinterpret_cast<const float4*>(mine + turned(16 * lane + 8 * h)), b = *reinterpret_cast<const float4*>(mine + turned(16 * lane + 8 * h + 4));
             y[h][0] = a.x; y[h][1] = a.y; y[h][2] = a.z; y[h][3] = a.w;
             y[h][4] = b.x; y[h][5] = b.y; y[h][6] = b.z; y[h][7] = b.w;
 #pragma unroll
@@ -219,7 +232,7 @@ mx4_unpack_kernel(const uint8_t* __restrict__ data, const uint8_t* __restrict__ 
 }
 
 // The same for rows on any boundary and for narrow ones: turned round in shared memory, stored element by element, coalesced.
-template <typename T>
+template <typename T, int W>
 __global__ void __launch_bounds__(kQThreads)
 mx4_unpack_any_kernel(const uint8_t* __restrict__ data, const uint8_t* __restrict__ scales, const uint32_t* __restrict__ n_rows_dev,
                       uint32_t capacity, uint32_t K, T* __restrict__ out, size_t ld, sf_dev_state* st)
@@ -244,24 +257,33 @@ mx4_unpack_any_kernel(const uint8_t* __restrict__ data, const uint8_t* __restric
             decode8(codes.y, scale, b);
         }
         __syncwarp();
-        float4* const m4 = reinterpret_cast<float4*>(mine) + 4 * lane;
-        m4[0] = make_float4(a[0], a[1], a[2], a[3]);
-        m4[1] = make_float4(a[4], a[5], a[6], a[7]);
-        m4[2] = make_float4(b[0], b[1], b[2], b[3]);
-        m4[3] = make_float4(b[4], b[5], b[6], b[7]);
+        *reinterpret_cast<float4*>(mine + turned(16 * lane)) = make_float4(a[0], a[1], a[2], a[3]);
+        *reinterpret_cast<float4*>(mine + turned(16 * lane + 4)) = make_float4(a[4], a[5], a[6], a[7]);
+        *reinterpret_cast<float4*>(mine + turned(16 * lane + 8)) = make_float4(b[0], b[1], b[2], b[3]);
+        *reinterpret_cast<float4*>(mine + turned(16 * lane + 12)) = make_float4(b[4], b[5], b[6], b[7]);
         __syncwarp();
 #pragma unroll
         for (int u = 0; u < 4; u++) {
+            T* const p = out + (size_t)r * ld + c * 128;
+            const uint32_t left = i0 + u < items ? K - c * 128 : 0u;
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const uint32_t col = c * 128 + j * 32 + lane;
-                if (i0 + u < items && col < K) out[(size_t)r * ld + col] = from_f32<T>(mine[u * 128 + j * 32 + lane]);
+            for (int j = 0; j < 4 / W; j++) {
+                const uint32_t k = (j * 32 + lane) * W;
+                if (k < left) {
+                    const float* const q = mine + turned(u * 128 + k);
+                    float y[W];
+#pragma unroll
+                    for (int w = 0; w < W; w++) y[w] = q[w];
+                    store_word<T, W>(p + k, y);
+                }
             }
             if (++c == kt) { c = 0; r++; }
         }
     }
 }
 
+// may 16-bit elements be moved in pairs?
+bool pairs_ok(const void* p, size_t ld, uint32_t K, size_t size) { return size == 2 && aligned(p, 4) && ld % 2 == 0 && K % 2 == 0; }
 // A grid that fills the machine but gives no warp an empty turn.
 uint32_t row_grid(const sf_ctx* ctx, uint64_t items, uint32_t blocks_per_sm) {
     const uint64_t want = (items + kQThreads / 32 - 1) / (kQThreads / 32);
@@ -300,7 +322,7 @@ int sf_launch_mx4_quantise(sf_ctx* ctx, const void* x, int dtype, uint32_t n_src
         typedef decltype(zero) T;
         constexpr int U = 8 / sizeof(T);               // 8 16-byte words a lane on their way, where there are pieces enough for all warps
         const bool many = al && items >= (uint64_t)ctx->num_sms * 64 * U;
-        auto k = al ? (many ? mx4_quantise_kernel<T, U> : mx4_quantise_kernel<T, 1>) : mx4_quantise_any_kernel<T>;
+        auto k = al ? (many ? mx4_quantise_kernel<T, U> : mx4_quantise_kernel<T, 1>) : (pairs_ok(x, ld, K, sizeof(T)) ? mx4_quantise_any_kernel<T, sizeof(T) == 2 ? 2 : 1> : mx4_quantise_any_kernel<T, 1>);
         SF_CUDA(sf_launch_chained(k, row_grid(ctx, many ? (items + U - 1) / U : items, 32), kQThreads, 0, st, (const T*)x, n_src, K, ld, row_ids, n_rows_dev, capacity, data, scales, ctx->d_state));
         return SF_OK;
     });
@@ -318,7 +340,7 @@ extern "C" int sf_mx4_unpack(sf_ctx* ctx, const uint8_t* data, const uint8_t* sc
     const uint32_t grid = al ? row_grid(ctx, ((uint64_t)capacity * ((K + kPCols - 1) / kPCols) + 1) / 2, 8) : row_grid(ctx, ((uint64_t)capacity * k_tiles(K) + 3) / 4, 32);
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        auto k = al ? mx4_unpack_kernel<T> : mx4_unpack_any_kernel<T>;
+        auto k = al ? mx4_unpack_kernel<T> : (pairs_ok(out, ld, K, sizeof(T)) ? mx4_unpack_any_kernel<T, sizeof(T) == 2 ? 2 : 1> : mx4_unpack_any_kernel<T, 1>);
         SF_CUDA(sf_launch_chained(k, grid, kQThreads, 0, (cudaStream_t)stream, data, scales, n_rows_dev, capacity, K, (T*)out, ld, ctx->d_state));
         return SF_OK;
     });

@@ -253,7 +253,7 @@ def laid(x, kind, ld, at, fill=7.0):
     return base, base[:, at:at + D]
 
 
-SHAPES = [(1, 1, 1, 1, 1), (10, 1, 8, 2048, 128), (13, 2, 8, 8, 16), (300, 2, 5, 100, 128), (257, 3, 4, 33, 1), (1500, 2, 16, 1024, 64), (5, 6, 9, 5000, 8), (3000, 1, 2, 3, 1)]
+SHAPES = [(1, 1, 1, 1, 1), (10, 1, 8, 2048, 128), (13, 2, 8, 8, 16), (300, 2, 5, 100, 128), (257, 3, 4, 33, 1), (1500, 2, 16, 1024, 64), (5, 6, 9, 5000, 8), (3000, 1, 2, 3, 1), (40000, 2, 3, 17, 16), (9000, 3, 5, 50, 1), (7000, 1, 4, 114, 8)]
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
@@ -414,6 +414,8 @@ def test_refusals(env):
                  lambda: sf.sf_expert_gather(ctx, x, ids[:10], z(5), z(4), x),
                  lambda: sf.sf_expert_gather(ctx, x.t(), ids, z(5), z(4), x),
                  lambda: sf.sf_expert_combine(ctx, x, ids, f[:1], x.clone()),
+                 lambda: sf.sf_expert_combine(ctx, x, f, None, x.clone()),                                 # whole numbers are wanted
+                 lambda: sf.sf_expert_combine(ctx, x, ids, ids, x.clone()),                                # real ones are wanted
                  lambda: sf.sf_expert_combine_backward(ctx, x, x, ids, f, z(5), z(4), None, None),
                  lambda: sf.sf_expert_combine_backward(ctx, x, x, ids, f, z(4), z(4), x.clone(), None)):
         with pytest.raises(sf.SfError) as e:

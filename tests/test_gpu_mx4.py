@@ -74,7 +74,7 @@ def check_packed(data, scales, x64, rows=None):
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
-@pytest.mark.parametrize("n,K", [(1, 1), (1, 32), (3, 33), (129, 100), (130, 416), (257, 2048), (5, 4097), (300, 7), (2, 260)])
+@pytest.mark.parametrize("n,K", [(1, 1), (1, 32), (3, 33), (129, 100), (130, 416), (257, 2048), (5, 4097), (300, 7), (2, 260), (40000, 2), (3001, 129), (500, 1066)])
 def test_quantise_bit_exact(env, n, K, kind):
     sf, ctx = env
     x, x64 = values_for(np.random.default_rng(n * 31 + K), n, K, kind)
@@ -359,7 +359,7 @@ def check_rows(got, a, w, bias, relu, kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp32"])
-@pytest.mark.parametrize("n,K,N,E", [(20011, 1024, 1024, 1), (5000, 2048, 1000, 1), (40000, 224, 257, 1), (19000, 4096, 512, 1), (30000, 512, 512, 7), (3000, 640, 160, 1)])
+@pytest.mark.parametrize("n,K,N,E", [(20011, 1024, 1024, 1), (5000, 2048, 1000, 1), (40000, 224, 257, 1), (19000, 4096, 512, 1), (30000, 512, 512, 7), (3000, 640, 160, 1), (9000, 300, 721, 3), (1200, 900, 1453, 2)])
 def test_product_of_many_rows(env, n, K, N, E, kind):
     """Sizes that fill the machine (CTA pairs): packed by the library, whose packing the tests above hold to the definition."""
     sf, ctx = env

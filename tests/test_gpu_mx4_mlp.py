@@ -142,6 +142,12 @@ def test_inside_the_composite_call(env):
     assert torch.equal(logits, again[:k])
     fast = ref["stage"] == 1
     got = label.cpu().numpy()
+    # the host entry point works in pieces of the assigned rows: the same answers
+    fp, wp = hz.pinned_packets(wl["fast"], with_hdr=False), hz.pinned_packets(wl["wide"])
+    hl, hs, he = np.zeros(n, np.uint8), np.zeros(n, np.uint8), np.zeros(1, np.uint32)
+    hcfg = sf.make_route_cfg(sf.SF_LC_GT, wl["tau"], sf.SF_MLP16, sf.SF_BF16, cfg.P, n)
+    sf.sf_serve_batch_host(ctx, forest, slow, fp["struct"], cfg.N, cfg.F, wp["struct"], hcfg, hl, hs, he)
+    assert int(he[0]) == k and np.array_equal(hl, got) and np.array_equal(hs, ref["stage"])
     assert np.array_equal(got[fast], ref["label_final"][fast]) and np.array_equal(got[~fast], lab[:k].cpu().numpy())
     sf.sf_slow_destroy(slow)
     sf.sf_forest_destroy(forest)
