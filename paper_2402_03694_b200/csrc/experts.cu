@@ -540,6 +540,21 @@ combine_narrow_kernel(const T* __restrict__ rows, uint32_t capacity, uint32_t D,
     }
 }
 
+// the rows that only fill a segment: zeros, by the blocks behind the flows' ones, fill_blocks of them an expert
+template <typename T, int V>
+__device__ __forceinline__ void fill_rows(uint32_t D, uint32_t E, const uint32_t* __restrict__ offsets, const uint32_t* __restrict__ counts, uint32_t capacity,
+                                          T* __restrict__ out, size_t ld, uint32_t flow_blocks, uint32_t fill_blocks)
+{
+    const uint32_t e = (blockIdx.x - flow_blocks) / fill_blocks, part = (blockIdx.x - flow_blocks) % fill_blocks;
+    const uint32_t lo = min(offsets[e] + counts[e], capacity), hi = min(offsets[e + 1], capacity), units = D / V;
+    const uint64_t all = e < E && lo < hi ? (uint64_t)(hi - lo) * units : 0;
+    const float zero[V] = {};
+    for (uint64_t i = part * kThreads + threadIdx.x; i < all; i += fill_blocks * kThreads) {
+        const uint32_t r = (uint32_t)(i / units), c = (uint32_t)(i - (uint64_t)r * units);
+        store_word<T, V>(out + (size_t)(lo + r) * ld + (size_t)c * V, zero);
+    }
+}
+
 // d_rows[row_of_pair[f][j]] = w[f][j] dy[f], d_w[f][j] = <dy[f], rows[row_of_pair[f][j]]>; J pairs of a flow at a time, U words of V elements.
 // A flow's dot products are summed over its lanes in a fixed tree (over the block's warps through shared memory).
 template <typename T, int V, int U, int J>
@@ -551,17 +566,7 @@ combine_backward_kernel(const T* __restrict__ dy, size_t ldy, const T* __restric
 {
     __shared__ float part[kWarps][J];
     sf_chain_enter();
-    if (blockIdx.x >= flow_blocks) {
-        const uint32_t e = (blockIdx.x - flow_blocks) / fill_blocks, part_ = (blockIdx.x - flow_blocks) % fill_blocks;
-        const uint32_t lo = min(offsets[e] + counts[e], capacity), hi = min(offsets[e + 1], capacity), units = D / V;
-        const uint64_t all = lo < hi ? (uint64_t)(hi - lo) * units : 0;
-        const float zero[V] = {};
-        for (uint64_t i = part_ * kThreads + threadIdx.x; i < all; i += fill_blocks * kThreads) {
-            const uint32_t r = (uint32_t)(i / units), c = (uint32_t)(i - (uint64_t)r * units);
-            store_word<T, V>(d_rows + (size_t)(lo + r) * ldd + (size_t)c * V, zero);
-        }
-        return;
-    }
+    if (blockIdx.x >= flow_blocks) { fill_rows<T, V>(D, E, offsets, counts, capacity, d_rows, ldd, flow_blocks, fill_blocks); return; }
     const uint32_t flows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
     const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1), warp = threadIdx.x >> 5;
     for (uint64_t base = (uint64_t)blockIdx.x * per; base < flows; base += (uint64_t)flow_blocks * per) {
@@ -637,6 +642,75 @@ combine_backward_kernel(const T* __restrict__ dy, size_t ldy, const T* __restric
             if (live && lane == 0) {
 #pragma unroll
                 for (int j = 0; j < J; j++) if (j0 + j < k) d_weights[f * k + j0 + j] = dot[j];
+            }
+        }
+    }
+}
+
+// The same for rows of at most U words a lane and up to a warp a flow: four flows at a time, their rows of dy in registers over the pairs.
+template <typename T, int V, int U>
+__global__ void __launch_bounds__(kThreads)
+combine_backward_narrow_kernel(const T* __restrict__ dy, size_t ldy, const T* __restrict__ rows, uint32_t capacity, uint32_t D, size_t ldr,
+                               const int32_t* __restrict__ row_of_pair, const float* __restrict__ weights, const uint32_t* __restrict__ n_dev,
+                               uint32_t n, uint32_t k, uint32_t E, const uint32_t* __restrict__ offsets, const uint32_t* __restrict__ counts,
+                               T* __restrict__ d_rows, size_t ldd, float* __restrict__ d_weights, uint32_t lanes, uint32_t flow_blocks, uint32_t fill_blocks, sf_dev_state* st)
+{
+    constexpr int F = 4;
+    sf_chain_enter();
+    if (blockIdx.x >= flow_blocks) { fill_rows<T, V>(D, E, offsets, counts, capacity, d_rows, ldd, flow_blocks, fill_blocks); return; }
+    const uint32_t flows = n_dev ? sf_clamp_rows(*n_dev, n, st) : n;
+    const uint32_t per = kThreads / lanes, lane = threadIdx.x & (lanes - 1);
+    const uint64_t hop = (uint64_t)flow_blocks * per;
+    for (uint64_t base = (uint64_t)blockIdx.x * per; base < flows; base += hop * F) {
+        const uint64_t f0 = base + threadIdx.x / lanes;       // (the sums over lanes below need whole warps)
+        float g[F][U][V];
+#pragma unroll
+        for (int i = 0; i < F; i++)
+#pragma unroll
+            for (int u = 0; u < U; u++) if (f0 + i * hop < flows && (lane + u * lanes) * V < D) load_word<T, V>(dy + (f0 + i * hop) * ldy + (lane + u * lanes) * V, g[i][u]);
+        for (uint32_t j = 0; j < k; j++) {
+            uint32_t r[F];
+            float w[F], dot[F];
+#pragma unroll
+            for (int i = 0; i < F; i++) {
+                const bool have = f0 + i * hop < flows;
+                r[i] = have ? (uint32_t)__ldg(row_of_pair + (f0 + i * hop) * k + j) : 0xFFFFFFFFu;
+                w[i] = have && weights ? __ldg(weights + (f0 + i * hop) * k + j) : 1.0f;
+                dot[i] = 0.0f;
+            }
+            if (d_weights) {
+                float x[F][U][V];
+#pragma unroll
+                for (int i = 0; i < F; i++)
+#pragma unroll
+                    for (int u = 0; u < U; u++) if (r[i] < capacity && (lane + u * lanes) * V < D) load_word<T, V>(rows + (size_t)r[i] * ldr + (lane + u * lanes) * V, x[i][u]);
+#pragma unroll
+                for (int i = 0; i < F; i++)
+#pragma unroll
+                    for (int u = 0; u < U; u++)
+                        if (r[i] < capacity && (lane + u * lanes) * V < D) {
+#pragma unroll
+                            for (int v = 0; v < V; v++) dot[i] = fmaf(g[i][u][v], x[i][u][v], dot[i]);
+                        }
+            }
+            if (d_rows) {
+#pragma unroll
+                for (int i = 0; i < F; i++)
+#pragma unroll
+                    for (int u = 0; u < U; u++)
+                        if (r[i] < capacity && (lane + u * lanes) * V < D) {
+                            float d[V];
+#pragma unroll
+                            for (int v = 0; v < V; v++) d[v] = w[i] * g[i][u][v];
+                            store_word<T, V>(d_rows + (size_t)r[i] * ldd + (lane + u * lanes) * V, d);
+                        }
+            }
+            if (d_weights) {
+#pragma unroll
+                for (int i = 0; i < F; i++) {
+                    for (uint32_t o = lanes / 2; o >= 1; o >>= 1) dot[i] += __shfl_xor_sync(0xFFFFFFFFu, dot[i], o);
+                    if (f0 + i * hop < flows && lane == 0) d_weights[(f0 + i * hop) * k + j] = dot[i];
+                }
             }
         }
     }
@@ -834,7 +908,8 @@ extern "C" int sf_expert_combine_backward(sf_ctx* ctx, const void* dy, int dtype
             // where flows fill the machine one pair at a time with two words on their way (120,003 x 1024 bf16, k = 2: 202 us; one word 276, two
             // pairs 226 to 239), else up to four pairs in flight
             constexpr int U2 = U == 1 ? 2 : U;
-            auto kern = (uint64_t)n * lanes >= (uint64_t)ctx->num_sms * 2048 ? combine_backward_kernel<T, V, U2, 1> : (k == 1 ? combine_backward_kernel<T, V, U, 1> :
+            auto kern = lanes <= 32 && units <= lanes ? combine_backward_narrow_kernel<T, V, 1> : lanes <= 32 && units <= 2 * lanes ? combine_backward_narrow_kernel<T, V, 2> :
+                        (uint64_t)n * lanes >= (uint64_t)ctx->num_sms * 2048 ? combine_backward_kernel<T, V, U2, 1> : (k == 1 ? combine_backward_kernel<T, V, U, 1> :
                         (k == 2 ? combine_backward_kernel<T, V, U, 2> : combine_backward_kernel<T, V, U, 4>));
             SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)dy, ldy, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, E,
                                       offsets, counts, (T*)d_rows_out, ldd, d_weights_out, lanes, fb, zb, ctx->d_state));
