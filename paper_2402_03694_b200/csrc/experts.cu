@@ -768,10 +768,10 @@ extern "C" int sf_expert_gate(sf_ctx* ctx, const void* scores, int dtype, const 
             constexpr int L = decltype(lpr)::value, V = decltype(v)::value, S = V < 4 ? V : 4;
             const bool al = fits(scores, ld, dtype, V);
             return by_mode(mode, [&](auto m) {
-            constexpr int M = decltype(m)::value;
-            auto kern = k <= S * L ? (al ? gate_kernel<T, L, V, S, M, true> : gate_kernel<T, L, V, S, M, false>) : (al ? gate_kernel<T, L, V, V, M, true> : gate_kernel<T, L, V, V, M, false>);
-            SF_CUDA(sf_launch_chained(kern, (n + kThreads / L - 1) / (kThreads / L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, ids_out, weights_out, ctx->d_state));
-            return SF_OK;
+                constexpr int M = decltype(m)::value;
+                auto kern = k <= S * L ? (al ? gate_kernel<T, L, V, S, M, true> : gate_kernel<T, L, V, S, M, false>) : (al ? gate_kernel<T, L, V, V, M, true> : gate_kernel<T, L, V, V, M, false>);
+                SF_CUDA(sf_launch_chained(kern, (n + kThreads / L - 1) / (kThreads / L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, ids_out, weights_out, ctx->d_state));
+                return SF_OK;
             });
         });
     });
@@ -792,11 +792,11 @@ extern "C" int sf_expert_gate_backward(sf_ctx* ctx, const void* scores, int dtyp
             constexpr int L = decltype(lpr)::value, V = decltype(v)::value;
             const bool al = fits(scores, ld, dtype, V) && fits(d_scores_out, ldd, dtype, V);
             return by_mode(mode, [&](auto m) {
-            constexpr int M = decltype(m)::value;
-            auto kern = al ? gate_backward_kernel<T, L, V, M, true> : gate_backward_kernel<T, L, V, M, false>;
-            SF_CUDA(sf_launch_chained(kern, (n + kThreads / L - 1) / (kThreads / L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, ids, d_weights,
-                                      (T*)d_scores_out, ldd, ctx->d_state));
-            return SF_OK;
+                constexpr int M = decltype(m)::value;
+                auto kern = al ? gate_backward_kernel<T, L, V, M, true> : gate_backward_kernel<T, L, V, M, false>;
+                SF_CUDA(sf_launch_chained(kern, (n + kThreads / L - 1) / (kThreads / L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, ids, d_weights,
+                                          (T*)d_scores_out, ldd, ctx->d_state));
+                return SF_OK;
             });
         });
     });
@@ -841,6 +841,7 @@ extern "C" int sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uin
         typedef decltype(q) Q;
         constexpr int U = sizeof(Q) == 16 ? 4 : 8;
         const uint32_t per = sizeof(Q) / size, units = D / per, lanes = lanes_for(ctx, units, n), fb = flow_grid(ctx, n, lanes), zb = fill_blocks(ctx, E, units);
+        // (rows of up to four words a lane: several flows at a time)
         auto kern = units <= lanes ? gather_kernel<Q, 1, 4> : (units <= 2 * lanes ? gather_kernel<Q, 2, 4> : (units <= 4 * lanes && sizeof(Q) < 16 ? gather_kernel<Q, 4, 2> : gather_kernel<Q, U, 1>));
         SF_CUDA(sf_launch_chained(kern, fb + E * zb, kThreads, 0, (cudaStream_t)stream, (const Q*)x, n_dev, n, units, ldx / per, k, row_of_pair, E,
                                   offsets, counts, capacity, (Q*)rows_out, ldr / per, lanes, fb, zb, ctx->d_state));

@@ -423,6 +423,45 @@ def test_refusals(env):
         assert e.value.status == sf.SF_ERR_ARG
 
 
+def test_two_streams_of_one_context_at_once(env):
+    """Each stream sorts, gathers, combines and takes gradients on its own data, many times over, with nothing between the two: every
+    pass gives what the same calls give alone."""
+    sf, ctx = env
+    rng = np.random.default_rng(17)
+    jobs = []
+    for n, k, E, D in ((20000, 2, 16, 96), (15000, 3, 300, 50)):
+        ids = dev(some_ids(rng, n, k, E))
+        cap = n * k + E * 15
+        i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
+        x, dy, w = torch.randn(n, D, device="cuda"), torch.randn(n, D, device="cuda"), torch.rand(n, k, device="cuda")
+        out = {"offsets": i32(E + 1), "counts": i32(E), "flow": i32(cap), "at": i32(n, k), "rows": torch.zeros(cap, D, device="cuda"),
+               "y": torch.zeros(n, D, device="cuda"), "d_rows": torch.zeros(cap, D, device="cuda"), "d_w": torch.zeros(n, k, device="cuda")}
+        work = i32(sf.sf_expert_sort_workspace(n, k, E) // 4 + 1)
+
+        def step(stream, ids=ids, x=x, dy=dy, w=w, o=out, work=work, E=E):
+            sf.sf_expert_sort(ctx, ids, E, 16, o["offsets"], o["counts"], o["flow"], o["at"], work, stream=stream)
+            sf.sf_expert_gather(ctx, x, o["at"], o["offsets"], o["counts"], o["rows"], stream=stream)
+            sf.sf_expert_combine(ctx, o["rows"], o["at"], w, o["y"], stream=stream)
+            sf.sf_expert_combine_backward(ctx, dy, o["rows"], o["at"], w, o["offsets"], o["counts"], o["d_rows"], o["d_w"], stream=stream)
+        step(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        jobs.append((step, out, {q: v.clone() for q, v in out.items()}))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for _, out, _ in jobs:
+            for v in out.values():
+                v.zero_()
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for (step, _, _), s in zip(jobs, streams):
+                step(s)
+        torch.cuda.synchronize()
+        for _, out, want in jobs:
+            for q in out:
+                assert torch.equal(out[q], want[q]), q
+    sf.sf_ctx_poll(ctx)
+
+
 # ---- all of them in a row -----------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("n,E,k,K,N", [(1, 4, 1, 64, 8), (10, 8, 2, 1024, 256), (700, 5, 2, 416, 200)])
 def test_experts_in_a_row(env, n, E, k, K, N):
