@@ -73,9 +73,12 @@ gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, ui
 #pragma unroll
         for (int v = 0; v < S; v++) { best_s[v] = kNegInf; best_id[v] = -1; }
         for (uint32_t j = 0; j < k; j++) {
-            float b = kNegInf; int id = 0x7FFFFFFF;
+            float b = left[0]; int id = 0x7FFFFFFF;
 #pragma unroll
-            for (int v = 0; v < V; v++) if (left[v] > b) { b = left[v]; id = (int)expert_of<LPR, V, ALIGNED>(lane, v); }
+            for (int v = 1; v + 1 < V; v += 2) b = fmaxf(b, fmaxf(left[v], left[v + 1]));
+            if (V % 2 == 0) b = fmaxf(b, left[V - 1]);
+#pragma unroll
+            for (int v = V - 1; v >= 0; v--) if (left[v] == b) id = (int)expert_of<LPR, V, ALIGNED>(lane, v);
 #pragma unroll
             for (int o = LPR / 2; o >= 1; o >>= 1) {
                 const float ob = __shfl_xor_sync(0xFFFFFFFFu, b, o);
@@ -92,8 +95,13 @@ gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, ui
         }
         if (mode == SF_GATE_SOFTMAX) {
             float t = 0.0f;
+            if (finite) {
 #pragma unroll
-            for (int v = 0; v < V; v++) t += near_top(s[v], m, finite);
+                for (int v = 0; v < V; v++) t += near_top(s[v], m, true);
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; v++) t += near_top(s[v], m, false);
+            }
             total = sum_lanes<LPR>(t);
         }
         if (live) {
@@ -114,8 +122,8 @@ gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, ui
 // d_s = p (g - sum g p); for shares d_s = (g - sum g w) / sum s at the picked experts.  Away from the picked experts that is
 // -p sum g p, or nothing, so a lane writes its part of the row without looking at the picks, and then the picked ones that are its own,
 // whose scores it reads again by their ids: comparing every id with every expert in registers took twice as long (61 us at
-// 1,000,000 x 16, k = 2).  Picks are fetched four at a time.
-template <typename T, int LPR, int V, int mode, bool ALIGNED>
+// 1,000,000 x 16, k = 2).  P picks are fetched at a time (4 or 8).
+template <typename T, int LPR, int V, int mode, int P, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads)
 gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, uint32_t n, uint32_t E, size_t ld, uint32_t k,
                      const int32_t* __restrict__ ids, const float* __restrict__ d_weights, T* d_scores, size_t ldd,
@@ -130,16 +138,16 @@ gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ 
         const bool live = row < rows;
         const uint64_t at = live ? row : base;
         const T* const x = scores + at * ld;
-        uint32_t id[4];
-        float g[4], sp[4];                             // of a pick that does not count: -inf and 0
+        uint32_t id[P];
+        float g[P], sp[P];                             // of a pick that does not count: -inf and 0
         auto picks = [&](uint32_t j0) {
 #pragma unroll
-            for (int q = 0; q < 4; q++) {
+            for (int q = 0; q < P; q++) {
                 id[q] = j0 + q < k ? (uint32_t)__ldg(ids + at * k + j0 + q) : 0xFFFFFFFFu;
                 g[q] = j0 + q < k ? __ldg(d_weights + at * k + j0 + q) : 0.0f;
             }
 #pragma unroll
-            for (int q = 0; q < 4; q++) {
+            for (int q = 0; q < P; q++) {
                 sp[q] = id[q] < E ? fmaxf(to_f32(x[id[q]]), kNegInf) : kNegInf;
                 if (sp[q] == kNegInf) g[q] = 0.0f;
             }
@@ -152,25 +160,30 @@ gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ 
             for (int v = 0; v < V; v++) m = fmaxf(m, s[v]);
             m = max_lanes<LPR>(m);
         } else if (mode == SF_GATE_SOFTMAX_PICKED) {
-            for (uint32_t j0 = 0; j0 < k; j0 += 4) {
+            for (uint32_t j0 = 0; j0 < k; j0 += P) {
                 if (j0) picks(j0);
 #pragma unroll
-                for (int q = 0; q < 4; q++) m = fmaxf(m, sp[q]);
+                for (int q = 0; q < P; q++) m = fmaxf(m, sp[q]);
             }
         }
         const bool finite = fabsf(m) < -kNegInf;
         auto part = [&](float score) { return mode == SF_GATE_SHARE ? (score == kNegInf ? 0.0f : score) : near_top(score, m, finite); };
         float t = 0.0f, dot = 0.0f;
-        if (k > 4 && mode == SF_GATE_SOFTMAX_PICKED) picks(0);
-        for (uint32_t j0 = 0; j0 < k; j0 += 4) {
+        if (k > P && mode == SF_GATE_SOFTMAX_PICKED) picks(0);
+        for (uint32_t j0 = 0; j0 < k; j0 += P) {
             if (j0) picks(j0);
 #pragma unroll
-            for (int q = 0; q < 4; q++) { const float e = part(sp[q]); dot = fmaf(g[q], e, dot); t += e; }
+            for (int q = 0; q < P; q++) { const float e = part(sp[q]); dot = fmaf(g[q], e, dot); t += e; }
         }
         if (mode == SF_GATE_SOFTMAX) {
             t = 0.0f;
+            if (finite) {
 #pragma unroll
-            for (int v = 0; v < V; v++) { s[v] = near_top(s[v], m, finite); t += s[v]; }
+                for (int v = 0; v < V; v++) { s[v] = near_top(s[v], m, true); t += s[v]; }
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; v++) { s[v] = near_top(s[v], m, false); t += s[v]; }
+            }
             t = sum_lanes<LPR>(t);
         }
         const float inv = t > 0.0f ? 1.0f / t : 0.0f;
@@ -188,10 +201,10 @@ gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ 
 #pragma unroll
             for (int v = 0; v < V; v++) { const uint32_t e = expert_of<LPR, V, ALIGNED>(lane, v); if (e < E) y[e] = from_f32<T>(d[v]); }
         }
-        for (uint32_t j0 = 0; j0 < k; j0 += 4) {
-            if (k > 4) picks(j0);
+        for (uint32_t j0 = 0; j0 < k; j0 += P) {
+            if (k > P) picks(j0);
 #pragma unroll
-            for (int q = 0; q < 4; q++)
+            for (int q = 0; q < P; q++)
                 if (id[q] < E && (ALIGNED ? id[q] / V : id[q] % LPR) == lane && sp[q] != kNegInf)
                     y[id[q]] = from_f32<T>(mode == SF_GATE_SHARE ? (g[q] - dot) * inv : part(sp[q]) * inv * (g[q] - dot));
         }
@@ -793,7 +806,8 @@ extern "C" int sf_expert_gate_backward(sf_ctx* ctx, const void* scores, int dtyp
             const bool al = fits(scores, ld, dtype, V) && fits(d_scores_out, ldd, dtype, V);
             return by_mode(mode, [&](auto m) {
                 constexpr int M = decltype(m)::value;
-                auto kern = al ? gate_backward_kernel<T, L, V, M, true> : gate_backward_kernel<T, L, V, M, false>;
+                auto kern = k <= 4 ? (al ? gate_backward_kernel<T, L, V, M, 4, true> : gate_backward_kernel<T, L, V, M, 4, false>) :
+                                     (al ? gate_backward_kernel<T, L, V, M, 8, true> : gate_backward_kernel<T, L, V, M, 8, false>);
                 SF_CUDA(sf_launch_chained(kern, (n + kThreads / L - 1) / (kThreads / L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, ids, d_weights,
                                           (T*)d_scores_out, ldd, ctx->d_state));
                 return SF_OK;
