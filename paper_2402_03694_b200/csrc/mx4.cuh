@@ -90,5 +90,8 @@ struct sf_mx4_product {
     const uint8_t* a; const uint8_t* a_scales; const uint32_t* n_rows_dev; const uint32_t* offsets; uint32_t E, capacity;
     const uint8_t* w; const uint8_t* w_scales; uint32_t N, K; const float* bias; int relu, out_dtype;
     void* out; size_t ld; uint8_t* out_scales;
+    // a head folded in (out unused): bf16 weights [16][N] with rows past C zero, bias, logits fp32 [capacity][C], labels (nullable)
+    const void* head_w; const float* head_b; uint32_t C; float* logits; uint8_t* label;
 };
 int sf_launch_mx4_product(sf_ctx* ctx, const sf_mx4_product& p, cudaStream_t st);
+bool sf_mx4_product_takes_head(sf_ctx* ctx, const sf_mx4_product& p);       // would the launch fold p's head in?

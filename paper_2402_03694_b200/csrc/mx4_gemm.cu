@@ -19,6 +19,10 @@
 // Every wait is bounded as in gemm_tc.cu: on a timeout the block records SF_ERR_DEVICE_TIMEOUT, lets its copies land, frees TMEM
 // and returns.
 //
+// Head<CH> (pairs only): a pair has whole panels, and a lane multiplies its row's bf16 outputs with the head's weights (shared memory,
+// the same address in all lanes) and keeps the logits: the activations are neither written nor read again.  The four column groups
+// of a row are summed apart and added in a fixed order.
+//
 // PAIR: two CTAs share every MMA (256 x 256 tiles, each CTA loads its 128 rows of A and of W; both need all 256 columns' scales).
 // Two 256-column fp32 accumulators would fill the TMEM and leave no room for scales, so they overlap by 64 columns
 // (0..255 and 192..447, scales from 448): the epilogue reads the shared columns first and the next tile's MMAs start then.
@@ -42,6 +46,14 @@ struct Bars {
     uint64_t a_full[5], a_empty[5], w_full[5], w_empty[5], acc_full[2], acc_free[2];
     uint32_t tmem_base, abort_flag;
 };
+struct Mx4 {};                                       // output type: packed again
+// output type: the logits of a head of up to CH classes over the bf16 outputs, which are not written
+template <uint32_t CH> struct Head {};
+template <typename T> struct HeadOf { static constexpr uint32_t kCh = 0; };
+template <uint32_t CH> struct HeadOf<Head<CH>> { static constexpr uint32_t kCh = CH; };
+constexpr uint32_t kHeadMaxN = 1024;                 // widest hidden layer whose head weights fit where outputs are staged
+template <typename T> constexpr uint32_t head_bytes() { return 128 * HeadOf<T>::kCh * 4; }      // one half's partial logits
+
 template <uint32_t BN, bool PAIR> struct Cfg {
     static constexpr uint32_t kRows = PAIR ? 256 : 128;                   // rows of a tile
     static constexpr uint32_t kNT = (BN + 127) / 128;                     // scale row tiles of W per stage
@@ -54,13 +66,11 @@ template <uint32_t BN, bool PAIR> struct Cfg {
     static constexpr uint32_t kSfCols = 8 + 8 * kNT;
     static_assert(kSecond + BN <= kSfCol && kSfCol + 2 * kSfCols <= 512, "TMEM");
     static_assert(kSlot % 1024 == 0 && kStage % 1024 == 0, "swizzled tiles start on 1024-byte boundaries");
-    static constexpr uint32_t smem(uint32_t E) { return 1024 + kSlots * kSlot + kStages * kStage + kStaging + sizeof(Bars) + (2 * E + 2) * 4; }
+    template <typename T = float> static constexpr uint32_t smem(uint32_t E) { return 1024 + kSlots * kSlot + kStages * kStage + kStaging + sizeof(Bars) + (2 * E + 2) * 4 + (head_bytes<T>() ? 16 + head_bytes<T>() : 0); }
 };
 
-static_assert(Cfg<256, true>::smem(SF_MAX_EXPERTS) <= 232448 && Cfg<128, false>::smem(SF_MAX_EXPERTS) <= 232448 &&
+static_assert(Cfg<256, true>::smem<Head<8>>(SF_MAX_EXPERTS) <= 232448 && kHeadMaxN * 32 <= kEpiWarps * 4096 && Cfg<128, false>::smem(SF_MAX_EXPERTS) <= 232448 &&
               Cfg<64, false>::smem(SF_MAX_EXPERTS) <= 232448, "shared memory of a block");
-
-struct Mx4 {};                                       // output type: packed again
 
 // 4-bit operands, fp32 accumulators, power-of-two scales per 32 values; sf = 0 or 2: which pair of a scale word's bytes
 __host__ __device__ constexpr uint32_t make_idesc(uint32_t M, uint32_t N, uint32_t sf) {
@@ -96,10 +106,10 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void mbar_arrive_relaxed(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// 128 threads meet at named barrier `id`: true in all of them if it is in each
-__device__ __forceinline__ bool half_agrees(uint32_t id, bool mine) {
+// `threads` threads meet at named barrier `id`: true in all of them if it is in each
+__device__ __forceinline__ bool all_agree(uint32_t id, uint32_t threads, bool mine) {
     uint32_t r;
-    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %2, 0;\nbar.red.and.pred q, %1, 128, p;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"(id), "r"((uint32_t)mine) : "memory");
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %3, 0;\nbar.red.and.pred q, %1, %2, p;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"(id), "r"(threads), "r"((uint32_t)mine) : "memory");
     return r != 0;
 }
 
@@ -142,6 +152,36 @@ template <typename T, uint32_t COLS, bool RELU> __device__ __forceinline__ void 
         } else {
 #pragma unroll
             for (int q = 0; q < 4; q++) v[g + q] = __float_as_uint(RELU ? relu_keep_nan(x[q]) : x[q]);
+        }
+    }
+}
+
+// logits += bf16 outputs (two a word, column col and the next first) x the head's weights
+template <uint32_t CH, uint32_t WORDS, uint32_t COLS> __device__ __forceinline__ void add_head(float (&lg)[CH], const uint32_t (&v)[COLS], const uint8_t* weights, uint32_t col) {
+#pragma unroll
+    for (uint32_t q = 0; q < WORDS; q++) {
+        const float a[2] = {__uint_as_float(v[q] << 16), __uint_as_float(v[q] & 0xFFFF0000u)};
+#pragma unroll
+        for (uint32_t h = 0; h < 2; h++) {
+            const float* const w = reinterpret_cast<const float*>(weights) + (size_t)(col + 2 * q + h) * CH;
+            float x[CH];
+            if constexpr (CH == 2) { const float2 y = *reinterpret_cast<const float2*>(w); x[0] = y.x; x[1] = y.y; }
+            else {
+#pragma unroll
+                for (uint32_t c = 0; c < CH; c += 4) {
+                    const float4 y = *reinterpret_cast<const float4*>(w + c);
+                    x[c] = y.x; x[c + 1] = y.y; x[c + 2] = y.z; x[c + 3] = y.w;
+                }
+            }
+#pragma unroll
+            for (uint32_t c = 0; c < CH; c += 2) {
+                uint64_t d, aa, ww;                  // two fused multiply-adds in one instruction
+                asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lg[c]), "f"(lg[c + 1]));
+                asm("mov.b64 %0, {%1, %1};" : "=l"(aa) : "f"(a[h]));
+                asm("mov.b64 %0, {%1, %2};" : "=l"(ww) : "f"(x[c]), "f"(x[c + 1]));
+                asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(aa), "l"(ww));
+                asm("mov.b64 {%0, %1}, %2;" : "=f"(lg[c]), "=f"(lg[c + 1]) : "l"(d));
+            }
         }
     }
 }
@@ -209,6 +249,8 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 
     const uint32_t warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     constexpr bool kPacked = std::is_same<T, Mx4>::value;
+    constexpr uint32_t kCh = HeadOf<T>::kCh;
+    static_assert(kCh == 0 || PAIR, "the head is folded into pairs only");
     const uint32_t tiles_n = ((kPacked ? k_tiles(p.N) * 128 : p.N) + BN - 1) / BN;      // packed rows: up to the last scale tile's end
     const uint32_t k_blocks = (p.K + kBK - 1) / kBK;
     const bool keep = k_blocks <= C::kSlots;          // a panel of A fits in the ring
@@ -244,6 +286,13 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             if (!p.offsets && p.n_rows_dev && blockIdx.x == 0 && *p.n_rows_dev > p.capacity) sf_dev_set_error(st, SF_ERR_CAPACITY);
         }
     }
+    float* const partial = reinterpret_cast<float*>(((uintptr_t)(seg_tile + p.E + 1) + 15) & ~(uintptr_t)15);      // [128][kCh]
+    if constexpr (kCh != 0) {                         // head weights: fp32 [column][kCh]
+        const __nv_bfloat16* const hw = reinterpret_cast<const __nv_bfloat16*>(p.head_w);
+        for (uint32_t i = threadIdx.x; i < p.N * kCh; i += kThreads) {
+            reinterpret_cast<float*>(staging)[i] = __bfloat162float(hw[(size_t)(i % kCh) * p.N + i / kCh]);
+        }
+    }
     if (warp == 1) { if constexpr (PAIR) tmem_alloc_pair(&bars->tmem_base, 512); else tmem_alloc(&bars->tmem_base, 512); }
     tc_fence_before();
     __syncthreads();
@@ -251,7 +300,8 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     tc_fence_after();
     const uint32_t tmem = uniform(bars->tmem_base);
     const uint32_t n_tiles = uniform(seg_tile[p.E]);
-    const uint32_t t_begin = (uint32_t)((uint64_t)n_tiles * unit / n_units), t_end = (uint32_t)((uint64_t)n_tiles * (unit + 1) / n_units);
+    const uint32_t grain = kCh ? tiles_n : 1u;        // (whole panels with a head)
+    const uint32_t t_begin = (uint32_t)((uint64_t)(n_tiles / grain) * unit / n_units) * grain, t_end = (uint32_t)((uint64_t)(n_tiles / grain) * (unit + 1) / n_units) * grain;
     Segments seg = {seg_begin, seg_tile, p.E, tiles_n};
 
     if (warp == 0) {
@@ -376,6 +426,7 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         constexpr uint32_t kCols = kHalf < 64 ? kHalf : 64;                  // columns read at once
         const uint32_t quarter = warp & 3u, half = (warp - 2u) >> 2;
         uint8_t* const stg = staging + (warp - 2u) * 4096u;
+        float lg[2][kCh ? kCh : 1] = {};                                     // this row's logits over the warp's first and second 64 columns
         const bool vec = !kPacked && (p.ld * sizeof(T)) % 16 == 0 && ((uintptr_t)p.out & 15) == 0;
         float* const bias_s = reinterpret_cast<float*>(staging + kEpiWarps * 4096) + half * kHalf;       // shared by the half's four warps
         uint32_t i = 0;
@@ -389,7 +440,9 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             const uint32_t bias_c = quarter * (kHalf / 4) + lane;
             const float bias_v = p.bias && lane < kHalf / 4 && col0 + bias_c < p.N ? __ldg(p.bias + (size_t)seg.e * p.N + col0 + bias_c) : 0.0f;
             // (the half's four warps go on, or leave, together: they meet again below.  All have written the tile before by now)
-            ok = half_agrees(1u + half, mbar_wait(&bars->acc_full[i & 1u], (i >> 1) & 1u, abort_flag));
+            // (with a head all eight meet: the halves exchange logits)
+            ok = mbar_wait(&bars->acc_full[i & 1u], (i >> 1) & 1u, abort_flag);
+            ok = kCh ? all_agree(3, 256, ok) : all_agree(1u + half, 128, ok);
             if (!ok) break;
             tc_fence_after();
             const uint32_t taddr = tmem + ((quarter * 32u) << 16) + (i & 1u) * C::kSecond + half * kHalf;
@@ -418,9 +471,13 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     asm volatile("bar.sync %0, 128;" ::"r"(1u + half) : "memory");
                 }
                 if (col0 + c >= (kPacked ? k_tiles(p.N) * 128 : p.N)) continue;
-                if (!kPacked && p.relu) finish<T, kCols, true>(v, bias_s + c);
+                if constexpr (kCh != 0) finish<__nv_bfloat16, kCols, true>(v, bias_s + c);
+                else if (!kPacked && p.relu) finish<T, kCols, true>(v, bias_s + c);
                 else finish<T, kCols, false>(v, bias_s + c);
-                if constexpr (kPacked) {
+                if constexpr (kCh != 0) {
+                    if (c == 0) add_head<kCh, kCols / 2>(lg[0], v, staging, col0);
+                    else add_head<kCh, kCols / 2>(lg[1], v, staging, col0 + c);
+                } else if constexpr (kPacked) {
                     // a lane's 32 consecutive columns are one scale block
                     const uint32_t col = col0 + c, pitch = row_bytes(p.N), kt = k_tiles(p.N);
                     if (col + kCols > p.N) {                                 // columns that fill the last block, and blocks behind it
@@ -508,8 +565,32 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     }
                 }
             }
+            if constexpr (kCh != 0) {
+                if (tn + 1 == tiles_n) {                                     // the panel's end: the halves meet
+                    if (half == 1) {
+#pragma unroll
+                        for (uint32_t q = 0; q < kCh; q++) partial[(quarter * 32 + lane) * kCh + q] = lg[0][q] + lg[1][q];
+                    }
+                    asm volatile("bar.sync 4, 256;" ::: "memory");
+                    if (half == 0 && row0 + lane < end) {
+                        float best = 0.0f;
+                        uint32_t arg = 0;
+#pragma unroll
+                        for (uint32_t q = 0; q < kCh; q++) {
+                            if (q < p.C) {
+                                const float x = ((lg[0][q] + lg[1][q]) + partial[(quarter * 32 + lane) * kCh + q]) + __ldg(p.head_b + q);
+                                p.logits[(size_t)(row0 + lane) * p.C + q] = x;
+                                if (q == 0 || x > best) { best = x; arg = q; }
+                            }
+                        }
+                        if (p.label) p.label[row0 + lane] = (uint8_t)arg;
+                    }
+#pragma unroll
+                    for (uint32_t q = 0; q < kCh; q++) lg[0][q] = lg[1][q] = 0.0f;
+                }
+            }
         }
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (PAIR && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
 
     __syncthreads();
@@ -541,7 +622,7 @@ int launch(sf_ctx* ctx, const sf_mx4_product& p, cudaStream_t st)
     if (rc == SF_OK) rc = encode_tmap_2d(&tmSA, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.a_scales, (p.capacity + 127) / 128, kt * 128, kt * 512, 1, 256, CU_TENSOR_MAP_SWIZZLE_NONE);
     if (rc == SF_OK) rc = encode_tmap_2d(&tmSW, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.w_scales, (uint64_t)p.E * ((p.N + 127) / 128), kt * 128, kt * 512, C::kNT, 256, CU_TENSOR_MAP_SWIZZLE_NONE);
     bool tma_out = false;
-    if constexpr (!std::is_same<T, Mx4>::value) {
+    if constexpr (!std::is_same<T, Mx4>::value && HeadOf<T>::kCh == 0) {
         tma_out = aligned(p.out, 16) && (p.ld * sizeof(T)) % 16 == 0 && (p.N * sizeof(T)) % 16 == 0 && !(BN == 64 && sizeof(T) == 2);      // (64 16-bit columns: a warp has 64 bytes of a row)
         if (rc == SF_OK && tma_out) rc = encode_tmap_2d(&tmO, sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, p.out,
                                                         p.capacity, p.N, p.ld * sizeof(T), 32, 128 / sizeof(T), CU_TENSOR_MAP_SWIZZLE_128B);
@@ -551,10 +632,10 @@ int launch(sf_ctx* ctx, const sf_mx4_product& p, cudaStream_t st)
     auto kern = mx4_product_kernel<BN, PAIR, T>;
     static bool set_dev[64] = {};                      // the opt-in is per device
     bool& set = set_dev[ctx->device & 63];
-    if (!set) { SF_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::smem(SF_MAX_EXPERTS))); set = true; }
+    if (!set) { SF_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::template smem<T>(SF_MAX_EXPERTS))); set = true; }
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((PAIR ? 2u : 1u) * (uint32_t)std::min<uint64_t>((uint64_t)ctx->num_sms / (PAIR ? 2 : 1), most));
-    lc.blockDim = dim3(kThreads); lc.dynamicSmemBytes = C::smem(p.E); lc.stream = st;
+    lc.blockDim = dim3(kThreads); lc.dynamicSmemBytes = C::template smem<T>(p.E); lc.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -573,13 +654,13 @@ template <typename T> bool pairs_supported(const sf_ctx* ctx) {
     if (c == 0) {
         auto kern = mx4_product_kernel<256, true, T>;
         cudaLaunchConfig_t lc = {};
-        lc.gridDim = dim3(2); lc.blockDim = dim3(kThreads); lc.dynamicSmemBytes = C::smem(SF_MAX_EXPERTS);
+        lc.gridDim = dim3(2); lc.blockDim = dim3(kThreads); lc.dynamicSmemBytes = C::template smem<T>(SF_MAX_EXPERTS);
         cudaLaunchAttribute at[1];
         at[0].id = cudaLaunchAttributeClusterDimension;
         at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
         lc.attrs = at; lc.numAttrs = 1;
         int n = 0;
-        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::smem(SF_MAX_EXPERTS));
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::template smem<T>(SF_MAX_EXPERTS));
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, kern, &lc);
         if (e != cudaSuccess) (void)cudaGetLastError();
         c = e == cudaSuccess && n > 0 ? 1 : -1;
@@ -602,11 +683,29 @@ int check(const sf_ctx* ctx, const sf_mx4_product& p)
 
 }  // namespace
 
+// Pairs where their tiles give every pair of SMs one (rows and tiles as far as the host knows them: the counts live on the device); 64-column
+// tiles where 128-column ones would not give every SM one.
+static bool use_pairs(const sf_ctx* ctx, const sf_mx4_product& p) {
+    const uint64_t rows = std::max<uint64_t>(1, p.capacity / p.E);
+    return p.N > 128 && rows >= 256 && (rows + 255) / 256 * p.E * ((p.N + 255) / 256) >= (uint64_t)ctx->num_sms / 2;
+}
+
+bool sf_mx4_product_takes_head(sf_ctx* ctx, const sf_mx4_product& p) {
+    // A pair has whole panels: from a panel for every pair on.  Up to eight classes: 240,000 rows, 1024 -> 1024 and the head take 113, 147 and 212
+    // us with 2, 4 and 8 classes folded in, about 220 in two launches; with 16 the epilogue's products take 600.
+    return use_pairs(ctx, p) && p.E == 1 && p.N <= kHeadMaxN && p.N % 64 == 0 && p.C >= 1 && p.C <= 8 && p.relu &&
+           (p.capacity + 255) / 256 >= (uint32_t)ctx->num_sms / 2 && pairs_supported<Head<8>>(ctx);
+}
+
 int sf_launch_mx4_product(sf_ctx* ctx, const sf_mx4_product& p, cudaStream_t st)
 {
-    // rows and tiles as far as the host knows them (the counts live on the device)
+    if (p.head_w) {
+        if (p.C <= 2) return launch<256, true, Head<2>>(ctx, p, st);
+        if (p.C <= 4) return launch<256, true, Head<4>>(ctx, p, st);
+        return launch<256, true, Head<8>>(ctx, p, st);
+    }
+    const bool pairs = use_pairs(ctx, p);
     const uint64_t rows = std::max<uint64_t>(1, p.capacity / p.E);
-    const bool pairs = p.N > 128 && rows >= 256 && (rows + 255) / 256 * p.E * ((p.N + 255) / 256) >= (uint64_t)ctx->num_sms / 2;
     const bool narrow = (rows + 127) / 128 * p.E * ((p.N + 127) / 128) < (uint64_t)ctx->num_sms;
     auto go = [&](auto zero) {
         typedef decltype(zero) T;
@@ -618,8 +717,8 @@ int sf_launch_mx4_product(sf_ctx* ctx, const sf_mx4_product& p, cudaStream_t st)
 
 // ---- the slow model's hidden layers in 4 bits ------------------------------------------------------------------
 // The wide rows (bf16) are packed once; every hidden layer but the last packs its own output in its epilogue (from the fp32 sums: no
-// activations in 16 bits in between), the last one writes bf16 for the head, which stays in bf16: its few columns cost
-// nothing and its logits decide labels.
+// activations in 16 bits in between); the head stays in bf16 (its logits decide labels) and takes the last layer's outputs rounded to
+// bf16, in that layer's epilogue for large batches, else by a launch of its own.
 namespace {
 struct MlpScratch { size_t data, scales, half, bytes; };      // two packed buffers, then the bf16 rows of the last hidden layer
 MlpScratch mlp_scratch(const sf_slow* s, uint32_t capacity) {
@@ -646,16 +745,22 @@ int sf_mlp_mx4_forward(sf_ctx* ctx, const sf_slow* s, const void* rows, const ui
     const uint32_t L = s->n_layers - 1;                  // the head
     sf_time_begin(ctx, SF_T_GEMM, st);
     int rc = sf_launch_mx4_quantise(ctx, rows, SF_BF16, capacity, s->dims[0], s->dims[0], nullptr, n_rows_dev, capacity, data[0], scales[0], st);
+    bool folded = false;
     for (uint32_t l = 0; l < L && rc == SF_OK; l++) {
         const bool last = l + 1 == L;
         const uint32_t i = l & 1u;
         sf_mx4_product p = {data[i], scales[i], n_rows_dev, nullptr, 1, capacity, (const uint8_t*)s->d_W[l], (const uint8_t*)s->d_S[l], s->dims[l + 1], s->dims[l],
-                            s->d_b[l], 1, SF_BF16, w + m.half, s->dims[l + 1], nullptr};
+                            s->d_b[l], 1, SF_BF16, w + m.half, s->dims[l + 1], nullptr, nullptr, nullptr, 0, nullptr, nullptr};
+        if (last) {
+            p.C = s->dims[L + 1];
+            if (sf_mx4_product_takes_head(ctx, p)) { p.head_w = s->d_W[L]; p.head_b = s->d_b[L]; p.logits = logits; p.label = label; }
+            folded = p.head_w != nullptr;
+        }
         if (!last) { p.out_dtype = SF_MX4; p.out = data[i ^ 1u]; p.out_scales = scales[i ^ 1u]; }
         rc = sf_launch_mx4_product(ctx, p, st);
     }
     sf_time_end(ctx, SF_T_GEMM, st);
-    if (rc != SF_OK) return rc;
+    if (rc != SF_OK || folded) return rc;
     sf_time_begin(ctx, SF_T_HEAD, st);
     rc = sf_mlp_head_bf16(ctx, w + m.half, s->d_W[L], s->d_b[L], n_rows_dev, capacity, s->dims[L], s->dims[L + 1], logits, label, st);
     sf_time_end(ctx, SF_T_HEAD, st);
@@ -666,7 +771,7 @@ extern "C" int sf_mx4_matmul(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_sca
                              const uint8_t* w, const uint8_t* w_scales, uint32_t N, uint32_t K, const float* bias, int relu,
                              int out_dtype, void* out, size_t ld, uint8_t* out_scales, void* stream)
 {
-    const sf_mx4_product p = {a, a_scales, n_rows_dev, nullptr, 1, capacity, w, w_scales, N, K, bias, relu, out_dtype, out, ld, out_scales};
+    const sf_mx4_product p = {a, a_scales, n_rows_dev, nullptr, 1, capacity, w, w_scales, N, K, bias, relu, out_dtype, out, ld, out_scales, nullptr, nullptr, 0, nullptr, nullptr};
     const int rc = check(ctx, p);
     if (rc != SF_OK || capacity == 0) return rc;
     SF_ON_DEVICE(ctx);
@@ -678,7 +783,7 @@ extern "C" int sf_mx4_matmul_experts(sf_ctx* ctx, const uint8_t* a, const uint8_
                                      const float* bias, int relu, int out_dtype, void* out, size_t ld, uint8_t* out_scales, void* stream)
 {
     if (E == 0 || E > SF_MAX_EXPERTS || (capacity && !offsets)) return SF_ERR_ARG;
-    const sf_mx4_product p = {a, a_scales, nullptr, offsets, E, capacity, w, w_scales, N, K, bias, relu, out_dtype, out, ld, out_scales};
+    const sf_mx4_product p = {a, a_scales, nullptr, offsets, E, capacity, w, w_scales, N, K, bias, relu, out_dtype, out, ld, out_scales, nullptr, nullptr, 0, nullptr, nullptr};
     const int rc = check(ctx, p);
     if (rc != SF_OK || capacity == 0) return rc;
     SF_ON_DEVICE(ctx);

@@ -35,7 +35,8 @@ def infer(sf, ctx, slow, rows, count, C):
 
 
 @pytest.mark.parametrize("dims,cap,count", [((1024, 256, 4), 300, 300), ((2048, 1024, 1024, 1024, 8), 500, 10), ((2048, 1024, 1024, 1024, 8), 70000, 61234),
-                                            ((64, 64, 2), 1, 1), ((128, 192, 320, 16), 1000, 0), ((1024, 192, 5), 40, 17), ((1024, 512, 512, 2), 30000, 29999)])
+                                            ((64, 64, 2), 1, 1), ((128, 192, 320, 16), 1000, 0), ((1024, 192, 5), 40, 17), ((1024, 512, 512, 2), 30000, 29999),
+                                            ((512, 256, 4), 20011, 20011), ((256, 320, 16), 25000, 24001), ((256, 704, 5), 19000, 300), ((128, 1024, 3), 40000, 40000)])
 def test_same_bits_as_the_staged_calls(env, dims, cap, count):
     sf, hz, ctx = env
     m = flowgen.gen_mlp(7, dims)
