@@ -175,6 +175,16 @@ gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ 
 #pragma unroll
             for (int q = 0; q < P; q++) { const float e = part(sp[q]); dot = fmaf(g[q], e, dot); t += e; }
         }
+        if (mode == SF_GATE_SHARE) {
+            // Shares by division: g - sum g w is then exactly 0 where one pick has the whole sum, and it is divided by a sum that may be small.
+            dot = 0.0f;
+            if (k > P) picks(0);
+            for (uint32_t j0 = 0; j0 < k; j0 += P) {
+                if (j0) picks(j0);
+#pragma unroll
+                for (int q = 0; q < P; q++) if (t > 0.0f) dot = fmaf(g[q], part(sp[q]) / t, dot);
+            }
+        }
         if (mode == SF_GATE_SOFTMAX) {
             t = 0.0f;
             if (finite) {
@@ -187,7 +197,7 @@ gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ 
             t = sum_lanes<LPR>(t);
         }
         const float inv = t > 0.0f ? 1.0f / t : 0.0f;
-        dot = inv > 0.0f ? dot * inv : 0.0f;           // (a sum that is not positive may have run to infinity)
+        if (mode != SF_GATE_SHARE) dot = inv > 0.0f ? dot * inv : 0.0f;
         if (!live) continue;
         float d[V];
 #pragma unroll
@@ -206,7 +216,7 @@ gate_backward_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ 
 #pragma unroll
             for (int q = 0; q < P; q++)
                 if (id[q] < E && (ALIGNED ? id[q] / V : id[q] % LPR) == lane && sp[q] != kNegInf)
-                    y[id[q]] = from_f32<T>(mode == SF_GATE_SHARE ? (g[q] - dot) * inv : part(sp[q]) * inv * (g[q] - dot));
+                    y[id[q]] = from_f32<T>(mode == SF_GATE_SHARE ? (t > 0.0f ? (g[q] - dot) / t : 0.0f) : part(sp[q]) * inv * (g[q] - dot));
         }
     }
 }

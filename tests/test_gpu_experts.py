@@ -125,6 +125,25 @@ def test_gate_and_its_gradient(env, n, E, k, kind, mode):
         assert (d[:, :at] == 5).all() and (d[:, at + E:] == 5).all()
 
 
+@pytest.mark.parametrize("mode", [1, 2])
+@pytest.mark.parametrize("E,k,kind", [(5, 1, "fp32"), (12, 1, "bf16"), (9, 6, "fp16"), (40, 9, "fp32")])
+def test_gate_gradient_of_a_lone_pick_is_nothing(env, E, k, kind, mode):
+    """One picked expert has weight 1 whatever its score, small ones too: its gradient is 0, not a rounding divided by the score."""
+    sf, ctx = env
+    rng = np.random.default_rng(E)
+    n = 500
+    x = np.full((n, E), -np.inf)
+    x[np.arange(n), rng.integers(0, E, n)] = 10.0 ** rng.uniform(-4, 0, n)
+    if k == 1:
+        x = np.where(np.isinf(x), 10.0 ** rng.uniform(-4, 0, (n, E)), x)
+    t = torch.from_numpy(x).to(TYPES[kind]).cuda()
+    ids, w, d = torch.zeros(n, k, dtype=torch.int32, device="cuda"), torch.zeros(n, k, device="cuda"), torch.full((n, E), 7.0, dtype=TYPES[kind], device="cuda")
+    sf.sf_expert_gate(ctx, t, mode, ids, w)
+    assert (w[:, 0] == 1).all() and (w[:, 1:] == 0).all()
+    sf.sf_expert_gate_backward(ctx, t, mode, ids, torch.randn(n, k, device="cuda"), d)
+    assert (d == 0).all()
+
+
 @pytest.mark.parametrize("mode", [0, 1, 2])
 def test_gate_gradient_against_differences(env, mode):
     """Central differences of the reference gate in doubles, far from a change of the picks."""
