@@ -590,7 +590,8 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 }
             }
         }
-        if (PAIR && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        // Every way out of the loop ends here: the block's shared memory is not given up before its last boxes have been read out of it.
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
 
     __syncthreads();

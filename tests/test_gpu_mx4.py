@@ -492,3 +492,47 @@ def test_captured_replayed_and_on_another_stream(env):
     step(stream=s)
     s.synchronize()
     check_product(out, pr.rounded(x.double().cpu().numpy()), rw, None, False, "fp32")
+
+
+def test_products_without_pairs_at_once_on_two_streams(env):
+    """Products of single CTAs that store by TMA, with nothing between them on two streams, each followed by packing, whose blocks take
+    over the shared memory that the last boxes were stored from: every pass gives the bits of the same calls alone."""
+    sf, ctx = env
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    jobs = []
+    for n, K, N, kind in ((20000, 256, 128, "bf16"), (20000, 200, 128, "fp32"), (700, 416, 200, "fp32"), (129, 64, 64, "fp32")):
+        x, w, bias = torch.randn(n, K, device="cuda", generator=g), torch.randn(N, K, device="cuda", generator=g) / K ** 0.5, torch.randn(N, device="cuda", generator=g)
+        def packed(v):
+            d, s = sf.sf_mx4_sizes(*v.shape)
+            return torch.zeros(d, dtype=torch.uint8, device="cuda"), torch.zeros(s, dtype=torch.uint8, device="cuda")
+        a, b = packed(x), packed(w)
+        sf.sf_mx4_quantise(ctx, x, *a)
+        sf.sf_mx4_quantise(ctx, w, *b)
+        outs, spare = [torch.zeros(n, N, dtype=TYPES[kind], device="cuda") for _ in range(6)], packed(x)
+
+        def step(stream, x=x, a=a, b=b, K=K, bias=bias, outs=outs, spare=spare):
+            for o in outs:
+                sf.sf_mx4_matmul(ctx, *a, *b, K, o, bias=bias, relu=True, stream=stream)
+                sf.sf_mx4_quantise(ctx, x[:, :x.shape[1] - 1], *spare, stream=stream)        # (rows on no 16-byte boundary: turned round in shared memory)
+        step(torch.cuda.current_stream())
+        ra, rw = torch.zeros_like(x), torch.zeros_like(w)
+        sf.sf_mx4_unpack(ctx, *a, ra)
+        sf.sf_mx4_unpack(ctx, *b, rw)
+        torch.cuda.synchronize()
+        for o in outs:
+            check_rows(o, ra.double(), rw.double(), bias.double(), True, kind)
+        jobs.append((step, outs, outs[0].clone()))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for _, outs, _ in jobs:
+            for o in outs:
+                o.zero_()
+        torch.cuda.synchronize()
+        for i, (step, _, _) in enumerate(jobs):
+            step(streams[i % 2])
+        torch.cuda.synchronize()
+        for _, outs, want in jobs:
+            for o in outs:
+                assert torch.equal(o, want)
+    sf.sf_ctx_poll(ctx)
