@@ -377,19 +377,25 @@ def sf_serve_batch_intermediates(ctx):
 _raw_stream = None
 
 
-def _stream_on(ctx, t, stream, where):
-    """Address of a stream for a call of `ctx` on tensor t; None = torch's current one on the tensor's device (by torch's raw accessor where
-    it has one: a torch.cuda.Stream object per call costs more than a small launch)."""
-    global _raw_stream
-    device = t.get_device()
-    if device != _ctx_device.get(getattr(ctx, "value", ctx), device):
+def _device_of(ctx, where):
+    """The device on which every tensor of a call of `ctx` has to be."""
+    on = _ctx_device.get(getattr(ctx, "value", ctx))
+    if on is None:
         raise SfError(SF_ERR_ARG, where)
+    return on
+
+
+def _stream_on(on, stream):
+    """Address of a stream for a call on device `on`; None = torch's current one there (by torch's raw accessor where it has one: a
+    torch.cuda.Stream object per call costs more than a small launch)."""
+    global _raw_stream
     if stream is None:
         if _raw_stream is None:
             import torch
             _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
-        return _raw_stream(device)
+        return _raw_stream(on)
     return stream if isinstance(stream, int) else stream.cuda_stream
+
 
 def _arg(ok, where):
     if not ok:
@@ -399,13 +405,13 @@ def _arg(ok, where):
 _TYPES = {}
 
 
-def _rows(t, where):
-    """(address, dtype code, rows, columns, row pitch) of a 2-D device tensor whose rows are contiguous."""
+def _rows(t, on, where):
+    """(address, dtype code, rows, columns, row pitch) of a 2-D tensor on device `on` (in host memory: -1) whose rows are contiguous."""
     if not _TYPES:
         import torch
         _TYPES.update({torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16})
     code, shape = _TYPES.get(t.dtype), t.shape
-    if code is None or len(shape) != 2 or not t.is_cuda:
+    if code is None or len(shape) != 2 or t.get_device() != on:
         raise SfError(SF_ERR_ARG, where)
     n, d = shape
     ld, s1 = t.stride()
@@ -416,18 +422,18 @@ def _rows(t, where):
     return t.data_ptr(), code, n, d, ld
 
 
-def _flat(t, count, size, where, real=False):
-    """Address of a contiguous device tensor of at least `count` whole (real: floating) numbers of `size` bytes; None stays None."""
+def _flat(t, count, size, on, where, real=False):
+    """Address of a contiguous tensor on device `on` of at least `count` whole (real: floating) numbers of `size` bytes; None stays None."""
     if t is None:
         return None
-    if not t.is_cuda or t.itemsize != size or t.nbytes < count * size or t.is_floating_point() != real or not t.is_contiguous():
+    if t.get_device() != on or t.itemsize != size or t.nbytes < count * size or t.is_floating_point() != real or not t.is_contiguous():
         raise SfError(SF_ERR_ARG, where)
     return t.data_ptr()
 
 
-def _whole(t, shape, where, real=False):
-    """Address of a contiguous device tensor of this shape of 4-byte whole (real: floating) numbers."""
-    if not t.is_cuda or t.itemsize != 4 or t.shape != shape or t.is_floating_point() != real or not t.is_contiguous():
+def _whole(t, shape, on, where, real=False):
+    """Address of a contiguous tensor on device `on` of this shape of 4-byte whole (real: floating) numbers."""
+    if t.get_device() != on or t.itemsize != 4 or t.shape != shape or t.is_floating_point() != real or not t.is_contiguous():
         raise SfError(SF_ERR_ARG, where)
     return t.data_ptr()
 
@@ -446,73 +452,79 @@ def sf_mx4_sizes(rows, K):
 def sf_mx4_quantise(ctx, x, data_out, scales_out, row_ids=None, n_rows_dev=None, stream=None):
     """Packs x[rows][K]; with row_ids (int32 device tensor) output row r is x[row_ids[r]]."""
     w = "sf_mx4_quantise"
-    p, dt, n, K, ld = _rows(x, w)
+    on = _device_of(ctx, w)
+    p, dt, n, K, ld = _rows(x, on, w)
     m = n if row_ids is None else row_ids.numel()
     pitch, sb = _mx4_bytes(m, K)
-    _check(_lib().sf_mx4_quantise(ctx, p, dt, n, K, ld, _flat(row_ids, m, 4, w), _flat(n_rows_dev, 1, 4, w), m,
-                                  _flat(data_out, m * pitch, 1, w), _flat(scales_out, sb, 1, w), _stream_on(ctx, x, stream, w)), w)
+    _check(_lib().sf_mx4_quantise(ctx, p, dt, n, K, ld, _flat(row_ids, m, 4, on, w), _flat(n_rows_dev, 1, 4, on, w), m,
+                                  _flat(data_out, m * pitch, 1, on, w), _flat(scales_out, sb, 1, on, w), _stream_on(on, stream)), w)
 
 
 def sf_mx4_unpack(ctx, data, scales, out, n_rows_dev=None, stream=None):
     w = "sf_mx4_unpack"
-    p, dt, n, K, ld = _rows(out, w)
+    on = _device_of(ctx, w)
+    p, dt, n, K, ld = _rows(out, on, w)
     pitch, sb = _mx4_bytes(n, K)
-    _check(_lib().sf_mx4_unpack(ctx, _flat(data, n * pitch, 1, w), _flat(scales, sb, 1, w), _flat(n_rows_dev, 1, 4, w), n, K, dt, p, ld,
-                                _stream_on(ctx, out, stream, w)), w)
+    _check(_lib().sf_mx4_unpack(ctx, _flat(data, n * pitch, 1, on, w), _flat(scales, sb, 1, on, w), _flat(n_rows_dev, 1, 4, on, w), n, K, dt, p, ld,
+                                _stream_on(on, stream)), w)
 
 
-def _product_out(out, out_scales, N, w):
+def _product_out(out, out_scales, N, on, w):
     """(address, type, rows, N, pitch, scales' address) of a product's output: a 2-D float tensor, or packed rows of N values."""
     if out_scales is None:
-        p, dt, n, cols, ld = _rows(out, w)
+        p, dt, n, cols, ld = _rows(out, on, w)
         _arg(N is None or N == cols, w)
         return p, dt, n, cols, ld, None
     _arg(N is not None and N >= 1 and out.dim() == 2 and out.shape[1] == -(-N // 32) * 16, w)
     n = out.shape[0]
-    return _flat(out, 0, 1, w), SF_MX4, n, N, 0, _flat(out_scales, _mx4_bytes(n, N)[1], 1, w)
+    return _flat(out, 0, 1, on, w), SF_MX4, n, N, 0, _flat(out_scales, _mx4_bytes(n, N)[1], 1, on, w)
 
 
 def sf_mx4_matmul(ctx, a, a_scales, w, w_scales, K, out, bias=None, relu=False, n_rows_dev=None, out_scales=None, N=None, stream=None):
     """out[rows][N] = act(A W^T + bias); A and W packed rows of K values, out bf16, fp16 or fp32 - or, with out_scales and N, packed rows
     again (out uint8 [rows][ceil(N/32)*16])."""
     s = "sf_mx4_matmul"
-    p, dt, n, N, ld, os_ = _product_out(out, out_scales, N, s)
+    on = _device_of(ctx, s)
+    p, dt, n, N, ld, os_ = _product_out(out, out_scales, N, on, s)
     pitch, ab = _mx4_bytes(n, K)
-    _check(_lib().sf_mx4_matmul(ctx, _flat(a, n * pitch, 1, s), _flat(a_scales, ab, 1, s), _flat(n_rows_dev, 1, 4, s), n,
-                                _flat(w, N * pitch, 1, s), _flat(w_scales, _mx4_bytes(N, K)[1], 1, s), N, K, _flat(bias, N, 4, s, True),
-                                int(relu), dt, p, ld, os_, _stream_on(ctx, out, stream, s)), s)
+    _check(_lib().sf_mx4_matmul(ctx, _flat(a, n * pitch, 1, on, s), _flat(a_scales, ab, 1, on, s), _flat(n_rows_dev, 1, 4, on, s), n,
+                                _flat(w, N * pitch, 1, on, s), _flat(w_scales, _mx4_bytes(N, K)[1], 1, on, s), N, K, _flat(bias, N, 4, on, s, True),
+                                int(relu), dt, p, ld, os_, _stream_on(on, stream)), s)
 
 
 def sf_mx4_matmul_experts(ctx, a, a_scales, w, w_scales, K, offsets, out, bias=None, relu=False, out_scales=None, N=None, stream=None):
     """The same over rows sorted by expert: offsets [E + 1] (device), w, w_scales and bias of the E experts one behind the other."""
     s = "sf_mx4_matmul_experts"
-    p, dt, n, N, ld, os_ = _product_out(out, out_scales, N, s)
+    on = _device_of(ctx, s)
+    p, dt, n, N, ld, os_ = _product_out(out, out_scales, N, on, s)
     E = offsets.numel() - 1
     _arg(E >= 1, s)
     pitch, ab = _mx4_bytes(n, K)
-    _check(_lib().sf_mx4_matmul_experts(ctx, _flat(a, n * pitch, 1, s), _flat(a_scales, ab, 1, s), _flat(offsets, E + 1, 4, s), E, n,
-                                        _flat(w, E * N * pitch, 1, s), _flat(w_scales, E * _mx4_bytes(N, K)[1], 1, s), N, K,
-                                        _flat(bias, E * N, 4, s, True), int(relu), dt, p, ld, os_, _stream_on(ctx, out, stream, s)), s)
+    _check(_lib().sf_mx4_matmul_experts(ctx, _flat(a, n * pitch, 1, on, s), _flat(a_scales, ab, 1, on, s), _flat(offsets, E + 1, 4, on, s), E, n,
+                                        _flat(w, E * N * pitch, 1, on, s), _flat(w_scales, E * _mx4_bytes(N, K)[1], 1, on, s), N, K,
+                                        _flat(bias, E * N, 4, on, s, True), int(relu), dt, p, ld, os_, _stream_on(on, stream)), s)
 
 
 def sf_expert_gate(ctx, scores, mode, ids_out, weights_out, n_dev=None, stream=None):
     """ids_out int32 [n][k], weights_out float32 [n][k] from scores [n][E]."""
     w = "sf_expert_gate"
-    p, dt, n, E, ld = _rows(scores, w)
+    on = _device_of(ctx, w)
+    p, dt, n, E, ld = _rows(scores, on, w)
     _arg(ids_out.dim() == 2, w)
     k = ids_out.shape[1]
-    _check(_lib().sf_expert_gate(ctx, p, dt, _flat(n_dev, 1, 4, w), n, E, ld, k, mode, _whole(ids_out, (n, k), w),
-                                 _whole(weights_out, (n, k), w, True), _stream_on(ctx, scores, stream, w)), w)
+    _check(_lib().sf_expert_gate(ctx, p, dt, _flat(n_dev, 1, 4, on, w), n, E, ld, k, mode, _whole(ids_out, (n, k), on, w),
+                                 _whole(weights_out, (n, k), on, w, True), _stream_on(on, stream)), w)
 
 
 def sf_expert_gate_backward(ctx, scores, mode, ids, d_weights, d_scores_out, n_dev=None, stream=None):
     w = "sf_expert_gate_backward"
-    p, dt, n, E, ld = _rows(scores, w)
-    q, dq, m, F, ldd = _rows(d_scores_out, w)
+    on = _device_of(ctx, w)
+    p, dt, n, E, ld = _rows(scores, on, w)
+    q, dq, m, F, ldd = _rows(d_scores_out, on, w)
     _arg(dq == dt and m == n and F == E and ids.dim() == 2, w)
     k = ids.shape[1]
-    _check(_lib().sf_expert_gate_backward(ctx, p, dt, _flat(n_dev, 1, 4, w), n, E, ld, k, mode, _whole(ids, (n, k), w),
-                                          _whole(d_weights, (n, k), w, True), q, ldd, _stream_on(ctx, scores, stream, w)), w)
+    _check(_lib().sf_expert_gate_backward(ctx, p, dt, _flat(n_dev, 1, 4, on, w), n, E, ld, k, mode, _whole(ids, (n, k), on, w),
+                                          _whole(d_weights, (n, k), on, w, True), q, ldd, _stream_on(on, stream)), w)
 
 
 def sf_expert_sort_workspace(n, k, E):
@@ -525,63 +537,68 @@ def sf_expert_sort_workspace(n, k, E):
 def sf_expert_sort(ctx, ids, E, align, offsets_out, counts_out, flow_of_row_out, row_of_pair_out, workspace=None, n_dev=None, stream=None):
     """ids int32 [n][k]; capacity = flow_of_row_out's length."""
     w = "sf_expert_sort"
+    on = _device_of(ctx, w)
     _arg(ids.dim() == 2, w)
     n, k = ids.shape
     wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _arg(workspace is None or (workspace.is_cuda and workspace.is_contiguous()), w)
+    _arg(workspace is None or (workspace.get_device() == on and workspace.is_contiguous()), w)
     cap = flow_of_row_out.numel()
-    _check(_lib().sf_expert_sort(ctx, _whole(ids, (n, k), w), _flat(n_dev, 1, 4, w), n, k, E, align, cap, _flat(offsets_out, E + 1, 4, w),
-                                 _flat(counts_out, E, 4, w), _flat(flow_of_row_out, cap, 4, w), _whole(row_of_pair_out, (n, k), w),
-                                 _dp(workspace), wb, _stream_on(ctx, ids, stream, w)), w)
+    _check(_lib().sf_expert_sort(ctx, _whole(ids, (n, k), on, w), _flat(n_dev, 1, 4, on, w), n, k, E, align, cap, _flat(offsets_out, E + 1, 4, on, w),
+                                 _flat(counts_out, E, 4, on, w), _flat(flow_of_row_out, cap, 4, on, w), _whole(row_of_pair_out, (n, k), on, w),
+                                 _dp(workspace), wb, _stream_on(on, stream)), w)
 
 
 def sf_expert_gather(ctx, x, row_of_pair, offsets, counts, rows_out, n_dev=None, stream=None):
     """rows_out [capacity][D] from x [n][D] by row_of_pair int32 [n][k]."""
     w = "sf_expert_gather"
-    p, dt, n, D, ld = _rows(x, w)
-    q, dq, cap, F, ldr = _rows(rows_out, w)
+    on = _device_of(ctx, w)
+    p, dt, n, D, ld = _rows(x, on, w)
+    q, dq, cap, F, ldr = _rows(rows_out, on, w)
     E = counts.numel()
     _arg(dq == dt and F == D and row_of_pair.dim() == 2, w)
     k = row_of_pair.shape[1]
-    _check(_lib().sf_expert_gather(ctx, p, dt, _flat(n_dev, 1, 4, w), n, D, ld, k, _whole(row_of_pair, (n, k), w), E,
-                                   _flat(offsets, E + 1, 4, w), _flat(counts, E, 4, w), cap, q, ldr, _stream_on(ctx, x, stream, w)), w)
+    _check(_lib().sf_expert_gather(ctx, p, dt, _flat(n_dev, 1, 4, on, w), n, D, ld, k, _whole(row_of_pair, (n, k), on, w), E,
+                                   _flat(offsets, E + 1, 4, on, w), _flat(counts, E, 4, on, w), cap, q, ldr, _stream_on(on, stream)), w)
 
 
-def _pairs_of(rows, row_of_pair, y, w):
-    p, dt, cap, D, ldr = _rows(rows, w)
-    q, dq, n, F, ldy = _rows(y, w)
+def _pairs_of(rows, row_of_pair, y, on, w):
+    p, dt, cap, D, ldr = _rows(rows, on, w)
+    q, dq, n, F, ldy = _rows(y, on, w)
     _arg(dq == dt and F == D and row_of_pair.dim() == 2, w)
     k = row_of_pair.shape[1]
-    return p, dt, cap, D, ldr, _whole(row_of_pair, (n, k), w), q, n, k, ldy
+    return p, dt, cap, D, ldr, _whole(row_of_pair, (n, k), on, w), q, n, k, ldy
 
 
 def sf_expert_gather_backward(ctx, d_rows, row_of_pair, dx_out, n_dev=None, stream=None):
     w = "sf_expert_gather_backward"
-    p, dt, cap, D, ldr, at, q, n, k, ldx = _pairs_of(d_rows, row_of_pair, dx_out, w)
-    _check(_lib().sf_expert_gather_backward(ctx, p, dt, cap, D, ldr, at, _flat(n_dev, 1, 4, w), n, k, q, ldx, _stream_on(ctx, dx_out, stream, w)), w)
+    on = _device_of(ctx, w)
+    p, dt, cap, D, ldr, at, q, n, k, ldx = _pairs_of(d_rows, row_of_pair, dx_out, on, w)
+    _check(_lib().sf_expert_gather_backward(ctx, p, dt, cap, D, ldr, at, _flat(n_dev, 1, 4, on, w), n, k, q, ldx, _stream_on(on, stream)), w)
 
 
 def sf_expert_combine(ctx, rows, row_of_pair, weights, y_out, n_dev=None, stream=None):
     """weights float32 [n][k] or None (all 1)."""
     w = "sf_expert_combine"
-    p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, y_out, w)
-    g = None if weights is None else _whole(weights, (n, k), w, True)
-    _check(_lib().sf_expert_combine(ctx, p, dt, cap, D, ldr, at, g, _flat(n_dev, 1, 4, w), n, k, q, ldy, _stream_on(ctx, y_out, stream, w)), w)
+    on = _device_of(ctx, w)
+    p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, y_out, on, w)
+    g = None if weights is None else _whole(weights, (n, k), on, w, True)
+    _check(_lib().sf_expert_combine(ctx, p, dt, cap, D, ldr, at, g, _flat(n_dev, 1, 4, on, w), n, k, q, ldy, _stream_on(on, stream)), w)
 
 
 def sf_expert_combine_backward(ctx, dy, rows, row_of_pair, weights, offsets, counts, d_rows_out, d_weights_out, n_dev=None, stream=None):
     """Either output may be None."""
     w = "sf_expert_combine_backward"
-    p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, dy, w)
-    g = None if weights is None else _whole(weights, (n, k), w, True)
+    on = _device_of(ctx, w)
+    p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, dy, on, w)
+    g = None if weights is None else _whole(weights, (n, k), on, w, True)
     E = counts.numel()
     r, ldd = None, 0
     if d_rows_out is not None:
-        r, dr, c2, D2, ldd = _rows(d_rows_out, w)
+        r, dr, c2, D2, ldd = _rows(d_rows_out, on, w)
         _arg((dr, c2, D2) == (dt, cap, D), w)
-    dw = None if d_weights_out is None else _whole(d_weights_out, (n, k), w, True)
-    _check(_lib().sf_expert_combine_backward(ctx, q, dt, ldy, p, cap, D, ldr, at, g, _flat(n_dev, 1, 4, w), n, k, E,
-                                             _flat(offsets, E + 1, 4, w), _flat(counts, E, 4, w), r, ldd, dw, _stream_on(ctx, dy, stream, w)), w)
+    dw = None if d_weights_out is None else _whole(d_weights_out, (n, k), on, w, True)
+    _check(_lib().sf_expert_combine_backward(ctx, q, dt, ldy, p, cap, D, ldr, at, g, _flat(n_dev, 1, 4, on, w), n, k, E,
+                                             _flat(offsets, E + 1, 4, on, w), _flat(counts, E, 4, on, w), r, ldd, dw, _stream_on(on, stream)), w)
 
 
 def sf_table_create(ctx, log2_slots, fast_pkts, slow_pkts, slow_slabs):
