@@ -403,6 +403,7 @@ def _arg(ok, where):
 
 
 _TYPES = {}
+_U32 = 0xFFFFFFFF                 # the library's sizes; ctypes would cut a larger one to its low half
 
 
 def _rows(t, on, where):
@@ -417,7 +418,7 @@ def _rows(t, on, where):
     ld, s1 = t.stride()
     if n <= 1:
         ld = d
-    if ld < d or (d > 1 and s1 != 1):
+    if ld < d or (d > 1 and s1 != 1) or n > _U32 or d > _U32:
         raise SfError(SF_ERR_ARG, where)
     return t.data_ptr(), code, n, d, ld
 
@@ -445,6 +446,7 @@ def _mx4_bytes(rows, K):
 def sf_mx4_sizes(rows, K):
     """(data bytes, scale bytes) of `rows` packed rows of K values."""
     d, s = C.c_size_t(), C.c_size_t()
+    _arg(0 <= rows <= _U32 and 0 < K <= _U32, "sf_mx4_sizes")
     _check(_lib().sf_mx4_sizes(rows, K, C.byref(d), C.byref(s)), "sf_mx4_sizes")
     return d.value, s.value
 
@@ -455,6 +457,7 @@ def sf_mx4_quantise(ctx, x, data_out, scales_out, row_ids=None, n_rows_dev=None,
     on = _device_of(ctx, w)
     p, dt, n, K, ld = _rows(x, on, w)
     m = n if row_ids is None else row_ids.numel()
+    _arg(m <= _U32, w)
     pitch, sb = _mx4_bytes(m, K)
     _check(_lib().sf_mx4_quantise(ctx, p, dt, n, K, ld, _flat(row_ids, m, 4, on, w), _flat(n_rows_dev, 1, 4, on, w), m,
                                   _flat(data_out, m * pitch, 1, on, w), _flat(scales_out, sb, 1, on, w), _stream_on(on, stream)), w)
@@ -477,6 +480,7 @@ def _product_out(out, out_scales, N, on, w):
         return p, dt, n, cols, ld, None
     _arg(N is not None and N >= 1 and out.dim() == 2 and out.shape[1] == -(-N // 32) * 16, w)
     n = out.shape[0]
+    _arg(n <= _U32 and N <= _U32, w)
     return _flat(out, 0, 1, on, w), SF_MX4, n, N, 0, _flat(out_scales, _mx4_bytes(n, N)[1], 1, on, w)
 
 
@@ -486,6 +490,7 @@ def sf_mx4_matmul(ctx, a, a_scales, w, w_scales, K, out, bias=None, relu=False, 
     s = "sf_mx4_matmul"
     on = _device_of(ctx, s)
     p, dt, n, N, ld, os_ = _product_out(out, out_scales, N, on, s)
+    _arg(0 < K <= _U32, s)
     pitch, ab = _mx4_bytes(n, K)
     _check(_lib().sf_mx4_matmul(ctx, _flat(a, n * pitch, 1, on, s), _flat(a_scales, ab, 1, on, s), _flat(n_rows_dev, 1, 4, on, s), n,
                                 _flat(w, N * pitch, 1, on, s), _flat(w_scales, _mx4_bytes(N, K)[1], 1, on, s), N, K, _flat(bias, N, 4, on, s, True),
@@ -498,7 +503,7 @@ def sf_mx4_matmul_experts(ctx, a, a_scales, w, w_scales, K, offsets, out, bias=N
     on = _device_of(ctx, s)
     p, dt, n, N, ld, os_ = _product_out(out, out_scales, N, on, s)
     E = offsets.numel() - 1
-    _arg(E >= 1, s)
+    _arg(1 <= E <= _U32 and 0 < K <= _U32, s)
     pitch, ab = _mx4_bytes(n, K)
     _check(_lib().sf_mx4_matmul_experts(ctx, _flat(a, n * pitch, 1, on, s), _flat(a_scales, ab, 1, on, s), _flat(offsets, E + 1, 4, on, s), E, n,
                                         _flat(w, E * N * pitch, 1, on, s), _flat(w_scales, E * _mx4_bytes(N, K)[1], 1, on, s), N, K,
@@ -510,7 +515,7 @@ def sf_expert_gate(ctx, scores, mode, ids_out, weights_out, n_dev=None, stream=N
     w = "sf_expert_gate"
     on = _device_of(ctx, w)
     p, dt, n, E, ld = _rows(scores, on, w)
-    _arg(ids_out.dim() == 2, w)
+    _arg(ids_out.dim() == 2 and ids_out.shape[1] <= _U32, w)
     k = ids_out.shape[1]
     _check(_lib().sf_expert_gate(ctx, p, dt, _flat(n_dev, 1, 4, on, w), n, E, ld, k, mode, _whole(ids_out, (n, k), on, w),
                                  _whole(weights_out, (n, k), on, w, True), _stream_on(on, stream)), w)
@@ -521,7 +526,7 @@ def sf_expert_gate_backward(ctx, scores, mode, ids, d_weights, d_scores_out, n_d
     on = _device_of(ctx, w)
     p, dt, n, E, ld = _rows(scores, on, w)
     q, dq, m, F, ldd = _rows(d_scores_out, on, w)
-    _arg(dq == dt and m == n and F == E and ids.dim() == 2, w)
+    _arg(dq == dt and m == n and F == E and ids.dim() == 2 and ids.shape[1] <= _U32, w)
     k = ids.shape[1]
     _check(_lib().sf_expert_gate_backward(ctx, p, dt, _flat(n_dev, 1, 4, on, w), n, E, ld, k, mode, _whole(ids, (n, k), on, w),
                                           _whole(d_weights, (n, k), on, w, True), q, ldd, _stream_on(on, stream)), w)
@@ -530,6 +535,7 @@ def sf_expert_gate_backward(ctx, scores, mode, ids, d_weights, d_scores_out, n_d
 def sf_expert_sort_workspace(n, k, E):
     """Bytes of device scratch that sorting n * k pairs over E experts needs at most."""
     b = C.c_size_t()
+    _arg(0 <= n <= _U32 and 0 < k <= _U32 and 0 < E <= _U32, "sf_expert_sort_workspace")
     _check(_lib().sf_expert_sort_workspace(n, k, E, C.byref(b)), "sf_expert_sort_workspace")
     return b.value
 
@@ -543,6 +549,7 @@ def sf_expert_sort(ctx, ids, E, align, offsets_out, counts_out, flow_of_row_out,
     wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _arg(workspace is None or (workspace.get_device() == on and workspace.is_contiguous()), w)
     cap = flow_of_row_out.numel()
+    _arg(n <= _U32 and k <= _U32 and 0 < E <= _U32 and 0 < align <= _U32 and cap <= _U32, w)
     _check(_lib().sf_expert_sort(ctx, _whole(ids, (n, k), on, w), _flat(n_dev, 1, 4, on, w), n, k, E, align, cap, _flat(offsets_out, E + 1, 4, on, w),
                                  _flat(counts_out, E, 4, on, w), _flat(flow_of_row_out, cap, 4, on, w), _whole(row_of_pair_out, (n, k), on, w),
                                  _dp(workspace), wb, _stream_on(on, stream)), w)
@@ -555,7 +562,7 @@ def sf_expert_gather(ctx, x, row_of_pair, offsets, counts, rows_out, n_dev=None,
     p, dt, n, D, ld = _rows(x, on, w)
     q, dq, cap, F, ldr = _rows(rows_out, on, w)
     E = counts.numel()
-    _arg(dq == dt and F == D and row_of_pair.dim() == 2, w)
+    _arg(E <= _U32 and dq == dt and F == D and row_of_pair.dim() == 2 and row_of_pair.shape[1] <= _U32, w)
     k = row_of_pair.shape[1]
     _check(_lib().sf_expert_gather(ctx, p, dt, _flat(n_dev, 1, 4, on, w), n, D, ld, k, _whole(row_of_pair, (n, k), on, w), E,
                                    _flat(offsets, E + 1, 4, on, w), _flat(counts, E, 4, on, w), cap, q, ldr, _stream_on(on, stream)), w)
@@ -564,7 +571,7 @@ def sf_expert_gather(ctx, x, row_of_pair, offsets, counts, rows_out, n_dev=None,
 def _pairs_of(rows, row_of_pair, y, on, w):
     p, dt, cap, D, ldr = _rows(rows, on, w)
     q, dq, n, F, ldy = _rows(y, on, w)
-    _arg(dq == dt and F == D and row_of_pair.dim() == 2, w)
+    _arg(dq == dt and F == D and row_of_pair.dim() == 2 and row_of_pair.shape[1] <= _U32, w)
     k = row_of_pair.shape[1]
     return p, dt, cap, D, ldr, _whole(row_of_pair, (n, k), on, w), q, n, k, ldy
 
@@ -592,6 +599,7 @@ def sf_expert_combine_backward(ctx, dy, rows, row_of_pair, weights, offsets, cou
     p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, dy, on, w)
     g = None if weights is None else _whole(weights, (n, k), on, w, True)
     E = counts.numel()
+    _arg(E <= _U32, w)
     r, ldd = None, 0
     if d_rows_out is not None:
         r, dr, c2, D2, ldd = _rows(d_rows_out, on, w)

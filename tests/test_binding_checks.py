@@ -124,3 +124,49 @@ def test_every_tensor_has_to_be_on_the_contexts_device(stub, name):
         with pytest.raises(sf.SfError):
             call(other, **{q: OnDevice(t) for q, t in tensors.items()})
     assert len(lib.calls) == 1
+
+
+BIG = (1 << 32) + 3                                      # its low half would be a size of 3
+
+
+def meta(*s, t=torch.float32):
+    """A tensor of any size without memory."""
+    return OnDevice(torch.empty(*s, dtype=t, device="meta"))
+
+
+@pytest.mark.parametrize("call", [
+    lambda c: sf.sf_mx4_quantise(c, meta(BIG, 1), meta(BIG * 16, t=torch.uint8), meta(BIG * 8, t=torch.uint8), stream=7),
+    lambda c: sf.sf_mx4_quantise(c, meta(1, BIG), meta(BIG, t=torch.uint8), meta(BIG * 8, t=torch.uint8), stream=7),
+    lambda c: sf.sf_mx4_quantise(c, meta(9, 1), meta(BIG * 16, t=torch.uint8), meta(BIG * 8, t=torch.uint8), row_ids=meta(BIG, t=torch.int32), stream=7),
+    lambda c: sf.sf_mx4_unpack(c, meta(BIG * 16, t=torch.uint8), meta(BIG * 8, t=torch.uint8), meta(BIG, 1), stream=7),
+    lambda c: sf.sf_mx4_matmul(c, meta(BIG * 16, t=torch.uint8), meta(BIG * 8, t=torch.uint8), meta(64, t=torch.uint8), meta(512, t=torch.uint8), 32, meta(BIG, 4), stream=7),
+    lambda c: sf.sf_mx4_matmul(c, meta(BIG * 2, t=torch.uint8), meta(BIG * 8, t=torch.uint8), meta(BIG * 4, t=torch.uint8), meta(BIG * 8, t=torch.uint8), BIG, meta(1, 4), stream=7),
+    lambda c: sf.sf_mx4_matmul(c, meta(BIG * 16, t=torch.uint8), meta(BIG * 8, t=torch.uint8), meta(64, t=torch.uint8), meta(512, t=torch.uint8), 32, meta(BIG, 16, t=torch.uint8),
+                               out_scales=meta(BIG * 8, t=torch.uint8), N=4, stream=7),
+    lambda c: sf.sf_mx4_matmul_experts(c, meta(64, t=torch.uint8), meta(512, t=torch.uint8), meta(BIG * 64, t=torch.uint8), meta(BIG * 512, t=torch.uint8), 32, meta(BIG + 1, t=torch.int32),
+                                       meta(4, 4), stream=7),
+    lambda c: sf.sf_expert_gate(c, meta(BIG, 4), 0, meta(BIG, 1, t=torch.int32), meta(BIG, 1), stream=7),
+    lambda c: sf.sf_expert_gate(c, meta(1, 4), 0, meta(1, BIG, t=torch.int32), meta(1, BIG), stream=7),
+    lambda c: sf.sf_expert_gate_backward(c, meta(BIG, 4), 0, meta(BIG, 1, t=torch.int32), meta(BIG, 1), meta(BIG, 4), stream=7),
+    lambda c: sf.sf_expert_gate_backward(c, meta(1, 4), 0, meta(1, BIG, t=torch.int32), meta(1, BIG), meta(1, 4), stream=7),
+    lambda c: sf.sf_expert_sort(c, meta(BIG, 1, t=torch.int32), 4, 1, meta(5, t=torch.int32), meta(4, t=torch.int32), meta(9, t=torch.int32), meta(BIG, 1, t=torch.int32), stream=7),
+    lambda c: sf.sf_expert_sort(c, meta(3, 1, t=torch.int32), 4, 1, meta(5, t=torch.int32), meta(4, t=torch.int32), meta(BIG, t=torch.int32), meta(3, 1, t=torch.int32), stream=7),
+    lambda c: sf.sf_expert_sort(c, meta(3, 1, t=torch.int32), 4, (1 << 32) + 128, meta(5, t=torch.int32), meta(4, t=torch.int32), meta(9, t=torch.int32), meta(3, 1, t=torch.int32), stream=7),
+    lambda c: sf.sf_expert_gather(c, meta(BIG, 4), meta(BIG, 1, t=torch.int32), meta(5, t=torch.int32), meta(4, t=torch.int32), meta(9, 4), stream=7),
+    lambda c: sf.sf_expert_gather(c, meta(3, 4), meta(3, 1, t=torch.int32), meta(5, t=torch.int32), meta(4, t=torch.int32), meta(BIG, 4), stream=7),
+    lambda c: sf.sf_expert_gather(c, meta(3, 4), meta(3, 1, t=torch.int32), meta(BIG + 1, t=torch.int32), meta(BIG, t=torch.int32), meta(9, 4), stream=7),
+    lambda c: sf.sf_expert_gather_backward(c, meta(9, 4), meta(BIG, 1, t=torch.int32), meta(BIG, 4), stream=7),
+    lambda c: sf.sf_expert_combine(c, meta(BIG, 4), meta(3, 1, t=torch.int32), None, meta(3, 4), stream=7),
+    lambda c: sf.sf_expert_combine(c, meta(9, 4), meta(3, BIG, t=torch.int32), None, meta(3, 4), stream=7),
+    lambda c: sf.sf_expert_combine_backward(c, meta(BIG, 4), meta(9, 4), meta(BIG, 1, t=torch.int32), None, meta(5, t=torch.int32), meta(4, t=torch.int32), None, meta(BIG, 1), stream=7),
+    lambda c: sf.sf_expert_combine_backward(c, meta(3, 4), meta(9, 4), meta(3, 1, t=torch.int32), None, meta(BIG + 1, t=torch.int32), meta(BIG, t=torch.int32), None, meta(3, 1), stream=7),
+    lambda c: sf.sf_mx4_sizes(BIG, 64),
+    lambda c: sf.sf_mx4_sizes(3, BIG),
+    lambda c: sf.sf_expert_sort_workspace(BIG, 1, 4),
+    lambda c: sf.sf_expert_sort_workspace(3, 1, BIG)])
+def test_sizes_past_32_bits_are_refused(stub, call):
+    """Their low halves are sizes that the library would take: a part of the rows would be done and the call succeed."""
+    lib, ctx = stub
+    with pytest.raises(sf.SfError) as e:
+        call(ctx)
+    assert e.value.status == sf.SF_ERR_ARG and lib.calls == []
