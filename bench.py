@@ -190,10 +190,10 @@ def hidden_flops_per_row(cfg):
 def kernel_launches_per_step(cfg, capacity):
     """Kernels of this library that one sf_serve_batch call launches (the ncu launch lists under profiles/ agree)."""
     if cfg.slow == "mlp":
-        slow = (len(cfg.dims) - 1) + (1 if cfg.slow_dtype == "f32" else 0)    # layers (+ argmax for fp32)
+        slow = (len(cfg.dims) - 1) + (0 if cfg.slow_bf16 else 1)    # layers (+ argmax for fp32)
         nl = cfg.dims[-2]
         bn = 256 if nl % 256 == 0 else (128 if nl % 128 == 0 else 64)
-        if cfg.slow_dtype == "bf16" and nl <= 1024 and nl // bn >= 2:
+        if cfg.slow_bf16 and nl <= 1024 and nl // bn >= 2:
             slow -= 1                                                         # the head runs inside the last hidden layer's launch
     else:
         slow = 1                                                              # the fused CNN kernel
@@ -212,7 +212,7 @@ def tensor_peak_for(peaks, clocks):
 def rooflines_for(cfg, n, k_esc, avg, peaks, clocks):
     in_b = cfg.N * 6 + 4 * ((cfg.N + 31) // 32)
     per_esc_in = cfg.P * (6 + cfg.H) + 4 * ((cfg.P + 31) // 32) + 4
-    esz = 2 if cfg.slow_dtype == "bf16" else 4
+    esz = 2 if cfg.slow_bf16 else 4
     Cf = cfg.C if cfg.kind == "rf" else 1
     tpeak, tkind = tensor_peak_for(peaks, clocks)
     work = {
@@ -224,11 +224,11 @@ def rooflines_for(cfg, n, k_esc, avg, peaks, clocks):
         "forest": ("alu", (n / 32.0) * cfg.T * (cfg.depth * FOREST_WAVEFRONTS_PER_VISIT - (4 if cfg.kind == "gbdt" and cfg.depth >= 2 and cfg.T <= 1024 else 0) +
                                                (4 * Cf * 32) / 128.0) / 1e9),
     }
-    if cfg.slow_dtype == "bf16":
+    if cfg.slow_bf16:
         work["gemm"] = ("tensor", k_esc * hidden_flops_per_row(cfg) / 1e12)
     else:
         work["gemm"] = ("fp32", k_esc * hidden_flops_per_row(cfg) / 1e12)
-    if cfg.slow == "mlp" and cfg.slow_dtype == "bf16" and avg.get("head", 0.0) > 0:
+    if cfg.slow == "mlp" and cfg.slow_bf16 and avg.get("head", 0.0) > 0:
         work["head"] = ("hbm", k_esc * (cfg.dims[-2] * esz + 4 * cfg.dims[-1]) / 1e9)       # reads the last hidden activations once
     out = {}
     for k, (bound, w) in work.items():
@@ -262,12 +262,12 @@ def oracle_stage_run(wl, threads):
     """The oracle's stages one after the other on the workload wl (tests/workload.make_workload), timed each."""
     import oracle
     cfg = wl["cfg"]
+    bf16 = cfg.slow_bf16
     t = [time.perf_counter()]
     feat = oracle.extract_features(wl["fast"], cfg.N, cfg.F, threads=threads); t.append(time.perf_counter())
     fo = oracle.forest_infer(wl["forest"], feat, threads=threads); t.append(time.perf_counter())
     r = oracle.route_lc(fo, wl["tau"]) if cfg.kind == "rf" else oracle.route_absmargin(fo, float(np.asarray(wl["tau"]).ravel()[0]))
     t.append(time.perf_counter())
-    bf16 = cfg.slow_dtype == "bf16"
     rows = oracle.wide_rows(0 if cfg.slow == "mlp" else 1, r["esc_ids"], wl["wide"], cfg.P, bf16, threads=threads)
     t.append(time.perf_counter())
     if cfg.slow == "mlp":
@@ -343,6 +343,7 @@ def bench_batch(cfg, n, args, env, with_e2e, with_cpu, cpu_budget_s):
     torch, sf, hz, ctx = env["torch"], env["sf"], env["hz"], env["ctx"]
     rank, world, local, dist = env["rank"], env["world"], env["local"], env["dist"]
     peaks = env["peaks"]
+    cfg.slow_bf16                                             # (refuses a type whose bytes and peaks are not counted here)
     wl = build_gpu_workload(cfg, n, rank, sf, hz, ctx, torch)
     cap = n
     rcfg = hz.route_cfg_for(cfg, hz.dev(wl["tau"], "cuda:%d" % local), cap)

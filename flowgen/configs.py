@@ -22,7 +22,7 @@ class Config:
     P: int                      # packets seen by the slow model
     H: int                      # header bytes per packet in the wide planes
     slow: str                   # "mlp" | "cnn"
-    slow_dtype: str             # "f32" | "bf16" | "mx4" (an MLP's hidden layers in 4 bits)
+    slow_dtype: str             # "f32" | "bf16" | "mx4" (an MLP's hidden layers in 4 bits: the library alone, see slow_bf16)
     dims: Tuple[int, ...]       # MLP layer widths, or () for the CNN
     q_percent: int              # Alg. 1 quantile (percent) used for tau; 0 = fixed rule
     n_val: int = 65536          # validation flows for threshold calibration
@@ -44,6 +44,13 @@ class Config:
     @property
     def D(self) -> int:
         return self.P * 16 if self.slow == "mlp" else self.P * 8
+
+    @property
+    def slow_bf16(self) -> bool:
+        """Slow model in bf16 or in fp32, for what knows these two: the oracle and the benchmark's bytes and peaks."""
+        if self.slow_dtype not in ("f32", "bf16"):
+            raise ValueError("slow_dtype %r: the oracle and the benchmark have a slow model in f32 and bf16 only" % (self.slow_dtype,))
+        return self.slow_dtype == "bf16"
 
     @property
     def n_slow_classes(self) -> int:

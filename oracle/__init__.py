@@ -301,10 +301,10 @@ def merge(label_fast, esc_ids, label_slow):
 
 def serve_batch(cfg, fast_pk, wide_pk, forest, slow_model, tau, threads=1):
     """All stages in order on one batch; returns every intermediate result."""
+    bf16 = cfg.slow_bf16
     feat = extract_features(fast_pk, cfg.N, cfg.F, threads=threads)
     fo = forest_infer(forest, feat, threads=threads)
     r = route_lc(fo, tau) if forest["kind"] == "rf" else route_absmargin(fo, float(np.asarray(tau).ravel()[0]))
-    bf16 = cfg.slow_dtype == "bf16"
     layout = 0 if cfg.slow == "mlp" else 1
     rows = wide_rows(layout, r["esc_ids"], wide_pk, cfg.P, bf16, threads=threads)
     if cfg.slow == "mlp":
@@ -320,6 +320,7 @@ def serve_batch3(cfg, fast_pk, wide_pk, fastest, fast, slow_model, tau1, tau2, t
     """Three-tier cascade (Sec. 3.1): the fastest model answers what it is sure of; the rest goes to the
     fast model on the SAME features; what that is still unsure of goes to the slow model, which sees more
     packets.  tau1 / tau2 are per-class thresholds (Sec. 3.2).  stage = 1, 2 or 3."""
+    bf16 = cfg.slow_bf16
     feat = extract_features(fast_pk, cfg.N, cfg.F, threads=threads)
     p1 = forest_infer(fastest, feat, threads=threads)
     r1 = route_lc(p1, tau1)
@@ -329,7 +330,6 @@ def serve_batch3(cfg, fast_pk, wide_pk, fastest, fast, slow_model, tau1, tau2, t
     r2 = route2(p2, tau2) if len(ids1) else {"esc_ids": np.zeros(0, np.uint32), "label": np.zeros(0, np.uint8),
                                                "n_esc": 0, "score": np.zeros(0, np.float32)}
     ids2 = ids1[r2["esc_ids"]]
-    bf16 = cfg.slow_dtype == "bf16"
     rows = wide_rows(0 if cfg.slow == "mlp" else 1, ids2, wide_pk, cfg.P, bf16, threads=threads)
     if cfg.slow == "mlp":
         logits, label_slow = mlp(slow_model, rows, bf16, threads=threads)

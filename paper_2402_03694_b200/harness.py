@@ -54,7 +54,7 @@ def bf16_bits_to_f32(t):
 def route_cfg_for(cfg, tau_dev, capacity, P_real=0):
     rule = sf.SF_LC_GT if cfg.kind == "rf" else sf.SF_ABSMARGIN_LT
     layout = sf.SF_MLP16 if cfg.slow == "mlp" else sf.SF_CNN8
-    dt = sf.SF_F32 if cfg.slow_dtype == "f32" else sf.SF_BF16
+    dt = {"f32": sf.SF_F32, "bf16": sf.SF_BF16, "mx4": sf.SF_BF16}[cfg.slow_dtype]
     return sf.make_route_cfg(rule, tau_dev, layout, dt, cfg.P, capacity, P_real)
 
 
