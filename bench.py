@@ -45,9 +45,9 @@ SM_COUNT, SM_MAX_MHZ = 148, 1965.0
 # of the method; node visits per second are printed beside it.
 FOREST_WAVEFRONTS_PER_VISIT = 3
 # DRAM bytes per launch measured with ncu for the dominant kernel class of a config, with the hash of the
-# kernel's source at capture time: the figure turns null as soon as the kernel changes
+# kernel's device code at capture time: the figure turns null as soon as the kernel changes
 # (profiles/gemm_traffic_config2_524288_flows.md).
-TRAFFIC_BY_SOURCE = {("gemm", 2): {"src_hash": "dfd4e62ca9f10121", "bytes_per_row_per_launch": 1468544768 / 3 / 123679}}
+TRAFFIC_BY_SOURCE = {("gemm", 2): {"src_hash": "2cb01f55791b0578", "bytes_per_row_per_launch": 1468544768 / 3 / 123679}}
 PAPER_CONTEXT = ("paper: over 48.5k new flows/s on a 16-core CPU server; 76.3% of flows inferred in under 16 ms "
                  "(other hardware, real traffic; not comparable)")
 
@@ -63,9 +63,21 @@ def load_peaks():
     return dict(FALLBACK_PEAKS), "fallback"
 
 
-def src_hash(name):
-    p = os.path.join(ROOT, "paper_2402_03694_b200", "csrc", name)
-    return hashlib.sha256(open(p, "rb").read()).hexdigest()[:16]
+CSRC = os.path.join(ROOT, "paper_2402_03694_b200", "csrc")
+
+
+def src_hash(name, csrc=CSRC):
+    """Hash of a kernel file's device code and of the tensor-core header's: what stands outside "// ---- host" sections, which reach up to
+    the next "// ---- kernels" line or the file's end.  Edits of host code leave it as it is."""
+    h = hashlib.sha256()
+    for f in (name, "tc_common.cuh"):
+        device = True
+        for line in open(os.path.join(csrc, f)):
+            if line.startswith(("// ---- host", "// ---- kernels")):
+                device = line.startswith("// ---- kernels")
+            elif device:
+                h.update(line.encode())
+    return h.hexdigest()[:16]
 
 
 class ClockSampler:

@@ -22,6 +22,7 @@
 // block records SF_ERR_DEVICE_TIMEOUT, lets its copies land, frees TMEM and returns.
 #include "tc_common.cuh"
 
+// ---- host: tensor maps ----------------------------------------------------------
 namespace sftc {
 
 int encode_tmap_2d(CUtensorMap* out, CUtensorMapDataType type, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch_bytes,
@@ -56,6 +57,7 @@ int encode_tmap_bf16_2d(CUtensorMap* out, const void* base, uint64_t rows, uint6
 
 }  // namespace sftc
 
+// ---- kernels ----------------------------------------------------------------------
 namespace {
 using namespace sftc;
 
@@ -563,6 +565,7 @@ gemm_bias_relu_bf16_kernel(const __grid_constant__ CUtensorMap tmA, const __grid
     }
 }
 
+// ---- host: launches ---------------------------------------------------------------
 // Can this device co-schedule two-CTA clusters of this kernel at all?  Asked once per kernel and device (the smem opt-in must
 // already be set); where the answer is no, or the query fails, the single-CTA kernel serves the layer instead.
 template <typename Kern>
