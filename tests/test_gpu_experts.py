@@ -534,3 +534,42 @@ def test_experts_in_a_row(env, n, E, k, K, N):
                     want[f] += want_w[f, j] * h
                     tol[f] += want_w[f, j] * ((K + 2) * 2.0 ** -23 * mass + (E + k + 12) * 2.0 ** -23 * h)
         assert (np.abs(num(y) - want) <= tol + 2.0 ** -24 * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n,m,k,E,D", [(90, 50, 2, 4, 24), (90, 0, 2, 4, 24), (700, 699, 3, 5, 17), (40, 1, 2, 3, 3000), (300, 211, 1, 8, 1024)])
+def test_device_count_values_of_the_flows_present(env, n, m, k, E, D, kind):
+    """With fewer flows than the arrays hold, the present ones get the sums of the definition and the others stay as they were."""
+    sf, ctx = env
+    rng = np.random.default_rng(n + m + D)
+    cnt = torch.tensor([m], dtype=torch.int32, device="cuda")
+    cap = n * k + E * 15
+    offsets, counts, flow, at = sort(sf, ctx, dev(some_ids(rng, n, k, E)), E, 16, cap, n_dev=cnt)
+    at[m:] = 0                                           # stale rows of flows that are not there
+    pairs, end = num(at)[:m], int(offsets[-1])
+    real = pairs >= 0
+    base, rows = laid(rng.normal(size=(cap, D)), kind, D, 0)
+    v = np.where(real[..., None], num(rows)[np.maximum(pairs, 0)], 0.0)
+    w = rng.random((n, k)).astype(np.float32)
+    ww = np.where(real, w[:m], 0.0).astype(float)
+    for weights, f in ((dev(w), ww), (None, real.astype(float))):
+        y = torch.full((n, D), 7.0, dtype=TYPES[kind], device="cuda")
+        sf.sf_expert_combine(ctx, rows, at, weights, y, n_dev=cnt)
+        want, mass = (f[..., None] * v).sum(1), np.abs(f[..., None] * v).sum(1)
+        slack = (k + 1) * 2.0 ** -24 * mass
+        assert (np.abs(num(y)[:m] - want) <= slack + HALF_STEP[kind] * (np.abs(want) + slack) + TINY[kind]).all() and (y[m:] == 7).all()
+        if weights is None:
+            dx = torch.full((n, D), 7.0, dtype=TYPES[kind], device="cuda")
+            sf.sf_expert_gather_backward(ctx, rows, at, dx, n_dev=cnt)
+            assert torch.equal(dx, y)                    # the same sum of the same rows in the same order
+    dy = laid(rng.normal(size=(n, D)), kind, D, 0)[1]
+    g = num(dy)[:m]
+    d_rows, d_w = torch.full((cap, D), 7.0, dtype=TYPES[kind], device="cuda"), torch.full((n, k), 7.0, device="cuda")
+    sf.sf_expert_combine_backward(ctx, dy, rows, at, dev(w), offsets, counts, d_rows, d_w, n_dev=cnt)
+    want = np.zeros((end, D))
+    f, j = np.nonzero(real)
+    want[pairs[f, j]] = ww[f, j, None] * g[f]
+    assert (np.abs(num(d_rows)[:end] - want) <= (2.0 ** -24 + HALF_STEP[kind] * (1 + 2.0 ** -24)) * np.abs(want) + TINY[kind]).all() and (d_rows[end:] == 7).all()
+    want_w = (g[:, None] * v).sum(-1)
+    assert (np.abs(num(d_w)[:m] - want_w) <= (D + 1) * 2.0 ** -24 * np.abs(g[:, None] * v).sum(-1)).all() and (d_w[m:] == 7).all()
+    sf.sf_ctx_poll(ctx)

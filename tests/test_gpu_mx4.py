@@ -536,3 +536,32 @@ def test_products_without_pairs_at_once_on_two_streams(env):
             for o in outs:
                 assert torch.equal(o, want)
     sf.sf_ctx_poll(ctx)
+
+
+@pytest.mark.parametrize("n,K,N", [(128, 160, 96), (300, 416, 200), (20011, 512, 512)])
+def test_rows_beside_a_nan_row_are_packed_as_if_alone(env, n, K, N):
+    """Packed outputs of the rows that share tiles (and scale words) with rows of NaN: the codes and scales of the definition, and the
+    bits that they get without the NaN."""
+    sf, ctx = env
+    rng = np.random.default_rng(n + K)
+    a, w, _, rw = operands(rng, n, N, K)
+    bad = np.unique(rng.integers(0, n, 5))
+    keep = np.setdiff1d(np.arange(n), bad)
+    b = a.copy()
+    b[bad, rng.integers(0, K, bad.size)] = np.nan
+    pw, bias = [dev(v) for v in pr.pack(w)], rng.normal(size=N).astype(np.float32)
+    got = []
+    for x in (a, b):
+        data = torch.full((n, -(-N // 32) * 16), 0xAA, dtype=torch.uint8, device="cuda")
+        scales = torch.full((sf.sf_mx4_sizes(n, N)[1],), 0x55, dtype=torch.uint8, device="cuda")
+        sf.sf_mx4_matmul(ctx, *[dev(v) for v in pr.pack(x)], *pw, K, data, bias=dev(bias), relu=True, out_scales=scales, N=N)
+        got.append((data.cpu().numpy(), scales.cpu().numpy()[pr.scale_index(n, N)]))
+    (data, scale), (data_nan, scale_nan) = got
+    blocks = -(-N // 32)
+    assert (scale_nan[bad, :blocks] == 255).all() and (scale_nan[:, blocks:] == 127).all()
+    assert np.array_equal(data_nan[keep], data[keep]) and np.array_equal(scale_nan[keep], scale[keep])
+    few = keep[:200]                                     # (rows of the first NaN's tile among them; laid out again as rows of their own)
+    laid = np.full(sf.sf_mx4_sizes(few.size, N)[1], 0x55, np.uint8)
+    laid[pr.scale_index(few.size, N)] = scale_nan[few]
+    check_packed_product(sf, ctx, torch.from_numpy(data_nan[few]), torch.from_numpy(laid), few.size, N, pr.rounded(a[few]), rw, bias)
+    sf.sf_ctx_poll(ctx)

@@ -191,3 +191,42 @@ def test_inside_the_streaming_table(env):
     sf.sf_table_destroy(table)
     sf.sf_slow_destroy(slow)
     sf.sf_forest_destroy(fh)
+
+
+def test_inside_the_three_tier_cascade(env):
+    """sf_serve_batch3 with a 4-bit slow model: stages, ids and the faster answers of the cascade, the slow answers of sf_slow_infer."""
+    sf, hz, ctx = env
+    n = 5000
+    cfg = dataclasses.replace(flowgen.get_config(2), n=n, slow_dtype="mx4")
+    wl = make_workload(cfg, n=n)
+    feat = oracle.extract_features(wl["fast"], cfg.N, cfg.F, threads=8)
+    fastest = flowgen.gen_forest(4242, "rf", 1, 7, cfg.F, cfg.C, feat)
+    rng = np.random.default_rng(2)
+    tau1 = rng.uniform(0.2, 0.7, cfg.C).astype(np.float32)
+    tau2 = (wl["tau"] + rng.uniform(-0.05, 0.05, cfg.C)).astype(np.float32)
+    ref = oracle.serve_batch3(dataclasses.replace(cfg, slow_dtype="bf16"), wl["fast"], wl["wide"], fastest, wl["forest"], wl["slow"], tau1, tau2, threads=8)
+    h1, h2, slow = hz.make_forest(ctx, fastest), hz.make_forest(ctx, wl["forest"]), hz.make_slow(ctx, cfg, wl["slow"])
+    fast_d, wide_d = hz.upload_packets(wl["fast"], with_hdr=False), hz.upload_packets(wl["wide"])
+    cfg1, cfg2 = hz.route_cfg_for(cfg, hz.dev(tau1), n), hz.route_cfg_for(cfg, hz.dev(tau2), n)
+    label, stage = torch.full((n,), 255, dtype=torch.uint8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    cnt = torch.zeros(2, dtype=torch.uint32, device="cuda")
+    sf.sf_ctx_poll(ctx, reset=True)
+    sf.sf_serve_batch3(ctx, h1, h2, slow, fast_d["struct"], cfg.N, cfg.F, wide_d["struct"], cfg1, cfg2, label, stage, cnt)
+    torch.cuda.synchronize()
+    c = sf.sf_ctx_poll(ctx, reset=True)
+    k1, k2 = [int(x) for x in cnt.cpu().numpy()]
+    assert (k1, k2) == (len(ref["ids1"]), len(ref["ids2"])) and 0 < k2 < k1 < n and c.n_slow_done == k2
+    st, lab = stage.cpu().numpy(), label.cpu().numpy()
+    assert np.array_equal(st, ref["stage"]) and np.array_equal(lab[st < 3], ref["label_final"][st < 3])
+    p = sf.sf_serve_batch_intermediates(ctx)
+    assert np.array_equal(hz.ptr_tensor(p["esc_ids"], (k2,), torch.uint32).cpu().numpy(), ref["ids2"])
+    logits = hz.ptr_tensor(p["logits"], (k2, 8), torch.float32).clone()
+    rows = torch.zeros(n, cfg.D, dtype=torch.bfloat16, device="cuda")
+    rows[:k2] = hz.ptr_tensor(p["rows"], (k2, cfg.D), torch.bfloat16)
+    assert np.array_equal(rows[:k2].float().cpu().numpy(), ref["rows"])
+    again, lab_slow = infer(sf, ctx, slow, rows, k2, 8)
+    assert torch.equal(logits, again[:k2])
+    assert np.array_equal(lab[ref["ids2"]], lab_slow[:k2].cpu().numpy())
+    sf.sf_slow_destroy(slow)
+    sf.sf_forest_destroy(h2)
+    sf.sf_forest_destroy(h1)
