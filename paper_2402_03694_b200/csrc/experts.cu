@@ -234,6 +234,9 @@ template <typename F> int by_experts(uint32_t E, F f) {
     return f(integral_constant<int, 32>(), integral_constant<int, 32>());
 }
 
+// ... with the weights' mode as a constant: as an argument of the kernel it made the gate 2 to 21 % and its gradient up to 58 % slower beyond 16
+// experts (400,000 x 64, k = 2, shares: 30 -> 36 and 35 -> 55 us; 50,000 x 1024, k = 2: 64 -> 69 and 63 -> 100 us), up to there the gate alone 30 %
+// (1,000,000 x 16, k = 2: 23 -> 30 us)
 template <typename F> int by_mode(int mode, F f) {
     if (mode == SF_GATE_SOFTMAX) return f(std::integral_constant<int, SF_GATE_SOFTMAX>());
     if (mode == SF_GATE_SOFTMAX_PICKED) return f(std::integral_constant<int, SF_GATE_SOFTMAX_PICKED>());
@@ -816,8 +819,9 @@ extern "C" int sf_expert_gate_backward(sf_ctx* ctx, const void* scores, int dtyp
             const bool al = fits(scores, ld, dtype, V) && fits(d_scores_out, ldd, dtype, V);
             return by_mode(mode, [&](auto m) {
                 constexpr int M = decltype(m)::value;
+                constexpr int P = L * V < 8 ? 4 : 8;       // (no more picks than experts)
                 auto kern = k <= 4 ? (al ? gate_backward_kernel<T, L, V, M, 4, true> : gate_backward_kernel<T, L, V, M, 4, false>) :
-                                     (al ? gate_backward_kernel<T, L, V, M, 8, true> : gate_backward_kernel<T, L, V, M, 8, false>);
+                                     (al ? gate_backward_kernel<T, L, V, M, P, true> : gate_backward_kernel<T, L, V, M, P, false>);
                 SF_CUDA(sf_launch_chained(kern, (n + kThreads / L - 1) / (kThreads / L), kThreads, 0, (cudaStream_t)stream, (const T*)scores, n_dev, n, E, ld, k, ids, d_weights,
                                           (T*)d_scores_out, ldd, ctx->d_state));
                 return SF_OK;
@@ -863,10 +867,10 @@ extern "C" int sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uin
     const uint32_t word = std::min({word_of(x, ldx, size), word_of(rows_out, ldr, size), word_of(nullptr, D, size)});
     auto go = [&](auto q) {
         typedef decltype(q) Q;
-        constexpr int U = sizeof(Q) == 16 ? 4 : 8;
+        constexpr int U = sizeof(Q) == 16 ? 4 : 8, S = sizeof(Q) == 16 ? 2 : 4;      // words a lane: wide rows, the most of several flows at a time
         const uint32_t per = sizeof(Q) / size, units = D / per, lanes = lanes_for(ctx, units, n), fb = flow_grid(ctx, n, lanes), zb = fill_blocks(ctx, E, units);
-        // (rows of up to four words a lane: several flows at a time)
-        auto kern = units <= lanes ? gather_kernel<Q, 1, 4> : (units <= 2 * lanes ? gather_kernel<Q, 2, 4> : (units <= 4 * lanes && sizeof(Q) < 16 ? gather_kernel<Q, 4, 2> : gather_kernel<Q, U, 1>));
+        // (rows of up to S words a lane: several flows at a time)
+        auto kern = units <= lanes ? gather_kernel<Q, 1, 4> : (units <= 2 * lanes ? gather_kernel<Q, 2, 4> : (units <= S * lanes ? gather_kernel<Q, S, 8 / S> : gather_kernel<Q, U, 1>));
         SF_CUDA(sf_launch_chained(kern, fb + E * zb, kThreads, 0, (cudaStream_t)stream, (const Q*)x, n_dev, n, units, ldx / per, k, row_of_pair, E,
                                   offsets, counts, capacity, (Q*)rows_out, ldr / per, lanes, fb, zb, ctx->d_state));
         return SF_OK;
