@@ -754,6 +754,10 @@ uint32_t flow_grid(const sf_ctx* ctx, uint32_t n, uint32_t lanes) {
     const uint32_t per = kThreads / lanes;
     return std::min<uint32_t>((n + per - 1) / per, (uint32_t)ctx->num_sms * 8);
 }
+// Do the flows give every thread of a full grid `times` of them?  Several flows at a time pay from about one and a half a thread on (combine, us: 60,000 x 64
+// bf16, k = 2: 10.1 with, 11.0 without; 30,000 x 64: 8.7 and 7.1): with fewer the lanes only wait for flows that are not there.
+constexpr double kSome = 1.5;
+bool many_flows(const sf_ctx* ctx, uint32_t n, uint32_t lanes, double times) { return (double)n * lanes >= (double)ctx->num_sms * 8 * kThreads * times; }
 // the largest word (16, 4 or sizeof(element) bytes) in which rows at p with pitch ld can be moved
 uint32_t word_of(const void* p, size_t ld, uint32_t size) {
     const size_t at = (uintptr_t)p | (ld * size);
@@ -869,8 +873,10 @@ extern "C" int sf_expert_gather(sf_ctx* ctx, const void* x, int dtype, const uin
         typedef decltype(q) Q;
         constexpr int U = sizeof(Q) == 16 ? 4 : 8, S = sizeof(Q) == 16 ? 2 : 4;      // words a lane: wide rows, the most of several flows at a time
         const uint32_t per = sizeof(Q) / size, units = D / per, lanes = lanes_for(ctx, units, n), fb = flow_grid(ctx, n, lanes), zb = fill_blocks(ctx, E, units);
-        // (rows of up to S words a lane: several flows at a time)
-        auto kern = units <= lanes ? gather_kernel<Q, 1, 4> : (units <= 2 * lanes ? gather_kernel<Q, 2, 4> : (units <= S * lanes ? gather_kernel<Q, S, 8 / S> : gather_kernel<Q, U, 1>));
+        // Rows of up to S words a lane: several flows at a time, 16-byte words where flows are many (30,000 x 64 bf16, k = 8: 8.5 us with, 6.6 without;
+        // 150,000 x 64, k = 2: 7.4 and 9.3); narrower words gain with few flows too (3,000 x 17 fp16, k = 2: 3.1 and 3.7).
+        const bool several = sizeof(Q) < 16 || many_flows(ctx, n, lanes, kSome);
+        auto kern = !several ? gather_kernel<Q, U, 1> : units <= lanes ? gather_kernel<Q, 1, 4> : (units <= 2 * lanes ? gather_kernel<Q, 2, 4> : (units <= S * lanes ? gather_kernel<Q, S, 8 / S> : gather_kernel<Q, U, 1>));
         SF_CUDA(sf_launch_chained(kern, fb + E * zb, kThreads, 0, (cudaStream_t)stream, (const Q*)x, n_dev, n, units, ldx / per, k, row_of_pair, E,
                                   offsets, counts, capacity, (Q*)rows_out, ldr / per, lanes, fb, zb, ctx->d_state));
         return SF_OK;
@@ -893,7 +899,12 @@ static int combine(sf_ctx* ctx, const void* rows, int dtype, uint32_t capacity, 
         return by_word<T>(word, [&](auto v) {
             constexpr int V = decltype(v)::value, U = V * sizeof(T) == 16 ? 4 : 8;
             const uint32_t units = D / V, lanes = lanes_for(ctx, units, n), grid = flow_grid(ctx, n, lanes);
-            auto kern = units > 2 * lanes ? combine_kernel<T, V, U> : (units > lanes ? combine_narrow_kernel<T, V, 2> : combine_narrow_kernel<T, V, 1>);
+            // Several flows at a time where flows are many (one word a lane, us: 150,000 x 64 bf16, k = 2: 12.5 with, 22 without).  Two words a lane: narrow words from the same number on (60,000 x 45 fp32, k = 2: 14.7 and 18.1), 16-byte words of fp32 later
+            // (100,000 x 256, k = 2: 64 and 66; 30,000 x 256: 19.7 and 17.5), of 16 bits never: the sums of four flows leave the registers (150,000 x
+            // 512 bf16, k = 2: 299 and 138).
+            constexpr int W = V * 2 <= 8 ? 2 : 1;
+            const bool one = units <= lanes && many_flows(ctx, n, lanes, kSome), two = W == 2 && units > lanes && units <= 2 * lanes && many_flows(ctx, n, lanes, V == 4 ? 8 : kSome);
+            auto kern = one ? combine_narrow_kernel<T, V, 1> : (two ? combine_narrow_kernel<T, V, W> : combine_kernel<T, V, U>);
             SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, (T*)y, ldy, lanes, ctx->d_state));
             return SF_OK;
         });
@@ -934,12 +945,18 @@ extern "C" int sf_expert_combine_backward(sf_ctx* ctx, const void* dy, int dtype
             constexpr int V = decltype(v)::value, U = V * sizeof(T) == 16 ? 1 : 4;
             const uint32_t units = D / V, lanes = lanes_for(ctx, units, n), fb = flow_grid(ctx, n, lanes), zb = fill_blocks(ctx, E, units), grid = fb + (d_rows_out ? E * zb : 0);
             if (grid == 0) return (int)SF_OK;
-            // where flows fill the machine one pair at a time with two words on their way (120,003 x 1024 bf16, k = 2: 202 us; one word 276, two
-            // pairs 226 to 239), else up to four pairs in flight
-            constexpr int U2 = U == 1 ? 2 : U;
-            auto kern = lanes <= 32 && units <= lanes ? combine_backward_narrow_kernel<T, V, 1> : lanes <= 32 && units <= 2 * lanes ? combine_backward_narrow_kernel<T, V, 2> :
-                        (uint64_t)n * lanes >= (uint64_t)ctx->num_sms * 2048 ? combine_backward_kernel<T, V, U2, 1> : (k == 1 ? combine_backward_kernel<T, V, U, 1> :
-                        (k == 2 ? combine_backward_kernel<T, V, U, 2> : combine_backward_kernel<T, V, U, 4>));
+            // Narrow words of rows that a warp holds: four flows at a time where flows are many, us: one word a lane (150,000 x 17 fp16, k = 2: 41 with, 60
+            // to 68 without; 3,000 x 17: 6.2 and 3.8), two words (100,000 x 45 fp32, k = 2: 44 and 54; 16-bit words later: 300,000 x 90 bf16 171 and 185,
+            // 100,000 x 90, k = 4: 117 and 110).  16-byte words one flow at a time: all pairs' loads of a flow on their way are enough
+            // (150,000 x 64 bf16, k = 2: 24 us, four flows at a time 28; 30,000 x 512, k = 8: 102 and 372).
+            // Else where flows fill the machine one pair at a time with two words on their way (120,003 x 1024 bf16, k = 2: 202 us; one word 276, two
+            // pairs 226 to 239) unless a lane has one 16-byte word alone (150,000 x 256 bf16, k = 2: 112 us, 90 with two pairs), and up to four
+            // pairs in flight elsewhere.
+            constexpr int U2 = U == 1 ? 2 : U, W = V * sizeof(T) < 16 ? 2 : 1;
+            const bool one = W == 2 && units <= lanes && many_flows(ctx, n, lanes, kSome), two = W == 2 && units > lanes && units <= 2 * lanes && many_flows(ctx, n, lanes, sizeof(T) == 4 ? kSome : 12);
+            const bool one_pair = (uint64_t)n * lanes >= (uint64_t)ctx->num_sms * 2048 && (W == 2 || units > 32);
+            auto kern = one_pair ? combine_backward_kernel<T, V, U2, 1> : (k == 1 ? combine_backward_kernel<T, V, U, 1> : (k == 2 ? combine_backward_kernel<T, V, U, 2> : combine_backward_kernel<T, V, U, 4>));
+            if constexpr (W == 2) { if (one) kern = combine_backward_narrow_kernel<T, V, 1>; if (two) kern = combine_backward_narrow_kernel<T, V, 2>; }
             SF_CUDA(sf_launch_chained(kern, grid, kThreads, 0, (cudaStream_t)stream, (const T*)dy, ldy, (const T*)rows, capacity, D, ldr, row_of_pair, weights, n_dev, n, k, E,
                                       offsets, counts, (T*)d_rows_out, ldd, d_weights_out, lanes, fb, zb, ctx->d_state));
             return (int)SF_OK;

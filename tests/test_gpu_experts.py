@@ -573,3 +573,59 @@ def test_device_count_values_of_the_flows_present(env, n, m, k, E, D, kind):
     want_w = (g[:, None] * v).sum(-1)
     assert (np.abs(num(d_w)[:m] - want_w) <= (D + 1) * 2.0 ** -24 * np.abs(g[:, None] * v).sum(-1)).all() and (d_w[m:] == 7).all()
     sf.sf_ctx_poll(ctx)
+
+
+@pytest.mark.parametrize("n,m,k,D,kind", [(20000, 19999, 3, 45, "fp32"), (152000, 151001, 2, 90, "bf16"), (152000, 152000, 1, 61, "fp16"), (76000, 75003, 2, 132, "fp32"),
+                                          (80000, 80000, 3, 64, "bf16"), (80000, 7, 2, 64, "fp16"), (30000, 29990, 5, 17, "fp16"), (310000, 310000, 2, 8, "fp32"),
+                                          (40000, 40000, 4, 512, "bf16"), (20001, 20001, 2, 256, "bf16"), (19000, 18999, 2, 33, "fp32"), (9000, 9000, 3, 50, "bf16")])
+def test_many_flows_of_narrow_rows(env, n, m, k, D, kind):
+    """Flows enough for several of them a thread, and just too few: gather, combine and their gradients against doubles on the device, m of n
+    flows present."""
+    sf, ctx = env
+    rng = np.random.default_rng(n + D)
+    E, T = 7, TYPES[kind]
+    cnt = torch.tensor([m], dtype=torch.int32, device="cuda")
+    cap = n * k + E * 15
+    offsets, counts, flow, at = sort(sf, ctx, dev(some_ids(rng, n, k, E)), E, 16, cap, n_dev=cnt)
+    end = int(offsets[-1])
+    at[m:] = 0                                           # stale rows of flows that are not there
+    pairs = at[:m].long()
+    real, where = pairs >= 0, pairs.clamp(min=0)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n)
+    new = lambda *s: torch.randn(*s, device="cuda", generator=gen)  # noqa: E731
+    x, dy, w = new(n, D).to(T), new(n, D).to(T), torch.rand(n, k, device="cuda", generator=gen)
+    rows = torch.full((cap, D), 7.0, dtype=T, device="cuda")
+    sf.sf_expert_gather(ctx, x, at, offsets, counts, rows, n_dev=cnt)
+    f = flow[:end].long()
+    assert torch.equal(rows[:end], torch.where((f >= 0)[:, None], x[f.clamp(min=0)], torch.zeros((), dtype=T, device="cuda"))) and (rows[end:] == 7).all()
+    rows = new(cap, D).to(T)
+    rows[end:] = float("nan")
+
+    def within(got, want, slack):
+        return bool(((got.double() - want).abs() <= slack + HALF_STEP[kind] * (want.abs() + slack) + TINY[kind]).all())
+    for weights in (w, None):
+        want, mass = torch.zeros(m, D, dtype=torch.float64, device="cuda"), torch.zeros(m, D, dtype=torch.float64, device="cuda")
+        for j in range(k):
+            t = torch.where(real[:, j, None], rows[where[:, j]].double() * (w[:m, j, None].double() if weights is not None else 1.0), 0.0)
+            want, mass = want + t, mass + t.abs()
+        y = torch.full((n, D), 7.0, dtype=T, device="cuda")
+        sf.sf_expert_combine(ctx, rows, at, weights, y, n_dev=cnt)
+        assert within(y[:m], want, (k + 1) * 2.0 ** -24 * mass) and (y[m:] == 7).all()
+    dx = torch.full((n, D), 7.0, dtype=T, device="cuda")
+    sf.sf_expert_gather_backward(ctx, rows, at, dx, n_dev=cnt)
+    assert torch.equal(dx, y)
+    d_rows, d_w = torch.full((cap, D), 7.0, dtype=T, device="cuda"), torch.full((n, k), 7.0, device="cuda")
+    sf.sf_expert_combine_backward(ctx, dy, rows, at, w, offsets, counts, d_rows, d_w, n_dev=cnt)
+    want = torch.zeros(end, D, dtype=torch.float64, device="cuda")
+    for j in range(k):
+        r = real[:, j]
+        want[pairs[r, j]] = w[:m][r, j, None].double() * dy[:m][r].double()
+        p = torch.where(r[:, None], rows[where[:, j]].double(), 0.0) * dy[:m].double()
+        assert bool(((d_w[:m, j].double() - p.sum(-1)).abs() <= (D + 1) * 2.0 ** -24 * p.abs().sum(-1)).all())
+    assert within(d_rows[:end], want, 2.0 ** -24 * want.abs()) and (d_rows[end:] == 7).all() and (d_w[m:] == 7).all()
+    only_w, only_rows = torch.zeros_like(d_w), torch.zeros_like(d_rows)
+    sf.sf_expert_combine_backward(ctx, dy, rows, at, w, offsets, counts, None, only_w, n_dev=cnt)
+    sf.sf_expert_combine_backward(ctx, dy, rows, at, w, offsets, counts, only_rows, None, n_dev=cnt)
+    assert torch.equal(only_w[:m], d_w[:m]) and torch.equal(only_rows[:end], d_rows[:end])
+    sf.sf_ctx_poll(ctx)
