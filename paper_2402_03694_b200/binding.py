@@ -377,8 +377,17 @@ def sf_serve_batch_intermediates(ctx):
 _raw_stream = None
 
 
+_TYPES = {}                       # element type -> dtype code of rows
+_SIZES = {}                       # element type -> bytes of a whole number, minus those of a floating one
+_U32 = 0xFFFFFFFF                 # the library's sizes; ctypes would cut a larger one to its low half
+
+
 def _device_of(ctx, where):
-    """The device on which every tensor of a call of `ctx` has to be."""
+    """The device on which every tensor of a call of `ctx` has to be (every call asks first: this knows torch's types from then on)."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16})
+        _SIZES.update({torch.int32: 4, torch.uint32: 4, torch.uint8: 1, torch.int8: 1, torch.bool: 1, torch.float32: -4})
     on = _ctx_device.get(getattr(ctx, "value", ctx))
     if on is None:
         raise SfError(SF_ERR_ARG, where)
@@ -402,15 +411,8 @@ def _arg(ok, where):
         raise SfError(SF_ERR_ARG, where)
 
 
-_TYPES = {}
-_U32 = 0xFFFFFFFF                 # the library's sizes; ctypes would cut a larger one to its low half
-
-
 def _rows(t, on, where):
     """(address, dtype code, rows, columns, row pitch) of a 2-D tensor on device `on` (in host memory: -1) whose rows are contiguous."""
-    if not _TYPES:
-        import torch
-        _TYPES.update({torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16})
     code, shape = _TYPES.get(t.dtype), t.shape
     if code is None or len(shape) != 2 or t.get_device() != on:
         raise SfError(SF_ERR_ARG, where)
@@ -418,7 +420,7 @@ def _rows(t, on, where):
     ld, s1 = t.stride()
     if n <= 1:
         ld = d
-    if ld < d or (d > 1 and s1 != 1) or n > _U32 or d > _U32:
+    if ld < d or (d > 1 and s1 != 1) or (n | d) > _U32:
         raise SfError(SF_ERR_ARG, where)
     return t.data_ptr(), code, n, d, ld
 
@@ -427,14 +429,14 @@ def _flat(t, count, size, on, where, real=False):
     """Address of a contiguous tensor on device `on` of at least `count` whole (real: floating) numbers of `size` bytes; None stays None."""
     if t is None:
         return None
-    if t.get_device() != on or t.itemsize != size or t.nbytes < count * size or t.is_floating_point() != real or not t.is_contiguous():
+    if t.get_device() != on or _SIZES.get(t.dtype) != (-size if real else size) or t.numel() < count or not t.is_contiguous():
         raise SfError(SF_ERR_ARG, where)
     return t.data_ptr()
 
 
 def _whole(t, shape, on, where, real=False):
     """Address of a contiguous tensor on device `on` of this shape of 4-byte whole (real: floating) numbers."""
-    if t.get_device() != on or t.itemsize != 4 or t.shape != shape or t.is_floating_point() != real or not t.is_contiguous():
+    if t.get_device() != on or _SIZES.get(t.dtype) != (-4 if real else 4) or t.shape != shape or not t.is_contiguous():
         raise SfError(SF_ERR_ARG, where)
     return t.data_ptr()
 
