@@ -595,12 +595,12 @@ def sf_expert_combine(ctx, rows, row_of_pair, weights, y_out, n_dev=None, stream
 
 
 def sf_expert_combine_backward(ctx, dy, rows, row_of_pair, weights, offsets, counts, d_rows_out, d_weights_out, n_dev=None, stream=None):
-    """Either output may be None."""
+    """Either output may be None; without d_rows_out offsets and counts are not needed and may be None too."""
     w = "sf_expert_combine_backward"
     on = _device_of(ctx, w)
     p, dt, cap, D, ldr, at, q, n, k, ldy = _pairs_of(rows, row_of_pair, dy, on, w)
     g = None if weights is None else _whole(weights, (n, k), on, w, True)
-    E = counts.numel()
+    E = 1 if counts is None and d_rows_out is None else counts.numel()
     _arg(E <= _U32, w)
     r, ldd = None, 0
     if d_rows_out is not None:

@@ -170,3 +170,14 @@ def test_sizes_past_32_bits_are_refused(stub, call):
     with pytest.raises(sf.SfError) as e:
         call(ctx)
     assert e.value.status == sf.SF_ERR_ARG and lib.calls == []
+
+
+def test_weights_gradient_alone_needs_no_segments(stub):
+    """Offsets and counts name the rows that only fill a segment of d_rows: without d_rows a call may leave them out."""
+    lib, ctx = stub
+    dy, rows, at, d_w = (OnDevice(t) for t in (f32(N, D), f32(CAP, D), i32(N, 2), f32(N, 2)))
+    sf.sf_expert_combine_backward(ctx, dy, rows, at, None, None, None, None, d_w, stream=7)
+    assert lib.calls == ["sf_expert_combine_backward"]
+    with pytest.raises((sf.SfError, AttributeError)):
+        sf.sf_expert_combine_backward(ctx, dy, rows, at, None, None, None, rows, d_w, stream=7)
+    assert len(lib.calls) == 1

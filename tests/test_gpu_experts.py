@@ -629,3 +629,14 @@ def test_many_flows_of_narrow_rows(env, n, m, k, D, kind):
     sf.sf_expert_combine_backward(ctx, dy, rows, at, w, offsets, counts, only_rows, None, n_dev=cnt)
     assert torch.equal(only_w[:m], d_w[:m]) and torch.equal(only_rows[:end], d_rows[:end])
     sf.sf_ctx_poll(ctx)
+
+
+def test_weights_gradient_alone_without_segments(env):
+    sf, ctx = env
+    rng = np.random.default_rng(8)
+    (offsets, counts, flow, at), cap = plan(sf, ctx, rng, 300, 2, 5, 16)
+    rows, dy = torch.randn(cap, 40, device="cuda"), torch.randn(300, 40, device="cuda")
+    with_, without = torch.zeros(300, 2, device="cuda"), torch.zeros(300, 2, device="cuda")
+    sf.sf_expert_combine_backward(ctx, dy, rows, at, None, offsets, counts, None, with_)
+    sf.sf_expert_combine_backward(ctx, dy, rows, at, None, None, None, None, without)
+    assert torch.equal(with_, without) and (with_ != 0).any()
