@@ -353,8 +353,9 @@ int  sf_mx4_matmul_experts(sf_ctx* ctx, const uint8_t* a, const uint8_t* a_scale
 
 /* ---- several slow models: experts -------------------------------------------- */
 /* sf_route assigns a flow to THE slow model; these calls assign it to k of E experts: gate -> sort -> gather (or sf_mx4_quantise
- * with flow_of_row) -> the experts' layers on their rows (sf_mx4_matmul_experts) -> combine, and the gradients of each for
- * training.  n = flows the arrays hold; n_dev (nullable, device) = flows present (a larger count is clamped and records
+ * with flow_of_row) -> the experts' layers on their rows (sf_mx4_matmul_experts) -> combine, and the gradients of gate, gather
+ * and combine for training (the 4-bit product has none: a layer that is trained runs in the caller's arithmetic between gather
+ * and combine).  n = flows the arrays hold; n_dev (nullable, device) = flows present (a larger count is clamped and records
  * SF_ERR_CAPACITY); what belongs to flows at or beyond it is left as it was.  E <= SF_MAX_EXPERTS, k <= E (where E is
  * given), n*k < 2^31, D <= SF_EXPERT_MAX_D.  None of them uses the context's workspace, so they may be captured in graphs and run on several streams of
  * one context at once.  All sums are fp32 in a fixed order; results do not vary from run to run.

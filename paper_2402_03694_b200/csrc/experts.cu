@@ -120,7 +120,7 @@ gate_kernel(const T* __restrict__ scores, const uint32_t* __restrict__ n_dev, ui
 
 // With p the weights' softmax (over all experts, or over the picked ones) and g the weights' gradient at the picked experts:
 // d_s = p (g - sum g p); for shares d_s = (g - sum g w) / sum s at the picked experts.  Away from the picked experts that is
-// -p sum g p, or nothing, so a lane writes its part of the row without looking at the picks, and then the picked ones that are its own,
+// -p sum g p, or nothing (p by a reciprocal, rounded once more than the gate's quotient: 2^-24 of it), so a lane writes its part of the row without looking at the picks, and then the picked ones that are its own,
 // whose scores it reads again by their ids: comparing every id with every expert in registers took twice as long (61 us at
 // 1,000,000 x 16, k = 2).  P picks are fetched at a time (4 or 8).
 template <typename T, int LPR, int V, int mode, int P, bool ALIGNED>

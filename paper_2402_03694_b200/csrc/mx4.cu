@@ -183,7 +183,8 @@ mx4_quantise_any_kernel(const T* __restrict__ x, uint32_t n_src, uint32_t K, siz
 }
 
 // data, scales -> out[rows][ld].  The same split the other way round: 16 values a lane, whole 32-byte sectors where rows are on
-// 32-byte boundaries.  Bound: HBM writes (this card writes 3.9 TB/s where it copies 6.5).
+// 32-byte boundaries.  Bound: HBM writes (240,001 x 2048 bf16: 231 us, 4.3 TB/s written beside 1.2 read; a kernel that only fills memory reaches 3.9
+// on this card, where a copy moves 6.5).
 template <typename T>
 __global__ void __launch_bounds__(kQThreads)
 mx4_unpack_kernel(const uint8_t* __restrict__ data, const uint8_t* __restrict__ scales, const uint32_t* __restrict__ n_rows_dev,
