@@ -953,7 +953,8 @@ extern "C" int sf_expert_combine_backward(sf_ctx* ctx, const void* dy, int dtype
             // pairs 226 to 239) unless a lane has one 16-byte word alone (150,000 x 256 bf16, k = 2: 112 us, 90 with two pairs), and up to four
             // pairs in flight elsewhere.
             constexpr int U2 = U == 1 ? 2 : U, W = V * sizeof(T) < 16 ? 2 : 1;
-            const bool one = W == 2 && units <= lanes && many_flows(ctx, n, lanes, kSome), two = W == 2 && units > lanes && units <= 2 * lanes && many_flows(ctx, n, lanes, sizeof(T) == 4 ? kSome : 12);
+            const bool warp = W == 2 && lanes <= 32;       // (the narrow kernel's sums stay within a warp)
+            const bool one = warp && units <= lanes && many_flows(ctx, n, lanes, kSome), two = warp && units > lanes && units <= 2 * lanes && many_flows(ctx, n, lanes, sizeof(T) == 4 ? kSome : 12);
             const bool one_pair = (uint64_t)n * lanes >= (uint64_t)ctx->num_sms * 2048 && (W == 2 || units > 32);
             auto kern = one_pair ? combine_backward_kernel<T, V, U2, 1> : (k == 1 ? combine_backward_kernel<T, V, U, 1> : (k == 2 ? combine_backward_kernel<T, V, U, 2> : combine_backward_kernel<T, V, U, 4>));
             if constexpr (W == 2) { if (one) kern = combine_backward_narrow_kernel<T, V, 1>; if (two) kern = combine_backward_narrow_kernel<T, V, 2>; }
