@@ -71,6 +71,10 @@ extern "C" {
 #define SF_GATE_SOFTMAX_PICKED 1   /* ... over the picked scores only */
 #define SF_GATE_SHARE          2   /* ... its share of the picked scores' sum (scores = class probabilities of the fast model) */
 #define SF_MAX_EXPERTS  1024
+#define SF_ACT_NONE     0
+#define SF_ACT_SILU     1          /* x * sigmoid(x) */
+#define SF_SCAN_MAX_STATES 64      /* states of a channel that sf_seq_scan takes */
+#define SF_MAX_TOP      32         /* alternatives that sf_label_logprobs gives */
 #define SF_EXPERT_MAX_D 16777216u  /* widest row that the expert calls move */
 
 /* |margin| threshold equivalent to |sigmoid(margin) - 0.5| < 0.2: fp32(ln(0.7/0.3)) */
@@ -400,6 +404,95 @@ int  sf_expert_combine_backward(sf_ctx* ctx, const void* dy, int dtype, size_t l
                                 size_t ldr, const int32_t* row_of_pair, const float* weights, const uint32_t* n_dev, uint32_t n,
                                 uint32_t k, uint32_t E, const uint32_t* offsets, const uint32_t* counts, void* d_rows_out,
                                 size_t ldd, float* d_weights_out, void* stream);
+
+/* ---- sequences of rows ---------------------------------------------------------- */
+/* Layers of a slow model that reads a flow's packets one after the other and carries a state from row to row: a window of packets
+ * costs its length, and the next packet of a flow (Sec. 3.1: the slow model sees more packets of the same flow) costs one row.
+ * A sequence is a run of rows: sequence s has the rows offsets[s] .. offsets[s+1] - 1 (uint32[n_seq + 1], rising), of which the first
+ * counts[s] are there (uint32[n_seq], nullable: all of them), so a batch is either packed (offsets alone) or planes of P rows a
+ * flow (offsets s * P, counts = n_valid).  Outputs of rows that belong to no sequence, or lie behind a sequence's count, are left as they were.
+ * max_len (host): rows of the longest sequence.  States are kept in pools of n_slots states; slots[s] (int32[n_seq], nullable: s)
+ * names the sequence's state; with an id outside 0..n_slots-1 a sequence starts from zeros and its state is dropped.  No slot may be named twice in
+ * a call that writes states (which of the sequences' states it then holds is not defined).  A call may read and write the same pool.
+ * On the device: offsets that fall give an empty sequence and record SF_ERR_ARG; rows beyond the arrays, counts beyond the offsets and
+ * sequences longer than max_len are cut and record SF_ERR_CAPACITY.
+ * Rows are SF_F32, SF_BF16 or SF_F16 with pitches in elements; filters, biases, A, states of the scan and their gradients are fp32,
+ * and so are all sums.  Outputs must not overlap inputs (but for the pools).  None of these calls uses the context's workspace,
+ * none allocates: they may be captured in graphs, and run on several streams of one context at once if their workspaces are different ones.
+ * Results do not vary from run to run. */
+typedef struct {
+    const uint32_t* offsets;
+    const uint32_t* counts;
+    const int32_t*  slots;
+    uint32_t n_seq, max_len;
+} sf_sequences;
+
+/* Short causal convolution, one filter of W taps (1..8) a channel: y_t[d] = act(bias[d] + sum_k w[d][k] x_{t-W+1+k}[d]) over the rows of each sequence, act
+ * SF_ACT_NONE or SF_ACT_SILU, w fp32[D][W], bias fp32[D] (nullable).  Rows before the first one come from the state (type of x, [n_slots][W-1][D],
+ * oldest row first; state_in NULL: zeros); state_out (nullable) gets the last W - 1 rows.  x: `rows` rows of D with pitch ldx. */
+int  sf_seq_conv(sf_ctx* ctx, const sf_sequences* seq, const void* x, int dtype, uint32_t rows, uint32_t D, size_t ldx, const float* w,
+                 const float* bias, uint32_t W, int act, const void* state_in, void* state_out, uint32_t n_slots, void* y_out, size_t ldy,
+                 void* stream);
+/* Its gradients: dx_out, dw_out fp32[D][W], dbias_out fp32[D], d_state_in_out (type of x, like the state; slots that no sequence names are left
+ * as they were), each nullable, from dy and, where the states went on to be used, d_state (gradient of the states after the call, nullable).
+ * state_in is the state BEFORE the forward call (a caller that let the call overwrite its pool keeps a copy).  workspace:
+ * sf_seq_conv_backward_workspace bytes (needed for dw_out and dbias_out only). */
+int  sf_seq_conv_backward_workspace(uint32_t n_seq, uint32_t max_len, uint32_t D, uint32_t W, size_t* bytes_out);
+int  sf_seq_conv_backward(sf_ctx* ctx, const sf_sequences* seq, const void* x, int dtype, uint32_t rows, uint32_t D, size_t ldx, const float* w,
+                          const float* bias, uint32_t W, int act, const void* state_in, const void* dy, size_t lddy, const void* d_state,
+                          uint32_t n_slots, void* dx_out, size_t lddx, float* dw_out, float* dbias_out, void* d_state_in_out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Selective state space scan.  Channel d belongs to group g = d / (D / G); its N <= SF_SCAN_MAX_STATES states follow
+ *   delta_t = softplus(delta_in_t[d] + delta_bias[d]) (softplus 0: the sum itself)
+ *   h_t[n] = exp(delta_t A[d][n]) h_{t-1}[n] + delta_t u_t[d] B_t[g][n]
+ *   y_t[d] = (sum_n C_t[g][n] h_t[n] + D_skip[d] u_t[d]) * z_t[d] sigmoid(z_t[d])
+ * u, delta, z: rows of D; B, C: rows of G * N; all of type dtype.  A fp32[D][N]; D_skip, delta_bias fp32[D] and z may be NULL (no such term). */
+typedef struct {
+    const void* u; const void* delta; const void* B; const void* C; const void* z;
+    size_t ldu, ld_delta, ldb, ldc, ldz;
+    const float* A; const float* D_skip; const float* delta_bias;
+    uint32_t D, N, G;
+    int dtype, softplus;
+} sf_scan_rows;
+/* state_in, state_out: fp32[n_slots][D][N], nullable (zeros; dropped).  starts_out (nullable): what the backward pass needs,
+ * sf_seq_scan_starts floats.  workspace: sf_seq_scan_workspace bytes (0 where every sequence is scanned in one go; few long ones are
+ * cut into parts that run side by side).  Sequences of one row (max_len 1) are the step of a stream: the state is read and written once. */
+int  sf_seq_scan_workspace(uint32_t n_seq, uint32_t max_len, uint32_t rows, uint32_t D, uint32_t N, uint32_t G, int backward, size_t* bytes_out);
+int  sf_seq_scan_starts(uint32_t n_seq, uint32_t rows, uint32_t D, uint32_t N, size_t* floats_out);
+int  sf_seq_scan(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_rows* in, uint32_t rows, const float* state_in, float* state_out,
+                 uint32_t n_slots, float* starts_out, void* y_out, size_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+/* Gradients, each nullable: of rows (type dtype) and of parameters (fp32, summed over all rows). */
+typedef struct {
+    void* du; void* d_delta; void* dB; void* dC; void* dz;
+    size_t lddu, ldd_delta, lddb, lddc, lddz;
+    float* dA; float* dD_skip; float* d_delta_bias;
+} sf_scan_grads;
+/* in and seq as in the forward call, starts what it wrote; d_state (nullable): gradient of the states after the call; d_state_in_out (nullable):
+ * that of the states before it (slots that no sequence names are left as they were).  workspace: sf_seq_scan_workspace bytes with backward = 1. */
+int  sf_seq_scan_backward(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_rows* in, uint32_t rows, const void* dy, size_t lddy,
+                          const float* starts, const float* d_state, float* d_state_in_out, uint32_t n_slots, const sf_scan_grads* out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- scores of answers -------------------------------------------------------------- */
+/* What sf_route's scores are to the fast model's class probabilities, for rows of any logits (a slow model's, a training step's): with
+ * x = scale * logits (scale > 0, 1 / temperature) and lse = ln sum_i exp(x_i), in one pass over rows of V entries (pitch ld)
+ *   logprob_out[r] = x[labels[r]] - lse         (labels int32[n]; a label outside 0..V-1 stands for none: 0)
+ *   entropy_out[r] = -sum_i p_i ln p_i          (the score of Sec. 3.2; goes into sf_universal_thresholds_dev as it is)
+ *   lse_out[r]
+ *   top_ids_out int32[n][k], top_logprobs_out fp32[n][k]: the k <= SF_MAX_TOP largest entries, largest first, ties to the lowest index;
+ *                                               1 - exp of the first is the least-confidence score.
+ * each nullable.  An entry of -infinity is masked: it adds nothing, is never picked (id -1, log probability -infinity where fewer than k are left), and
+ * as a label has log probability -infinity.  A row with nothing but masked entries has lse -infinity and entropy 0.  A NaN or +infinity
+ * makes the row's lse, entropy and log probabilities NaN; NaN is never picked.  n_dev as in the expert calls.  No workspace. */
+int  sf_label_logprobs(sf_ctx* ctx, const void* logits, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t V, size_t ld, float scale,
+                       const int32_t* labels, float* logprob_out, float* entropy_out, float* lse_out, uint32_t k, int32_t* top_ids_out,
+                       float* top_logprobs_out, void* stream);
+/* Gradient of the logits (d_logits_out[n][ldd], their type) from those of the outputs, each nullable: d_logprob fp32[n], d_entropy fp32[n] (needs
+ * entropy), d_top_logprobs fp32[n][k] (needs top_ids).  lse, entropy and top_ids are what the forward call gave.  Masked entries get 0. */
+int  sf_label_logprobs_backward(sf_ctx* ctx, const void* logits, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t V, size_t ld, float scale,
+                                const int32_t* labels, const float* lse, const float* d_logprob, const float* entropy, const float* d_entropy,
+                                uint32_t k, const int32_t* top_ids, const float* d_top_logprobs, void* d_logits_out, size_t ldd, void* stream);
 
 /* ---- S1..S5: the whole cascade on one batch -------------------------------- */
 /* Features of fast_ctx (first N packets) -> fast model -> assignment -> wide rows

@@ -24,6 +24,8 @@ SF_MLP16, SF_CNN8 = 0, 1
 SF_F32, SF_BF16, SF_F16, SF_MX4 = 0, 1, 2, 3
 SF_GATE_SOFTMAX, SF_GATE_SOFTMAX_PICKED, SF_GATE_SHARE = 0, 1, 2
 SF_MAX_EXPERTS = 1024
+SF_ACT_NONE, SF_ACT_SILU = 0, 1
+SF_SCAN_MAX_STATES, SF_MAX_TOP = 64, 32
 SF_TAU_MARGIN_DEFAULT = float.fromhex("0x1.b1d106p-1")
 
 
@@ -51,6 +53,21 @@ class sf_packets(C.Structure):
 class sf_route_cfg(C.Structure):
     _fields_ = [("rule", C.c_int), ("tau", C.c_void_p), ("wide_layout", C.c_int), ("row_dtype", C.c_int),
                 ("P", C.c_uint32), ("P_real", C.c_uint32), ("capacity", C.c_uint32)]
+
+
+class sf_sequences(C.Structure):
+    _fields_ = [("offsets", C.c_void_p), ("counts", C.c_void_p), ("slots", C.c_void_p), ("n_seq", C.c_uint32), ("max_len", C.c_uint32)]
+
+
+class sf_scan_rows(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("u", "delta", "B", "C", "z")] + [(k, C.c_size_t) for k in ("ldu", "ld_delta", "ldb", "ldc", "ldz")] + \
+               [(k, C.c_void_p) for k in ("A", "D_skip", "delta_bias")] + [(k, C.c_uint32) for k in ("D", "N", "G")] + \
+               [("dtype", C.c_int), ("softplus", C.c_int)]
+
+
+class sf_scan_grads(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("du", "d_delta", "dB", "dC", "dz")] + [(k, C.c_size_t) for k in ("lddu", "ldd_delta", "lddb", "lddc", "lddz")] + \
+               [(k, C.c_void_p) for k in ("dA", "dD_skip", "d_delta_bias")]
 
 
 class sf_pkt_batch(C.Structure):
@@ -90,6 +107,8 @@ EXPORTS = [
     "sf_mx4_sizes", "sf_mx4_quantise", "sf_mx4_unpack", "sf_mx4_matmul", "sf_mx4_matmul_experts",
     "sf_expert_gate", "sf_expert_gate_backward", "sf_expert_sort_workspace", "sf_expert_sort", "sf_expert_gather",
     "sf_expert_gather_backward", "sf_expert_combine", "sf_expert_combine_backward",
+    "sf_seq_conv", "sf_seq_conv_backward_workspace", "sf_seq_conv_backward", "sf_seq_scan_workspace", "sf_seq_scan_starts", "sf_seq_scan",
+    "sf_seq_scan_backward", "sf_label_logprobs", "sf_label_logprobs_backward",
     "sf_table_create", "sf_table_destroy", "sf_table_ingest", "sf_table_ingest_host", "sf_table_lookup", "sf_table_set_time", "sf_table_sweep", "sf_table_set_pipelined", "sf_table_flush",
 ]
 
@@ -148,6 +167,16 @@ def _lib():
         L.sf_expert_gather_backward.argtypes = [V, V, I, U32, U32, Z, V, V, U32, U32, V, Z, V]
         L.sf_expert_combine.argtypes = [V, V, I, U32, U32, Z, V, V, V, U32, U32, V, Z, V]
         L.sf_expert_combine_backward.argtypes = [V, V, I, Z, V, U32, U32, Z, V, V, V, U32, U32, U32, V, V, V, Z, V, V]
+        Q = C.POINTER(sf_sequences)
+        L.sf_seq_conv.argtypes = [V, Q, V, I, U32, U32, Z, V, V, U32, I, V, V, U32, V, Z, V]
+        L.sf_seq_conv_backward_workspace.argtypes = [U32, U32, U32, U32, C.POINTER(Z)]
+        L.sf_seq_conv_backward.argtypes = [V, Q, V, I, U32, U32, Z, V, V, U32, I, V, V, Z, V, U32, V, Z, V, V, V, V, Z, V]
+        L.sf_seq_scan_workspace.argtypes = [U32, U32, U32, U32, U32, U32, I, C.POINTER(Z)]
+        L.sf_seq_scan_starts.argtypes = [U32, U32, U32, U32, C.POINTER(Z)]
+        L.sf_seq_scan.argtypes = [V, Q, C.POINTER(sf_scan_rows), U32, V, V, U32, V, V, Z, V, Z, V]
+        L.sf_seq_scan_backward.argtypes = [V, Q, C.POINTER(sf_scan_rows), U32, V, Z, V, V, V, U32, C.POINTER(sf_scan_grads), V, Z, V]
+        L.sf_label_logprobs.argtypes = [V, V, I, V, U32, U32, Z, C.c_float, V, V, V, V, U32, V, V, V]
+        L.sf_label_logprobs_backward.argtypes = [V, V, I, V, U32, U32, Z, C.c_float, V, V, V, V, V, U32, V, V, V, Z, V]
         L.sf_table_create.argtypes = [V, U32, U32, U32, U32, C.POINTER(V)]
         L.sf_table_ingest.argtypes = [V, V, C.POINTER(sf_pkt_batch), V, U32, V, C.POINTER(sf_route_cfg), V, V]
         L.sf_table_ingest_host.argtypes = L.sf_table_ingest.argtypes
@@ -382,12 +411,16 @@ _SIZES = {}                       # element type -> bytes of a whole number, min
 _U32 = 0xFFFFFFFF                 # the library's sizes; ctypes would cut a larger one to its low half
 
 
+def _types():
+    import torch
+    _TYPES.update({torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16})
+    _SIZES.update({torch.int32: 4, torch.uint32: 4, torch.uint8: 1, torch.int8: 1, torch.bool: 1, torch.float32: -4})
+
+
 def _device_of(ctx, where):
     """The device on which every tensor of a call of `ctx` has to be (every call asks first: this knows torch's types from then on)."""
     if not _TYPES:
-        import torch
-        _TYPES.update({torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16})
-        _SIZES.update({torch.int32: 4, torch.uint32: 4, torch.uint8: 1, torch.int8: 1, torch.bool: 1, torch.float32: -4})
+        _types()
     on = _ctx_device.get(getattr(ctx, "value", ctx))
     if on is None:
         raise SfError(SF_ERR_ARG, where)
@@ -609,6 +642,211 @@ def sf_expert_combine_backward(ctx, dy, rows, row_of_pair, weights, offsets, cou
     dw = None if d_weights_out is None else _whole(d_weights_out, (n, k), on, w, True)
     _check(_lib().sf_expert_combine_backward(ctx, q, dt, ldy, p, cap, D, ldr, at, g, _flat(n_dev, 1, 4, on, w), n, k, E,
                                              _flat(offsets, E + 1, 4, on, w), _flat(counts, E, 4, on, w), r, ldd, dw, _stream_on(on, stream)), w)
+
+
+# ---- sequences of rows, scores of answers: device tensors in, as above --------------------------------------------------------
+def make_sequences(offsets, max_len, counts=None, slots=None):
+    """sf_sequences from device tensors: offsets int32 / uint32 [n_seq + 1], counts [n_seq] or None, slots int32 [n_seq] or None; max_len a number."""
+    w = "make_sequences"
+    on = offsets.get_device()
+    _arg(on >= 0 and offsets.numel() >= 1 and 1 <= max_len <= _U32, w)
+    if not _SIZES:
+        _types()
+    q = sf_sequences()
+    n = offsets.numel() - 1
+    _arg(n <= _U32, w)
+    q.offsets, q.counts, q.slots = _flat(offsets, n + 1, 4, on, w), _flat(counts, n, 4, on, w), _flat(slots, n, 4, on, w)
+    q.n_seq, q.max_len = n, max_len
+    q._keep, q._on = (offsets, counts, slots), on
+    return q
+
+
+def _of(t, code, n, d, on, w):
+    """(address, pitch) of rows of the same type and shape; None stays None."""
+    if t is None:
+        return None, 0
+    p, c, m, e, ld = _rows(t, on, w)
+    if (c, m, e) != (code, n, d):
+        raise SfError(SF_ERR_ARG, w)
+    return p, ld
+
+
+def _reals(t, shape, on, w):
+    return None if t is None else _whole(t, shape, on, w, True)
+
+
+def _pool(t, shape, like, on, w):
+    """(address, states) of a pool of states [slots][..shape] of type `like` (None: no pool)."""
+    if t is None:
+        return None, None
+    if t.get_device() != on or t.dtype != like or t.dim() != 1 + len(shape) or tuple(t.shape[1:]) != shape or not t.is_contiguous() or t.shape[0] > _U32:
+        raise SfError(SF_ERR_ARG, w)
+    return t.data_ptr(), t.shape[0]
+
+
+def _slots_of(w, *counts):
+    """The number of states of a call's pools, which all have as many (none: 0)."""
+    have = {c for c in counts if c is not None}
+    _arg(len(have) <= 1, w)
+    return have.pop() if have else 0
+
+
+def _bytes(t, on, w):
+    if t is None:
+        return None, 0
+    _arg(t.get_device() == on and t.is_contiguous(), w)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def sf_seq_conv(ctx, seq, x, w, y_out, bias=None, act=SF_ACT_NONE, state_in=None, state_out=None, stream=None):
+    """y_out [rows][D] from x [rows][D] by filters w float32 [D][W]; states [slots][W - 1][D] of x's type."""
+    s = "sf_seq_conv"
+    on = _device_of(ctx, s)
+    p, dt, n, D, ld = _rows(x, on, s)
+    q, ldy = _of(y_out, dt, n, D, on, s)
+    _arg(w.dim() == 2 and w.shape[0] == D and seq._on == on, s)
+    W = w.shape[1]
+    si, m1 = _pool(state_in, (W - 1, D), x.dtype, on, s)
+    so, m2 = _pool(state_out, (W - 1, D), x.dtype, on, s)
+    _check(_lib().sf_seq_conv(ctx, seq, p, dt, n, D, ld, _whole(w, (D, W), on, s, True), _reals(bias, (D,), on, s), W, act, si, so,
+                              _slots_of(s, m1, m2), q, ldy, _stream_on(on, stream)), s)
+
+
+def sf_seq_conv_backward_workspace(n_seq, max_len, D, W):
+    """Bytes of device scratch that the gradients of the filters need."""
+    b = C.c_size_t()
+    s = "sf_seq_conv_backward_workspace"
+    _arg(0 <= n_seq <= _U32 and 0 < max_len <= _U32 and 0 < D <= _U32 and 0 < W <= _U32, s)
+    _check(_lib().sf_seq_conv_backward_workspace(n_seq, max_len, D, W, C.byref(b)), s)
+    return b.value
+
+
+def sf_seq_conv_backward(ctx, seq, x, w, dy, workspace, bias=None, act=SF_ACT_NONE, state_in=None, d_state=None, dx_out=None, dw_out=None,
+                         dbias_out=None, d_state_in_out=None, stream=None):
+    s = "sf_seq_conv_backward"
+    on = _device_of(ctx, s)
+    p, dt, n, D, ld = _rows(x, on, s)
+    g, ldg = _of(dy, dt, n, D, on, s)
+    q, ldq = _of(dx_out, dt, n, D, on, s)
+    _arg(w.dim() == 2 and w.shape[0] == D and seq._on == on, s)
+    W = w.shape[1]
+    si, m1 = _pool(state_in, (W - 1, D), x.dtype, on, s)
+    ds, m2 = _pool(d_state, (W - 1, D), x.dtype, on, s)
+    do, m3 = _pool(d_state_in_out, (W - 1, D), x.dtype, on, s)
+    wp, wb = _bytes(workspace, on, s)
+    _check(_lib().sf_seq_conv_backward(ctx, seq, p, dt, n, D, ld, _whole(w, (D, W), on, s, True), _reals(bias, (D,), on, s), W, act, si, g, ldg, ds,
+                                       _slots_of(s, m1, m2, m3), q, ldq, _reals(dw_out, (D, W), on, s), _reals(dbias_out, (D,), on, s), do, wp, wb,
+                                       _stream_on(on, stream)), s)
+
+
+def sf_seq_scan_workspace(n_seq, max_len, rows, D, N, G=1, backward=False):
+    """Bytes of device scratch for a scan (backward: for it and its gradients)."""
+    b = C.c_size_t()
+    s = "sf_seq_scan_workspace"
+    _arg(all(0 <= v <= _U32 for v in (n_seq, max_len, rows, D, N, G)), s)
+    _check(_lib().sf_seq_scan_workspace(n_seq, max_len, rows, D, N, G, int(backward), C.byref(b)), s)
+    return b.value
+
+
+def sf_seq_scan_starts(n_seq, rows, D, N):
+    """Floats that the forward call keeps for the backward one."""
+    b = C.c_size_t()
+    s = "sf_seq_scan_starts"
+    _arg(all(0 <= v <= _U32 for v in (n_seq, rows, D, N)), s)
+    _check(_lib().sf_seq_scan_starts(n_seq, rows, D, N, C.byref(b)), s)
+    return b.value
+
+
+def _scan_rows(ctx, seq, u, delta, A, B, C_, D_skip, delta_bias, z, softplus, s):
+    on = _device_of(ctx, s)
+    r = sf_scan_rows()
+    r.u, dt, n, D, r.ldu = _rows(u, on, s)
+    _arg(A.dim() == 2 and A.shape[0] == D and A.shape[1] >= 1 and B.dim() == 2 and seq._on == on, s)
+    N = A.shape[1]
+    GN = B.shape[1]
+    _arg(GN % N == 0, s)
+    r.delta, r.ld_delta = _of(delta, dt, n, D, on, s)
+    r.z, r.ldz = _of(z, dt, n, D, on, s)
+    r.B, r.ldb = _of(B, dt, n, GN, on, s)
+    r.C, r.ldc = _of(C_, dt, n, GN, on, s)
+    r.A, r.D_skip, r.delta_bias = _whole(A, (D, N), on, s, True), _reals(D_skip, (D,), on, s), _reals(delta_bias, (D,), on, s)
+    r.D, r.N, r.G, r.dtype, r.softplus = D, N, GN // N, dt, int(softplus)
+    return on, r, n
+
+
+def _room(t, floats, on, w):
+    if t is None:
+        return None
+    return _flat(t, floats, 4, on, w, True)
+
+
+def sf_seq_scan(ctx, seq, u, delta, A, B, C, y_out, D=None, delta_bias=None, z=None, softplus=False, state_in=None, state_out=None, starts_out=None,
+                workspace=None, stream=None):
+    """y_out [rows][D] from u, delta [rows][D] (z likewise), B, C [rows][G * N], A float32 [D][N], D and delta_bias float32 [D]; states float32
+    [slots][D][N]."""
+    s = "sf_seq_scan"
+    on, r, n = _scan_rows(ctx, seq, u, delta, A, B, C, D, delta_bias, z, softplus, s)
+    q, ldy = _of(y_out, r.dtype, n, r.D, on, s)
+    si, m1 = _pool(state_in, (r.D, r.N), A.dtype, on, s)
+    so, m2 = _pool(state_out, (r.D, r.N), A.dtype, on, s)
+    wp, wb = _bytes(workspace, on, s)
+    _check(_lib().sf_seq_scan(ctx, seq, r, n, si, so, _slots_of(s, m1, m2), _room(starts_out, (n // 16 + seq.n_seq) * r.D * r.N, on, s), q, ldy, wp, wb,
+                              _stream_on(on, stream)), s)
+
+
+def sf_seq_scan_backward(ctx, seq, u, delta, A, B, C, dy, starts, workspace, D=None, delta_bias=None, z=None, softplus=False, du_out=None, d_delta_out=None,
+                         dA_out=None, dB_out=None, dC_out=None, dD_out=None, d_delta_bias_out=None, dz_out=None, d_state=None, d_state_in_out=None,
+                         stream=None):
+    """Inputs as in sf_seq_scan and the starts it wrote; any gradient may be None."""
+    s = "sf_seq_scan_backward"
+    on, r, n = _scan_rows(ctx, seq, u, delta, A, B, C, D, delta_bias, z, softplus, s)
+    g, ldg = _of(dy, r.dtype, n, r.D, on, s)
+    o = sf_scan_grads()
+    o.du, o.lddu = _of(du_out, r.dtype, n, r.D, on, s)
+    o.d_delta, o.ldd_delta = _of(d_delta_out, r.dtype, n, r.D, on, s)
+    o.dz, o.lddz = _of(dz_out, r.dtype, n, r.D, on, s)
+    o.dB, o.lddb = _of(dB_out, r.dtype, n, r.G * r.N, on, s)
+    o.dC, o.lddc = _of(dC_out, r.dtype, n, r.G * r.N, on, s)
+    o.dA, o.dD_skip, o.d_delta_bias = _reals(dA_out, (r.D, r.N), on, s), _reals(dD_out, (r.D,), on, s), _reals(d_delta_bias_out, (r.D,), on, s)
+    ds, m1 = _pool(d_state, (r.D, r.N), A.dtype, on, s)
+    do, m2 = _pool(d_state_in_out, (r.D, r.N), A.dtype, on, s)
+    wp, wb = _bytes(workspace, on, s)
+    _check(_lib().sf_seq_scan_backward(ctx, seq, r, n, g, ldg, _room(starts, (n // 16 + seq.n_seq) * r.D * r.N, on, s), ds, do, _slots_of(s, m1, m2), o, wp, wb,
+                                       _stream_on(on, stream)), s)
+
+
+def _top(ids, values, n, on, w):
+    k = None
+    for t in (ids, values):
+        if t is not None:
+            _arg(t.dim() == 2 and t.shape[0] == n and k in (None, t.shape[1]), w)
+            k = t.shape[1]
+    k = k or 0
+    return k, None if ids is None or not k else _whole(ids, (n, k), on, w), None if values is None or not k else _whole(values, (n, k), on, w, True)
+
+
+def sf_label_logprobs(ctx, logits, labels, logprob_out, entropy_out=None, lse_out=None, top_ids_out=None, top_logprobs_out=None, scale=1.0, n_dev=None,
+                      stream=None):
+    """logits [n][V]; labels int32 [n] (None where logprob_out is); outputs float32 [n], alternatives [n][k]."""
+    w = "sf_label_logprobs"
+    on = _device_of(ctx, w)
+    p, dt, n, V, ld = _rows(logits, on, w)
+    k, ti, tl = _top(top_ids_out, top_logprobs_out, n, on, w)
+    _check(_lib().sf_label_logprobs(ctx, p, dt, _flat(n_dev, 1, 4, on, w), n, V, ld, scale, None if labels is None else _whole(labels, (n,), on, w),
+                                    _reals(logprob_out, (n,), on, w), _reals(entropy_out, (n,), on, w), _reals(lse_out, (n,), on, w), k, ti, tl,
+                                    _stream_on(on, stream)), w)
+
+
+def sf_label_logprobs_backward(ctx, logits, labels, lse, d_logits_out, d_logprob=None, entropy=None, d_entropy=None, top_ids=None, d_top_logprobs=None,
+                               scale=1.0, n_dev=None, stream=None):
+    w = "sf_label_logprobs_backward"
+    on = _device_of(ctx, w)
+    p, dt, n, V, ld = _rows(logits, on, w)
+    q, ldd = _of(d_logits_out, dt, n, V, on, w)
+    k, ti, tl = _top(top_ids, d_top_logprobs, n, on, w)
+    _check(_lib().sf_label_logprobs_backward(ctx, p, dt, _flat(n_dev, 1, 4, on, w), n, V, ld, scale, None if labels is None else _whole(labels, (n,), on, w),
+                                             _reals(lse, (n,), on, w), _reals(d_logprob, (n,), on, w), _reals(entropy, (n,), on, w), _reals(d_entropy, (n,), on, w),
+                                             k, ti, tl, q, ldd, _stream_on(on, stream)), w)
 
 
 def sf_table_create(ctx, log2_slots, fast_pkts, slow_pkts, slow_slabs):

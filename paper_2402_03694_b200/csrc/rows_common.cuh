@@ -1,4 +1,4 @@
-// Pieces shared by the kernels that work on rows of bf16, fp16 or fp32 (mx4.cu, experts.cu): element types, 16-byte
+// Pieces shared by the kernels that work on rows of bf16, fp16 or fp32 (mx4.cu, experts.cu, seq_conv.cu, seq_scan.cu, logprobs.cu): element types, 16-byte
 // vectors of elements, a host-side guard of the current device.
 #pragma once
 #include <cuda_fp16.h>
@@ -43,10 +43,11 @@ __device__ __forceinline__ void store_f32(T* __restrict__ p, const float (&x)[N]
     }
 }
 
-// N elements as one access of N * sizeof(T) = 2, 4 or 16 bytes (p on a boundary of as many)
+// N elements as one access of N * sizeof(T) = 2, 4, 8 or 16 bytes (p on a boundary of as many)
 template <int BYTES> struct Word;
 template <> struct Word<2> { typedef uint16_t type; };
 template <> struct Word<4> { typedef uint32_t type; };
+template <> struct Word<8> { typedef uint2 type; };
 template <> struct Word<16> { typedef uint4 type; };
 template <typename T, int N> __device__ __forceinline__ void load_word(const T* __restrict__ p, float (&x)[N]) {
     typedef typename Word<N * sizeof(T)>::type W;

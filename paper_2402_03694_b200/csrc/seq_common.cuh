@@ -1,0 +1,58 @@
+// Pieces shared by the kernels that work on sequences of rows (seq_conv.cu, seq_scan.cu).
+#pragma once
+#include "rows_common.cuh"
+
+namespace sfseq {
+
+using namespace sfrow;
+
+// What the kernels need of the sequences: sf_sequences, the rows that the arrays hold, the states that the pools hold.
+struct Seqs {
+    const uint32_t* offsets; const uint32_t* counts; const int32_t* slots;
+    uint32_t n_seq, max_len, rows, n_slots;
+};
+struct Range { uint32_t first, len; int32_t slot; };
+
+// Sequence s as far as the arrays hold it: offsets beyond the rows, counts beyond the offsets and lengths beyond max_len are cut
+// (SF_ERR_CAPACITY), offsets that fall give no rows (SF_ERR_ARG), so no kernel reads or writes beyond what the caller named.
+__device__ __forceinline__ Range range_of(const Seqs& q, uint32_t s, sf_dev_state* st) {
+    Range r;
+    const uint32_t a = __ldg(q.offsets + s);
+    uint32_t b = __ldg(q.offsets + s + 1);
+    int err = 0;
+    if (b > q.rows) { b = q.rows; err = SF_ERR_CAPACITY; }
+    if (b < a) { err = a > q.rows && err ? SF_ERR_CAPACITY : SF_ERR_ARG; b = a; }
+    r.first = a; r.len = b - a;
+    if (q.counts) { const uint32_t c = __ldg(q.counts + s); if (c > r.len) err = err ? err : SF_ERR_CAPACITY; else r.len = c; }
+    if (r.len > q.max_len) { r.len = q.max_len; err = err ? err : SF_ERR_CAPACITY; }
+    if (err) sf_dev_set_error(st, err);
+    const int32_t slot = q.slots ? __ldg(q.slots + s) : (int32_t)s;
+    r.slot = (uint32_t)slot < q.n_slots ? slot : -1;
+    return r;
+}
+
+// ---- elementary functions in fp32 (relative errors of a few 2^-23) --------------------------------------------------
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float sigmoid(float x) { return rcp(1.0f + ex2(-kLog2e * x)); }
+
+// two fp32 values in a 64-bit register: one instruction for both
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pack2(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpack2(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// ---- host ---------------------------------------------------------------------------------------------------------------
+inline int check_sequences(const sf_sequences* q, uint32_t rows) {
+    if (!q || q->max_len == 0 || rows > 0x7FFFFFFFu || q->n_seq > 0x7FFFFFFFu || q->max_len > 0x7FFFFFFFu) return SF_ERR_ARG;
+    if (q->n_seq && !q->offsets) return SF_ERR_ARG;
+    return aligned(q->offsets, 4) && aligned(q->counts, 4) && aligned(q->slots, 4) ? SF_OK : SF_ERR_ARG;
+}
+inline Seqs seqs_of(const sf_sequences* q, uint32_t rows, uint32_t n_slots) {
+    return {q->offsets, q->counts, q->slots, q->n_seq, q->max_len, rows, n_slots};
+}
+
+}  // namespace sfseq
