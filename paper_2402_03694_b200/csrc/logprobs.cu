@@ -63,7 +63,7 @@ __device__ __forceinline__ Answer answer_of(const Stat& a, float scale) {
     r.m = a.m;
     if (a.s == 0.0f) { r.ln_s = 0.0f; r.lse = -INFINITY; r.h = 0.0f; return r; }
     r.ln_s = logf(a.s);
-    r.lse = fmaf(scale, a.m, r.ln_s);
+    r.lse = __fadd_rn(__fmul_rn(scale, a.m), r.ln_s);      // (two roundings, as in the gradient: where a row has one entry its p is exactly 1)
     r.h = r.ln_s - kLn2 * (a.w / a.s);
     return r;
 }
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kThreads) back_kernel(const Back<T> a) {
         float d[8];
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            const float lp = fmaf(a.scale, v[e], -lse), p = ex2(lp * kLog2e);
+            const float lp = __fsub_rn(__fmul_rn(a.scale, v[e]), lse), p = ex2(lp * kLog2e);
             d[e] = -p * (sum + (ge == 0.0f ? 0.0f : ge * (fmaxf(lp, -1e4f) + h)));
             if (i0 + e == (uint32_t)label) d[e] += g;
         }

@@ -45,6 +45,14 @@ __device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1,
 __device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 
+__device__ __forceinline__ f2 dup2(float a) { return pack2(a, a); }
+__device__ __forceinline__ f2 sigmoid2(f2 x) {
+    float a, b;
+    unpack2(mul2(x, dup2(-kLog2e)), a, b);
+    unpack2(add2(pack2(ex2(a), ex2(b)), dup2(1.0f)), a, b);
+    return pack2(rcp(a), rcp(b));
+}
+
 // ---- host ---------------------------------------------------------------------------------------------------------------
 inline int check_sequences(const sf_sequences* q, uint32_t rows) {
     if (!q || q->max_len == 0 || rows > 0x7FFFFFFFu || q->n_seq > 0x7FFFFFFFu || q->max_len > 0x7FFFFFFFu) return SF_ERR_ARG;

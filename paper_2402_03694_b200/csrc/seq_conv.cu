@@ -12,7 +12,7 @@ using namespace sfseq;
 
 constexpr uint32_t kThreads = 128;
 constexpr uint32_t kMaxTaps = 8;
-constexpr uint32_t kParts = 1024;          // partial sums of the filters' gradient at most
+constexpr int kAheadF = 4, kAheadB = 3;     // rows on their way while others are worked on: forward, backward
 
 struct Tiling {
     uint32_t lanes;        // threads side by side on a row (a power of two), of V channels each
@@ -35,55 +35,88 @@ template <typename T> struct Conv {
     sf_dev_state* st;
 };
 
-template <int V> __device__ __forceinline__ void zero(float (&v)[V]) {
+// V channels side by side
+template <int V> struct Ch {
+    float p[V];
+    __device__ __forceinline__ void set(const float (&x)[V]) {
 #pragma unroll
-    for (int i = 0; i < V; i++) v[i] = 0.0f;
-}
-// (a pool that the same call writes is read as ordinary memory)
-template <typename T, int V> __device__ __forceinline__ void load_plain(const T* p, float (&x)[V]) {
-    typedef typename Word<V * sizeof(T)>::type Q;
-    union { Q w; T e[V]; } u;
-    u.w = *reinterpret_cast<const Q*>(p);
-#pragma unroll
-    for (int i = 0; i < V; i++) x[i] = to_f32(u.e[i]);
-}
-
-// Filters of the thread's channels.  Tap k of W sits at WT - W + k, so that the newest row has the last one; what lies before is not used.
-template <int V, int WT>
-__device__ __forceinline__ void load_taps(const float* __restrict__ w, uint32_t c, uint32_t W, float (&tap)[WT][V]) {
-#pragma unroll
-    for (int k = 0; k < WT; k++)
-#pragma unroll
-        for (int i = 0; i < V; i++) tap[k][i] = k + (int)W >= WT ? __ldg(w + (size_t)(c + i) * W + (k + (int)W - WT)) : 0.0f;
-}
-
-// Row p of a sequence; for p < 0 row W - 1 + p of the state it starts from (rows before that are never asked for by a tap that counts)
-template <typename T, int V>
-__device__ __forceinline__ void row_at(const Conv<T>& a, const Range& r, int p, uint32_t c, float (&v)[V]) {
-    if (p >= 0) load_word<T, V>(a.x + (size_t)(r.first + p) * a.ldx + c, v);
-    else if (a.state_in && r.slot >= 0 && p + (int)a.W >= 1) load_plain<T, V>(a.state_in + ((size_t)r.slot * (a.W - 1) + (a.W - 1 + p)) * a.D + c, v);
-    else zero<V>(v);
-}
-
-// bias + the filter over the rows win[0] (oldest) .. win[WT - 1]
-template <int V, int WT, bool EXACT>
-__device__ __forceinline__ void filter(const float (&tap)[WT][V], const float (&win)[WT][V], const float (&bias)[V], uint32_t W, float (&pre)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; i++) pre[i] = bias[i];
-#pragma unroll
-    for (int k = 0; k < WT; k++) {
-        if (!EXACT && k + (int)W < WT) continue;
-#pragma unroll
-        for (int i = 0; i < V; i++) pre[i] = fmaf(tap[k][i], win[k][i], pre[i]);
+        for (int i = 0; i < V; i++) p[i] = x[i];
     }
+    __device__ __forceinline__ void get(float (&x)[V]) const {
+#pragma unroll
+        for (int i = 0; i < V; i++) x[i] = p[i];
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < V; i++) p[i] = 0.0f;
+    }
+    __device__ __forceinline__ void add_product(const Ch& a, const Ch& b) {
+#pragma unroll
+        for (int i = 0; i < V; i++) p[i] = fmaf(a.p[i], b.p[i], p[i]);
+    }
+    __device__ __forceinline__ void add(const Ch& a) {
+#pragma unroll
+        for (int i = 0; i < V; i++) p[i] += a.p[i];
+    }
+    __device__ __forceinline__ void silu() {
+#pragma unroll
+        for (int i = 0; i < V; i++) p[i] *= sigmoid(p[i]);
+    }
+    __device__ __forceinline__ void mul_silu_slope(const Ch& x) {      // times silu'(x) = s (1 + x (1 - s))
+#pragma unroll
+        for (int i = 0; i < V; i++) { const float s = sigmoid(x.p[i]); p[i] *= s * fmaf(x.p[i], 1.0f - s, 1.0f); }
+    }
+};
+
+// V elements of T as they lie in memory
+template <typename T, int V> struct Raw {
+    typename Word<V * sizeof(T)>::type w;
+    __device__ __forceinline__ void fetch(const T* p) { w = __ldg(reinterpret_cast<const decltype(w)*>(p)); }
+    __device__ __forceinline__ void fetch_plain(const T* p) { w = *reinterpret_cast<const decltype(w)*>(p); }     // (a pool that the same call writes)
+    __device__ __forceinline__ void open(Ch<V>& c) const {
+        union { decltype(w) q; T e[V]; } u;
+        u.q = w;
+        float x[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) x[i] = to_f32(u.e[i]);
+        c.set(x);
+    }
+};
+template <typename T, int V> __device__ __forceinline__ void store(T* p, const Ch<V>& c) { float x[V]; c.get(x); store_word<T, V>(p, x); }
+
+// Filters of the thread's channels by lag: tap[m] is what x_{t-m} is multiplied with, m < W; what lies behind is not used.  Four taps in one
+// access where they lie on a boundary (a thread's filters are its own: narrow accesses of a warp touch as many lines each).
+template <int V, int WT> __device__ __forceinline__ void load_taps(const float* __restrict__ w, uint32_t c, uint32_t W, Ch<V> (&tap)[WT]) {
+    if constexpr (WT == 4) if (((uintptr_t)w & 15u) == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const float4 q = __ldg(reinterpret_cast<const float4*>(w) + c + i);
+            tap[3].p[i] = q.x; tap[2].p[i] = q.y; tap[1].p[i] = q.z; tap[0].p[i] = q.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int m = 0; m < WT; m++)
+#pragma unroll
+        for (int i = 0; i < V; i++) tap[m].p[i] = m < (int)W ? __ldg(w + (size_t)(c + i) * W + (W - 1 - m)) : 0.0f;
+}
+template <int V> __device__ __forceinline__ void load_bias(const float* __restrict__ b, uint32_t c, Ch<V>& o) {
+    float x[V];
+#pragma unroll
+    for (int i = 0; i < V; i++) x[i] = b ? __ldg(b + c + i) : 0.0f;
+    o.set(x);
 }
 
-template <int V, int WT>
-__device__ __forceinline__ void shift(float (&win)[WT][V]) {
+// The WT - 1 rows before row p (oldest first); row -j of a sequence is row W - 1 - j of the state it starts from, zero without one.
+template <typename T, int V, int WT, int AT> __device__ __forceinline__ void rows_before(const Conv<T>& a, const Range& r, int p, uint32_t c, Ch<V> (&x)[AT]) {
 #pragma unroll
-    for (int k = 0; k + 1 < WT; k++)
-#pragma unroll
-        for (int i = 0; i < V; i++) win[k][i] = win[k + 1][i];
+    for (int k = 0; k + 1 < WT; k++) {
+        const int q = p - (WT - 1) + k;
+        Raw<T, V> v = {};
+        if (q >= 0) v.fetch(a.x + (size_t)(r.first + q) * a.ldx + c);
+        else if (a.state_in && r.slot >= 0 && q + (int)a.W >= 1) v.fetch_plain(a.state_in + ((size_t)r.slot * (a.W - 1) + (a.W - 1 + q)) * a.D + c);
+        v.open(x[k]);
+    }
 }
 
 template <typename T, int V, int WT, bool EXACT>
@@ -93,165 +126,185 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(const Conv<T> a) {
     const uint32_t c = (blockIdx.x % t.cblocks * t.lanes + threadIdx.x % t.lanes) * V, per = kThreads / t.lanes;
     if (c >= a.D) return;
     const uint32_t W = EXACT ? WT : a.W;
-    float tap[WT][V], bias[V];
+    Ch<V> tap[WT], bias;
     load_taps<V, WT>(a.w, c, W, tap);
-#pragma unroll
-    for (int i = 0; i < V; i++) bias[i] = a.bias ? __ldg(a.bias + c + i) : 0.0f;
+    load_bias<V>(a.bias, c, bias);
     const uint64_t items = (uint64_t)a.q.n_seq * t.tiles;
     for (uint64_t it = (uint64_t)(blockIdx.x / t.cblocks) * per + threadIdx.x / t.lanes; it < items; it += (uint64_t)t.parts * per) {
-        const uint32_t s = (uint32_t)(it / t.tiles), j = (uint32_t)(it % t.tiles);
+        const uint32_t j = (uint32_t)(it / a.q.n_seq), s = (uint32_t)(it % a.q.n_seq);
         const Range r = range_of(a.q, s, a.st);
         const int p0 = (int)(j * t.tile), p1 = (int)min(r.len, (j + 1) * t.tile);
         if (p0 >= p1 && (j || !a.state_out)) continue;
-        float win[WT][V];
+        const T* xr = a.x + (size_t)r.first * a.ldx + c;
+        Raw<T, V> next[kAheadF] = {};                          // rows on their way
 #pragma unroll
-        for (int k = 0; k + 1 < WT; k++) row_at<T, V>(a, r, p0 - (WT - 1) + k, c, win[k + 1]);
+        for (int u = 0; u < kAheadF; u++) if (p0 + u < p1) next[u].fetch(xr + (size_t)(p0 + u) * a.ldx);
+        Ch<V> x[WT + kAheadF - 1];
+        rows_before<T, V, WT, WT + kAheadF - 1>(a, r, p0, c, x);
         if (j == 0 && a.state_out && r.slot >= 0) {
-            // The sequence's last W - 1 rows, which where it is shorter begin with rows of the state it started from: win holds those
-            // (row p < 0 at win[WT + p]).  The first tile writes them all: it alone has read the old state, so the pools may be one.
+            // The sequence's last W - 1 rows, which where it is shorter begin with rows of the state it started from.  The first tile writes them
+            // all: it alone reads the old state, and a row from a later place than it goes to, so the pools may be one.
             T* so = a.state_out + (size_t)r.slot * (W - 1) * a.D + c;
             for (int i = 0; i + 1 < (int)W; i++) {
-                const int p = (int)r.len - (int)(W - 1) + i;
-                float o[V];
-                if (p >= 0) load_word<T, V>(a.x + (size_t)(r.first + p) * a.ldx + c, o);
-                else {
-#pragma unroll
-                    for (int k = 1; k < WT; k++) if (k == WT + p) {
-#pragma unroll
-                        for (int e = 0; e < V; e++) o[e] = win[k][e];
-                    }
-                }
-                store_word<T, V>(so + (size_t)i * a.D, o);
+                const int q = (int)r.len - (int)(W - 1) + i;
+                Raw<T, V> v = {};
+                if (q >= 0) v.fetch(xr + (size_t)q * a.ldx);
+                else if (a.state_in) v.fetch_plain(a.state_in + ((size_t)r.slot * (W - 1) + (W - 1 + q)) * a.D + c);
+                *reinterpret_cast<decltype(v.w)*>(so + (size_t)i * a.D) = v.w;
             }
         }
-        const T* x = a.x + (size_t)(r.first + p0) * a.ldx + c;
         T* y = a.y + (size_t)(r.first + p0) * a.ldy + c;
-        for (int p = p0; p < p1; p++, x += a.ldx, y += a.ldy) {
-            shift<V, WT>(win);
-            load_word<T, V>(x, win[WT - 1]);
-            float pre[V];
-            filter<V, WT, EXACT>(tap, win, bias, W, pre);
-            if (a.silu) {
+        xr += (size_t)(p0 + kAheadF) * a.ldx;              // the rows after those on their way
+        // kAheadF rows; ALL: they and as many more are there, so nothing is asked row by row
+        auto rows = [&](auto all, int p) {
+            constexpr bool ALL = decltype(all)::value;
 #pragma unroll
-                for (int i = 0; i < V; i++) pre[i] *= sigmoid(pre[i]);
+            for (int u = 0; u < kAheadF; u++) next[u].open(x[WT - 1 + u]);
+#pragma unroll
+            for (int u = 0; u < kAheadF; u++) { if (ALL || p + kAheadF + u < p1) next[u].fetch(xr); xr += a.ldx; }
+#pragma unroll
+            for (int u = 0; u < kAheadF; u++) {
+                if (ALL || p + u < p1) {
+                    Ch<V> pre = bias;
+#pragma unroll
+                    for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) pre.add_product(tap[m], x[WT - 1 + u - m]);
+                    if (a.silu) pre.silu();
+                    store<T, V>(y, pre);
+                }
+                y += a.ldy;
             }
-            store_word<T, V>(y, pre);
-        }
+#pragma unroll
+            for (int k = 0; k + 1 < WT; k++) x[k] = x[k + kAheadF];
+        };
+        int p = p0;
+        for (; p + 2 * kAheadF <= p1; p += kAheadF) rows(std::true_type(), p);
+        for (; p < p1; p += kAheadF) rows(std::false_type(), p);
     }
 }
 
-// The same walk with W - 1 rows more at a tile's end: dx_j is complete once dpre_{j+W-1} is there.
+// The same walk with WT - 1 rows more at a tile's end: dx_o = sum_m tap[m] dpre_{o+m} is complete once dpre_{o+WT-1} is there.
 template <typename T, int V, int WT, bool EXACT>
-__global__ void __launch_bounds__(kThreads) conv_backward_kernel(const Conv<T> a) {
+__global__ void __launch_bounds__(kThreads, 4) conv_backward_kernel(const Conv<T> a) {
     sf_chain_enter();
-    extern __shared__ float sums[];                        // [threads][(WT + 1) * V] where the block joins its sums
+    extern __shared__ float sums[];                        // [threads][V][WT + 1] where the block joins its sums
     const Tiling& t = a.t;
     const uint32_t c = (blockIdx.x % t.cblocks * t.lanes + threadIdx.x % t.lanes) * V, per = kThreads / t.lanes;
     const uint32_t W = EXACT ? WT : a.W;
-    float dw[WT][V], db[V];
+    Ch<V> dw[WT], db;
 #pragma unroll
-    for (int k = 0; k < WT; k++) zero<V>(dw[k]);
-    zero<V>(db);
+    for (int m = 0; m < WT; m++) dw[m].zero();
+    db.zero();
     if (c < a.D) {
-        float tap[WT][V], bias[V];
+        Ch<V> tap[WT], bias;
         load_taps<V, WT>(a.w, c, W, tap);
-#pragma unroll
-        for (int i = 0; i < V; i++) bias[i] = a.bias ? __ldg(a.bias + c + i) : 0.0f;
+        load_bias<V>(a.bias, c, bias);
         const uint64_t items = (uint64_t)a.q.n_seq * t.tiles;
         for (uint64_t it = (uint64_t)(blockIdx.x / t.cblocks) * per + threadIdx.x / t.lanes; it < items; it += (uint64_t)t.parts * per) {
-            const uint32_t s = (uint32_t)(it / t.tiles), j = (uint32_t)(it % t.tiles);
+            const uint32_t j = (uint32_t)(it / a.q.n_seq), s = (uint32_t)(it % a.q.n_seq);
             const Range r = range_of(a.q, s, a.st);
-            const int p0 = (int)(j * t.tile), p1 = (int)min(r.len, (j + 1) * t.tile), len = (int)r.len, H = (int)W - 1;
+            const int len = (int)r.len, H = (int)W - 1, p0 = (int)(j * t.tile), p1 = min(len, (int)((j + 1) * t.tile)), pe = min(len, p1 + H);
             const bool d0 = j == 0 && a.d_state0 && r.slot >= 0;
             if (p0 >= p1 && !d0) continue;
-            float win[WT][V], dp[WT][V];                   // x_{p-WT+1} .. x_p; dpre_p, dpre_{p-1}, ..
+            const T* xr = a.x + (size_t)r.first * a.ldx + c;
+            const T* gr = a.dy + (size_t)r.first * a.lddy + c;
+            Raw<T, V> nx[kAheadB] = {}, ng[kAheadB] = {};
 #pragma unroll
-            for (int k = 0; k + 1 < WT; k++) row_at<T, V>(a, r, p0 - (WT - 1) + k, c, win[k + 1]);
+            for (int u = 0; u < kAheadB; u++) if (p0 + u < pe) { nx[u].fetch(xr + (size_t)(p0 + u) * a.ldx); ng[u].fetch(gr + (size_t)(p0 + u) * a.lddy); }
+            Ch<V> x[WT + kAheadB - 1], dp[WT + kAheadB - 1];
+            rows_before<T, V, WT, WT + kAheadB - 1>(a, r, p0, c, x);
 #pragma unroll
-            for (int k = 0; k < WT; k++) zero<V>(dp[k]);
-            for (int p = p0; p < p1 + H; p++) {
-                shift<V, WT>(win);
+            for (int k = 0; k + 1 < WT; k++) dp[k].zero();
+            xr += (size_t)(p0 + kAheadB) * a.ldx;
+            gr += (size_t)(p0 + kAheadB) * a.lddy;
+            T* out = a.dx + ((ptrdiff_t)r.first + p0 - (WT - 1)) * (ptrdiff_t)a.lddx + c;      // (used from row 0 on)
+            // kAheadB rows; ALL: they and as many more are there, and so are the rows whose gradient is complete by them
+            auto rows = [&](auto all, int p) {
+                constexpr bool ALL = decltype(all)::value;
 #pragma unroll
-                for (int k = WT - 1; k > 0; k--)
+                for (int u = 0; u < kAheadB; u++) { nx[u].open(x[WT - 1 + u]); ng[u].open(dp[WT - 1 + u]); }
 #pragma unroll
-                    for (int i = 0; i < V; i++) dp[k][i] = dp[k - 1][i];
-                zero<V>(dp[0]);
-                if (p < len) {
-                    row_at<T, V>(a, r, p, c, win[WT - 1]);
-                    float g[V];
-                    load_word<T, V>(a.dy + (size_t)(r.first + p) * a.lddy + c, g);
+                for (int u = 0; u < kAheadB; u++) { if (ALL || p + kAheadB + u < pe) { nx[u].fetch(xr); ng[u].fetch(gr); } xr += a.ldx; gr += a.lddy; }
+#pragma unroll
+                for (int u = 0; u < kAheadB; u++) {
+                    Ch<V>& g = dp[WT - 1 + u];
                     if (a.silu) {
-                        float pre[V];
-                        filter<V, WT, EXACT>(tap, win, bias, W, pre);
+                        Ch<V> pre = bias;
 #pragma unroll
-                        for (int i = 0; i < V; i++) { const float e = sigmoid(pre[i]); g[i] *= e * (1.0f + pre[i] * (1.0f - e)); }
+                        for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) pre.add_product(tap[m], x[WT - 1 + u - m]);
+                        g.mul_silu_slope(pre);
                     }
+                    if (!ALL && p + u >= pe) g.zero();
+                    if (ALL || p + u < p1) {
+                        db.add(g);
 #pragma unroll
-                    for (int i = 0; i < V; i++) dp[0][i] = g[i];
-                    if (p < p1) {
-#pragma unroll
-                        for (int i = 0; i < V; i++) db[i] += g[i];
-#pragma unroll
-                        for (int k = 0; k < WT; k++) {
-                            if (!EXACT && k + (int)W < WT) continue;
-#pragma unroll
-                            for (int i = 0; i < V; i++) dw[k][i] = fmaf(g[i], win[k][i], dw[k][i]);
-                        }
+                        for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) dw[m].add_product(g, x[WT - 1 + u - m]);
                     }
-                } else zero<V>(win[WT - 1]);
-                const int o = p - H;                       // the row whose gradient is complete now
-                if (o >= p0 ? a.dx == nullptr : !d0) continue;
-                float d[V];
-                zero<V>(d);
-#pragma unroll
-                for (int k = 0; k < WT; k++) {             // tap k of W meets dpre_{o+W-1-k} = dp[k]
-                    if (!EXACT && k >= (int)W) continue;
-#pragma unroll
-                    for (int i = 0; i < V; i++) d[i] = fmaf(EXACT ? tap[k][i] : __ldg(a.w + (size_t)(c + i) * W + k), dp[k][i], d[i]);
                 }
-                if (a.d_state && r.slot >= 0 && o >= len - H) {
-                    float e[V];
-                    load_plain<T, V>(a.d_state + ((size_t)r.slot * H + (o - (len - H))) * a.D + c, e);
 #pragma unroll
-                    for (int i = 0; i < V; i++) d[i] += e[i];
+                for (int u = 0; u < kAheadB; u++, out += a.lddx) {
+                    const int o = p + u - (WT - 1);        // the row whose gradient is complete now
+                    if (ALL ? a.dx == nullptr : o >= p1 || (o >= p0 ? a.dx == nullptr : !d0 || o < -H)) continue;
+                    Ch<V> d;
+                    d.zero();
+#pragma unroll
+                    for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) d.add_product(tap[m], dp[u + m]);
+                    if (!ALL && a.d_state && r.slot >= 0 && o >= len - H) {
+                        Raw<T, V> v;
+                        Ch<V> e;
+                        v.fetch_plain(a.d_state + ((size_t)r.slot * H + (o - (len - H))) * a.D + c);
+                        v.open(e);
+                        d.add(e);
+                    }
+                    if (ALL || o >= 0) store<T, V>(out, d);
+                    else store<T, V>(a.d_state0 + ((size_t)r.slot * H + (o + H)) * a.D + c, d);
                 }
-                if (o >= 0) store_word<T, V>(a.dx + (size_t)(r.first + o) * a.lddx + c, d);
-                else store_word<T, V>(a.d_state0 + ((size_t)r.slot * H + (o + H)) * a.D + c, d);
-            }
+#pragma unroll
+                for (int k = 0; k + 1 < WT; k++) { x[k] = x[k + kAheadB]; dp[k] = dp[k + kAheadB]; }
+            };
+            int p = p0;
+            for (; p < p0 + WT - 1 && p < p1 + WT - 1; p += kAheadB) rows(std::false_type(), p);
+            for (; p + 2 * kAheadB <= p1; p += kAheadB) rows(std::true_type(), p);
+            for (; p < p1 + WT - 1; p += kAheadB) rows(std::false_type(), p);
         }
     }
     if (!a.parts) return;
     // the block's threads on the same channels add up their sums, in the order of the threads
     constexpr int Q = (WT + 1) * V;
     float* mine = sums + (size_t)threadIdx.x * Q;
+    float v[V];
 #pragma unroll
-    for (int i = 0; i < V; i++) {
+    for (int m = 0; m <= WT; m++) {
+        (m < WT ? dw[m < WT ? m : 0] : db).get(v);
 #pragma unroll
-        for (int k = 0; k < WT; k++) mine[i * (WT + 1) + k] = dw[k][i];
-        mine[i * (WT + 1) + WT] = db[i];
+        for (int i = 0; i < V; i++) mine[i * (WT + 1) + m] = v[i];
     }
     __syncthreads();
     const uint32_t n = t.lanes * V * (W + 1), c0 = blockIdx.x % t.cblocks * t.lanes * V;
     for (uint32_t e = threadIdx.x; e < n; e += kThreads) {
         const uint32_t ch = e / (W + 1), k = e % (W + 1);
         if (c0 + ch >= a.D) break;
-        const float* p = sums + (size_t)(ch / V) * Q + (ch % V) * (WT + 1) + (WT - W) + k;
-        float v = 0.0f;
-        for (uint32_t y = 0; y < per; y++) v += p[(size_t)y * t.lanes * Q];
-        a.parts[((size_t)(blockIdx.x / t.cblocks) * a.D + c0 + ch) * (W + 1) + k] = v;
+        const float* p = sums + (size_t)(ch / V) * Q + (ch % V) * (WT + 1) + (k < W ? W - 1 - k : WT);
+        float q = 0.0f;
+        for (uint32_t y = 0; y < per; y++) q += p[(size_t)y * t.lanes * Q];
+        a.parts[((size_t)(blockIdx.x / t.cblocks) * a.D + c0 + ch) * (W + 1) + k] = q;
     }
 }
 
-// dw[c][k] and db[c] from the blocks' sums: a warp per value, lanes over the blocks
+// dw[c][k] and db[c] from the blocks' sums: 32 values a block, a warp takes every eighth sum of each
 __global__ void __launch_bounds__(256) conv_join_kernel(const float* __restrict__ parts, uint32_t n_parts, uint32_t D, uint32_t W, float* dw, float* db) {
     sf_chain_enter();
-    const uint32_t lane = threadIdx.x & 31, e = blockIdx.x * 8 + threadIdx.x / 32, n = D * (W + 1);
-    if (e >= n) return;
+    __shared__ float sh[8][32];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32, e = blockIdx.x * 32 + lane, n = D * (W + 1);
     float v = 0.0f;
-    for (uint32_t p = lane; p < n_parts; p += 32) v += parts[(size_t)p * n + e];
+    if (e < n) {
+#pragma unroll 4
+        for (uint32_t p = warp; p < n_parts; p += 8) v += parts[(size_t)p * n + e];
+    }
+    sh[warp][lane] = v;
+    __syncthreads();
+    if (warp || e >= n) return;
 #pragma unroll
-    for (int m = 16; m; m >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
-    if (lane) return;
+    for (int i = 1; i < 8; i++) v += sh[i][lane];
     const uint32_t c = e / (W + 1), k = e % (W + 1);
     if (k < W) { if (dw) dw[(size_t)c * W + k] = v; }
     else if (db) db[c] = v;
@@ -263,20 +316,21 @@ uint32_t word_of(const void* p, size_t ld, uint32_t size) {          // the wide
     return v % 16 == 0 ? 16 : (v % 8 == 0 ? 8 : (v % 4 == 0 ? 4 : 2));
 }
 
-// Tiles of 32 rows (8 where the sequences are too few to fill the machine with those), threads over tiles in turn once the machine is full.
-Tiling tiling(const sf_sequences* q, uint32_t D, uint32_t V, uint32_t most_parts) {
+// Tiles of 128 rows, shorter (down to 8) while the sequences are too few to fill the machine with those; threads over tiles in turn once the
+// machine is full (`resident` blocks an SM).
+Tiling tiling(const sf_sequences* q, uint32_t D, uint32_t V, uint32_t resident) {
     Tiling t;
     const uint32_t units = (D + V - 1) / V;
     t.lanes = 1;
     while (t.lanes < kThreads && t.lanes < units) t.lanes *= 2;
     t.cblocks = (units + t.lanes - 1) / t.lanes;
-    const uint64_t full = (uint64_t)SF_NUM_SMS_DEFAULT * 1024;
-    t.tile = 32;
-    while (t.tile > 8 && (uint64_t)q->n_seq * ((q->max_len + t.tile - 1) / t.tile) * units < full) t.tile /= 2;
+    const uint64_t full = (uint64_t)SF_NUM_SMS_DEFAULT * resident;
+    t.tile = 128;
+    while (t.tile > 8 && (uint64_t)q->n_seq * ((q->max_len + t.tile - 1) / t.tile) * units < full * kThreads) t.tile /= 2;
     t.tiles = (q->max_len + t.tile - 1) / t.tile;
     const uint32_t per = kThreads / t.lanes;
     const uint64_t blocks = ((uint64_t)q->n_seq * t.tiles + per - 1) / per;
-    t.parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({blocks, most_parts, std::max<uint64_t>(1, (uint64_t)SF_NUM_SMS_DEFAULT * 16 / t.cblocks)}));
+    t.parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(blocks, std::max<uint64_t>(1, full / t.cblocks)));
     return t;
 }
 
@@ -291,7 +345,7 @@ int check(sf_ctx* ctx, const sf_sequences* seq, const void* x, int dtype, uint32
 template <typename T, int MOST, typename F> int by_width(uint32_t word, F f) {
     constexpr int size = sizeof(T);
     if (word >= MOST) return f(std::integral_constant<int, MOST / size>());
-    if (size == 2 && word >= 4) return f(std::integral_constant<int, 4 / size>());
+    if (size == 2 && MOST > 4 && word >= 4) return f(std::integral_constant<int, 4 / size>());
     return f(std::integral_constant<int, 1>());
 }
 template <typename F> int by_taps(uint32_t W, F f) {
@@ -315,13 +369,13 @@ extern "C" int sf_seq_conv(sf_ctx* ctx, const sf_sequences* seq, const void* x, 
     const uint32_t word = std::min({word_of(x, ldx, size), word_of(y_out, ldy, size), word_of(state_in, D, size), word_of(state_out, D, size), word_of(nullptr, D, size)});
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        return by_width<T, 16>(word, [&](auto v) {
+        return by_width<T, (sizeof(T) == 2 ? 8 : 16)>(word, [&](auto v) {
             return by_taps(W, [&](auto taps, auto exact) {
                 constexpr int V = decltype(v)::value, WT = decltype(taps)::value;
                 Conv<T> a = {};
                 a.q = seqs_of(seq, rows, n_slots); a.x = (const T*)x; a.ldx = ldx; a.w = w; a.bias = bias; a.D = D; a.W = W; a.silu = act == SF_ACT_SILU;
                 a.state_in = (const T*)state_in; a.state_out = (T*)state_out; a.y = (T*)y_out; a.ldy = ldy; a.st = ctx->d_state;
-                a.t = tiling(seq, D, V, 0x7FFFFFFFu);
+                a.t = tiling(seq, D, V, 32);
                 SF_CUDA(sf_launch_chained(conv_kernel<T, V, WT, decltype(exact)::value>, a.t.cblocks * a.t.parts, kThreads, 0, (cudaStream_t)stream, a));
                 return (int)SF_OK;
             });
@@ -334,7 +388,7 @@ extern "C" int sf_seq_conv_backward_workspace(uint32_t n_seq, uint32_t max_len, 
     if (!bytes_out || max_len == 0 || D == 0 || D > SF_EXPERT_MAX_D || W == 0 || W > kMaxTaps) return SF_ERR_ARG;
     const sf_sequences q = {nullptr, nullptr, nullptr, n_seq, max_len};
     uint32_t parts = 1;
-    for (uint32_t v : {1u, 2u, 4u}) parts = std::max(parts, tiling(&q, D, v, kParts).parts);
+    for (uint32_t v : {1u, 2u, 4u}) parts = std::max(parts, tiling(&q, D, v, 4).parts);
     *bytes_out = (size_t)parts * D * (W + 1) * 4;
     return SF_OK;
 }
@@ -364,12 +418,12 @@ extern "C" int sf_seq_conv_backward(sf_ctx* ctx, const sf_sequences* seq, const 
                 a.q = seqs_of(seq, rows, n_slots); a.x = (const T*)x; a.ldx = ldx; a.w = w; a.bias = bias; a.D = D; a.W = W; a.silu = act == SF_ACT_SILU;
                 a.state_in = (const T*)state_in; a.dy = (const T*)dy; a.lddy = lddy; a.d_state = (const T*)d_state; a.d_state0 = (T*)d_state_in_out;
                 a.dx = (T*)dx_out; a.lddx = lddx; a.st = ctx->d_state;
-                a.t = tiling(seq, D, V, kParts);
+                a.t = tiling(seq, D, V, 4);
                 if (sums && (!workspace || workspace_bytes < (size_t)a.t.parts * D * (W + 1) * 4)) return (int)SF_ERR_ARG;
                 a.parts = sums ? (float*)workspace : nullptr;
                 SF_CUDA(sf_launch_chained(conv_backward_kernel<T, V, WT, decltype(exact)::value>, a.t.cblocks * a.t.parts, kThreads, sums ? kThreads * (WT + 1) * V * 4 : 0,
                                           (cudaStream_t)stream, a));
-                if (sums) SF_CUDA(sf_launch_chained(conv_join_kernel, (D * (W + 1) + 7) / 8, 256, 0, (cudaStream_t)stream, (const float*)workspace, a.t.parts, D, W, dw_out, dbias_out));
+                if (sums) SF_CUDA(sf_launch_chained(conv_join_kernel, (D * (W + 1) + 31) / 32, 256, 0, (cudaStream_t)stream, (const float*)workspace, a.t.parts, D, W, dw_out, dbias_out));
                 return (int)SF_OK;
             });
         });
