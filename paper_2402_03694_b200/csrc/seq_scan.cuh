@@ -1,0 +1,268 @@
+// Selective state space scan over the rows of sequences, and its gradients.  Per channel d (group g of channels) and state n:
+//   delta_t = softplus(raw_t + bias) (or raw_t),  a_t = exp(delta_t A[n]),  h_t[n] = a_t[n] h_{t-1}[n] + delta_t u_t B_t[g][n],
+//   y_t = sum_n C_t[g][n] h_t[n] + D u_t,  out_t = y_t silu(z_t) (or y_t).
+// Backward, from the last row to the first, with e_t = dout_t silu(z_t) and G the gradient of h_t that later rows leave:
+//   g_t = G + e_t C_t,  dC_t = sum_d e_t h_t,  dB_t = sum_d g_t delta_t u_t,  G <- a_t g_t,
+//   du_t = D e_t + delta_t sum_n g_t B_t,  ddelta_t = u_t sum_n g_t B_t + sum_n (a_t g_t) h_{t-1} A,  dA = sum_t (a_t g_t) h_{t-1} delta_t,
+//   dD = sum_t e_t u_t,  dz_t = dout_t y_t silu'(z_t),  draw_t = ddelta_t sigmoid(raw_t + bias) = dbias_t.
+// States, decays and sums are fp32.
+//
+// Mapping: a warp owns CH = 128 / SL channels of one sequence; its lanes are CL = 32 / SL groups of 4 channels times SL groups of 4 states
+// (SL the power of two with 4 SL >= N), so a thread holds 4 x 4 states and the sums over states and over channels are both half done in registers.  Rows go by tiles:
+// steps, inputs times steps and B, C are staged in shared memory of the warp's own (softplus once an element), nothing waits for another warp.
+#pragma once
+#include <algorithm>
+#include "seq_common.cuh"
+
+namespace sfscan {
+
+using namespace sfseq;
+
+constexpr int kWarps = 4;                  // warps of a block
+constexpr uint32_t kEvery = 16;            // rows between two states that are kept for the backward pass
+constexpr uint32_t kMaxStates = SF_SCAN_MAX_STATES;
+
+struct Scan {
+    Seqs q;
+    const void* u; const void* delta; const void* z; const void* B; const void* C;
+    size_t ldu, lddelta, ldz, ldb, ldc;
+    const float* A; const float* Dk; const float* dbias;
+    uint32_t D, N, G, per;                 // per: channels of a group
+    int softplus;
+    const float* state_in; float* state_out;
+    float* starts;
+    int n4;                                // states lie four by four on 16-byte boundaries
+    void* y; size_t ldy;
+    // sequences in parts
+    uint32_t part_len, parts;              // rows of a part (a multiple of kEvery), parts of the longest sequence
+    float* part_state; float* part_step;   // [n_seq][parts][D][N] state at a part's end from zero, then at its start; [n_seq][parts][D] sum of its steps
+    // backward
+    const void* dy; size_t lddy;
+    const float* d_state; float* d_state0;
+    void* du; void* ddelta; void* dz; void* dB; void* dC;
+    size_t lddu, ldddelta, lddz, lddb, lddc;
+    float* dA; float* dD; float* dbias_out;
+    float* sum_bc;                         // [blocks of channels of a group][rows][G][2][N] where a group takes several blocks
+    float* sum_par;                        // [runs][D][N + 2]: dA, dD, dbias
+    uint32_t runs;                         // blocks behind one another over the sequences' parts
+    uint32_t cwarps;                       // warps over the channels of a group
+    uint32_t cblocks;                      // blocks over them
+    sf_dev_state* st;
+};
+
+// index of the state kept before row t (a multiple of kEvery) of sequence s, which begins at row `first`: sequences do not overlap
+__device__ __forceinline__ size_t start_index(uint32_t first, uint32_t s, uint32_t t) { return (size_t)first / kEvery + s + t / kEvery; }
+
+// softplus(x) = max(x, 0) + ln(1 + e), e = exp(-|x|) <= 1; ln(1 + e) = 2 artanh(e / (2 + e)) by its series in q = e / (2 + e) <= 1/3 (the first
+// term left out is q^14 / 15 < 2e-8 of the sum).  Keeps its relative accuracy where e is small, which ln(1 + e) by a logarithm does not.
+__device__ __forceinline__ float softplus_of(float x, float& e) {
+    e = ex2(-kLog2e * fabsf(x));
+    const float q = e * rcp(2.0f + e), q2 = q * q;
+    float p = fmaf(q2, 1.0f / 13, 1.0f / 11);
+    p = fmaf(q2, p, 1.0f / 9); p = fmaf(q2, p, 1.0f / 7); p = fmaf(q2, p, 1.0f / 5); p = fmaf(q2, p, 1.0f / 3); p = fmaf(q2, p, 1.0f);
+    return fmaf(2.0f * q, p, fmaxf(x, 0.0f));
+}
+
+// the same for two values
+__device__ __forceinline__ f2 softplus2(f2 x) {
+    float a, b;
+    unpack2(x, a, b);
+    const f2 t = mul2(pack2(fabsf(a), fabsf(b)), dup2(-kLog2e));
+    float e, f;
+    unpack2(t, e, f);
+    const f2 ee = pack2(ex2(e), ex2(f));
+    unpack2(add2(ee, dup2(2.0f)), e, f);
+    const f2 q = mul2(ee, pack2(rcp(e), rcp(f))), q2 = mul2(q, q);
+    f2 p = fma2(q2, dup2(1.0f / 13), dup2(1.0f / 11));
+    p = fma2(q2, p, dup2(1.0f / 9)); p = fma2(q2, p, dup2(1.0f / 7)); p = fma2(q2, p, dup2(1.0f / 5)); p = fma2(q2, p, dup2(1.0f / 3)); p = fma2(q2, p, dup2(1.0f));
+    return fma2(add2(q, q), p, pack2(fmaxf(a, 0.0f), fmaxf(b, 0.0f)));
+}
+
+// a = exp(delta A) with A in units of log2.  ex2.approx is low by 0.35 to 0.8 of 2^-24 on average (measured; by a thousand steps of 0.001 the state would be off by
+// 2e-5): the argument is raised by as much as takes that out near 0, where states live long.
+constexpr float kCentre = 3.2e-8f;
+__device__ __forceinline__ float decay(float delta, float A) { return ex2(fmaf(delta, A, kCentre)); }
+__device__ __forceinline__ f2 decay2(f2 delta, f2 A) {
+    float a, b;
+    unpack2(fma2(delta, A, dup2(kCentre)), a, b);
+    return pack2(ex2(a), ex2(b));
+}
+
+template <int SL> struct Shape {
+    static constexpr int CL = 32 / SL, CH = 4 * CL, NP = 4 * SL;               // channel lanes, channels of a warp, states with those that fill up
+    static constexpr int K = SL == 1 ? 4 : (SL <= 4 ? 8 : 16);                 // rows of a tile (kEvery is a multiple)
+    static constexpr int E = K * CH / 32;                                      // elements of a tile a lane stages
+};
+
+// one value a lane from four a lane: lane sl of SL gets the sum over the SL lanes of value j = 2 (sl & 1) + (sl >> 1 & 1) (SL = 1: none)
+template <int SL> __device__ __forceinline__ void sum_states(float (&v)[4], int sl) {
+    if constexpr (SL >= 2) {
+        const bool hi = sl & 1;
+        const float k0 = hi ? v[2] : v[0], k1 = hi ? v[3] : v[1], s0 = hi ? v[0] : v[2], s1 = hi ? v[1] : v[3];
+        v[0] = k0 + __shfl_xor_sync(0xFFFFFFFFu, s0, 1);
+        v[1] = k1 + __shfl_xor_sync(0xFFFFFFFFu, s1, 1);
+    }
+    if constexpr (SL >= 4) {
+        const bool hi = sl & 2;
+        const float k0 = hi ? v[1] : v[0], s0 = hi ? v[0] : v[1];
+        v[0] = k0 + __shfl_xor_sync(0xFFFFFFFFu, s0, 2);
+    }
+#pragma unroll
+    for (int m = 4; m < SL; m <<= 1) v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], m);
+}
+// writes what sum_states left to p[0..3] of the lane's channels
+template <int SL> __device__ __forceinline__ void put_states(float* p, const float (&v)[4], int sl) {
+    if constexpr (SL == 1) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else if constexpr (SL == 2) *reinterpret_cast<float2*>(p + 2 * sl) = make_float2(v[0], v[1]);
+    else if (sl < 4) p[2 * (sl & 1) + (sl >> 1 & 1)] = v[0];
+}
+
+// VV elements at once: 16 bytes of T, or one element
+template <typename T, int VV> struct Piece { typename Word<VV * sizeof(T)>::type w; };
+template <typename T, int VV> __device__ __forceinline__ void open(const Piece<T, VV>& p, float (&x)[VV]) {
+    union { typename Word<VV * sizeof(T)>::type w; T e[VV]; } u;
+    u.w = p.w;
+#pragma unroll
+    for (int i = 0; i < VV; i++) x[i] = to_f32(u.e[i]);
+}
+template <typename T, int VV> __device__ __forceinline__ Piece<T, VV> fetch(const void* base, size_t at, bool there) {
+    Piece<T, VV> p = {};
+    if (there) p.w = __ldg(reinterpret_cast<const typename Word<VV * sizeof(T)>::type*>(reinterpret_cast<const T*>(base) + at));
+    return p;
+}
+
+// B and C of a tile on their way (PV states at once, pieces of B first); stage writes them as [2][K][NP], zeros where there is nothing.
+template <typename T, int VV, int K, int NP> struct States {
+    static constexpr int PV = NP >= VV ? VV : 1, PR = NP / PV, I = (2 * K * PR + 31) / 32;
+    Piece<T, PV> p[I];
+    __device__ __forceinline__ void fetch_all(const Scan& a, size_t row0, uint32_t col, int rows, int lane) {
+#pragma unroll
+        for (int i = 0; i < I; i++) {
+            const int k = i * 32 + lane, t = k / PR % K, n = k % PR * PV;
+            const bool second = k >= K * PR;
+            p[i] = fetch<T, PV>(second ? a.C : a.B, (row0 + t) * (second ? a.ldc : a.ldb) + col + n, k < 2 * K * PR && t < rows && n < (int)a.N);
+        }
+    }
+    __device__ __forceinline__ void stage(float* sh, int lane) const {
+#pragma unroll
+        for (int i = 0; i < I; i++) {
+            const int k = i * 32 + lane;
+            if (k >= 2 * K * PR) break;
+            float x[PV];
+            open<T, PV>(p[i], x);
+            if constexpr (PV == 1) sh[k] = x[0];
+            else {
+#pragma unroll
+                for (int e = 0; e < PV; e += 4) *reinterpret_cast<float4*>(sh + k * PV + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+            }
+        }
+    }
+};
+
+// States at the parts' starts from those at their ends: h <- exp(A sum of steps) h + end, a thread per channel and state.  BACK: the same for the
+// gradients, from the last part to the first (what a part holds then is the gradient at its start that its own rows cause).
+template <bool BACK>
+__global__ void __launch_bounds__(256) parts_kernel(const Scan a) {
+    sf_chain_enter();
+    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t s = blockIdx.y;
+    const uint64_t DN = (uint64_t)a.D * a.N;
+    if (at >= DN) return;
+    const Range r = range_of(a.q, s, a.st);
+    const uint32_t parts = (r.len + a.part_len - 1) / a.part_len;
+    const float A = __ldg(a.A + at) * kLog2e;
+    const float* in = BACK ? a.d_state : a.state_in;
+    float* out = BACK ? a.d_state0 : a.state_out;
+    float h = in && r.slot >= 0 ? in[(size_t)r.slot * DN + at] : 0.0f;
+    float* ps = a.part_state + (size_t)s * a.parts * DN + at;
+    const float* steps = a.part_step + (size_t)s * a.parts * a.D + at / a.N;
+    for (uint32_t i = 0; i < parts; i++) {
+        const uint32_t p = BACK ? parts - 1 - i : i;
+        const float end = ps[(size_t)p * DN];
+        ps[(size_t)p * DN] = h;
+        h = fmaf(decay(steps[(size_t)p * a.D], A), h, end);
+    }
+    if (!BACK && parts == 0) ps[0] = h;
+    if (out && r.slot >= 0) out[(size_t)r.slot * DN + at] = h;
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------------------------
+inline int state_lanes(uint32_t N) { int sl = 1; while ((uint32_t)(4 * sl) < N) sl *= 2; return sl; }
+
+struct Plan { uint32_t sl, cwarps, cblocks, part_len, parts, runs; bool split; };
+
+// Sequences go in parts where the warps of whole sequences would leave most of the machine idle: two passes over the inputs then, so only
+// where parts make three times as many warps.
+inline Plan plan_of(uint32_t n_seq, uint32_t max_len, uint32_t D, uint32_t N, uint32_t G, bool backward) {
+    Plan p;
+    p.sl = state_lanes(N);
+    const uint32_t CH = 128 / p.sl, per = D / G;
+    p.cwarps = (per + CH - 1) / CH;
+    p.cblocks = (p.cwarps + kWarps - 1) / kWarps;
+    const uint64_t warps = std::max<uint64_t>(1, (uint64_t)n_seq * G * p.cwarps), full = (uint64_t)SF_NUM_SMS_DEFAULT * (backward ? 8 : 16);
+    uint64_t want = full / warps;
+    p.part_len = (max_len + kEvery - 1) / kEvery * kEvery;
+    if (want >= 3 && max_len > 2 * 64) p.part_len = (uint32_t)std::max<uint64_t>(64, ((max_len + want - 1) / want + kEvery - 1) / kEvery * kEvery);
+    p.parts = (max_len + p.part_len - 1) / p.part_len;
+    p.split = p.parts > 1;
+    const uint64_t blocks = (uint64_t)G * p.cblocks, items = std::max<uint64_t>(1, (uint64_t)n_seq * p.parts);
+    p.runs = (uint32_t)std::min<uint64_t>({items, 65535, std::max<uint64_t>(1, (uint64_t)SF_NUM_SMS_DEFAULT * 4 / blocks)});
+    return p;
+}
+inline size_t part_bytes(const Plan& p, uint32_t n_seq, uint32_t D, uint32_t N) { return p.split ? sf_align256((size_t)n_seq * p.parts * D * N * 4) + sf_align256((size_t)n_seq * p.parts * D * 4) : 0; }
+inline size_t back_bytes(const Plan& p, uint32_t n_seq, uint32_t rows, uint32_t D, uint32_t N, uint32_t G) {
+    return part_bytes(p, n_seq, D, N) + sf_align256((size_t)p.runs * D * (N + 2) * 4) + (p.cblocks > 1 ? sf_align256((size_t)p.cblocks * rows * G * 2 * N * 4) : 0);
+}
+
+inline bool sizes_ok(uint32_t rows, uint32_t n_seq, uint32_t max_len, uint32_t D, uint32_t N, uint32_t G) {
+    return rows <= 0x7FFFFFFFu && n_seq <= 0x7FFFFFFFu && max_len && max_len <= 0x7FFFFFFFu && D && D <= SF_EXPERT_MAX_D && N && N <= kMaxStates && G && D % G == 0;
+}
+
+template <typename F> int by_states(uint32_t sl, F f) {
+    switch (sl) {
+        case 1: return f(std::integral_constant<int, 1>());
+        case 2: return f(std::integral_constant<int, 2>());
+        case 4: return f(std::integral_constant<int, 4>());
+        case 8: return f(std::integral_constant<int, 8>());
+        default: return f(std::integral_constant<int, 16>());
+    }
+}
+
+inline int check(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_rows* in, uint32_t rows) {
+    if (!ctx || !in || !type_ok(in->dtype)) return SF_ERR_ARG;
+    const int ok = check_sequences(seq, rows);
+    if (ok != SF_OK) return ok;
+    if (!sizes_ok(rows, seq->n_seq, seq->max_len, in->D, in->N, in->G)) return SF_ERR_ARG;
+    const size_t GN = (size_t)in->G * in->N;
+    if (in->ldu < in->D || in->ld_delta < in->D || (in->z && in->ldz < in->D) || in->ldb < GN || in->ldc < GN || !in->A) return SF_ERR_ARG;
+    if (rows && (!in->u || !in->delta || !in->B || !in->C)) return SF_ERR_ARG;
+    const uint32_t size = type_bytes(in->dtype);
+    if (!aligned(in->u, size) || !aligned(in->delta, size) || !aligned(in->z, size) || !aligned(in->B, size) || !aligned(in->C, size)) return SF_ERR_ARG;
+    return aligned(in->A, 4) && aligned(in->D_skip, 4) && aligned(in->delta_bias, 4) ? SF_OK : SF_ERR_ARG;
+}
+inline void fill(Scan& a, const sf_sequences* seq, const sf_scan_rows* in, uint32_t rows, uint32_t n_slots, const Plan& p, sf_ctx* ctx) {
+    a = {};
+    a.q = seqs_of(seq, rows, n_slots);
+    a.u = in->u; a.delta = in->delta; a.z = in->z; a.B = in->B; a.C = in->C;
+    a.ldu = in->ldu; a.lddelta = in->ld_delta; a.ldz = in->ldz; a.ldb = in->ldb; a.ldc = in->ldc;
+    a.A = in->A; a.Dk = in->D_skip; a.dbias = in->delta_bias;
+    a.D = in->D; a.N = in->N; a.G = in->G; a.per = in->D / in->G; a.softplus = in->softplus != 0;
+    a.n4 = in->N % 4 == 0;
+    a.part_len = p.part_len; a.parts = p.parts; a.runs = p.runs; a.cwarps = p.cwarps; a.cblocks = p.cblocks;
+    a.st = ctx->d_state;
+}
+// rows begin on 16-byte boundaries, and so does every group's first channel and state
+inline bool fits(const sf_scan_rows* in) {
+    const uint32_t size = type_bytes(in->dtype), v = 16 / size;
+    auto row = [&](const void* p, size_t ld) { return !p || (aligned(p, 16) && ld % v == 0); };
+    return row(in->u, in->ldu) && row(in->delta, in->ld_delta) && row(in->z, in->ldz) && row(in->B, in->ldb) && row(in->C, in->ldc) && in->D / in->G % v == 0 && in->N % v == 0;
+}
+inline bool fits(const void* p, size_t ld, int dtype) { return !p || (aligned(p, 16) && ld % (16 / type_bytes(dtype)) == 0); }
+
+template <typename K> int launch(K kernel, dim3 grid, uint32_t block, size_t smem, cudaStream_t st, const Scan& a) {
+    if (smem > 48 * 1024) SF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    SF_CUDA(sf_launch_chained(kernel, grid, block, smem, st, a));
+    return SF_OK;
+}
+
+}  // namespace sfscan
