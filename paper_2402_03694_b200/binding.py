@@ -774,6 +774,9 @@ def _scan_rows(ctx, seq, u, delta, A, B, C_, D_skip, delta_bias, z, softplus, s)
     return on, r, n
 
 
+_EVERY = 8                        # rows between two states that the scan keeps for its backward pass
+
+
 def _room(t, floats, on, w):
     if t is None:
         return None
@@ -790,7 +793,7 @@ def sf_seq_scan(ctx, seq, u, delta, A, B, C, y_out, D=None, delta_bias=None, z=N
     si, m1 = _pool(state_in, (r.D, r.N), A.dtype, on, s)
     so, m2 = _pool(state_out, (r.D, r.N), A.dtype, on, s)
     wp, wb = _bytes(workspace, on, s)
-    _check(_lib().sf_seq_scan(ctx, seq, r, n, si, so, _slots_of(s, m1, m2), _room(starts_out, (n // 16 + seq.n_seq) * r.D * r.N, on, s), q, ldy, wp, wb,
+    _check(_lib().sf_seq_scan(ctx, seq, r, n, si, so, _slots_of(s, m1, m2), _room(starts_out, (n // _EVERY + seq.n_seq) * r.D * r.N, on, s), q, ldy, wp, wb,
                               _stream_on(on, stream)), s)
 
 
@@ -811,7 +814,7 @@ def sf_seq_scan_backward(ctx, seq, u, delta, A, B, C, dy, starts, workspace, D=N
     ds, m1 = _pool(d_state, (r.D, r.N), A.dtype, on, s)
     do, m2 = _pool(d_state_in_out, (r.D, r.N), A.dtype, on, s)
     wp, wb = _bytes(workspace, on, s)
-    _check(_lib().sf_seq_scan_backward(ctx, seq, r, n, g, ldg, _room(starts, (n // 16 + seq.n_seq) * r.D * r.N, on, s), ds, do, _slots_of(s, m1, m2), o, wp, wb,
+    _check(_lib().sf_seq_scan_backward(ctx, seq, r, n, g, ldg, _room(starts, (n // _EVERY + seq.n_seq) * r.D * r.N, on, s), ds, do, _slots_of(s, m1, m2), o, wp, wb,
                                        _stream_on(on, stream)), s)
 
 

@@ -22,7 +22,8 @@ template <typename T, int SL, int VV, bool ENDS>
 __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     sf_chain_enter();
     typedef Shape<SL> S;
-    constexpr int K = S::K, CH = S::CH, NP = S::NP, VR = CH / VV, I = S::E / VV;
+    typedef Pieces<S::K, S::CH, VV> P;
+    constexpr int K = S::K, CH = S::CH, NP = S::NP, I = P::I;
     extern __shared__ __align__(16) unsigned char shared[];
     Forward<SL>& sh = reinterpret_cast<Forward<SL>*>(shared)[threadIdx.x / 32];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
@@ -36,22 +37,18 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     // rows on their way while others are worked on
     Piece<T, VV> nd[I], nu[I], nz[I];
     States<T, VV, K, NP> ns;
-    // piece i of a lane: row ti(i) of the tile, channel ci(i) of the warp
-    constexpr int RI = VR <= 32 ? 32 / VR : 1, CI = VR <= 32 ? 1 : VR / 32;
-    const int lt = VR <= 32 ? lane / VR : 0, lc = (VR <= 32 ? lane % VR : lane) * VV;
-    auto ti = [&](int i) { return lt + i / CI * RI; };
-    auto ci = [&](int i) { return lc + i % CI * 32 * VV; };
-    const size_t at0 = (size_t)r.first + t_begin + lt;
-    const T* pd = (const T*)a.delta + at0 * a.lddelta + ch0 + lc; const T* pu = (const T*)a.u + at0 * a.ldu + ch0 + lc; const T* pz = (const T*)a.z + at0 * a.ldz + ch0 + lc;
-    T* py = (T*)a.y + at0 * a.ldy + ch0 + lc;
+    const P pc(lane);
+    const size_t at0 = (size_t)r.first + t_begin + pc.lt;
+    const T* pd = (const T*)a.delta + at0 * a.lddelta + ch0 + pc.lc; const T* pu = (const T*)a.u + at0 * a.ldu + ch0 + pc.lc; const T* pz = (const T*)a.z + at0 * a.ldz + ch0 + pc.lc;
+    T* py = (T*)a.y + at0 * a.ldy + ch0 + pc.lc;
     auto ask = [&](uint32_t t0) {
         const int rows = (int)min((uint32_t)K, t_end - t0);
 #pragma unroll
         for (int i = 0; i < I; i++) {
-            const bool there = ci(i) < (int)have && ti(i) < rows;
-            nd[i] = fetch<T, VV>(pd, (i / CI * RI) * a.lddelta + i % CI * 32 * VV, there);
-            nu[i] = fetch<T, VV>(pu, (i / CI * RI) * a.ldu + i % CI * 32 * VV, there);
-            if (!ENDS && a.z) nz[i] = fetch<T, VV>(pz, (i / CI * RI) * a.ldz + i % CI * 32 * VV, there);
+            const bool there = pc.c(i) < (int)have && pc.t(i) < rows;
+            nd[i] = fetch<T, VV>(pd, P::step(i, a.lddelta), there);
+            nu[i] = fetch<T, VV>(pu, P::step(i, a.ldu), there);
+            if (!ENDS && a.z) nz[i] = fetch<T, VV>(pz, P::step(i, a.ldz), there);
         }
         ns.fetch_all(a, (size_t)r.first + t0, g * a.N, rows, lane);
         pd += K * a.lddelta; pu += K * a.ldu; pz += K * a.ldz;
@@ -112,7 +109,8 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
         Piece<T, VV> cu[I], cz[I];
 #pragma unroll
         for (int i = 0; i < I; i++) {
-            const int k = i * 32 + lane, t = k / VR, c = k % VR * VV;
+            const int t = pc.t(i), c = pc.c(i);
+            if (t >= K) continue;
             float d[VV], u[VV];
             cu[i] = nu[i];
             if (!ENDS) cz[i] = nz[i];
@@ -171,7 +169,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
         if constexpr (!ENDS) {
 #pragma unroll
             for (int i = 0; i < I; i++) {
-                const int t = ti(i), c = ci(i);
+                const int t = pc.t(i), c = pc.c(i);
                 if (c >= (int)have || t >= rows) continue;
                 float u[VV], z[VV], y[VV];
                 open<T, VV>(cu[i], u);
@@ -198,7 +196,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
                         unpack2(v, y[e], y[e + 1]); unpack2(w, y[e + 2], y[e + 3]);
                     }
                 }
-                store_word<T, VV>(py + (i / CI * RI) * a.ldy + i % CI * 32 * VV, y);
+                store_word<T, VV>(py + P::step(i, a.ldy), y);
             }
             py += K * a.ldy;
         }
@@ -210,7 +208,8 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
         float* sum = &sh.y[0][0];                         // [rows of a tile][CH]
 #pragma unroll
         for (int i = 0; i < I; i++) {
-            const int t = ti(i), c = ci(i);
+            const int t = pc.t(i), c = pc.c(i);
+            if (t >= K) continue;
 #pragma unroll
             for (int e = 0; e < VV; e += 2) {
                 float x, y;
@@ -348,7 +347,7 @@ extern "C" int sf_seq_scan(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_r
     return by_type(in->dtype, [&](auto zero) {
         typedef decltype(zero) T;
         return by_states(p.sl, [&](auto lanes) {
-            constexpr int SL = decltype(lanes)::value, VV = std::min(16 / (int)sizeof(T), Shape<SL>::E);
+            constexpr int SL = decltype(lanes)::value, VV = 16 / (int)sizeof(T);
             if (seq->max_len == 1 && !starts_out) {
                 const bool v4 = in->N % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16);
                 return launch(v4 ? step_kernel<T, SL, true> : step_kernel<T, SL, false>, (uint32_t)blocks, 32 * kWarps, 0, st, a);

@@ -19,7 +19,7 @@ namespace sfscan {
 using namespace sfseq;
 
 constexpr int kWarps = 4;                  // warps of a block
-constexpr uint32_t kEvery = 16;            // rows between two states that are kept for the backward pass
+constexpr uint32_t kEvery = 8;             // rows between two states that are kept for the backward pass
 constexpr uint32_t kMaxStates = SF_SCAN_MAX_STATES;
 
 struct Scan {
@@ -90,32 +90,19 @@ __device__ __forceinline__ f2 decay2(f2 delta, f2 A) {
 
 template <int SL> struct Shape {
     static constexpr int CL = 32 / SL, CH = 4 * CL, NP = 4 * SL;               // channel lanes, channels of a warp, states with those that fill up
-    static constexpr int K = SL == 1 ? 4 : (SL <= 4 ? 8 : 16);                 // rows of a tile (kEvery is a multiple)
-    static constexpr int E = K * CH / 32;                                      // elements of a tile a lane stages
+    static constexpr int K = SL == 1 ? 4 : 8;                                  // rows of a tile of the forward pass (kEvery is a multiple)
 };
 
-// one value a lane from four a lane: lane sl of SL gets the sum over the SL lanes of value j = 2 (sl & 1) + (sl >> 1 & 1) (SL = 1: none)
-template <int SL> __device__ __forceinline__ void sum_states(float (&v)[4], int sl) {
-    if constexpr (SL >= 2) {
-        const bool hi = sl & 1;
-        const float k0 = hi ? v[2] : v[0], k1 = hi ? v[3] : v[1], s0 = hi ? v[0] : v[2], s1 = hi ? v[1] : v[3];
-        v[0] = k0 + __shfl_xor_sync(0xFFFFFFFFu, s0, 1);
-        v[1] = k1 + __shfl_xor_sync(0xFFFFFFFFu, s1, 1);
-    }
-    if constexpr (SL >= 4) {
-        const bool hi = sl & 2;
-        const float k0 = hi ? v[1] : v[0], s0 = hi ? v[0] : v[1];
-        v[0] = k0 + __shfl_xor_sync(0xFFFFFFFFu, s0, 2);
-    }
-#pragma unroll
-    for (int m = 4; m < SL; m <<= 1) v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], m);
-}
-// writes what sum_states left to p[0..3] of the lane's channels
-template <int SL> __device__ __forceinline__ void put_states(float* p, const float (&v)[4], int sl) {
-    if constexpr (SL == 1) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    else if constexpr (SL == 2) *reinterpret_cast<float2*>(p + 2 * sl) = make_float2(v[0], v[1]);
-    else if (sl < 4) p[2 * (sl & 1) + (sl >> 1 & 1)] = v[0];
-}
+// How a warp stages a tile of K rows of CH channels: pieces of VV channels, piece i of a lane at row t(i), channel c(i).  Lanes without a piece have rows from K on.
+template <int K, int CH, int VV> struct Pieces {
+    static constexpr int VR = CH / VV, I = (K * VR + 31) / 32, RI = VR <= 32 ? 32 / VR : 1, CI = VR <= 32 ? 1 : VR / 32;
+    int lt, lc;
+    __device__ __forceinline__ explicit Pieces(int lane) : lt(VR <= 32 ? lane / VR : 0), lc((VR <= 32 ? lane % VR : lane) * VV) {}
+    __device__ __forceinline__ int t(int i) const { return lt + i / CI * RI; }
+    __device__ __forceinline__ int c(int i) const { return lc + i % CI * 32 * VV; }
+    // what piece i lies beyond piece 0 in rows of pitch ld
+    __device__ __forceinline__ static size_t step(int i, size_t ld) { return (size_t)(i / CI * RI) * ld + i % CI * 32 * VV; }
+};
 
 // VV elements at once: 16 bytes of T, or one element
 template <typename T, int VV> struct Piece { typename Word<VV * sizeof(T)>::type w; };
@@ -147,7 +134,7 @@ template <typename T, int VV, int K, int NP> struct States {
 #pragma unroll
         for (int i = 0; i < I; i++) {
             const int k = i * 32 + lane;
-            if (k >= 2 * K * PR) break;
+            if (k >= 2 * K * PR) continue;
             float x[PV];
             open<T, PV>(p[i], x);
             if constexpr (PV == 1) sh[k] = x[0];

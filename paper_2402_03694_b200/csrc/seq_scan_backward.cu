@@ -5,38 +5,133 @@ namespace {
 
 using namespace sfscan;
 
-template <int SL> struct Old {
-    static constexpr int CL = 32 / SL, CH = 4 * CL, NP = 4 * SL, K = 512 / CH < 16 ? 512 / CH : 16, E = K * CH / 32;
+constexpr int K = (int)kEvery;             // rows of a tile
+
+// What a warp keeps in shared memory for a tile; rows of channels spaced so that 16-byte accesses of eight lanes meet no common bank
+template <int SL> struct __align__(16) Backward {
+    typedef Shape<SL> S;
+    static constexpr int PX = S::CH + 4;
+    float step[K][PX], u[K][PX], e[K][PX];                 // delta; u; dout silu(z)
+    float dstep[K][PX], dgate[K][PX];                      // d delta / d raw; dout silu'(z)
+    float bc[2][K][S::NP];                                 // B, C
+    float s1[K][PX], s2[K][PX], y[K][PX];                  // sum g B; sum (a g) h_{t-1} A; sum C h
+    float sum[K][2][S::NP];                                // the warp's dB, dC
+    float4 start[2][4][32];                                // the states before rows 0 and 4, every lane its own
+    float bias[S::CH], skip[S::CH];
 };
-// B or C of a tile (rows t0 .. t0 + K - 1 as far as there) into shared memory as [K][NP], zeros elsewhere
-template <typename T, int VV, int K, int NP>
-__device__ __forceinline__ void stage_states(float* sh, const void* base, size_t ld, size_t row0, uint32_t col, uint32_t N, int rows, int lane) {
-    constexpr int PV = NP >= VV ? VV : 1, PR = NP / PV;
+
+// stages steps, inputs and gradients of the rows t0 .. t0 + K - 1 as far as there (zeros behind: they then change nothing); ENDS: what the pass for the parts' ends needs
+template <typename T, int SL, int VV, bool ENDS>
+__device__ __forceinline__ void stage(const Scan& a, Backward<SL>& sh, size_t row0, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
+    typedef Shape<SL> S;
+    typedef Pieces<K, S::CH, VV> P;
+    const P pc(lane);
+    const size_t at = row0 + pc.lt;
+    const T* pd = (const T*)a.delta + at * a.lddelta + ch0 + pc.lc; const T* pu = (const T*)a.u + at * a.ldu + ch0 + pc.lc;
+    const T* pz = (const T*)a.z + at * a.ldz + ch0 + pc.lc; const T* pg = (const T*)a.dy + at * a.lddy + ch0 + pc.lc;
+    Piece<T, VV> nd[P::I], nu[P::I], nz[P::I], ng[P::I];
+    States<T, VV, K, S::NP> ns;
 #pragma unroll
-    for (int i = lane; i < K * PR; i += 32) {
-        const int t = i / PR, n = i % PR * PV;
-        float x[PV];
-        open<T, PV>(fetch<T, PV>(base, (row0 + t) * ld + col + n, t < rows && n < (int)N), x);
-#pragma unroll
-        for (int e = 0; e < PV; e++) sh[t * NP + n + e] = x[e];
+    for (int i = 0; i < P::I; i++) {
+        const bool there = pc.t(i) < rows && pc.c(i) < (int)have;
+        nd[i] = fetch<T, VV>(pd, P::step(i, a.lddelta), there);
+        if (!ENDS) nu[i] = fetch<T, VV>(pu, P::step(i, a.ldu), there);
+        if (a.z) nz[i] = fetch<T, VV>(pz, P::step(i, a.ldz), there);
+        ng[i] = fetch<T, VV>(pg, P::step(i, a.lddy), there);
     }
+    ns.fetch_all(a, row0, g * a.N, rows, lane);
+#pragma unroll
+    for (int i = 0; i < P::I; i++) {
+        const int t = pc.t(i), c = pc.c(i);
+        if (t >= K) continue;
+        const bool there = t < rows && c < (int)have;
+        float d[VV], u[VV], z[VV], o[VV];
+        open<T, VV>(nd[i], d);
+        if (!ENDS) open<T, VV>(nu[i], u);
+        if (a.z) open<T, VV>(nz[i], z);
+        open<T, VV>(ng[i], o);
+        float ds[VV], dg[VV];
+#pragma unroll
+        for (int e = 0; e < VV; e++) {
+            d[e] += sh.bias[c + e];
+            ds[e] = 1.0f; dg[e] = 0.0f;
+            if (a.softplus) {
+                float x;                                   // exp(-|raw|): the slope is 1 / (1 + x), or x / (1 + x) left of 0
+                const float raw = d[e];
+                d[e] = softplus_of(raw, x);
+                if (!ENDS) ds[e] = (raw >= 0.0f ? 1.0f : x) * rcp(1.0f + x);
+            }
+            if (a.z) {
+                const float sg = sigmoid(z[e]);
+                if (!ENDS) dg[e] = o[e] * sg * fmaf(z[e], 1.0f - sg, 1.0f);
+                o[e] *= z[e] * sg;
+            }
+            if (!there) { d[e] = 0.0f; o[e] = 0.0f; }
+        }
+        auto put = [&](float* p, const float (&v)[VV]) {
+            if constexpr (VV == 1) p[0] = v[0];
+            else {
+#pragma unroll
+                for (int e = 0; e < VV; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+            }
+        };
+        put(&sh.step[t][c], d);
+        put(&sh.e[t][c], o);
+        if (!ENDS) { put(&sh.u[t][c], u); put(&sh.dstep[t][c], ds); if (a.z) put(&sh.dgate[t][c], dg); }
+    }
+    ns.stage(&sh.bc[0][0][0], lane);
 }
 
-template <int SL> struct Forward {
-    typedef Old<SL> S;
-    float step[S::K][S::CH], in[S::K][S::CH];              // delta; delta u, then y
-    float B[S::K][S::NP], C[S::K][S::NP];
-};
+template <int SL> __device__ __forceinline__ void channel_params(const Scan& a, Backward<SL>& sh, uint32_t ch0, uint32_t have, int lane) {
+    for (int c = lane; c < Shape<SL>::CH; c += 32) {
+        sh.bias[c] = c < (int)have && a.dbias ? __ldg(a.dbias + ch0 + c) : 0.0f;
+        sh.skip[c] = c < (int)have && a.Dk ? __ldg(a.Dk + ch0 + c) : 0.0f;
+    }
+}
+// the lane's 4 x 4 values of an array [channel][state], channels 2 j and 2 j + 1 side by side
+__device__ __forceinline__ void load_states(f2 (&v)[2][4], const float* p, const Scan& a, uint32_t ch0, uint32_t have, int cl, int sl, float scale) {
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+        float x[2][4];
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const uint32_t c = cl * 4 + 2 * j + k;
+            const float* q = p + (size_t)(ch0 + c) * a.N + sl * 4;
+#pragma unroll
+            for (int n = 0; n < 4; n++) x[k][n] = 0.0f;
+            if (p && c < have) {
+                if (a.n4 && ((uintptr_t)q & 15u) == 0) { if (sl * 4 < (int)a.N) { const float4 w = *reinterpret_cast<const float4*>(q); x[k][0] = w.x; x[k][1] = w.y; x[k][2] = w.z; x[k][3] = w.w; } }
+                else {
+#pragma unroll
+                    for (int n = 0; n < 4; n++) if (sl * 4 + n < (int)a.N) x[k][n] = q[n];
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < 4; n++) v[j][n] = pack2(x[0][n] * scale, x[1][n] * scale);
+    }
+}
+__device__ __forceinline__ void store_states(const f2 (&v)[2][4], float* p, size_t ld, const Scan& a, uint32_t ch0, uint32_t have, int cl, int sl) {
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int n = 0; n < 4; n++) {
+            float x, y;
+            unpack2(v[j][n], x, y);
+            const uint32_t c = cl * 4 + 2 * j;
+            if (sl * 4 + n >= (int)a.N) continue;
+            if (c < have) p[(size_t)(ch0 + c) * ld + sl * 4 + n] = x;
+            if (c + 1 < have) p[(size_t)(ch0 + c + 1) * ld + sl * 4 + n] = y;
+        }
+}
 
-// ---- backward --------------------------------------------------------------------------------------------------------------------------
-// ENDS of the backward pass: the gradient at a part's first state that the part's own rows cause, and the sum of its steps.
+// Parts: the gradient at a part's first state that the part's own rows cause, and the sum of its steps.
 template <typename T, int SL, int VV>
 __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
     sf_chain_enter();
-    typedef Old<SL> S;
-    constexpr int K = S::K, CH = S::CH, NP = S::NP, VR = CH / VV, I = S::E / VV, NB = VR > 32 ? VR / 32 : 1, VL = VR < 32 ? VR : 32;
+    constexpr int CH = Shape<SL>::CH;
     extern __shared__ __align__(16) unsigned char shared[];
-    Forward<SL>& sh = reinterpret_cast<Forward<SL>*>(shared)[threadIdx.x / 32];
+    Backward<SL>& sh = reinterpret_cast<Backward<SL>*>(shared)[threadIdx.x / 32];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
     const uint64_t item = (uint64_t)blockIdx.x * kWarps + threadIdx.x / 32, warps = (uint64_t)a.G * a.cwarps;
     if (item >= warps * a.q.n_seq) return;
@@ -45,349 +140,266 @@ __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
     const Range r = range_of(a.q, s, a.st);
     const uint32_t part = blockIdx.y, t_begin = part * a.part_len, t_end = min(r.len, t_begin + a.part_len);
     if (t_begin >= r.len) return;
-    float A[4][4], h[4][4];
+    f2 A[2][4], G[2][4], steps[2] = {0, 0};
+    load_states(A, a.A, a, ch0, have, cl, sl, kLog2e);
 #pragma unroll
-    for (int j = 0; j < 4; j++)
+    for (int j = 0; j < 2; j++)
 #pragma unroll
-        for (int n = 0; n < 4; n++) {
-            const uint32_t c = cl * 4 + j, st = sl * 4 + n;
-            A[j][n] = c < have && st < a.N ? __ldg(a.A + (size_t)(ch0 + c) * a.N + st) * kLog2e : 0.0f;
-            h[j][n] = 0.0f;
-        }
-    float bias[NB][VV], steps[NB][VV];
-#pragma unroll
-    for (int b = 0; b < NB; b++)
-#pragma unroll
-        for (int e = 0; e < VV; e++) {
-            const uint32_t c = (b * 32 + lane % VL) * VV + e;
-            bias[b][e] = c < have && a.dbias ? __ldg(a.dbias + ch0 + c) : 0.0f;
-            steps[b][e] = 0.0f;
-        }
-    const uint32_t tiles = (t_end - t_begin + K - 1) / K;
-    for (uint32_t tile = tiles; tile-- > 0;) {
+        for (int n = 0; n < 4; n++) G[j][n] = 0;
+    channel_params<SL>(a, sh, ch0, have, lane);
+    __syncwarp();
+    for (uint32_t tile = (t_end - t_begin + K - 1) / K; tile-- > 0;) {
         const uint32_t t0 = t_begin + tile * K;
-        const int rows = (int)min((uint32_t)K, t_end - t0);
-        const size_t row0 = (size_t)r.first + t0;
-#pragma unroll
-        for (int i = 0; i < I; i++) {
-            const int t = (i * 32 + lane) / VR, b = i % NB, vc = (b * 32 + lane % VL) * VV;
-            const bool vthere = vc < (int)have;
-            const bool there = vthere && t < rows;
-            float d[VV], e_[VV], z[VV];
-            open<T, VV>(fetch<T, VV>(a.delta, (row0 + t) * a.lddelta + ch0 + vc, there), d);
-            open<T, VV>(fetch<T, VV>(a.dy, (row0 + t) * a.lddy + ch0 + vc, there), e_);
-            if (a.z) open<T, VV>(fetch<T, VV>(a.z, (row0 + t) * a.ldz + ch0 + vc, there), z);
-#pragma unroll
-            for (int e = 0; e < VV; e++) {
-                float unused;
-                d[e] += bias[b][e];
-                if (a.softplus) d[e] = softplus_of(d[e], unused);
-                if (!there) d[e] = 0.0f;
-                if (a.z) e_[e] *= z[e] * sigmoid(z[e]);
-                steps[b][e] += d[e];
-                sh.step[t][vc + e] = d[e];
-                sh.in[t][vc + e] = there ? e_[e] : 0.0f;
-            }
-        }
-        stage_states<T, VV, K, NP>(&sh.C[0][0], a.C, a.ldc, row0, g * a.N, a.N, rows, lane);
+        stage<T, SL, VV, true>(a, sh, (size_t)r.first + t0, ch0, have, g, (int)min((uint32_t)K, t_end - t0), lane);
         __syncwarp();
-        for (int t = rows - 1; t >= 0; t--) {
-            const float4 d4 = *reinterpret_cast<const float4*>(&sh.step[t][cl * 4]), i4 = *reinterpret_cast<const float4*>(&sh.in[t][cl * 4]);
-            const float4 c4 = *reinterpret_cast<const float4*>(&sh.C[t][sl * 4]);
-            const float d[4] = {d4.x, d4.y, d4.z, d4.w}, in[4] = {i4.x, i4.y, i4.z, i4.w}, c[4] = {c4.x, c4.y, c4.z, c4.w};
 #pragma unroll
-            for (int j = 0; j < 4; j++)
+        for (int t = K - 1; t >= 0; t--) {
+            const ulonglong2 d2 = *reinterpret_cast<const ulonglong2*>(&sh.step[t][cl * 4]), e2 = *reinterpret_cast<const ulonglong2*>(&sh.e[t][cl * 4]);
+            const float4 c4 = *reinterpret_cast<const float4*>(&sh.bc[1][t][sl * 4]);
+            const f2 d[2] = {d2.x, d2.y}, e[2] = {e2.x, e2.y}, c[4] = {dup2(c4.x), dup2(c4.y), dup2(c4.z), dup2(c4.w)};
 #pragma unroll
-                for (int n = 0; n < 4; n++) h[j][n] = decay(d[j], A[j][n]) * fmaf(in[j], c[n], h[j][n]);
+            for (int j = 0; j < 2; j++) {
+                steps[j] = add2(steps[j], d[j]);
+#pragma unroll
+                for (int n = 0; n < 4; n++) G[j][n] = mul2(decay2(d[j], A[j][n]), fma2(e[j], c[n], G[j][n]));
+            }
         }
         __syncwarp();
     }
-    float* out = a.part_state + ((size_t)s * a.parts + part) * a.D * a.N;
+    store_states(G, a.part_state + ((size_t)s * a.parts + part) * a.D * a.N, a.N, a, ch0, have, cl, sl);
+    if (sl == 0) {
 #pragma unroll
-    for (int j = 0; j < 4; j++)
-#pragma unroll
-        for (int n = 0; n < 4; n++)
-            if (cl * 4 + j < (int)have && sl * 4 + n < (int)a.N) out[(size_t)(ch0 + cl * 4 + j) * a.N + sl * 4 + n] = h[j][n];
-#pragma unroll
-    for (int b = 0; b < NB; b++)
-#pragma unroll
-        for (int e = 0; e < VV; e++) {
-            const uint32_t c = (b * 32 + lane % VL) * VV + e;
-            for (int m = VR; m < 32; m <<= 1) steps[b][e] += __shfl_xor_sync(0xFFFFFFFFu, steps[b][e], m);
-            if (lane < VR && c < have) a.part_step[((size_t)s * a.parts + part) * a.D + ch0 + c] = steps[b][e];
+        for (int j = 0; j < 2; j++) {
+            float x, y;
+            unpack2(steps[j], x, y);
+            float* p = a.part_step + ((size_t)s * a.parts + part) * a.D + ch0 + cl * 4 + 2 * j;
+            if (cl * 4 + 2 * j < (int)have) p[0] = x;
+            if (cl * 4 + 2 * j + 1 < (int)have) p[1] = y;
         }
+    }
 }
 
-template <int SL> struct Backward {
-    typedef Old<SL> S;
-    static constexpr int K = S::K, Q = K / 4;              // rows of a tile, groups of 4 rows
-    float step[K][S::CH], u[K][S::CH], e[K][S::CH], y[K][S::CH];      // delta, u, dout silu(z); y
-    float s1[K][S::CH], s2[K][S::CH];                      // sum g B; sum (a g) h_{t-1} A
-    float B[K][S::NP], C[K][S::NP];
-    float4 start[Q][4][32];                                // states before each group of 4 rows
-    float sum[K][2][S::NP];                                // the warp's dB, dC
-};
-
-// Sums of 32 values v[i] over the CL lanes that differ in cl; lane cl ends up with the 32 / CL sums i = cl * (32 / CL) ..
-template <int SL> __device__ __forceinline__ void sum_channels(float (&v)[32], int lane) {
-    int n = 32;
+// The sums over the SL state lanes of the four values of v: with SL >= 4 lane sl gets channel 2 (sl & 1) + (sl >> 1 & 1) of the lane's four; put writes them.
+template <int SL> __device__ __forceinline__ void put_sum(float* p, f2 (&v)[2], int sl) {
+    if constexpr (SL == 1) *reinterpret_cast<ulonglong2*>(p) = make_ulonglong2(v[0], v[1]);
+    else {
+        const bool hi = sl & 1;
+        const f2 keep = hi ? v[1] : v[0], give = hi ? v[0] : v[1];
+        const f2 w = add2(keep, __shfl_xor_sync(0xFFFFFFFFu, give, 1));
+        if constexpr (SL == 2) *reinterpret_cast<f2*>(p + 2 * sl) = w;
+        else {
+            float x, y;
+            unpack2(w, x, y);
+            const bool up = sl & 2;
+            float z = (up ? y : x) + __shfl_xor_sync(0xFFFFFFFFu, up ? x : y, 2);
+#pragma unroll
+            for (int m = 4; m < SL; m <<= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, m);
+            if (SL == 4 || sl < 4) p[2 * (sl & 1) + (sl >> 1 & 1)] = z;
+        }
+    }
+}
+// Sums of 8 values over the CL channel lanes; they end up in lane cl as the 8 / CL (at least one) values from index (cl * 8 / CL) % 8 on; put writes
+// them to p[value / 4][state]
+template <int SL> __device__ __forceinline__ void put_states(float* p0, float* p1, float (&v)[8], int lane, int cl, int sl) {
+    int n = 8;
 #pragma unroll
     for (int m = 16; m >= SL; m >>= 1) {
-        n >>= 1;
-        const bool hi = lane & m;
+        if (n > 1) {
+            n >>= 1;
+            const bool hi = lane & m;
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            if (i >= n) break;
-            const float keep = hi ? v[i + n] : v[i], give = hi ? v[i] : v[i + n];
-            v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, m);
-        }
+            for (int i = 0; i < 4; i++) {
+                if (i >= n) break;
+                const float keep = hi ? v[i + n] : v[i], give = hi ? v[i] : v[i + n];
+                v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, m);
+            }
+        } else v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], m);
+    }
+    constexpr int CL = 32 / SL, NV = CL >= 8 ? 1 : 8 / CL, SAME = CL > 8 ? CL / 8 : 1;       // values a lane has, lanes that have the same
+    if (cl % SAME) return;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        const int k = cl / SAME * NV + i;
+        (k < 4 ? p0 : p1)[sl * 4 + k % 4] = v[i];
     }
 }
 
 // One block: up to kWarps warps over neighbouring channels of a group, one part of one sequence after the other (a run), rows from last to first.
+// A tile's states are stepped from the state kept before it: rows 0 to 3 to reach row 4, rows 4 to 7 with decays and states held in registers, back over
+// them, then rows 0 to 3 the same way.
 template <typename T, int SL, int VV>
 __global__ void __launch_bounds__(32 * kWarps) back_kernel(const Scan a) {
     sf_chain_enter();
-    typedef Old<SL> S;
-    typedef Backward<SL> Sh;
-    constexpr int K = S::K, CH = S::CH, NP = S::NP, VR = CH / VV, I = S::E / VV, NB = VR > 32 ? VR / 32 : 1, VL = VR < 32 ? VR : 32, Q = Sh::Q, CL = S::CL;
+    typedef Shape<SL> S;
+    typedef Pieces<K, S::CH, VV> P;
+    constexpr int CH = S::CH, I = P::I;
     extern __shared__ __align__(16) unsigned char shared[];
-    Sh* all = reinterpret_cast<Sh*>(shared);
+    Backward<SL>* all = reinterpret_cast<Backward<SL>*>(shared);
     const int warp = threadIdx.x / 32, warps = blockDim.x / 32;
-    Sh& sh = all[warp];
+    Backward<SL>& sh = all[warp];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
     const uint32_t gb = blockIdx.x, g = gb / a.cblocks, cb = gb % a.cblocks;
     const uint32_t c0 = min(a.per, (cb * (uint32_t)kWarps + warp) * CH);
     const uint32_t ch0 = g * a.per + c0, have = min((uint32_t)CH, a.per - c0);     // (a warp behind the group's last channel has none, but meets the others)
-    float A[4][4], dA[4][4];
+    const P pc(lane);
+    f2 A[2][4], dA[2][4], G[2][4];
+    load_states(A, a.A, a, ch0, have, cl, sl, kLog2e);
+    float dD[I][VV], db[I][VV];                            // of the channels that this lane's pieces have
 #pragma unroll
-    for (int j = 0; j < 4; j++)
+    for (int j = 0; j < 2; j++)
 #pragma unroll
-        for (int n = 0; n < 4; n++) {
-            const uint32_t c = cl * 4 + j, st = sl * 4 + n;
-            A[j][n] = c < have && st < a.N ? __ldg(a.A + (size_t)(ch0 + c) * a.N + st) * kLog2e : 0.0f;
-            dA[j][n] = 0.0f;
-        }
-    float bias[NB][VV], Dk[NB][VV], dD[NB][VV], db[NB][VV];
+        for (int n = 0; n < 4; n++) dA[j][n] = 0;
 #pragma unroll
-    for (int b = 0; b < NB; b++)
+    for (int i = 0; i < I; i++)
 #pragma unroll
-        for (int e = 0; e < VV; e++) {
-            const uint32_t c = (b * 32 + lane % VL) * VV + e;
-            bias[b][e] = c < have && a.dbias ? __ldg(a.dbias + ch0 + c) : 0.0f;
-            Dk[b][e] = c < have && a.Dk ? __ldg(a.Dk + ch0 + c) : 0.0f;
-            dD[b][e] = db[b][e] = 0.0f;
-        }
+        for (int e = 0; e < VV; e++) dD[i][e] = db[i][e] = 0.0f;
+    channel_params<SL>(a, sh, ch0, have, lane);
+    __syncwarp();
     const uint64_t items = (uint64_t)a.q.n_seq * a.parts;
     for (uint64_t it = blockIdx.y; it < items; it += a.runs) {
-        const uint32_t s = (uint32_t)(it / a.parts), part = (uint32_t)(it % a.parts);
+        const uint32_t part = (uint32_t)(it / a.q.n_seq), s = (uint32_t)(it % a.q.n_seq);
         const Range r = range_of(a.q, s, a.st);
         const uint32_t t_begin = part * a.part_len, t_end = min(r.len, t_begin + a.part_len);
         const bool whole = a.part_state == nullptr;        // the sequence in one part: gradients of states here
         if (t_begin >= r.len && !(whole && a.d_state0 && r.slot >= 0)) continue;
-        float G[4][4];
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-#pragma unroll
-            for (int n = 0; n < 4; n++) {
-                const uint32_t c = cl * 4 + j, st = sl * 4 + n;
-                const size_t at = (size_t)(ch0 + c) * a.N + st;
-                G[j][n] = 0.0f;
-                if (c < have && st < a.N) {
-                    if (!whole) G[j][n] = a.part_state[((size_t)s * a.parts + part) * a.D * a.N + at];
-                    else if (a.d_state && r.slot >= 0) G[j][n] = a.d_state[(size_t)r.slot * a.D * a.N + at];
-                }
-            }
+        const size_t DN = (size_t)a.D * a.N;
+        load_states(G, whole ? (a.d_state && r.slot >= 0 ? a.d_state + (size_t)r.slot * DN : nullptr) : a.part_state + ((size_t)s * a.parts + part) * DN, a, ch0, have, cl, sl, 1.0f);
         const uint32_t tiles = t_end > t_begin ? (t_end - t_begin + K - 1) / K : 0;
         for (uint32_t tile = tiles; tile-- > 0;) {
             const uint32_t t0 = t_begin + tile * K;
             const int rows = (int)min((uint32_t)K, t_end - t0);
             const size_t row0 = (size_t)r.first + t0;
-            // the state before the tile: kept every kEvery rows, stepped on from there where tiles are shorter
-            float h[4][4];
-            const uint32_t kept = t0 / kEvery * kEvery;
-            {
-                const float* p = a.starts + start_index(r.first, s, kept) * a.D * a.N;
+            f2 h[2][4];
+            load_states(h, a.starts + start_index(r.first, s, t0) * DN, a, ch0, have, cl, sl, 1.0f);
+            stage<T, SL, VV, false>(a, sh, row0, ch0, have, g, rows, lane);
+            __syncwarp();
+            auto keep = [&](int q) {
 #pragma unroll
-                for (int j = 0; j < 4; j++)
+                for (int j = 0; j < 2; j++)
+#pragma unroll
+                    for (int n = 0; n < 4; n += 2) *reinterpret_cast<ulonglong2*>(&sh.start[q][2 * j + n / 2][lane]) = make_ulonglong2(h[j][n], h[j][n + 1]);
+            };
+            auto take = [&](f2 (&v)[2][4], int q) {
+#pragma unroll
+                for (int j = 0; j < 2; j++)
+#pragma unroll
+                    for (int n = 0; n < 4; n += 2) { const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&sh.start[q][2 * j + n / 2][lane]); v[j][n] = w.x; v[j][n + 1] = w.y; }
+            };
+            keep(0);
+#pragma unroll
+            for (int t = 0; t < 4; t++) {
+                const ulonglong2 d2 = *reinterpret_cast<const ulonglong2*>(&sh.step[t][cl * 4]), u2 = *reinterpret_cast<const ulonglong2*>(&sh.u[t][cl * 4]);
+                const float4 b4 = *reinterpret_cast<const float4*>(&sh.bc[0][t][sl * 4]);
+                const f2 d[2] = {d2.x, d2.y}, in[2] = {mul2(d2.x, u2.x), mul2(d2.y, u2.y)}, b[4] = {dup2(b4.x), dup2(b4.y), dup2(b4.z), dup2(b4.w)};
+#pragma unroll
+                for (int j = 0; j < 2; j++)
+#pragma unroll
+                    for (int n = 0; n < 4; n++) h[j][n] = fma2(decay2(d[j], A[j][n]), h[j][n], mul2(in[j], b[n]));
+            }
+            keep(1);
+#pragma unroll 1
+            for (int q = 1; q >= 0; q--) {
+                f2 al[4][2][4], hs[5][2][4];               // decays; states before the rows and after them
+                take(hs[0], q);
+#pragma unroll
+                for (int t = 0; t < 4; t++) {
+                    const int tt = 4 * q + t;
+                    const ulonglong2 d2 = *reinterpret_cast<const ulonglong2*>(&sh.step[tt][cl * 4]), u2 = *reinterpret_cast<const ulonglong2*>(&sh.u[tt][cl * 4]);
+                    const float4 b4 = *reinterpret_cast<const float4*>(&sh.bc[0][tt][sl * 4]);
+                    const f2 d[2] = {d2.x, d2.y}, in[2] = {mul2(d2.x, u2.x), mul2(d2.y, u2.y)}, b[4] = {dup2(b4.x), dup2(b4.y), dup2(b4.z), dup2(b4.w)};
+#pragma unroll
+                    for (int j = 0; j < 2; j++)
+#pragma unroll
+                        for (int n = 0; n < 4; n++) { al[t][j][n] = decay2(d[j], A[j][n]); hs[t + 1][j][n] = fma2(al[t][j][n], hs[t][j][n], mul2(in[j], b[n])); }
+                }
+#pragma unroll
+                for (int t = 3; t >= 0; t--) {
+                    const int tt = 4 * q + t;
+                    const ulonglong2 d2 = *reinterpret_cast<const ulonglong2*>(&sh.step[tt][cl * 4]), u2 = *reinterpret_cast<const ulonglong2*>(&sh.u[tt][cl * 4]), e2 = *reinterpret_cast<const ulonglong2*>(&sh.e[tt][cl * 4]);
+                    const float4 b4 = *reinterpret_cast<const float4*>(&sh.bc[0][tt][sl * 4]), c4 = *reinterpret_cast<const float4*>(&sh.bc[1][tt][sl * 4]);
+                    const f2 d[2] = {d2.x, d2.y}, in[2] = {mul2(d2.x, u2.x), mul2(d2.y, u2.y)}, e[2] = {e2.x, e2.y};
+                    const f2 b[4] = {dup2(b4.x), dup2(b4.y), dup2(b4.z), dup2(b4.w)}, c[4] = {dup2(c4.x), dup2(c4.y), dup2(c4.z), dup2(c4.w)};
+                    f2 dB[4], dC[4], s1[2], s2[2], y[2];
+#pragma unroll
+                    for (int j = 0; j < 2; j++)
+#pragma unroll
+                        for (int n = 0; n < 4; n++) {
+                            const f2 gt = fma2(e[j], c[n], G[j][n]);
+                            dB[n] = j ? fma2(gt, in[j], dB[n]) : mul2(gt, in[j]);
+                            dC[n] = j ? fma2(e[j], hs[t + 1][j][n], dC[n]) : mul2(e[j], hs[t + 1][j][n]);
+                            s1[j] = n ? fma2(gt, b[n], s1[j]) : mul2(gt, b[n]);
+                            G[j][n] = mul2(gt, al[t][j][n]);
+                            const f2 x = mul2(G[j][n], hs[t][j][n]);
+                            s2[j] = n ? fma2(x, A[j][n], s2[j]) : mul2(x, A[j][n]);
+                            dA[j][n] = fma2(x, d[j], dA[j][n]);
+                            y[j] = n ? fma2(hs[t + 1][j][n], c[n], y[j]) : mul2(hs[t + 1][j][n], c[n]);
+                        }
+                    put_sum<SL>(&sh.s1[tt][cl * 4], s1, sl);
+                    put_sum<SL>(&sh.s2[tt][cl * 4], s2, sl);
+                    if (a.z) put_sum<SL>(&sh.y[tt][cl * 4], y, sl);
+                    float v[8];
 #pragma unroll
                     for (int n = 0; n < 4; n++) {
-                        const uint32_t c = cl * 4 + j, st = sl * 4 + n;
-                        h[j][n] = c < have && st < a.N ? p[(size_t)(ch0 + c) * a.N + st] : 0.0f;
+                        float x, w;
+                        unpack2(dB[n], x, w); v[n] = x + w;
+                        unpack2(dC[n], x, w); v[4 + n] = x + w;
                     }
-            }
-            Piece<T, VV> pz[I], pg[I];
-            for (uint32_t tt = kept; tt <= t0; tt += K) {
-                const bool last = tt == t0;
-                const int rr = last ? rows : K;
-                const size_t row = (size_t)r.first + tt;
-#pragma unroll
-                for (int i = 0; i < I; i++) {
-                    const int t = (i * 32 + lane) / VR, b = i % NB, vc = (b * 32 + lane % VL) * VV;
-                    const bool vthere = vc < (int)have;
-                    const bool there = vthere && t < rr;
-                    float d[VV], u[VV], e_[VV], z[VV];
-                    open<T, VV>(fetch<T, VV>(a.delta, (row + t) * a.lddelta + ch0 + vc, there), d);
-                    open<T, VV>(fetch<T, VV>(a.u, (row + t) * a.ldu + ch0 + vc, there), u);
-                    pg[i] = fetch<T, VV>(a.dy, (row + t) * a.lddy + ch0 + vc, there);
-                    open<T, VV>(pg[i], e_);
-                    if (a.z) { pz[i] = fetch<T, VV>(a.z, (row + t) * a.ldz + ch0 + vc, there); open<T, VV>(pz[i], z); }
-#pragma unroll
-                    for (int e = 0; e < VV; e++) {
-                        float unused;
-                        d[e] += bias[b][e];
-                        if (a.softplus) d[e] = softplus_of(d[e], unused);
-                        if (a.z) e_[e] *= z[e] * sigmoid(z[e]);
-                        sh.step[t][vc + e] = there ? d[e] : 0.0f;
-                        sh.u[t][vc + e] = u[e];
-                        sh.e[t][vc + e] = there ? e_[e] : 0.0f;
-                    }
-                }
-                stage_states<T, VV, K, NP>(&sh.B[0][0], a.B, a.ldb, row, g * a.N, a.N, rr, lane);
-                stage_states<T, VV, K, NP>(&sh.C[0][0], a.C, a.ldc, row, g * a.N, a.N, rr, lane);
-                __syncwarp();
-                for (int t = 0; t < K; t++) {              // (rows that are not there: step 0, nothing comes in)
-                    if (t % 4 == 0) {
-#pragma unroll
-                        for (int j = 0; j < 4; j++) sh.start[t / 4][j][lane] = make_float4(h[j][0], h[j][1], h[j][2], h[j][3]);
-                    }
-                    const float4 d4 = *reinterpret_cast<const float4*>(&sh.step[t][cl * 4]), u4 = *reinterpret_cast<const float4*>(&sh.u[t][cl * 4]);
-                    const float4 b4 = *reinterpret_cast<const float4*>(&sh.B[t][sl * 4]), c4 = *reinterpret_cast<const float4*>(&sh.C[t][sl * 4]);
-                    const float d[4] = {d4.x, d4.y, d4.z, d4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w}, b[4] = {b4.x, b4.y, b4.z, b4.w};
-                    float y[4];
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const float in = d[j] * u[j];
-#pragma unroll
-                        for (int n = 0; n < 4; n++) h[j][n] = fmaf(decay(d[j], A[j][n]), h[j][n], in * b[n]);
-                        y[j] = h[j][0] * c4.x + h[j][1] * c4.y + h[j][2] * c4.z + h[j][3] * c4.w;
-                    }
-                    if (a.z) { sum_states<SL>(y, sl); put_states<SL>(&sh.y[t][cl * 4], y, sl); }
-                }
-                __syncwarp();
-            }
-            // groups of 4 rows from the last to the first; within a group channel by channel
-            for (int q = Q - 1; q >= 0; q--) {
-                float bc[32];                              // [row][dB, dC][state]
-#pragma unroll
-                for (int i = 0; i < 32; i++) bc[i] = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    float ha[4][4], al[4][4], hp[4];
-                    const float4 s4 = sh.start[q][j][lane];
-                    hp[0] = s4.x; hp[1] = s4.y; hp[2] = s4.z; hp[3] = s4.w;
-#pragma unroll
-                    for (int t = 0; t < 4; t++) {
-                        const float d = sh.step[4 * q + t][cl * 4 + j], in = d * sh.u[4 * q + t][cl * 4 + j];
-                        const float4 b4 = *reinterpret_cast<const float4*>(&sh.B[4 * q + t][sl * 4]);
-                        const float b[4] = {b4.x, b4.y, b4.z, b4.w};
-#pragma unroll
-                        for (int n = 0; n < 4; n++) {
-                            al[t][n] = decay(d, A[j][n]);
-                            ha[t][n] = fmaf(al[t][n], t ? ha[t - 1][n] : hp[n], in * b[n]);
-                        }
-                    }
-                    float s1[4], s2[4];
-#pragma unroll
-                    for (int t = 3; t >= 0; t--) {
-                        const float d = sh.step[4 * q + t][cl * 4 + j], in = d * sh.u[4 * q + t][cl * 4 + j], e = sh.e[4 * q + t][cl * 4 + j];
-                        const float4 b4 = *reinterpret_cast<const float4*>(&sh.B[4 * q + t][sl * 4]), c4 = *reinterpret_cast<const float4*>(&sh.C[4 * q + t][sl * 4]);
-                        const float b[4] = {b4.x, b4.y, b4.z, b4.w}, c[4] = {c4.x, c4.y, c4.z, c4.w};
-                        s1[t] = s2[t] = 0.0f;
-#pragma unroll
-                        for (int n = 0; n < 4; n++) {
-                            const float gt = fmaf(e, c[n], G[j][n]);
-                            bc[t * 8 + n] = fmaf(gt, in, bc[t * 8 + n]);
-                            bc[t * 8 + 4 + n] = fmaf(e, ha[t][n], bc[t * 8 + 4 + n]);
-                            s1[t] = fmaf(gt, b[n], s1[t]);
-                            G[j][n] = gt * al[t][n];
-                            const float x = G[j][n] * (t ? ha[t - 1][n] : hp[n]);
-                            s2[t] = fmaf(x, A[j][n], s2[t]);
-                            dA[j][n] = fmaf(x, d, dA[j][n]);
-                        }
-                    }
-                    sum_states<SL>(s1, sl);
-                    sum_states<SL>(s2, sl);
-                    // (here the four values are rows, not channels)
-                    if constexpr (SL == 1) {
-#pragma unroll
-                        for (int t = 0; t < 4; t++) { sh.s1[4 * q + t][cl * 4 + j] = s1[t]; sh.s2[4 * q + t][cl * 4 + j] = s2[t]; }
-                    } else if constexpr (SL == 2) {
-#pragma unroll
-                        for (int t = 0; t < 2; t++) { sh.s1[4 * q + 2 * sl + t][cl * 4 + j] = s1[t]; sh.s2[4 * q + 2 * sl + t][cl * 4 + j] = s2[t]; }
-                    } else if (sl < 4) {
-                        const int t = 2 * (sl & 1) + (sl >> 1 & 1);
-                        sh.s1[4 * q + t][cl * 4 + j] = s1[0]; sh.s2[4 * q + t][cl * 4 + j] = s2[0];
-                    }
-                }
-                sum_channels<SL>(bc, lane);
-                constexpr int P = 32 / CL;                 // = SL
-                // sum_channels halves by the highest lane bit first, so lane cl holds values rev .. : value index = cl * P + i
-#pragma unroll
-                for (int i = 0; i < P; i++) {
-                    const int v = cl * P + i;
-                    sh.sum[4 * q + v / 8][v / 4 & 1][sl * 4 + v % 4] = bc[i];
+                    put_states<SL>(sh.sum[tt][0], sh.sum[tt][1], v, lane, cl, sl);
                 }
             }
             __syncwarp();
+            const size_t at = row0 + pc.lt;
 #pragma unroll
             for (int i = 0; i < I; i++) {
-                const int t = (i * 32 + lane) / VR, b = i % NB, vc = (b * 32 + lane % VL) * VV;
-                const bool vthere = vc < (int)have;
-                if (!(vthere && t < rows)) continue;
-                float du[VV], dd[VV], dzv[VV], z[VV], gy[VV], raw[VV];
-                open<T, VV>(pg[i], gy);
-                if (a.z) open<T, VV>(pz[i], z);
-                open<T, VV>(fetch<T, VV>(a.delta, (row0 + t) * a.lddelta + ch0 + vc, a.softplus), raw);
+                const int t = pc.t(i), c = pc.c(i);
+                if (t >= rows || c >= (int)have) continue;
+                float du[VV], dd[VV], dz[VV];
 #pragma unroll
                 for (int e = 0; e < VV; e++) {
-                    const float step = sh.step[t][vc + e], u = sh.u[t][vc + e], ee = sh.e[t][vc + e], s1 = sh.s1[t][vc + e];
-                    du[e] = fmaf(Dk[b][e], ee, step * s1);
-                    dd[e] = fmaf(u, s1, kLn2 * sh.s2[t][vc + e]);
-                    if (a.softplus) dd[e] *= sigmoid(raw[e] + bias[b][e]);
-                    dD[b][e] = fmaf(ee, u, dD[b][e]);
-                    db[b][e] += dd[e];
-                    if (a.z) { const float sg = sigmoid(z[e]); dzv[e] = gy[e] * fmaf(Dk[b][e], u, sh.y[t][vc + e]) * sg * (1.0f + z[e] * (1.0f - sg)); }
+                    const float step = sh.step[t][c + e], u = sh.u[t][c + e], o = sh.e[t][c + e], s1 = sh.s1[t][c + e], skip = sh.skip[c + e];
+                    du[e] = fmaf(skip, o, step * s1);
+                    dd[e] = fmaf(u, s1, kLn2 * sh.s2[t][c + e]) * sh.dstep[t][c + e];
+                    dD[i][e] = fmaf(o, u, dD[i][e]);
+                    db[i][e] += dd[e];
+                    dz[e] = a.z ? fmaf(skip, u, sh.y[t][c + e]) * sh.dgate[t][c + e] : 0.0f;
                 }
-                if (a.du) store_word<T, VV>((T*)a.du + (row0 + t) * a.lddu + ch0 + vc, du);
-                if (a.ddelta) store_word<T, VV>((T*)a.ddelta + (row0 + t) * a.ldddelta + ch0 + vc, dd);
-                if (a.dz) store_word<T, VV>((T*)a.dz + (row0 + t) * a.lddz + ch0 + vc, dzv);
+                if (a.du) store_word<T, VV>((T*)a.du + at * a.lddu + ch0 + pc.lc + P::step(i, a.lddu), du);
+                if (a.ddelta) store_word<T, VV>((T*)a.ddelta + at * a.ldddelta + ch0 + pc.lc + P::step(i, a.ldddelta), dd);
+                if (a.dz) store_word<T, VV>((T*)a.dz + at * a.lddz + ch0 + pc.lc + P::step(i, a.lddz), dz);
             }
             // dB and dC: the block's warps, in their order
             __syncthreads();
-            for (int i = threadIdx.x; i < rows * 2 * (int)a.N; i += blockDim.x) {
-                const int t = i / (2 * (int)a.N), k = i / (int)a.N % 2, n = i % (int)a.N;
-                float v = 0.0f;
-                for (int w = 0; w < warps; w++) v += all[w].sum[t][k][n];
+            for (int i = threadIdx.x; i < rows * 2 * S::NP; i += blockDim.x) {
+                const int t = i / (2 * S::NP), k = i / S::NP % 2, n = i % S::NP;
+                if (n >= (int)a.N) continue;
+                float v = all[0].sum[t][k][n];
+                for (int w = 1; w < warps; w++) v += all[w].sum[t][k][n];
                 if (a.sum_bc) a.sum_bc[((((size_t)cb * a.q.rows + row0 + t) * a.G + g) * 2 + k) * a.N + n] = v;
                 else if (k == 0) { if (a.dB) ((T*)a.dB)[(row0 + t) * a.lddb + g * a.N + n] = from_f32<T>(v); }
                 else if (a.dC) ((T*)a.dC)[(row0 + t) * a.lddc + g * a.N + n] = from_f32<T>(v);
             }
             __syncthreads();
         }
-        if (whole && a.d_state0 && r.slot >= 0) {
-#pragma unroll
-            for (int j = 0; j < 4; j++)
-#pragma unroll
-                for (int n = 0; n < 4; n++)
-                    if (cl * 4 + j < (int)have && sl * 4 + n < (int)a.N) a.d_state0[((size_t)r.slot * a.D + ch0 + cl * 4 + j) * a.N + sl * 4 + n] = G[j][n];
-        }
+        if (whole && a.d_state0 && r.slot >= 0) store_states(G, a.d_state0 + (size_t)r.slot * DN, a.N, a, ch0, have, cl, sl);
     }
-    if (!a.sum_par) return;
     float* par = a.sum_par + (size_t)blockIdx.y * a.D * (a.N + 2);
+    store_states(dA, par, a.N + 2, a, ch0, have, cl, sl);
+    // a channel's sums over the lanes that have pieces of it, by way of shared memory, in the order of the rows
 #pragma unroll
-    for (int j = 0; j < 4; j++)
+    for (int i = 0; i < I; i++) {
+        const int t = pc.t(i), c = pc.c(i);
+        if (t >= K) continue;
 #pragma unroll
-        for (int n = 0; n < 4; n++)
-            if (cl * 4 + j < (int)have && sl * 4 + n < (int)a.N) par[(size_t)(ch0 + cl * 4 + j) * (a.N + 2) + sl * 4 + n] = dA[j][n];
+        for (int e = 0; e < VV; e++) { sh.s1[t][c + e] = dD[i][e]; sh.s2[t][c + e] = db[i][e]; }
+    }
+    __syncwarp();
+    for (int c = lane; c < (int)have; c += 32) {
+        float x = 0.0f, y = 0.0f;
 #pragma unroll
-    for (int b = 0; b < NB; b++)
-#pragma unroll
-        for (int e = 0; e < VV; e++) {
-            const uint32_t c = (b * 32 + lane % VL) * VV + e;
-            for (int m = VR; m < 32; m <<= 1) { dD[b][e] += __shfl_xor_sync(0xFFFFFFFFu, dD[b][e], m); db[b][e] += __shfl_xor_sync(0xFFFFFFFFu, db[b][e], m); }
-            if (lane < VR && c < have) { par[(size_t)(ch0 + c) * (a.N + 2) + a.N] = dD[b][e]; par[(size_t)(ch0 + c) * (a.N + 2) + a.N + 1] = db[b][e]; }
-        }
+        for (int t = 0; t < K; t++) { x += sh.s1[t][c]; y += sh.s2[t][c]; }
+        par[(size_t)(ch0 + c) * (a.N + 2) + a.N] = x;
+        par[(size_t)(ch0 + c) * (a.N + 2) + a.N + 1] = y;
+    }
 }
 
 // dB and dC from the channel blocks' sums, in their order; rows of sequences only
@@ -455,10 +467,10 @@ extern "C" int sf_seq_scan_backward(sf_ctx* ctx, const sf_sequences* seq, const 
     return by_type(in->dtype, [&](auto zero) {
         typedef decltype(zero) T;
         return by_states(p.sl, [&](auto lanes) {
-            constexpr int SL = decltype(lanes)::value, VV = std::min(16 / (int)sizeof(T), Old<SL>::E);
+            constexpr int SL = decltype(lanes)::value, VV = 16 / (int)sizeof(T);
             int e = SF_OK;
             if (p.split) {
-                e = launch(vec ? back_ends_kernel<T, SL, VV> : back_ends_kernel<T, SL, 1>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, sizeof(Forward<SL>) * kWarps, st, a);
+                e = launch(vec ? back_ends_kernel<T, SL, VV> : back_ends_kernel<T, SL, 1>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, sizeof(Backward<SL>) * kWarps, st, a);
                 if (e == SF_OK) e = launch(parts_kernel<true>, dim3((uint32_t)(((uint64_t)in->D * in->N + 255) / 256), seq->n_seq), 256, 0, st, a);
                 if (e != SF_OK) return e;
             }
