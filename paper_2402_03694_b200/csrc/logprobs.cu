@@ -25,29 +25,29 @@ template <typename T> struct Rows {
     sf_dev_state* st;
 };
 
-// running statistics of a part of a row, in units of log2: w2 = w / ln 2
-struct Stat { float m, s, w; };                       // m = largest z seen (-FLT_MAX at first, so that nothing is infinite minus infinite)
-__device__ __forceinline__ Stat stat_none() { return {-FLT_MAX, 0.0f, 0.0f}; }
+// Running statistics of a part of a row, in units of log2 (w / ln 2).  m = largest entry seen (-FLT_MAX at first, so that nothing is infinite minus infinite).
+struct Stat { float m, s, w; };
 // brings (s, w) from maximum m to a larger one
 __device__ __forceinline__ void stat_raise(Stat& a, float m, float c) {
     const float d = (a.m - m) * c, f = ex2(d);
     a.w = a.s == 0.0f ? 0.0f : (a.w + a.s * d) * f;
     a.s *= f; a.m = m;
 }
-__device__ __forceinline__ Stat stat_join(Stat a, Stat b, float c) {
-    const float m = fmaxf(a.m, b.m);
-    stat_raise(a, m, c); stat_raise(b, m, c);
-    return {m, a.s + b.s, a.w + b.w};
-}
-// N values more, cm their maximum; masked ones (-infinity) add nothing, a NaN (or an infinity, minus itself) makes s a NaN
-template <int N> __device__ __forceinline__ void stat_add(Stat& a, const float (&v)[N], float cm, float c) {
-    if (cm > a.m) stat_raise(a, cm, c);
+// N entries more, none above m: masked ones (-infinity) add nothing, a NaN (or an infinity, minus itself) makes s a NaN
+template <int N> __device__ __forceinline__ void stat_add(Stat& a, const float (&v)[N], float c) {
+    const f2 m2 = dup2(-a.m), c2 = dup2(c);
+    f2 s = 0, w = 0;
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-        const float d = (v[i] - a.m) * c, e = ex2(d);
-        a.s += e;
-        a.w = fmaf(e, fmaxf(d, -1e4f), a.w);
+    for (int i = 0; i < N; i += 2) {
+        float x, y;
+        unpack2(mul2(add2(pack2(v[i], v[i + 1]), m2), c2), x, y);
+        const f2 e = pack2(ex2(x), ex2(y));
+        s = add2(s, e);
+        w = fma2(e, pack2(fmaxf(x, -1e4f), fmaxf(y, -1e4f)), w);
     }
+    float x, y;
+    unpack2(s, x, y); a.s += x + y;
+    unpack2(w, x, y); a.w += x + y;
 }
 template <int N> __device__ __forceinline__ float max_of(const float (&v)[N]) {
     float m = v[0];
@@ -106,9 +106,14 @@ template <typename T> __device__ __forceinline__ void load_chunk(const T* __rest
 }
 
 // ---- rows of up to 1024 entries: L lanes a row, C chunks a lane, the row in registers -----------------------------------------
+// Alternatives: one after the other, the largest entry that is left (of equals the lowest index); where a warp has the row and more than four are
+// asked, by a bound: the k-th largest of the lanes' own maxima is reached by k entries at least, and the entries that reach it are collected and ranked.
+constexpr uint32_t kWarpList = 128;                        // candidates of a warp
+
 template <typename T, int L, int C>
 __global__ void __launch_bounds__(kThreads) row_kernel(const Rows<T> a) {
     sf_chain_enter();
+    __shared__ uint64_t lists[C > 1 || L == 32 ? kThreads / 32 : 1][kWarpList];
     uint32_t n = a.n;
     if (a.n_dev) n = sf_clamp_rows(*a.n_dev, a.n, a.st);
     const uint32_t lane = threadIdx.x % L;
@@ -117,7 +122,7 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Rows<T> a) {
     const T* z = a.z + (live ? row : 0) * a.ld;
     float v[C][8];
     const float c = a.scale * kLog2e;
-    float m = -INFINITY;
+    float mine = -INFINITY;
 #pragma unroll
     for (int j = 0; j < C; j++) {
         const int i0 = (int)(lane + L * j) * 8;
@@ -126,192 +131,231 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Rows<T> a) {
 #pragma unroll
             for (int e = 0; e < 8; e++) v[j][e] = live && (uint32_t)(i0 + e) < a.V ? to_f32(z[i0 + e]) : -INFINITY;
         }
-        m = fmaxf(m, max_of(v[j]));
+        mine = fmaxf(mine, max_of(v[j]));
     }
+    float m = mine;
 #pragma unroll
     for (int d = L / 2; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-    Stat q = stat_none();
-    q.m = fmaxf(q.m, m);
+    Stat q = {fmaxf(m, -FLT_MAX), 0.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < C; j++) stat_add(q, v[j], -INFINITY, c);
+    for (int j = 0; j < C; j++) stat_add(q, v[j], c);
 #pragma unroll
     for (int d = L / 2; d; d >>= 1) { q.s += __shfl_xor_sync(0xFFFFFFFFu, q.s, d); q.w += __shfl_xor_sync(0xFFFFFFFFu, q.w, d); }
     const Answer r = answer_of(q, a.scale);
     if (live && lane == 0) write_row(a, (uint32_t)row, r);
-    uint64_t last = ~0ull;
-    for (uint32_t t = 0; t < a.k; t++) {                   // the best behind the last one picked
-        uint64_t best = 0;
+    if (a.k == 0) return;
+    if constexpr (L == 32) if (a.k > 4) {
+        uint32_t before = 0;
+        for (int o = 0; o < 32; o++) { const float x = __shfl_sync(0xFFFFFFFFu, mine, o); before += x > mine || (x == mine && o < (int)lane); }
+        const float bound = __shfl_sync(0xFFFFFFFFu, mine, __ffs(__ballot_sync(0xFFFFFFFFu, before == a.k - 1)) - 1);
+        uint64_t* list = lists[threadIdx.x / 32];
+        uint32_t found = 0;
 #pragma unroll
         for (int j = 0; j < C; j++)
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const uint64_t key = key_of(v[j][e], (lane + L * j) * 8 + e);
-                if (key < last && key > best) best = key;
+                const bool in = v[j][e] >= bound && v[j][e] > -INFINITY;
+                const uint32_t who = __ballot_sync(0xFFFFFFFFu, in);
+                if (who == 0) continue;
+                const uint32_t at = found + __popc(who & ((1u << lane) - 1));
+                if (in && at < kWarpList) list[at] = key_of(v[j][e], (lane + L * j) * 8 + e);
+                found += __popc(who);
             }
+        __syncwarp();
+        if (found <= kWarpList) {
+            for (uint32_t i = lane; i < found; i += 32) {
+                const uint64_t key = list[i];
+                uint32_t rank = 0;
+                for (uint32_t o = 0; o < found; o++) rank += list[o] > key;
+                if (live && rank < a.k) write_top(a, (uint32_t)row, rank, key, r);
+            }
+            for (uint32_t t = found + lane; t < a.k; t += 32) if (live) write_top(a, (uint32_t)row, t, 0, r);
+            return;
+        }
+    }
+    for (uint32_t t = 0; t < a.k; t++) {
+        if (t) {
+            m = -INFINITY;
 #pragma unroll
-        for (int d = L / 2; d; d >>= 1) { const uint64_t o = __shfl_xor_sync(0xFFFFFFFFu, best, d); best = o > best ? o : best; }
-        if (live && lane == 0) write_top(a, (uint32_t)row, t, best, r);
-        last = best;                                       // (none left: 0, behind which there is nothing)
+            for (int j = 0; j < C; j++) m = fmaxf(m, max_of(v[j]));
+#pragma unroll
+            for (int d = L / 2; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+        }
+        uint32_t at = 0xFFFFFFFFu;
+#pragma unroll
+        for (int j = C - 1; j >= 0; j--)
+#pragma unroll
+            for (int e = 7; e >= 0; e--) if (v[j][e] == m) at = (lane + L * j) * 8 + e;
+#pragma unroll
+        for (int d = L / 2; d; d >>= 1) at = min(at, __shfl_xor_sync(0xFFFFFFFFu, at, d));
+        if (live && lane == 0) write_top(a, (uint32_t)row, t, m > -INFINITY ? key_of(m, at) : 0, r);
+#pragma unroll
+        for (int j = 0; j < C; j++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) if ((lane + L * j) * 8 + e == at) v[j][e] = -INFINITY;
     }
 }
 
-// ---- longer rows: a block a row, or a cluster of blocks where rows are few ---------------------------------------------------------
-constexpr uint32_t kWide = 512;                            // threads of a block
-constexpr uint32_t kList = 1024;                           // candidates for the alternatives that a block collects
+// ---- longer rows: a block of TH threads a row, or a cluster of CL blocks where rows are few --------------------------------------
+// One pass over the row with a running maximum.  Alternatives: every thread knows the largest of its entries; the k-th largest of 64 groups' maxima is a
+// bound that at least k entries reach, and only entries of threads that reach it can be among the k best: their chunks alone are read
+// again (from L2), what reaches the bound is collected and ranked.  Many equals can overflow the list; then k searches over the row follow.
+constexpr uint32_t kList = 1024;                           // candidates that a block collects
+constexpr uint32_t kGroups = 64;
 
-__device__ __forceinline__ Stat block_stat(Stat q, float c, Stat* sh) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) {
-        const Stat o = {__shfl_xor_sync(0xFFFFFFFFu, q.m, d), __shfl_xor_sync(0xFFFFFFFFu, q.s, d), __shfl_xor_sync(0xFFFFFFFFu, q.w, d)};
-        q = stat_join(q, o, c);
-    }
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x / 32] = q;
-    __syncthreads();
-    q = sh[0];
-    for (uint32_t i = 1; i < kWide / 32; i++) q = stat_join(q, sh[i], c);
-    return q;
-}
+template <int TH> struct Shared {
+    float m[TH / 32], s[TH / 32], w[TH / 32];
+    float group[kGroups];
+    float bound;
+    uint32_t n_threads, n_list;
+    uint16_t thread[TH];
+    uint64_t list[kList];
+    uint64_t best[kMaxTop], merged[kMaxTop];
+    Stat part;
+};
 
-// Alternatives of the block's part of the row.  Every thread knows the largest of its entries; the k-th largest of those is a bound that
-// at least k entries reach, and only entries of threads that reach it can be among the k best: their chunks alone are read again and
-// what reaches the bound is collected and ranked.  Many equals can overflow the list; then k searches over the part follow.
-template <typename T>
-__device__ void block_top(const T* __restrict__ z, uint32_t V, int i_first, uint32_t chunks, float mine, uint32_t k, uint64_t* list, float* tmax, uint32_t* n_list, uint64_t* out) {
-    const uint32_t tid = threadIdx.x, lane = tid & 31;
-    __syncthreads();
-    tmax[tid] = mine;
-    if (tid == 0) { n_list[0] = 0; n_list[1] = __float_as_uint(-INFINITY); }
-    if (tid < kMaxTop) out[tid] = 0;
-    __syncthreads();
-    uint32_t before = 0;
-    for (uint32_t i = 0; i < kWide; i += 4) {
-        const float4 o = *reinterpret_cast<const float4*>(tmax + i);
-        before += (o.x > mine || (o.x == mine && i < tid)) + (o.y > mine || (o.y == mine && i + 1 < tid)) + (o.z > mine || (o.z == mine && i + 2 < tid)) + (o.w > mine || (o.w == mine && i + 3 < tid));
-    }
-    if (before == k - 1) n_list[1] = __float_as_uint(mine);
-    __syncthreads();
-    const float bound = __uint_as_float(n_list[1]);
-    for (uint32_t f = tid / 32; f < kWide; f += kWide / 32) {
-        if (!(tmax[f] >= bound && tmax[f] > -INFINITY)) continue;
-        for (uint32_t ch = f + lane * kWide; ch < chunks; ch += 32 * kWide) {
-            float v[8];
-            const int i0 = i_first + (int)ch * 8;
-            load_chunk(z, i0, V, v);
-#pragma unroll
-            for (int e = 0; e < 8; e++)
-                if (v[e] >= bound && v[e] > -INFINITY) { const uint32_t at = atomicAdd(n_list, 1u); if (at < kList) list[at] = key_of(v[e], (uint32_t)(i0 + e)); }
-        }
-    }
-    __syncthreads();
-    const uint32_t n = n_list[0];
-    if (n <= kList) {
-        for (uint32_t i = tid; i < n; i += kWide) {
-            const uint64_t key = list[i];
-            uint32_t rank = 0;
-            for (uint32_t j = 0; j < n; j++) rank += list[j] > key;
-            if (rank < k) out[rank] = key;
-        }
-        __syncthreads();
-        return;
-    }
-    uint64_t last = ~0ull;
-    for (uint32_t t = 0; t < k; t++) {
-        uint64_t best = 0;
-        for (uint32_t ch = tid; ch < chunks; ch += kWide) {
-            float v[8];
-            const int i0 = i_first + (int)ch * 8;
-            load_chunk(z, i0, V, v);
-#pragma unroll
-            for (int e = 0; e < 8; e++) { const uint64_t key = key_of(v[e], (uint32_t)(i0 + e)); if (key < last && key > best) best = key; }
-        }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) { const uint64_t o = __shfl_xor_sync(0xFFFFFFFFu, best, d); best = o > best ? o : best; }
-        if (lane == 0) list[tid / 32] = best;
-        __syncthreads();
-        best = 0;
-        for (uint32_t i = 0; i < kWide / 32; i++) best = list[i] > best ? list[i] : best;
-        __syncthreads();
-        if (tid == 0) out[t] = best;
-        last = best;
-    }
-    __syncthreads();
-}
-
-template <typename T, int CL>
-__global__ void __launch_bounds__(kWide) long_row_kernel(const Rows<T> a) {
+template <typename T, int TH, int CL>
+__global__ void __launch_bounds__(TH) long_row_kernel(const Rows<T> a) {
     sf_chain_enter();
-    __shared__ Stat sh[kWide / 32];
-    __shared__ Stat part;
-    __shared__ uint64_t list[kList];
-    __shared__ __align__(16) float tmax[kWide];
-    __shared__ uint64_t best[kMaxTop];
-    __shared__ uint64_t merged[kMaxTop];
-    __shared__ uint32_t n_list[2];
+    __shared__ Shared<TH> sh;
     uint32_t n = a.n;
     if (a.n_dev) n = sf_clamp_rows(*a.n_dev, a.n, a.st);
+    const uint64_t row = blockIdx.x / CL;
+    if (row >= n) return;                                  // (with all blocks of its cluster)
     const float c = a.scale * kLog2e;
-    const uint32_t rank = CL > 1 ? blockIdx.x % CL : 0;
-    // (every block of a cluster has the same rows, so they all meet at the same barriers)
-    for (uint64_t row = blockIdx.x / CL; row < n; row += gridDim.x / CL) {
-        const T* z = a.z + row * a.ld;
-        const uint32_t shift = shift_of(z);
-        const uint32_t all = (a.V + shift + 7) / 8, per = (all + CL - 1) / CL, c0 = min(all, rank * per), chunks = min(all, c0 + per) - c0;
-        const int i_first = (int)(c0 * 8) - (int)shift;
-        Stat q = stat_none();
-        float mine = -INFINITY;
-        uint32_t ch = threadIdx.x;
-        for (; ch + 3 * kWide < chunks; ch += 4 * kWide) {
-            float v[4][8];
+    const uint32_t rank = CL > 1 ? blockIdx.x % CL : 0, tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+    const T* z = a.z + row * a.ld;
+    const uint32_t shift = shift_of(z);
+    const uint32_t all = (a.V + shift + 7) / 8, per = (all + CL - 1) / CL, c0 = min(all, rank * per), chunks = min(all, c0 + per) - c0;
+    const int i_first = (int)(c0 * 8) - (int)shift;
+    Stat q = {-FLT_MAX, 0.0f, 0.0f};
+    float mine = -INFINITY;
+    uint32_t ch = tid;
+    for (; ch + 3 * TH < chunks; ch += 4 * TH) {
+        float v[4][8];
 #pragma unroll
-            for (int u = 0; u < 4; u++) load_chunk(z, i_first + (int)(ch + u * kWide) * 8, a.V, v[u]);
-            const float cm = fmaxf(fmaxf(max_of(v[0]), max_of(v[1])), fmaxf(max_of(v[2]), max_of(v[3])));
-            mine = fmaxf(mine, cm);
-            if (cm > q.m) stat_raise(q, cm, c);
+        for (int u = 0; u < 4; u++) load_chunk(z, i_first + (int)(ch + u * TH) * 8, a.V, v[u]);
+        mine = fmaxf(mine, fmaxf(fmaxf(max_of(v[0]), max_of(v[1])), fmaxf(max_of(v[2]), max_of(v[3]))));
+        if (mine > q.m) stat_raise(q, mine, c);
 #pragma unroll
-            for (int u = 0; u < 4; u++) stat_add(q, v[u], -INFINITY, c);
-        }
-        for (; ch < chunks; ch += kWide) {
+        for (int u = 0; u < 4; u++) stat_add(q, v[u], c);
+    }
+    for (; ch < chunks; ch += TH) {
+        float v[8];
+        load_chunk(z, i_first + (int)ch * 8, a.V, v);
+        mine = fmaxf(mine, max_of(v));
+        if (mine > q.m) stat_raise(q, mine, c);
+        stat_add(q, v, c);
+    }
+    constexpr int GL = TH / kGroups;                       // lanes of a group
+    float m = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        if (d == GL && lane % GL == 0) sh.group[tid / GL] = m;
+        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+    }
+    if (lane == 0) sh.m[warp] = m;
+    if (tid == 0) { sh.n_threads = sh.n_list = 0; sh.bound = -INFINITY; }
+    if (tid < kMaxTop) sh.best[tid] = 0;
+    __syncthreads();
+    m = -FLT_MAX;
+#pragma unroll
+    for (int i = 0; i < TH / 32; i++) m = fmaxf(m, sh.m[i]);
+    stat_raise(q, m, c);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) { q.s += __shfl_xor_sync(0xFFFFFFFFu, q.s, d); q.w += __shfl_xor_sync(0xFFFFFFFFu, q.w, d); }
+    if (lane == 0) { sh.s[warp] = q.s; sh.w[warp] = q.w; }
+    if (a.k && tid < kGroups) {
+        const float g = sh.group[tid];
+        uint32_t before = 0;
+#pragma unroll 8
+        for (uint32_t i = 0; i < kGroups; i++) { const float o = sh.group[i]; before += o > g || (o == g && i < tid); }
+        if (before == a.k - 1) sh.bound = g;
+    }
+    __syncthreads();
+    q.s = q.w = 0.0f;
+#pragma unroll
+    for (int i = 0; i < TH / 32; i++) { q.s += sh.s[i]; q.w += sh.w[i]; }
+    if (a.k) {
+        const float bound = sh.bound;
+        if (mine >= bound && mine > -INFINITY) sh.thread[atomicAdd(&sh.n_threads, 1u)] = (uint16_t)tid;
+        __syncthreads();
+        const uint32_t each = (chunks + TH - 1) / TH, F = sh.n_threads;
+        for (uint32_t p = tid; p < F * each; p += TH) {
+            const uint32_t k = sh.thread[p / each] + p % each * TH;
+            if (k >= chunks) continue;
             float v[8];
-            load_chunk(z, i_first + (int)ch * 8, a.V, v);
-            const float cm = max_of(v);
-            mine = fmaxf(mine, cm);
-            stat_add(q, v, cm, c);
+            const int i0 = i_first + (int)k * 8;
+            load_chunk(z, i0, a.V, v);
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (v[e] >= bound && v[e] > -INFINITY) { const uint32_t at = atomicAdd(&sh.n_list, 1u); if (at < kList) sh.list[at] = key_of(v[e], (uint32_t)(i0 + e)); }
         }
-        q = block_stat(q, c, sh);
-        if (a.k) block_top(z, a.V, i_first, chunks, mine, a.k, list, tmax, n_list, best);
-        if constexpr (CL > 1) {
-            namespace cg = cooperative_groups;
-            cg::cluster_group cl = cg::this_cluster();
-            if (threadIdx.x == 0) part = q;
-            cl.sync();
-            if (rank == 0) {
-                for (int o = 1; o < CL; o++) q = stat_join(q, *cl.map_shared_rank(&part, o), c);
-                if (a.k) {                                 // the k best of all blocks' k best: a key's rank is the number of larger ones
-                    if (threadIdx.x < kMaxTop) merged[threadIdx.x] = 0;
-                    __syncthreads();
-                    for (uint32_t i = threadIdx.x; i < CL * a.k; i += kWide) {
-                        const uint64_t key = *cl.map_shared_rank(best + i % a.k, i / a.k);
-                        list[i] = key;
-                    }
-                    __syncthreads();
-                    for (uint32_t i = threadIdx.x; i < CL * a.k; i += kWide) {
-                        const uint64_t key = list[i];
-                        uint32_t r = 0;
-                        for (uint32_t j = 0; j < CL * a.k; j++) r += list[j] > key;
-                        if (key && r < a.k) merged[r] = key;
-                    }
-                    __syncthreads();
-                }
+        __syncthreads();
+        const uint32_t found = sh.n_list;
+        if (found <= kList) {
+            for (uint32_t i = tid; i < found; i += TH) {
+                const uint64_t key = sh.list[i];
+                uint32_t r = 0;
+                for (uint32_t o = 0; o < found; o++) r += sh.list[o] > key;
+                if (r < a.k) sh.best[r] = key;
             }
-            cl.sync();                                     // (no block leaves or goes on while another reads its shared memory)
-        }
-        if (rank == 0) {
-            const Answer r = answer_of(q, a.scale);
-            if (threadIdx.x == 0) write_row(a, (uint32_t)row, r);
-            if (threadIdx.x < a.k) write_top(a, (uint32_t)row, threadIdx.x, CL > 1 ? merged[threadIdx.x] : best[threadIdx.x], r);
+        } else {
+            uint64_t last = ~0ull;
+            for (uint32_t t = 0; t < a.k; t++) {
+                uint64_t best = 0;
+                for (uint32_t k = tid; k < chunks; k += TH) {
+                    float v[8];
+                    const int i0 = i_first + (int)k * 8;
+                    load_chunk(z, i0, a.V, v);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) { const uint64_t key = key_of(v[e], (uint32_t)(i0 + e)); if (key < last && key > best) best = key; }
+                }
+#pragma unroll
+                for (int d = 16; d; d >>= 1) { const uint64_t o = __shfl_xor_sync(0xFFFFFFFFu, best, d); best = o > best ? o : best; }
+                if (lane == 0) sh.list[warp] = best;
+                __syncthreads();
+                best = 0;
+                for (uint32_t i = 0; i < TH / 32; i++) best = sh.list[i] > best ? sh.list[i] : best;
+                __syncthreads();
+                if (tid == 0) sh.best[t] = best;
+                last = best;
+            }
         }
         __syncthreads();
     }
+    uint64_t* top = sh.best;
+    if constexpr (CL > 1) {
+        namespace cg = cooperative_groups;
+        cg::cluster_group cl = cg::this_cluster();
+        if (tid == 0) sh.part = {m, q.s, q.w};
+        if (tid < kMaxTop) sh.merged[tid] = 0;
+        cl.sync();
+        if (rank == 0) {
+            float top_m = m;
+            for (int o = 1; o < CL; o++) top_m = fmaxf(top_m, cl.map_shared_rank(&sh.part, o)->m);
+            q.m = m;
+            stat_raise(q, top_m, c);
+            for (int o = 1; o < CL; o++) { Stat p = *cl.map_shared_rank(&sh.part, o); stat_raise(p, top_m, c); q.s += p.s; q.w += p.w; }
+            m = top_m;
+            for (uint32_t i = tid; i < CL * a.k; i += TH) sh.list[i] = *cl.map_shared_rank(sh.best + i % a.k, i / a.k);
+            __syncthreads();
+            for (uint32_t i = tid; i < CL * a.k; i += TH) {                    // the k best of all blocks' k best
+                const uint64_t key = sh.list[i];
+                uint32_t r = 0;
+                for (uint32_t o = 0; o < CL * a.k; o++) r += sh.list[o] > key;
+                if (key && r < a.k) sh.merged[r] = key;
+            }
+            __syncthreads();
+            top = sh.merged;
+        }
+        cl.sync();                                         // (no block leaves while another reads its shared memory)
+        if (rank) return;
+    }
+    q.m = m;
+    const Answer r = answer_of(q, a.scale);
+    if (tid == 0) write_row(a, (uint32_t)row, r);
+    if (tid < a.k) write_top(a, (uint32_t)row, tid, top[tid], r);
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------------------------
@@ -324,6 +368,7 @@ template <typename T> struct Back {
     uint32_t k; const int32_t* top_ids; const float* d_top;
     T* dz; size_t ldd;
     uint32_t chunks, groups;                               // chunks of a row, groups of C chunks a thread takes
+    bool few;                                              // threads in 32 bits
     sf_dev_state* st;
 };
 
@@ -333,45 +378,55 @@ __global__ void __launch_bounds__(kThreads) back_kernel(const Back<T> a) {
     sf_chain_enter();
     uint32_t n = a.n;
     if (a.n_dev) n = sf_clamp_rows(*a.n_dev, a.n, a.st);
-    const uint64_t at = (uint64_t)blockIdx.x * kThreads + threadIdx.x, row = at / a.groups;
-    const uint32_t g0 = (uint32_t)(at % a.groups);
+    uint64_t row;
+    uint32_t g0;
+    if (a.few) { const uint32_t at = blockIdx.x * kThreads + threadIdx.x; row = at / a.groups; g0 = at % a.groups; }
+    else { const uint64_t at = (uint64_t)blockIdx.x * kThreads + threadIdx.x; row = at / a.groups; g0 = (uint32_t)(at % a.groups); }
     if (row >= n) return;
     const T* z = a.z + row * a.ld;
     T* dz = a.dz + row * a.ldd;
-    const float lse = a.lse[row], ge = a.d_entropy ? a.d_entropy[row] : 0.0f, h = a.d_entropy ? a.entropy[row] : 0.0f;
-    int32_t label = -1;
+    // with t = log2 p:  d z = -p (sum' + ge' (t + h')) + what belongs to the label and the alternatives, everything times scale
+    const float lse_ = a.lse[row], lse = lse_ == -INFINITY ? 0.0f : lse_;      // (a row with nothing but masked entries: every p is 0)
+    const float ge = a.d_entropy ? a.d_entropy[row] * a.scale * kLn2 : 0.0f, h = a.d_entropy ? a.entropy[row] * kLog2e : 0.0f;
+    uint32_t label = 0xFFFFFFFFu;
     float g = 0.0f, sum = 0.0f;
-    if (a.d_logprob) { label = a.labels[row]; if ((uint32_t)label < a.V) g = sum = a.d_logprob[row]; else label = -1; }
-    if (a.d_top) for (uint32_t j = 0; j < a.k; j++) if ((uint32_t)a.top_ids[row * a.k + j] < a.V) sum += a.d_top[row * a.k + j];
+    if (a.d_logprob) { label = (uint32_t)a.labels[row]; if (label < a.V) g = sum = a.d_logprob[row] * a.scale; else label = 0xFFFFFFFFu; }
+    if (a.d_top) for (uint32_t j = 0; j < a.k; j++) if ((uint32_t)a.top_ids[row * a.k + j] < a.V) sum += a.d_top[row * a.k + j] * a.scale;
+    const f2 c2 = dup2(a.scale), l2 = dup2(-lse), e2 = dup2(kLog2e), s2 = dup2(-sum), g2 = dup2(-ge), h2 = dup2(h);
 #pragma unroll
     for (int u = 0; u < C; u++) {
         const uint32_t ch = g0 + u * a.groups;
-        if (ch >= a.chunks) break;
+        if (ch >= a.chunks) continue;
         const uint32_t i0 = ch * 8;
-        float v[8];
+        float v[8], d[8];
         const bool whole = ALIGNED && i0 + 8 <= a.V;
         if (whole) load_f32<T, 8, true>(z + i0, v);
         else {
 #pragma unroll
             for (int e = 0; e < 8; e++) v[e] = i0 + e < a.V ? to_f32(z[i0 + e]) : -INFINITY;
         }
-        float d[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const float lp = __fsub_rn(__fmul_rn(a.scale, v[e]), lse), p = ex2(lp * kLog2e);
-            d[e] = -p * (sum + (ge == 0.0f ? 0.0f : ge * (fmaxf(lp, -1e4f) + h)));
-            if (i0 + e == (uint32_t)label) d[e] += g;
+        for (int e = 0; e < 8; e += 2) {                   // (the product is rounded before lse is taken off, as lse was: with one entry t is exactly 0)
+            float x, y;
+            const f2 t = mul2(add2(mul2(pack2(v[e], v[e + 1]), c2), l2), e2);
+            unpack2(t, x, y);
+            const f2 p = pack2(ex2(x), ex2(y));
+            f2 q = s2;
+            if (ge != 0.0f) q = fma2(g2, add2(pack2(fmaxf(x, -1e4f), fmaxf(y, -1e4f)), h2), s2);
+            unpack2(mul2(p, q), d[e], d[e + 1]);
+        }
+        if (label - i0 < 8u) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) if (label == i0 + e) d[e] = v[e] == -INFINITY ? 0.0f : d[e] + g;
         }
         if (a.d_top) for (uint32_t j = 0; j < a.k; j++) {
             const uint32_t id = (uint32_t)a.top_ids[row * a.k + j];
             if (id - i0 < 8u && id < a.V) {
-                const float t = a.d_top[row * a.k + j];
+                const float t = a.d_top[row * a.k + j] * a.scale;
 #pragma unroll
                 for (int e = 0; e < 8; e++) if (id == i0 + e) d[e] += t;
             }
         }
-#pragma unroll
-        for (int e = 0; e < 8; e++) d[e] = v[e] == -INFINITY ? 0.0f : d[e] * a.scale;
         if (whole) store_f32<T, 8, true>(dz + i0, d);
         else {
 #pragma unroll
@@ -384,16 +439,16 @@ template <typename T, int L, int C> int launch_rows(const Rows<T>& a, cudaStream
     SF_CUDA(sf_launch_chained(row_kernel<T, L, C>, (uint32_t)(((uint64_t)a.n + kThreads / L - 1) / (kThreads / L)), kThreads, 0, st, a));
     return SF_OK;
 }
-template <typename T, int CL> int launch_long(const Rows<T>& a, uint32_t most, cudaStream_t st) {
+template <typename T, int TH, int CL> int launch_long(const Rows<T>& a, cudaStream_t st) {
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = std::min(a.n, most) * CL; lc.blockDim = kWide; lc.stream = st;
+    lc.gridDim = a.n * CL; lc.blockDim = TH; lc.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim = {CL, 1, 1};
     lc.attrs = at; lc.numAttrs = CL > 1 ? 2 : 1;
-    SF_CUDA(cudaLaunchKernelEx(&lc, long_row_kernel<T, CL>, a));
+    SF_CUDA(cudaLaunchKernelEx(&lc, long_row_kernel<T, TH, CL>, a));
     return SF_OK;
 }
 
@@ -426,8 +481,8 @@ extern "C" int sf_label_logprobs(sf_ctx* ctx, const void* logits, int dtype, con
         if (V <= 512) return launch_rows<T, 32, 2>(a, st);
         if (V <= 1024) return launch_rows<T, 32, 4>(a, st);
         // a cluster of eight blocks a row where the rows alone do not fill the machine and are long enough for eight blocks
-        if (n < (uint32_t)ctx->num_sms && V >= 16384) return launch_long<T, 8>(a, n, st);
-        return launch_long<T, 1>(a, 0x7FFFFFFFu, st);
+        if (n < (uint32_t)ctx->num_sms && V >= 16384) return V >= 131072 ? launch_long<T, 512, 8>(a, st) : launch_long<T, 256, 8>(a, st);
+        return V <= 8192 ? launch_long<T, 128, 1>(a, st) : (V <= 65536 ? launch_long<T, 256, 1>(a, st) : launch_long<T, 512, 1>(a, st));
     });
 }
 
@@ -445,13 +500,14 @@ extern "C" int sf_label_logprobs_backward(sf_ctx* ctx, const void* logits, int d
     SF_ON_DEVICE(ctx);
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        Back<T> a = {(const T*)logits, ld, n_dev, n, V, scale, labels, lse, entropy, d_logprob, d_entropy, k, top_ids, d_top_logprobs, (T*)d_logits_out, ldd, (V + 7) / 8, 0, ctx->d_state};
+        Back<T> a = {(const T*)logits, ld, n_dev, n, V, scale, labels, lse, entropy, d_logprob, d_entropy, k, top_ids, d_top_logprobs, (T*)d_logits_out, ldd, (V + 7) / 8, 0, false, ctx->d_state};
         const bool al = aligned(logits, 16) && aligned(d_logits_out, 16) && (ld * size) % 16 == 0 && (ldd * size) % 16 == 0;
         constexpr int C = 4;
         const bool one = a.chunks < 64;
         a.groups = one ? a.chunks : (a.chunks + C - 1) / C;
         const uint64_t blocks = ((uint64_t)n * a.groups + kThreads - 1) / kThreads;
         if (blocks > 0x7FFFFFFFu) return (int)SF_ERR_ARG;
+        a.few = blocks * kThreads <= 0xFFFFFFFFu;
         auto kern = one ? (al ? back_kernel<T, 1, true> : back_kernel<T, 1, false>) : (al ? back_kernel<T, C, true> : back_kernel<T, C, false>);
         SF_CUDA(sf_launch_chained(kern, (uint32_t)blocks, kThreads, 0, (cudaStream_t)stream, a));
         return (int)SF_OK;

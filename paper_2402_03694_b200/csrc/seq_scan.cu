@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
                 for (int e = 0; e < VV; e += 4) {
                     const float4 b4 = *reinterpret_cast<const float4*>(&sh.bias[c + e]);
                     f2 x = add2(pack2(d[e], d[e + 1]), pack2(b4.x, b4.y)), y = add2(pack2(d[e + 2], d[e + 3]), pack2(b4.z, b4.w));
-                    if (a.softplus) { x = softplus2(x); y = softplus2(y); }
+                    if (a.softplus) { f2 unused; x = softplus2(x, unused); y = softplus2(y, unused); }
                     if (ENDS) {
                         if (t >= rows) x = y = 0;
                         steps[i][e / 2] = add2(steps[i][e / 2], x); steps[i][e / 2 + 1] = add2(steps[i][e / 2 + 1], y);

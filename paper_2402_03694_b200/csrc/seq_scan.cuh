@@ -63,14 +63,14 @@ __device__ __forceinline__ float softplus_of(float x, float& e) {
     return fmaf(2.0f * q, p, fmaxf(x, 0.0f));
 }
 
-// the same for two values
-__device__ __forceinline__ f2 softplus2(f2 x) {
+// the same for two values; ee: their exp(-|x|)
+__device__ __forceinline__ f2 softplus2(f2 x, f2& ee) {
     float a, b;
     unpack2(x, a, b);
     const f2 t = mul2(pack2(fabsf(a), fabsf(b)), dup2(-kLog2e));
     float e, f;
     unpack2(t, e, f);
-    const f2 ee = pack2(ex2(e), ex2(f));
+    ee = pack2(ex2(e), ex2(f));
     unpack2(add2(ee, dup2(2.0f)), e, f);
     const f2 q = mul2(ee, pack2(rcp(e), rcp(f))), q2 = mul2(q, q);
     f2 p = fma2(q2, dup2(1.0f / 13), dup2(1.0f / 11));
@@ -193,7 +193,7 @@ inline Plan plan_of(uint32_t n_seq, uint32_t max_len, uint32_t D, uint32_t N, ui
     p.parts = (max_len + p.part_len - 1) / p.part_len;
     p.split = p.parts > 1;
     const uint64_t blocks = (uint64_t)G * p.cblocks, items = std::max<uint64_t>(1, (uint64_t)n_seq * p.parts);
-    p.runs = (uint32_t)std::min<uint64_t>({items, 65535, std::max<uint64_t>(1, (uint64_t)SF_NUM_SMS_DEFAULT * 4 / blocks)});
+    p.runs = (uint32_t)std::min<uint64_t>({items, 65535, std::max<uint64_t>(1, (uint64_t)SF_NUM_SMS_DEFAULT * 2 / blocks)});
     return p;
 }
 inline size_t part_bytes(const Plan& p, uint32_t n_seq, uint32_t D, uint32_t N) { return p.split ? sf_align256((size_t)n_seq * p.parts * D * N * 4) + sf_align256((size_t)n_seq * p.parts * D * 4) : 0; }

@@ -6,17 +6,17 @@ namespace {
 using namespace sfscan;
 
 constexpr int K = (int)kEvery;             // rows of a tile
+constexpr int R = 4;                       // rows whose decays and states a thread holds at once
 
 // What a warp keeps in shared memory for a tile; rows of channels spaced so that 16-byte accesses of eight lanes meet no common bank
 template <int SL> struct __align__(16) Backward {
     typedef Shape<SL> S;
     static constexpr int PX = S::CH + 4;
     float step[K][PX], u[K][PX], e[K][PX];                 // delta; u; dout silu(z)
-    float dstep[K][PX], dgate[K][PX];                      // d delta / d raw; dout silu'(z)
+    float dstep[K][PX], dgate[K][PX];                      // d delta / d raw; dout silu'(z).  A row that is done leaves du (without D e), ddelta and dz in step, dstep and dgate
     float bc[2][K][S::NP];                                 // B, C
-    float s1[K][PX], s2[K][PX], y[K][PX];                  // sum g B; sum (a g) h_{t-1} A; sum C h
     float sum[K][2][S::NP];                                // the warp's dB, dC
-    float4 start[2][4][32];                                // the states before rows 0 and 4, every lane its own
+    float4 start[K / R][4][32];                            // the states before rows 0, R, .., every lane its own
     float bias[S::CH], skip[S::CH];
 };
 
@@ -51,22 +51,37 @@ __device__ __forceinline__ void stage(const Scan& a, Backward<SL>& sh, size_t ro
         if (a.z) open<T, VV>(nz[i], z);
         open<T, VV>(ng[i], o);
         float ds[VV], dg[VV];
+        if constexpr (VV == 1) {
+            float x;                                       // exp(-|raw|): the slope of softplus is 1 / (1 + x), or x / (1 + x) left of 0
+            const float raw = d[0] + sh.bias[c], sg = a.z ? sigmoid(z[0]) : 1.0f;
+            d[0] = a.softplus ? softplus_of(raw, x) : raw;
+            ds[0] = a.softplus ? (raw >= 0.0f ? 1.0f : x) * rcp(1.0f + x) : 1.0f;
+            dg[0] = a.z ? o[0] * sg * fmaf(z[0], 1.0f - sg, 1.0f) : 0.0f;
+            if (a.z) o[0] *= z[0] * sg;
+        } else {
 #pragma unroll
-        for (int e = 0; e < VV; e++) {
-            d[e] += sh.bias[c + e];
-            ds[e] = 1.0f; dg[e] = 0.0f;
-            if (a.softplus) {
-                float x;                                   // exp(-|raw|): the slope is 1 / (1 + x), or x / (1 + x) left of 0
-                const float raw = d[e];
-                d[e] = softplus_of(raw, x);
-                if (!ENDS) ds[e] = (raw >= 0.0f ? 1.0f : x) * rcp(1.0f + x);
+            for (int e = 0; e < VV; e += 2) {
+                const f2 one = dup2(1.0f);
+                f2 raw = add2(pack2(d[e], d[e + 1]), *reinterpret_cast<const f2*>(&sh.bias[c + e])), x, v = raw, w = one;
+                if (a.softplus) {
+                    v = softplus2(raw, x);
+                    float p, q, r0, r1;
+                    unpack2(add2(x, one), p, q);
+                    unpack2(raw, r0, r1);
+                    if (!ENDS) { float x0, x1; unpack2(x, x0, x1); w = mul2(pack2(r0 >= 0.0f ? 1.0f : x0, r1 >= 0.0f ? 1.0f : x1), pack2(rcp(p), rcp(q))); }
+                }
+                unpack2(v, d[e], d[e + 1]);
+                unpack2(w, ds[e], ds[e + 1]);
+                if (a.z) {
+                    const f2 zz = pack2(z[e], z[e + 1]), oo = pack2(o[e], o[e + 1]), sg = sigmoid2(zz), os = mul2(oo, sg);
+                    if (!ENDS) unpack2(mul2(os, fma2(zz, fma2(sg, dup2(-1.0f), one), one)), dg[e], dg[e + 1]);
+                    unpack2(mul2(os, zz), o[e], o[e + 1]);
+                }
             }
-            if (a.z) {
-                const float sg = sigmoid(z[e]);
-                if (!ENDS) dg[e] = o[e] * sg * fmaf(z[e], 1.0f - sg, 1.0f);
-                o[e] *= z[e] * sg;
-            }
-            if (!there) { d[e] = 0.0f; o[e] = 0.0f; }
+        }
+        if (!there) {
+#pragma unroll
+            for (int e = 0; e < VV; e++) d[e] = o[e] = 0.0f;
         }
         auto put = [&](float* p, const float (&v)[VV]) {
             if constexpr (VV == 1) p[0] = v[0];
@@ -179,25 +194,27 @@ __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
     }
 }
 
-// The sums over the SL state lanes of the four values of v: with SL >= 4 lane sl gets channel 2 (sl & 1) + (sl >> 1 & 1) of the lane's four; put writes them.
-template <int SL> __device__ __forceinline__ void put_sum(float* p, f2 (&v)[2], int sl) {
-    if constexpr (SL == 1) *reinterpret_cast<ulonglong2*>(p) = make_ulonglong2(v[0], v[1]);
-    else {
-        const bool hi = sl & 1;
-        const f2 keep = hi ? v[1] : v[0], give = hi ? v[0] : v[1];
-        const f2 w = add2(keep, __shfl_xor_sync(0xFFFFFFFFu, give, 1));
-        if constexpr (SL == 2) *reinterpret_cast<f2*>(p + 2 * sl) = w;
+// The sums over the SL state lanes of the lane's four channels: a lane gets those of NC of them (all, two, one), from channel first(sl) on.
+template <int SL> struct ByState {
+    static constexpr int NC = SL == 1 ? 4 : (SL == 2 ? 2 : 1);
+    __device__ __forceinline__ static int first(int sl) { return SL == 1 ? 0 : (SL == 2 ? 2 * sl : 2 * (sl & 1) + (sl >> 1 & 1)); }
+    __device__ __forceinline__ static void sum(const f2 (&v)[2], int sl, float (&o)[NC]) {
+        if constexpr (SL == 1) { unpack2(v[0], o[0], o[1]); unpack2(v[1], o[2], o[3]); }
         else {
+            const bool hi = sl & 1;
+            const f2 w = add2(hi ? v[1] : v[0], __shfl_xor_sync(0xFFFFFFFFu, hi ? v[0] : v[1], 1));
             float x, y;
             unpack2(w, x, y);
-            const bool up = sl & 2;
-            float z = (up ? y : x) + __shfl_xor_sync(0xFFFFFFFFu, up ? x : y, 2);
+            if constexpr (SL == 2) { o[0] = x; o[1] = y; }
+            else {
+                const bool up = sl & 2;
+                o[0] = (up ? y : x) + __shfl_xor_sync(0xFFFFFFFFu, up ? x : y, 2);
 #pragma unroll
-            for (int m = 4; m < SL; m <<= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, m);
-            if (SL == 4 || sl < 4) p[2 * (sl & 1) + (sl >> 1 & 1)] = z;
+                for (int m = 4; m < SL; m <<= 1) o[0] += __shfl_xor_sync(0xFFFFFFFFu, o[0], m);
+            }
         }
     }
-}
+};
 // Sums of 8 values over the CL channel lanes; they end up in lane cl as the 8 / CL (at least one) values from index (cl * 8 / CL) % 8 on; put writes
 // them to p[value / 4][state]
 template <int SL> __device__ __forceinline__ void put_states(float* p0, float* p1, float (&v)[8], int lane, int cl, int sl) {
@@ -228,7 +245,7 @@ template <int SL> __device__ __forceinline__ void put_states(float* p0, float* p
 // A tile's states are stepped from the state kept before it: rows 0 to 3 to reach row 4, rows 4 to 7 with decays and states held in registers, back over
 // them, then rows 0 to 3 the same way.
 template <typename T, int SL, int VV>
-__global__ void __launch_bounds__(32 * kWarps) back_kernel(const Scan a) {
+__global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
     sf_chain_enter();
     typedef Shape<SL> S;
     typedef Pieces<K, S::CH, VV> P;
@@ -285,9 +302,9 @@ __global__ void __launch_bounds__(32 * kWarps) back_kernel(const Scan a) {
 #pragma unroll
                     for (int n = 0; n < 4; n += 2) { const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&sh.start[q][2 * j + n / 2][lane]); v[j][n] = w.x; v[j][n + 1] = w.y; }
             };
-            keep(0);
 #pragma unroll
-            for (int t = 0; t < 4; t++) {
+            for (int t = 0; t < K - R; t++) {
+                if (t % R == 0) keep(t / R);
                 const ulonglong2 d2 = *reinterpret_cast<const ulonglong2*>(&sh.step[t][cl * 4]), u2 = *reinterpret_cast<const ulonglong2*>(&sh.u[t][cl * 4]);
                 const float4 b4 = *reinterpret_cast<const float4*>(&sh.bc[0][t][sl * 4]);
                 const f2 d[2] = {d2.x, d2.y}, in[2] = {mul2(d2.x, u2.x), mul2(d2.y, u2.y)}, b[4] = {dup2(b4.x), dup2(b4.y), dup2(b4.z), dup2(b4.w)};
@@ -296,14 +313,14 @@ __global__ void __launch_bounds__(32 * kWarps) back_kernel(const Scan a) {
 #pragma unroll
                     for (int n = 0; n < 4; n++) h[j][n] = fma2(decay2(d[j], A[j][n]), h[j][n], mul2(in[j], b[n]));
             }
-            keep(1);
+            keep(K / R - 1);
 #pragma unroll 1
-            for (int q = 1; q >= 0; q--) {
-                f2 al[4][2][4], hs[5][2][4];               // decays; states before the rows and after them
+            for (int q = K / R - 1; q >= 0; q--) {
+                f2 al[R][2][4], hs[R + 1][2][4];               // decays; states before the rows and after them
                 take(hs[0], q);
 #pragma unroll
-                for (int t = 0; t < 4; t++) {
-                    const int tt = 4 * q + t;
+                for (int t = 0; t < R; t++) {
+                    const int tt = R * q + t;
                     const ulonglong2 d2 = *reinterpret_cast<const ulonglong2*>(&sh.step[tt][cl * 4]), u2 = *reinterpret_cast<const ulonglong2*>(&sh.u[tt][cl * 4]);
                     const float4 b4 = *reinterpret_cast<const float4*>(&sh.bc[0][tt][sl * 4]);
                     const f2 d[2] = {d2.x, d2.y}, in[2] = {mul2(d2.x, u2.x), mul2(d2.y, u2.y)}, b[4] = {dup2(b4.x), dup2(b4.y), dup2(b4.z), dup2(b4.w)};
@@ -313,8 +330,8 @@ __global__ void __launch_bounds__(32 * kWarps) back_kernel(const Scan a) {
                         for (int n = 0; n < 4; n++) { al[t][j][n] = decay2(d[j], A[j][n]); hs[t + 1][j][n] = fma2(al[t][j][n], hs[t][j][n], mul2(in[j], b[n])); }
                 }
 #pragma unroll
-                for (int t = 3; t >= 0; t--) {
-                    const int tt = 4 * q + t;
+                for (int t = R - 1; t >= 0; t--) {
+                    const int tt = R * q + t;
                     const ulonglong2 d2 = *reinterpret_cast<const ulonglong2*>(&sh.step[tt][cl * 4]), u2 = *reinterpret_cast<const ulonglong2*>(&sh.u[tt][cl * 4]), e2 = *reinterpret_cast<const ulonglong2*>(&sh.e[tt][cl * 4]);
                     const float4 b4 = *reinterpret_cast<const float4*>(&sh.bc[0][tt][sl * 4]), c4 = *reinterpret_cast<const float4*>(&sh.bc[1][tt][sl * 4]);
                     const f2 d[2] = {d2.x, d2.y}, in[2] = {mul2(d2.x, u2.x), mul2(d2.y, u2.y)}, e[2] = {e2.x, e2.y};
@@ -334,9 +351,11 @@ __global__ void __launch_bounds__(32 * kWarps) back_kernel(const Scan a) {
                             dA[j][n] = fma2(x, d[j], dA[j][n]);
                             y[j] = n ? fma2(hs[t + 1][j][n], c[n], y[j]) : mul2(hs[t + 1][j][n], c[n]);
                         }
-                    put_sum<SL>(&sh.s1[tt][cl * 4], s1, sl);
-                    put_sum<SL>(&sh.s2[tt][cl * 4], s2, sl);
-                    if (a.z) put_sum<SL>(&sh.y[tt][cl * 4], y, sl);
+                    typedef ByState<SL> Q;
+                    float o1[Q::NC], o2[Q::NC], oy[Q::NC];
+                    Q::sum(s1, sl, o1);
+                    Q::sum(s2, sl, o2);
+                    if (a.z) Q::sum(y, sl, oy);
                     float v[8];
 #pragma unroll
                     for (int n = 0; n < 4; n++) {
@@ -345,6 +364,17 @@ __global__ void __launch_bounds__(32 * kWarps) back_kernel(const Scan a) {
                         unpack2(dC[n], x, w); v[4 + n] = x + w;
                     }
                     put_states<SL>(sh.sum[tt][0], sh.sum[tt][1], v, lane, cl, sl);
+                    __syncwarp();                          // (every lane has read the row)
+                    if (SL <= 4 || sl < 4) {
+#pragma unroll
+                        for (int i = 0; i < Q::NC; i++) {
+                            const int k = cl * 4 + Q::first(sl) + i;
+                            const float uu = sh.u[tt][k];
+                            sh.step[tt][k] *= o1[i];
+                            sh.dstep[tt][k] *= fmaf(uu, o1[i], kLn2 * o2[i]);
+                            if (a.z) sh.dgate[tt][k] *= fmaf(sh.skip[k], uu, oy[i]);
+                        }
+                    }
                 }
             }
             __syncwarp();
@@ -356,12 +386,12 @@ __global__ void __launch_bounds__(32 * kWarps) back_kernel(const Scan a) {
                 float du[VV], dd[VV], dz[VV];
 #pragma unroll
                 for (int e = 0; e < VV; e++) {
-                    const float step = sh.step[t][c + e], u = sh.u[t][c + e], o = sh.e[t][c + e], s1 = sh.s1[t][c + e], skip = sh.skip[c + e];
-                    du[e] = fmaf(skip, o, step * s1);
-                    dd[e] = fmaf(u, s1, kLn2 * sh.s2[t][c + e]) * sh.dstep[t][c + e];
+                    const float u = sh.u[t][c + e], o = sh.e[t][c + e];
+                    du[e] = fmaf(sh.skip[c + e], o, sh.step[t][c + e]);
+                    dd[e] = sh.dstep[t][c + e];
+                    dz[e] = sh.dgate[t][c + e];
                     dD[i][e] = fmaf(o, u, dD[i][e]);
                     db[i][e] += dd[e];
-                    dz[e] = a.z ? fmaf(skip, u, sh.y[t][c + e]) * sh.dgate[t][c + e] : 0.0f;
                 }
                 if (a.du) store_word<T, VV>((T*)a.du + at * a.lddu + ch0 + pc.lc + P::step(i, a.lddu), du);
                 if (a.ddelta) store_word<T, VV>((T*)a.ddelta + at * a.ldddelta + ch0 + pc.lc + P::step(i, a.ldddelta), dd);
@@ -390,13 +420,13 @@ __global__ void __launch_bounds__(32 * kWarps) back_kernel(const Scan a) {
         const int t = pc.t(i), c = pc.c(i);
         if (t >= K) continue;
 #pragma unroll
-        for (int e = 0; e < VV; e++) { sh.s1[t][c + e] = dD[i][e]; sh.s2[t][c + e] = db[i][e]; }
+        for (int e = 0; e < VV; e++) { sh.u[t][c + e] = dD[i][e]; sh.e[t][c + e] = db[i][e]; }
     }
     __syncwarp();
     for (int c = lane; c < (int)have; c += 32) {
         float x = 0.0f, y = 0.0f;
 #pragma unroll
-        for (int t = 0; t < K; t++) { x += sh.s1[t][c]; y += sh.s2[t][c]; }
+        for (int t = 0; t < K; t++) { x += sh.u[t][c]; y += sh.e[t][c]; }
         par[(size_t)(ch0 + c) * (a.N + 2) + a.N] = x;
         par[(size_t)(ch0 + c) * (a.N + 2) + a.N + 1] = y;
     }
