@@ -89,20 +89,40 @@ __device__ __forceinline__ float value_of(uint64_t key) {
     const uint32_t b = (uint32_t)(key >> 32);
     return __uint_as_float(b & 0x80000000u ? b & 0x7FFFFFFFu : ~b);
 }
+// alternative j of a row: entry i of value z, or none (z -infinity)
+template <typename T> __device__ __forceinline__ void write_top(const Rows<T>& a, uint32_t row, uint32_t j, float z, uint32_t i, const Answer& r) {
+    const bool none = !(z > -INFINITY);
+    if (a.top_ids) a.top_ids[(size_t)row * a.k + j] = none ? -1 : (int32_t)i;
+    if (a.top_lp) a.top_lp[(size_t)row * a.k + j] = none ? -INFINITY : logprob_of(z, r, a.scale);
+}
 template <typename T> __device__ __forceinline__ void write_top(const Rows<T>& a, uint32_t row, uint32_t j, uint64_t key, const Answer& r) {
-    if (a.top_ids) a.top_ids[(size_t)row * a.k + j] = key ? (int32_t)(0xFFFFFFFFu - (uint32_t)key) : -1;
-    if (a.top_lp) a.top_lp[(size_t)row * a.k + j] = key ? logprob_of(value_of(key), r, a.scale) : -INFINITY;
+    write_top(a, row, j, key ? value_of(key) : -INFINITY, 0xFFFFFFFFu - (uint32_t)key, r);
 }
 
 // Eight entries of a row: chunk c covers entries 8 c - shift .. 8 c - shift + 7 (shift: entries by which the row begins behind a 16-byte
 // boundary, so that every chunk inside the row is loaded whole); entries outside the row read as -infinity.
 template <typename T> __device__ __forceinline__ uint32_t shift_of(const T* row) { return (uint32_t)((uintptr_t)row & 15u) / sizeof(T); }
-template <typename T> __device__ __forceinline__ void load_chunk(const T* __restrict__ row, int i0, uint32_t V, float (&v)[8]) {
-    if (i0 >= 0 && i0 + 8 <= (int)V) load_f32<T, 8, true>(row + i0, v);
-    else {
+template <typename T> struct Chunk {
+    union { uint4 q[sizeof(T) / 2]; T e[8]; };
+    __device__ __forceinline__ Chunk() {}
+    __device__ __forceinline__ void fetch(const T* __restrict__ row, int i0, uint32_t V) {
+        if (i0 >= 0 && i0 + 8 <= (int)V) {
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = (uint32_t)(i0 + e) < V ? to_f32(row[i0 + e]) : -INFINITY;
+            for (int i = 0; i < (int)sizeof(T) / 2; i++) q[i] = __ldg(reinterpret_cast<const uint4*>(row + i0) + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) e[i] = (uint32_t)(i0 + i) < V ? row[i0 + i] : from_f32<T>(-INFINITY);
+        }
     }
+    __device__ __forceinline__ void open(float (&v)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = to_f32(e[i]);
+    }
+};
+template <typename T> __device__ __forceinline__ void load_chunk(const T* __restrict__ row, int i0, uint32_t V, float (&v)[8]) {
+    Chunk<T> c;
+    c.fetch(row, i0, V);
+    c.open(v);
 }
 
 // ---- rows of up to 1024 entries: L lanes a row, C chunks a lane, the row in registers -----------------------------------------
@@ -120,17 +140,13 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Rows<T> a) {
     const uint64_t row = (uint64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
     const bool live = row < n;
     const T* z = a.z + (live ? row : 0) * a.ld;
+    const int first = (int)lane * 8 - (int)shift_of(z);    // the entry that the lane's first chunk begins with
     float v[C][8];
     const float c = a.scale * kLog2e;
     float mine = -INFINITY;
 #pragma unroll
     for (int j = 0; j < C; j++) {
-        const int i0 = (int)(lane + L * j) * 8;
-        if (live && ((uintptr_t)z & 15u) == 0) load_chunk(z, i0, a.V, v[j]);
-        else {
-#pragma unroll
-            for (int e = 0; e < 8; e++) v[j][e] = live && (uint32_t)(i0 + e) < a.V ? to_f32(z[i0 + e]) : -INFINITY;
-        }
+        load_chunk(z, first + L * j * 8, live ? a.V : 0, v[j]);
         mine = fmaxf(mine, max_of(v[j]));
     }
     float m = mine;
@@ -158,7 +174,7 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Rows<T> a) {
                 const uint32_t who = __ballot_sync(0xFFFFFFFFu, in);
                 if (who == 0) continue;
                 const uint32_t at = found + __popc(who & ((1u << lane) - 1));
-                if (in && at < kWarpList) list[at] = key_of(v[j][e], (lane + L * j) * 8 + e);
+                if (in && at < kWarpList) list[at] = key_of(v[j][e], (uint32_t)(first + L * j * 8 + e));
                 found += __popc(who);
             }
         __syncwarp();
@@ -169,7 +185,7 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Rows<T> a) {
                 for (uint32_t o = 0; o < found; o++) rank += list[o] > key;
                 if (live && rank < a.k) write_top(a, (uint32_t)row, rank, key, r);
             }
-            for (uint32_t t = found + lane; t < a.k; t += 32) if (live) write_top(a, (uint32_t)row, t, 0, r);
+            for (uint32_t t = found + lane; t < a.k; t += 32) if (live) write_top(a, (uint32_t)row, t, -INFINITY, 0u, r);
             return;
         }
     }
@@ -185,14 +201,14 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Rows<T> a) {
 #pragma unroll
         for (int j = C - 1; j >= 0; j--)
 #pragma unroll
-            for (int e = 7; e >= 0; e--) if (v[j][e] == m) at = (lane + L * j) * 8 + e;
+            for (int e = 7; e >= 0; e--) if (v[j][e] == m) at = (uint32_t)(first + L * j * 8 + e);
 #pragma unroll
         for (int d = L / 2; d; d >>= 1) at = min(at, __shfl_xor_sync(0xFFFFFFFFu, at, d));
-        if (live && lane == 0) write_top(a, (uint32_t)row, t, m > -INFINITY ? key_of(m, at) : 0, r);
+        if (live && lane == 0) write_top(a, (uint32_t)row, t, m, at, r);
 #pragma unroll
         for (int j = 0; j < C; j++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) if ((lane + L * j) * 8 + e == at) v[j][e] = -INFINITY;
+            for (int e = 0; e < 8; e++) if ((uint32_t)(first + L * j * 8 + e) == at) v[j][e] = -INFINITY;
     }
 }
 
@@ -230,15 +246,24 @@ __global__ void __launch_bounds__(TH) long_row_kernel(const Rows<T> a) {
     const int i_first = (int)(c0 * 8) - (int)shift;
     Stat q = {-FLT_MAX, 0.0f, 0.0f};
     float mine = -INFINITY;
-    uint32_t ch = tid;
-    for (; ch + 3 * TH < chunks; ch += 4 * TH) {
-        float v[4][8];
+    constexpr int U = 4;                                   // chunks worked on while as many are on their way
+    Chunk<T> next[U];
+    auto fetch = [&](uint32_t ch) {
 #pragma unroll
-        for (int u = 0; u < 4; u++) load_chunk(z, i_first + (int)(ch + u * TH) * 8, a.V, v[u]);
+        for (int u = 0; u < U; u++) next[u].fetch(z, i_first + (int)(ch + u * TH) * 8, a.V);
+    };
+    const uint32_t full = chunks / (U * TH) * (U * TH);    // (chunks behind the block's part are another block's: whole groups only)
+    uint32_t ch = tid;
+    if (full) fetch(ch);
+    for (; ch < full; ch += U * TH) {
+        float v[U][8];
+#pragma unroll
+        for (int u = 0; u < U; u++) next[u].open(v[u]);
+        if (ch + U * TH < full) fetch(ch + U * TH);
         mine = fmaxf(mine, fmaxf(fmaxf(max_of(v[0]), max_of(v[1])), fmaxf(max_of(v[2]), max_of(v[3]))));
         if (mine > q.m) stat_raise(q, mine, c);
 #pragma unroll
-        for (int u = 0; u < 4; u++) stat_add(q, v[u], c);
+        for (int u = 0; u < U; u++) stat_add(q, v[u], c);
     }
     for (; ch < chunks; ch += TH) {
         float v[8];
@@ -367,70 +392,97 @@ template <typename T> struct Back {
     const float* d_logprob; const float* d_entropy;
     uint32_t k; const int32_t* top_ids; const float* d_top;
     T* dz; size_t ldd;
-    uint32_t chunks, groups;                               // chunks of a row, groups of C chunks a thread takes
+    uint32_t chunks, groups;                               // chunks of a row; threads that share them, where a thread takes several of one row
     bool few;                                              // threads in 32 bits
     sf_dev_state* st;
 };
 
-// a thread takes up to C chunks of one row, lanes of a row side by side
-template <typename T, int C, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads) back_kernel(const Back<T> a) {
-    sf_chain_enter();
-    uint32_t n = a.n;
-    if (a.n_dev) n = sf_clamp_rows(*a.n_dev, a.n, a.st);
-    uint64_t row;
-    uint32_t g0;
-    if (a.few) { const uint32_t at = blockIdx.x * kThreads + threadIdx.x; row = at / a.groups; g0 = at % a.groups; }
-    else { const uint64_t at = (uint64_t)blockIdx.x * kThreads + threadIdx.x; row = at / a.groups; g0 = (uint32_t)(at % a.groups); }
-    if (row >= n) return;
-    const T* z = a.z + row * a.ld;
-    T* dz = a.dz + row * a.ldd;
-    // with t = log2 p:  d z = -p (sum' + ge' (t + h')) + what belongs to the label and the alternatives, everything times scale
-    const float lse_ = a.lse[row], lse = lse_ == -INFINITY ? 0.0f : lse_;      // (a row with nothing but masked entries: every p is 0)
-    const float ge = a.d_entropy ? a.d_entropy[row] * a.scale * kLn2 : 0.0f, h = a.d_entropy ? a.entropy[row] * kLog2e : 0.0f;
-    uint32_t label = 0xFFFFFFFFu;
-    float g = 0.0f, sum = 0.0f;
-    if (a.d_logprob) { label = (uint32_t)a.labels[row]; if (label < a.V) g = sum = a.d_logprob[row] * a.scale; else label = 0xFFFFFFFFu; }
-    if (a.d_top) for (uint32_t j = 0; j < a.k; j++) if ((uint32_t)a.top_ids[row * a.k + j] < a.V) sum += a.d_top[row * a.k + j] * a.scale;
-    const f2 c2 = dup2(a.scale), l2 = dup2(-lse), e2 = dup2(kLog2e), s2 = dup2(-sum), g2 = dup2(-ge), h2 = dup2(h);
+// What a row's gradient takes besides its entries.  With t = log2 p:  d z = -p (sum + ge (t + h)) + what belongs to the label and the alternatives, everything
+// times scale.
+template <typename T> struct RowBack {
+    float lse, ge, h, g, sum;
+    uint32_t label;
+    __device__ __forceinline__ void load(const Back<T>& a, size_t row) {
+        lse = a.lse[row];
+        ge = a.d_entropy ? a.d_entropy[row] : 0.0f;
+        h = a.d_entropy ? a.entropy[row] : 0.0f;
+        label = a.d_logprob ? (uint32_t)a.labels[row] : 0xFFFFFFFFu;
+        g = a.d_logprob ? a.d_logprob[row] : 0.0f;
+        sum = 0.0f;
+        if (a.d_top) for (uint32_t j = 0; j < a.k; j++) if ((uint32_t)a.top_ids[row * a.k + j] < a.V) sum += a.d_top[row * a.k + j] * a.scale;
+    }
+    __device__ __forceinline__ void ready(const Back<T>& a) {
+        if (lse == -INFINITY) lse = 0.0f;                  // (a row with nothing but masked entries: every p is 0)
+        ge *= a.scale * kLn2; h *= kLog2e;
+        if (label >= a.V) { label = 0xFFFFFFFFu; g = 0.0f; }
+        g = __fmul_rn(g, a.scale);                         // (rounded here, so that g taken off and g added cancel)
+        sum += g;
+    }
+    __device__ __forceinline__ void chunk(const Back<T>& a, size_t row, int i0, const Chunk<T>& in, float (&d)[8]) const {
+        const f2 e2 = dup2(kLog2e), l2 = dup2(-lse), s2 = dup2(-sum), g2 = dup2(-ge), h2 = dup2(h);
+        float v[8];
+        in.open(v);
 #pragma unroll
-    for (int u = 0; u < C; u++) {
-        const uint32_t ch = g0 + u * a.groups;
-        if (ch >= a.chunks) continue;
-        const uint32_t i0 = ch * 8;
-        float v[8], d[8];
-        const bool whole = ALIGNED && i0 + 8 <= a.V;
-        if (whole) load_f32<T, 8, true>(z + i0, v);
-        else {
-#pragma unroll
-            for (int e = 0; e < 8; e++) v[e] = i0 + e < a.V ? to_f32(z[i0 + e]) : -INFINITY;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {                   // (the product is rounded before lse is taken off, as lse was: with one entry t is exactly 0)
-            float x, y;
-            const f2 t = mul2(add2(mul2(pack2(v[e], v[e + 1]), c2), l2), e2);
+        for (int e = 0; e < 8; e += 2) {
+            float x, y;                                    // (the product is rounded before lse is taken off, as lse was, and never fused: with one entry t is exactly 0)
+            const f2 t = mul2(add2(pack2(__fmul_rn(v[e], a.scale), __fmul_rn(v[e + 1], a.scale)), l2), e2);
             unpack2(t, x, y);
             const f2 p = pack2(ex2(x), ex2(y));
             f2 q = s2;
             if (ge != 0.0f) q = fma2(g2, add2(pack2(fmaxf(x, -1e4f), fmaxf(y, -1e4f)), h2), s2);
             unpack2(mul2(p, q), d[e], d[e + 1]);
         }
-        if (label - i0 < 8u) {
+        if (label - (uint32_t)i0 < 8u) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) if (label == i0 + e) d[e] = v[e] == -INFINITY ? 0.0f : d[e] + g;
+            for (int e = 0; e < 8; e++) if (label == (uint32_t)(i0 + e)) d[e] = v[e] == -INFINITY ? 0.0f : d[e] + g;
         }
         if (a.d_top) for (uint32_t j = 0; j < a.k; j++) {
             const uint32_t id = (uint32_t)a.top_ids[row * a.k + j];
-            if (id - i0 < 8u && id < a.V) {
+            if (id - (uint32_t)i0 < 8u && id < a.V) {
                 const float t = a.d_top[row * a.k + j] * a.scale;
 #pragma unroll
-                for (int e = 0; e < 8; e++) if (id == i0 + e) d[e] += t;
+                for (int e = 0; e < 8; e++) if (id == (uint32_t)(i0 + e)) d[e] += t;
             }
         }
-        if (whole) store_f32<T, 8, true>(dz + i0, d);
+    }
+};
+
+// A thread takes C chunks, everything they need on its way before the first is worked on.  SAME: of one row, `groups` apart (long rows);
+// else the next ones are a whole grid's width further on.  Chunks begin on 16-byte boundaries of the logits' row; where the gradient's row lies on
+// the same ones they are stored whole too.
+template <typename T, int C, bool SAME>
+__global__ void __launch_bounds__(kThreads) back_kernel(const Back<T> a) {
+    sf_chain_enter();
+    uint32_t n = a.n;
+    if (a.n_dev) n = sf_clamp_rows(*a.n_dev, a.n, a.st);
+    const uint32_t width = SAME ? a.groups : a.chunks;
+    size_t row[C];
+    int i0[C];
+    Chunk<T> in[C];
+    RowBack<T> r[SAME ? 1 : C];
+#pragma unroll
+    for (int u = 0; u < C; u++) {
+        if (SAME && u) { row[u] = row[0]; i0[u] = i0[0] + u * (int)a.groups * 8; }
+        else {
+            const uint64_t at = ((uint64_t)blockIdx.x + (SAME ? 0 : (uint64_t)u * gridDim.x)) * kThreads + threadIdx.x;
+            if (a.few) { row[u] = (uint32_t)at / width; i0[u] = (int)((uint32_t)at % width * 8); }
+            else { row[u] = at / width; i0[u] = (int)(at % width * 8); }
+            if (row[u] < n) { r[u].load(a, row[u]); i0[u] -= (int)shift_of(a.z + row[u] * a.ld); }
+            else i0[u] = (int)a.V;
+        }
+        if (i0[u] < (int)a.V) in[u].fetch(a.z + row[u] * a.ld, i0[u], a.V);
+    }
+#pragma unroll
+    for (int u = 0; u < C; u++) {
+        if (i0[u] >= (int)a.V) continue;
+        if (!SAME || u == 0) r[SAME ? 0 : u].ready(a);
+        float d[8];
+        r[SAME ? 0 : u].chunk(a, row[u], i0[u], in[u], d);
+        T* dz = a.dz + row[u] * a.ldd;
+        if (i0[u] >= 0 && i0[u] + 8 <= (int)a.V && ((uintptr_t)(dz + i0[u]) & 15u) == 0) store_f32<T, 8, true>(dz + i0[u], d);
         else {
 #pragma unroll
-            for (int e = 0; e < 8; e++) if (i0 + e < a.V) dz[i0 + e] = from_f32<T>(d[e]);
+            for (int e = 0; e < 8; e++) if ((uint32_t)(i0[u] + e) < a.V) dz[i0[u] + e] = from_f32<T>(d[e]);
         }
     }
 }
@@ -450,6 +502,11 @@ template <typename T, int TH, int CL> int launch_long(const Rows<T>& a, cudaStre
     lc.attrs = at; lc.numAttrs = CL > 1 ? 2 : 1;
     SF_CUDA(cudaLaunchKernelEx(&lc, long_row_kernel<T, TH, CL>, a));
     return SF_OK;
+}
+
+// entries that the chunks of a row have room for: rows that do not begin on 16-byte boundaries may reach into one chunk more
+uint32_t room_of(const void* p, size_t ld, int dtype, uint32_t V) {
+    return V + (aligned(p, 16) && ld * type_bytes(dtype) % 16 == 0 ? 0 : 16 / type_bytes(dtype) - 1);
 }
 
 bool scale_ok(float s) { return s > 0.0f && s < INFINITY; }
@@ -472,14 +529,15 @@ extern "C" int sf_label_logprobs(sf_ctx* ctx, const void* logits, int dtype, con
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
         const Rows<T> a = {(const T*)logits, ld, n_dev, n, V, scale, labels, logprob_out, entropy_out, lse_out, k, top_ids_out, top_logprobs_out, ctx->d_state};
-        if (V <= 8) return launch_rows<T, 1, 1>(a, st);
-        if (V <= 16) return launch_rows<T, 2, 1>(a, st);
-        if (V <= 32) return launch_rows<T, 4, 1>(a, st);
-        if (V <= 64) return launch_rows<T, 8, 1>(a, st);
-        if (V <= 128) return launch_rows<T, 16, 1>(a, st);
-        if (V <= 256) return launch_rows<T, 32, 1>(a, st);
-        if (V <= 512) return launch_rows<T, 32, 2>(a, st);
-        if (V <= 1024) return launch_rows<T, 32, 4>(a, st);
+        const uint32_t room = room_of(logits, ld, dtype, V);
+        if (room <= 8) return launch_rows<T, 1, 1>(a, st);
+        if (room <= 16) return launch_rows<T, 2, 1>(a, st);
+        if (room <= 32) return launch_rows<T, 4, 1>(a, st);
+        if (room <= 64) return launch_rows<T, 8, 1>(a, st);
+        if (room <= 128) return launch_rows<T, 16, 1>(a, st);
+        if (room <= 256) return launch_rows<T, 32, 1>(a, st);
+        if (room <= 512) return launch_rows<T, 32, 2>(a, st);
+        if (room <= 1024) return launch_rows<T, 32, 4>(a, st);
         // a cluster of eight blocks a row where the rows alone do not fill the machine and are long enough for eight blocks
         if (n < (uint32_t)ctx->num_sms && V >= 16384) return V >= 131072 ? launch_long<T, 512, 8>(a, st) : launch_long<T, 256, 8>(a, st);
         return V <= 8192 ? launch_long<T, 128, 1>(a, st) : (V <= 65536 ? launch_long<T, 256, 1>(a, st) : launch_long<T, 512, 1>(a, st));
@@ -500,15 +558,16 @@ extern "C" int sf_label_logprobs_backward(sf_ctx* ctx, const void* logits, int d
     SF_ON_DEVICE(ctx);
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        Back<T> a = {(const T*)logits, ld, n_dev, n, V, scale, labels, lse, entropy, d_logprob, d_entropy, k, top_ids, d_top_logprobs, (T*)d_logits_out, ldd, (V + 7) / 8, 0, false, ctx->d_state};
-        const bool al = aligned(logits, 16) && aligned(d_logits_out, 16) && (ld * size) % 16 == 0 && (ldd * size) % 16 == 0;
-        constexpr int C = 4;
-        const bool one = a.chunks < 64;
-        a.groups = one ? a.chunks : (a.chunks + C - 1) / C;
-        const uint64_t blocks = ((uint64_t)n * a.groups + kThreads - 1) / kThreads;
+        Back<T> a = {(const T*)logits, ld, n_dev, n, V, scale, labels, lse, entropy, d_logprob, d_entropy, k, top_ids, d_top_logprobs, (T*)d_logits_out, ldd, 0, 0, false, ctx->d_state};
+        a.chunks = (room_of(logits, ld, dtype, V) + 7) / 8;
+        constexpr int C = 4, S = 2;
+        const bool lng = a.chunks >= 64, two = !lng && (uint64_t)n * a.chunks >= (uint64_t)ctx->num_sms * 2048 * S;
+        a.groups = (a.chunks + C - 1) / C;
+        const uint64_t threads = lng ? (uint64_t)n * a.groups : ((uint64_t)n * a.chunks + (two ? S : 1) - 1) / (two ? S : 1);
+        const uint64_t blocks = (threads + kThreads - 1) / kThreads;
         if (blocks > 0x7FFFFFFFu) return (int)SF_ERR_ARG;
-        a.few = blocks * kThreads <= 0xFFFFFFFFu;
-        auto kern = one ? (al ? back_kernel<T, 1, true> : back_kernel<T, 1, false>) : (al ? back_kernel<T, C, true> : back_kernel<T, C, false>);
+        a.few = blocks * kThreads * S <= 0xFFFFFFFFu;
+        auto kern = lng ? back_kernel<T, C, true> : (two ? back_kernel<T, S, false> : back_kernel<T, 1, false>);
         SF_CUDA(sf_launch_chained(kern, (uint32_t)blocks, kThreads, 0, (cudaStream_t)stream, a));
         return (int)SF_OK;
     });
