@@ -29,8 +29,8 @@ template <typename T> struct Rows {
 struct Stat { float m, s, w; };
 // brings (s, w) from maximum m to a larger one
 __device__ __forceinline__ void stat_raise(Stat& a, float m, float c) {
-    const float d = (a.m - m) * c, f = ex2(d);
-    a.w = a.s == 0.0f ? 0.0f : (a.w + a.s * d) * f;
+    const float d = fmaxf((a.m - m) * c, -1e4f), f = ex2(d);       // (from a maximum of -FLT_MAX it would be infinite; 2^-10000 is 0 all the same)
+    a.w = (a.w + a.s * d) * f;
     a.s *= f; a.m = m;
 }
 // N entries more, none above m: masked ones (-infinity) add nothing, a NaN (or an infinity, minus itself) makes s a NaN
