@@ -27,10 +27,9 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     extern __shared__ __align__(16) unsigned char shared[];
     Forward<SL>& sh = reinterpret_cast<Forward<SL>*>(shared)[threadIdx.x / 32];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
-    const uint64_t item = (uint64_t)blockIdx.x * kWarps + threadIdx.x / 32, warps = (uint64_t)a.G * a.cwarps;
-    if (item >= warps * a.q.n_seq) return;
-    const uint32_t s = (uint32_t)(item / warps), g = (uint32_t)(item % warps) / a.cwarps, c0 = (uint32_t)(item % warps) % a.cwarps * CH;
-    const uint32_t ch0 = g * a.per + c0, have = min((uint32_t)CH, a.per - c0);      // the warp's first channel, its channels
+    const Item it = item_of(a, CH);
+    if (it.have == 0) return;
+    const uint32_t s = it.s, g = it.g, ch0 = it.ch0, have = it.have;
     const Range r = range_of(a.q, s, a.st);
     const uint32_t part = blockIdx.y, t_begin = part * a.part_len, t_end = min(r.len, t_begin + a.part_len);
     if (ENDS ? t_begin >= r.len : (part && t_begin >= r.len)) return;
@@ -230,67 +229,98 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
 
 // Single rows (max_len 1): a warp reads its channels' states once, steps them and writes them.
 template <typename T, int SL, bool VEC>
-__global__ void __launch_bounds__(32 * kWarps) step_kernel(const Scan a) {
+__global__ void __launch_bounds__(32 * kWarps, 8) step_kernel(const Scan a) {
     sf_chain_enter();
     constexpr int CL = 32 / SL, CH = 4 * CL;
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
-    const uint64_t item = (uint64_t)blockIdx.x * kWarps + threadIdx.x / 32, warps = (uint64_t)a.G * a.cwarps;
-    if (item >= warps * a.q.n_seq) return;
-    const uint32_t s = (uint32_t)(item / warps), g = (uint32_t)(item % warps) / a.cwarps, c0 = (uint32_t)(item % warps) % a.cwarps * CH;
-    const uint32_t ch0 = g * a.per + c0, have = min((uint32_t)CH, a.per - c0);
+    const Item it = item_of(a, CH);
+    if (it.have == 0) return;
+    const uint32_t s = it.s, g = it.g, ch0 = it.ch0, have = it.have;
     const Range r = range_of(a.q, s, a.st);
     const bool row = r.len > 0;
     if (!row && !a.state_out) return;
     const size_t at = r.first;
-    const T* u_ = (const T*)a.u + at * a.ldu + ch0; const T* d_ = (const T*)a.delta + at * a.lddelta + ch0; const T* z_ = (const T*)a.z + at * a.ldz + ch0;
-    const T* B_ = (const T*)a.B + at * a.ldb + g * a.N; const T* C_ = (const T*)a.C + at * a.ldc + g * a.N;
-    float h[4][4];
+    const bool mine = sl * 4 < (int)a.N;                   // (VEC: all four states are there or none)
     // channel j CL + cl: the warp's accesses to the states of CL channels lie side by side
+    auto read = [&](const float* p, uint32_t c, float (&v)[4]) {
+#pragma unroll
+        for (int n = 0; n < 4; n++) v[n] = 0.0f;
+        if (!p || c >= have) return;
+        if constexpr (VEC) { if (mine) { const float4 q = *reinterpret_cast<const float4*>(p + c * a.N + sl * 4); v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w; } }
+        else {
+#pragma unroll
+            for (int n = 0; n < 4; n++) if (sl * 4 + n < (int)a.N) v[n] = p[c * a.N + sl * 4 + n];
+        }
+    };
+    float h[4][4];
     const float* si = a.state_in && r.slot >= 0 ? a.state_in + ((size_t)r.slot * a.D + ch0) * a.N : nullptr;
     float* so = a.state_out && r.slot >= 0 ? a.state_out + ((size_t)r.slot * a.D + ch0) * a.N : nullptr;
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-        const uint32_t c = j * CL + cl;
-#pragma unroll
-        for (int n = 0; n < 4; n++) h[j][n] = 0.0f;
-        if (si && c < have) {
-            if constexpr (VEC) {
-                if (sl * 4 < (int)a.N) { const float4 v = *reinterpret_cast<const float4*>(si + c * a.N + sl * 4); h[j][0] = v.x; h[j][1] = v.y; h[j][2] = v.z; h[j][3] = v.w; }
-            } else {
-#pragma unroll
-                for (int n = 0; n < 4; n++) if (sl * 4 + n < (int)a.N) h[j][n] = si[c * a.N + sl * 4 + n];
-            }
-        }
-    }
+    for (int j = 0; j < 4; j++) read(si, j * CL + cl, h[j]);
     if (row) {
-        float b[4], cc[4];
+        // What a channel has one of (step, gate) is worked out by one of its SL lanes: a lane owns NO of its four channels
+        constexpr int NO = SL == 1 ? 4 : (SL == 2 ? 2 : 1);
+        auto owned = [&](int i) { return SL == 1 ? i : (SL == 2 ? 2 * sl + i : 2 * (sl & 1) + (sl >> 1 & 1)); };
+        auto owner = [&](int j) { return lane - sl + (SL == 1 ? 0 : (SL == 2 ? j / 2 : j / 2 + 2 * (j % 2))); };
+        float b[4], cc[4], u[NO], d[NO], z[NO], in[NO];
+#pragma unroll
+        for (int i = 0; i < NO; i++) {
+            const uint32_t c = owned(i) * CL + cl;
+            const bool there = c < have;
+            u[i] = there ? to_f32(((const T*)a.u)[at * a.ldu + ch0 + c]) : 0.0f;
+            d[i] = there ? to_f32(((const T*)a.delta)[at * a.lddelta + ch0 + c]) : 0.0f;
+            z[i] = there && a.z ? to_f32(((const T*)a.z)[at * a.ldz + ch0 + c]) : 0.0f;
+        }
 #pragma unroll
         for (int n = 0; n < 4; n++) {
             const bool there = sl * 4 + n < (int)a.N;
-            b[n] = there ? to_f32(B_[sl * 4 + n]) : 0.0f;
-            cc[n] = there ? to_f32(C_[sl * 4 + n]) : 0.0f;
+            b[n] = there ? to_f32(((const T*)a.B)[at * a.ldb + g * a.N + sl * 4 + n]) : 0.0f;
+            cc[n] = there ? to_f32(((const T*)a.C)[at * a.ldc + g * a.N + sl * 4 + n]) : 0.0f;
         }
 #pragma unroll
+        for (int i = 0; i < NO; i++) {
+            const uint32_t c = owned(i) * CL + cl;
+            float unused;
+            if (c < have && a.dbias) d[i] += __ldg(a.dbias + ch0 + c);
+            if (a.softplus) d[i] = softplus_of(d[i], unused);
+            in[i] = d[i] * u[i];
+        }
+        float y[4];
+#pragma unroll
         for (int j = 0; j < 4; j++) {
-            const uint32_t c = j * CL + cl;
-            const bool there = c < have;
-            const float u = there ? to_f32(u_[c]) : 0.0f;
-            float d = there ? to_f32(d_[c]) : 0.0f, unused;
-            if (there && a.dbias) d += __ldg(a.dbias + ch0 + c);
-            if (a.softplus) d = softplus_of(d, unused);
-            float y = 0.0f;
+            const int i = SL == 1 ? j : (SL == 2 ? j % 2 : 0);
+            const float dj = SL == 1 ? d[i] : __shfl_sync(0xFFFFFFFFu, d[i], owner(j)), ij = SL == 1 ? in[i] : __shfl_sync(0xFFFFFFFFu, in[i], owner(j));
+            float A[4];
+            read(a.A + (size_t)ch0 * a.N, j * CL + cl, A);
+            y[j] = 0.0f;
 #pragma unroll
             for (int n = 0; n < 4; n++) {
-                const float A = there && sl * 4 + n < (int)a.N ? __ldg(a.A + (size_t)(ch0 + c) * a.N + sl * 4 + n) * kLog2e : 0.0f;
-                h[j][n] = fmaf(decay(d, A), h[j][n], d * u * b[n]);
-                y = fmaf(h[j][n], cc[n], y);
+                h[j][n] = fmaf(decay(dj, A[n] * kLog2e), h[j][n], ij * b[n]);
+                y[j] = fmaf(h[j][n], cc[n], y[j]);
             }
+        }
+        if constexpr (SL >= 2) {
+            const bool hi = sl & 1;
+            const float k0 = hi ? y[2] : y[0], k1 = hi ? y[3] : y[1], s0 = hi ? y[0] : y[2], s1 = hi ? y[1] : y[3];
+            y[0] = k0 + __shfl_xor_sync(0xFFFFFFFFu, s0, 1);
+            y[1] = k1 + __shfl_xor_sync(0xFFFFFFFFu, s1, 1);
+        }
+        if constexpr (SL >= 4) {
+            const bool hi = sl & 2;
+            const float k0 = hi ? y[1] : y[0], s0 = hi ? y[0] : y[1];
+            y[0] = k0 + __shfl_xor_sync(0xFFFFFFFFu, s0, 2);
+        }
 #pragma unroll
-            for (int m = 1; m < SL; m <<= 1) y += __shfl_xor_sync(0xFFFFFFFFu, y, m);
-            if (there && sl == 0) {
-                if (a.Dk) y = fmaf(__ldg(a.Dk + ch0 + c), u, y);
-                if (a.z) { const float z = to_f32(z_[c]); y *= z * sigmoid(z); }
-                ((T*)a.y)[at * a.ldy + ch0 + c] = from_f32<T>(y);
+        for (int m = 4; m < SL; m <<= 1) y[0] += __shfl_xor_sync(0xFFFFFFFFu, y[0], m);
+        if (SL <= 4 || sl < 4) {
+#pragma unroll
+            for (int i = 0; i < NO; i++) {
+                const uint32_t c = owned(i) * CL + cl;
+                if (c >= have) continue;
+                float v = y[i];
+                if (a.Dk) v = fmaf(__ldg(a.Dk + ch0 + c), u[i], v);
+                if (a.z) v *= z[i] * sigmoid(z[i]);
+                ((T*)a.y)[at * a.ldy + ch0 + c] = from_f32<T>(v);
             }
         }
     }
@@ -299,9 +329,8 @@ __global__ void __launch_bounds__(32 * kWarps) step_kernel(const Scan a) {
         for (int j = 0; j < 4; j++) {
             const uint32_t c = j * CL + cl;
             if (c >= have) continue;
-            if constexpr (VEC) {
-                if (sl * 4 < (int)a.N) *reinterpret_cast<float4*>(so + c * a.N + sl * 4) = make_float4(h[j][0], h[j][1], h[j][2], h[j][3]);
-            } else {
+            if constexpr (VEC) { if (mine) *reinterpret_cast<float4*>(so + c * a.N + sl * 4) = make_float4(h[j][0], h[j][1], h[j][2], h[j][3]); }
+            else {
 #pragma unroll
                 for (int n = 0; n < 4; n++) if (sl * 4 + n < (int)a.N) so[c * a.N + sl * 4 + n] = h[j][n];
             }
@@ -349,7 +378,7 @@ extern "C" int sf_seq_scan(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_r
         return by_states(p.sl, [&](auto lanes) {
             constexpr int SL = decltype(lanes)::value, VV = 16 / (int)sizeof(T);
             if (seq->max_len == 1 && !starts_out) {
-                const bool v4 = in->N % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16);
+                const bool v4 = in->N % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16) && aligned(in->A, 16);
                 return launch(v4 ? step_kernel<T, SL, true> : step_kernel<T, SL, false>, (uint32_t)blocks, 32 * kWarps, 0, st, a);
             }
             const size_t smem = sizeof(Forward<SL>) * kWarps;

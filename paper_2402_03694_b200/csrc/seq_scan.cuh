@@ -46,6 +46,7 @@ struct Scan {
     float* sum_par;                        // [runs][D][N + 2]: dA, dD, dbias
     uint32_t runs;                         // blocks behind one another over the sequences' parts
     uint32_t cwarps;                       // warps over the channels of a group
+    bool few;                              // warps of all sequences in 32 bits
     uint32_t cblocks;                      // blocks over them
     sf_dev_state* st;
 };
@@ -92,6 +93,21 @@ template <int SL> struct Shape {
     static constexpr int CL = 32 / SL, CH = 4 * CL, NP = 4 * SL;               // channel lanes, channels of a warp, states with those that fill up
     static constexpr int K = SL == 1 ? 4 : 8;                                  // rows of a tile of the forward pass (kEvery is a multiple)
 };
+
+// What a warp works on: sequence, group, first of its channels within the group and of all, and how many it has (none: nothing to do)
+struct Item { uint32_t s, g, c0, ch0, have; };
+__device__ __forceinline__ Item item_of(const Scan& a, uint32_t CH) {
+    const uint32_t warps = a.G * a.cwarps, w = threadIdx.x / 32;
+    Item i;
+    uint32_t k;
+    if (a.few) { const uint32_t at = blockIdx.x * kWarps + w; i.s = at / warps; k = at % warps; }
+    else { const uint64_t at = (uint64_t)blockIdx.x * kWarps + w; i.s = (uint32_t)(at / warps); k = (uint32_t)(at % warps); }
+    i.g = a.G == 1 ? 0 : k / a.cwarps;
+    i.c0 = (k - i.g * a.cwarps) * CH;
+    i.ch0 = i.g * a.per + i.c0;
+    i.have = i.s < a.q.n_seq ? min(CH, a.per - i.c0) : 0;
+    return i;
+}
 
 // How a warp stages a tile of K rows of CH channels: pieces of VV channels, piece i of a lane at row t(i), channel c(i).  Lanes without a piece have rows from K on.
 template <int K, int CH, int VV> struct Pieces {
@@ -163,11 +179,21 @@ __global__ void __launch_bounds__(256) parts_kernel(const Scan a) {
     float h = in && r.slot >= 0 ? in[(size_t)r.slot * DN + at] : 0.0f;
     float* ps = a.part_state + (size_t)s * a.parts * DN + at;
     const float* steps = a.part_step + (size_t)s * a.parts * a.D + at / a.N;
-    for (uint32_t i = 0; i < parts; i++) {
-        const uint32_t p = BACK ? parts - 1 - i : i;
-        const float end = ps[(size_t)p * DN];
-        ps[(size_t)p * DN] = h;
-        h = fmaf(decay(steps[(size_t)p * a.D], A), h, end);
+    constexpr uint32_t U = 8;                              // parts on their way at once: only h goes from one to the next
+    for (uint32_t i0 = 0; i0 < parts; i0 += U) {
+        float end[U], step[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; u++) {
+            const uint32_t p = BACK ? parts - 1 - (i0 + u) : i0 + u;
+            if (i0 + u < parts) { end[u] = ps[(size_t)p * DN]; step[u] = steps[(size_t)p * a.D]; }
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < U; u++) {
+            const uint32_t p = BACK ? parts - 1 - (i0 + u) : i0 + u;
+            if (i0 + u >= parts) continue;
+            ps[(size_t)p * DN] = h;
+            h = fmaf(decay(step[u], A), h, end[u]);
+        }
     }
     if (!BACK && parts == 0) ps[0] = h;
     if (out && r.slot >= 0) out[(size_t)r.slot * DN + at] = h;
@@ -178,18 +204,20 @@ inline int state_lanes(uint32_t N) { int sl = 1; while ((uint32_t)(4 * sl) < N) 
 
 struct Plan { uint32_t sl, cwarps, cblocks, part_len, parts, runs; bool split; };
 
-// Sequences go in parts where the warps of whole sequences would leave most of the machine idle: two passes over the inputs then, so only
-// where parts make three times as many warps.
+// Where warps or channels are few a warp takes fewer channels (more state lanes than states need: lanes stay idle, but a tile is staged and walked by more warps),
+// and where they would still leave most of the machine idle, sequences go in parts: two passes over the inputs then, so only where parts make three times
+// as many warps.
 inline Plan plan_of(uint32_t n_seq, uint32_t max_len, uint32_t D, uint32_t N, uint32_t G, bool backward) {
     Plan p;
     p.sl = state_lanes(N);
-    const uint32_t CH = 128 / p.sl, per = D / G;
-    p.cwarps = (per + CH - 1) / CH;
+    const uint32_t per = D / G;
+    const uint64_t full = (uint64_t)SF_NUM_SMS_DEFAULT * (backward ? 8 : 16);
+    auto warps = [&]() { p.cwarps = (per + 128 / p.sl - 1) / (128 / p.sl); return std::max<uint64_t>(1, (uint64_t)n_seq * G * p.cwarps); };
+    while (max_len > 1 && p.sl < 16 && (64 / p.sl >= per || warps() * ((max_len + 63) / 64) < full / 4)) p.sl *= 2;
+    const uint64_t want = full / warps();
     p.cblocks = (p.cwarps + kWarps - 1) / kWarps;
-    const uint64_t warps = std::max<uint64_t>(1, (uint64_t)n_seq * G * p.cwarps), full = (uint64_t)SF_NUM_SMS_DEFAULT * (backward ? 8 : 16);
-    uint64_t want = full / warps;
     p.part_len = (max_len + kEvery - 1) / kEvery * kEvery;
-    if (want >= 3 && max_len > 2 * 64) p.part_len = (uint32_t)std::max<uint64_t>(64, ((max_len + want - 1) / want + kEvery - 1) / kEvery * kEvery);
+    if (want >= 3 && max_len > 2 * 32) p.part_len = (uint32_t)std::max<uint64_t>(32, ((max_len + want - 1) / want + kEvery - 1) / kEvery * kEvery);
     p.parts = (max_len + p.part_len - 1) / p.part_len;
     p.split = p.parts > 1;
     const uint64_t blocks = (uint64_t)G * p.cblocks, items = std::max<uint64_t>(1, (uint64_t)n_seq * p.parts);
@@ -236,6 +264,7 @@ inline void fill(Scan& a, const sf_sequences* seq, const sf_scan_rows* in, uint3
     a.D = in->D; a.N = in->N; a.G = in->G; a.per = in->D / in->G; a.softplus = in->softplus != 0;
     a.n4 = in->N % 4 == 0;
     a.part_len = p.part_len; a.parts = p.parts; a.runs = p.runs; a.cwarps = p.cwarps; a.cblocks = p.cblocks;
+    a.few = ((uint64_t)seq->n_seq + 1) * in->G * p.cwarps + kWarps <= 0xFFFFFFFFu;
     a.st = ctx->d_state;
 }
 // rows begin on 16-byte boundaries, and so does every group's first channel and state

@@ -97,6 +97,22 @@ __device__ __forceinline__ void stage(const Scan& a, Backward<SL>& sh, size_t ro
     ns.stage(&sh.bc[0][0][0], lane);
 }
 
+// asks for the rows of the next tile and the state before it, so that they are in L2 by then
+__device__ __forceinline__ void to_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+template <typename T, int SL, int VV>
+__device__ __forceinline__ void ahead(const Scan& a, size_t row0, size_t start, uint32_t ch0, uint32_t have, int lane) {
+    const Pieces<K, Shape<SL>::CH, VV> pc(lane);
+    if (VV > 1 && pc.lc < (int)have && pc.lt < K) {        // (the first piece of a row's line will do; narrow pieces would ask a line many times)
+        const size_t at = row0 + pc.lt;
+        to_l2((const T*)a.delta + at * a.lddelta + ch0 + pc.lc);
+        to_l2((const T*)a.u + at * a.ldu + ch0 + pc.lc);
+        to_l2((const T*)a.dy + at * a.lddy + ch0 + pc.lc);
+        if (a.z) to_l2((const T*)a.z + at * a.ldz + ch0 + pc.lc);
+    }
+    const uint32_t floats = have * a.N;                    // (the warp's channels lie side by side)
+    for (uint32_t i = lane * 32; i < floats; i += 32 * 32) to_l2(a.starts + start * a.D * a.N + (size_t)ch0 * a.N + i);
+}
+
 template <int SL> __device__ __forceinline__ void channel_params(const Scan& a, Backward<SL>& sh, uint32_t ch0, uint32_t have, int lane) {
     for (int c = lane; c < Shape<SL>::CH; c += 32) {
         sh.bias[c] = c < (int)have && a.dbias ? __ldg(a.dbias + ch0 + c) : 0.0f;
@@ -148,10 +164,9 @@ __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
     extern __shared__ __align__(16) unsigned char shared[];
     Backward<SL>& sh = reinterpret_cast<Backward<SL>*>(shared)[threadIdx.x / 32];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
-    const uint64_t item = (uint64_t)blockIdx.x * kWarps + threadIdx.x / 32, warps = (uint64_t)a.G * a.cwarps;
-    if (item >= warps * a.q.n_seq) return;
-    const uint32_t s = (uint32_t)(item / warps), g = (uint32_t)(item % warps) / a.cwarps, c0 = (uint32_t)(item % warps) % a.cwarps * CH;
-    const uint32_t ch0 = g * a.per + c0, have = min((uint32_t)CH, a.per - c0);
+    const Item it = item_of(a, CH);
+    if (it.have == 0) return;
+    const uint32_t s = it.s, g = it.g, ch0 = it.ch0, have = it.have;
     const Range r = range_of(a.q, s, a.st);
     const uint32_t part = blockIdx.y, t_begin = part * a.part_len, t_end = min(r.len, t_begin + a.part_len);
     if (t_begin >= r.len) return;
@@ -289,6 +304,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
             f2 h[2][4];
             load_states(h, a.starts + start_index(r.first, s, t0) * DN, a, ch0, have, cl, sl, 1.0f);
             stage<T, SL, VV, false>(a, sh, row0, ch0, have, g, rows, lane);
+            if (tile) ahead<T, SL, VV>(a, row0 - K, start_index(r.first, s, t0 - K), ch0, have, lane);
             __syncwarp();
             auto keep = [&](int q) {
 #pragma unroll
