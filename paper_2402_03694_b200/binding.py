@@ -661,34 +661,40 @@ def make_sequences(offsets, max_len, counts=None, slots=None):
     return q
 
 
-def _of(t, code, n, d, on, w):
-    """(address, pitch) of rows of the same type and shape; None stays None."""
+def _of(t, like, shape, on, w):
+    """(address, pitch) of rows of the type `like` and this shape on device `on`; None stays None."""
     if t is None:
         return None, 0
-    p, c, m, e, ld = _rows(t, on, w)
-    if (c, m, e) != (code, n, d):
+    if t.dtype != like or t.shape != shape or t.get_device() != on:
         raise SfError(SF_ERR_ARG, w)
-    return p, ld
+    n, d = shape
+    ld, s1 = t.stride()
+    if n <= 1:
+        ld = d
+    if ld < d or (d > 1 and s1 != 1):
+        raise SfError(SF_ERR_ARG, w)
+    return t.data_ptr(), ld
 
 
 def _reals(t, shape, on, w):
     return None if t is None else _whole(t, shape, on, w, True)
 
 
-def _pool(t, shape, like, on, w):
-    """(address, states) of a pool of states [slots][..shape] of type `like` (None: no pool)."""
-    if t is None:
-        return None, None
-    if t.get_device() != on or t.dtype != like or t.dim() != 1 + len(shape) or tuple(t.shape[1:]) != shape or not t.is_contiguous() or t.shape[0] > _U32:
-        raise SfError(SF_ERR_ARG, w)
-    return t.data_ptr(), t.shape[0]
-
-
-def _slots_of(w, *counts):
-    """The number of states of a call's pools, which all have as many (none: 0)."""
-    have = {c for c in counts if c is not None}
-    _arg(len(have) <= 1, w)
-    return have.pop() if have else 0
+def _pools(w, on, like, shape, *pools):
+    """Number of states of a call's pools [slots][..shape] of type `like`, which all have as many (none: 0), and their addresses."""
+    m, out = None, []
+    for t in pools:
+        if t is None:
+            out.append(None)
+            continue
+        if m is None:
+            m = t.shape[0] if t.dim() else 0
+            if m > _U32:
+                raise SfError(SF_ERR_ARG, w)
+        if t.dtype != like or t.shape != (m, *shape) or t.get_device() != on or not t.is_contiguous():
+            raise SfError(SF_ERR_ARG, w)
+        out.append(t.data_ptr())
+    return (m or 0, *out)
 
 
 def _bytes(t, on, w):
@@ -703,13 +709,13 @@ def sf_seq_conv(ctx, seq, x, w, y_out, bias=None, act=SF_ACT_NONE, state_in=None
     s = "sf_seq_conv"
     on = _device_of(ctx, s)
     p, dt, n, D, ld = _rows(x, on, s)
-    q, ldy = _of(y_out, dt, n, D, on, s)
-    _arg(w.dim() == 2 and w.shape[0] == D and seq._on == on, s)
+    q, ldy = _of(y_out, x.dtype, x.shape, on, s)
+    if w.dim() != 2 or seq._on != on:
+        raise SfError(SF_ERR_ARG, s)
     W = w.shape[1]
-    si, m1 = _pool(state_in, (W - 1, D), x.dtype, on, s)
-    so, m2 = _pool(state_out, (W - 1, D), x.dtype, on, s)
-    _check(_lib().sf_seq_conv(ctx, seq, p, dt, n, D, ld, _whole(w, (D, W), on, s, True), _reals(bias, (D,), on, s), W, act, si, so,
-                              _slots_of(s, m1, m2), q, ldy, _stream_on(on, stream)), s)
+    m, si, so = _pools(s, on, x.dtype, (W - 1, D), state_in, state_out)
+    _check(_lib().sf_seq_conv(ctx, seq, p, dt, n, D, ld, _whole(w, (D, W), on, s, True), _reals(bias, (D,), on, s), W, act, si, so, m, q, ldy,
+                              _stream_on(on, stream)), s)
 
 
 def sf_seq_conv_backward_workspace(n_seq, max_len, D, W):
@@ -726,16 +732,15 @@ def sf_seq_conv_backward(ctx, seq, x, w, dy, workspace, bias=None, act=SF_ACT_NO
     s = "sf_seq_conv_backward"
     on = _device_of(ctx, s)
     p, dt, n, D, ld = _rows(x, on, s)
-    g, ldg = _of(dy, dt, n, D, on, s)
-    q, ldq = _of(dx_out, dt, n, D, on, s)
-    _arg(w.dim() == 2 and w.shape[0] == D and seq._on == on, s)
+    g, ldg = _of(dy, x.dtype, x.shape, on, s)
+    q, ldq = _of(dx_out, x.dtype, x.shape, on, s)
+    if g is None or w.dim() != 2 or seq._on != on:
+        raise SfError(SF_ERR_ARG, s)
     W = w.shape[1]
-    si, m1 = _pool(state_in, (W - 1, D), x.dtype, on, s)
-    ds, m2 = _pool(d_state, (W - 1, D), x.dtype, on, s)
-    do, m3 = _pool(d_state_in_out, (W - 1, D), x.dtype, on, s)
+    m, si, ds, do = _pools(s, on, x.dtype, (W - 1, D), state_in, d_state, d_state_in_out)
     wp, wb = _bytes(workspace, on, s)
     _check(_lib().sf_seq_conv_backward(ctx, seq, p, dt, n, D, ld, _whole(w, (D, W), on, s, True), _reals(bias, (D,), on, s), W, act, si, g, ldg, ds,
-                                       _slots_of(s, m1, m2, m3), q, ldq, _reals(dw_out, (D, W), on, s), _reals(dbias_out, (D,), on, s), do, wp, wb,
+                                       m, q, ldq, _reals(dw_out, (D, W), on, s), _reals(dbias_out, (D,), on, s), do, wp, wb,
                                        _stream_on(on, stream)), s)
 
 
@@ -759,27 +764,23 @@ def sf_seq_scan_starts(n_seq, rows, D, N):
 
 def _scan_rows(ctx, seq, u, delta, A, B, C_, D_skip, delta_bias, z, softplus, s):
     on = _device_of(ctx, s)
-    r = sf_scan_rows()
-    r.u, dt, n, D, r.ldu = _rows(u, on, s)
-    _arg(A.dim() == 2 and A.shape[0] == D and A.shape[1] >= 1 and B.dim() == 2 and seq._on == on, s)
-    N = A.shape[1]
-    GN = B.shape[1]
-    _arg(GN % N == 0, s)
-    r.delta, r.ld_delta = _of(delta, dt, n, D, on, s)
-    r.z, r.ldz = _of(z, dt, n, D, on, s)
-    r.B, r.ldb = _of(B, dt, n, GN, on, s)
-    r.C, r.ldc = _of(C_, dt, n, GN, on, s)
-    r.A, r.D_skip, r.delta_bias = _whole(A, (D, N), on, s, True), _reals(D_skip, (D,), on, s), _reals(delta_bias, (D,), on, s)
-    r.D, r.N, r.G, r.dtype, r.softplus = D, N, GN // N, dt, int(softplus)
-    return on, r, n
+    pu, dt, n, D, ldu = _rows(u, on, s)
+    if A.dim() != 2 or B.dim() != 2 or seq._on != on or A.shape[1] == 0 or B.shape[1] % A.shape[1]:
+        raise SfError(SF_ERR_ARG, s)
+    N, GN, t, wide = A.shape[1], B.shape[1], u.dtype, u.shape
+    pd, ldd = _of(delta, t, wide, on, s)
+    pz, ldz = _of(z, t, wide, on, s)
+    pb, ldb = _of(B, t, (n, GN), on, s)
+    pc, ldc = _of(C_, t, (n, GN), on, s)
+    r = sf_scan_rows(pu, pd, pb, pc, pz, ldu, ldd, ldb, ldc, ldz, _whole(A, (D, N), on, s, True), _reals(D_skip, (D,), on, s), _reals(delta_bias, (D,), on, s),
+                     D, N, GN // N, dt, 1 if softplus else 0)
+    return on, r, n, D, N, GN // N
 
 
 _EVERY = 8                        # rows between two states that the scan keeps for its backward pass
 
 
 def _room(t, floats, on, w):
-    if t is None:
-        return None
     return _flat(t, floats, 4, on, w, True)
 
 
@@ -788,13 +789,12 @@ def sf_seq_scan(ctx, seq, u, delta, A, B, C, y_out, D=None, delta_bias=None, z=N
     """y_out [rows][D] from u, delta [rows][D] (z likewise), B, C [rows][G * N], A float32 [D][N], D and delta_bias float32 [D]; states float32
     [slots][D][N]."""
     s = "sf_seq_scan"
-    on, r, n = _scan_rows(ctx, seq, u, delta, A, B, C, D, delta_bias, z, softplus, s)
-    q, ldy = _of(y_out, r.dtype, n, r.D, on, s)
-    si, m1 = _pool(state_in, (r.D, r.N), A.dtype, on, s)
-    so, m2 = _pool(state_out, (r.D, r.N), A.dtype, on, s)
+    on, r, n, d, N, _ = _scan_rows(ctx, seq, u, delta, A, B, C, D, delta_bias, z, softplus, s)
+    q, ldy = _of(y_out, u.dtype, u.shape, on, s)
+    m, si, so = _pools(s, on, A.dtype, (d, N), state_in, state_out)
     wp, wb = _bytes(workspace, on, s)
-    _check(_lib().sf_seq_scan(ctx, seq, r, n, si, so, _slots_of(s, m1, m2), _room(starts_out, (n // _EVERY + seq.n_seq) * r.D * r.N, on, s), q, ldy, wp, wb,
-                              _stream_on(on, stream)), s)
+    _check(_lib().sf_seq_scan(ctx, seq, r, n, si, so, m, None if starts_out is None else _room(starts_out, (n // _EVERY + seq.n_seq) * d * N, on, s), q, ldy,
+                              wp, wb, _stream_on(on, stream)), s)
 
 
 def sf_seq_scan_backward(ctx, seq, u, delta, A, B, C, dy, starts, workspace, D=None, delta_bias=None, z=None, softplus=False, du_out=None, d_delta_out=None,
@@ -802,19 +802,18 @@ def sf_seq_scan_backward(ctx, seq, u, delta, A, B, C, dy, starts, workspace, D=N
                          stream=None):
     """Inputs as in sf_seq_scan and the starts it wrote; any gradient may be None."""
     s = "sf_seq_scan_backward"
-    on, r, n = _scan_rows(ctx, seq, u, delta, A, B, C, D, delta_bias, z, softplus, s)
-    g, ldg = _of(dy, r.dtype, n, r.D, on, s)
-    o = sf_scan_grads()
-    o.du, o.lddu = _of(du_out, r.dtype, n, r.D, on, s)
-    o.d_delta, o.ldd_delta = _of(d_delta_out, r.dtype, n, r.D, on, s)
-    o.dz, o.lddz = _of(dz_out, r.dtype, n, r.D, on, s)
-    o.dB, o.lddb = _of(dB_out, r.dtype, n, r.G * r.N, on, s)
-    o.dC, o.lddc = _of(dC_out, r.dtype, n, r.G * r.N, on, s)
-    o.dA, o.dD_skip, o.d_delta_bias = _reals(dA_out, (r.D, r.N), on, s), _reals(dD_out, (r.D,), on, s), _reals(d_delta_bias_out, (r.D,), on, s)
-    ds, m1 = _pool(d_state, (r.D, r.N), A.dtype, on, s)
-    do, m2 = _pool(d_state_in_out, (r.D, r.N), A.dtype, on, s)
+    on, r, n, d, N, G = _scan_rows(ctx, seq, u, delta, A, B, C, D, delta_bias, z, softplus, s)
+    t, wide, states = u.dtype, u.shape, (n, G * N)
+    g, ldg = _of(dy, t, wide, on, s)
+    pu, lu = _of(du_out, t, wide, on, s)
+    pd, ld = _of(d_delta_out, t, wide, on, s)
+    pz, lz = _of(dz_out, t, wide, on, s)
+    pb, lb = _of(dB_out, t, states, on, s)
+    pc, lc = _of(dC_out, t, states, on, s)
+    o = sf_scan_grads(pu, pd, pb, pc, pz, lu, ld, lb, lc, lz, _reals(dA_out, (d, N), on, s), _reals(dD_out, (d,), on, s), _reals(d_delta_bias_out, (d,), on, s))
+    m, ds, do = _pools(s, on, A.dtype, (d, N), d_state, d_state_in_out)
     wp, wb = _bytes(workspace, on, s)
-    _check(_lib().sf_seq_scan_backward(ctx, seq, r, n, g, ldg, _room(starts, (n // _EVERY + seq.n_seq) * r.D * r.N, on, s), ds, do, _slots_of(s, m1, m2), o, wp, wb,
+    _check(_lib().sf_seq_scan_backward(ctx, seq, r, n, g, ldg, _room(starts, (n // _EVERY + seq.n_seq) * d * N, on, s), ds, do, m, o, wp, wb,
                                        _stream_on(on, stream)), s)
 
 
@@ -845,7 +844,7 @@ def sf_label_logprobs_backward(ctx, logits, labels, lse, d_logits_out, d_logprob
     w = "sf_label_logprobs_backward"
     on = _device_of(ctx, w)
     p, dt, n, V, ld = _rows(logits, on, w)
-    q, ldd = _of(d_logits_out, dt, n, V, on, w)
+    q, ldd = _of(d_logits_out, logits.dtype, logits.shape, on, w)
     k, ti, tl = _top(top_ids, d_top_logprobs, n, on, w)
     _check(_lib().sf_label_logprobs_backward(ctx, p, dt, _flat(n_dev, 1, 4, on, w), n, V, ld, scale, None if labels is None else _whole(labels, (n,), on, w),
                                              _reals(lse, (n,), on, w), _reals(d_logprob, (n,), on, w), _reals(entropy, (n,), on, w), _reals(d_entropy, (n,), on, w),
