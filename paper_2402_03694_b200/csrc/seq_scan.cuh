@@ -138,14 +138,23 @@ template <typename T, int VV> __device__ __forceinline__ Piece<T, VV> fetch(cons
 template <typename T, int VV, int K, int NP> struct States {
     static constexpr int PV = NP >= VV ? VV : 1, PR = NP / PV, I = (2 * K * PR + 31) / 32;
     Piece<T, PV> p[I];
+    // where piece i of a lane lies, and whether it is there
+    template <typename U> __device__ __forceinline__ static const U* piece(const Scan& a, int i, size_t row0, uint32_t col, int rows, int lane, bool& there) {
+        const int k = i * 32 + lane, t = k / PR % K, n = k % PR * PV;
+        const bool second = k >= K * PR;
+        there = k < 2 * K * PR && t < rows && n < (int)a.N;
+        const U* p = (const U*)(second ? a.C : a.B);
+        return there ? p + (row0 + t) * (second ? a.ldc : a.ldb) + col + n : p;
+    }
     __device__ __forceinline__ void fetch_all(const Scan& a, size_t row0, uint32_t col, int rows, int lane) {
 #pragma unroll
         for (int i = 0; i < I; i++) {
-            const int k = i * 32 + lane, t = k / PR % K, n = k % PR * PV;
-            const bool second = k >= K * PR;
-            p[i] = fetch<T, PV>(second ? a.C : a.B, (row0 + t) * (second ? a.ldc : a.ldb) + col + n, k < 2 * K * PR && t < rows && n < (int)a.N);
+            bool there;
+            const T* q = piece<T>(a, i, row0, col, rows, lane, there);
+            p[i] = fetch<T, PV>(q, 0, there);
         }
     }
+    __device__ __forceinline__ void take(int i, uint4 w) { if constexpr (PV * sizeof(T) == 16) p[i].w = w; }
     __device__ __forceinline__ void stage(float* sh, int lane) const {
 #pragma unroll
         for (int i = 0; i < I; i++) {

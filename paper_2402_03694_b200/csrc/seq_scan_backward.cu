@@ -8,38 +8,99 @@ using namespace sfscan;
 constexpr int K = (int)kEvery;             // rows of a tile
 constexpr int R = 4;                       // rows whose decays and states a thread holds at once
 
-// What a warp keeps in shared memory for a tile; rows of channels spaced so that 16-byte accesses of eight lanes meet no common bank
-template <int SL> struct __align__(16) Backward {
+// What a warp keeps in shared memory.  Sums over states (s1, s2, y) and over channels (dbc) are left as one part a lane, for R rows, and joined where they are
+// used; rows are spaced so that the 16-byte accesses of eight lanes meet no common bank.
+template <typename T, int SL, int VV> struct __align__(16) Backward {
     typedef Shape<SL> S;
-    static constexpr int PX = S::CH + 4;
+    typedef Pieces<K, S::CH, VV> P;
+    typedef States<T, VV, K, S::NP> ST;
+    static constexpr int PX = S::CH + 4, PY = S::CH + (SL == 1 ? 0 : (SL == 2 ? 16 : (SL == 4 ? 8 : 4))), PT = SL * PY + 4;
+    static constexpr int ON_WAY = VV > 1 ? 4 * P::I + ST::I + 4 : 1;
     float step[K][PX], u[K][PX], e[K][PX];                 // delta; u; dout silu(z)
-    float dstep[K][PX], dgate[K][PX];                      // d delta / d raw; dout silu'(z).  A row that is done leaves du (without D e), ddelta and dz in step, dstep and dgate
+    float dstep[K][PX], dgate[K][PX];                      // d delta / d raw; dout silu'(z)
     float bc[2][K][S::NP];                                 // B, C
-    float sum[K][2][S::NP];                                // the warp's dB, dC
-    float4 start[K / R][4][32];                            // the states before rows 0, R, .., every lane its own
+    float s1[R][PT], s2[R][PT], y[R][PT];                  // sum g B; sum (a g) h_{t-1} A; sum C h
+    float dbc[R][2][S::CL][S::NP];                         // dB, dC
+    float4 start[K / R][4][32];                            // the states before rows 0 and R, every lane its own
+    uint4 way[ON_WAY][32];                                 // the next tile's pieces on their way, every lane its own
     float bias[S::CH], skip[S::CH];
 };
 
+__device__ __forceinline__ void copy16(void* to, const void* from, bool there) {     // (zeros where there is nothing)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// Asks for a tile's pieces: steps, gradients of the outputs, gates, and (not ENDS) inputs and the state before the tile.  Whole pieces only; others are read when staged.
+template <typename T, int SL, int VV, bool ENDS>
+__device__ __forceinline__ void ask(const Scan& a, Backward<T, SL, VV>& sh, size_t row0, size_t start, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
+    if constexpr (VV > 1) {
+        typedef Backward<T, SL, VV> Sh;
+        typedef typename Sh::P P;
+        const P pc(lane);
+        const size_t at = row0 + pc.lt;
+        const T* from[4] = {(const T*)a.delta, (const T*)a.dy, (const T*)a.z, (const T*)a.u};
+        const size_t ld[4] = {a.lddelta, a.lddy, a.ldz, a.ldu};
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            if (k == 2 ? a.z == nullptr : (k == 3 && ENDS)) continue;
+#pragma unroll
+            for (int i = 0; i < P::I; i++) {
+                const bool there = pc.t(i) < rows && pc.c(i) < (int)have;
+                copy16(&sh.way[k * P::I + i][lane], there ? from[k] + at * ld[k] + ch0 + pc.lc + P::step(i, ld[k]) : from[k], there);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < Sh::ST::I; i++) {
+            bool there;
+            const T* p = Sh::ST::template piece<T>(a, i, row0, g * a.N, rows, lane, there);
+            copy16(&sh.way[4 * P::I + i][lane], p, there);
+        }
+        if (!ENDS) {
+            const int cl = lane / SL, sl = lane % SL;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const bool there = cl * 4 + j < (int)have && sl * 4 < (int)a.N;
+                const float* p = a.starts + start * a.D * a.N;
+                copy16(&sh.way[4 * P::I + Sh::ST::I + j][lane], there ? p + (size_t)(ch0 + cl * 4 + j) * a.N + sl * 4 : p, there);
+            }
+        }
+    }
+}
+
 // stages steps, inputs and gradients of the rows t0 .. t0 + K - 1 as far as there (zeros behind: they then change nothing); ENDS: what the pass for the parts' ends needs
 template <typename T, int SL, int VV, bool ENDS>
-__device__ __forceinline__ void stage(const Scan& a, Backward<SL>& sh, size_t row0, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
-    typedef Shape<SL> S;
-    typedef Pieces<K, S::CH, VV> P;
+__device__ __forceinline__ void stage(const Scan& a, Backward<T, SL, VV>& sh, size_t row0, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
+    typedef Backward<T, SL, VV> Sh;
+    typedef typename Sh::P P;
     const P pc(lane);
-    const size_t at = row0 + pc.lt;
-    const T* pd = (const T*)a.delta + at * a.lddelta + ch0 + pc.lc; const T* pu = (const T*)a.u + at * a.ldu + ch0 + pc.lc;
-    const T* pz = (const T*)a.z + at * a.ldz + ch0 + pc.lc; const T* pg = (const T*)a.dy + at * a.lddy + ch0 + pc.lc;
     Piece<T, VV> nd[P::I], nu[P::I], nz[P::I], ng[P::I];
-    States<T, VV, K, S::NP> ns;
+    typename Sh::ST ns;
+    if constexpr (VV > 1) {
+        copies_done();
 #pragma unroll
-    for (int i = 0; i < P::I; i++) {
-        const bool there = pc.t(i) < rows && pc.c(i) < (int)have;
-        nd[i] = fetch<T, VV>(pd, P::step(i, a.lddelta), there);
-        if (!ENDS) nu[i] = fetch<T, VV>(pu, P::step(i, a.ldu), there);
-        if (a.z) nz[i] = fetch<T, VV>(pz, P::step(i, a.ldz), there);
-        ng[i] = fetch<T, VV>(pg, P::step(i, a.lddy), there);
+        for (int i = 0; i < P::I; i++) {
+            nd[i].w = sh.way[i][lane];
+            ng[i].w = sh.way[P::I + i][lane];
+            if (a.z) nz[i].w = sh.way[2 * P::I + i][lane];
+            if (!ENDS) nu[i].w = sh.way[3 * P::I + i][lane];
+        }
+#pragma unroll
+        for (int i = 0; i < Sh::ST::I; i++) ns.take(i, sh.way[4 * P::I + i][lane]);
+    } else {
+        const size_t at = row0 + pc.lt;
+        const T* pd = (const T*)a.delta + at * a.lddelta + ch0 + pc.lc; const T* pu = (const T*)a.u + at * a.ldu + ch0 + pc.lc;
+        const T* pz = (const T*)a.z + at * a.ldz + ch0 + pc.lc; const T* pg = (const T*)a.dy + at * a.lddy + ch0 + pc.lc;
+#pragma unroll
+        for (int i = 0; i < P::I; i++) {
+            const bool there = pc.t(i) < rows && pc.c(i) < (int)have;
+            nd[i] = fetch<T, VV>(pd, P::step(i, a.lddelta), there);
+            if (!ENDS) nu[i] = fetch<T, VV>(pu, P::step(i, a.ldu), there);
+            if (a.z) nz[i] = fetch<T, VV>(pz, P::step(i, a.ldz), there);
+            ng[i] = fetch<T, VV>(pg, P::step(i, a.lddy), there);
+        }
+        ns.fetch_all(a, row0, g * a.N, rows, lane);
     }
-    ns.fetch_all(a, row0, g * a.N, rows, lane);
 #pragma unroll
     for (int i = 0; i < P::I; i++) {
         const int t = pc.t(i), c = pc.c(i);
@@ -97,23 +158,7 @@ __device__ __forceinline__ void stage(const Scan& a, Backward<SL>& sh, size_t ro
     ns.stage(&sh.bc[0][0][0], lane);
 }
 
-// asks for the rows of the next tile and the state before it, so that they are in L2 by then
-__device__ __forceinline__ void to_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-template <typename T, int SL, int VV>
-__device__ __forceinline__ void ahead(const Scan& a, size_t row0, size_t start, uint32_t ch0, uint32_t have, int lane) {
-    const Pieces<K, Shape<SL>::CH, VV> pc(lane);
-    if (VV > 1 && pc.lc < (int)have && pc.lt < K) {        // (the first piece of a row's line will do; narrow pieces would ask a line many times)
-        const size_t at = row0 + pc.lt;
-        to_l2((const T*)a.delta + at * a.lddelta + ch0 + pc.lc);
-        to_l2((const T*)a.u + at * a.ldu + ch0 + pc.lc);
-        to_l2((const T*)a.dy + at * a.lddy + ch0 + pc.lc);
-        if (a.z) to_l2((const T*)a.z + at * a.ldz + ch0 + pc.lc);
-    }
-    const uint32_t floats = have * a.N;                    // (the warp's channels lie side by side)
-    for (uint32_t i = lane * 32; i < floats; i += 32 * 32) to_l2(a.starts + start * a.D * a.N + (size_t)ch0 * a.N + i);
-}
-
-template <int SL> __device__ __forceinline__ void channel_params(const Scan& a, Backward<SL>& sh, uint32_t ch0, uint32_t have, int lane) {
+template <typename T, int SL, int VV> __device__ __forceinline__ void channel_params(const Scan& a, Backward<T, SL, VV>& sh, uint32_t ch0, uint32_t have, int lane) {
     for (int c = lane; c < Shape<SL>::CH; c += 32) {
         sh.bias[c] = c < (int)have && a.dbias ? __ldg(a.dbias + ch0 + c) : 0.0f;
         sh.skip[c] = c < (int)have && a.Dk ? __ldg(a.Dk + ch0 + c) : 0.0f;
@@ -162,7 +207,7 @@ __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
     sf_chain_enter();
     constexpr int CH = Shape<SL>::CH;
     extern __shared__ __align__(16) unsigned char shared[];
-    Backward<SL>& sh = reinterpret_cast<Backward<SL>*>(shared)[threadIdx.x / 32];
+    Backward<T, SL, VV>& sh = reinterpret_cast<Backward<T, SL, VV>*>(shared)[threadIdx.x / 32];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
     const Item it = item_of(a, CH);
     if (it.have == 0) return;
@@ -176,11 +221,15 @@ __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
     for (int j = 0; j < 2; j++)
 #pragma unroll
         for (int n = 0; n < 4; n++) G[j][n] = 0;
-    channel_params<SL>(a, sh, ch0, have, lane);
+    channel_params<T, SL, VV>(a, sh, ch0, have, lane);
     __syncwarp();
-    for (uint32_t tile = (t_end - t_begin + K - 1) / K; tile-- > 0;) {
+    const uint32_t tiles = (t_end - t_begin + K - 1) / K;
+    auto next = [&](uint32_t tile) { const uint32_t t = t_begin + tile * K; ask<T, SL, VV, true>(a, sh, (size_t)r.first + t, 0, ch0, have, g, (int)min((uint32_t)K, t_end - t), lane); };
+    next(tiles - 1);
+    for (uint32_t tile = tiles; tile-- > 0;) {
         const uint32_t t0 = t_begin + tile * K;
         stage<T, SL, VV, true>(a, sh, (size_t)r.first + t0, ch0, have, g, (int)min((uint32_t)K, t_end - t0), lane);
+        if (tile) next(tile - 1);
         __syncwarp();
 #pragma unroll
         for (int t = K - 1; t >= 0; t--) {
@@ -209,53 +258,6 @@ __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
     }
 }
 
-// The sums over the SL state lanes of the lane's four channels: a lane gets those of NC of them (all, two, one), from channel first(sl) on.
-template <int SL> struct ByState {
-    static constexpr int NC = SL == 1 ? 4 : (SL == 2 ? 2 : 1);
-    __device__ __forceinline__ static int first(int sl) { return SL == 1 ? 0 : (SL == 2 ? 2 * sl : 2 * (sl & 1) + (sl >> 1 & 1)); }
-    __device__ __forceinline__ static void sum(const f2 (&v)[2], int sl, float (&o)[NC]) {
-        if constexpr (SL == 1) { unpack2(v[0], o[0], o[1]); unpack2(v[1], o[2], o[3]); }
-        else {
-            const bool hi = sl & 1;
-            const f2 w = add2(hi ? v[1] : v[0], __shfl_xor_sync(0xFFFFFFFFu, hi ? v[0] : v[1], 1));
-            float x, y;
-            unpack2(w, x, y);
-            if constexpr (SL == 2) { o[0] = x; o[1] = y; }
-            else {
-                const bool up = sl & 2;
-                o[0] = (up ? y : x) + __shfl_xor_sync(0xFFFFFFFFu, up ? x : y, 2);
-#pragma unroll
-                for (int m = 4; m < SL; m <<= 1) o[0] += __shfl_xor_sync(0xFFFFFFFFu, o[0], m);
-            }
-        }
-    }
-};
-// Sums of 8 values over the CL channel lanes; they end up in lane cl as the 8 / CL (at least one) values from index (cl * 8 / CL) % 8 on; put writes
-// them to p[value / 4][state]
-template <int SL> __device__ __forceinline__ void put_states(float* p0, float* p1, float (&v)[8], int lane, int cl, int sl) {
-    int n = 8;
-#pragma unroll
-    for (int m = 16; m >= SL; m >>= 1) {
-        if (n > 1) {
-            n >>= 1;
-            const bool hi = lane & m;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                if (i >= n) break;
-                const float keep = hi ? v[i + n] : v[i], give = hi ? v[i] : v[i + n];
-                v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, m);
-            }
-        } else v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], m);
-    }
-    constexpr int CL = 32 / SL, NV = CL >= 8 ? 1 : 8 / CL, SAME = CL > 8 ? CL / 8 : 1;       // values a lane has, lanes that have the same
-    if (cl % SAME) return;
-#pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const int k = cl / SAME * NV + i;
-        (k < 4 ? p0 : p1)[sl * 4 + k % 4] = v[i];
-    }
-}
-
 // One block: up to kWarps warps over neighbouring channels of a group, one part of one sequence after the other (a run), rows from last to first.
 // A tile's states are stepped from the state kept before it: rows 0 to 3 to reach row 4, rows 4 to 7 with decays and states held in registers, back over
 // them, then rows 0 to 3 the same way.
@@ -263,12 +265,14 @@ template <typename T, int SL, int VV>
 __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
     sf_chain_enter();
     typedef Shape<SL> S;
-    typedef Pieces<K, S::CH, VV> P;
-    constexpr int CH = S::CH, I = P::I;
+    typedef Backward<T, SL, VV> Sh;
+    constexpr int CH = S::CH, CL = S::CL, VE = VV > 1 ? 4 : 1;
+    typedef Pieces<R, CH, VE> P;                           // as rows are written: R at a time, 4 channels a piece
+    constexpr int I = P::I;
     extern __shared__ __align__(16) unsigned char shared[];
-    Backward<SL>* all = reinterpret_cast<Backward<SL>*>(shared);
+    Sh* all = reinterpret_cast<Sh*>(shared);
     const int warp = threadIdx.x / 32, warps = blockDim.x / 32;
-    Backward<SL>& sh = all[warp];
+    Sh& sh = all[warp];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
     const uint32_t gb = blockIdx.x, g = gb / a.cblocks, cb = gb % a.cblocks;
     const uint32_t c0 = min(a.per, (cb * (uint32_t)kWarps + warp) * CH);
@@ -276,7 +280,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
     const P pc(lane);
     f2 A[2][4], dA[2][4], G[2][4];
     load_states(A, a.A, a, ch0, have, cl, sl, kLog2e);
-    float dD[I][VV], db[I][VV];                            // of the channels that this lane's pieces have
+    float dD[I][VE], db[I][VE];                            // of the channels that this lane's pieces have
 #pragma unroll
     for (int j = 0; j < 2; j++)
 #pragma unroll
@@ -284,9 +288,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
 #pragma unroll
     for (int i = 0; i < I; i++)
 #pragma unroll
-        for (int e = 0; e < VV; e++) dD[i][e] = db[i][e] = 0.0f;
-    channel_params<SL>(a, sh, ch0, have, lane);
+        for (int e = 0; e < VE; e++) dD[i][e] = db[i][e] = 0.0f;
+    channel_params<T, SL, VV>(a, sh, ch0, have, lane);
     __syncwarp();
+    const size_t DN = (size_t)a.D * a.N;
     const uint64_t items = (uint64_t)a.q.n_seq * a.parts;
     for (uint64_t it = blockIdx.y; it < items; it += a.runs) {
         const uint32_t part = (uint32_t)(it / a.q.n_seq), s = (uint32_t)(it % a.q.n_seq);
@@ -294,18 +299,26 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
         const uint32_t t_begin = part * a.part_len, t_end = min(r.len, t_begin + a.part_len);
         const bool whole = a.part_state == nullptr;        // the sequence in one part: gradients of states here
         if (t_begin >= r.len && !(whole && a.d_state0 && r.slot >= 0)) continue;
-        const size_t DN = (size_t)a.D * a.N;
-        load_states(G, whole ? (a.d_state && r.slot >= 0 ? a.d_state + (size_t)r.slot * DN : nullptr) : a.part_state + ((size_t)s * a.parts + part) * DN, a, ch0, have, cl, sl, 1.0f);
         const uint32_t tiles = t_end > t_begin ? (t_end - t_begin + K - 1) / K : 0;
+        auto next = [&](uint32_t tile) {
+            const uint32_t t = t_begin + tile * K;
+            ask<T, SL, VV, false>(a, sh, (size_t)r.first + t, start_index(r.first, s, t), ch0, have, g, (int)min((uint32_t)K, t_end - t), lane);
+        };
+        if (tiles) next(tiles - 1);
+        load_states(G, whole ? (a.d_state && r.slot >= 0 ? a.d_state + (size_t)r.slot * DN : nullptr) : a.part_state + ((size_t)s * a.parts + part) * DN, a, ch0, have, cl, sl, 1.0f);
         for (uint32_t tile = tiles; tile-- > 0;) {
             const uint32_t t0 = t_begin + tile * K;
             const int rows = (int)min((uint32_t)K, t_end - t0);
             const size_t row0 = (size_t)r.first + t0;
-            f2 h[2][4];
-            load_states(h, a.starts + start_index(r.first, s, t0) * DN, a, ch0, have, cl, sl, 1.0f);
             stage<T, SL, VV, false>(a, sh, row0, ch0, have, g, rows, lane);
-            if (tile) ahead<T, SL, VV>(a, row0 - K, start_index(r.first, s, t0 - K), ch0, have, lane);
-            __syncwarp();
+            f2 h[2][4];
+            if constexpr (VV > 1) {
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    const float4 x = *reinterpret_cast<const float4*>(&sh.way[Sh::ON_WAY - 4 + 2 * j][lane]), y = *reinterpret_cast<const float4*>(&sh.way[Sh::ON_WAY - 3 + 2 * j][lane]);
+                    h[j][0] = pack2(x.x, y.x); h[j][1] = pack2(x.y, y.y); h[j][2] = pack2(x.z, y.z); h[j][3] = pack2(x.w, y.w);
+                }
+            } else load_states(h, a.starts + start_index(r.first, s, t0) * DN, a, ch0, have, cl, sl, 1.0f);
             auto keep = [&](int q) {
 #pragma unroll
                 for (int j = 0; j < 2; j++)
@@ -318,9 +331,11 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
 #pragma unroll
                     for (int n = 0; n < 4; n += 2) { const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&sh.start[q][2 * j + n / 2][lane]); v[j][n] = w.x; v[j][n + 1] = w.y; }
             };
+            keep(0);
+            if (tile) next(tile - 1);                      // (what this lane had on its way it has read)
+            __syncwarp();
 #pragma unroll
-            for (int t = 0; t < K - R; t++) {
-                if (t % R == 0) keep(t / R);
+            for (int t = 0; t < R; t++) {
                 const ulonglong2 d2 = *reinterpret_cast<const ulonglong2*>(&sh.step[t][cl * 4]), u2 = *reinterpret_cast<const ulonglong2*>(&sh.u[t][cl * 4]);
                 const float4 b4 = *reinterpret_cast<const float4*>(&sh.bc[0][t][sl * 4]);
                 const f2 d[2] = {d2.x, d2.y}, in[2] = {mul2(d2.x, u2.x), mul2(d2.y, u2.y)}, b[4] = {dup2(b4.x), dup2(b4.y), dup2(b4.z), dup2(b4.w)};
@@ -329,10 +344,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
 #pragma unroll
                     for (int n = 0; n < 4; n++) h[j][n] = fma2(decay2(d[j], A[j][n]), h[j][n], mul2(in[j], b[n]));
             }
-            keep(K / R - 1);
+            keep(1);
 #pragma unroll 1
             for (int q = K / R - 1; q >= 0; q--) {
-                f2 al[R][2][4], hs[R + 1][2][4];               // decays; states before the rows and after them
+                f2 al[R][2][4], hs[R + 1][2][4];           // decays; states before the rows and after them
                 take(hs[0], q);
 #pragma unroll
                 for (int t = 0; t < R; t++) {
@@ -367,11 +382,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
                             dA[j][n] = fma2(x, d[j], dA[j][n]);
                             y[j] = n ? fma2(hs[t + 1][j][n], c[n], y[j]) : mul2(hs[t + 1][j][n], c[n]);
                         }
-                    typedef ByState<SL> Q;
-                    float o1[Q::NC], o2[Q::NC], oy[Q::NC];
-                    Q::sum(s1, sl, o1);
-                    Q::sum(s2, sl, o2);
-                    if (a.z) Q::sum(y, sl, oy);
+                    const int at = sl * Sh::PY + cl * 4;
+                    *reinterpret_cast<ulonglong2*>(&sh.s1[t][at]) = make_ulonglong2(s1[0], s1[1]);
+                    *reinterpret_cast<ulonglong2*>(&sh.s2[t][at]) = make_ulonglong2(s2[0], s2[1]);
+                    if (a.z) *reinterpret_cast<ulonglong2*>(&sh.y[t][at]) = make_ulonglong2(y[0], y[1]);
                     float v[8];
 #pragma unroll
                     for (int n = 0; n < 4; n++) {
@@ -379,52 +393,78 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
                         unpack2(dB[n], x, w); v[n] = x + w;
                         unpack2(dC[n], x, w); v[4 + n] = x + w;
                     }
-                    put_states<SL>(sh.sum[tt][0], sh.sum[tt][1], v, lane, cl, sl);
-                    __syncwarp();                          // (every lane has read the row)
-                    if (SL <= 4 || sl < 4) {
+                    *reinterpret_cast<float4*>(&sh.dbc[t][0][cl][sl * 4]) = make_float4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<float4*>(&sh.dbc[t][1][cl][sl * 4]) = make_float4(v[4], v[5], v[6], v[7]);
+                }
+                __syncthreads();
+                const int left = rows - R * q;             // rows of the group that are there
+                const size_t at = row0 + R * q + pc.lt;
 #pragma unroll
-                        for (int i = 0; i < Q::NC; i++) {
-                            const int k = cl * 4 + Q::first(sl) + i;
-                            const float uu = sh.u[tt][k];
-                            sh.step[tt][k] *= o1[i];
-                            sh.dstep[tt][k] *= fmaf(uu, o1[i], kLn2 * o2[i]);
-                            if (a.z) sh.dgate[tt][k] *= fmaf(sh.skip[k], uu, oy[i]);
+                for (int i = 0; i < I; i++) {
+                    const int t = pc.t(i), tt = R * q + t, c = pc.c(i);
+                    if (t >= R || t >= left || c >= (int)have) continue;
+                    float du[VE], dd[VE], dz[VE];
+                    float s1[VE], s2[VE], y[VE];
+                    auto join = [&](const float* p, float (&o)[VE]) {
+                        if constexpr (VE == 1) {
+                            o[0] = p[c];
+#pragma unroll
+                            for (int l = 1; l < SL; l++) o[0] += p[l * Sh::PY + c];
+                        } else {
+                            ulonglong2 x = *reinterpret_cast<const ulonglong2*>(p + c);
+#pragma unroll
+                            for (int l = 1; l < SL; l++) { const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(p + l * Sh::PY + c); x.x = add2(x.x, w.x); x.y = add2(x.y, w.y); }
+                            unpack2(x.x, o[0], o[1]); unpack2(x.y, o[2], o[3]);
                         }
+                    };
+                    auto get = [&](const float* p, float (&o)[VE]) {
+                        if constexpr (VE == 1) o[0] = p[c];
+                        else { const float4 w = *reinterpret_cast<const float4*>(p + c); o[0] = w.x; o[1] = w.y; o[2] = w.z; o[3] = w.w; }
+                    };
+                    join(sh.s1[t], s1);
+                    join(sh.s2[t], s2);
+                    float st[VE], u[VE], o[VE], ds[VE], skip[VE];
+                    get(sh.step[tt], st); get(sh.u[tt], u); get(sh.e[tt], o); get(sh.dstep[tt], ds); get(sh.skip, skip);
+#pragma unroll
+                    for (int e = 0; e < VE; e++) {
+                        du[e] = fmaf(skip[e], o[e], st[e] * s1[e]);
+                        dd[e] = fmaf(u[e], s1[e], kLn2 * s2[e]) * ds[e];
+                        dD[i][e] = fmaf(o[e], u[e], dD[i][e]);
+                        db[i][e] += dd[e];
+                    }
+                    if (a.du) store_word<T, VE>((T*)a.du + at * a.lddu + ch0 + pc.lc + P::step(i, a.lddu), du);
+                    if (a.ddelta) store_word<T, VE>((T*)a.ddelta + at * a.ldddelta + ch0 + pc.lc + P::step(i, a.ldddelta), dd);
+                    if (a.dz) {
+                        float dg[VE];
+                        join(sh.y[t], y);
+                        get(sh.dgate[tt], dg);
+#pragma unroll
+                        for (int e = 0; e < VE; e++) dz[e] = fmaf(skip[e], u[e], y[e]) * dg[e];
+                        store_word<T, VE>((T*)a.dz + at * a.lddz + ch0 + pc.lc + P::step(i, a.lddz), dz);
                     }
                 }
-            }
-            __syncwarp();
-            const size_t at = row0 + pc.lt;
+                // dB and dC over the block's channels: four threads for four states of a row, each every fourth of the lanes' parts, in their order
+                for (int o = threadIdx.x / 4; o < min(left, R) * 2 * SL; o += blockDim.x / 4) {
+                    const int t = o / (2 * SL), k = o / SL % 2, n = o % SL * 4, sub = threadIdx.x & 3;
+                    f2 x = 0, y = 0;
+                    for (int i = sub; i < warps * CL; i += 4) {
+                        const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&all[i / CL].dbc[t][k][i % CL][n]);
+                        x = add2(x, w.x); y = add2(y, w.y);
+                    }
+                    const uint32_t who = 0xFu << (lane & 28);
 #pragma unroll
-            for (int i = 0; i < I; i++) {
-                const int t = pc.t(i), c = pc.c(i);
-                if (t >= rows || c >= (int)have) continue;
-                float du[VV], dd[VV], dz[VV];
-#pragma unroll
-                for (int e = 0; e < VV; e++) {
-                    const float u = sh.u[t][c + e], o = sh.e[t][c + e];
-                    du[e] = fmaf(sh.skip[c + e], o, sh.step[t][c + e]);
-                    dd[e] = sh.dstep[t][c + e];
-                    dz[e] = sh.dgate[t][c + e];
-                    dD[i][e] = fmaf(o, u, dD[i][e]);
-                    db[i][e] += dd[e];
+                    for (int m = 1; m < 4; m <<= 1) { x = add2(x, __shfl_xor_sync(who, x, m)); y = add2(y, __shfl_xor_sync(who, y, m)); }
+                    float v[4];
+                    unpack2(x, v[0], v[1]); unpack2(y, v[2], v[3]);
+                    const float mine = sub == 0 ? v[0] : (sub == 1 ? v[1] : (sub == 2 ? v[2] : v[3]));
+                    if (n + sub >= (int)a.N) continue;
+                    const size_t row = row0 + R * q + t;
+                    if (a.sum_bc) a.sum_bc[((((size_t)cb * a.q.rows + row) * a.G + g) * 2 + k) * a.N + n + sub] = mine;
+                    else if (k == 0) { if (a.dB) ((T*)a.dB)[row * a.lddb + g * a.N + n + sub] = from_f32<T>(mine); }
+                    else if (a.dC) ((T*)a.dC)[row * a.lddc + g * a.N + n + sub] = from_f32<T>(mine);
                 }
-                if (a.du) store_word<T, VV>((T*)a.du + at * a.lddu + ch0 + pc.lc + P::step(i, a.lddu), du);
-                if (a.ddelta) store_word<T, VV>((T*)a.ddelta + at * a.ldddelta + ch0 + pc.lc + P::step(i, a.ldddelta), dd);
-                if (a.dz) store_word<T, VV>((T*)a.dz + at * a.lddz + ch0 + pc.lc + P::step(i, a.lddz), dz);
+                __syncthreads();
             }
-            // dB and dC: the block's warps, in their order
-            __syncthreads();
-            for (int i = threadIdx.x; i < rows * 2 * S::NP; i += blockDim.x) {
-                const int t = i / (2 * S::NP), k = i / S::NP % 2, n = i % S::NP;
-                if (n >= (int)a.N) continue;
-                float v = all[0].sum[t][k][n];
-                for (int w = 1; w < warps; w++) v += all[w].sum[t][k][n];
-                if (a.sum_bc) a.sum_bc[((((size_t)cb * a.q.rows + row0 + t) * a.G + g) * 2 + k) * a.N + n] = v;
-                else if (k == 0) { if (a.dB) ((T*)a.dB)[(row0 + t) * a.lddb + g * a.N + n] = from_f32<T>(v); }
-                else if (a.dC) ((T*)a.dC)[(row0 + t) * a.lddc + g * a.N + n] = from_f32<T>(v);
-            }
-            __syncthreads();
         }
         if (whole && a.d_state0 && r.slot >= 0) store_states(G, a.d_state0 + (size_t)r.slot * DN, a.N, a, ch0, have, cl, sl);
     }
@@ -434,15 +474,15 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
 #pragma unroll
     for (int i = 0; i < I; i++) {
         const int t = pc.t(i), c = pc.c(i);
-        if (t >= K) continue;
+        if (t >= R) continue;
 #pragma unroll
-        for (int e = 0; e < VV; e++) { sh.u[t][c + e] = dD[i][e]; sh.e[t][c + e] = db[i][e]; }
+        for (int e = 0; e < VE; e++) { sh.u[t][c + e] = dD[i][e]; sh.e[t][c + e] = db[i][e]; }
     }
     __syncwarp();
     for (int c = lane; c < (int)have; c += 32) {
         float x = 0.0f, y = 0.0f;
 #pragma unroll
-        for (int t = 0; t < K; t++) { x += sh.u[t][c]; y += sh.e[t][c]; }
+        for (int t = 0; t < R; t++) { x += sh.u[t][c]; y += sh.e[t][c]; }
         par[(size_t)(ch0 + c) * (a.N + 2) + a.N] = x;
         par[(size_t)(ch0 + c) * (a.N + 2) + a.N + 1] = y;
     }
@@ -509,19 +549,19 @@ extern "C" int sf_seq_scan_backward(sf_ctx* ctx, const sf_sequences* seq, const 
     if (p.cblocks > 1) a.sum_bc = (float*)(ws + sf_align256((size_t)p.runs * in->D * (in->N + 2) * 4));
     const uint64_t blocks = ((uint64_t)seq->n_seq * in->G * p.cwarps + kWarps - 1) / kWarps;
     if (blocks > 0x7FFFFFFFu) return SF_ERR_ARG;
-    const bool vec = fits(in) && fits(dy, lddy, in->dtype) && fits(out->du, out->lddu, in->dtype) && fits(out->d_delta, out->ldd_delta, in->dtype) && fits(out->dz, out->lddz, in->dtype);
+    const bool vec = fits(in) && aligned(starts, 16) && fits(dy, lddy, in->dtype) && fits(out->du, out->lddu, in->dtype) && fits(out->d_delta, out->ldd_delta, in->dtype) && fits(out->dz, out->lddz, in->dtype);
     return by_type(in->dtype, [&](auto zero) {
         typedef decltype(zero) T;
         return by_states(p.sl, [&](auto lanes) {
             constexpr int SL = decltype(lanes)::value, VV = 16 / (int)sizeof(T);
             int e = SF_OK;
             if (p.split) {
-                e = launch(vec ? back_ends_kernel<T, SL, VV> : back_ends_kernel<T, SL, 1>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, sizeof(Backward<SL>) * kWarps, st, a);
+                e = launch(vec ? back_ends_kernel<T, SL, VV> : back_ends_kernel<T, SL, 1>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, vec ? sizeof(Backward<T, SL, VV>) * kWarps : sizeof(Backward<T, SL, 1>) * kWarps, st, a);
                 if (e == SF_OK) e = launch(parts_kernel<true>, dim3((uint32_t)(((uint64_t)in->D * in->N + 255) / 256), seq->n_seq), 256, 0, st, a);
                 if (e != SF_OK) return e;
             }
             const uint32_t w = std::min((uint32_t)kWarps, p.cwarps);
-            e = launch(vec ? back_kernel<T, SL, VV> : back_kernel<T, SL, 1>, dim3(in->G * p.cblocks, p.runs), 32 * w, sizeof(Backward<SL>) * w, st, a);
+            e = launch(vec ? back_kernel<T, SL, VV> : back_kernel<T, SL, 1>, dim3(in->G * p.cblocks, p.runs), 32 * w, vec ? sizeof(Backward<T, SL, VV>) * w : sizeof(Backward<T, SL, 1>) * w, st, a);
             if (e == SF_OK && a.sum_bc && (a.dB || a.dC)) {
                 for (uint32_t s = 0; s < seq->n_seq && e == SF_OK; s += 65535) {
                     Scan b = a;
