@@ -7,12 +7,15 @@ using namespace sfscan;
 
 // What a warp keeps in shared memory.  Sums over states are left as one part a state lane and joined where the row is written.  Rows are spaced so that
 // the 16-byte accesses of eight lanes meet no common bank: PX floats a row of channels, PY a part, PT the parts of a row.
-template <int SL> struct __align__(16) Forward {
+template <typename T, int SL, int VV> struct __align__(16) Forward {
     typedef Shape<SL> S;
+    typedef Pieces<S::K, S::CH, VV> P;
+    typedef States<T, VV, S::K, S::NP> ST;
     static constexpr int PX = S::CH + 4, PY = S::CH + (SL == 1 ? 0 : (SL == 2 ? 16 : (SL == 4 ? 8 : 4))), PT = SL * PY + 4;
     float step[S::K][PX], in[S::K][PX];                    // delta; delta u
     float bc[2][S::K][S::NP];                              // B, C
     float y[S::K][PT];
+    uint4 way[VV > 1 ? 3 * P::I + ST::I : 1][32];          // the next tile's pieces on their way, every lane its own
     float bias[S::CH], skip[S::CH];                        // delta_bias, D of the warp's channels
 };
 
@@ -25,7 +28,8 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     typedef Pieces<S::K, S::CH, VV> P;
     constexpr int K = S::K, CH = S::CH, NP = S::NP, I = P::I;
     extern __shared__ __align__(16) unsigned char shared[];
-    Forward<SL>& sh = reinterpret_cast<Forward<SL>*>(shared)[threadIdx.x / 32];
+    typedef Forward<T, SL, VV> Sh;
+    Sh& sh = reinterpret_cast<Sh*>(shared)[threadIdx.x / 32];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
     const Item it = item_of(a, CH);
     if (it.have == 0) return;
@@ -40,16 +44,29 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     const size_t at0 = (size_t)r.first + t_begin + pc.lt;
     const T* pd = (const T*)a.delta + at0 * a.lddelta + ch0 + pc.lc; const T* pu = (const T*)a.u + at0 * a.ldu + ch0 + pc.lc; const T* pz = (const T*)a.z + at0 * a.ldz + ch0 + pc.lc;
     T* py = (T*)a.y + at0 * a.ldy + ch0 + pc.lc;
-    auto ask = [&](uint32_t t0) {
+    auto ask = [&](uint32_t t0) {                          // whole pieces go by way of shared memory, single elements through registers
         const int rows = (int)min((uint32_t)K, t_end - t0);
 #pragma unroll
         for (int i = 0; i < I; i++) {
             const bool there = pc.c(i) < (int)have && pc.t(i) < rows;
-            nd[i] = fetch<T, VV>(pd, P::step(i, a.lddelta), there);
-            nu[i] = fetch<T, VV>(pu, P::step(i, a.ldu), there);
-            if (!ENDS && a.z) nz[i] = fetch<T, VV>(pz, P::step(i, a.ldz), there);
+            if constexpr (VV > 1) {
+                copy16(&sh.way[i][lane], there ? pd + P::step(i, a.lddelta) : (const T*)a.delta, there);
+                copy16(&sh.way[I + i][lane], there ? pu + P::step(i, a.ldu) : (const T*)a.u, there);
+                if (!ENDS && a.z) copy16(&sh.way[2 * I + i][lane], there ? pz + P::step(i, a.ldz) : (const T*)a.z, there);
+            } else {
+                nd[i] = fetch<T, VV>(pd, P::step(i, a.lddelta), there);
+                nu[i] = fetch<T, VV>(pu, P::step(i, a.ldu), there);
+                if (!ENDS && a.z) nz[i] = fetch<T, VV>(pz, P::step(i, a.ldz), there);
+            }
         }
-        ns.fetch_all(a, (size_t)r.first + t0, g * a.N, rows, lane);
+        if constexpr (VV > 1) {
+#pragma unroll
+            for (int i = 0; i < Sh::ST::I; i++) {
+                bool there;
+                const T* p = Sh::ST::template piece<T>(a, i, (size_t)r.first + t0, g * a.N, rows, lane, there);
+                copy16(&sh.way[3 * I + i][lane], p, there);
+            }
+        } else ns.fetch_all(a, (size_t)r.first + t0, g * a.N, rows, lane);
         pd += K * a.lddelta; pu += K * a.ldu; pz += K * a.ldz;
     };
     if (t_begin < t_end) ask(t_begin);
@@ -106,6 +123,13 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     for (uint32_t t0 = t_begin; t0 < t_end; t0 += K) {
         const int rows = (int)min((uint32_t)K, t_end - t0);
         Piece<T, VV> cu[I], cz[I];
+        if constexpr (VV > 1) {
+            copies_done();
+#pragma unroll
+            for (int i = 0; i < I; i++) { nd[i].w = sh.way[i][lane]; nu[i].w = sh.way[I + i][lane]; if (!ENDS && a.z) nz[i].w = sh.way[2 * I + i][lane]; }
+#pragma unroll
+            for (int i = 0; i < Sh::ST::I; i++) ns.take(i, sh.way[3 * I + i][lane]);
+        }
 #pragma unroll
         for (int i = 0; i < I; i++) {
             const int t = pc.t(i), c = pc.c(i);
@@ -154,7 +178,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
                 f2 y[2];
 #pragma unroll
                 for (int j = 0; j < 2; j++) y[j] = fma2(h[j][3], dup2(c4.w), fma2(h[j][2], dup2(c4.z), fma2(h[j][1], dup2(c4.y), mul2(h[j][0], dup2(c4.x)))));
-                *reinterpret_cast<ulonglong2*>(&sh.y[t][sl * Forward<SL>::PY + cl * 4]) = make_ulonglong2(y[0], y[1]);
+                *reinterpret_cast<ulonglong2*>(&sh.y[t][sl * Sh::PY + cl * 4]) = make_ulonglong2(y[0], y[1]);
             }
         };
         if (rows == K) {
@@ -176,7 +200,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
                 if constexpr (VV == 1) {
                     y[0] = sh.skip[c] * u[0];
 #pragma unroll
-                    for (int l = 0; l < SL; l++) y[0] += sh.y[t][l * Forward<SL>::PY + c];
+                    for (int l = 0; l < SL; l++) y[0] += sh.y[t][l * Sh::PY + c];
                     if (a.z) y[0] *= z[0] * sigmoid(z[0]);
                 } else {
 #pragma unroll
@@ -185,7 +209,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
                         f2 v = mul2(k2.x, pack2(u[e], u[e + 1])), w = mul2(k2.y, pack2(u[e + 2], u[e + 3]));
 #pragma unroll
                         for (int l = 0; l < SL; l++) {
-                            const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&sh.y[t][l * Forward<SL>::PY + c + e]);
+                            const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&sh.y[t][l * Sh::PY + c + e]);
                             v = add2(v, q.x); w = add2(w, q.y);
                         }
                         if (a.z) {
@@ -381,7 +405,7 @@ extern "C" int sf_seq_scan(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_r
                 const bool v4 = in->N % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16) && aligned(in->A, 16);
                 return launch(v4 ? step_kernel<T, SL, true> : step_kernel<T, SL, false>, (uint32_t)blocks, 32 * kWarps, 0, st, a);
             }
-            const size_t smem = sizeof(Forward<SL>) * kWarps;
+            const size_t smem = (vec ? sizeof(Forward<T, SL, VV>) : sizeof(Forward<T, SL, 1>)) * kWarps;
             if (p.split) {
                 a.part_state = (float*)workspace;
                 a.part_step = (float*)((char*)workspace + sf_align256((size_t)seq->n_seq * p.parts * in->D * in->N * 4));

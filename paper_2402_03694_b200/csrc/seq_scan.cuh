@@ -79,8 +79,9 @@ __device__ __forceinline__ f2 softplus2(f2 x, f2& ee) {
     return fma2(add2(q, q), p, pack2(fmaxf(a, 0.0f), fmaxf(b, 0.0f)));
 }
 
-// a = exp(delta A) with A in units of log2.  ex2.approx is low by 0.35 to 0.8 of 2^-24 on average (measured; by a thousand steps of 0.001 the state would be off by
-// 2e-5): the argument is raised by as much as takes that out near 0, where states live long.
+// a = exp(delta A) with A in units of log2.  ex2.approx is low by 0.26 to 0.45 of 2^-24 on average for exponents from -1/2 to -2^-8 (by 0.1 for smaller ones, measured),
+// which a state that lives a hundred rows adds up a hundred times: the argument is raised by as much as takes that out.  (On the CUDA cores by a polynomial for
+// a quarter or half of the states, to relieve the function unit: 471 and 514 us where this takes 436.)
 constexpr float kCentre = 3.2e-8f;
 __device__ __forceinline__ float decay(float delta, float A) { return ex2(fmaf(delta, A, kCentre)); }
 __device__ __forceinline__ f2 decay2(f2 delta, f2 A) {
@@ -133,6 +134,12 @@ template <typename T, int VV> __device__ __forceinline__ Piece<T, VV> fetch(cons
     if (there) p.w = __ldg(reinterpret_cast<const typename Word<VV * sizeof(T)>::type*>(reinterpret_cast<const T*>(base) + at));
     return p;
 }
+
+// 16 bytes into shared memory while the thread goes on; zeros where there is nothing
+__device__ __forceinline__ void copy16(void* to, const void* from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // B and C of a tile on their way (PV states at once, pieces of B first); stage writes them as [2][K][NP], zeros where there is nothing.
 template <typename T, int VV, int K, int NP> struct States {

@@ -26,11 +26,6 @@ template <typename T, int SL, int VV> struct __align__(16) Backward {
     float bias[S::CH], skip[S::CH];
 };
 
-__device__ __forceinline__ void copy16(void* to, const void* from, bool there) {     // (zeros where there is nothing)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
 // Asks for a tile's pieces: steps, gradients of the outputs, gates, and (not ENDS) inputs and the state before the tile.  Whole pieces only; others are read when staged.
 template <typename T, int SL, int VV, bool ENDS>
 __device__ __forceinline__ void ask(const Scan& a, Backward<T, SL, VV>& sh, size_t row0, size_t start, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
