@@ -125,7 +125,7 @@ template <typename T> __device__ __forceinline__ void load_chunk(const T* __rest
     c.open(v);
 }
 
-// ---- rows of up to 1024 entries: L lanes a row, C chunks a lane, the row in registers -----------------------------------------
+// ---- rows of up to 2048 entries: L lanes a row, C chunks a lane, the row in registers -----------------------------------------
 // Alternatives: one after the other, the largest entry that is left (of equals the lowest index); where a warp has the row and more than four are
 // asked, by a bound: the k-th largest of the lanes' own maxima is reached by k entries at least, and the entries that reach it are collected and ranked.
 constexpr uint32_t kWarpList = 128;                        // candidates of a warp
@@ -248,29 +248,20 @@ __global__ void __launch_bounds__(TH) long_row_kernel(const Rows<T> a) {
     float mine = -INFINITY;
     constexpr int U = 4;                                   // chunks worked on while as many are on their way
     Chunk<T> next[U];
-    auto fetch = [&](uint32_t ch) {
+    auto fetch = [&](uint32_t ch) {                        // (chunks behind the block's part are another block's: nothing)
 #pragma unroll
-        for (int u = 0; u < U; u++) next[u].fetch(z, i_first + (int)(ch + u * TH) * 8, a.V);
+        for (int u = 0; u < U; u++) next[u].fetch(z, i_first + (int)(ch + u * TH) * 8, ch + u * TH < chunks ? a.V : 0);
     };
-    const uint32_t full = chunks / (U * TH) * (U * TH);    // (chunks behind the block's part are another block's: whole groups only)
-    uint32_t ch = tid;
-    if (full) fetch(ch);
-    for (; ch < full; ch += U * TH) {
+    fetch(tid);
+    for (uint32_t ch = tid; ch < chunks; ch += U * TH) {
         float v[U][8];
 #pragma unroll
         for (int u = 0; u < U; u++) next[u].open(v[u]);
-        if (ch + U * TH < full) fetch(ch + U * TH);
+        if (ch + U * TH < chunks) fetch(ch + U * TH);
         mine = fmaxf(mine, fmaxf(fmaxf(max_of(v[0]), max_of(v[1])), fmaxf(max_of(v[2]), max_of(v[3]))));
         if (mine > q.m) stat_raise(q, mine, c);
 #pragma unroll
         for (int u = 0; u < U; u++) stat_add(q, v[u], c);
-    }
-    for (; ch < chunks; ch += TH) {
-        float v[8];
-        load_chunk(z, i_first + (int)ch * 8, a.V, v);
-        mine = fmaxf(mine, max_of(v));
-        if (mine > q.m) stat_raise(q, mine, c);
-        stat_add(q, v, c);
     }
     constexpr int GL = TH / kGroups;                       // lanes of a group
     float m = mine;
@@ -538,6 +529,8 @@ extern "C" int sf_label_logprobs(sf_ctx* ctx, const void* logits, int dtype, con
         if (room <= 256) return launch_rows<T, 32, 1>(a, st);
         if (room <= 512) return launch_rows<T, 32, 2>(a, st);
         if (room <= 1024) return launch_rows<T, 32, 4>(a, st);
+        // (20,000 rows of 2,000 fp32, k = 2: 66 us by warps, 106 by blocks; twice as long rows no longer fit a warp's registers: 246 and 98)
+        if (room <= 2048) return launch_rows<T, 32, 8>(a, st);
         // a cluster of eight blocks a row where the rows alone do not fill the machine and are long enough for eight blocks
         if (n < (uint32_t)ctx->num_sms && V >= 16384) return V >= 131072 ? launch_long<T, 512, 8>(a, st) : launch_long<T, 256, 8>(a, st);
         return V <= 8192 ? launch_long<T, 128, 1>(a, st) : (V <= 65536 ? launch_long<T, 256, 1>(a, st) : launch_long<T, 512, 1>(a, st));
