@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(const Conv<T> a) {
 
 // The same walk with WT - 1 rows more at a tile's end: dx_o = sum_m tap[m] dpre_{o+m} is complete once dpre_{o+WT-1} is there.
 template <typename T, int V, int WT, bool EXACT>
-__global__ void __launch_bounds__(kThreads, 4) conv_backward_kernel(const Conv<T> a) {
+__global__ void __launch_bounds__(kThreads, WT <= 4 ? 4 : 2) conv_backward_kernel(const Conv<T> a) {
     sf_chain_enter();
     extern __shared__ float sums[];                        // [threads][V][WT + 1] where the block joins its sums
     const Tiling& t = a.t;
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(256) conv_join_kernel(const float* __restrict_
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32, e = blockIdx.x * 32 + lane, n = D * (W + 1);
     float v = 0.0f;
     if (e < n) {
-#pragma unroll 4
+#pragma unroll 8
         for (uint32_t p = warp; p < n_parts; p += 8) v += parts[(size_t)p * n + e];
     }
     sh[warp][lane] = v;

@@ -438,25 +438,45 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
                         store_word<T, VE>((T*)a.dz + at * a.lddz + ch0 + pc.lc + P::step(i, a.lddz), dz);
                     }
                 }
-                // dB and dC over the block's channels: four threads for four states of a row, each every fourth of the lanes' parts, in their order
-                for (int o = threadIdx.x / 4; o < min(left, R) * 2 * SL; o += blockDim.x / 4) {
-                    const int t = o / (2 * SL), k = o / SL % 2, n = o % SL * 4, sub = threadIdx.x & 3;
-                    f2 x = 0, y = 0;
-                    for (int i = sub; i < warps * CL; i += 4) {
+                // dB and dC over the block's channels: a thread takes four states of a row, or four threads do, each every fourth of the lanes' parts, where
+                // those are many; always in the parts' order
+                auto join_part = [&](int t, int k, int n, int from, int by, f2& x, f2& y) {
+                    x = y = 0;
+                    for (int i = from; i < warps * CL; i += by) {
                         const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&all[i / CL].dbc[t][k][i % CL][n]);
                         x = add2(x, w.x); y = add2(y, w.y);
                     }
-                    const uint32_t who = 0xFu << (lane & 28);
-#pragma unroll
-                    for (int m = 1; m < 4; m <<= 1) { x = add2(x, __shfl_xor_sync(who, x, m)); y = add2(y, __shfl_xor_sync(who, y, m)); }
-                    float v[4];
-                    unpack2(x, v[0], v[1]); unpack2(y, v[2], v[3]);
-                    const float mine = sub == 0 ? v[0] : (sub == 1 ? v[1] : (sub == 2 ? v[2] : v[3]));
-                    if (n + sub >= (int)a.N) continue;
+                };
+                auto put = [&](int t, int k, int n, float v) {
+                    if (n >= (int)a.N) return;
                     const size_t row = row0 + R * q + t;
-                    if (a.sum_bc) a.sum_bc[((((size_t)cb * a.q.rows + row) * a.G + g) * 2 + k) * a.N + n + sub] = mine;
-                    else if (k == 0) { if (a.dB) ((T*)a.dB)[row * a.lddb + g * a.N + n + sub] = from_f32<T>(mine); }
-                    else if (a.dC) ((T*)a.dC)[row * a.lddc + g * a.N + n + sub] = from_f32<T>(mine);
+                    if (a.sum_bc) a.sum_bc[((((size_t)cb * a.q.rows + row) * a.G + g) * 2 + k) * a.N + n] = v;
+                    else if (k == 0) { if (a.dB) ((T*)a.dB)[row * a.lddb + g * a.N + n] = from_f32<T>(v); }
+                    else if (a.dC) ((T*)a.dC)[row * a.lddc + g * a.N + n] = from_f32<T>(v);
+                };
+                const int outs = min(left, R) * 2 * SL;
+                if (warps * CL >= 16) {
+                    for (int o = threadIdx.x / 4; o < outs; o += blockDim.x / 4) {
+                        const int t = o / (2 * SL), k = o / SL % 2, n = o % SL * 4, sub = threadIdx.x & 3;
+                        f2 x, y;
+                        join_part(t, k, n, sub, 4, x, y);
+                        const uint32_t who = 0xFu << (lane & 28);
+#pragma unroll
+                        for (int m = 1; m < 4; m <<= 1) { x = add2(x, __shfl_xor_sync(who, x, m)); y = add2(y, __shfl_xor_sync(who, y, m)); }
+                        float v[4];
+                        unpack2(x, v[0], v[1]); unpack2(y, v[2], v[3]);
+                        put(t, k, n + sub, sub == 0 ? v[0] : (sub == 1 ? v[1] : (sub == 2 ? v[2] : v[3])));
+                    }
+                } else {
+                    for (int o = threadIdx.x; o < outs; o += blockDim.x) {
+                        const int t = o / (2 * SL), k = o / SL % 2, n = o % SL * 4;
+                        f2 x, y;
+                        join_part(t, k, n, 0, 1, x, y);
+                        float v[4];
+                        unpack2(x, v[0], v[1]); unpack2(y, v[2], v[3]);
+#pragma unroll
+                        for (int e = 0; e < 4; e++) put(t, k, n + e, v[e]);
+                    }
                 }
                 __syncthreads();
             }
@@ -500,13 +520,22 @@ __global__ void __launch_bounds__(256) join_states_kernel(const Scan a) {
     }
 }
 
-// dA, dD and dbias from the runs' sums
+// dA, dD and dbias from the runs' sums: 32 values a block, a warp takes every eighth sum of each
 __global__ void __launch_bounds__(256) join_params_kernel(const Scan a) {
     sf_chain_enter();
-    const uint64_t e = (uint64_t)blockIdx.x * 256 + threadIdx.x, n = (uint64_t)a.D * (a.N + 2);
-    if (e >= n) return;
+    __shared__ float sh[8][32];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    const uint64_t e = (uint64_t)blockIdx.x * 32 + lane, n = (uint64_t)a.D * (a.N + 2);
     float v = 0.0f;
-    for (uint32_t p = 0; p < a.runs; p++) v += a.sum_par[(size_t)p * n + e];
+    if (e < n) {
+#pragma unroll 8
+        for (uint32_t p = warp; p < a.runs; p += 8) v += a.sum_par[(size_t)p * n + e];
+    }
+    sh[warp][lane] = v;
+    __syncthreads();
+    if (warp || e >= n) return;
+#pragma unroll
+    for (int i = 1; i < 8; i++) v += sh[i][lane];
     const uint32_t c = (uint32_t)(e / (a.N + 2)), k = (uint32_t)(e % (a.N + 2));
     if (k < a.N) { if (a.dA) a.dA[(size_t)c * a.N + k] = v; }
     else if (k == a.N) { if (a.dD) a.dD[c] = v; }
@@ -566,7 +595,7 @@ extern "C" int sf_seq_scan_backward(sf_ctx* ctx, const sf_sequences* seq, const 
                     e = launch(join_states_kernel<T>, dim3((uint32_t)gx, b.q.n_seq), 256, 0, st, b);
                 }
             }
-            if (e == SF_OK && (a.dA || a.dD || a.dbias_out)) e = launch(join_params_kernel, (uint32_t)(((uint64_t)in->D * (in->N + 2) + 255) / 256), 256, 0, st, a);
+            if (e == SF_OK && (a.dA || a.dD || a.dbias_out)) e = launch(join_params_kernel, (uint32_t)(((uint64_t)in->D * (in->N + 2) + 31) / 32), 256, 0, st, a);
             return e;
         });
     });
