@@ -182,6 +182,58 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(const Conv<T> a) {
     }
 }
 
+// Single rows (max_len 1): the state's rows are read once, moved up by one and written; several sequences on their way at once.
+template <typename T, int V, int WT, bool EXACT>
+__global__ void __launch_bounds__(kThreads) conv_step_kernel(const Conv<T> a) {
+    sf_chain_enter();
+    constexpr int U = WT <= 4 ? 4 : 2;
+    const Tiling& t = a.t;
+    const uint32_t c = (blockIdx.x % t.cblocks * t.lanes + threadIdx.x % t.lanes) * V, per = kThreads / t.lanes;
+    if (c >= a.D) return;
+    const int H = (EXACT ? WT : (int)a.W) - 1;             // rows of a state; the last is at [WT - 2]
+    Ch<V> tap[WT], bias;
+    load_taps<V, WT>(a.w, c, a.W, tap);
+    load_bias<V>(a.bias, c, bias);
+    const uint64_t stride = (uint64_t)t.parts * per;
+    for (uint64_t s0 = (uint64_t)(blockIdx.x / t.cblocks) * per + threadIdx.x / t.lanes; s0 < a.q.n_seq; s0 += U * stride) {
+        Range r[U];
+        Raw<T, V> x[U] = {}, st[U][WT - 1] = {};
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            r[u].len = 0; r[u].slot = -1;
+            if (s0 + u * stride < a.q.n_seq) r[u] = range_of(a.q, (uint32_t)(s0 + u * stride), a.st);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (r[u].len) x[u].fetch(a.x + (size_t)r[u].first * a.ldx + c);
+            if (a.state_in && r[u].slot >= 0) {
+#pragma unroll
+                for (int k = 0; k + 1 < WT; k++)
+                    if (EXACT || k >= WT - 1 - H) st[u][k].fetch_plain(a.state_in + ((size_t)r[u].slot * H + (k - (WT - 1 - H))) * a.D + c);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const bool row = r[u].len > 0;
+            if (row) {
+                Ch<V> pre = bias, v;
+                x[u].open(v);
+                pre.add_product(tap[0], v);
+#pragma unroll
+                for (int m = 1; m < WT; m++) if (EXACT || m <= H) { st[u][WT - 1 - m].open(v); pre.add_product(tap[m], v); }
+                if (a.silu) pre.silu();
+                store<T, V>(a.y + (size_t)r[u].first * a.ldy + c, pre);
+            }
+            if (a.state_out && r[u].slot >= 0) {
+                T* so = a.state_out + (size_t)r[u].slot * H * a.D + c;
+#pragma unroll
+                for (int k = 0; k + 1 < WT; k++)
+                    if (EXACT || k >= WT - 1 - H) *reinterpret_cast<decltype(x[u].w)*>(so + (size_t)(k - (WT - 1 - H)) * a.D) = !row ? st[u][k].w : (k + 2 < WT ? st[u][k + 2 < WT ? k + 1 : k].w : x[u].w);
+            }
+        }
+    }
+}
+
 // The same walk with WT - 1 rows more at a tile's end: dx_o = sum_m tap[m] dpre_{o+m} is complete once dpre_{o+WT-1} is there.
 template <typename T, int V, int WT, bool EXACT>
 __global__ void __launch_bounds__(kThreads, WT <= 4 ? 4 : 2) conv_backward_kernel(const Conv<T> a) {
@@ -375,6 +427,11 @@ extern "C" int sf_seq_conv(sf_ctx* ctx, const sf_sequences* seq, const void* x, 
                 Conv<T> a = {};
                 a.q = seqs_of(seq, rows, n_slots); a.x = (const T*)x; a.ldx = ldx; a.w = w; a.bias = bias; a.D = D; a.W = W; a.silu = act == SF_ACT_SILU;
                 a.state_in = (const T*)state_in; a.state_out = (T*)state_out; a.y = (T*)y_out; a.ldy = ldy; a.st = ctx->d_state;
+                if (seq->max_len == 1) {
+                    a.t = tiling(seq, D, V, 8);
+                    SF_CUDA(sf_launch_chained(conv_step_kernel<T, V, WT, decltype(exact)::value>, a.t.cblocks * a.t.parts, kThreads, 0, (cudaStream_t)stream, a));
+                    return (int)SF_OK;
+                }
                 a.t = tiling(seq, D, V, 32);
                 SF_CUDA(sf_launch_chained(conv_kernel<T, V, WT, decltype(exact)::value>, a.t.cblocks * a.t.parts, kThreads, 0, (cudaStream_t)stream, a));
                 return (int)SF_OK;
