@@ -73,6 +73,7 @@ extern "C" {
 #define SF_MAX_EXPERTS  1024
 #define SF_ACT_NONE     0
 #define SF_ACT_SILU     1          /* x * sigmoid(x) */
+#define SF_SEQ_MAX_ROWS 2147418112u  /* rows of the arrays, sequences, rows of a sequence that the sf_seq_* calls take (2^31 - 2^16) */
 #define SF_SCAN_MAX_STATES 64      /* states of a channel that sf_seq_scan takes */
 #define SF_MAX_TOP      32         /* alternatives that sf_label_logprobs gives */
 #define SF_EXPERT_MAX_D 16777216u  /* widest row that the expert calls move */
@@ -476,13 +477,13 @@ int  sf_seq_scan_backward(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_ro
 
 /* ---- scores of answers -------------------------------------------------------------- */
 /* What sf_route's scores are to the fast model's class probabilities, for rows of any logits (a slow model's, a training step's): with
- * x = scale * logits (scale > 0, 1 / temperature) and lse = ln sum_i exp(x_i), in one pass over rows of V entries (pitch ld)
+ * x = scale * logits (0 < scale <= 1e30, 1 / temperature) and lse = ln sum_i exp(x_i), in one pass over rows of V entries (pitch ld)
  *   logprob_out[r] = x[labels[r]] - lse         (labels int32[n]; a label outside 0..V-1 stands for none: 0)
  *   entropy_out[r] = -sum_i p_i ln p_i          (the score of Sec. 3.2; goes into sf_universal_thresholds_dev as it is)
  *   lse_out[r]
  *   top_ids_out int32[n][k], top_logprobs_out fp32[n][k]: the k <= SF_MAX_TOP largest entries, largest first, ties to the lowest index;
  *                                               1 - exp of the first is the least-confidence score.
- * each nullable.  An entry of -infinity is masked: it adds nothing, is never picked (id -1, log probability -infinity where fewer than k are left), and
+ * each nullable; V < 2^31 - 2^20.  An entry of -infinity is masked: it adds nothing, is never picked (id -1, log probability -infinity where fewer than k are left), and
  * as a label has log probability -infinity.  A row with nothing but masked entries has lse -infinity and entropy 0.  A NaN or +infinity
  * makes the row's lse, entropy and log probabilities NaN; NaN is never picked.  n_dev as in the expert calls.  No workspace. */
 int  sf_label_logprobs(sf_ctx* ctx, const void* logits, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t V, size_t ld, float scale,

@@ -25,7 +25,7 @@ SF_F32, SF_BF16, SF_F16, SF_MX4 = 0, 1, 2, 3
 SF_GATE_SOFTMAX, SF_GATE_SOFTMAX_PICKED, SF_GATE_SHARE = 0, 1, 2
 SF_MAX_EXPERTS = 1024
 SF_ACT_NONE, SF_ACT_SILU = 0, 1
-SF_SCAN_MAX_STATES, SF_MAX_TOP = 64, 32
+SF_SEQ_MAX_ROWS, SF_SCAN_MAX_STATES, SF_MAX_TOP = 2 ** 31 - 2 ** 16, 64, 32
 SF_TAU_MARGIN_DEFAULT = float.fromhex("0x1.b1d106p-1")
 
 

@@ -14,6 +14,7 @@ using namespace sfseq;
 
 constexpr uint32_t kThreads = 256;
 constexpr uint32_t kMaxTop = SF_MAX_TOP;
+constexpr uint32_t kMaxV = 0x7FF00000;              // (entries and those of the chunks behind them in 31 bits)
 
 template <typename T> struct Rows {
     const T* z; size_t ld;
@@ -423,6 +424,10 @@ template <typename T> struct RowBack {
             if (ge != 0.0f) q = fma2(g2, add2(pack2(fmaxf(x, -1e4f), fmaxf(y, -1e4f)), h2), s2);
             unpack2(mul2(p, q), d[e], d[e + 1]);
         }
+        if (!(lse > -INFINITY)) {                          // (a row with a NaN: its masked entries get 0 all the same)
+#pragma unroll
+            for (int e = 0; e < 8; e++) if (v[e] == -INFINITY) d[e] = 0.0f;
+        }
         if (label - (uint32_t)i0 < 8u) {
 #pragma unroll
             for (int e = 0; e < 8; e++) if (label == (uint32_t)(i0 + e)) d[e] = v[e] == -INFINITY ? 0.0f : d[e] + g;
@@ -500,7 +505,7 @@ uint32_t room_of(const void* p, size_t ld, int dtype, uint32_t V) {
     return V + (aligned(p, 16) && ld * type_bytes(dtype) % 16 == 0 ? 0 : 16 / type_bytes(dtype) - 1);
 }
 
-bool scale_ok(float s) { return s > 0.0f && s < INFINITY; }
+bool scale_ok(float s) { return s > 0.0f && s <= 1e30f; }      // (a larger one times log2 e or an entry's distance of 1 would be infinite)
 
 }  // namespace
 
@@ -508,7 +513,7 @@ extern "C" int sf_label_logprobs(sf_ctx* ctx, const void* logits, int dtype, con
                                  const int32_t* labels, float* logprob_out, float* entropy_out, float* lse_out, uint32_t k, int32_t* top_ids_out,
                                  float* top_logprobs_out, void* stream)
 {
-    if (!ctx || !type_ok(dtype) || V == 0 || V > 0x7FFFFFFFu - 64 || ld < V || n > 0x7FFFFFFFu || k > kMaxTop || k > V || !scale_ok(scale)) return SF_ERR_ARG;
+    if (!ctx || !type_ok(dtype) || V == 0 || V > kMaxV || ld < V || n > 0x7FFFFFFFu || k > kMaxTop || k > V || !scale_ok(scale)) return SF_ERR_ARG;
     if (k == 0) { top_ids_out = nullptr; top_logprobs_out = nullptr; }
     if (!logprob_out && !entropy_out && !lse_out && !top_ids_out && !top_logprobs_out) return SF_ERR_ARG;
     if (n == 0) return SF_OK;
@@ -541,7 +546,7 @@ extern "C" int sf_label_logprobs_backward(sf_ctx* ctx, const void* logits, int d
                                           const int32_t* labels, const float* lse, const float* d_logprob, const float* entropy, const float* d_entropy,
                                           uint32_t k, const int32_t* top_ids, const float* d_top_logprobs, void* d_logits_out, size_t ldd, void* stream)
 {
-    if (!ctx || !type_ok(dtype) || V == 0 || V > 0x7FFFFFFFu - 64 || ld < V || ldd < V || n > 0x7FFFFFFFu || k > kMaxTop || k > V || !scale_ok(scale)) return SF_ERR_ARG;
+    if (!ctx || !type_ok(dtype) || V == 0 || V > kMaxV || ld < V || ldd < V || n > 0x7FFFFFFFu || k > kMaxTop || k > V || !scale_ok(scale)) return SF_ERR_ARG;
     if (k == 0) d_top_logprobs = nullptr;
     if (n == 0) return SF_OK;
     if (!logits || !lse || !d_logits_out || (d_logprob && !labels) || (d_entropy && !entropy) || (d_top_logprobs && !top_ids)) return SF_ERR_ARG;

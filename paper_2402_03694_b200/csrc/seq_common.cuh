@@ -55,7 +55,7 @@ __device__ __forceinline__ f2 sigmoid2(f2 x) {
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
 inline int check_sequences(const sf_sequences* q, uint32_t rows) {
-    if (!q || q->max_len == 0 || rows > 0x7FFFFFFFu || q->n_seq > 0x7FFFFFFFu || q->max_len > 0x7FFFFFFFu) return SF_ERR_ARG;
+    if (!q || q->max_len == 0 || rows > SF_SEQ_MAX_ROWS || q->n_seq > SF_SEQ_MAX_ROWS || q->max_len > SF_SEQ_MAX_ROWS) return SF_ERR_ARG;
     if (q->n_seq && !q->offsets) return SF_ERR_ARG;
     return aligned(q->offsets, 4) && aligned(q->counts, 4) && aligned(q->slots, 4) ? SF_OK : SF_ERR_ARG;
 }

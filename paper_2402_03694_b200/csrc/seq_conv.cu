@@ -442,7 +442,7 @@ extern "C" int sf_seq_conv(sf_ctx* ctx, const sf_sequences* seq, const void* x, 
 
 extern "C" int sf_seq_conv_backward_workspace(uint32_t n_seq, uint32_t max_len, uint32_t D, uint32_t W, size_t* bytes_out)
 {
-    if (!bytes_out || max_len == 0 || D == 0 || D > SF_EXPERT_MAX_D || W == 0 || W > kMaxTaps) return SF_ERR_ARG;
+    if (!bytes_out || n_seq > SF_SEQ_MAX_ROWS || max_len == 0 || max_len > SF_SEQ_MAX_ROWS || D == 0 || D > SF_EXPERT_MAX_D || W == 0 || W > kMaxTaps) return SF_ERR_ARG;
     const sf_sequences q = {nullptr, nullptr, nullptr, n_seq, max_len};
     uint32_t parts = 1;
     for (uint32_t v : {1u, 2u, 4u}) parts = std::max(parts, tiling(&q, D, v, 4).parts);

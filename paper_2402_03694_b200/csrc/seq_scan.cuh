@@ -233,7 +233,7 @@ inline Plan plan_of(uint32_t n_seq, uint32_t max_len, uint32_t D, uint32_t N, ui
     const uint64_t want = full / warps();
     p.cblocks = (p.cwarps + kWarps - 1) / kWarps;
     p.part_len = (max_len + kEvery - 1) / kEvery * kEvery;
-    if (want >= 3 && max_len > 2 * 32) p.part_len = (uint32_t)std::max<uint64_t>(32, ((max_len + want - 1) / want + kEvery - 1) / kEvery * kEvery);
+    if (n_seq && want >= 3 && max_len > 2 * 32) p.part_len = (uint32_t)std::max<uint64_t>(32, ((max_len + want - 1) / want + kEvery - 1) / kEvery * kEvery);
     p.parts = (max_len + p.part_len - 1) / p.part_len;
     p.split = p.parts > 1;
     const uint64_t blocks = (uint64_t)G * p.cblocks, items = std::max<uint64_t>(1, (uint64_t)n_seq * p.parts);
@@ -246,7 +246,7 @@ inline size_t back_bytes(const Plan& p, uint32_t n_seq, uint32_t rows, uint32_t 
 }
 
 inline bool sizes_ok(uint32_t rows, uint32_t n_seq, uint32_t max_len, uint32_t D, uint32_t N, uint32_t G) {
-    return rows <= 0x7FFFFFFFu && n_seq <= 0x7FFFFFFFu && max_len && max_len <= 0x7FFFFFFFu && D && D <= SF_EXPERT_MAX_D && N && N <= kMaxStates && G && D % G == 0;
+    return rows <= SF_SEQ_MAX_ROWS && n_seq <= SF_SEQ_MAX_ROWS && max_len && max_len <= SF_SEQ_MAX_ROWS && D && D <= SF_EXPERT_MAX_D && N && N <= kMaxStates && G && D % G == 0;
 }
 
 template <typename F> int by_states(uint32_t sl, F f) {

@@ -147,6 +147,7 @@ def test_lowest_values_infinities_and_nan(env, V):
     x[3, 2] = float("nan")
     x[4, 5] = -0.0
     x[5] = -low                                            # the largest numbers
+    x[3, 7] = -float("inf")
     labels = torch.full((6,), 1, dtype=torch.int32, device="cuda")
     o = run(sf, ctx, x, labels, 3, 1.0)
     lp, h, ids = num(o["logprob"]), num(o["entropy"]), num(o["top_ids"])
@@ -161,7 +162,7 @@ def test_lowest_values_infinities_and_nan(env, V):
     sf.sf_label_logprobs_backward(ctx, x, labels, o["lse"], d, d_logprob=torch.ones(6, device="cuda"), entropy=o["entropy"], d_entropy=torch.ones(6, device="cuda"))
     g = num(d)
     assert np.isnan(g[2]).any() and np.isnan(g[3]).any() and np.isfinite(g[[0, 1, 4, 5]]).all()
-    assert abs(g[4, 1] - (1 - 1 / V)) < 4 * c
+    assert abs(g[4, 1] - (1 - 1 / V)) < 4 * c and g[3, 7] == 0          # masked: 0 in a row with a NaN too
 
 
 def test_rows_behind_the_count_and_each_output_alone(env):

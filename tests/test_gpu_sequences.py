@@ -156,6 +156,8 @@ SCAN = [
     (9, 5, 1, "fp16", [1] * 3, False, True, 0, 1, False, True, True, False),
     (24, 16, 1, "fp32", [300], False, True, 0, 0, True, True, True, True),             # in parts
     (32, 4, 2, "bf16", [260, 0, 131], True, True, 0, 0, True, True, True, True),       # in parts, one empty
+    (520, 4, 1, "fp32", [2, 9] + [1] * 158, False, False, 0, 0, True, True, True, True),       # a whole block of wide warps
+    (1032, 3, 1, "bf16", [3] * 150, False, False, 0, 0, True, True, True, True),
 ]
 
 
@@ -311,10 +313,10 @@ def bad_sequences(sf):
             "falling offsets": (sf.make_sequences(i32(0, 6, 4, 9), 12), sf.SF_ERR_ARG, [(0, 6), (4, 9)]),
             "counts beyond the offsets": (sf.make_sequences(i32(0, 4, 9), 12, counts=i32(9, 2)), sf.SF_ERR_CAPACITY, [(0, 4), (4, 6)]),
             "longer than max_len": (sf.make_sequences(i32(0, 9), 5), sf.SF_ERR_CAPACITY, [(0, 5)]),
-            "nothing": (sf.make_sequences(i32(0), 5), sf.SF_OK, [])}
+            "nothing": (sf.make_sequences(i32(0), 5), sf.SF_OK, []), "nothing of long sequences": (sf.make_sequences(i32(0), 5000), sf.SF_OK, [])}
 
 
-@pytest.mark.parametrize("which", ["rows behind the arrays", "first row behind the arrays", "falling offsets", "counts beyond the offsets", "longer than max_len", "nothing"])
+@pytest.mark.parametrize("which", ["rows behind the arrays", "first row behind the arrays", "falling offsets", "counts beyond the offsets", "longer than max_len", "nothing", "nothing of long sequences"])
 def test_sequences_that_do_not_fit_are_cut(env, which):
     sf, ctx = env
     q, status, parts = bad_sequences(sf)[which]

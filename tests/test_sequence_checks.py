@@ -124,8 +124,8 @@ def seq(n_seq=2, max_len=5, offsets=P, counts=None, slots=None):
 def test_convolution_refusals(lib):
     good = dict(ctx=P, seq=seq(), x=P, dtype=0, rows=6, D=8, ldx=8, w=P, bias=P, W=4, act=1, state_in=P, state_out=P, n_slots=2, y=P, ldy=8, stream=0)
     bad = [dict(ctx=None), dict(seq=None), dict(x=None), dict(w=None), dict(y=None), dict(dtype=3), dict(dtype=-1), dict(D=0), dict(D=2 ** 24 + 1), dict(ldx=7), dict(ldy=7), dict(W=0),
-           dict(W=9), dict(act=2), dict(rows=2 ** 31), dict(n_slots=2 ** 31), dict(x=P + 2), dict(w=P + 1), dict(bias=P + 2), dict(state_in=P + 1), dict(y=P + 1), dict(dtype=1, x=P + 1),
-           dict(seq=seq(max_len=0)), dict(seq=seq(offsets=None)), dict(seq=seq(offsets=P + 2)), dict(seq=seq(counts=P + 1)), dict(seq=seq(slots=P + 1)), dict(seq=seq(n_seq=2 ** 31))]
+           dict(W=9), dict(act=2), dict(rows=sf.SF_SEQ_MAX_ROWS + 1), dict(n_slots=2 ** 31), dict(x=P + 2), dict(w=P + 1), dict(bias=P + 2), dict(state_in=P + 1), dict(y=P + 1), dict(dtype=1, x=P + 1),
+           dict(seq=seq(max_len=0)), dict(seq=seq(max_len=sf.SF_SEQ_MAX_ROWS + 1)), dict(seq=seq(offsets=None)), dict(seq=seq(offsets=P + 2)), dict(seq=seq(counts=P + 1)), dict(seq=seq(slots=P + 1)), dict(seq=seq(n_seq=2 ** 31))]
     for b in bad:
         assert lib.sf_seq_conv(*{**good, **b}.values()) == sf.SF_ERR_ARG, b
     back = dict(ctx=P, seq=seq(), x=P, dtype=0, rows=6, D=8, ldx=8, w=P, bias=P, W=4, act=1, state_in=P, dy=P, lddy=8, d_state=P, n_slots=2, dx=P, lddx=8, dw=P, db=P, di=P, work=P,
@@ -156,7 +156,7 @@ def test_scan_refusals(lib):
 
 def test_logprob_refusals(lib):
     good = dict(ctx=P, x=P, dtype=0, n_dev=None, n=6, V=10, ld=10, scale=1.0, labels=P, lp=P, h=P, lse=P, k=2, ids=P, top=P, stream=0)
-    bad = [dict(ctx=None), dict(x=None), dict(dtype=3), dict(V=0), dict(V=2 ** 31), dict(ld=9), dict(n=2 ** 31), dict(k=33, V=100, ld=100), dict(k=11), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")),
+    bad = [dict(ctx=None), dict(x=None), dict(dtype=3), dict(V=0), dict(V=0x7FF00001, ld=2 ** 31), dict(ld=9), dict(n=2 ** 31), dict(k=33, V=100, ld=100), dict(k=11), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=2e30),
            dict(scale=float("nan")), dict(x=P + 2), dict(labels=P + 1), dict(n_dev=P + 1)]
     for b in bad + [dict(labels=None), dict(lp=None, h=None, lse=None, ids=None, top=None), dict(lp=None, h=None, lse=None, k=0), dict(lp=P + 1), dict(ids=None, top=None), dict(top=P + 2)]:
         assert lib.sf_label_logprobs(*{**good, **b}.values()) == sf.SF_ERR_ARG, b
