@@ -7,8 +7,8 @@ using namespace sfscan;
 
 // What a warp keeps in shared memory.  Sums over states are left as one part a state lane and joined where the row is written.  Rows are spaced so that
 // the 16-byte accesses of eight lanes meet no common bank: PX floats a row of channels, PY a part, PT the parts of a row.
-template <typename T, int SL, int VV> struct __align__(16) Forward {
-    typedef Shape<SL> S;
+template <typename T, int SL, int VV, int J> struct __align__(16) Forward {
+    typedef Shape<SL, J> S;
     typedef Pieces<S::K, S::CH, VV> P;
     typedef States<T, VV, S::K, S::NP> ST;
     static constexpr int PX = S::CH + 4, PY = S::CH + (SL == 1 ? 0 : (SL == 2 ? 16 : (SL == 4 ? 8 : 4))), PT = SL * PY + 4;
@@ -21,14 +21,15 @@ template <typename T, int SL, int VV> struct __align__(16) Forward {
 
 // The scan of a sequence, or of one part of it (blockIdx.y): from the state that `part_state` holds where sequences go in parts.
 // ENDS: only the state at the part's end, from zero, and the sum of the part's steps.
-template <typename T, int SL, int VV, bool ENDS>
+template <typename T, int SL, int VV, bool ENDS, int J>
 __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     sf_chain_enter();
-    typedef Shape<SL> S;
+    typedef Shape<SL, J> S;
     typedef Pieces<S::K, S::CH, VV> P;
+    constexpr int JP = J / 2;                              // pairs of channels of a lane
     constexpr int K = S::K, CH = S::CH, NP = S::NP, I = P::I;
     extern __shared__ __align__(16) unsigned char shared[];
-    typedef Forward<T, SL, VV> Sh;
+    typedef Forward<T, SL, VV, J> Sh;
     Sh& sh = reinterpret_cast<Sh*>(shared)[threadIdx.x / 32];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
     const Item it = item_of(a, CH);
@@ -74,15 +75,15 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
         sh.bias[c] = c < (int)have && a.dbias ? __ldg(a.dbias + ch0 + c) : 0.0f;
         sh.skip[c] = c < (int)have && a.Dk ? __ldg(a.Dk + ch0 + c) : 0.0f;
     }
-    f2 A[2][4], h[2][4];                                   // channels 2 j and 2 j + 1 of the lane's four side by side
+    f2 A[JP][4], h[JP][4];                                 // channels 2 j and 2 j + 1 of the lane's side by side
 #pragma unroll
-    for (int j = 0; j < 2; j++)
+    for (int j = 0; j < JP; j++)
 #pragma unroll
         for (int n = 0; n < 4; n++) {
             float A_[2], h_[2];
 #pragma unroll
             for (int k = 0; k < 2; k++) {
-                const uint32_t c = cl * 4 + 2 * j + k, st = sl * 4 + n;
+                const uint32_t c = cl * J + 2 * j + k, st = sl * 4 + n;
                 const bool there = c < have && st < a.N;
                 const size_t at = (size_t)(ch0 + c) * a.N + st;
                 A_[k] = there ? __ldg(a.A + at) * kLog2e : 0.0f;
@@ -97,13 +98,13 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     // the warp's states into [channel][state]
     auto put = [&](float* p) {
 #pragma unroll
-        for (int j = 0; j < 2; j++) {
+        for (int j = 0; j < JP; j++) {
             float v[2][4];
 #pragma unroll
             for (int n = 0; n < 4; n++) unpack2(h[j][n], v[0][n], v[1][n]);
 #pragma unroll
             for (int k = 0; k < 2; k++) {
-                const uint32_t c = cl * 4 + 2 * j + k;
+                const uint32_t c = cl * J + 2 * j + k;
                 float* o = p + (size_t)(ch0 + c) * a.N + sl * 4;
                 if (c >= have) continue;
                 if (a.n4 && ((uintptr_t)o & 15u) == 0) { if (sl * 4 < (int)a.N) *reinterpret_cast<float4*>(o) = make_float4(v[k][0], v[k][1], v[k][2], v[k][3]); }
@@ -166,19 +167,25 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
         if (t0 + K < t_end) ask(t0 + K);
         if (!ENDS && a.starts && t0 % kEvery == 0) put(a.starts + start_index(r.first, s, t0) * a.D * a.N);
         auto row = [&](int t) {
-            const ulonglong2 d2 = *reinterpret_cast<const ulonglong2*>(&sh.step[t][cl * 4]), i2 = *reinterpret_cast<const ulonglong2*>(&sh.in[t][cl * 4]);
+            if (!ENDS && K > (int)kEvery && t % kEvery == 0 && t && a.starts) put(a.starts + start_index(r.first, s, t0 + t) * a.D * a.N);
+            f2 d[JP], in[JP];
+            if constexpr (J == 4) {
+                const ulonglong2 d2 = *reinterpret_cast<const ulonglong2*>(&sh.step[t][cl * J]), i2 = *reinterpret_cast<const ulonglong2*>(&sh.in[t][cl * J]);
+                d[0] = d2.x; d[1] = d2.y; in[0] = i2.x; in[1] = i2.y;
+            } else { d[0] = *reinterpret_cast<const f2*>(&sh.step[t][cl * J]); in[0] = *reinterpret_cast<const f2*>(&sh.in[t][cl * J]); }
             const float4 b4 = *reinterpret_cast<const float4*>(&sh.bc[0][t][sl * 4]);
-            const f2 d[2] = {d2.x, d2.y}, in[2] = {i2.x, i2.y}, b[4] = {dup2(b4.x), dup2(b4.y), dup2(b4.z), dup2(b4.w)};
+            const f2 b[4] = {dup2(b4.x), dup2(b4.y), dup2(b4.z), dup2(b4.w)};
 #pragma unroll
-            for (int j = 0; j < 2; j++)
+            for (int j = 0; j < JP; j++)
 #pragma unroll
                 for (int n = 0; n < 4; n++) h[j][n] = fma2(decay2(d[j], A[j][n]), h[j][n], mul2(in[j], b[n]));
             if constexpr (!ENDS) {
                 const float4 c4 = *reinterpret_cast<const float4*>(&sh.bc[1][t][sl * 4]);
-                f2 y[2];
+                f2 y[JP];
 #pragma unroll
-                for (int j = 0; j < 2; j++) y[j] = fma2(h[j][3], dup2(c4.w), fma2(h[j][2], dup2(c4.z), fma2(h[j][1], dup2(c4.y), mul2(h[j][0], dup2(c4.x)))));
-                *reinterpret_cast<ulonglong2*>(&sh.y[t][sl * Sh::PY + cl * 4]) = make_ulonglong2(y[0], y[1]);
+                for (int j = 0; j < JP; j++) y[j] = fma2(h[j][3], dup2(c4.w), fma2(h[j][2], dup2(c4.z), fma2(h[j][1], dup2(c4.y), mul2(h[j][0], dup2(c4.x)))));
+                if constexpr (J == 4) *reinterpret_cast<ulonglong2*>(&sh.y[t][sl * Sh::PY + cl * J]) = make_ulonglong2(y[0], y[1]);
+                else *reinterpret_cast<f2*>(&sh.y[t][sl * Sh::PY + cl * J]) = y[0];
             }
         };
         if (rows == K) {
@@ -405,15 +412,22 @@ extern "C" int sf_seq_scan(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_r
                 const bool v4 = in->N % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16) && aligned(in->A, 16);
                 return launch(v4 ? step_kernel<T, SL, true> : step_kernel<T, SL, false>, (uint32_t)blocks, 32 * kWarps, 0, st, a);
             }
-            const size_t smem = (vec ? sizeof(Forward<T, SL, VV>) : sizeof(Forward<T, SL, 1>)) * kWarps;
+            // Where whole sequences leave half of the machine idle and are too many to go in parts: two channels a lane, twice the warps
+            // (64 sequences of 512 rows x 512: 145 us with four channels a lane, 135 with two; 4096 of up to 128 x 256, where warps are many: 414 with four)
+            if constexpr (SL == 4) if (vec && !p.split && (uint64_t)seq->n_seq * in->G * p.cwarps < (uint64_t)SF_NUM_SMS_DEFAULT * 10) {
+                set_warps(a, (a.per + 15) / 16);
+                const uint64_t b = ((uint64_t)seq->n_seq * in->G * a.cwarps + kWarps - 1) / kWarps;
+                return launch(scan_kernel<T, SL, VV, false, 2>, dim3((uint32_t)b, 1), 32 * kWarps, sizeof(Forward<T, SL, VV, 2>) * kWarps, st, a);
+            }
+            const size_t smem = (vec ? sizeof(Forward<T, SL, VV, 4>) : sizeof(Forward<T, SL, 1, 4>)) * kWarps;
             if (p.split) {
                 a.part_state = (float*)workspace;
                 a.part_step = (float*)((char*)workspace + sf_align256((size_t)seq->n_seq * p.parts * in->D * in->N * 4));
-                int e = launch(vec ? scan_kernel<T, SL, VV, true> : scan_kernel<T, SL, 1, true>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, smem, st, a);
+                int e = launch(vec ? scan_kernel<T, SL, VV, true, 4> : scan_kernel<T, SL, 1, true, 4>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, smem, st, a);
                 if (e == SF_OK) e = launch(parts_kernel<false>, dim3((uint32_t)(((uint64_t)in->D * in->N + 255) / 256), seq->n_seq), 256, 0, st, a);
                 if (e != SF_OK) return e;
             }
-            return launch(vec ? scan_kernel<T, SL, VV, false> : scan_kernel<T, SL, 1, false>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, smem, st, a);
+            return launch(vec ? scan_kernel<T, SL, VV, false, 4> : scan_kernel<T, SL, 1, false, 4>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, smem, st, a);
         });
     });
 }

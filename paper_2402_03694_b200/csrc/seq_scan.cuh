@@ -90,9 +90,10 @@ __device__ __forceinline__ f2 decay2(f2 delta, f2 A) {
     return pack2(ex2(a), ex2(b));
 }
 
-template <int SL> struct Shape {
-    static constexpr int CL = 32 / SL, CH = 4 * CL, NP = 4 * SL;               // channel lanes, channels of a warp, states with those that fill up
-    static constexpr int K = SL == 1 ? 4 : 8;                                  // rows of a tile of the forward pass (kEvery is a multiple)
+// J: channels of a lane (4; the forward pass also 2, where warps are few)
+template <int SL, int J = 4> struct Shape {
+    static constexpr int CL = 32 / SL, CH = J * CL, NP = 4 * SL;               // channel lanes, channels of a warp, states with those that fill up
+    static constexpr int K = J == 2 ? 16 : (SL == 1 ? 4 : 8);                  // rows of a tile of the forward pass (a multiple of kEvery, or kEvery of it)
 };
 
 // What a warp works on: sequence, group, first of its channels within the group and of all, and how many it has (none: nothing to do)
@@ -271,6 +272,10 @@ inline int check(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_rows* in, u
     if (!aligned(in->u, size) || !aligned(in->delta, size) || !aligned(in->z, size) || !aligned(in->B, size) || !aligned(in->C, size)) return SF_ERR_ARG;
     return aligned(in->A, 4) && aligned(in->D_skip, 4) && aligned(in->delta_bias, 4) ? SF_OK : SF_ERR_ARG;
 }
+inline void set_warps(Scan& a, uint32_t cwarps) {
+    a.cwarps = cwarps;
+    a.few = ((uint64_t)a.q.n_seq + 1) * a.G * cwarps + kWarps <= 0xFFFFFFFFu;
+}
 inline void fill(Scan& a, const sf_sequences* seq, const sf_scan_rows* in, uint32_t rows, uint32_t n_slots, const Plan& p, sf_ctx* ctx) {
     a = {};
     a.q = seqs_of(seq, rows, n_slots);
@@ -279,8 +284,8 @@ inline void fill(Scan& a, const sf_sequences* seq, const sf_scan_rows* in, uint3
     a.A = in->A; a.Dk = in->D_skip; a.dbias = in->delta_bias;
     a.D = in->D; a.N = in->N; a.G = in->G; a.per = in->D / in->G; a.softplus = in->softplus != 0;
     a.n4 = in->N % 4 == 0;
-    a.part_len = p.part_len; a.parts = p.parts; a.runs = p.runs; a.cwarps = p.cwarps; a.cblocks = p.cblocks;
-    a.few = ((uint64_t)seq->n_seq + 1) * in->G * p.cwarps + kWarps <= 0xFFFFFFFFu;
+    a.part_len = p.part_len; a.parts = p.parts; a.runs = p.runs; a.cblocks = p.cblocks;
+    set_warps(a, p.cwarps);
     a.st = ctx->d_state;
 }
 // rows begin on 16-byte boundaries, and so does every group's first channel and state

@@ -156,6 +156,7 @@ SCAN = [
     (9, 5, 1, "fp16", [1] * 3, False, True, 0, 1, False, True, True, False),
     (24, 16, 1, "fp32", [300], False, True, 0, 0, True, True, True, True),             # in parts
     (32, 4, 2, "bf16", [260, 0, 131], True, True, 0, 0, True, True, True, True),       # in parts, one empty
+    (64, 16, 1, "bf16", [33, 16, 8, 9, 1, 17] * 50, False, False, 0, 0, True, True, True, True),      # too many for parts, too few to fill the machine
     (520, 4, 1, "fp32", [2, 9] + [1] * 158, False, False, 0, 0, True, True, True, True),       # a whole block of wide warps
     (1032, 3, 1, "bf16", [3] * 150, False, False, 0, 0, True, True, True, True),
 ]
