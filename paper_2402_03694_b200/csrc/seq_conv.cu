@@ -12,7 +12,8 @@ using namespace sfseq;
 
 constexpr uint32_t kThreads = 128;
 constexpr uint32_t kMaxTaps = 8;
-constexpr int kAheadF = 4, kAheadB = 3;     // rows on their way while others are worked on: forward, backward
+constexpr int kAheadF = 4, kAheadB = 4;     // rows on their way while others are worked on: forward, backward
+constexpr int kBlocksB = 3;                // blocks of the backward kernel an SM: its registers (four with fewer rows ahead: 280 us, these 247)
 
 struct Tiling {
     uint32_t lanes;        // threads side by side on a row (a power of two), of V channels each
@@ -35,8 +36,8 @@ template <typename T> struct Conv {
     sf_dev_state* st;
 };
 
-// V channels side by side
-template <int V> struct Ch {
+// V channels side by side; PAIRS: two an instruction (fewer instructions, more moves: the gradients gain, 280 -> 247 us, the forward pass loses, 122 -> 129)
+template <int V, bool PAIRS> struct Ch {
     float p[V];
     __device__ __forceinline__ void set(const float (&x)[V]) {
 #pragma unroll
@@ -49,6 +50,10 @@ template <int V> struct Ch {
     __device__ __forceinline__ void zero() {
 #pragma unroll
         for (int i = 0; i < V; i++) p[i] = 0.0f;
+    }
+    __device__ __forceinline__ void set_product(const Ch& a, const Ch& b) {
+#pragma unroll
+        for (int i = 0; i < V; i++) p[i] = a.p[i] * b.p[i];
     }
     __device__ __forceinline__ void add_product(const Ch& a, const Ch& b) {
 #pragma unroll
@@ -68,12 +73,48 @@ template <int V> struct Ch {
     }
 };
 
+template <int V> struct Ch<V, true> {
+    static constexpr int P = V / 2;
+    f2 p[P];
+    __device__ __forceinline__ void set(const float (&x)[V]) {
+#pragma unroll
+        for (int i = 0; i < P; i++) p[i] = pack2(x[2 * i], x[2 * i + 1]);
+    }
+    __device__ __forceinline__ void get(float (&x)[V]) const {
+#pragma unroll
+        for (int i = 0; i < P; i++) unpack2(p[i], x[2 * i], x[2 * i + 1]);
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < P; i++) p[i] = 0;
+    }
+    __device__ __forceinline__ void set_product(const Ch& a, const Ch& b) {
+#pragma unroll
+        for (int i = 0; i < P; i++) p[i] = mul2(a.p[i], b.p[i]);
+    }
+    __device__ __forceinline__ void add_product(const Ch& a, const Ch& b) {
+#pragma unroll
+        for (int i = 0; i < P; i++) p[i] = fma2(a.p[i], b.p[i], p[i]);
+    }
+    __device__ __forceinline__ void add(const Ch& a) {
+#pragma unroll
+        for (int i = 0; i < P; i++) p[i] = add2(a.p[i], p[i]);
+    }
+    __device__ __forceinline__ void mul_silu_slope(const Ch& x) {
+#pragma unroll
+        for (int i = 0; i < P; i++) {
+            const f2 s = sigmoid2(x.p[i]), one = dup2(1.0f);
+            p[i] = mul2(mul2(p[i], s), fma2(x.p[i], fma2(s, dup2(-1.0f), one), one));
+        }
+    }
+};
+
 // V elements of T as they lie in memory
 template <typename T, int V> struct Raw {
     typename Word<V * sizeof(T)>::type w;
     __device__ __forceinline__ void fetch(const T* p) { w = __ldg(reinterpret_cast<const decltype(w)*>(p)); }
     __device__ __forceinline__ void fetch_plain(const T* p) { w = *reinterpret_cast<const decltype(w)*>(p); }     // (a pool that the same call writes)
-    __device__ __forceinline__ void open(Ch<V>& c) const {
+    template <bool PAIRS> __device__ __forceinline__ void open(Ch<V, PAIRS>& c) const {
         union { decltype(w) q; T e[V]; } u;
         u.q = w;
         float x[V];
@@ -82,25 +123,31 @@ template <typename T, int V> struct Raw {
         c.set(x);
     }
 };
-template <typename T, int V> __device__ __forceinline__ void store(T* p, const Ch<V>& c) { float x[V]; c.get(x); store_word<T, V>(p, x); }
+template <typename T, int V, bool PAIRS> __device__ __forceinline__ void store(T* p, const Ch<V, PAIRS>& c) { float x[V]; c.get(x); store_word<T, V>(p, x); }
 
 // Filters of the thread's channels by lag: tap[m] is what x_{t-m} is multiplied with, m < W; what lies behind is not used.  Four taps in one
 // access where they lie on a boundary (a thread's filters are its own: narrow accesses of a warp touch as many lines each).
-template <int V, int WT> __device__ __forceinline__ void load_taps(const float* __restrict__ w, uint32_t c, uint32_t W, Ch<V> (&tap)[WT]) {
+template <int V, int WT, bool PAIRS> __device__ __forceinline__ void load_taps(const float* __restrict__ w, uint32_t c, uint32_t W, Ch<V, PAIRS> (&tap)[WT]) {
+    float x[WT][V];
+    bool whole = false;
     if constexpr (WT == 4) if (((uintptr_t)w & 15u) == 0) {
+        whole = true;
 #pragma unroll
         for (int i = 0; i < V; i++) {
             const float4 q = __ldg(reinterpret_cast<const float4*>(w) + c + i);
-            tap[3].p[i] = q.x; tap[2].p[i] = q.y; tap[1].p[i] = q.z; tap[0].p[i] = q.w;
+            x[3][i] = q.x; x[2][i] = q.y; x[1][i] = q.z; x[0][i] = q.w;
         }
-        return;
+    }
+    if (!whole) {
+#pragma unroll
+        for (int m = 0; m < WT; m++)
+#pragma unroll
+            for (int i = 0; i < V; i++) x[m][i] = m < (int)W ? __ldg(w + (size_t)(c + i) * W + (W - 1 - m)) : 0.0f;
     }
 #pragma unroll
-    for (int m = 0; m < WT; m++)
-#pragma unroll
-        for (int i = 0; i < V; i++) tap[m].p[i] = m < (int)W ? __ldg(w + (size_t)(c + i) * W + (W - 1 - m)) : 0.0f;
+    for (int m = 0; m < WT; m++) tap[m].set(x[m]);
 }
-template <int V> __device__ __forceinline__ void load_bias(const float* __restrict__ b, uint32_t c, Ch<V>& o) {
+template <int V, bool PAIRS> __device__ __forceinline__ void load_bias(const float* __restrict__ b, uint32_t c, Ch<V, PAIRS>& o) {
     float x[V];
 #pragma unroll
     for (int i = 0; i < V; i++) x[i] = b ? __ldg(b + c + i) : 0.0f;
@@ -108,7 +155,7 @@ template <int V> __device__ __forceinline__ void load_bias(const float* __restri
 }
 
 // The WT - 1 rows before row p (oldest first); row -j of a sequence is row W - 1 - j of the state it starts from, zero without one.
-template <typename T, int V, int WT, int AT> __device__ __forceinline__ void rows_before(const Conv<T>& a, const Range& r, int p, uint32_t c, Ch<V> (&x)[AT]) {
+template <typename T, int V, int WT, int AT, bool PAIRS> __device__ __forceinline__ void rows_before(const Conv<T>& a, const Range& r, int p, uint32_t c, Ch<V, PAIRS> (&x)[AT]) {
 #pragma unroll
     for (int k = 0; k + 1 < WT; k++) {
         const int q = p - (WT - 1) + k;
@@ -126,9 +173,9 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(const Conv<T> a) {
     const uint32_t c = (blockIdx.x % t.cblocks * t.lanes + threadIdx.x % t.lanes) * V, per = kThreads / t.lanes;
     if (c >= a.D) return;
     const uint32_t W = EXACT ? WT : a.W;
-    Ch<V> tap[WT], bias;
-    load_taps<V, WT>(a.w, c, W, tap);
-    load_bias<V>(a.bias, c, bias);
+    Ch<V, false> tap[WT], bias;
+    load_taps(a.w, c, W, tap);
+    load_bias(a.bias, c, bias);
     const uint64_t items = (uint64_t)a.q.n_seq * t.tiles;
     for (uint64_t it = (uint64_t)(blockIdx.x / t.cblocks) * per + threadIdx.x / t.lanes; it < items; it += (uint64_t)t.parts * per) {
         const uint32_t j = (uint32_t)(it / a.q.n_seq), s = (uint32_t)(it % a.q.n_seq);
@@ -139,8 +186,8 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(const Conv<T> a) {
         Raw<T, V> next[kAheadF] = {};                          // rows on their way
 #pragma unroll
         for (int u = 0; u < kAheadF; u++) if (p0 + u < p1) next[u].fetch(xr + (size_t)(p0 + u) * a.ldx);
-        Ch<V> x[WT + kAheadF - 1];
-        rows_before<T, V, WT, WT + kAheadF - 1>(a, r, p0, c, x);
+        Ch<V, false> x[WT + kAheadF - 1];
+        rows_before<T, V, WT>(a, r, p0, c, x);
         if (j == 0 && a.state_out && r.slot >= 0) {
             // The sequence's last W - 1 rows, which where it is shorter begin with rows of the state it started from.  The first tile writes them
             // all: it alone reads the old state, and a row from a later place than it goes to, so the pools may be one.
@@ -165,11 +212,11 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(const Conv<T> a) {
 #pragma unroll
             for (int u = 0; u < kAheadF; u++) {
                 if (ALL || p + u < p1) {
-                    Ch<V> pre = bias;
+                    Ch<V, false> pre = bias;
 #pragma unroll
                     for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) pre.add_product(tap[m], x[WT - 1 + u - m]);
                     if (a.silu) pre.silu();
-                    store<T, V>(y, pre);
+                    store(y, pre);
                 }
                 y += a.ldy;
             }
@@ -191,9 +238,9 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(const Conv<T> a) {
     const uint32_t c = (blockIdx.x % t.cblocks * t.lanes + threadIdx.x % t.lanes) * V, per = kThreads / t.lanes;
     if (c >= a.D) return;
     const int H = (EXACT ? WT : (int)a.W) - 1;             // rows of a state; the last is at [WT - 2]
-    Ch<V> tap[WT], bias;
-    load_taps<V, WT>(a.w, c, a.W, tap);
-    load_bias<V>(a.bias, c, bias);
+    Ch<V, false> tap[WT], bias;
+    load_taps(a.w, c, a.W, tap);
+    load_bias(a.bias, c, bias);
     const uint64_t stride = (uint64_t)t.parts * per;
     for (uint64_t s0 = (uint64_t)(blockIdx.x / t.cblocks) * per + threadIdx.x / t.lanes; s0 < a.q.n_seq; s0 += U * stride) {
         Range r[U];
@@ -216,13 +263,13 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(const Conv<T> a) {
         for (int u = 0; u < U; u++) {
             const bool row = r[u].len > 0;
             if (row) {
-                Ch<V> pre = bias, v;
+                Ch<V, false> pre = bias, v;
                 x[u].open(v);
                 pre.add_product(tap[0], v);
 #pragma unroll
                 for (int m = 1; m < WT; m++) if (EXACT || m <= H) { st[u][WT - 1 - m].open(v); pre.add_product(tap[m], v); }
                 if (a.silu) pre.silu();
-                store<T, V>(a.y + (size_t)r[u].first * a.ldy + c, pre);
+                store(a.y + (size_t)r[u].first * a.ldy + c, pre);
             }
             if (a.state_out && r[u].slot >= 0) {
                 T* so = a.state_out + (size_t)r[u].slot * H * a.D + c;
@@ -236,20 +283,21 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(const Conv<T> a) {
 
 // The same walk with WT - 1 rows more at a tile's end: dx_o = sum_m tap[m] dpre_{o+m} is complete once dpre_{o+WT-1} is there.
 template <typename T, int V, int WT, bool EXACT>
-__global__ void __launch_bounds__(kThreads, WT <= 4 ? 4 : 2) conv_backward_kernel(const Conv<T> a) {
+__global__ void __launch_bounds__(kThreads, WT <= 4 ? kBlocksB : 2) conv_backward_kernel(const Conv<T> a) {
     sf_chain_enter();
+    typedef Ch<V, (V > 1)> C;
     extern __shared__ float sums[];                        // [threads][V][WT + 1] where the block joins its sums
     const Tiling& t = a.t;
     const uint32_t c = (blockIdx.x % t.cblocks * t.lanes + threadIdx.x % t.lanes) * V, per = kThreads / t.lanes;
     const uint32_t W = EXACT ? WT : a.W;
-    Ch<V> dw[WT], db;
+    C dw[WT], db;
 #pragma unroll
     for (int m = 0; m < WT; m++) dw[m].zero();
     db.zero();
     if (c < a.D) {
-        Ch<V> tap[WT], bias;
-        load_taps<V, WT>(a.w, c, W, tap);
-        load_bias<V>(a.bias, c, bias);
+        C tap[WT], bias;
+        load_taps(a.w, c, W, tap);
+        load_bias(a.bias, c, bias);
         const uint64_t items = (uint64_t)a.q.n_seq * t.tiles;
         for (uint64_t it = (uint64_t)(blockIdx.x / t.cblocks) * per + threadIdx.x / t.lanes; it < items; it += (uint64_t)t.parts * per) {
             const uint32_t j = (uint32_t)(it / a.q.n_seq), s = (uint32_t)(it % a.q.n_seq);
@@ -262,8 +310,8 @@ __global__ void __launch_bounds__(kThreads, WT <= 4 ? 4 : 2) conv_backward_kerne
             Raw<T, V> nx[kAheadB] = {}, ng[kAheadB] = {};
 #pragma unroll
             for (int u = 0; u < kAheadB; u++) if (p0 + u < pe) { nx[u].fetch(xr + (size_t)(p0 + u) * a.ldx); ng[u].fetch(gr + (size_t)(p0 + u) * a.lddy); }
-            Ch<V> x[WT + kAheadB - 1], dp[WT + kAheadB - 1];
-            rows_before<T, V, WT, WT + kAheadB - 1>(a, r, p0, c, x);
+            C x[WT + kAheadB - 1], dp[WT + kAheadB - 1];
+            rows_before<T, V, WT>(a, r, p0, c, x);
 #pragma unroll
             for (int k = 0; k + 1 < WT; k++) dp[k].zero();
             xr += (size_t)(p0 + kAheadB) * a.ldx;
@@ -278,9 +326,9 @@ __global__ void __launch_bounds__(kThreads, WT <= 4 ? 4 : 2) conv_backward_kerne
                 for (int u = 0; u < kAheadB; u++) { if (ALL || p + kAheadB + u < pe) { nx[u].fetch(xr); ng[u].fetch(gr); } xr += a.ldx; gr += a.lddy; }
 #pragma unroll
                 for (int u = 0; u < kAheadB; u++) {
-                    Ch<V>& g = dp[WT - 1 + u];
+                    C& g = dp[WT - 1 + u];
                     if (a.silu) {
-                        Ch<V> pre = bias;
+                        C pre = bias;
 #pragma unroll
                         for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) pre.add_product(tap[m], x[WT - 1 + u - m]);
                         g.mul_silu_slope(pre);
@@ -296,19 +344,19 @@ __global__ void __launch_bounds__(kThreads, WT <= 4 ? 4 : 2) conv_backward_kerne
                 for (int u = 0; u < kAheadB; u++, out += a.lddx) {
                     const int o = p + u - (WT - 1);        // the row whose gradient is complete now
                     if (ALL ? a.dx == nullptr : o >= p1 || (o >= p0 ? a.dx == nullptr : !d0 || o < -H)) continue;
-                    Ch<V> d;
-                    d.zero();
+                    C d;
+                    d.set_product(tap[0], dp[u]);
 #pragma unroll
-                    for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) d.add_product(tap[m], dp[u + m]);
+                    for (int m = 1; m < WT; m++) if (EXACT || m < (int)W) d.add_product(tap[m], dp[u + m]);
                     if (!ALL && a.d_state && r.slot >= 0 && o >= len - H) {
                         Raw<T, V> v;
-                        Ch<V> e;
+                        C e;
                         v.fetch_plain(a.d_state + ((size_t)r.slot * H + (o - (len - H))) * a.D + c);
                         v.open(e);
                         d.add(e);
                     }
-                    if (ALL || o >= 0) store<T, V>(out, d);
-                    else store<T, V>(a.d_state0 + ((size_t)r.slot * H + (o + H)) * a.D + c, d);
+                    if (ALL || o >= 0) store(out, d);
+                    else store(a.d_state0 + ((size_t)r.slot * H + (o + H)) * a.D + c, d);
                 }
 #pragma unroll
                 for (int k = 0; k + 1 < WT; k++) { x[k] = x[k + kAheadB]; dp[k] = dp[k + kAheadB]; }
@@ -445,7 +493,7 @@ extern "C" int sf_seq_conv_backward_workspace(uint32_t n_seq, uint32_t max_len, 
     if (!bytes_out || n_seq > SF_SEQ_MAX_ROWS || max_len == 0 || max_len > SF_SEQ_MAX_ROWS || D == 0 || D > SF_EXPERT_MAX_D || W == 0 || W > kMaxTaps) return SF_ERR_ARG;
     const sf_sequences q = {nullptr, nullptr, nullptr, n_seq, max_len};
     uint32_t parts = 1;
-    for (uint32_t v : {1u, 2u, 4u}) parts = std::max(parts, tiling(&q, D, v, 4).parts);
+    for (uint32_t v : {1u, 2u, 4u}) parts = std::max(parts, tiling(&q, D, v, kBlocksB).parts);
     *bytes_out = (size_t)parts * D * (W + 1) * 4;
     return SF_OK;
 }
@@ -475,7 +523,7 @@ extern "C" int sf_seq_conv_backward(sf_ctx* ctx, const sf_sequences* seq, const 
                 a.q = seqs_of(seq, rows, n_slots); a.x = (const T*)x; a.ldx = ldx; a.w = w; a.bias = bias; a.D = D; a.W = W; a.silu = act == SF_ACT_SILU;
                 a.state_in = (const T*)state_in; a.dy = (const T*)dy; a.lddy = lddy; a.d_state = (const T*)d_state; a.d_state0 = (T*)d_state_in_out;
                 a.dx = (T*)dx_out; a.lddx = lddx; a.st = ctx->d_state;
-                a.t = tiling(seq, D, V, 4);
+                a.t = tiling(seq, D, V, kBlocksB);
                 if (sums && (!workspace || workspace_bytes < (size_t)a.t.parts * D * (W + 1) * 4)) return (int)SF_ERR_ARG;
                 a.parts = sums ? (float*)workspace : nullptr;
                 SF_CUDA(sf_launch_chained(conv_backward_kernel<T, V, WT, decltype(exact)::value>, a.t.cblocks * a.t.parts, kThreads, sums ? kThreads * (WT + 1) * V * 4 : 0,
