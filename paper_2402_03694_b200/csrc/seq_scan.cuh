@@ -8,8 +8,12 @@
 // States, decays and sums are fp32.
 //
 // Mapping: a warp owns CH = 128 / SL channels of one sequence; its lanes are CL = 32 / SL groups of 4 channels times SL groups of 4 states
-// (SL the power of two with 4 SL >= N), so a thread holds 4 x 4 states and the sums over states and over channels are both half done in registers.  Rows go by tiles:
-// steps, inputs times steps and B, C are staged in shared memory of the warp's own (softplus once an element), nothing waits for another warp.
+// (SL a power of two with 4 SL >= N), so a thread holds 4 x 4 states, the sums over states and over channels are both half done in registers, and what a lane
+// reads of a row (steps, inputs, B, C) serves 16 states.  Rows go by tiles that the warp stages in shared memory of its own (softplus once an element) while the
+// next tile's pieces are copied ahead.  In the forward pass nothing waits for another warp; the backward pass joins dB and dC over a block.
+// Bound: an exponential a state, 16 a clock and SM, at N = 16 three times the time of the bytes.  4096 flows of up to 128 x 256 bf16 take 414 us (function unit 301),
+// 64 x 512 x 512 with gradients 580 us: 144 forward, 441 backward (325 instructions a row and warp, eight warps an SM).  A thread per channel would read B and C 16 states at
+// a time for one channel and need 31 exchanges a row for dB and dC; 8 x 2 or 2 x 8 states a thread read as much and exchange more.
 #pragma once
 #include <algorithm>
 #include "seq_common.cuh"
@@ -93,7 +97,7 @@ __device__ __forceinline__ f2 decay2(f2 delta, f2 A) {
 // J: channels of a lane (4; the forward pass also 2, where warps are few)
 template <int SL, int J = 4> struct Shape {
     static constexpr int CL = 32 / SL, CH = J * CL, NP = 4 * SL;               // channel lanes, channels of a warp, states with those that fill up
-    static constexpr int K = J == 2 ? 16 : (SL == 1 ? 4 : 8);                  // rows of a tile of the forward pass (a multiple of kEvery, or kEvery of it)
+    static constexpr int K = J == 2 ? 16 : (SL == 1 ? 4 : 8);                  // rows of a tile of the forward pass (kEvery divides them, or they divide it)
 };
 
 // What a warp works on: sequence, group, first of its channels within the group and of all, and how many it has (none: nothing to do)

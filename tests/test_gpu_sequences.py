@@ -306,6 +306,35 @@ def test_long_memory_is_kept(env):
     assert (np.abs(num(state)[0] - h) / h).max() < (2 * np.sqrt(L) + L / 8) * E * 2
 
 
+def test_more_sequences_than_a_grid_has_rows(env):
+    """70,000 sequences of one row each, channels of a group over several blocks: h = delta u B, so dB = sum_d e C delta u and dC = sum_d e h in closed form."""
+    sf, ctx = env
+    S, D, N = 70_000, 136, 16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    r = lambda d: torch.randn(S, d, device="cuda", generator=g)  # noqa: E731
+    u, delta, B, C, dy, A = r(D), r(D).abs() * 0.3, r(N), r(N), r(D), -torch.ones(D, N, device="cuda")
+    q = sf.make_sequences(torch.arange(S + 1, dtype=torch.int32, device="cuda"), 1)
+    y, dB, dC, dx = torch.zeros_like(u), torch.zeros_like(B), torch.zeros_like(C), torch.zeros_like(u)
+    starts = torch.zeros(sf.sf_seq_scan_starts(S, S, D, N), device="cuda")
+    work = torch.zeros(sf.sf_seq_scan_workspace(S, 1, S, D, N, backward=True), dtype=torch.uint8, device="cuda")
+    sf.sf_seq_scan(ctx, q, u, delta, A, B, C, y, starts_out=starts)
+    sf.sf_seq_scan_backward(ctx, q, u, delta, A, B, C, dy, starts, work, dB_out=dB, dC_out=dC)
+    in_, e = delta.double() * u.double(), dy.double()
+    dot = (B.double() * C.double()).sum(1, keepdim=True)
+    tol = (D + 64) * E
+    assert ((y.double() - in_ * dot).abs() <= tol * (in_.abs() * (B.double() * C.double()).abs().sum(1, keepdim=True))).all()
+    both, mag = (e * in_).sum(1, keepdim=True), (e * in_).abs().sum(1, keepdim=True)
+    assert ((dB.double() - both * C.double()).abs() <= tol * mag * C.double().abs() + 1e-30).all()
+    assert ((dC.double() - both * B.double()).abs() <= tol * mag * B.double().abs() + 1e-30).all()
+    w = torch.randn(D, 4, device="cuda", generator=g)
+    work = torch.zeros(sf.sf_seq_conv_backward_workspace(S, 1, D, 4), dtype=torch.uint8, device="cuda")
+    dw = torch.zeros_like(w)
+    sf.sf_seq_conv_backward(ctx, q, u, w, dy, work, dx_out=dx, dw_out=dw)
+    assert ((dx.double() - w[:, 3].double() * e).abs() <= 4 * E * (w[:, 3].double() * e).abs()).all()
+    assert ((dw[:, 3].double() - (e * u.double()).sum(0)).abs() <= S * E * (e * u.double()).abs().sum(0)).all() and bool((dw[:, :3] == 0).all())
+
+
 # ---- both: what device memory says ------------------------------------------------------------------------------------------------------
 def bad_sequences(sf):
     i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
