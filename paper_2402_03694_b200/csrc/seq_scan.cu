@@ -131,23 +131,38 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
 #pragma unroll
             for (int i = 0; i < Sh::ST::I; i++) ns.take(i, sh.way[3 * I + i][lane]);
         }
+        if constexpr (VV == 1) {                           // single elements, two at a time
+            static_assert(I % 2 == 0, "every lane has an even number of single elements");
 #pragma unroll
-        for (int i = 0; i < I; i++) {
-            const int t = pc.t(i), c = pc.c(i);
-            if (t >= K) continue;
-            float d[VV], u[VV];
-            cu[i] = nu[i];
-            if (!ENDS) cz[i] = nz[i];
-            open<T, VV>(nd[i], d);
-            open<T, VV>(nu[i], u);
-            if constexpr (VV == 1) {
-                float unused;
-                d[0] += sh.bias[c];
-                if (a.softplus) d[0] = softplus_of(d[0], unused);
-                if (ENDS) { if (t >= rows) d[0] = 0.0f; steps[i][0] = add2(steps[i][0], pack2(d[0], 0.0f)); }
-                sh.step[t][c] = d[0];
-                sh.in[t][c] = d[0] * u[0];
-            } else {
+            for (int i = 0; i < I; i += 2) {
+                const int t0_ = pc.t(i), c0 = pc.c(i), t1 = pc.t(i + 1), c1 = pc.c(i + 1);
+                float d0[1], d1[1], u0[1], u1[1];
+                open<T, 1>(nd[i], d0); open<T, 1>(nd[i + 1], d1); open<T, 1>(nu[i], u0); open<T, 1>(nu[i + 1], u1);
+                cu[i] = nu[i]; cu[i + 1] = nu[i + 1];
+                if (!ENDS) { cz[i] = nz[i]; cz[i + 1] = nz[i + 1]; }
+                f2 x = add2(pack2(d0[0], d1[0]), pack2(sh.bias[c0], sh.bias[c1])), unused;
+                if (a.softplus) x = softplus2(x, unused);
+                float p, q;
+                unpack2(x, p, q);
+                if (ENDS) {
+                    if (t0_ >= rows) p = 0.0f;
+                    if (t1 >= rows) q = 0.0f;
+                    steps[i][0] = add2(steps[i][0], pack2(p, 0.0f)); steps[i + 1][0] = add2(steps[i + 1][0], pack2(q, 0.0f));
+                }
+                sh.step[t0_][c0] = p; sh.step[t1][c1] = q;
+                unpack2(mul2(pack2(p, q), pack2(u0[0], u1[0])), p, q);
+                sh.in[t0_][c0] = p; sh.in[t1][c1] = q;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < I; i++) {
+                const int t = pc.t(i), c = pc.c(i);
+                if (t >= K) continue;
+                float d[VV], u[VV];
+                cu[i] = nu[i];
+                if (!ENDS) cz[i] = nz[i];
+                open<T, VV>(nd[i], d);
+                open<T, VV>(nu[i], u);
 #pragma unroll
                 for (int e = 0; e < VV; e += 4) {
                     const float4 b4 = *reinterpret_cast<const float4*>(&sh.bias[c + e]);
@@ -197,19 +212,32 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
         }
         __syncwarp();
         if constexpr (!ENDS) {
+            if constexpr (VV == 1) {
 #pragma unroll
-            for (int i = 0; i < I; i++) {
-                const int t = pc.t(i), c = pc.c(i);
-                if (c >= (int)have || t >= rows) continue;
-                float u[VV], z[VV], y[VV];
-                open<T, VV>(cu[i], u);
-                if (a.z) open<T, VV>(cz[i], z);
-                if constexpr (VV == 1) {
-                    y[0] = sh.skip[c] * u[0];
+                for (int i = 0; i < I; i += 2) {
+                    float v[2], z[2], u[1];
 #pragma unroll
-                    for (int l = 0; l < SL; l++) y[0] += sh.y[t][l * Sh::PY + c];
-                    if (a.z) y[0] *= z[0] * sigmoid(z[0]);
-                } else {
+                    for (int k = 0; k < 2; k++) {
+                        const int t = pc.t(i + k), c = pc.c(i + k);
+                        open<T, 1>(cu[i + k], u);
+                        if (a.z) { float w[1]; open<T, 1>(cz[i + k], w); z[k] = w[0]; }
+                        v[k] = sh.skip[c] * u[0];
+#pragma unroll
+                        for (int l = 0; l < SL; l++) v[k] += sh.y[t][l * Sh::PY + c];
+                    }
+                    if (a.z) { const f2 zz = pack2(z[0], z[1]); unpack2(mul2(pack2(v[0], v[1]), mul2(zz, sigmoid2(zz))), v[0], v[1]); }
+#pragma unroll
+                    for (int k = 0; k < 2; k++)
+                        if (pc.c(i + k) < (int)have && pc.t(i + k) < rows) { const float o[1] = {v[k]}; store_word<T, 1>(py + P::step(i + k, a.ldy), o); }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < I; i++) {
+                    const int t = pc.t(i), c = pc.c(i);
+                    if (c >= (int)have || t >= rows) continue;
+                    float u[VV], z[VV], y[VV];
+                    open<T, VV>(cu[i], u);
+                    if (a.z) open<T, VV>(cz[i], z);
 #pragma unroll
                     for (int e = 0; e < VV; e += 4) {
                         const ulonglong2 k2 = *reinterpret_cast<const ulonglong2*>(&sh.skip[c + e]);
@@ -225,8 +253,8 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
                         }
                         unpack2(v, y[e], y[e + 1]); unpack2(w, y[e + 2], y[e + 3]);
                     }
+                    store_word<T, VV>(py + P::step(i, a.ldy), y);
                 }
-                store_word<T, VV>(py + P::step(i, a.ldy), y);
             }
             py += K * a.ldy;
         }

@@ -15,20 +15,20 @@ template <typename T, int SL, int VV> struct __align__(16) Backward {
     typedef Pieces<K, S::CH, VV> P;
     typedef States<T, VV, K, S::NP> ST;
     static constexpr int PX = S::CH + 4, PY = S::CH + (SL == 1 ? 0 : (SL == 2 ? 16 : (SL == 4 ? 8 : 4))), PT = SL * PY + 4;
-    static constexpr int ON_WAY = VV > 1 ? 4 * P::I + ST::I + 4 : 1;
+    static constexpr int ON_WAY = VV > 1 ? 4 * P::I + ST::I : 1;
     float step[K][PX], u[K][PX], e[K][PX];                 // delta; u; dout silu(z)
     float dstep[K][PX], dgate[K][PX];                      // d delta / d raw; dout silu'(z)
     float bc[2][K][S::NP];                                 // B, C
     float s1[R][PT], s2[R][PT], y[R][PT];                  // sum g B; sum (a g) h_{t-1} A; sum C h
     float dbc[R][2][S::CL][S::NP];                         // dB, dC
-    float4 start[K / R][4][32];                            // the states before rows 0 and R, every lane its own
+    float4 start[K / R][4][32];                            // the states before rows 0 and R by channel, every lane its own
     uint4 way[ON_WAY][32];                                 // the next tile's pieces on their way, every lane its own
     float bias[S::CH], skip[S::CH];
 };
 
-// Asks for a tile's pieces: steps, gradients of the outputs, gates, and (not ENDS) inputs and the state before the tile.  Whole pieces only; others are read when staged.
+// Asks for a tile's pieces: steps, gradients of the outputs, gates, and (not ENDS) inputs.  Whole pieces only; others are read when staged.
 template <typename T, int SL, int VV, bool ENDS>
-__device__ __forceinline__ void ask(const Scan& a, Backward<T, SL, VV>& sh, size_t row0, size_t start, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
+__device__ __forceinline__ void ask(const Scan& a, Backward<T, SL, VV>& sh, size_t row0, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
     if constexpr (VV > 1) {
         typedef Backward<T, SL, VV> Sh;
         typedef typename Sh::P P;
@@ -51,14 +51,18 @@ __device__ __forceinline__ void ask(const Scan& a, Backward<T, SL, VV>& sh, size
             const T* p = Sh::ST::template piece<T>(a, i, row0, g * a.N, rows, lane, there);
             copy16(&sh.way[4 * P::I + i][lane], p, there);
         }
-        if (!ENDS) {
-            const int cl = lane / SL, sl = lane % SL;
+    }
+}
+// The state before a tile into start[0], likewise
+template <typename T, int SL, int VV>
+__device__ __forceinline__ void ask_start(const Scan& a, Backward<T, SL, VV>& sh, size_t start, uint32_t ch0, uint32_t have, int lane) {
+    if constexpr (VV > 1) {
+        const int cl = lane / SL, sl = lane % SL;
+        const float* p = a.starts + start * a.D * a.N;
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const bool there = cl * 4 + j < (int)have && sl * 4 < (int)a.N;
-                const float* p = a.starts + start * a.D * a.N;
-                copy16(&sh.way[4 * P::I + Sh::ST::I + j][lane], there ? p + (size_t)(ch0 + cl * 4 + j) * a.N + sl * 4 : p, there);
-            }
+        for (int j = 0; j < 4; j++) {
+            const bool there = cl * 4 + j < (int)have && sl * 4 < (int)a.N;
+            copy16(&sh.start[0][j][lane], there ? p + (size_t)(ch0 + cl * 4 + j) * a.N + sl * 4 : p, there);
         }
     }
 }
@@ -96,59 +100,69 @@ __device__ __forceinline__ void stage(const Scan& a, Backward<T, SL, VV>& sh, si
         }
         ns.fetch_all(a, row0, g * a.N, rows, lane);
     }
+    constexpr int AT = VV == 1 ? 2 : 1, W = VV * AT;       // single elements two at a time
+    static_assert(P::I % AT == 0, "every lane has an even number of single elements");
 #pragma unroll
-    for (int i = 0; i < P::I; i++) {
-        const int t = pc.t(i), c = pc.c(i);
-        if (t >= K) continue;
-        const bool there = t < rows && c < (int)have;
-        float d[VV], u[VV], z[VV], o[VV];
-        open<T, VV>(nd[i], d);
-        if (!ENDS) open<T, VV>(nu[i], u);
-        if (a.z) open<T, VV>(nz[i], z);
-        open<T, VV>(ng[i], o);
-        float ds[VV], dg[VV];
-        if constexpr (VV == 1) {
-            float x;                                       // exp(-|raw|): the slope of softplus is 1 / (1 + x), or x / (1 + x) left of 0
-            const float raw = d[0] + sh.bias[c], sg = a.z ? sigmoid(z[0]) : 1.0f;
-            d[0] = a.softplus ? softplus_of(raw, x) : raw;
-            ds[0] = a.softplus ? (raw >= 0.0f ? 1.0f : x) * rcp(1.0f + x) : 1.0f;
-            dg[0] = a.z ? o[0] * sg * fmaf(z[0], 1.0f - sg, 1.0f) : 0.0f;
-            if (a.z) o[0] *= z[0] * sg;
-        } else {
+    for (int i = 0; i < P::I; i += AT) {
+        if (pc.t(i) >= K) continue;
+        float d[W], u[W], z[W], o[W], ds[W], dg[W];
+        f2 bias[W / 2];
+        auto opened = [&](const Piece<T, VV>* n, float (&x)[W]) {
 #pragma unroll
-            for (int e = 0; e < VV; e += 2) {
-                const f2 one = dup2(1.0f);
-                f2 raw = add2(pack2(d[e], d[e + 1]), *reinterpret_cast<const f2*>(&sh.bias[c + e])), x, v = raw, w = one;
-                if (a.softplus) {
-                    v = softplus2(raw, x);
-                    float p, q, r0, r1;
-                    unpack2(add2(x, one), p, q);
-                    unpack2(raw, r0, r1);
-                    if (!ENDS) { float x0, x1; unpack2(x, x0, x1); w = mul2(pack2(r0 >= 0.0f ? 1.0f : x0, r1 >= 0.0f ? 1.0f : x1), pack2(rcp(p), rcp(q))); }
-                }
-                unpack2(v, d[e], d[e + 1]);
-                unpack2(w, ds[e], ds[e + 1]);
-                if (a.z) {
-                    const f2 zz = pack2(z[e], z[e + 1]), oo = pack2(o[e], o[e + 1]), sg = sigmoid2(zz), os = mul2(oo, sg);
-                    if (!ENDS) unpack2(mul2(os, fma2(zz, fma2(sg, dup2(-1.0f), one), one)), dg[e], dg[e + 1]);
-                    unpack2(mul2(os, zz), o[e], o[e + 1]);
-                }
-            }
-        }
-        if (!there) {
+            for (int k = 0; k < AT; k++) {
+                float v[VV];
+                open<T, VV>(n[i + k], v);
 #pragma unroll
-            for (int e = 0; e < VV; e++) d[e] = o[e] = 0.0f;
-        }
-        auto put = [&](float* p, const float (&v)[VV]) {
-            if constexpr (VV == 1) p[0] = v[0];
-            else {
-#pragma unroll
-                for (int e = 0; e < VV; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                for (int e = 0; e < VV; e++) x[k * VV + e] = v[e];
             }
         };
-        put(&sh.step[t][c], d);
-        put(&sh.e[t][c], o);
-        if (!ENDS) { put(&sh.u[t][c], u); put(&sh.dstep[t][c], ds); if (a.z) put(&sh.dgate[t][c], dg); }
+        opened(nd, d);
+        if (!ENDS) opened(nu, u);
+        if (a.z) opened(nz, z);
+        opened(ng, o);
+        if constexpr (VV == 1) bias[0] = pack2(sh.bias[pc.c(i)], sh.bias[pc.c(i + 1)]);
+        else {
+#pragma unroll
+            for (int e = 0; e < VV; e += 2) bias[e / 2] = *reinterpret_cast<const f2*>(&sh.bias[pc.c(i) + e]);
+        }
+#pragma unroll
+        for (int e = 0; e < W; e += 2) {
+            const f2 one = dup2(1.0f);
+            f2 raw = add2(pack2(d[e], d[e + 1]), bias[e / 2]), x, v = raw, w = one;
+            if (a.softplus) {                              // x is exp(-|raw|): the slope of softplus is 1 / (1 + x), or x / (1 + x) left of 0
+                v = softplus2(raw, x);
+                float p, q, r0, r1;
+                unpack2(add2(x, one), p, q);
+                unpack2(raw, r0, r1);
+                if (!ENDS) { float x0, x1; unpack2(x, x0, x1); w = mul2(pack2(r0 >= 0.0f ? 1.0f : x0, r1 >= 0.0f ? 1.0f : x1), pack2(rcp(p), rcp(q))); }
+            }
+            unpack2(v, d[e], d[e + 1]);
+            unpack2(w, ds[e], ds[e + 1]);
+            if (a.z) {
+                const f2 zz = pack2(z[e], z[e + 1]), oo = pack2(o[e], o[e + 1]), sg = sigmoid2(zz), os = mul2(oo, sg);
+                if (!ENDS) unpack2(mul2(os, fma2(zz, fma2(sg, dup2(-1.0f), one), one)), dg[e], dg[e + 1]);
+                unpack2(mul2(os, zz), o[e], o[e + 1]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < AT; k++) {
+            const int t = pc.t(i + k), c = pc.c(i + k);
+            const bool there = t < rows && c < (int)have;
+            if (!there) {
+#pragma unroll
+                for (int e = 0; e < VV; e++) d[k * VV + e] = o[k * VV + e] = 0.0f;
+            }
+            auto put = [&](float* p, const float (&v)[W]) {
+                if constexpr (VV == 1) p[0] = v[k];
+                else {
+#pragma unroll
+                    for (int e = 0; e < VV; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                }
+            };
+            put(&sh.step[t][c], d);
+            put(&sh.e[t][c], o);
+            if (!ENDS) { put(&sh.u[t][c], u); put(&sh.dstep[t][c], ds); if (a.z) put(&sh.dgate[t][c], dg); }
+        }
     }
     ns.stage(&sh.bc[0][0][0], lane);
 }
@@ -219,7 +233,7 @@ __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
     channel_params<T, SL, VV>(a, sh, ch0, have, lane);
     __syncwarp();
     const uint32_t tiles = (t_end - t_begin + K - 1) / K;
-    auto next = [&](uint32_t tile) { const uint32_t t = t_begin + tile * K; ask<T, SL, VV, true>(a, sh, (size_t)r.first + t, 0, ch0, have, g, (int)min((uint32_t)K, t_end - t), lane); };
+    auto next = [&](uint32_t tile) { const uint32_t t = t_begin + tile * K; ask<T, SL, VV, true>(a, sh, (size_t)r.first + t, ch0, have, g, (int)min((uint32_t)K, t_end - t), lane); };
     next(tiles - 1);
     for (uint32_t tile = tiles; tile-- > 0;) {
         const uint32_t t0 = t_begin + tile * K;
@@ -297,9 +311,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
         const uint32_t tiles = t_end > t_begin ? (t_end - t_begin + K - 1) / K : 0;
         auto next = [&](uint32_t tile) {
             const uint32_t t = t_begin + tile * K;
-            ask<T, SL, VV, false>(a, sh, (size_t)r.first + t, start_index(r.first, s, t), ch0, have, g, (int)min((uint32_t)K, t_end - t), lane);
+            ask<T, SL, VV, false>(a, sh, (size_t)r.first + t, ch0, have, g, (int)min((uint32_t)K, t_end - t), lane);
         };
-        if (tiles) next(tiles - 1);
+        auto next_start = [&](uint32_t tile) { ask_start<T, SL, VV>(a, sh, start_index(r.first, s, t_begin + tile * K), ch0, have, lane); };
+        if (tiles) { next(tiles - 1); next_start(tiles - 1); }
         load_states(G, whole ? (a.d_state && r.slot >= 0 ? a.d_state + (size_t)r.slot * DN : nullptr) : a.part_state + ((size_t)s * a.parts + part) * DN, a, ch0, have, cl, sl, 1.0f);
         for (uint32_t tile = tiles; tile-- > 0;) {
             const uint32_t t0 = t_begin + tile * K;
@@ -307,26 +322,25 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
             const size_t row0 = (size_t)r.first + t0;
             stage<T, SL, VV, false>(a, sh, row0, ch0, have, g, rows, lane);
             f2 h[2][4];
-            if constexpr (VV > 1) {
-#pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    const float4 x = *reinterpret_cast<const float4*>(&sh.way[Sh::ON_WAY - 4 + 2 * j][lane]), y = *reinterpret_cast<const float4*>(&sh.way[Sh::ON_WAY - 3 + 2 * j][lane]);
-                    h[j][0] = pack2(x.x, y.x); h[j][1] = pack2(x.y, y.y); h[j][2] = pack2(x.z, y.z); h[j][3] = pack2(x.w, y.w);
-                }
-            } else load_states(h, a.starts + start_index(r.first, s, t0) * DN, a, ch0, have, cl, sl, 1.0f);
             auto keep = [&](int q) {
 #pragma unroll
-                for (int j = 0; j < 2; j++)
+                for (int j = 0; j < 2; j++) {
+                    float x[4], y[4];
 #pragma unroll
-                    for (int n = 0; n < 4; n += 2) *reinterpret_cast<ulonglong2*>(&sh.start[q][2 * j + n / 2][lane]) = make_ulonglong2(h[j][n], h[j][n + 1]);
+                    for (int n = 0; n < 4; n++) unpack2(h[j][n], x[n], y[n]);
+                    sh.start[q][2 * j][lane] = make_float4(x[0], x[1], x[2], x[3]);
+                    sh.start[q][2 * j + 1][lane] = make_float4(y[0], y[1], y[2], y[3]);
+                }
             };
             auto take = [&](f2 (&v)[2][4], int q) {
 #pragma unroll
-                for (int j = 0; j < 2; j++)
-#pragma unroll
-                    for (int n = 0; n < 4; n += 2) { const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&sh.start[q][2 * j + n / 2][lane]); v[j][n] = w.x; v[j][n + 1] = w.y; }
+                for (int j = 0; j < 2; j++) {
+                    const float4 x = sh.start[q][2 * j][lane], y = sh.start[q][2 * j + 1][lane];
+                    v[j][0] = pack2(x.x, y.x); v[j][1] = pack2(x.y, y.y); v[j][2] = pack2(x.z, y.z); v[j][3] = pack2(x.w, y.w);
+                }
             };
-            keep(0);
+            if constexpr (VV > 1) take(h, 0);
+            else { load_states(h, a.starts + start_index(r.first, s, t0) * DN, a, ch0, have, cl, sl, 1.0f); keep(0); }
             if (tile) next(tile - 1);                      // (what this lane had on its way it has read)
             __syncwarp();
 #pragma unroll
@@ -344,6 +358,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
             for (int q = K / R - 1; q >= 0; q--) {
                 f2 al[R][2][4], hs[R + 1][2][4];           // decays; states before the rows and after them
                 take(hs[0], q);
+                if (q == 0 && tile) next_start(tile - 1);  // (this lane's is in registers now)
 #pragma unroll
                 for (int t = 0; t < R; t++) {
                     const int tt = R * q + t;
