@@ -53,16 +53,20 @@ __device__ __forceinline__ void ask(const Scan& a, Backward<T, SL, VV>& sh, size
         }
     }
 }
-// The state before a tile into start[0], likewise
+// The state before a tile into start[0], likewise; four by four where they lie so
 template <typename T, int SL, int VV>
 __device__ __forceinline__ void ask_start(const Scan& a, Backward<T, SL, VV>& sh, size_t start, uint32_t ch0, uint32_t have, int lane) {
-    if constexpr (VV > 1) {
-        const int cl = lane / SL, sl = lane % SL;
-        const float* p = a.starts + start * a.D * a.N;
+    const int cl = lane / SL, sl = lane % SL;
+    const float* p = a.starts + start * a.D * a.N;
+    const bool fours = VV > 1 || (a.n4 && ((uintptr_t)p & 15u) == 0);
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const bool there = cl * 4 + j < (int)have && sl * 4 < (int)a.N;
-            copy16(&sh.start[0][j][lane], there ? p + (size_t)(ch0 + cl * 4 + j) * a.N + sl * 4 : p, there);
+    for (int j = 0; j < 4; j++) {
+        const bool there = cl * 4 + j < (int)have;
+        const float* q = p + (size_t)(ch0 + cl * 4 + j) * a.N + sl * 4;
+        if (fours) copy16(&sh.start[0][j][lane], there && sl * 4 < (int)a.N ? q : p, there && sl * 4 < (int)a.N);
+        else {
+#pragma unroll
+            for (int n = 0; n < 4; n++) copy4(&reinterpret_cast<float*>(&sh.start[0][j][lane])[n], there && sl * 4 + n < (int)a.N ? q + n : p, there && sl * 4 + n < (int)a.N);
         }
     }
 }
@@ -75,8 +79,8 @@ __device__ __forceinline__ void stage(const Scan& a, Backward<T, SL, VV>& sh, si
     const P pc(lane);
     Piece<T, VV> nd[P::I], nu[P::I], nz[P::I], ng[P::I];
     typename Sh::ST ns;
+    copies_done();
     if constexpr (VV > 1) {
-        copies_done();
 #pragma unroll
         for (int i = 0; i < P::I; i++) {
             nd[i].w = sh.way[i][lane];
@@ -339,8 +343,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
                     v[j][0] = pack2(x.x, y.x); v[j][1] = pack2(x.y, y.y); v[j][2] = pack2(x.z, y.z); v[j][3] = pack2(x.w, y.w);
                 }
             };
-            if constexpr (VV > 1) take(h, 0);
-            else { load_states(h, a.starts + start_index(r.first, s, t0) * DN, a, ch0, have, cl, sl, 1.0f); keep(0); }
+            take(h, 0);
             if (tile) next(tile - 1);                      // (what this lane had on its way it has read)
             __syncwarp();
 #pragma unroll
