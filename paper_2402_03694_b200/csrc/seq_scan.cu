@@ -7,10 +7,10 @@ using namespace sfscan;
 
 // What a warp keeps in shared memory.  Sums over states are left as one part a state lane and joined where the row is written.  Rows are spaced so that
 // the 16-byte accesses of eight lanes meet no common bank: PX floats a row of channels, PY a part, PT the parts of a row.
-template <typename T, int SL, int VV, int J> struct __align__(16) Forward {
+template <typename T, int SL, int VV, int PB, int J> struct __align__(16) Forward {
     typedef Shape<SL, J> S;
     typedef Pieces<S::K, S::CH, VV> P;
-    typedef States<T, VV, S::K, S::NP> ST;
+    typedef States<T, PB, S::K, S::NP> ST;
     static constexpr int PX = S::CH + 4, PY = S::CH + (SL == 1 ? 0 : (SL == 2 ? 16 : (SL == 4 ? 8 : 4))), PT = SL * PY + 4;
     float step[S::K][PX], in[S::K][PX];                    // delta; delta u
     float bc[2][S::K][S::NP];                              // B, C
@@ -21,7 +21,7 @@ template <typename T, int SL, int VV, int J> struct __align__(16) Forward {
 
 // The scan of a sequence, or of one part of it (blockIdx.y): from the state that `part_state` holds where sequences go in parts.
 // ENDS: only the state at the part's end, from zero, and the sum of the part's steps.
-template <typename T, int SL, int VV, bool ENDS, int J>
+template <typename T, int SL, int VV, int PB, bool ENDS, int J>
 __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     sf_chain_enter();
     typedef Shape<SL, J> S;
@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     constexpr int JP = J / 2;                              // pairs of channels of a lane
     constexpr int K = S::K, CH = S::CH, NP = S::NP, I = P::I;
     extern __shared__ __align__(16) unsigned char shared[];
-    typedef Forward<T, SL, VV, J> Sh;
+    typedef Forward<T, SL, VV, PB, J> Sh;
     Sh& sh = reinterpret_cast<Sh*>(shared)[threadIdx.x / 32];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
     const Item it = item_of(a, CH);
@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
     if (ENDS ? t_begin >= r.len : (part && t_begin >= r.len)) return;
     // rows on their way while others are worked on
     Piece<T, VV> nd[I], nu[I], nz[I];
-    States<T, VV, K, NP> ns;
+    States<T, PB, K, NP> ns;
     const P pc(lane);
     const size_t at0 = (size_t)r.first + t_begin + pc.lt;
     const T* pd = (const T*)a.delta + at0 * a.lddelta + ch0 + pc.lc; const T* pu = (const T*)a.u + at0 * a.ldu + ch0 + pc.lc; const T* pz = (const T*)a.z + at0 * a.ldz + ch0 + pc.lc;
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
                 if (!ENDS && a.z) nz[i] = fetch<T, VV>(pz, P::step(i, a.ldz), there);
             }
         }
-        if constexpr (VV > 1) {
+        if constexpr (Sh::ST::WHOLE) {
 #pragma unroll
             for (int i = 0; i < Sh::ST::I; i++) {
                 bool there;
@@ -128,8 +128,10 @@ __global__ void __launch_bounds__(32 * kWarps, 4) scan_kernel(const Scan a) {
             copies_done();
 #pragma unroll
             for (int i = 0; i < I; i++) { nd[i].w = sh.way[i][lane]; nu[i].w = sh.way[I + i][lane]; if (!ENDS && a.z) nz[i].w = sh.way[2 * I + i][lane]; }
+            if constexpr (Sh::ST::WHOLE) {
 #pragma unroll
-            for (int i = 0; i < Sh::ST::I; i++) ns.take(i, sh.way[3 * I + i][lane]);
+                for (int i = 0; i < Sh::ST::I; i++) ns.take(i, sh.way[3 * I + i][lane]);
+            }
         }
         if constexpr (VV == 1) {                           // single elements, two at a time
             static_assert(I % 2 == 0, "every lane has an even number of single elements");
@@ -435,27 +437,31 @@ extern "C" int sf_seq_scan(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_r
     return by_type(in->dtype, [&](auto zero) {
         typedef decltype(zero) T;
         return by_states(p.sl, [&](auto lanes) {
-            constexpr int SL = decltype(lanes)::value, VV = 16 / (int)sizeof(T);
+            constexpr int SL = decltype(lanes)::value;
             if (seq->max_len == 1 && !starts_out) {
                 const bool v4 = in->N % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16) && aligned(in->A, 16);
                 return launch(v4 ? step_kernel<T, SL, true> : step_kernel<T, SL, false>, (uint32_t)blocks, 32 * kWarps, 0, st, a);
             }
             // Where whole sequences leave half of the machine idle and are too many to go in parts: two channels a lane, twice the warps
             // (64 sequences of 512 rows x 512: 145 us with four channels a lane, 135 with two; 4096 of up to 128 x 256, where warps are many: 414 with four)
-            if constexpr (SL == 4) if (vec && !p.split && (uint64_t)seq->n_seq * in->G * p.cwarps < (uint64_t)SF_NUM_SMS_DEFAULT * 10) {
-                set_warps(a, (a.per + 15) / 16);
-                const uint64_t b = ((uint64_t)seq->n_seq * in->G * a.cwarps + kWarps - 1) / kWarps;
-                return launch(scan_kernel<T, SL, VV, false, 2>, dim3((uint32_t)b, 1), 32 * kWarps, sizeof(Forward<T, SL, VV, 2>) * kWarps, st, a);
-            }
-            const size_t smem = (vec ? sizeof(Forward<T, SL, VV, 4>) : sizeof(Forward<T, SL, 1, 4>)) * kWarps;
-            if (p.split) {
-                a.part_state = (float*)workspace;
-                a.part_step = (float*)((char*)workspace + sf_align256((size_t)seq->n_seq * p.parts * in->D * in->N * 4));
-                int e = launch(vec ? scan_kernel<T, SL, VV, true, 4> : scan_kernel<T, SL, 1, true, 4>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, smem, st, a);
-                if (e == SF_OK) e = launch(parts_kernel<false>, dim3((uint32_t)(((uint64_t)in->D * in->N + 255) / 256), seq->n_seq), 256, 0, st, a);
-                if (e != SF_OK) return e;
-            }
-            return launch(vec ? scan_kernel<T, SL, VV, false, 4> : scan_kernel<T, SL, 1, false, 4>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, smem, st, a);
+            const bool two = SL == 4 && vec && !p.split && (uint64_t)seq->n_seq * in->G * p.cwarps < (uint64_t)SF_NUM_SMS_DEFAULT * 10;
+            return by_width<T, SL>(vec, states_fit(in), [&](auto v, auto pb) {
+                constexpr int VV = decltype(v)::value, PB = decltype(pb)::value;
+                if constexpr (SL == 4 && VV > 1) if (two) {
+                    set_warps(a, (a.per + 15) / 16);
+                    const uint64_t b = ((uint64_t)seq->n_seq * in->G * a.cwarps + kWarps - 1) / kWarps;
+                    return launch(scan_kernel<T, SL, VV, PB, false, 2>, dim3((uint32_t)b, 1), 32 * kWarps, sizeof(Forward<T, SL, VV, PB, 2>) * kWarps, st, a);
+                }
+                const size_t smem = sizeof(Forward<T, SL, VV, PB, 4>) * kWarps;
+                if (p.split) {
+                    a.part_state = (float*)workspace;
+                    a.part_step = (float*)((char*)workspace + sf_align256((size_t)seq->n_seq * p.parts * in->D * in->N * 4));
+                    int e = launch(scan_kernel<T, SL, VV, PB, true, 4>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, smem, st, a);
+                    if (e == SF_OK) e = launch(parts_kernel<false>, dim3((uint32_t)(((uint64_t)in->D * in->N + 255) / 256), seq->n_seq), 256, 0, st, a);
+                    if (e != SF_OK) return e;
+                }
+                return launch(scan_kernel<T, SL, VV, PB, false, 4>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, smem, st, a);
+            });
         });
     });
 }

@@ -150,8 +150,10 @@ __device__ __forceinline__ void copy4(void* to, const void* from, bool there) {
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // B and C of a tile on their way (PV states at once, pieces of B first); stage writes them as [2][K][NP], zeros where there is nothing.
-template <typename T, int VV, int K, int NP> struct States {
-    static constexpr int PV = NP >= VV ? VV : 1, PR = NP / PV, I = (2 * K * PR + 31) / 32;
+// (PB: how many elements at once may be read.)
+template <typename T, int PB, int K, int NP> struct States {
+    static constexpr int PV = NP >= PB ? PB : 1, PR = NP / PV, I = (2 * K * PR + 31) / 32;
+    static constexpr bool WHOLE = PV * sizeof(T) == 16;
     Piece<T, PV> p[I];
     // where piece i of a lane lies, and whether it is there
     template <typename U> __device__ __forceinline__ static const U* piece(const Scan& a, int i, size_t row0, uint32_t col, int rows, int lane, bool& there) {
@@ -169,7 +171,7 @@ template <typename T, int VV, int K, int NP> struct States {
             p[i] = fetch<T, PV>(q, 0, there);
         }
     }
-    __device__ __forceinline__ void take(int i, uint4 w) { if constexpr (PV * sizeof(T) == 16) p[i].w = w; }
+    __device__ __forceinline__ void take(int i, uint4 w) { if constexpr (WHOLE) p[i].w = w; }
     __device__ __forceinline__ void stage(float* sh, int lane) const {
 #pragma unroll
         for (int i = 0; i < I; i++) {
@@ -295,13 +297,27 @@ inline void fill(Scan& a, const sf_sequences* seq, const sf_scan_rows* in, uint3
     set_warps(a, p.cwarps);
     a.st = ctx->d_state;
 }
-// rows begin on 16-byte boundaries, and so does every group's first channel and state
+// rows of channels begin on 16-byte boundaries, and so does every group's first channel
 inline bool fits(const sf_scan_rows* in) {
     const uint32_t size = type_bytes(in->dtype), v = 16 / size;
     auto row = [&](const void* p, size_t ld) { return !p || (aligned(p, 16) && ld % v == 0); };
-    return row(in->u, in->ldu) && row(in->delta, in->ld_delta) && row(in->z, in->ldz) && row(in->B, in->ldb) && row(in->C, in->ldc) && in->D / in->G % v == 0 && in->N % v == 0;
+    return row(in->u, in->ldu) && row(in->delta, in->ld_delta) && row(in->z, in->ldz) && in->D / in->G % v == 0;
+}
+// rows of B and C do, and every group's first state.  They are asked for apart: rows of a few states seldom fit where rows of channels do
+// (N = 3, 64 sequences of 512 rows x 512 with gradients: 1052 us with single elements for all, 550 with them for B and C alone).
+inline bool states_fit(const sf_scan_rows* in) {
+    const uint32_t v = 16 / type_bytes(in->dtype);
+    return in->N % v == 0 && aligned(in->B, 16) && in->ldb % v == 0 && aligned(in->C, 16) && in->ldc % v == 0;
 }
 inline bool fits(const void* p, size_t ld, int dtype) { return !p || (aligned(p, 16) && ld % (16 / type_bytes(dtype)) == 0); }
+
+// elements at once of rows of channels, and of rows of states
+template <typename T, int SL, typename F> int by_width(bool rows, bool states, F f) {
+    constexpr int V = 16 / (int)sizeof(T), P = 4 * SL >= V ? V : 1;
+    typedef std::integral_constant<int, 1> One;
+    if (!rows) return f(One(), One());
+    return states && P > 1 ? f(std::integral_constant<int, V>(), std::integral_constant<int, P>()) : f(std::integral_constant<int, V>(), One());
+}
 
 template <typename K> int launch(K kernel, dim3 grid, uint32_t block, size_t smem, cudaStream_t st, const Scan& a) {
     if (smem > 48 * 1024) SF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));

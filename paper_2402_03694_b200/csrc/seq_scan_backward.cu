@@ -10,10 +10,10 @@ constexpr int R = 4;                       // rows whose decays and states a thr
 
 // What a warp keeps in shared memory.  Sums over states (s1, s2, y) and over channels (dbc) are left as one part a lane, for R rows, and joined where they are
 // used; rows are spaced so that the 16-byte accesses of eight lanes meet no common bank.
-template <typename T, int SL, int VV> struct __align__(16) Backward {
+template <typename T, int SL, int VV, int PB> struct __align__(16) Backward {
     typedef Shape<SL> S;
     typedef Pieces<K, S::CH, VV> P;
-    typedef States<T, VV, K, S::NP> ST;
+    typedef States<T, PB, K, S::NP> ST;
     static constexpr int PX = S::CH + 4, PY = S::CH + (SL == 1 ? 0 : (SL == 2 ? 16 : (SL == 4 ? 8 : 4))), PT = SL * PY + 4;
     static constexpr int ON_WAY = VV > 1 ? 4 * P::I + ST::I : 1;
     float step[K][PX], u[K][PX], e[K][PX];                 // delta; u; dout silu(z)
@@ -27,10 +27,10 @@ template <typename T, int SL, int VV> struct __align__(16) Backward {
 };
 
 // Asks for a tile's pieces: steps, gradients of the outputs, gates, and (not ENDS) inputs.  Whole pieces only; others are read when staged.
-template <typename T, int SL, int VV, bool ENDS>
-__device__ __forceinline__ void ask(const Scan& a, Backward<T, SL, VV>& sh, size_t row0, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
+template <typename T, int SL, int VV, int PB, bool ENDS>
+__device__ __forceinline__ void ask(const Scan& a, Backward<T, SL, VV, PB>& sh, size_t row0, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
     if constexpr (VV > 1) {
-        typedef Backward<T, SL, VV> Sh;
+        typedef Backward<T, SL, VV, PB> Sh;
         typedef typename Sh::P P;
         const P pc(lane);
         const size_t at = row0 + pc.lt;
@@ -45,20 +45,22 @@ __device__ __forceinline__ void ask(const Scan& a, Backward<T, SL, VV>& sh, size
                 copy16(&sh.way[k * P::I + i][lane], there ? from[k] + at * ld[k] + ch0 + pc.lc + P::step(i, ld[k]) : from[k], there);
             }
         }
+        if constexpr (Sh::ST::WHOLE) {
 #pragma unroll
-        for (int i = 0; i < Sh::ST::I; i++) {
-            bool there;
-            const T* p = Sh::ST::template piece<T>(a, i, row0, g * a.N, rows, lane, there);
-            copy16(&sh.way[4 * P::I + i][lane], p, there);
+            for (int i = 0; i < Sh::ST::I; i++) {
+                bool there;
+                const T* p = Sh::ST::template piece<T>(a, i, row0, g * a.N, rows, lane, there);
+                copy16(&sh.way[4 * P::I + i][lane], p, there);
+            }
         }
     }
 }
-// The state before a tile into start[0], likewise; four by four where they lie so
-template <typename T, int SL, int VV>
-__device__ __forceinline__ void ask_start(const Scan& a, Backward<T, SL, VV>& sh, size_t start, uint32_t ch0, uint32_t have, int lane) {
+// The state before a tile into start[0], likewise; four by four where states lie so
+template <typename T, int SL, int VV, int PB>
+__device__ __forceinline__ void ask_start(const Scan& a, Backward<T, SL, VV, PB>& sh, size_t start, uint32_t ch0, uint32_t have, int lane) {
     const int cl = lane / SL, sl = lane % SL;
     const float* p = a.starts + start * a.D * a.N;
-    const bool fours = VV > 1 || (a.n4 && ((uintptr_t)p & 15u) == 0);
+    const bool fours = Backward<T, SL, VV, PB>::ST::WHOLE || (a.n4 && ((uintptr_t)p & 15u) == 0);      // (whole pieces of states: N is a multiple of 4)
 #pragma unroll
     for (int j = 0; j < 4; j++) {
         const bool there = cl * 4 + j < (int)have;
@@ -72,13 +74,14 @@ __device__ __forceinline__ void ask_start(const Scan& a, Backward<T, SL, VV>& sh
 }
 
 // stages steps, inputs and gradients of the rows t0 .. t0 + K - 1 as far as there (zeros behind: they then change nothing); ENDS: what the pass for the parts' ends needs
-template <typename T, int SL, int VV, bool ENDS>
-__device__ __forceinline__ void stage(const Scan& a, Backward<T, SL, VV>& sh, size_t row0, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
-    typedef Backward<T, SL, VV> Sh;
+template <typename T, int SL, int VV, int PB, bool ENDS>
+__device__ __forceinline__ void stage(const Scan& a, Backward<T, SL, VV, PB>& sh, size_t row0, uint32_t ch0, uint32_t have, uint32_t g, int rows, int lane) {
+    typedef Backward<T, SL, VV, PB> Sh;
     typedef typename Sh::P P;
     const P pc(lane);
     Piece<T, VV> nd[P::I], nu[P::I], nz[P::I], ng[P::I];
     typename Sh::ST ns;
+    if constexpr (VV > 1 && !Sh::ST::WHOLE) ns.fetch_all(a, row0, g * a.N, rows, lane);
     copies_done();
     if constexpr (VV > 1) {
 #pragma unroll
@@ -88,8 +91,10 @@ __device__ __forceinline__ void stage(const Scan& a, Backward<T, SL, VV>& sh, si
             if (a.z) nz[i].w = sh.way[2 * P::I + i][lane];
             if (!ENDS) nu[i].w = sh.way[3 * P::I + i][lane];
         }
+        if constexpr (Sh::ST::WHOLE) {
 #pragma unroll
-        for (int i = 0; i < Sh::ST::I; i++) ns.take(i, sh.way[4 * P::I + i][lane]);
+            for (int i = 0; i < Sh::ST::I; i++) ns.take(i, sh.way[4 * P::I + i][lane]);
+        }
     } else {
         const size_t at = row0 + pc.lt;
         const T* pd = (const T*)a.delta + at * a.lddelta + ch0 + pc.lc; const T* pu = (const T*)a.u + at * a.ldu + ch0 + pc.lc;
@@ -171,7 +176,7 @@ __device__ __forceinline__ void stage(const Scan& a, Backward<T, SL, VV>& sh, si
     ns.stage(&sh.bc[0][0][0], lane);
 }
 
-template <typename T, int SL, int VV> __device__ __forceinline__ void channel_params(const Scan& a, Backward<T, SL, VV>& sh, uint32_t ch0, uint32_t have, int lane) {
+template <typename T, int SL, int VV, int PB> __device__ __forceinline__ void channel_params(const Scan& a, Backward<T, SL, VV, PB>& sh, uint32_t ch0, uint32_t have, int lane) {
     for (int c = lane; c < Shape<SL>::CH; c += 32) {
         sh.bias[c] = c < (int)have && a.dbias ? __ldg(a.dbias + ch0 + c) : 0.0f;
         sh.skip[c] = c < (int)have && a.Dk ? __ldg(a.Dk + ch0 + c) : 0.0f;
@@ -215,12 +220,12 @@ __device__ __forceinline__ void store_states(const f2 (&v)[2][4], float* p, size
 }
 
 // Parts: the gradient at a part's first state that the part's own rows cause, and the sum of its steps.
-template <typename T, int SL, int VV>
+template <typename T, int SL, int VV, int PB>
 __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
     sf_chain_enter();
     constexpr int CH = Shape<SL>::CH;
     extern __shared__ __align__(16) unsigned char shared[];
-    Backward<T, SL, VV>& sh = reinterpret_cast<Backward<T, SL, VV>*>(shared)[threadIdx.x / 32];
+    Backward<T, SL, VV, PB>& sh = reinterpret_cast<Backward<T, SL, VV, PB>*>(shared)[threadIdx.x / 32];
     const int lane = threadIdx.x & 31, cl = lane / SL, sl = lane % SL;
     const Item it = item_of(a, CH);
     if (it.have == 0) return;
@@ -234,14 +239,14 @@ __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
     for (int j = 0; j < 2; j++)
 #pragma unroll
         for (int n = 0; n < 4; n++) G[j][n] = 0;
-    channel_params<T, SL, VV>(a, sh, ch0, have, lane);
+    channel_params<T, SL, VV, PB>(a, sh, ch0, have, lane);
     __syncwarp();
     const uint32_t tiles = (t_end - t_begin + K - 1) / K;
-    auto next = [&](uint32_t tile) { const uint32_t t = t_begin + tile * K; ask<T, SL, VV, true>(a, sh, (size_t)r.first + t, ch0, have, g, (int)min((uint32_t)K, t_end - t), lane); };
+    auto next = [&](uint32_t tile) { const uint32_t t = t_begin + tile * K; ask<T, SL, VV, PB, true>(a, sh, (size_t)r.first + t, ch0, have, g, (int)min((uint32_t)K, t_end - t), lane); };
     next(tiles - 1);
     for (uint32_t tile = tiles; tile-- > 0;) {
         const uint32_t t0 = t_begin + tile * K;
-        stage<T, SL, VV, true>(a, sh, (size_t)r.first + t0, ch0, have, g, (int)min((uint32_t)K, t_end - t0), lane);
+        stage<T, SL, VV, PB, true>(a, sh, (size_t)r.first + t0, ch0, have, g, (int)min((uint32_t)K, t_end - t0), lane);
         if (tile) next(tile - 1);
         __syncwarp();
 #pragma unroll
@@ -274,11 +279,11 @@ __global__ void __launch_bounds__(32 * kWarps) back_ends_kernel(const Scan a) {
 // One block: up to kWarps warps over neighbouring channels of a group, one part of one sequence after the other (a run), rows from last to first.
 // A tile's states are stepped from the state kept before it: rows 0 to 3 to reach row 4, rows 4 to 7 with decays and states held in registers, back over
 // them, then rows 0 to 3 the same way.
-template <typename T, int SL, int VV>
+template <typename T, int SL, int VV, int PB>
 __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
     sf_chain_enter();
     typedef Shape<SL> S;
-    typedef Backward<T, SL, VV> Sh;
+    typedef Backward<T, SL, VV, PB> Sh;
     constexpr int CH = S::CH, CL = S::CL, VE = VV > 1 ? 4 : 1;
     typedef Pieces<R, CH, VE> P;                           // as rows are written: R at a time, 4 channels a piece
     constexpr int I = P::I;
@@ -302,7 +307,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
     for (int i = 0; i < I; i++)
 #pragma unroll
         for (int e = 0; e < VE; e++) dD[i][e] = db[i][e] = 0.0f;
-    channel_params<T, SL, VV>(a, sh, ch0, have, lane);
+    channel_params<T, SL, VV, PB>(a, sh, ch0, have, lane);
     __syncwarp();
     const size_t DN = (size_t)a.D * a.N;
     const uint64_t items = (uint64_t)a.q.n_seq * a.parts;
@@ -315,16 +320,16 @@ __global__ void __launch_bounds__(32 * kWarps, 2) back_kernel(const Scan a) {
         const uint32_t tiles = t_end > t_begin ? (t_end - t_begin + K - 1) / K : 0;
         auto next = [&](uint32_t tile) {
             const uint32_t t = t_begin + tile * K;
-            ask<T, SL, VV, false>(a, sh, (size_t)r.first + t, ch0, have, g, (int)min((uint32_t)K, t_end - t), lane);
+            ask<T, SL, VV, PB, false>(a, sh, (size_t)r.first + t, ch0, have, g, (int)min((uint32_t)K, t_end - t), lane);
         };
-        auto next_start = [&](uint32_t tile) { ask_start<T, SL, VV>(a, sh, start_index(r.first, s, t_begin + tile * K), ch0, have, lane); };
+        auto next_start = [&](uint32_t tile) { ask_start<T, SL, VV, PB>(a, sh, start_index(r.first, s, t_begin + tile * K), ch0, have, lane); };
         if (tiles) { next(tiles - 1); next_start(tiles - 1); }
         load_states(G, whole ? (a.d_state && r.slot >= 0 ? a.d_state + (size_t)r.slot * DN : nullptr) : a.part_state + ((size_t)s * a.parts + part) * DN, a, ch0, have, cl, sl, 1.0f);
         for (uint32_t tile = tiles; tile-- > 0;) {
             const uint32_t t0 = t_begin + tile * K;
             const int rows = (int)min((uint32_t)K, t_end - t0);
             const size_t row0 = (size_t)r.first + t0;
-            stage<T, SL, VV, false>(a, sh, row0, ch0, have, g, rows, lane);
+            stage<T, SL, VV, PB, false>(a, sh, row0, ch0, have, g, rows, lane);
             f2 h[2][4];
             auto keep = [&](int q) {
 #pragma unroll
@@ -595,15 +600,18 @@ extern "C" int sf_seq_scan_backward(sf_ctx* ctx, const sf_sequences* seq, const 
     return by_type(in->dtype, [&](auto zero) {
         typedef decltype(zero) T;
         return by_states(p.sl, [&](auto lanes) {
-            constexpr int SL = decltype(lanes)::value, VV = 16 / (int)sizeof(T);
-            int e = SF_OK;
-            if (p.split) {
-                e = launch(vec ? back_ends_kernel<T, SL, VV> : back_ends_kernel<T, SL, 1>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, vec ? sizeof(Backward<T, SL, VV>) * kWarps : sizeof(Backward<T, SL, 1>) * kWarps, st, a);
-                if (e == SF_OK) e = launch(parts_kernel<true>, dim3((uint32_t)(((uint64_t)in->D * in->N + 255) / 256), seq->n_seq), 256, 0, st, a);
-                if (e != SF_OK) return e;
-            }
-            const uint32_t w = std::min((uint32_t)kWarps, p.cwarps);
-            e = launch(vec ? back_kernel<T, SL, VV> : back_kernel<T, SL, 1>, dim3(in->G * p.cblocks, p.runs), 32 * w, vec ? sizeof(Backward<T, SL, VV>) * w : sizeof(Backward<T, SL, 1>) * w, st, a);
+            constexpr int SL = decltype(lanes)::value;
+            int e = by_width<T, SL>(vec, states_fit(in), [&](auto v, auto pb) {
+                constexpr int VV = decltype(v)::value, PB = decltype(pb)::value;
+                const size_t each = sizeof(Backward<T, SL, VV, PB>);
+                if (p.split) {
+                    int e = launch(back_ends_kernel<T, SL, VV, PB>, dim3((uint32_t)blocks, p.parts), 32 * kWarps, each * kWarps, st, a);
+                    if (e == SF_OK) e = launch(parts_kernel<true>, dim3((uint32_t)(((uint64_t)in->D * in->N + 255) / 256), seq->n_seq), 256, 0, st, a);
+                    if (e != SF_OK) return e;
+                }
+                const uint32_t w = std::min((uint32_t)kWarps, p.cwarps);
+                return launch(back_kernel<T, SL, VV, PB>, dim3(in->G * p.cblocks, p.runs), 32 * w, each * w, st, a);
+            });
             if (e == SF_OK && a.sum_bc && (a.dB || a.dC)) {
                 for (uint32_t s = 0; s < seq->n_seq && e == SF_OK; s += 65535) {
                     Scan b = a;
