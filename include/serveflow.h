@@ -414,7 +414,8 @@ int  sf_expert_combine_backward(sf_ctx* ctx, const void* dy, int dtype, size_t l
  * flow (offsets s * P, counts = n_valid).  Outputs of rows that belong to no sequence, or lie behind a sequence's count, are left as they were.
  * max_len (host): rows of the longest sequence.  States are kept in pools of n_slots states; slots[s] (int32[n_seq], nullable: s)
  * names the sequence's state; with an id outside 0..n_slots-1 a sequence starts from zeros and its state is dropped.  No slot may be named twice in
- * a call that writes states (which of the sequences' states it then holds is not defined).  A call may read and write the same pool.
+ * a call that writes states (which of the sequences' states it then holds is not defined).  A call may read and write the same pool, gradients of states included;
+ * pools that overlap in part are refused.
  * On the device: offsets that fall give an empty sequence and record SF_ERR_ARG; rows beyond the arrays, counts beyond the offsets and
  * sequences longer than max_len are cut and record SF_ERR_CAPACITY.
  * Rows are SF_F32, SF_BF16 or SF_F16 with pitches in elements; filters, biases, A, states of the scan and their gradients are fp32,

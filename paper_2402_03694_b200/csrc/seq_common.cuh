@@ -59,6 +59,11 @@ inline int check_sequences(const sf_sequences* q, uint32_t rows) {
     if (q->n_seq && !q->offsets) return SF_ERR_ARG;
     return aligned(q->offsets, 4) && aligned(q->counts, 4) && aligned(q->slots, 4) ? SF_OK : SF_ERR_ARG;
 }
+// Two pools of `bytes` bytes that are neither one pool nor apart: what is read of the one would be what the call writes to another slot of the other.
+inline bool overlap_in_part(const void* p, const void* q, size_t bytes) {
+    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+    return p && q && a != b && (a < b ? b - a : a - b) < bytes;
+}
 inline Seqs seqs_of(const sf_sequences* q, uint32_t rows, uint32_t n_slots) {
     return {q->offsets, q->counts, q->slots, q->n_seq, q->max_len, rows, n_slots};
 }

@@ -391,6 +391,64 @@ __global__ void __launch_bounds__(kThreads, WT <= 4 ? kBlocksB : 2) conv_backwar
     }
 }
 
+// The gradient of the states written over that of the states after the call (one pool).  conv_backward_kernel reads rows of the latter at the sequences' ends, in
+// other blocks too, so there the pool is only written when it is done, by this kernel: row i of a state takes row i - len of the gradient it replaces, so a thread that goes
+// from the last row to the first never reads what it has written.
+template <typename T, int V, int WT, bool EXACT>
+__global__ void __launch_bounds__(kThreads) conv_state_backward_kernel(const Conv<T> a) {
+    sf_chain_enter();
+    typedef Ch<V, (V > 1)> C;
+    const Tiling& t = a.t;
+    const uint32_t c = (blockIdx.x % t.cblocks * t.lanes + threadIdx.x % t.lanes) * V, per = kThreads / t.lanes;
+    if (c >= a.D) return;
+    const uint32_t W = EXACT ? WT : a.W;
+    const int H = (int)W - 1;
+    C tap[WT], bias;
+    load_taps(a.w, c, W, tap);
+    load_bias(a.bias, c, bias);
+    for (uint64_t s = (uint64_t)(blockIdx.x / t.cblocks) * per + threadIdx.x / t.lanes; s < a.q.n_seq; s += (uint64_t)t.parts * per) {
+        const Range r = range_of(a.q, (uint32_t)s, a.st);
+        if (r.slot < 0) continue;
+        const int len = (int)r.len, rows = min(len, H);        // rows that reach back into the state
+        C x[2 * WT - 2], dp[WT - 1];
+        rows_before<T, V, WT>(a, r, 0, c, x);
+#pragma unroll
+        for (int u = 0; u + 1 < WT; u++) {
+            Raw<T, V> nx = {}, ng = {};
+            if (u < rows) { nx.fetch(a.x + (size_t)(r.first + u) * a.ldx + c); ng.fetch(a.dy + (size_t)(r.first + u) * a.lddy + c); }
+            nx.open(x[WT - 1 + u]); ng.open(dp[u]);
+        }
+        if (a.silu) {
+#pragma unroll
+            for (int u = 0; u + 1 < WT; u++) {
+                C pre = bias;
+#pragma unroll
+                for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) pre.add_product(tap[m], x[WT - 1 + u - m]);
+                dp[u].mul_silu_slope(pre);
+                if (u >= rows) dp[u].zero();
+            }
+        }
+        T* state = a.d_state0 + (size_t)r.slot * H * a.D + c;
+#pragma unroll
+        for (int k = WT - 2; k >= 0; k--) {
+            const int o = k - (WT - 1), i = o + H;             // row -1, -2, .. of the sequence, row i of its state
+            if (!EXACT && i < 0) continue;
+            C d;
+            d.zero();
+#pragma unroll
+            for (int m = 1; m < WT; m++) if (o + m >= 0 && (EXACT || m < (int)W)) d.add_product(tap[m], dp[o + m >= 0 ? o + m : 0]);
+            if (i >= len) {
+                Raw<T, V> v;
+                C e;
+                v.fetch_plain(state + (size_t)(i - len) * a.D);
+                v.open(e);
+                d.add(e);
+            }
+            store(state + (size_t)i * a.D, d);
+        }
+    }
+}
+
 // dw[c][k] and db[c] from the blocks' sums: 32 values a block, a warp takes every eighth sum of each
 __global__ void __launch_bounds__(256) conv_join_kernel(const float* __restrict__ parts, uint32_t n_parts, uint32_t D, uint32_t W, float* dw, float* db) {
     sf_chain_enter();
@@ -465,8 +523,9 @@ extern "C" int sf_seq_conv(sf_ctx* ctx, const sf_sequences* seq, const void* x, 
     if (ok != SF_OK || ldy < D || (rows && !y_out) || !aligned(y_out, type_bytes(dtype)) || !aligned(state_in, type_bytes(dtype)) || !aligned(state_out, type_bytes(dtype))) return SF_ERR_ARG;
     if (seq->n_seq == 0) return SF_OK;
     if (W == 1) state_in = state_out = nullptr;
-    SF_ON_DEVICE(ctx);
     const uint32_t size = type_bytes(dtype);
+    if (overlap_in_part(state_in, state_out, (size_t)n_slots * (W - 1) * D * size)) return SF_ERR_ARG;
+    SF_ON_DEVICE(ctx);
     const uint32_t word = std::min({word_of(x, ldx, size), word_of(y_out, ldy, size), word_of(state_in, D, size), word_of(state_out, D, size), word_of(nullptr, D, size)});
     return by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
@@ -512,6 +571,9 @@ extern "C" int sf_seq_conv_backward(sf_ctx* ctx, const sf_sequences* seq, const 
     const bool sums = dw_out || dbias_out;
     if (!sums && !dx_out && !d_state_in_out) return SF_ERR_ARG;
     if (W == 1) { state_in = nullptr; d_state = nullptr; d_state_in_out = nullptr; }
+    const size_t pool = (size_t)n_slots * (W - 1) * D * size;
+    if (overlap_in_part(d_state, d_state_in_out, pool) || overlap_in_part(state_in, d_state_in_out, pool)) return SF_ERR_ARG;
+    const bool one_pool = d_state && d_state == d_state_in_out;
     SF_ON_DEVICE(ctx);
     const uint32_t word = std::min({word_of(x, ldx, size), word_of(dy, lddy, size), word_of(dx_out, lddx, size), word_of(state_in, D, size), word_of(d_state, D, size),
                                     word_of(d_state_in_out, D, size), word_of(nullptr, D, size)});
@@ -522,14 +584,22 @@ extern "C" int sf_seq_conv_backward(sf_ctx* ctx, const sf_sequences* seq, const 
                 constexpr int V = decltype(v)::value, WT = decltype(taps)::value;
                 Conv<T> a = {};
                 a.q = seqs_of(seq, rows, n_slots); a.x = (const T*)x; a.ldx = ldx; a.w = w; a.bias = bias; a.D = D; a.W = W; a.silu = act == SF_ACT_SILU;
-                a.state_in = (const T*)state_in; a.dy = (const T*)dy; a.lddy = lddy; a.d_state = (const T*)d_state; a.d_state0 = (T*)d_state_in_out;
+                a.state_in = (const T*)state_in; a.dy = (const T*)dy; a.lddy = lddy; a.d_state = (const T*)d_state; a.d_state0 = one_pool ? nullptr : (T*)d_state_in_out;
                 a.dx = (T*)dx_out; a.lddx = lddx; a.st = ctx->d_state;
                 a.t = tiling(seq, D, V, kBlocksB);
                 if (sums && (!workspace || workspace_bytes < (size_t)a.t.parts * D * (W + 1) * 4)) return (int)SF_ERR_ARG;
                 a.parts = sums ? (float*)workspace : nullptr;
-                SF_CUDA(sf_launch_chained(conv_backward_kernel<T, V, WT, decltype(exact)::value>, a.t.cblocks * a.t.parts, kThreads, sums ? kThreads * (WT + 1) * V * 4 : 0,
-                                          (cudaStream_t)stream, a));
+                if (sums || dx_out || !one_pool)
+                    SF_CUDA(sf_launch_chained(conv_backward_kernel<T, V, WT, decltype(exact)::value>, a.t.cblocks * a.t.parts, kThreads, sums ? kThreads * (WT + 1) * V * 4 : 0,
+                                              (cudaStream_t)stream, a));
                 if (sums) SF_CUDA(sf_launch_chained(conv_join_kernel, (D * (W + 1) + 31) / 32, 256, 0, (cudaStream_t)stream, (const float*)workspace, a.t.parts, D, W, dw_out, dbias_out));
+                if (one_pool && seq->n_seq) {
+                    sf_sequences ends = *seq;
+                    ends.max_len = 1;                      // (one item a sequence)
+                    a.t = tiling(&ends, D, V, kBlocksB);
+                    a.d_state0 = (T*)d_state_in_out;
+                    SF_CUDA(sf_launch_chained(conv_state_backward_kernel<T, V, WT, decltype(exact)::value>, a.t.cblocks * a.t.parts, kThreads, 0, (cudaStream_t)stream, a));
+                }
                 return (int)SF_OK;
             });
         });

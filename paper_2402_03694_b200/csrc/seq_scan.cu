@@ -422,7 +422,7 @@ extern "C" int sf_seq_scan(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_r
     const int ok = check(ctx, seq, in, rows);
     if (ok != SF_OK) return ok;
     if (n_slots > 0x7FFFFFFFu || ldy < in->D || (rows && !y_out) || !aligned(y_out, type_bytes(in->dtype)) || !aligned(state_in, 4) || !aligned(state_out, 4) || !aligned(starts_out, 4) ||
-        !aligned(workspace, 4)) return SF_ERR_ARG;
+        !aligned(workspace, 4) || overlap_in_part(state_in, state_out, (size_t)n_slots * in->D * in->N * 4)) return SF_ERR_ARG;
     if (seq->n_seq == 0) return SF_OK;
     const Plan p = plan_of(seq->n_seq, seq->max_len, in->D, in->N, in->G, false);
     if (p.split && (!workspace || workspace_bytes < part_bytes(p, seq->n_seq, in->D, in->N))) return SF_ERR_ARG;

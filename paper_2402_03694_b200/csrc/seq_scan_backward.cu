@@ -578,7 +578,8 @@ extern "C" int sf_seq_scan_backward(sf_ctx* ctx, const sf_sequences* seq, const 
     const size_t GN = (size_t)in->G * in->N;
     if ((out->du && out->lddu < in->D) || (out->d_delta && out->ldd_delta < in->D) || (out->dz && (out->lddz < in->D || !in->z)) || (out->dB && out->lddb < GN) || (out->dC && out->lddc < GN)) return SF_ERR_ARG;
     if (!aligned(dy, size) || !aligned(out->du, size) || !aligned(out->d_delta, size) || !aligned(out->dz, size) || !aligned(out->dB, size) || !aligned(out->dC, size) || !aligned(starts, 4) ||
-        !aligned(d_state, 4) || !aligned(d_state_in_out, 4) || !aligned(out->dA, 4) || !aligned(out->dD_skip, 4) || !aligned(out->d_delta_bias, 4) || !aligned(workspace, 4)) return SF_ERR_ARG;
+        !aligned(d_state, 4) || !aligned(d_state_in_out, 4) || !aligned(out->dA, 4) || !aligned(out->dD_skip, 4) || !aligned(out->d_delta_bias, 4) || !aligned(workspace, 4) ||
+        overlap_in_part(d_state, d_state_in_out, (size_t)n_slots * in->D * in->N * 4)) return SF_ERR_ARG;
     const Plan p = plan_of(seq->n_seq, seq->max_len, in->D, in->N, in->G, true);
     if (!workspace || workspace_bytes < back_bytes(p, seq->n_seq, rows, in->D, in->N, in->G)) return SF_ERR_ARG;
     SF_ON_DEVICE(ctx);
