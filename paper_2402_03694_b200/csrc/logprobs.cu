@@ -15,7 +15,9 @@ using namespace sfseq;
 
 constexpr uint32_t kThreads = 256;
 constexpr uint32_t kMaxTop = SF_MAX_TOP;
-constexpr uint32_t kMaxV = 0x7FF00000;              // (entries and those of the chunks behind them in 31 bits)
+constexpr uint32_t kMaxV = 0x7FF00000;              // longest row
+// Indexes of entries are ints: those of the chunks that a thread looks at behind a row's end (two turns of four chunks by 512 threads at most) are to fit them too.
+static_assert(kMaxV + 14 + 2 * 4 * 512 * 8 <= 0x7FFFFFFFu, "entries in 31 bits");
 
 template <typename T> struct Rows {
     const T* z; size_t ld;
@@ -455,23 +457,24 @@ __global__ void __launch_bounds__(kThreads) back_kernel(const Back<T> a) {
     const uint32_t width = SAME ? a.groups : a.chunks;
     size_t row[C];
     int i0[C];
+    bool there[C];                                         // (a thread without a row has no entries: nothing is derived from its place)
     Chunk<T> in[C];
     RowBack<T> r[SAME ? 1 : C];
 #pragma unroll
     for (int u = 0; u < C; u++) {
-        if (SAME && u) { row[u] = row[0]; i0[u] = i0[0] + u * (int)a.groups * 8; }
+        if (SAME && u) { row[u] = row[0]; i0[u] = i0[0] + u * (int)a.groups * 8; there[u] = there[0] && i0[u] < (int)a.V; }
         else {
             const uint64_t at = ((uint64_t)blockIdx.x + (SAME ? 0 : (uint64_t)u * gridDim.x)) * kThreads + threadIdx.x;
             if (a.few) { row[u] = (uint32_t)at / width; i0[u] = (int)((uint32_t)at % width * 8); }
             else { row[u] = at / width; i0[u] = (int)(at % width * 8); }
-            if (row[u] < n) { r[u].load(a, row[u]); i0[u] -= (int)shift_of(a.z + row[u] * a.ld); }
-            else i0[u] = (int)a.V;
+            there[u] = row[u] < n;
+            if (there[u]) { r[u].load(a, row[u]); i0[u] -= (int)shift_of(a.z + row[u] * a.ld); there[u] = i0[u] < (int)a.V; }
         }
-        if (i0[u] < (int)a.V) in[u].fetch(a.z + row[u] * a.ld, i0[u], a.V);
+        if (there[u]) in[u].fetch(a.z + row[u] * a.ld, i0[u], a.V);
     }
 #pragma unroll
     for (int u = 0; u < C; u++) {
-        if (i0[u] >= (int)a.V) continue;
+        if (!there[u]) continue;
         if (!SAME || u == 0) r[SAME ? 0 : u].ready(a);
         float d[8];
         r[SAME ? 0 : u].chunk(a, row[u], i0[u], in[u], d);
