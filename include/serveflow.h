@@ -491,7 +491,8 @@ int  sf_label_logprobs(sf_ctx* ctx, const void* logits, int dtype, const uint32_
                        const int32_t* labels, float* logprob_out, float* entropy_out, float* lse_out, uint32_t k, int32_t* top_ids_out,
                        float* top_logprobs_out, void* stream);
 /* Gradient of the logits (d_logits_out[n][ldd], their type) from those of the outputs, each nullable: d_logprob fp32[n], d_entropy fp32[n] (needs
- * entropy), d_top_logprobs fp32[n][k] (needs top_ids).  lse, entropy and top_ids are what the forward call gave.  Masked entries get 0. */
+ * entropy), d_top_logprobs fp32[n][k] (needs top_ids).  lse, entropy and top_ids are what the forward call gave.  Masked entries get 0.
+ * (A finite number is no mask: a row of nothing but the type's lowest value is a row of equals.  scale times an entry has to stay finite in fp32.) */
 int  sf_label_logprobs_backward(sf_ctx* ctx, const void* logits, int dtype, const uint32_t* n_dev, uint32_t n, uint32_t V, size_t ld, float scale,
                                 const int32_t* labels, const float* lse, const float* d_logprob, const float* entropy, const float* d_entropy,
                                 uint32_t k, const int32_t* top_ids, const float* d_top_logprobs, void* d_logits_out, size_t ldd, void* stream);

@@ -392,6 +392,8 @@ template <typename T> struct Back {
     sf_dev_state* st;
 };
 
+constexpr float kFar = 1024.0f;                            // from this |lse| on a row's p is worked out from its entries (p would be off by more than 2^-14)
+
 // What a row's gradient takes besides its entries.  With t = log2 p:  d z = -p (sum + ge (t + h)) + what belongs to the label and the alternatives, everything
 // times scale.
 template <typename T> struct RowBack {
@@ -413,6 +415,8 @@ template <typename T> struct RowBack {
         g = __fmul_rn(g, a.scale);                         // (rounded here, so that g taken off and g added cancel)
         sum += g;
     }
+    // lse as an fp32 number is off by half a step, up to |lse| 2^-24, and p by as much: nothing is left of ln s in the lse of a row of the type's lowest value
+    __device__ __forceinline__ bool far() const { return fabsf(lse) >= kFar && (sum != 0.0f || ge != 0.0f); }
     __device__ __forceinline__ void chunk(const Back<T>& a, size_t row, int i0, const Chunk<T>& in, float (&d)[8]) const {
         const f2 e2 = dup2(kLog2e), l2 = dup2(-lse), s2 = dup2(-sum), g2 = dup2(-ge), h2 = dup2(h);
         float v[8];
@@ -446,9 +450,85 @@ template <typename T> struct RowBack {
     }
 };
 
+// The gradient of a row whose lse lies far from zero, by TH threads (a warp or a block): maximum, sum and gradient from the entries themselves, differences from
+// the maximum before anything is rounded.
+template <typename T, int TH> __device__ __forceinline__ void far_row(const Back<T>& a, size_t row, float* sh) {
+    const T* z = a.z + row * a.ld;
+    T* dz = a.dz + row * a.ldd;
+    const int begin = (int)(threadIdx.x % TH) * 8 - (int)shift_of(z);
+    const float c = a.scale * kLog2e;
+    auto join = [&](float v, auto both) {                  // over the threads, always in the same order
+#pragma unroll
+        for (int d = 16; d; d >>= 1) v = both(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+        if constexpr (TH > 32) {
+            __syncthreads();
+            if (threadIdx.x % 32 == 0) sh[threadIdx.x / 32] = v;
+            __syncthreads();
+            v = sh[0];
+            for (int i = 1; i < TH / 32; i++) v = both(v, sh[i]);
+        }
+        return v;
+    };
+    float m = -FLT_MAX, s = 0.0f, v[8];
+    for (int i0 = begin; i0 < (int)a.V; i0 += TH * 8) {
+        load_chunk(z, i0, a.V, v);
+        m = fmaxf(m, max_of(v));
+    }
+    m = join(m, [](float x, float y) { return fmaxf(x, y); });
+    for (int i0 = begin; i0 < (int)a.V; i0 += TH * 8) {
+        load_chunk(z, i0, a.V, v);
+#pragma unroll
+        for (int e = 0; e < 8; e++) s += ex2((v[e] - m) * c);
+    }
+    s = join(s, [](float x, float y) { return x + y; });
+    const float log2_s = log2f(s);
+    RowBack<T> r;
+    r.load(a, row);
+    r.ready(a);
+    for (int i0 = begin; i0 < (int)a.V; i0 += TH * 8) {
+        load_chunk(z, i0, a.V, v);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const uint32_t i = (uint32_t)(i0 + e);
+            const float t = (v[e] - m) * c - log2_s;
+            float d = ex2(t) * (-r.sum - r.ge * (fmaxf(t, -1e4f) + r.h));
+            if (i == r.label) d += r.g;
+            if (a.d_top) for (uint32_t j = 0; j < a.k; j++) if ((uint32_t)a.top_ids[row * a.k + j] == i) d += a.d_top[row * a.k + j] * a.scale;
+            if (i < a.V) dz[i] = from_f32<T>(v[e] == -INFINITY ? 0.0f : d);
+        }
+    }
+}
+
+// Such rows of back_kernel<SAME>, which leaves them.  (2048 x 32768 bf16 with the forward call: 99 us; 97 without a look at the rows, 110 with a loop for them at that
+// kernel's end and 101 with blocks of their own in it: its registers suffice for neither.)
+template <typename T> __global__ void __launch_bounds__(kThreads) far_rows_kernel(const Back<T> a) {
+    sf_chain_enter();
+    __shared__ float sh[kThreads / 32];
+    __shared__ uint32_t rows[kThreads], n_rows;
+    uint32_t n = a.n;
+    if (a.n_dev) n = sf_clamp_rows(*a.n_dev, a.n, a.st);
+    for (uint64_t first = blockIdx.x; first < n; first += (uint64_t)gridDim.x * kThreads) {      // a row a thread to look at, then one after the other
+        const uint64_t row = first + (uint64_t)threadIdx.x * gridDim.x;
+        bool far = false;
+        if (row < n && fabsf(a.lse[row]) >= kFar) {
+            RowBack<T> r;
+            r.load(a, row);
+            r.ready(a);
+            far = r.far();
+        }
+        if (!__syncthreads_or(far)) continue;
+        if (threadIdx.x == 0) n_rows = 0;
+        __syncthreads();
+        if (far) rows[atomicAdd(&n_rows, 1u)] = (uint32_t)row;
+        __syncthreads();
+        for (uint32_t i = 0; i < n_rows; i++) far_row<T, kThreads>(a, rows[i], sh);
+        __syncthreads();
+    }
+}
+
 // A thread takes C chunks, everything they need on its way before the first is worked on.  SAME: of one row, `groups` apart (long rows);
 // else the next ones are a whole grid's width further on.  Chunks begin on 16-byte boundaries of the logits' row; where the gradient's row lies on
-// the same ones they are stored whole too.
+// the same ones they are stored whole too.  Rows far from zero are left out: of short rows the warp in which one begins does it.
 template <typename T, int C, bool SAME>
 __global__ void __launch_bounds__(kThreads) back_kernel(const Back<T> a) {
     sf_chain_enter();
@@ -472,10 +552,16 @@ __global__ void __launch_bounds__(kThreads) back_kernel(const Back<T> a) {
         }
         if (there[u]) in[u].fetch(a.z + row[u] * a.ld, i0[u], a.V);
     }
+    bool far[C];                                           // of this thread's rows
+#pragma unroll
+    for (int u = 0; u < C; u++) {
+        far[u] = false;
+        if (there[u] && (!SAME || u == 0)) { r[SAME ? 0 : u].ready(a); far[u] = r[SAME ? 0 : u].far(); }
+        if (far[SAME ? 0 : u]) there[u] = false;
+    }
 #pragma unroll
     for (int u = 0; u < C; u++) {
         if (!there[u]) continue;
-        if (!SAME || u == 0) r[SAME ? 0 : u].ready(a);
         float d[8];
         r[SAME ? 0 : u].chunk(a, row[u], i0[u], in[u], d);
         T* dz = a.dz + row[u] * a.ldd;
@@ -484,6 +570,12 @@ __global__ void __launch_bounds__(kThreads) back_kernel(const Back<T> a) {
 #pragma unroll
             for (int e = 0; e < 8; e++) if ((uint32_t)(i0[u] + e) < a.V) dz[i0[u] + e] = from_f32<T>(d[e]);
         }
+    }
+    if constexpr (!SAME) {                                 // a row that lies far from zero: the warp in which it begins (its first chunk begins at entry 0 or in front of it)
+#pragma unroll
+        for (int u = 0; u < C; u++)
+            for (uint32_t begin = __ballot_sync(0xFFFFFFFFu, far[u] && i0[u] <= 0); begin; begin &= begin - 1)
+                far_row<T, 32>(a, (size_t)__shfl_sync(0xFFFFFFFFu, (unsigned long long)row[u], __ffs(begin) - 1), nullptr);
     }
 }
 
@@ -571,6 +663,7 @@ extern "C" int sf_label_logprobs_backward(sf_ctx* ctx, const void* logits, int d
         a.few = blocks * kThreads * S <= 0xFFFFFFFFu;
         auto kern = lng ? back_kernel<T, C, true> : (two ? back_kernel<T, S, false> : back_kernel<T, 1, false>);
         SF_CUDA(sf_launch_chained(kern, (uint32_t)blocks, kThreads, 0, (cudaStream_t)stream, a));
+        if (lng) SF_CUDA(sf_launch_chained(far_rows_kernel<T>, std::min(n, 2u * (uint32_t)ctx->num_sms), kThreads, 0, (cudaStream_t)stream, a));
         return (int)SF_OK;
     });
 }

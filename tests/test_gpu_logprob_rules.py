@@ -1,11 +1,12 @@
-"""What the calls on logits promise beyond their values: rows of more than 2^30 entries, threads without a row."""
+"""What the calls on logits promise at the ends of their range: rows of more than 2^30 entries, threads without a row, rows that lie far from zero."""
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_logprobs import E, MARK, env  # noqa: E402, F401
+import sequences as ref  # noqa: E402
+from test_gpu_logprobs import E, HALF_STEP, MARK, TINY, TYPES, dev, env, num, run, span_of  # noqa: E402, F401
 
 
 def test_gradient_of_a_row_of_more_than_a_billion_entries(env):  # noqa: F811
@@ -30,3 +31,64 @@ def test_gradient_of_a_row_of_more_than_a_billion_entries(env):  # noqa: F811
     rest = d[0].clone()
     rest[torch.tensor([5, 7, V - 1], device="cuda")] = d[0, 0]
     assert bool((rest == d[0, 0]).all()) and bool((d[1] == MARK).all())
+
+
+FAR = [  # n, V, k, kind, scale, pitch
+    (300, 1, 1, "fp32", 1.0, 0), (70, 2, 1, "bf16", 0.7, 0), (200, 16, 2, "fp32", 1.0, 0), (50, 17, 3, "fp16", 1.5, 1), (40, 100, 2, "fp32", 0.7, 3), (20, 511, 0, "bf16", 1.0, 0),
+    (40, 515, 2, "fp32", 1.0, 1), (30, 600, 2, "bf16", 1.0, 0), (9, 5000, 4, "fp32", 0.7, 0), (5, 40000, 8, "bf16", 1.0, 0),
+]
+
+
+@pytest.mark.parametrize("n,V,k,kind,scale,pitch", FAR)
+def test_gradient_of_rows_far_from_zero(env, n, V, k, kind, scale, pitch):  # noqa: F811
+    """Rows of nothing but the type's lowest or largest value, and rows around a large number, between ordinary ones.  The tolerance is the one of ordinary rows without
+    the rounding of lse where |lse| >= 1024: exponentials of differences from the row's maximum are off by (4 + 2 span) e each, their sum by one e a term."""
+    sf, ctx = env
+    rng = np.random.default_rng(V + k)
+    low = float(torch.finfo(TYPES[kind]).min) if kind != "fp16" else -60000.0
+    x = rng.standard_normal((n, V)) * 2
+    for r in range(n):
+        if r % 5 == 0:
+            x[r] = low if r % 10 == 0 else -low
+        elif r % 5 == 1:
+            x[r] += (1e6 if kind == "fp32" else 2e4) * rng.choice([-1, 1])
+        elif r % 5 == 2:
+            x[r, rng.random(V) < 0.4] = low                # a mask by the lowest value
+        elif r % 5 == 3:
+            x[r] -= 5000
+            x[r, rng.random(V) < 0.3] = -np.inf
+    t = torch.zeros(n, V + pitch, dtype=TYPES[kind], device="cuda")[:, :V]
+    t.copy_(torch.from_numpy(x))
+    X, scale = num(t), float(np.float32(scale))
+    labels = rng.integers(0, V, n)
+    labels[rng.random(n) < 0.2] = -1
+    f = ref.logprobs(X, scale, labels, k)
+    o = run(sf, ctx, t, dev(labels, np.int32), k, scale)
+    assert np.array_equal(num(o["top_ids"]), f["top_ids"])
+    dl, de, dt = rng.standard_normal(n), rng.standard_normal(n), rng.standard_normal((n, k))
+    quiet = rng.random(n) < 0.2                            # rows whose outputs nobody uses
+    dl[quiet] = de[quiet] = 0
+    span, lse = span_of(X, scale), np.abs(np.where(np.isfinite(f["lse"]), f["lse"], 0))[:, None]
+    with np.errstate(divide="ignore", invalid="ignore"):
+        logp = np.where(f["p"] > 0, np.log(f["p"]), 0.0)
+    for use in ((1, 0, 0), (0, 1, 0), (1, 1, 1)):
+        g = [v.astype(np.float32).astype(float) if u else None for u, v in zip(use, (dl, de, dt))]
+        if k == 0:
+            g[2] = None
+        d = torch.full((n, V + pitch), MARK, dtype=t.dtype, device="cuda")[:, :V]
+        sf.sf_label_logprobs_backward(ctx, t, dev(labels, np.int32), o["lse"], d, d_logprob=None if g[0] is None else dev(g[0]), entropy=o["entropy"],
+                                      d_entropy=None if g[1] is None else dev(g[1]), top_ids=o["top_ids"] if g[2] is not None else None,
+                                      d_top_logprobs=None if g[2] is None else dev(g[2]), scale=scale)
+        want = ref.logprobs_gradient(X, scale, labels, f, *g)
+        pull = np.abs(dl) * (g[0] is not None) + (np.abs(dt).sum(1) if g[2] is not None else 0)
+        mag = f["p"] * (pull[:, None] + (np.abs(de)[:, None] * (np.abs(logp) + np.abs(f["entropy"])[:, None] + 1) if g[1] is not None else 0))
+        c = (V / 8 + 64 + 2 * span + 8 * np.where(lse < 1024, lse, 0)) * E
+        tol = scale * (c * mag + (k + 4) * E * pull[:, None])
+        got = num(d)
+        bad = ~(np.abs(got - want) <= tol + HALF_STEP[kind] * np.abs(want) + TINY[kind])
+        assert not bad.any(), (use, np.argwhere(bad)[:3], got[bad][:3], want[bad][:3])
+    again = torch.full((n, V + pitch), MARK, dtype=t.dtype, device="cuda")[:, :V]
+    sf.sf_label_logprobs_backward(ctx, t, dev(labels, np.int32), o["lse"], again, d_logprob=dev(g[0]), entropy=o["entropy"], d_entropy=dev(g[1]),
+                                  top_ids=o["top_ids"] if k else None, d_top_logprobs=dev(g[2]) if k else None, scale=scale)
+    assert torch.equal(d, again)
+    sf.sf_ctx_poll(ctx)
