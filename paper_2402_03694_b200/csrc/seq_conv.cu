@@ -64,13 +64,13 @@ template <int V, bool PAIRS> struct Ch {
 #pragma unroll
         for (int i = 0; i < V; i++) p[i] += a.p[i];
     }
-    __device__ __forceinline__ void silu() {
+    template <typename T> __device__ __forceinline__ void silu() {
 #pragma unroll
-        for (int i = 0; i < V; i++) p[i] *= sigmoid(p[i]);
+        for (int i = 0; i < V; i++) p[i] *= sigmoid<T>(p[i]);
     }
-    __device__ __forceinline__ void mul_silu_slope(const Ch& x) {      // times silu'(x) = s (1 + x (1 - s))
+    template <typename T> __device__ __forceinline__ void mul_silu_slope(const Ch& x) {      // times silu'(x) = s (1 + x (1 - s))
 #pragma unroll
-        for (int i = 0; i < V; i++) { const float s = sigmoid(x.p[i]); p[i] *= s * fmaf(x.p[i], 1.0f - s, 1.0f); }
+        for (int i = 0; i < V; i++) { const float s = sigmoid<T>(x.p[i]); p[i] *= s * fmaf(x.p[i], 1.0f - s, 1.0f); }
     }
 };
 
@@ -101,10 +101,10 @@ template <int V> struct Ch<V, true> {
 #pragma unroll
         for (int i = 0; i < P; i++) p[i] = add2(a.p[i], p[i]);
     }
-    __device__ __forceinline__ void mul_silu_slope(const Ch& x) {
+    template <typename T> __device__ __forceinline__ void mul_silu_slope(const Ch& x) {
 #pragma unroll
         for (int i = 0; i < P; i++) {
-            const f2 s = sigmoid2(x.p[i]), one = dup2(1.0f);
+            const f2 s = sigmoid2<T>(x.p[i]), one = dup2(1.0f);
             p[i] = mul2(mul2(p[i], s), fma2(x.p[i], fma2(s, dup2(-1.0f), one), one));
         }
     }
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(const Conv<T> a) {
                     Ch<V, false> pre = bias;
 #pragma unroll
                     for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) pre.add_product(tap[m], x[WT - 1 + u - m]);
-                    if (a.silu) pre.silu();
+                    if (a.silu) pre.template silu<T>();
                     store(y, pre);
                 }
                 y += a.ldy;
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(const Conv<T> a) {
                 pre.add_product(tap[0], v);
 #pragma unroll
                 for (int m = 1; m < WT; m++) if (EXACT || m <= H) { st[u][WT - 1 - m].open(v); pre.add_product(tap[m], v); }
-                if (a.silu) pre.silu();
+                if (a.silu) pre.template silu<T>();
                 store(a.y + (size_t)r[u].first * a.ldy + c, pre);
             }
             if (a.state_out && r[u].slot >= 0) {
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, WT <= 4 ? kBlocksB : 2) conv_backwar
                         C pre = bias;
 #pragma unroll
                         for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) pre.add_product(tap[m], x[WT - 1 + u - m]);
-                        g.mul_silu_slope(pre);
+                        g.template mul_silu_slope<T>(pre);
                     }
                     if (!ALL && p + u >= pe) g.zero();
                     if (ALL || p + u < p1) {
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(kThreads) conv_state_backward_kernel(const Con
                 C pre = bias;
 #pragma unroll
                 for (int m = 0; m < WT; m++) if (EXACT || m < (int)W) pre.add_product(tap[m], x[WT - 1 + u - m]);
-                dp[u].mul_silu_slope(pre);
+                dp[u].template mul_silu_slope<T>(pre);
                 if (u >= rows) dp[u].zero();
             }
         }

@@ -60,9 +60,8 @@ __device__ __forceinline__ size_t start_index(uint32_t first, uint32_t s, uint32
 
 // softplus(x) = max(x, 0) + ln(1 + e), e = exp(-|x|) <= 1; ln(1 + e) = 2 artanh(e / (2 + e)) by its series in q = e / (2 + e) <= 1/3 (the first
 // term left out is q^14 / 15 < 2e-8 of the sum).  Keeps its relative accuracy where e is small, which ln(1 + e) by a logarithm does not.
-__device__ __forceinline__ float softplus_of(float x, float& e) {
-    e = ex2(-kLog2e * fabsf(x));
-    const float q = e * rcp(2.0f + e), q2 = q * q;
+__device__ __forceinline__ float softplus_of(float x) {
+    const float e = exp_minus_abs(x), q = e * rcp(2.0f + e), q2 = q * q;
     float p = fmaf(q2, 1.0f / 13, 1.0f / 11);
     p = fmaf(q2, p, 1.0f / 9); p = fmaf(q2, p, 1.0f / 7); p = fmaf(q2, p, 1.0f / 5); p = fmaf(q2, p, 1.0f / 3); p = fmaf(q2, p, 1.0f);
     return fmaf(2.0f * q, p, fmaxf(x, 0.0f));
@@ -70,12 +69,9 @@ __device__ __forceinline__ float softplus_of(float x, float& e) {
 
 // the same for two values; ee: their exp(-|x|)
 __device__ __forceinline__ f2 softplus2(f2 x, f2& ee) {
-    float a, b;
+    float a, b, e, f;
     unpack2(x, a, b);
-    const f2 t = mul2(pack2(fabsf(a), fabsf(b)), dup2(-kLog2e));
-    float e, f;
-    unpack2(t, e, f);
-    ee = pack2(ex2(e), ex2(f));
+    ee = exp_minus_abs2(x);
     unpack2(add2(ee, dup2(2.0f)), e, f);
     const f2 q = mul2(ee, pack2(rcp(e), rcp(f))), q2 = mul2(q, q);
     f2 p = fma2(q2, dup2(1.0f / 13), dup2(1.0f / 11));

@@ -148,7 +148,7 @@ __device__ __forceinline__ void stage(const Scan& a, Backward<T, SL, VV, PB>& sh
             unpack2(v, d[e], d[e + 1]);
             unpack2(w, ds[e], ds[e + 1]);
             if (a.z) {
-                const f2 zz = pack2(z[e], z[e + 1]), oo = pack2(o[e], o[e + 1]), sg = sigmoid2(zz), os = mul2(oo, sg);
+                const f2 zz = pack2(z[e], z[e + 1]), oo = pack2(o[e], o[e + 1]), sg = sigmoid2<T>(zz), os = mul2(oo, sg);
                 if (!ENDS) unpack2(mul2(os, fma2(zz, fma2(sg, dup2(-1.0f), one), one)), dg[e], dg[e + 1]);
                 unpack2(mul2(os, zz), o[e], o[e + 1]);
             }

@@ -1,12 +1,12 @@
-"""What the calls on sequences promise beyond their values: pools that are read and written by one call."""
+"""What the calls on sequences promise beyond their values: pools that are read and written by one call, small steps and gates."""
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-import test_gpu_sequences as base  # noqa: E402
-from test_gpu_sequences import MARK, TYPES, env, lay_out, like, rows_in, scan_case  # noqa: E402, F401
+import sequences as ref  # noqa: E402
+from test_gpu_sequences import E, MARK, TYPES, env, lay_out, like, num, rows_in, scan_case  # noqa: E402, F401
 
 
 # ---- one pool, read and written by a call ----------------------------------------------------------------------------------------------
@@ -73,4 +73,60 @@ def test_scan_gradients_of_states_in_one_pool(env, lengths, D, kind):  # noqa: F
         sf.sf_seq_scan_backward(ctx, q, *rows, t["dy"], starts, work, d_state=d if one else after, d_state_in_out=d, du_out=du, **rest)
         out.append((d, du))
     assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1]) and bool(torch.isfinite(out[1][0]).all())
+    sf.sf_ctx_poll(ctx)
+
+
+# ---- steps and gates of large arguments ----------------------------------------------------------------------------------------------------
+# exp(-|x|) is off by 4 e (two units in the last place), 1 + it by e, a reciprocal by 2 e, each product by e.  Sigmoid: 7 e; the slope of softplus, e^-|x| / (1 + e^-|x|): 8 e;
+# softplus itself, 2 q (1 + q^2 / 3 + ..) with q = e / (2 + e): 8 e for q, 3 e for the series, 2 e for the rest, 16 e with room.  All relative, wherever the argument lies.
+def within(got, want, tol):
+    got = num(got)
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:3], got[bad][:3], want[bad][:3], (np.abs(got - want) / tol)[bad].max())
+
+
+@pytest.mark.parametrize("D", [64, 33, 6])                 # rows on 16-byte boundaries, and not
+def test_small_steps_and_gates_keep_their_relative_accuracy(env, D):  # noqa: F811
+    sf, ctx = env
+    S, N = 120, 2
+    x = torch.linspace(-85, 85, S * D, dtype=torch.float64).float().view(S, D).cuda()
+    X, one, ones, A = num(x), torch.ones(S, D, device="cuda"), torch.ones(S, N, device="cuda"), -torch.ones(D, N, device="cuda")
+    half = ones / N                                        # N states of delta u / N each: y = delta u
+    q = sf.make_sequences(torch.arange(S + 1, dtype=torch.int32, device="cuda"), 1)
+    starts = torch.zeros(sf.sf_seq_scan_starts(S, S, D, N), device="cuda")
+    work = torch.zeros(sf.sf_seq_scan_workspace(S, 1, S, D, N, backward=True), dtype=torch.uint8, device="cuda")
+    step, slope = ref.softplus(X), np.exp(-np.maximum(-X, 0)) / (1 + np.exp(-np.abs(X)))
+    for kept in (None, starts):                            # the single step's kernel, the scan's
+        y = torch.zeros_like(x)
+        sf.sf_seq_scan(ctx, q, one, x, A, ones, half, y, softplus=True, starts_out=kept)
+        within(y, step, 18 * E * step)
+    du, dd = torch.zeros_like(x), torch.zeros_like(x)
+    sf.sf_seq_scan_backward(ctx, q, one, x, A, ones, half, one, starts, work, softplus=True, du_out=du, d_delta_out=dd)
+    within(du, step, 20 * E * step)
+    within(dd, slope, 12 * E * slope)
+    s = np.exp(-np.maximum(-X, 0)) / (1 + np.exp(-np.abs(X)))
+    gate, d_gate, mag = X * s, s * (1 + X * (1 - s)), s * (1 + np.abs(X) * (1 - s))
+    for kept in (None, starts):
+        y = torch.zeros_like(x)
+        sf.sf_seq_scan(ctx, q, one, one, A, ones, half, y, z=x, starts_out=kept)
+        within(y, gate, 12 * E * np.abs(gate))
+    dz = torch.zeros_like(x)
+    sf.sf_seq_scan_backward(ctx, q, one, one, A, ones, half, one, starts, work, z=x, du_out=du, dz_out=dz)
+    within(du, gate, 12 * E * np.abs(gate))
+    # slope: 1 - s is off by 7 e s + e (1 - s); for large x it is a difference of equals, off by a step of 1, and times x
+    within(dz, d_gate, 14 * E * mag + 10 * E * np.abs(X) * s)
+    b = x.bfloat16()                                       # rows of 16 bits, states of 32
+    B, state = num(b), torch.zeros(S, D, N, device="cuda")
+    for kept in (None, starts):
+        sf.sf_seq_scan(ctx, q, one.bfloat16(), b, A, ones.bfloat16(), half.bfloat16(), torch.zeros_like(b), softplus=True, state_out=state, starts_out=kept)
+        within(state, np.repeat(ref.softplus(B)[:, :, None], N, 2), 18 * E * ref.softplus(B)[:, :, None])
+        state.zero_()
+    w = torch.ones(D, 1, device="cuda")
+    long = sf.make_sequences(torch.tensor([0, S], dtype=torch.int32, device="cuda"), S)
+    for seq in (q, long):                                  # single rows and whole sequences: with one tap the same
+        y, dx = torch.zeros_like(x), torch.zeros_like(x)
+        sf.sf_seq_conv(ctx, seq, x, w, y, act=sf.SF_ACT_SILU)
+        within(y, gate, 10 * E * np.abs(gate))
+        sf.sf_seq_conv_backward(ctx, seq, x, w, one, None, act=sf.SF_ACT_SILU, dx_out=dx)
+        within(dx, d_gate, 14 * E * mag + 10 * E * np.abs(X) * s)
     sf.sf_ctx_poll(ctx)
