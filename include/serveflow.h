@@ -75,6 +75,7 @@ extern "C" {
 #define SF_ACT_SILU     1          /* x * sigmoid(x) */
 #define SF_SEQ_MAX_ROWS 2147418112u  /* rows of the arrays, sequences, rows of a sequence that the sf_seq_* calls take (2^31 - 2^16) */
 #define SF_SCAN_MAX_STATES 64      /* states of a channel that sf_seq_scan takes */
+#define SF_SCAN_EVERY   8          /* rows between two states that sf_seq_scan keeps for its gradients */
 #define SF_MAX_TOP      32         /* alternatives that sf_label_logprobs gives */
 #define SF_EXPERT_MAX_D 16777216u  /* widest row that the expert calls move */
 

@@ -25,7 +25,7 @@ SF_F32, SF_BF16, SF_F16, SF_MX4 = 0, 1, 2, 3
 SF_GATE_SOFTMAX, SF_GATE_SOFTMAX_PICKED, SF_GATE_SHARE = 0, 1, 2
 SF_MAX_EXPERTS = 1024
 SF_ACT_NONE, SF_ACT_SILU = 0, 1
-SF_SEQ_MAX_ROWS, SF_SCAN_MAX_STATES, SF_MAX_TOP = 2 ** 31 - 2 ** 16, 64, 32
+SF_SEQ_MAX_ROWS, SF_SCAN_MAX_STATES, SF_SCAN_EVERY, SF_MAX_TOP = 2 ** 31 - 2 ** 16, 64, 8, 32
 SF_TAU_MARGIN_DEFAULT = float.fromhex("0x1.b1d106p-1")
 
 
@@ -777,11 +777,9 @@ def _scan_rows(ctx, seq, u, delta, A, B, C_, D_skip, delta_bias, z, softplus, s)
     return on, r, n, D, N, GN // N
 
 
-_EVERY = 8                        # rows between two states that the scan keeps for its backward pass
-
-
-def _room(t, floats, on, w):
-    return _flat(t, floats, 4, on, w, True)
+def _starts(t, n, n_seq, D, N, on, w):
+    """Address of the states that the scan keeps for its backward pass: as many floats as sf_seq_scan_starts says (worked out here: no call into the library more)."""
+    return _flat(t, (n // SF_SCAN_EVERY + n_seq) * D * N, 4, on, w, True)
 
 
 def sf_seq_scan(ctx, seq, u, delta, A, B, C, y_out, D=None, delta_bias=None, z=None, softplus=False, state_in=None, state_out=None, starts_out=None,
@@ -793,7 +791,7 @@ def sf_seq_scan(ctx, seq, u, delta, A, B, C, y_out, D=None, delta_bias=None, z=N
     q, ldy = _of(y_out, u.dtype, u.shape, on, s)
     m, si, so = _pools(s, on, A.dtype, (d, N), state_in, state_out)
     wp, wb = _bytes(workspace, on, s)
-    _check(_lib().sf_seq_scan(ctx, seq, r, n, si, so, m, None if starts_out is None else _room(starts_out, (n // _EVERY + seq.n_seq) * d * N, on, s), q, ldy,
+    _check(_lib().sf_seq_scan(ctx, seq, r, n, si, so, m, _starts(starts_out, n, seq.n_seq, d, N, on, s), q, ldy,
                               wp, wb, _stream_on(on, stream)), s)
 
 
@@ -813,7 +811,7 @@ def sf_seq_scan_backward(ctx, seq, u, delta, A, B, C, dy, starts, workspace, D=N
     o = sf_scan_grads(pu, pd, pb, pc, pz, lu, ld, lb, lc, lz, _reals(dA_out, (d, N), on, s), _reals(dD_out, (d,), on, s), _reals(d_delta_bias_out, (d,), on, s))
     m, ds, do = _pools(s, on, A.dtype, (d, N), d_state, d_state_in_out)
     wp, wb = _bytes(workspace, on, s)
-    _check(_lib().sf_seq_scan_backward(ctx, seq, r, n, g, ldg, _room(starts, (n // _EVERY + seq.n_seq) * d * N, on, s), ds, do, m, o, wp, wb,
+    _check(_lib().sf_seq_scan_backward(ctx, seq, r, n, g, ldg, _starts(starts, n, seq.n_seq, d, N, on, s), ds, do, m, o, wp, wb,
                                        _stream_on(on, stream)), s)
 
 

@@ -23,7 +23,7 @@ namespace sfscan {
 using namespace sfseq;
 
 constexpr int kWarps = 4;                  // warps of a block
-constexpr uint32_t kEvery = 8;             // rows between two states that are kept for the backward pass
+constexpr uint32_t kEvery = SF_SCAN_EVERY; // rows between two states that are kept for the backward pass
 constexpr uint32_t kMaxStates = SF_SCAN_MAX_STATES;
 
 struct Scan {

@@ -1,4 +1,8 @@
-"""Pools of states that a call reads and writes, without a device: one pool is taken, pools that overlap in part are refused."""
+"""Memory that the calls on sequences are given, without a device: one pool read and written is taken, pools that overlap in part are refused; the binding's sizes are the header's and
+the library's."""
+import os
+import re
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -42,3 +46,39 @@ def test_pools_that_overlap_in_part_are_refused(lib):
     back = dict(ctx=P, seq=seq(2), rows_in=rows, rows=6, dy=P, lddy=8, starts=P, ds=P, di=P, n_slots=2, out=grads, work=P, bytes=need, stream=0)
     for kw in (dict(di=P + 128), dict(ds=P + 128)):
         assert lib.sf_seq_scan_backward(*{**back, **kw}.values()) == sf.SF_ERR_ARG, kw
+
+
+def test_the_bindings_constants_are_the_headers(lib):
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "serveflow.h")).read()
+    defined = dict(re.findall(r"#define\s+(SF_\w+)\s+(-?\d+)u?\s", text))
+    for name in ("SF_ACT_NONE", "SF_ACT_SILU", "SF_SEQ_MAX_ROWS", "SF_SCAN_MAX_STATES", "SF_SCAN_EVERY", "SF_MAX_TOP"):
+        assert int(defined[name]) == getattr(sf, name), name
+
+
+class Tensor:
+    """As much of a device tensor as the check of the kept states looks at."""
+    dtype = torch.float32
+
+    def __init__(self, n):
+        self.n = n
+
+    def get_device(self):
+        return 0
+
+    def numel(self):
+        return self.n
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return P
+
+
+@pytest.mark.parametrize("n_seq,rows,D,N", [(1, 0, 3, 1), (2, 7, 8, 4), (5, 8, 1, 16), (3, 100, 8, 64), (9, 12345, 77, 5)])
+def test_room_for_kept_states_is_what_the_library_asks_for(lib, n_seq, rows, D, N):
+    need = sf.sf_seq_scan_starts(n_seq, rows, D, N)
+    sf._types()
+    assert sf._starts(Tensor(need), rows, n_seq, D, N, 0, "scan") == P
+    with pytest.raises(sf.SfError):
+        sf._starts(Tensor(need - 1), rows, n_seq, D, N, 0, "scan")
