@@ -499,15 +499,25 @@ template <typename T, int TH> __device__ __forceinline__ void far_row(const Back
     }
 }
 
-// Such rows of back_kernel<SAME>, which leaves them.  (2048 x 32768 bf16 with the forward call: 99 us; 97 without a look at the rows, 110 with a loop for them at that
-// kernel's end and 101 with blocks of their own in it: its registers suffice for neither.)
-template <typename T> __global__ void __launch_bounds__(kThreads) far_rows_kernel(const Back<T> a) {
-    sf_chain_enter();
+// Those among a thread's row and the block's other threads', one after the other, by the block
+template <typename T> __device__ __forceinline__ void far_rows(const Back<T>& a, bool far, uint64_t row) {
     __shared__ float sh[kThreads / 32];
     __shared__ uint32_t rows[kThreads], n_rows;
+    if (!__syncthreads_or(far)) return;
+    if (threadIdx.x == 0) n_rows = 0;
+    __syncthreads();
+    if (far) rows[atomicAdd(&n_rows, 1u)] = (uint32_t)row;
+    __syncthreads();
+    for (uint32_t i = 0; i < n_rows; i++) far_row<T, kThreads>(a, rows[i], sh);
+    __syncthreads();
+}
+
+// The rows that back_kernel leaves: a row a thread to look at.
+template <typename T> __global__ void __launch_bounds__(kThreads) far_rows_kernel(const Back<T> a) {
+    sf_chain_enter();
     uint32_t n = a.n;
     if (a.n_dev) n = sf_clamp_rows(*a.n_dev, a.n, a.st);
-    for (uint64_t first = blockIdx.x; first < n; first += (uint64_t)gridDim.x * kThreads) {      // a row a thread to look at, then one after the other
+    for (uint64_t first = blockIdx.x; first < n; first += (uint64_t)gridDim.x * kThreads) {
         const uint64_t row = first + (uint64_t)threadIdx.x * gridDim.x;
         bool far = false;
         if (row < n && fabsf(a.lse[row]) >= kFar) {
@@ -516,20 +526,16 @@ template <typename T> __global__ void __launch_bounds__(kThreads) far_rows_kerne
             r.ready(a);
             far = r.far();
         }
-        if (!__syncthreads_or(far)) continue;
-        if (threadIdx.x == 0) n_rows = 0;
-        __syncthreads();
-        if (far) rows[atomicAdd(&n_rows, 1u)] = (uint32_t)row;
-        __syncthreads();
-        for (uint32_t i = 0; i < n_rows; i++) far_row<T, kThreads>(a, rows[i], sh);
-        __syncthreads();
+        far_rows(a, far, row);
     }
 }
 
 // A thread takes C chunks, everything they need on its way before the first is worked on.  SAME: of one row, `groups` apart (long rows);
 // else the next ones are a whole grid's width further on.  Chunks begin on 16-byte boundaries of the logits' row; where the gradient's row lies on
-// the same ones they are stored whole too.  Rows far from zero are left out: of short rows the warp in which one begins does it.
-template <typename T, int C, bool SAME>
+// the same ones they are stored whole too.  Rows far from zero are left to the end, where the warp or (SAME) the block in which one begins does it, or (FAR false) to
+// far_rows_kernel: that is a launch more (3 x 20088 with the forward call: 17.5 us without, 19.7 with it), but of many long rows the registers do not suffice for what such a row
+// takes (2048 x 32768 bf16: 99 us, 110 with it in here).
+template <typename T, int C, bool SAME, bool FAR>
 __global__ void __launch_bounds__(kThreads) back_kernel(const Back<T> a) {
     sf_chain_enter();
     uint32_t n = a.n;
@@ -571,7 +577,9 @@ __global__ void __launch_bounds__(kThreads) back_kernel(const Back<T> a) {
             for (int e = 0; e < 8; e++) if ((uint32_t)(i0[u] + e) < a.V) dz[i0[u] + e] = from_f32<T>(d[e]);
         }
     }
-    if constexpr (!SAME) {                                 // a row that lies far from zero: the warp in which it begins (its first chunk begins at entry 0 or in front of it)
+    // (a row's first chunk begins at entry 0 or in front of it)
+    if constexpr (FAR && SAME) far_rows(a, far[0] && i0[0] <= 0, row[0]);
+    if constexpr (FAR && !SAME) {
 #pragma unroll
         for (int u = 0; u < C; u++)
             for (uint32_t begin = __ballot_sync(0xFFFFFFFFu, far[u] && i0[u] <= 0); begin; begin &= begin - 1)
@@ -661,9 +669,10 @@ extern "C" int sf_label_logprobs_backward(sf_ctx* ctx, const void* logits, int d
         const uint64_t blocks = (threads + kThreads - 1) / kThreads;
         if (blocks > 0x7FFFFFFFu) return (int)SF_ERR_ARG;
         a.few = blocks * kThreads * S <= 0xFFFFFFFFu;
-        auto kern = lng ? back_kernel<T, C, true> : (two ? back_kernel<T, S, false> : back_kernel<T, 1, false>);
+        const bool here = !lng || blocks <= (uint64_t)ctx->num_sms * 4;       // far rows too: all blocks are on the machine at once
+        auto kern = lng ? (here ? back_kernel<T, C, true, true> : back_kernel<T, C, true, false>) : (two ? back_kernel<T, S, false, true> : back_kernel<T, 1, false, true>);
         SF_CUDA(sf_launch_chained(kern, (uint32_t)blocks, kThreads, 0, (cudaStream_t)stream, a));
-        if (lng) SF_CUDA(sf_launch_chained(far_rows_kernel<T>, std::min(n, 2u * (uint32_t)ctx->num_sms), kThreads, 0, (cudaStream_t)stream, a));
+        if (!here) SF_CUDA(sf_launch_chained(far_rows_kernel<T>, std::min(n, 2u * (uint32_t)ctx->num_sms), kThreads, 0, (cudaStream_t)stream, a));
         return (int)SF_OK;
     });
 }

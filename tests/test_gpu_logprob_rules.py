@@ -92,3 +92,33 @@ def test_gradient_of_rows_far_from_zero(env, n, V, k, kind, scale, pitch):  # no
                                   top_ids=o["top_ids"] if k else None, d_top_logprobs=dev(g[2]) if k else None, scale=scale)
     assert torch.equal(d, again)
     sf.sf_ctx_poll(ctx)
+
+
+@pytest.mark.parametrize("V,kind", [(11000, "bf16"), (700, "fp32")])      # (rows on 16-byte boundaries: sums in the same order wherever a row lies)
+def test_gradient_of_rows_far_from_zero_among_many(env, V, kind):  # noqa: F811
+    """More rows than the machine takes at once: each as it comes out among a few, where the rows above are compared with the formula."""
+    sf, ctx = env
+    few, times = 10, 5_000_000 // V // 10
+    g = torch.Generator(device="cuda")
+    g.manual_seed(V)
+    x = torch.randn(few, V, device="cuda", generator=g) * 2
+    x[::5] = float(torch.finfo(TYPES[kind]).min)
+    x[1::5] += 20000
+    x[3::5, ::3] = -float("inf")
+    x = x.to(TYPES[kind])
+    labels = torch.arange(few, device="cuda", dtype=torch.int32) * 7
+    labels[4] = -1
+    dl, de = torch.randn(few, device="cuda", generator=g), torch.randn(few, device="cuda", generator=g)
+
+    def grad(times):
+        many = lambda t: t.repeat(times, *[1] * (t.dim() - 1))  # noqa: E731
+        z, y = many(x), many(labels)
+        o = run(sf, ctx, z, y, 1, 1.0)
+        d = torch.full_like(z, MARK)
+        sf.sf_label_logprobs_backward(ctx, z, y, o["lse"], d, d_logprob=many(dl), entropy=o["entropy"], d_entropy=many(de))
+        return o, d
+    o, want = grad(1)
+    p, got = grad(times)
+    assert bool(torch.isfinite(want).all()) and torch.equal(got, want.repeat(times, 1))
+    for k in o:
+        assert torch.equal(p[k], o[k].repeat(times, *[1] * (o[k].dim() - 1))), k
