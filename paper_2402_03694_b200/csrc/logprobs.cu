@@ -640,9 +640,16 @@ extern "C" int sf_label_logprobs(sf_ctx* ctx, const void* logits, int dtype, con
         if (room <= 1024) return launch_rows<T, 32, 4>(a, st);
         // (20,000 rows of 2,000 fp32, k = 2: 66 us by warps, 106 by blocks; twice as long rows no longer fit a warp's registers: 246 and 98)
         if (room <= 2048) return launch_rows<T, 32, 8>(a, st);
-        // a cluster of eight blocks a row where the rows alone do not fill the machine and are long enough for eight blocks
-        if (n < (uint32_t)ctx->num_sms && V >= 16384) return V >= 131072 ? launch_long<T, 512, 8>(a, st) : launch_long<T, 256, 8>(a, st);
-        return V <= 8192 ? launch_long<T, 128, 1>(a, st) : (V <= 65536 ? launch_long<T, 256, 1>(a, st) : launch_long<T, 512, 1>(a, st));
+        // Longer rows, as measured (16 bits; us):
+        //   a cluster of eight blocks a row where all rows' clusters fit the machine at once: 8 x 49152 5.9, by one block 7.0; 12 x 131072 8.7 and 12.6; but 18 x 32768 6.5 and 5.9,
+        //   74 x 65536 12.3 and 8.2.  Of 512 threads for the longest: 12 x 250001 9.8, of 256 10.7; but 12 x 65536 9.1 and 7.8
+        //   the widest block where every row has an SM to itself: 148 x 65536 8.9 by 512 threads, 10.6 by 256; 148 x 131072 13.6 and 17.2; but 222 x 65536 16.1 and 15.5, 2048 x 131072 161 and 100
+        //   256 threads or 128: 296 x 16384 6.0 and 6.9, 148 x 32768 6.2 and 8.0, 1184 x 65536 34.5 and 36.5; but 148 x 12288 5.4 and 4.9, 1184 x 16384 15.4 and 13.2, 4096 x 32768 63 and 57
+        const uint32_t sms = (uint32_t)ctx->num_sms;
+        if (V > 32768 && (uint64_t)n * 9 <= sms) return V >= 196608 ? launch_long<T, 512, 8>(a, st) : launch_long<T, 256, 8>(a, st);
+        if (V > 32768 && n <= sms) return launch_long<T, 512, 1>(a, st);
+        if (V > 32768 || (V > 12288 && n <= 2 * sms)) return launch_long<T, 256, 1>(a, st);
+        return launch_long<T, 128, 1>(a, st);
     });
 }
 

@@ -94,6 +94,33 @@ def test_gradient_of_rows_far_from_zero(env, n, V, k, kind, scale, pitch):  # no
     sf.sf_ctx_poll(ctx)
 
 
+@pytest.mark.parametrize("n,V", [(n, V) for n in (1, 16, 17, 148, 149, 296, 297) for V in (12288, 12289, 32768, 32769)] + [(n, V) for n in (2, 16, 17) for V in (196607, 196608)])
+def test_scores_on_both_sides_of_every_choice_of_threads(env, n, V):  # noqa: F811
+    """Threads a row are chosen by n and V: labels, entropies and alternatives of rows that are alike but for their order have to come out alike, and right."""
+    sf, ctx = env
+    k = 5
+    g = torch.Generator(device="cuda")
+    g.manual_seed(V + n)
+    row = (torch.randn(V, device="cuda", generator=g) * 2).bfloat16()
+    shift = torch.arange(n, device="cuda") * 37 % V
+    x = torch.stack([row.roll(int(s)) for s in shift])
+    labels = ((shift + 3) % V).int()                       # entry 3 of the row wherever it lies now
+    o = run(sf, ctx, x, labels, k, 1.0)
+    z = num(row)
+    lse = z.max() + np.log(np.exp(z - z.max()).sum())
+    p = np.exp(z - lse)
+    c = (V / 8 + 64 + 2 * (z.max() - z.min())) * E
+    assert (np.abs(num(o["lse"]) - lse) <= c + 4 * E * np.abs(lse)).all()
+    assert (np.abs(num(o["logprob"]) - (z[3] - lse)) <= c + 6 * E * np.abs(z[3] - lse)).all()
+    h = -(p * (z - lse)).sum()
+    assert (np.abs(num(o["entropy"]) - h) <= c * (1 + h)).all()
+    X = num(x)
+    order = np.argsort(-X, axis=1, kind="stable")[:, :k]   # ties to the lowest index
+    assert np.array_equal(num(o["top_ids"]), order)
+    top = np.take_along_axis(X, order, 1) - lse
+    assert (np.abs(num(o["top_logprobs"]) - top) <= c + 6 * E * np.abs(top)).all()
+
+
 @pytest.mark.parametrize("V,kind", [(11000, "bf16"), (700, "fp32")])      # (rows on 16-byte boundaries: sums in the same order wherever a row lies)
 def test_gradient_of_rows_far_from_zero_among_many(env, V, kind):  # noqa: F811
     """More rows than the machine takes at once: each as it comes out among a few, where the rows above are compared with the formula."""
