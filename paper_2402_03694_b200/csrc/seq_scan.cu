@@ -442,8 +442,9 @@ extern "C" int sf_seq_scan(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_r
                 const bool v4 = in->N % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16) && aligned(in->A, 16);
                 return launch(v4 ? step_kernel<T, SL, true> : step_kernel<T, SL, false>, (uint32_t)blocks, 32 * kWarps, 0, st, a);
             }
-            // Where whole sequences leave half of the machine idle and are too many to go in parts: two channels a lane, twice the warps
-            // (64 sequences of 512 rows x 512: 145 us with four channels a lane, 135 with two; 4096 of up to 128 x 256, where warps are many: 414 with four)
+            // Where whole sequences leave much of the machine idle and are too many to go in parts: two channels a lane, twice the warps (us, with two and with four channels a lane:
+            // 128 sequences of 64 rows x 256 bf16, 1024 warps with four, 20.9 and 27.9; 96 of 1024 x 512 415 and 477; but 512 of 64 x 256, 4096 warps, 66.6 and 59.2; 64 of 256 x 1024
+            // fp32, 2048 warps, 141 and 130)
             const bool two = SL == 4 && vec && !p.split && (uint64_t)seq->n_seq * in->G * p.cwarps < (uint64_t)SF_NUM_SMS_DEFAULT * 10;
             return by_width<T, SL>(vec, states_fit(in), [&](auto v, auto pb) {
                 constexpr int VV = decltype(v)::value, PB = decltype(pb)::value;

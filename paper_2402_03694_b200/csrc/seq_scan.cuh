@@ -227,8 +227,7 @@ inline int state_lanes(uint32_t N) { int sl = 1; while ((uint32_t)(4 * sl) < N) 
 struct Plan { uint32_t sl, cwarps, cblocks, part_len, parts, runs; bool split; };
 
 // Where warps or channels are few a warp takes fewer channels (more state lanes than states need: lanes stay idle, but a tile is staged and walked by more warps),
-// and where they would still leave most of the machine idle, sequences go in parts: two passes over the inputs then, so only where parts make three times
-// as many warps.
+// and where they would still leave most of the machine idle, sequences go in parts.
 inline Plan plan_of(uint32_t n_seq, uint32_t max_len, uint32_t D, uint32_t N, uint32_t G, bool backward) {
     Plan p;
     p.sl = state_lanes(N);
@@ -239,7 +238,11 @@ inline Plan plan_of(uint32_t n_seq, uint32_t max_len, uint32_t D, uint32_t N, ui
     const uint64_t want = full / warps();
     p.cblocks = (p.cwarps + kWarps - 1) / kWarps;
     p.part_len = (max_len + kEvery - 1) / kEvery * kEvery;
-    if (n_seq && want >= 3 && max_len > 2 * 32) p.part_len = (uint32_t)std::max<uint64_t>(32, ((max_len + want - 1) / want + kEvery - 1) / kEvery * kEvery);
+    // Parts are two passes over the inputs and a kernel between them.  Forward they pay from six times as many warps on, and of short sequences from more (256 channels bf16, us, in parts
+    // and not: 32 x 256 rows 39 and 41, 48 x 256 53 and 45; 48 x 1024 160 and 170, 64 x 1024 228 and 213; 4 x 96 22 and 29, 32 x 96 38 and 30); backward, where a warp waits for itself,
+    // from twice as many (64 x 256 146 and 206, 64 x 1024 543 and 807).
+    const bool parts = backward ? want >= 2 : want >= 6 && want * max_len >= 1700;
+    if (n_seq && parts && max_len > 2 * 32) p.part_len = (uint32_t)std::max<uint64_t>(32, ((max_len + want - 1) / want + kEvery - 1) / kEvery * kEvery);
     p.parts = (max_len + p.part_len - 1) / p.part_len;
     p.split = p.parts > 1;
     const uint64_t blocks = (uint64_t)G * p.cblocks, items = std::max<uint64_t>(1, (uint64_t)n_seq * p.parts);
