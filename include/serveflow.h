@@ -460,7 +460,8 @@ typedef struct {
 } sf_scan_rows;
 /* state_in, state_out: fp32[n_slots][D][N], nullable (zeros; dropped).  starts_out (nullable): what the backward pass needs,
  * sf_seq_scan_starts floats.  workspace: sf_seq_scan_workspace bytes (0 where every sequence is scanned in one go; few long ones are
- * cut into parts that run side by side).  Sequences of one row (max_len 1) are the step of a stream: the state is read and written once. */
+ * cut into parts that run side by side).  Sequences of one row (max_len 1) are the step of a stream: the state is read and written once.
+ * What a state, step or input that is no finite number leads to in its channel is infinite or NaN; which of the two is not defined. */
 int  sf_seq_scan_workspace(uint32_t n_seq, uint32_t max_len, uint32_t rows, uint32_t D, uint32_t N, uint32_t G, int backward, size_t* bytes_out);
 int  sf_seq_scan_starts(uint32_t n_seq, uint32_t rows, uint32_t D, uint32_t N, size_t* floats_out);
 int  sf_seq_scan(sf_ctx* ctx, const sf_sequences* seq, const sf_scan_rows* in, uint32_t rows, const float* state_in, float* state_out,

@@ -2,8 +2,9 @@
 // With x = scale * z, m = max x, s = sum e^(x - m), w = sum e^(x - m) (x - m) over a row (one pass, running maximum):
 //   lse = m + ln s,  log p_i = x_i - lse,  H = -sum p ln p = ln s - w / s      (both terms of H are positive: nothing cancels)
 //   d z_i = scale * ( sum_j g_j ([i = t_j] - p_i) - g_H p_i (ln p_i + H) ),    g_j the gradient of a log probability, t_j what it belongs to.
-// Sums and statistics are fp32.  The bytes are the logits once, and for the gradient once in and once out; what bounds is the issue of the dozen instructions an entry
-// takes: 2048 x 32,768 bf16, k = 8: 42 us forward (20 of bytes), 53 us gradient (41); 1,000,000 x 16 fp32, k = 2: 28 (15) and 25 us (20).
+// Sums and statistics are fp32.  The bytes are the logits once, and for the gradient once in and once out; what bounds is the issue of instructions: a
+// dozen an entry of a long row (2048 x 32,768 bf16, k = 8: 39 us forward, 20 of bytes; gradient 57, 41 of bytes), 44 an entry and thread in rows of 16, most of them lane exchanges in search of
+// the alternatives (1,000,000 x 16 fp32, k = 2: 28 us, 15 of bytes; gradient 24, 20 of bytes).
 #include <algorithm>
 #include <cfloat>
 #include <cooperative_groups.h>

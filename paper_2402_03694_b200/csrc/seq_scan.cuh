@@ -11,8 +11,8 @@
 // (SL a power of two with 4 SL >= N), so a thread holds 4 x 4 states, the sums over states and over channels are both half done in registers, and what a lane
 // reads of a row (steps, inputs, B, C) serves 16 states.  Rows go by tiles that the warp stages in shared memory of its own (softplus once an element) while the
 // next tile's pieces are copied ahead.  In the forward pass nothing waits for another warp; the backward pass joins dB and dC over a block.
-// Bound: an exponential a state, 16 a clock and SM, at N = 16 three times the time of the bytes.  4096 flows of up to 128 x 256 bf16 take 414 us (function unit 301),
-// 64 x 512 x 512 with gradients 580 us: 144 forward, 441 backward (325 instructions a row and warp, eight warps an SM).  A thread per channel would read B and C 16 states at
+// Bound: an exponential a state, 16 a clock and SM, at N = 16 three times the time of the bytes.  4096 flows of up to 128 x 256 bf16 take 411 us (function unit 301),
+// 64 x 512 x 512 with gradients 584 us, three quarters of them backward (325 instructions a row and warp, eight warps an SM).  A thread per channel would read B and C 16 states at
 // a time for one channel and need 31 exchanges a row for dB and dC; 8 x 2 or 2 x 8 states a thread read as much and exchange more.
 #pragma once
 #include <algorithm>
